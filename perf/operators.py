@@ -189,12 +189,12 @@ def prepare(case, seed):
         s["out"] = empty(T, d)
     elif op == "linear":
         m = -(-c["K"] // 64) * 64
-        s["ctx"] = _context(64, m, 1000, code, T, L.STEM_RESERVE_Q8)
-        s["pW"] = L.stem_q8_pack(s["ctx"], s["W"])
+        s["ctx"] = _context(64, m, 1000, code, T, L.STEM_RESERVE_QUANT)
+        s["pW"] = L.stem_quant_weights(s["ctx"], s["W"])
         s["out"] = empty(T, c["N"])
     else:
-        s["ctx"] = _context(c["d"], c["F"], c["V"], code, T, L.STEM_RESERVE_Q8)
-        s["pWg"], s["pWd"] = L.stem_q8_pack(s["ctx"], s["Wg"]), L.stem_q8_pack(s["ctx"], s["Wd"])
+        s["ctx"] = _context(c["d"], c["F"], c["V"], code, T, L.STEM_RESERVE_QUANT)
+        s["pWg"], s["pWd"] = L.stem_quant_weights(s["ctx"], s["Wg"]), L.stem_quant_weights(s["ctx"], s["Wd"])
         s["norm"] = L.stem_norm(L.STEM_NORM_RMS, EPS, s["w"])
         s["out"] = empty(T, c["d"])
     return s
@@ -320,9 +320,9 @@ def _own(s):
     if op == "dropout":
         L.stem_dropout(s["ctx"], s["x"], s["out"], c["p"], s["seed"], s["offset"])
     elif op == "linear":
-        L.stem_q8_linear(s["ctx"], s["x"], s["pW"], s["out"], residual=s["res"])
+        L.stem_quant_linear(s["ctx"], s["x"], s["pW"], s["out"], residual=s["res"])
     else:
-        L.stem_q8_ffn_forward(s["ctx"], s["x"], s["ids"], s["pWg"], s["pWd"], s["E"], s["out"], residual=s["x"], norm=s["norm"])
+        L.stem_quant_ffn_forward(s["ctx"], s["x"], s["ids"], s["pWg"], s["pWd"], s["E"], s["out"], residual=s["x"], norm=s["norm"])
     return s["out"]
 
 
