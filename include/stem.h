@@ -85,10 +85,13 @@ stem_status stem_create(stem_ctx** out, const stem_layer_desc* desc, int64_t max
  * enqueues nothing).  what: a sum of
  *   STEM_RESERVE_UP    one more [max_tokens, d_ff] activation and one more [d_ff, d_model] weight buffer,
  *                      for stem_ffn_up_forward / stem_ffn_up_backward (bf16 contexts);
- *   STEM_RESERVE_EDIT  index lists and 64 replacement rows for stem_edit_rows.
+ *   STEM_RESERVE_EDIT  index lists and 64 replacement rows for stem_edit_rows;
+ *   STEM_RESERVE_QUANT 8-bit copies of [max_tokens, max(d_model, d_ff)] and of 4096 tokens' hidden values, these in fp32 too, for
+ *                      stem_quant_linear / stem_quant_ffn_forward (bf16 contexts).
  * Those entry points return STEM_ERR_WORKSPACE until their scratch has been reserved. */
 #define STEM_RESERVE_UP 1u
 #define STEM_RESERVE_EDIT 2u
+#define STEM_RESERVE_QUANT 4u
 stem_status stem_reserve(stem_ctx* ctx, uint32_t what);
 /* Synchronises the device and frees the context's scratch.  NULL is allowed. */
 void stem_destroy(stem_ctx* ctx);
@@ -230,6 +233,96 @@ stem_status stem_ffn_up_backward(stem_ctx* ctx, const void* dy, const void* x, c
                                  int64_t E_rows, const void* saved_G, const void* saved_Up,
                                  const void* saved_H, int64_t T, void* dx, float* dW_gate, float* dW_up,
                                  float* dW_down, void* dV, int accumulate, void* stream);
+
+/* ---- the block around the layer: norms, gate, dropout, residual -------------------- */
+
+/* A norm of rows of d values.  STEM_NORM_RMS: v / sqrt(mean v^2 + eps);  STEM_NORM_LAYER: (v - mean) / sqrt(var + eps), var the mean of the
+ * squared differences;  STEM_NORM_NONE: v.  weight (device, [d], context dtype) multiplies the result channel by channel; NULL: nothing
+ * does.  eps >= 0.  No bias, as nowhere in the layer. */
+typedef enum { STEM_NORM_NONE = 0, STEM_NORM_RMS = 1, STEM_NORM_LAYER = 2 } stem_norm_kind;
+typedef struct {
+  int32_t kind;
+  float eps;
+  const void* weight;
+} stem_norm;
+
+/* Dropout from a counter-based generator (Philox 4x32, ten rounds), whose mask is never stored: forward and backward make it again.
+ * Element c of row r has 16 bits of the generator's output for the counter (c / 8, r, low and high word of o) and the key (low and high word
+ * of seed), o = offset + *step: bits 16 (c % 2) .. of word (c % 8) / 2.  It is dropped, that is 0 whatever it was, where they are below
+ * threshold = rint(65536 p), and is multiplied by 65536 / (65536 - threshold) otherwise.  p in [0, 1]; 0: nothing is dropped.
+ * step (device, may be NULL) is read when the kernel runs: a captured graph draws another mask on every replay when it counts on. */
+typedef struct {
+  float p;
+  uint64_t seed, offset;
+  const uint64_t* step;
+} stem_drop;
+
+/* The end of a block and the norm in front of the next, for residual stream x and block output f (both [T,d]):
+ *     u = N_out(f) * w_out;   y = residual_scale x + branch_scale g * D(u);   n = N_next(y) * w_next
+ * Any of N_out, g, D, N_next may be absent.  The gate g (device, context dtype): STEM_GATE_CHANNEL [d], a learned scale of each channel;
+ * STEM_GATE_TOKEN [T]; STEM_GATE_FULL [T,d]; STEM_GATE_NONE: 1.  host pointers: to this struct. */
+typedef enum { STEM_GATE_NONE = 0, STEM_GATE_CHANNEL = 1, STEM_GATE_TOKEN = 2, STEM_GATE_FULL = 3 } stem_gate_kind;
+typedef struct {
+  stem_norm out, next;
+  float residual_scale, branch_scale;
+  int32_t gate_kind;
+  const void* gate;
+  stem_drop drop;
+} stem_leave;
+
+/* For all of these: d is the context's d_model, up to 16384; sums and statistics in fp32, every output rounded once; in the calls of this
+ * section an output [T,d] may be one of the inputs [T,d] (the same address), and overlaps nothing otherwise. */
+
+/* n = N(x) * w: the norm in front of a block.  norm (host): not STEM_NORM_NONE. */
+stem_status stem_block_enter_forward(stem_ctx* ctx, const void* x, int64_t T, const stem_norm* norm, void* n, void* stream);
+
+/* Its backward pass: dx = dres + the gradient of x for the gradient dn of n; dw [d] fp32 = sum over tokens of dn N(x), overwritten or added
+ * to as `accumulate` says.  dres [T,d]: the gradient that reaches x along the residual stream, NULL: none.  dw may be NULL. */
+stem_status stem_block_enter_backward(stem_ctx* ctx, const void* dn, const void* x, int64_t T, const stem_norm* norm, const void* dres,
+                                      void* dx, float* dw, int accumulate, void* stream);
+
+/* y and n as above; n NULL exactly when L->next.kind is STEM_NORM_NONE.  n is made of y before it is rounded. */
+stem_status stem_block_leave_forward(stem_ctx* ctx, const void* f, const void* x, int64_t T, const stem_leave* L, void* y, void* n,
+                                     void* stream);
+
+/* Its backward pass, for the gradients dy of y and dn of n; y as the forward call left it.  Either gradient may be NULL: none.
+ *   G = dy + N_next'(dn * w_next);  dx = residual_scale G;  h = branch_scale G;  du = D'(h * g);  df = N_out'(du * w_out)
+ * Outputs, each may be NULL: dx, df [T,d]; dgate: h * D(u), summed over tokens for STEM_GATE_CHANNEL ([d] fp32), over channels for
+ * STEM_GATE_TOKEN ([T], context dtype), as it is for STEM_GATE_FULL ([T,d], context dtype); dw_out [d] fp32 = sum over tokens of
+ * du N_out(f); dw_next [d] fp32 = sum over tokens of dn N_next(y).  The fp32 sums are overwritten, or added to when accumulate != 0; they
+ * are taken in one order, so repeated calls give the same bits.  y is read only where dn is given, f only where a norm or a gate needs it:
+ * they may be NULL otherwise. */
+stem_status stem_block_leave_backward(stem_ctx* ctx, const void* dy, const void* dn, const void* f, const void* y, int64_t T,
+                                      const stem_leave* L, void* dx, void* df, void* dgate, float* dw_out, float* dw_next, int accumulate,
+                                      void* stream);
+
+/* y = D(x) for rows of any width (x, y [T,width], context dtype; y may be x).  The backward pass is the same call on the gradient: with
+ * the same seed, offset and *step the mask is the same, and the same as in the calls above. */
+stem_status stem_dropout(stem_ctx* ctx, const void* x, int64_t T, int64_t width, const stem_drop* drop, void* y, void* stream);
+
+/* ---- the layer in 8-bit integers, for serving (bf16 contexts) ------------------------ */
+
+/* Q(v) of a row: s = max |v| / 127 and the integers rint(v / s).  A product is s_t s_n (sum over k of q_tk q_nk), its sum exact: a scale for
+ * each token, taken from the row within the call, and one for each channel of the weights, which are quantised once.
+ * A row with a NaN or an infinity makes NaN of all that depends on it, and of nothing else. */
+
+/* Bytes of the 8-bit form of a weight matrix [N,K], which only these calls read (blocks of 32 rows by 32 k, padded). */
+int64_t stem_quant_bytes(int64_t N, int64_t K);
+/* W [N,K] (bf16) -> q (stem_quant_bytes(N, K) bytes) and scale [N] fp32.  N, K >= 1, K <= 131072; W is only read here. */
+stem_status stem_quant_weights(stem_ctx* ctx, const void* W, int64_t N, int64_t K, void* q, float* scale, void* stream);
+
+/* y = Q(N(x)) Q(W)^T (+ residual): x [T,K], y and residual [T,N] bf16, any N >= 1 and 1 <= K <= max(d_model, d_ff); q, scale: of
+ * stem_quant_weights.  norm (host) may be NULL: none.  residual may be NULL, and may be y.  y may be x where T N fits it.
+ * Needs stem_reserve(ctx, STEM_RESERVE_QUANT). */
+stem_status stem_quant_linear(stem_ctx* ctx, const void* x, int64_t T, int64_t K, const stem_norm* norm, const void* q, const float* scale,
+                              int64_t N, const void* residual, void* y, void* stream);
+
+/* The layer on Q of both weight matrices: y = Q(SiLU(Q(N(x)) Q(W_gate)^T) * E[ids]) Q(W_down)^T (+ residual); ids and the bf16 table as in
+ * stem_ffn_forward.  The hidden values stay in fp32 until they are quantised: rounded to bf16 first, one in a hundred would become
+ * another integer.  norm and residual may be NULL; y may be x and residual.  Needs stem_reserve(ctx, STEM_RESERVE_QUANT). */
+stem_status stem_quant_ffn_forward(stem_ctx* ctx, const void* x, const int32_t* ids, int64_t T, const stem_norm* norm, const void* gate_q,
+                                   const float* gate_scale, const void* down_q, const float* down_scale, const void* E, int64_t E_rows,
+                                   const void* residual, void* y, void* stream);
 
 /* ---- host-resident table (System Implementation: CPU offloading, asynchronous
  *      prefetch, token de-duplication) ------------------------------------------- */

@@ -11,7 +11,8 @@
 #include <thread>
 #include <vector>
 
-#include "stem_internal.h"
+#include "block.h"
+#include "quant.h"
 
 namespace {
 
@@ -22,7 +23,9 @@ const char* const kKernelNames[K_COUNT_] = {
     "gemm_dw_gate",    "silu_gather",      "sort_count",    "sort_scan",    "sort_scatter",
     "sort_fused",      "unique",          "seg_reduce",   "seg_combine",   "sparse_adamw", "row_copy",
     "splitk_reduce",   "gemm_up",      "gemm_dw_up",   "sort_merge",
-    "grads_f32", "gemm_dw", "list_copy", "ffn_decode"};
+    "grads_f32", "gemm_dw", "list_copy", "ffn_decode",
+    "block_enter", "block_enter_back", "block_leave", "block_leave_back", "dropout",
+    "quant_weights", "quant_rows", "quant_hidden", "quant_gate", "quant_down"};
 
 #define fail stem_fail
 
@@ -163,6 +166,8 @@ void release(stem_ctx* c) {
   free(c->slot);
   free(c->cache_id_in_slot); free(c->cache_slot_of); free(c->cache_freq);
   (void)hipFree(c->edit_idx_dev); (void)hipFree(c->edit_rep_dev);
+  (void)hipFree(c->block_part);
+  (void)hipFree(c->quant_x); (void)hipFree(c->quant_h); (void)hipFree(c->quant_sx); (void)hipFree(c->quant_sh); (void)hipFree(c->quant_hidden);
   if (c->inst_pinned) (void)hipHostFree(c->inst_pinned);
   (void)hipFree(c->inst_dev);
   if (c->side) copy_streams_put(c->device);
@@ -205,6 +210,8 @@ stem_status stem_fail(stem_ctx* c, stem_status st, const char* fmt, ...) {
   va_end(ap);
   return st;
 }
+
+stem_status stem_enter(stem_ctx* c, int64_t T) { return enter(c, T); }
 
 extern "C" {
 
@@ -329,6 +336,8 @@ stem_status stem_create(stem_ctx** out, const stem_layer_desc* desc, int64_t max
   ok(dmalloc(&c->sort_counts, (size_t)stem_sort_count_entries(std::max<int64_t>(max_tokens, 1))));
   ok(dmalloc(&c->seg_of, (size_t)max_tokens));
   ok(dmalloc(&c->seg_part, (size_t)stem_seg_chunks(std::max<int64_t>(max_tokens, 1)) * 2 * desc->d_ff));
+  if (desc->d_model <= STEM_BLOCK_MAX_WIDTH)
+    ok(dmalloc(&c->block_part, (size_t)std::min<int64_t>(max_tokens, STEM_BLOCK_GRID) * 3 * desc->d_model));
   ok(dmalloc(&c->uniq_dev, (size_t)max_tokens));
   ok(dmalloc(&c->order_dev, 2 * (size_t)max_tokens));
   ok(hipHostMalloc(reinterpret_cast<void**>(&c->order_pinned), std::max<size_t>(max_tokens, 1) * 8, hipHostMallocDefault));
@@ -361,7 +370,7 @@ void stem_destroy(stem_ctx* ctx) { release(ctx); }
 
 stem_status stem_reserve(stem_ctx* c, uint32_t what) {
   if (!c) return STEM_ERR_INVALID_ARG;
-  if (what & ~(uint32_t)(STEM_RESERVE_UP | STEM_RESERVE_EDIT))
+  if (what & ~(uint32_t)(STEM_RESERVE_UP | STEM_RESERVE_EDIT | STEM_RESERVE_QUANT))
     return fail(c, STEM_ERR_INVALID_ARG, "stem_reserve: unknown bits in 0x%x", what);
   HIP_TRY(c, hipSetDevice(c->device));
   if ((what & STEM_RESERVE_UP) && !c->Up_ws) {
@@ -371,6 +380,16 @@ stem_status stem_reserve(stem_ctx* c, uint32_t what) {
   if ((what & STEM_RESERVE_EDIT) && !c->edit_idx_dev) {
     HIP_TRY(c, hipMalloc(reinterpret_cast<void**>(&c->edit_idx_dev), 3 * STEM_EDIT_MAX_TOKENS * sizeof(int32_t)));
     HIP_TRY(c, hipMalloc(&c->edit_rep_dev, (size_t)STEM_EDIT_MAX_TOKENS * c->desc.d_ff * esize(c)));
+  }
+  if ((what & STEM_RESERVE_QUANT) && !c->quant_hidden) {
+    if (c->desc.dtype != STEM_BF16) return fail(c, STEM_ERR_UNSUPPORTED, "stem_reserve: STEM_RESERVE_QUANT needs a bf16 context");
+    const int64_t T = std::max<int64_t>(c->max_tokens, 1), chunk = std::min<int64_t>(T, STEM_QUANT_CHUNK), F = c->desc.d_ff;
+    // (the one that says that all are there comes last)
+    if (!c->quant_x) HIP_TRY(c, dmalloc(&c->quant_x, (size_t)stem_quant_size(T, std::max<int64_t>(c->desc.d_model, F))));
+    if (!c->quant_h) HIP_TRY(c, dmalloc(&c->quant_h, (size_t)stem_quant_size(chunk, F)));
+    if (!c->quant_sx) HIP_TRY(c, dmalloc(&c->quant_sx, (size_t)T));
+    if (!c->quant_sh) HIP_TRY(c, dmalloc(&c->quant_sh, (size_t)chunk));
+    HIP_TRY(c, dmalloc(&c->quant_hidden, (size_t)(chunk * F)));
   }
   return STEM_OK;
 }

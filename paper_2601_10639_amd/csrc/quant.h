@@ -1,0 +1,38 @@
+// 8-bit integer products: layout, arguments and launches (quant.hip), called by their entry points (api_block.hip).
+//
+// Layout.  A matrix [rows, K] is kept as blocks of 32 rows x 32 k, 1 KB each: chunk h of row r, 16 bytes of k = 16 h .. 16 h + 15, lies at
+// (32 h + r) * 16, so that a block is one operand of v_mfma_i32_32x32x32_i8 with lane l's 16 bytes at 16 l, and a load of it is 1 KB in a
+// row wherever it is made from.  The blocks of 32 rows follow each other along k; k is padded with zeros to a multiple of 128 and the
+// rows to one of 32.
+#pragma once
+#include "stem_internal.h"
+
+#define STEM_QUANT_CHUNK 4096   // tokens whose hidden values a layer call has in fp32 at a time
+
+inline int64_t stem_quant_pitch(int64_t K) { return (K + 127) / 128 * 128; }
+inline int64_t stem_quant_size(int64_t rows, int64_t K) { return (rows + 31) / 32 * 32 * stem_quant_pitch(K); }
+
+struct QuantRowsArgs {
+  const void* x;       // [rows, K], bf16 or fp32
+  int64_t rows;
+  int K;
+  int pad_rows;        // write zeros for the rows that fill the last block
+  stem_norm norm;      // of a row, before it is quantised (bf16 weight)
+  int8_t* q;
+  float* scale;        // [rows]
+};
+hipError_t stem_quant_rows_launch(stem_ctx* ctx, int kid, int is_bf16, const QuantRowsArgs& a, hipStream_t s);
+
+struct QuantGemmArgs {
+  const int8_t *A, *B;              // tokens [M, K] and weights [N, K], in the layout above
+  const float *scale_a, *scale_b;
+  int M, N, K;                      // K: padded
+  bf16_t* y;                        // [M, N], or null:
+  const bf16_t* residual;           // [M, N], may be null
+  float* h;                         // [M, N] = SiLU(product) * E[ids]
+  const int32_t* ids;
+  const bf16_t* E;
+  int E_rows;
+  int32_t* flag;
+};
+hipError_t stem_quant_gemm_launch(stem_ctx* ctx, int kid, const QuantGemmArgs& a, hipStream_t s);

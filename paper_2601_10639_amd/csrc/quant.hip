@@ -1,0 +1,227 @@
+// Products in 8-bit integers with a scale for each token and each channel, for serving.
+//
+//     s_t = max_k |x_tk| / 127,  q_tk = rint(x_tk / s_t);   y_tn = s_t s_n sum_k q_tk q_nk
+//
+// The sums are exact in 32 bits up to K = 133 000 (127^2 K < 2^31).  A row that holds a NaN or an infinity has no scale: its
+// integers are zero and its scale NaN, so that what is made of it is NaN and nothing else is.  A row of zeros, or of values so small that
+// their scale would be subnormal, has the scale 2^-126.
+#include "quant.h"
+
+typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8_t;
+typedef __attribute__((ext_vector_type(4))) __bf16 bf16x4_t;
+typedef __attribute__((ext_vector_type(4))) int i32x4_t;
+typedef __attribute__((ext_vector_type(16))) int i32x16_t;
+
+namespace {
+
+__device__ __forceinline__ float sigmoidf(float z) { return 1.0f / (1.0f + __expf(-z)); }
+
+// ---- rows to integers -------------------------------------------------------------------------------------
+// 16 elements of a row from p on, of which `left` are the row's; the others read as zero.  VEC: rows are multiples of 8 elements.
+template <bool VEC>
+__device__ __forceinline__ void load16(const bf16_t* p, int left, float (&v)[16]) {
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    if (VEC) {
+      bf16x8_t u = {};
+      if (left > 8 * h) u = *reinterpret_cast<const bf16x8_t*>(p + 8 * h);
+#pragma unroll
+      for (int q = 0; q < 8; ++q) v[8 * h + q] = (float)u[q];
+    } else {
+#pragma unroll
+      for (int q = 8 * h; q < 8 * h + 8; ++q) v[q] = q < left ? __uint_as_float((uint32_t)p[q] << 16) : 0.f;
+    }
+  }
+}
+template <bool VEC>
+__device__ __forceinline__ void load16(const float* p, int left, float (&v)[16]) {
+#pragma unroll
+  for (int h = 0; h < 4; ++h) {
+    if (VEC) {
+      const float4 u = left > 4 * h ? *reinterpret_cast<const float4*>(p + 4 * h) : make_float4(0.f, 0.f, 0.f, 0.f);
+      v[4 * h] = u.x; v[4 * h + 1] = u.y; v[4 * h + 2] = u.z; v[4 * h + 3] = u.w;
+    } else {
+#pragma unroll
+      for (int q = 4 * h; q < 4 * h + 4; ++q) v[q] = q < left ? p[q] : 0.f;
+    }
+  }
+}
+
+__device__ __forceinline__ float block_sum(float v, float* red) {
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) v += __shfl_xor(v, o);
+  __syncthreads();
+  if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
+  __syncthreads();
+  return (red[0] + red[1]) + (red[2] + red[3]);
+}
+__device__ __forceinline__ uint32_t block_max(uint32_t v, uint32_t* red) {
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) v = max(v, (uint32_t)__shfl_xor((int)v, o));
+  __syncthreads();
+  if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
+  __syncthreads();
+  return max(max(red[0], red[1]), max(red[2], red[3]));
+}
+
+// A workgroup has a row.  VPT: chunks of 16 elements a thread holds; 0: the row is longer than that and is read again for each step.
+template <class E, bool VEC, int VPT>
+__global__ __launch_bounds__(256) void quant_rows_kernel(QuantRowsArgs p) {
+  __shared__ float red[4];
+  __shared__ uint32_t redm[4];
+  const int64_t row = blockIdx.x;
+  const int chunks = (int)((p.K + 127) / 128 * 8);
+  int8_t* const out = p.q + (row >> 5) * 32 * (int64_t)chunks * 16 + (row & 31) * 16;
+  const E* const x = static_cast<const E*>(p.x) + row * p.K;
+  constexpr int HELD = VPT ? VPT : 1;
+  float v[HELD][16];
+  const bool live = row < p.rows;
+  const int steps = VPT ? VPT : (chunks + 255) / 256;
+  auto fetch = [&](int t, float (&u)[16]) {
+    const int c = t * 256 + threadIdx.x;
+    if (live && c * 16 < p.K) load16<VEC>(x + c * 16, p.K - c * 16, u);
+    else
+#pragma unroll
+      for (int q = 0; q < 16; ++q) u[q] = 0.f;
+  };
+  if (VPT) {
+#pragma unroll
+    for (int t = 0; t < HELD; ++t) fetch(t, v[t]);
+  }
+  // what the row's values are before they are quantised: a norm's mean and factor, and its weight
+  float mean = 0.f, r = 1.f;
+  if (p.norm.kind != STEM_NORM_NONE) {
+    if (p.norm.kind == STEM_NORM_LAYER) {
+      float s = 0.f;
+      for (int t = 0; t < steps; ++t) {
+        if (!VPT) fetch(t, v[0]);
+#pragma unroll
+        for (int q = 0; q < 16; ++q) s += v[VPT ? t : 0][q];
+      }
+      mean = block_sum(s, red) / (float)p.K;
+    }
+    float s = 0.f;
+    for (int t = 0; t < steps; ++t) {
+      if (!VPT) fetch(t, v[0]);
+      const int left = p.K - (t * 256 + (int)threadIdx.x) * 16;
+#pragma unroll
+      for (int q = 0; q < 16; ++q) {
+        const float c = q < left ? v[VPT ? t : 0][q] - mean : 0.f;
+        s += c * c;
+      }
+    }
+    r = 1.0f / sqrtf(block_sum(s, red) / (float)p.K + p.norm.eps);
+  }
+  auto finish = [&](int t, float (&u)[16]) {
+    if (p.norm.kind == STEM_NORM_NONE) return;
+    const int c = t * 256 + threadIdx.x, left = p.K - c * 16;
+    float w[16];
+    if (p.norm.weight && left > 0) load16<VEC>(static_cast<const bf16_t*>(p.norm.weight) + c * 16, left, w);
+#pragma unroll
+    for (int q = 0; q < 16; ++q) u[q] = q < left ? (u[q] - mean) * r * (p.norm.weight ? w[q] : 1.f) : 0.f;
+  };
+  uint32_t top = 0;
+  for (int t = 0; t < steps; ++t) {
+    if (!VPT) fetch(t, v[0]);
+    float (&u)[16] = v[VPT ? t : 0];
+    finish(t, u);
+#pragma unroll
+    for (int q = 0; q < 16; ++q) top = max(top, __float_as_uint(u[q]) & 0x7fffffffu);
+  }
+  top = block_max(top, redm);
+  const bool finite = top < 0x7f800000u;
+  const float s = fmaxf(__uint_as_float(top) / 127.0f, 0x1p-126f), inv = finite ? 1.0f / s : 0.f;
+  if (threadIdx.x == 0 && live) p.scale[row] = finite ? s : __uint_as_float(0x7fc00000u);
+  for (int t = 0; t < steps; ++t) {
+    const int c = t * 256 + threadIdx.x;
+    if (c >= chunks) break;
+    float (&u)[16] = v[VPT ? t : 0];
+    if (!VPT) {
+      fetch(t, u);
+      finish(t, u);
+    }
+    uint32_t w[4];
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      w[q] = 0;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        // |u / s| is at most 127 and a rounding
+        const int i = finite ? (int)fminf(fmaxf(rintf(u[4 * q + k] * inv), -127.f), 127.f) : 0;
+        w[q] |= (uint32_t)(i & 0xff) << (8 * k);
+      }
+    }
+    *reinterpret_cast<uint4*>(out + (int64_t)(c >> 1) * 1024 + (c & 1) * 512) = make_uint4(w[0], w[1], w[2], w[3]);
+  }
+}
+
+// ---- the product ----------------------------------------------------------------------------------------------
+// A wavefront has 32 tokens x 32 channels and reads its blocks from memory.  With the weights as the first operand a lane holds, for one
+// token, groups of four neighbouring channels.
+template <bool GATE>
+__global__ __launch_bounds__(256) void quant_gemm_kernel(QuantGemmArgs p) {
+  const int lane = threadIdx.x & 63;
+  const int mt = (p.M + 31) / 32, nt = (p.N + 31) / 32;
+  const int64_t tile = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+  if (tile >= (int64_t)mt * nt) return;
+  const int tm = (int)(tile % mt), tn = (int)(tile / mt);
+  const i32x4_t* a = reinterpret_cast<const i32x4_t*>(p.A + (int64_t)tm * 32 * p.K) + lane;
+  const i32x4_t* b = reinterpret_cast<const i32x4_t*>(p.B + (int64_t)tn * 32 * p.K) + lane;
+  i32x16_t acc = {};
+  for (int k = 0; k < p.K / 32; ++k) acc = __builtin_amdgcn_mfma_i32_32x32x32_i8(b[k * 64], a[k * 64], acc, 0, 0, 0);
+  const int m = tm * 32 + (lane & 31);
+  if (m >= p.M) return;
+  const float sa = p.scale_a[m];
+  int id = 0;
+  if (GATE) {
+    id = p.ids[m];
+    if ((unsigned)id >= (unsigned)p.E_rows) {
+      *p.flag = 1;
+      id = id < 0 ? 0 : p.E_rows - 1;
+    }
+  }
+#pragma unroll
+  for (int g = 0; g < 4; ++g) {
+    const int n = tn * 32 + 8 * g + 4 * (lane >> 5);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      if (n + e >= p.N) break;
+      const float z = (float)acc[4 * g + e] * (sa * p.scale_b[n + e]);
+      const size_t at = (size_t)m * p.N + n + e;
+      if (GATE) {
+        const float u = __uint_as_float((uint32_t)p.E[(size_t)id * p.N + n + e] << 16);
+        p.h[at] = z * sigmoidf(z) * u;
+      } else {
+        const float o = p.residual ? z + __uint_as_float((uint32_t)p.residual[at] << 16) : z;
+        reinterpret_cast<__bf16*>(p.y)[at] = (__bf16)o;
+      }
+    }
+  }
+}
+
+template <class E, bool VEC>
+hipError_t rows(const QuantRowsArgs& a, hipStream_t s) {
+  const unsigned grid = (unsigned)(a.pad_rows ? (a.rows + 31) / 32 * 32 : a.rows);
+  if (a.K <= 4096) quant_rows_kernel<E, VEC, 1><<<grid, 256, 0, s>>>(a);
+  else if (a.K <= 8192) quant_rows_kernel<E, VEC, 2><<<grid, 256, 0, s>>>(a);
+  else quant_rows_kernel<E, VEC, 0><<<grid, 256, 0, s>>>(a);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t stem_quant_rows_launch(stem_ctx* ctx, int kid, int is_bf16, const QuantRowsArgs& a, hipStream_t s) {
+  ProfScope prof(ctx, kid, s);
+  const bool vec = a.K % 8 == 0;
+  if (is_bf16) return vec ? rows<bf16_t, true>(a, s) : rows<bf16_t, false>(a, s);
+  return vec ? rows<float, true>(a, s) : rows<float, false>(a, s);
+}
+
+hipError_t stem_quant_gemm_launch(stem_ctx* ctx, int kid, const QuantGemmArgs& a, hipStream_t s) {
+  ProfScope prof(ctx, kid, s);
+  const int64_t tiles = (int64_t)((a.M + 31) / 32) * ((a.N + 31) / 32);
+  const unsigned grid = (unsigned)((tiles + 3) / 4);
+  if (a.y) quant_gemm_kernel<false><<<grid, 256, 0, s>>>(a);
+  else quant_gemm_kernel<true><<<grid, 256, 0, s>>>(a);
+  return hipGetLastError();
+}

@@ -34,6 +34,16 @@ enum StemKernelId {
   K_GEMM_DW,         // two or three weight gradients in one launch
   K_LIST_COPY,       // host-resident table: remap and the row copy's lists
   K_FFN_DECODE,      // a decode step's layer in one launch
+  K_BLOCK_ENTER,     // the norm in front of a block
+  K_BLOCK_ENTER_BACK,
+  K_BLOCK_LEAVE,     // norm, dropout, gate, residual, next norm
+  K_BLOCK_LEAVE_BACK,
+  K_DROPOUT,
+  K_QUANT_WEIGHTS,   // bf16 weights to 8-bit integers
+  K_QUANT_ROWS,      // (normed) activations to 8-bit integers
+  K_QUANT_HIDDEN,    // hidden values to 8-bit integers
+  K_QUANT_GATE,      // 8-bit gate product with SiLU*gather
+  K_QUANT_DOWN,      // 8-bit product
   K_COUNT_
 };
 
@@ -107,6 +117,14 @@ struct stem_ctx {
   // knowledge editing: device scratch for up to STEM_EDIT_MAX_TOKENS source / target tokens
   int32_t* edit_idx_dev;     // [3 * STEM_EDIT_MAX_TOKENS]: source rows, picked rows, target rows
   void* edit_rep_dev;        // [STEM_EDIT_MAX_TOKENS, F] replacement rows
+
+  // gradients of the block around the layer that are sums over tokens: partial sums, [3][workgroups][d_model]
+  float* block_part;
+
+  // 8-bit products (STEM_RESERVE_QUANT)
+  int8_t *quant_x, *quant_h;      // rows of a call; hidden values of STEM_QUANT_CHUNK tokens
+  float *quant_sx, *quant_sh;     // their scales
+  float* quant_hidden;            // those hidden values in fp32
 
   // profiling
   int prof_on;
@@ -362,6 +380,8 @@ hipError_t stem_table_grad(stem_ctx* prof, const EmbedScratch& ws, int is_bf16, 
                            hipStream_t s);
 int64_t stem_seg_chunks(int64_t max_tokens);
 int64_t stem_sort_count_entries(int64_t max_tokens);
+// what every call with a context begins with (T < 0, T > max_tokens, the device, the sticky id-range flag); STEM_OK to proceed
+stem_status stem_enter(stem_ctx* c, int64_t T);
 // error text for calls that have no context (stem_last_error(NULL) returns it)
 stem_status stem_fail(stem_ctx* c, stem_status st, const char* fmt, ...);
 

@@ -27,6 +27,8 @@ SYMBOLS = [
     "stem_create", "stem_reserve", "stem_set_prefetch_mode", "stem_destroy", "stem_last_error", "stem_status_string", "stem_sync_status",
     "stem_ffn_forward", "stem_ffn_forward_residual", "stem_ffn_backward", "stem_ffn_up_forward", "stem_ffn_up_backward",
     "stem_embed_grad", "stem_embed_grad_presorted", "stem_embed_grad_noalloc", "stem_embed_sparse_adamw",
+    "stem_block_enter_forward", "stem_block_enter_backward", "stem_block_leave_forward", "stem_block_leave_backward", "stem_dropout",
+    "stem_quant_bytes", "stem_quant_weights", "stem_quant_linear", "stem_quant_ffn_forward",
     "stem_prefetch_rows", "stem_cache_init", "stem_prefetch_rows_cached", "stem_cache_state",
     "stem_edit_rows", "stem_profile_enable", "stem_profile_kernels", "stem_profile_read",
     "stem_profile_reset", "stem_measure_peak",
@@ -41,6 +43,56 @@ class stem_layer_desc(ctypes.Structure):
 class stem_adamw_hparams(ctypes.Structure):
     _fields_ = [("lr", ctypes.c_float), ("beta1", ctypes.c_float), ("beta2", ctypes.c_float),
                 ("eps", ctypes.c_float), ("weight_decay", ctypes.c_float), ("step", ctypes.c_int64)]
+
+
+STEM_NORM_NONE, STEM_NORM_RMS, STEM_NORM_LAYER = range(3)
+STEM_GATE_NONE, STEM_GATE_CHANNEL, STEM_GATE_TOKEN, STEM_GATE_FULL = range(4)
+
+
+class stem_norm(ctypes.Structure):
+    """A norm and its weight, a device tensor [d] or None.  Made once and passed to every call."""
+
+    _fields_ = [("kind", ctypes.c_int32), ("eps", ctypes.c_float), ("weight", ctypes.c_void_p)]
+
+    def __init__(self, kind: int = STEM_NORM_NONE, eps: float = 1e-6, weight=None):
+        super().__init__(kind, eps, _ptr(weight, name="weight"))
+        self.tensor = weight   # kept alive
+
+    def _check(self, ctx, width: int, name: str):
+        if self.tensor is not None:
+            _shaped(self.tensor, ctx.torch_dtype, (width,), name + ".weight")
+
+
+class stem_drop(ctypes.Structure):
+    """step: a device int64 tensor of one element that is added to offset when the kernel runs, or None."""
+
+    _fields_ = [("p", ctypes.c_float), ("seed", ctypes.c_uint64), ("offset", ctypes.c_uint64), ("step", ctypes.c_void_p)]
+
+    def __init__(self, p: float = 0.0, seed: int = 0, offset: int = 0, step=None):
+        super().__init__(p, seed, offset, _ptr(step, torch.int64, name="step"))
+        self.step_tensor = step
+
+
+class stem_leave(ctypes.Structure):
+    """What the end of a block consists of (include/stem.h).  Made once and passed to every call; `drop` may be changed in between."""
+
+    _fields_ = [("out", stem_norm), ("next", stem_norm), ("residual_scale", ctypes.c_float), ("branch_scale", ctypes.c_float),
+                ("gate_kind", ctypes.c_int32), ("gate", ctypes.c_void_p), ("drop", stem_drop)]
+
+    def __init__(self, out=None, next=None, residual_scale: float = 1.0, branch_scale: float = 1.0, gate_kind: int = STEM_GATE_NONE, gate=None,
+                 p: float = 0.0, seed: int = 0, offset: int = 0, step=None):
+        self.norms = (out or stem_norm(), next or stem_norm())
+        super().__init__(*self.norms, residual_scale, branch_scale, gate_kind, _ptr(gate, name="gate"), stem_drop(p, seed, offset, step))
+        self.gate_tensor, self.step_tensor = gate, step
+
+    def _check(self, ctx, T: int):
+        d = ctx.d_model
+        self.norms[0]._check(ctx, d, "out")
+        self.norms[1]._check(ctx, d, "next")
+        if self.gate_tensor is not None:
+            shape = {STEM_GATE_CHANNEL: (d,), STEM_GATE_TOKEN: (T,), STEM_GATE_FULL: (T, d)}.get(self.gate_kind)
+            if shape:
+                _shaped(self.gate_tensor, ctx.torch_dtype, shape, "gate")
 
 
 class StemError(RuntimeError):
@@ -107,6 +159,25 @@ def lib() -> ctypes.CDLL:
         L.stem_cache_state.restype = i32
         L.stem_edit_rows.argtypes = [vp, vp, vp, i64, vp, i64, i32, i32, vp, vp]
         L.stem_edit_rows.restype = i32
+        norm, leave = ctypes.POINTER(stem_norm), ctypes.POINTER(stem_leave)
+        L.stem_block_enter_forward.argtypes = [vp, vp, i64, norm, vp, vp]
+        L.stem_block_enter_forward.restype = i32
+        L.stem_block_enter_backward.argtypes = [vp, vp, vp, i64, norm, vp, vp, vp, i32, vp]
+        L.stem_block_enter_backward.restype = i32
+        L.stem_block_leave_forward.argtypes = [vp, vp, vp, i64, leave, vp, vp, vp]
+        L.stem_block_leave_forward.restype = i32
+        L.stem_block_leave_backward.argtypes = [vp, vp, vp, vp, vp, i64, leave, vp, vp, vp, vp, vp, i32, vp]
+        L.stem_block_leave_backward.restype = i32
+        L.stem_dropout.argtypes = [vp, vp, i64, i64, ctypes.POINTER(stem_drop), vp, vp]
+        L.stem_dropout.restype = i32
+        L.stem_quant_bytes.argtypes = [i64, i64]
+        L.stem_quant_bytes.restype = i64
+        L.stem_quant_weights.argtypes = [vp, vp, i64, i64, vp, vp, vp]
+        L.stem_quant_weights.restype = i32
+        L.stem_quant_linear.argtypes = [vp, vp, i64, i64, norm, vp, vp, i64, vp, vp, vp]
+        L.stem_quant_linear.restype = i32
+        L.stem_quant_ffn_forward.argtypes = [vp, vp, vp, i64, norm, vp, vp, vp, vp, vp, i64, vp, vp, vp]
+        L.stem_quant_ffn_forward.restype = i32
         L.stem_profile_enable.argtypes = [vp, i32]
         L.stem_profile_enable.restype = i32
         L.stem_profile_kernels.argtypes = []
@@ -207,7 +278,14 @@ def _ptr(t, dtype=None, cuda=True, name="tensor"):
     return t.data_ptr()
 
 
-STEM_RESERVE_UP, STEM_RESERVE_EDIT = 1, 2
+def _shaped(t, dtype, shape, name: str):
+    """The pointer of a device tensor that has to have this shape (None stays None)."""
+    if t is not None and t.shape != shape:
+        raise ValueError(f"{name}: expected shape {tuple(shape)}, got {tuple(t.shape)}")
+    return _ptr(t, dtype, name=name)
+
+
+STEM_RESERVE_UP, STEM_RESERVE_EDIT, STEM_RESERVE_QUANT = 1, 2, 4
 STEM_NOALLOC_MAX_TOKENS = 65536
 STEM_PREFETCH_KERNEL, STEM_PREFETCH_MEMCPY = 0, 1
 
@@ -450,6 +528,121 @@ def stem_edit_rows(ctx: StemCtx, E, src_ids, tgt_ids, mode: int, pad_id: int = 0
     st = lib().stem_edit_rows(ctx.handle, _ptr(E, ctx.torch_dtype, name="E"), src, len(src_ids), tgt, len(tgt_ids),
                               mode, pad_id, _ptr(backup, ctx.torch_dtype, name="backup"), _stream(stream))
     _check(ctx, st, "stem_edit_rows")
+
+
+def stem_block_enter_forward(ctx: StemCtx, x, norm: stem_norm, n, stream=None):
+    """n = N(x) * w."""
+    dt, shape = ctx.torch_dtype, (x.shape[0], ctx.d_model)
+    norm._check(ctx, ctx.d_model, "norm")
+    st = lib().stem_block_enter_forward(ctx.handle, _shaped(x, dt, shape, "x"), shape[0], norm, _shaped(n, dt, shape, "n"), _stream(stream))
+    if st != STEM_OK:
+        _check(ctx, st, "stem_block_enter_forward")
+
+
+def stem_block_enter_backward(ctx: StemCtx, dn, x, norm: stem_norm, dx, dw=None, dres=None, accumulate: bool = False, stream=None):
+    """dx = dres + the gradient of x; dw fp32."""
+    dt, d = ctx.torch_dtype, ctx.d_model
+    shape = (x.shape[0], d)
+    norm._check(ctx, d, "norm")
+    st = lib().stem_block_enter_backward(ctx.handle, _shaped(dn, dt, shape, "dn"), _shaped(x, dt, shape, "x"), shape[0], norm,
+                                         _shaped(dres, dt, shape, "dres"), _shaped(dx, dt, shape, "dx"),
+                                         _shaped(dw, torch.float32, (d,), "dw"), 1 if accumulate else 0, _stream(stream))
+    if st != STEM_OK:
+        _check(ctx, st, "stem_block_enter_backward")
+
+
+def stem_block_leave_forward(ctx: StemCtx, f, x, leave: stem_leave, y, n=None, stream=None):
+    """y = residual_scale x + branch_scale gate * drop(N_out(f) * w_out), n = N_next(y) * w_next; y may be x."""
+    dt, shape = ctx.torch_dtype, (x.shape[0], ctx.d_model)
+    leave._check(ctx, shape[0])
+    st = lib().stem_block_leave_forward(ctx.handle, _shaped(f, dt, shape, "f"), _shaped(x, dt, shape, "x"), shape[0], leave,
+                                        _shaped(y, dt, shape, "y"), _shaped(n, dt, shape, "n"), _stream(stream))
+    if st != STEM_OK:
+        _check(ctx, st, "stem_block_leave_forward")
+
+
+def stem_block_leave_backward(ctx: StemCtx, dy, dn, f, y, leave: stem_leave, dx, df, dgate=None, dw_out=None, dw_next=None,
+                              accumulate: bool = False, stream=None):
+    """Gradients of stem_block_leave_forward; dy or dn may be None, and so may every output."""
+    dt, d, f32 = ctx.torch_dtype, ctx.d_model, torch.float32
+    shape = ((dy if dy is not None else dn).shape[0], d)
+    leave._check(ctx, shape[0])
+    gate_shape = {STEM_GATE_CHANNEL: (d,), STEM_GATE_TOKEN: shape[:1]}.get(leave.gate_kind, shape)
+    st = lib().stem_block_leave_backward(ctx.handle, _shaped(dy, dt, shape, "dy"), _shaped(dn, dt, shape, "dn"), _shaped(f, dt, shape, "f"),
+                                         _shaped(y, dt, shape, "y"), shape[0], leave, _shaped(dx, dt, shape, "dx"),
+                                         _shaped(df, dt, shape, "df"),
+                                         _shaped(dgate, f32 if leave.gate_kind == STEM_GATE_CHANNEL else dt, gate_shape, "dgate"),
+                                         _shaped(dw_out, f32, (d,), "dw_out"), _shaped(dw_next, f32, (d,), "dw_next"),
+                                         1 if accumulate else 0, _stream(stream))
+    if st != STEM_OK:
+        _check(ctx, st, "stem_block_leave_backward")
+
+
+def stem_dropout(ctx: StemCtx, x, y, p: float, seed: int, offset: int = 0, step=None, stream=None):
+    """y = D(x), rows of any width; on the gradient the same call is the backward pass.  y may be x."""
+    shape = (x.shape[0], x.shape[1])
+    st = lib().stem_dropout(ctx.handle, _shaped(x, ctx.torch_dtype, shape, "x"), *shape, stem_drop(p, seed, offset, step),
+                            _shaped(y, ctx.torch_dtype, shape, "y"), _stream(stream))
+    if st != STEM_OK:
+        _check(ctx, st, "stem_dropout")
+
+
+class StemQuant:
+    """A weight matrix [N, K] in the 8-bit form that stem_quant_linear and stem_quant_ffn_forward read."""
+
+    def __init__(self, q, scale, N: int, K: int):
+        self.q, self.scale, self.N, self.K = q, scale, N, K
+
+
+def stem_quant_bytes(N: int, K: int) -> int:
+    return lib().stem_quant_bytes(N, K)
+
+
+def stem_quant_weights(ctx: StemCtx, W, out: StemQuant | None = None, stream=None) -> StemQuant:
+    """W [N, K] quantised by rows, into `out` or new buffers."""
+    N, K = W.shape
+    if out is None:
+        out = StemQuant(torch.empty(lib().stem_quant_bytes(N, K), dtype=torch.int8, device=W.device),
+                        torch.empty(N, dtype=torch.float32, device=W.device), N, K)
+    st = lib().stem_quant_weights(ctx.handle, _shaped(W, ctx.torch_dtype, (out.N, out.K), "W"), N, K,
+                                  _shaped(out.q, torch.int8, (lib().stem_quant_bytes(N, K),), "out.q"),
+                                  _shaped(out.scale, torch.float32, (N,), "out.scale"), _stream(stream))
+    _check(ctx, st, "stem_quant_weights")
+    return out
+
+
+def _quant(w: StemQuant, N: int, K: int, name: str):
+    if (w.N, w.K) != (N, K):
+        raise ValueError(f"{name}: expected weights of shape {(N, K)}, got {(w.N, w.K)}")
+    return _ptr(w.q, torch.int8, name=name + ".q"), _ptr(w.scale, torch.float32, name=name + ".scale")
+
+
+def stem_quant_linear(ctx: StemCtx, x, W: StemQuant, y, residual=None, norm: stem_norm | None = None, stream=None):
+    """y = Q(N(x)) W^T (+ residual)."""
+    dt, T = ctx.torch_dtype, x.shape[0]
+    q, scale = _quant(W, W.N, W.K, "W")
+    if norm is not None:
+        norm._check(ctx, W.K, "norm")
+    st = lib().stem_quant_linear(ctx.handle, _shaped(x, dt, (T, W.K), "x"), T, W.K, norm, q, scale, W.N,
+                                 _shaped(residual, dt, (T, W.N), "residual"), _shaped(y, dt, (T, W.N), "y"), _stream(stream))
+    if st != STEM_OK:
+        _check(ctx, st, "stem_quant_linear")
+
+
+def stem_quant_ffn_forward(ctx: StemCtx, x, ids, gate: StemQuant, down: StemQuant, E, y, residual=None, norm: stem_norm | None = None,
+                           stream=None, E_rows=None):
+    """y = Q(SiLU(Q(N(x)) gate^T) * E[ids]) down^T (+ residual); y may be x and residual."""
+    dt, T, d, F = ctx.torch_dtype, x.shape[0], ctx.d_model, ctx.d_ff
+    gq, gs = _quant(gate, F, d, "gate")
+    dq, ds = _quant(down, d, F, "down")
+    if norm is not None:
+        norm._check(ctx, d, "norm")
+    E_rows = E.shape[0] if E_rows is None else E_rows
+    st = lib().stem_quant_ffn_forward(ctx.handle, _shaped(x, dt, (T, d), "x"), _shaped(ids, torch.int32, (T,), "ids"), T, norm, gq, gs, dq, ds,
+                                      _shaped(E, dt, (E.shape[0], F), "E"), E_rows, _shaped(residual, dt, (T, d), "residual"),
+                                      _shaped(y, dt, (T, d), "y"), _stream(stream))
+    if st != STEM_OK:
+        _check(ctx, st, "stem_quant_ffn_forward")
 
 
 def stem_profile_enable(ctx: StemCtx, on: bool):
