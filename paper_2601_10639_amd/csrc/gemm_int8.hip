@@ -1,0 +1,420 @@
+// 8-bit MFMA products for gfx950: y[m,n] = s_m t_n sum_k a_mk b_nk, tokens a and weights b in blocks of 32 rows x 32 k (quant.h).
+//
+// A block is one operand of v_mfma_i32_32x32x32_i8 as it lies in memory, so a tile of an operand is 4 KB for each 32 rows and 128 k, in
+// a row; it goes to LDS as it is (buffer_load ... lds), and a fragment is the 16 bytes at 16 x lane of a block: no swizzle, no bank
+// conflict, one address register for an operand.  The sums are integers, so neither the order of K nor its cuts change a result.
+//
+// The instruction multiplies twice as many k as the bf16 one of the same shape in the same 32 clocks on operands of the same bytes, so
+// the large tile is that product's (gemm_bf16.hip): 256 x 256, 4 wavefronts of 4 x 4 accumulators, a ring of five 32 KB slots.
+#include "quant.h"
+
+typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8_t;
+typedef __attribute__((ext_vector_type(4))) __bf16 bf16x4_t;
+typedef __attribute__((ext_vector_type(4))) int i32x4_t;
+typedef __attribute__((ext_vector_type(16))) int i32x16_t;
+typedef __attribute__((ext_vector_type(4))) float f32x4_t;
+typedef __attribute__((ext_vector_type(4))) uint32_t u32x4_t;
+typedef __attribute__((ext_vector_type(2))) uint32_t u32x2_t;
+typedef __attribute__((address_space(3))) void* lds_ptr_t;
+typedef __amdgpu_buffer_rsrc_t rsrc_t;
+
+namespace {
+
+constexpr uint32_t OOB = 0x80000000u;   // a buffer offset beyond any operand: reads as zero, is not stored
+
+__device__ __forceinline__ float sigmoidf_fast(float z) { return __builtin_amdgcn_rcpf(1.0f + __expf(-z)); }
+__device__ __forceinline__ void lds_dma_16(rsrc_t rs, char* lds_dst, uint32_t off, int soff) {
+  __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (lds_ptr_t)lds_dst, 16, off, soff, 0, 0);
+}
+__device__ __forceinline__ rsrc_t resource(const void* p, int bytes) {
+  return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(p), 0, bytes, 0x00020000);
+}
+
+// Workgroup -> tile, as the bf16 products do it: the workgroups of an XCD take a contiguous run of tiles, walked in bands of 4 token tiles.
+__device__ __forceinline__ void tile_of(int b, int nb, int ntm, int ntn, int& tm, int& tn) {
+  const int q = nb >> 3, r = nb & 7, xcd = b & 7;
+  const int L = xcd * q + (xcd < r ? xcd : r) + (b >> 3);
+  const int per = 4 * ntn, group = L / per, first = group * 4, rows = ntm - first < 4 ? ntm - first : 4, in = L - group * per;
+  tm = first + in % rows;
+  tn = in / rows;
+}
+
+// The operand tiles of a workgroup: EDGE rows x 128 k, LOADS loads of 1 KB for each of LOADERS wavefronts
+template <int EDGE, int LOADERS>
+struct Loader {
+  static constexpr int LOADS = EDGE * 128 / 1024 / LOADERS;
+  rsrc_t r;
+  uint32_t off[(LOADS + 3) / 4];   // of the 32-row groups this wavefront loads from
+  const void* base;
+  int bytes;
+  __device__ __forceinline__ void init(const int8_t* p, int rows, int K, int row0, int wave, int lane) {
+    base = p;
+    bytes = (rows + 31) / 32 * 32 * K;
+    r = resource(p, bytes);
+#pragma unroll
+    for (int i = 0; i < (LOADS + 3) / 4; ++i) {
+      const int group = row0 / 32 + (wave * LOADS + i * 4) / 4;
+      off[i] = group * 32 < rows ? (uint32_t)(group * 32 * K + lane * 16) : OOB;
+    }
+  }
+  // load i of the K tile at byte `k` of a group
+  __device__ __forceinline__ void issue(int i, char* tile, int wave, int k) const {
+    const int piece = wave * LOADS + i;
+    lds_dma_16(r, tile + piece * 1024, off[LOADS < 4 ? 0 : i / 4], k + (piece & 3) * 1024);
+  }
+};
+
+// ---- epilogue: a wavefront's 32 MI x 32 NJ results, 32 rows at a time through LDS ------------------------------------------
+// acc[i][j]: token block i, channel block j; a lane holds token lane & 31 and channels 8 g + 4 (lane >> 5) + 0..3 of each.
+template <bool GATE, int MI, int NJ>
+struct Epilogue {
+  static constexpr int COLS = 32 * NJ;
+  static constexpr int PITCH = COLS + 4;                  // of a staged row, in words
+  static constexpr int BYTES = 32 * PITCH * 4;            // of LDS, for each wavefront
+  static constexpr int CPL = GATE ? 4 : 8;                // columns of a lane: 16 bytes of fp32 or of bf16
+  static constexpr int LPR = COLS / CPL, RPP = 64 / LPR, PASSES = 32 / RPP;
+
+  static __device__ __forceinline__ void run(const QuantGemmArgs& p, const i32x16_t (&acc)[MI][NJ], char* stg, int m0, int n0, int lane) {
+    int* const st = reinterpret_cast<int*>(stg);
+    const int srow = lane / LPR, scol = (lane % LPR) * CPL, n = n0 + scol;
+    const bool whole = p.N % 8 == 0;                      // rows of y and h are 16-byte aligned
+    float sb[CPL];
+#pragma unroll
+    for (int q = 0; q < CPL; ++q) sb[q] = n + q < p.N ? p.scale_b[n + q] : 0.f;
+#pragma unroll
+    for (int i = 0; i < MI; ++i) {
+      const int mi = m0 + i * 32;
+      if (mi >= p.M) break;
+#pragma unroll
+      for (int j = 0; j < NJ; ++j)
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+          const i32x4_t w = {acc[i][j][4 * g], acc[i][j][4 * g + 1], acc[i][j][4 * g + 2], acc[i][j][4 * g + 3]};
+          *reinterpret_cast<i32x4_t*>(st + (lane & 31) * PITCH + j * 32 + g * 8 + (lane >> 5) * 4) = w;
+        }
+      // scale, and for the gate product the table row, of the row that lane & 31 names
+      const int mr = mi + (lane & 31) < p.M ? mi + (lane & 31) : p.M - 1;
+      const float sa_row = p.scale_a[mr];
+      int id_row = 0;
+      if (GATE) {
+        id_row = p.ids[mr];
+        if ((unsigned)id_row >= (unsigned)p.E_rows) {
+          *p.flag = 1;
+          id_row = id_row < 0 ? 0 : p.E_rows - 1;
+        }
+      }
+      __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+      __builtin_amdgcn_wave_barrier();
+      __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+      if (GATE || whole) {
+#pragma unroll
+        for (int pass = 0; pass < PASSES; ++pass) {
+          const int r = pass * RPP + srow, m = mi + r;
+          const float sa = __shfl(sa_row, r);
+          const int id = GATE ? __shfl(id_row, r) : 0;
+          if (m >= p.M || n >= p.N) continue;
+          const int* const src = st + r * PITCH + scol;
+          float z[CPL];
+#pragma unroll
+          for (int h = 0; h < CPL; h += 4) {
+            const i32x4_t c = *reinterpret_cast<const i32x4_t*>(src + h);
+#pragma unroll
+            for (int q = 0; q < 4; ++q) z[h + q] = (float)c[q] * (sa * sb[h + q]);
+          }
+          const size_t at = (size_t)m * p.N + n;
+          if constexpr (GATE) {
+            const u32x2_t e = *reinterpret_cast<const u32x2_t*>(p.E + (size_t)id * p.N + n);
+            const float u[4] = {__uint_as_float(e[0] << 16), __uint_as_float(e[0] & 0xffff0000u), __uint_as_float(e[1] << 16),
+                                __uint_as_float(e[1] & 0xffff0000u)};
+            f32x4_t o;
+#pragma unroll
+            for (int q = 0; q < 4; ++q) o[q] = z[q] * sigmoidf_fast(z[q]) * u[q];
+            *reinterpret_cast<f32x4_t*>(p.h + at) = o;
+          } else {
+            bf16x8_t o;
+            if (p.residual) {
+              const bf16x8_t rz = *reinterpret_cast<const bf16x8_t*>(p.residual + at);
+#pragma unroll
+              for (int q = 0; q < 8; ++q) z[q] += (float)rz[q];
+            }
+#pragma unroll
+            for (int q = 0; q < 8; ++q) o[q] = (__bf16)z[q];
+            *reinterpret_cast<bf16x8_t*>(p.y + at) = o;
+          }
+        }
+      } else {
+        // rows of y at any 2-byte address: neighbouring lanes have neighbouring columns
+        for (int r = 0; r < 32; ++r) {
+          const float sa = __shfl(sa_row, r);
+          const int m = mi + r;
+          if (m >= p.M) break;
+#pragma unroll
+          for (int c = 0; c < COLS; c += 64) {
+            const int col = c + lane;
+            if (col >= COLS || n0 + col >= p.N) continue;
+            float z = (float)st[r * PITCH + col] * (sa * p.scale_b[n0 + col]);
+            const size_t at = (size_t)m * p.N + n0 + col;
+            if (p.residual) z += __uint_as_float((uint32_t)p.residual[at] << 16);
+            reinterpret_cast<__bf16*>(p.y)[at] = (__bf16)z;
+          }
+        }
+      }
+      __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+      __builtin_amdgcn_wave_barrier();   // all have read the rows before they are staged over
+      __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+    }
+  }
+};
+
+// ---- 256 x 256 ----------------------------------------------------------------------------------------------------------------
+constexpr int SLOT = 32768;   // an operand tile: 256 rows x 128 k
+
+template <bool GATE>
+__global__ __launch_bounds__(256) void gemm_int8_256_kernel(QuantGemmArgs p) {
+  __shared__ __attribute__((aligned(16))) char smem[5 * SLOT];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int wm = wave >> 1, wn = wave & 1;
+  int tm, tn;
+  tile_of(blockIdx.x, gridDim.x, (p.M + 255) / 256, (p.N + 255) / 256, tm, tn);
+  const int m0 = tm * 256, n0 = tn * 256;
+  Loader<256, 4> la, lb;
+  la.init(p.A, p.M, p.K, m0, wave, lane);
+  lb.init(p.B, p.N, p.K, n0, wave, lane);
+  const int nk = p.K / 128, kbytes = nk * 4096;
+  // every XCD starts at another eighth of K: the rows' groups are a power of two apart where K is, and so their blocks at one k in the
+  // same few memory channels
+  int ka = nk >= 16 ? (int)(blockIdx.x & 7) * nk / 8 * 4096 : 0, kb = ka;
+  int left_a = nk, left_b = nk;   // tiles still to be requested; requests beyond the last one read nothing
+  auto next = [&](int& k, int& left, auto& l) __attribute__((always_inline)) {
+    k += 4096;
+    if (k >= kbytes) k = 0;
+    if (--left <= 0) l.r = resource(l.base, 0);
+  };
+  i32x16_t acc[4][4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) acc[i][j] = i32x16_t{};
+
+  i32x4_t xa[4], xb[4], ya[4], yb[4];
+  const uint32_t fa = wm * 16384 + lane * 16, fb = wn * 16384 + lane * 16;
+  auto frag = [&](int slot, uint32_t f, int ks, int i) __attribute__((always_inline)) {
+    return *reinterpret_cast<const i32x4_t*>(smem + slot * SLOT + f + i * 4096 + ks * 1024);
+  };
+  // order of a k-step's fragments and of the products that use them, two a fragment
+  auto mma2 = [&](int q, i32x4_t(&a)[4], i32x4_t(&b)[4]) __attribute__((always_inline)) {
+    constexpr int ii[16] = {0, 0, 1, 1, 0, 1, 0, 1, 2, 2, 2, 2, 3, 3, 3, 3};
+    constexpr int jj[16] = {0, 1, 0, 1, 2, 2, 3, 3, 0, 1, 2, 3, 0, 1, 2, 3};
+#pragma unroll
+    for (int h = 2 * q; h < 2 * q + 2; ++h)
+      acc[ii[h]][jj[h]] = __builtin_amdgcn_mfma_i32_32x32x32_i8(b[jj[h]], a[ii[h]], acc[ii[h]][jj[h]], 0, 0, 0);
+  };
+  auto read = [&](int sa, int sb, int ks, int q, i32x4_t(&a)[4], i32x4_t(&b)[4]) __attribute__((always_inline)) {
+    constexpr int isA[8] = {1, 0, 0, 1, 0, 0, 1, 1};
+    constexpr int idx[8] = {0, 0, 1, 1, 2, 3, 2, 3};
+    if (isA[q]) a[idx[q]] = frag(sa, fa, ks, idx[q]);
+    else b[idx[q]] = frag(sb, fb, ks, idx[q]);
+  };
+  // Operand tiles alternate through the slots: A of K tile t in slot 2t mod 5, B in 2t+1 mod 5.  A(t+2) is requested during the first two
+  // k-steps of tile t, B(t+2) behind the barrier before its last: whole K tiles before they are needed, and the wait in front of the
+  // barrier leaves the youngest 8 loads in flight.
+#pragma unroll
+  for (int h = 0; h < 4; ++h) {
+#pragma unroll
+    for (int q = 0; q < 8; ++q) {
+      if (h & 1) lb.issue(q, smem + h * SLOT, wave, kb);
+      else la.issue(q, smem + h * SLOT, wave, ka);
+    }
+    if (h & 1) next(kb, left_b, lb); else next(ka, left_a, la);
+  }
+  asm volatile("s_waitcnt vmcnt(%0)" ::"n"(16) : "memory");
+  __builtin_amdgcn_s_barrier();
+  __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+  for (int q = 0; q < 8; ++q) read(0, 1, 0, q, xa, xb);
+  auto ring_iteration = [&](const int tmod) __attribute__((always_inline)) {
+    const int sa = (2 * tmod) % 5, sb = (2 * tmod + 1) % 5, na = (2 * tmod + 2) % 5, nb = (2 * tmod + 3) % 5, ia = (2 * tmod + 4) % 5;
+#pragma unroll
+    for (int q = 0; q < 8; ++q) {
+      read(sa, sb, 1, q, ya, yb);
+      if (q < 4) la.issue(q, smem + ia * SLOT, wave, ka);
+      mma2(q, xa, xb);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+#pragma unroll
+    for (int q = 0; q < 8; ++q) {
+      read(sa, sb, 2, q, xa, xb);
+      if (q < 4) la.issue(4 + q, smem + ia * SLOT, wave, ka);
+      mma2(q, ya, yb);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    next(ka, left_a, la);
+#pragma unroll
+    for (int q = 0; q < 8; ++q) {
+      read(sa, sb, 3, q, ya, yb);
+      mma2(q, xa, xb);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(8) : "memory");
+    __builtin_amdgcn_s_barrier();
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int q = 0; q < 8; ++q) {
+      read(na, nb, 0, q, xa, xb);
+      lb.issue(q, smem + sa * SLOT, wave, kb);
+      mma2(q, ya, yb);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    next(kb, left_b, lb);
+  };
+  int kt = 0;
+  for (; kt + 5 <= nk; kt += 5) {
+    ring_iteration(0);
+    ring_iteration(1);
+    ring_iteration(2);
+    ring_iteration(3);
+    ring_iteration(4);
+  }
+  if (kt < nk) ring_iteration(0);
+  if (kt + 1 < nk) ring_iteration(1);
+  if (kt + 2 < nk) ring_iteration(2);
+  if (kt + 3 < nk) ring_iteration(3);
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+  __syncthreads();
+  typedef Epilogue<GATE, 4, 4> Out;
+  static_assert(4 * Out::BYTES <= 5 * SLOT, "staging");
+  Out::run(p, acc, smem + wave * Out::BYTES, m0 + wm * 128, n0 + wn * 128, lane);
+}
+
+// ---- smaller tiles: STAGES whole K tiles in LDS, filled by LW wavefronts of their own ---------------------------------------------
+template <int MI_, int NJ_, int WM_, int WN_, int STAGES_, int LW_>
+struct Tiling {
+  static constexpr int MI = MI_, NJ = NJ_, WM = WM_, WN = WN_, STAGES = STAGES_, LW = LW_, WAVES = WM * WN;
+  static constexpr int TM = 32 * MI * WM, TN = 32 * NJ * WN;
+  static constexpr int A_BYTES = TM * 128, STAGE = (TM + TN) * 128;
+};
+
+template <bool GATE, class C>
+__global__ __launch_bounds__((C::WAVES + C::LW) * 64) void gemm_int8_kernel(QuantGemmArgs p) {
+  constexpr int MI = C::MI, NJ = C::NJ, S = C::STAGES, STAGE = C::STAGE;
+  typedef Epilogue<GATE, MI, NJ> Out;
+  constexpr int LDS = S * STAGE > C::WAVES * Out::BYTES ? S * STAGE : C::WAVES * Out::BYTES;
+  __shared__ __attribute__((aligned(16))) char smem[LDS];
+  const int lane = threadIdx.x & 63, wave_id = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const bool load_wave = wave_id >= C::WAVES;
+  const int wave = load_wave ? wave_id - C::WAVES : wave_id, wm = wave / C::WN, wn = wave % C::WN;
+  int tm, tn;
+  tile_of(blockIdx.x, gridDim.x, (p.M + C::TM - 1) / C::TM, (p.N + C::TN - 1) / C::TN, tm, tn);
+  const int m0 = tm * C::TM, n0 = tn * C::TN;
+  const int nk = p.K / 128, kbytes = nk * 4096;
+  if (load_wave) {
+    Loader<C::TM, C::LW> la;
+    Loader<C::TN, C::LW> lb;
+    constexpr int LOADS = la.LOADS + lb.LOADS;
+    la.init(p.A, p.M, p.K, m0, wave, lane);
+    lb.init(p.B, p.N, p.K, n0, wave, lane);
+    int k = nk >= 16 ? (int)(blockIdx.x & 7) * nk / 8 * 4096 : 0, left = nk;
+    auto request = [&](const int st) __attribute__((always_inline)) {
+#pragma unroll
+      for (int q = 0; q < la.LOADS; ++q) la.issue(q, smem + st * STAGE, wave, k);
+#pragma unroll
+      for (int q = 0; q < lb.LOADS; ++q) lb.issue(q, smem + st * STAGE + C::A_BYTES, wave, k);
+      k += 4096;
+      if (k >= kbytes) k = 0;
+      if (--left <= 0) { la.r = resource(p.A, 0); lb.r = resource(p.B, 0); }
+    };
+#pragma unroll
+    for (int st = 0; st < S; ++st) request(st);
+    asm volatile("s_waitcnt vmcnt(%0)" ::"n"((S - 1) * LOADS) : "memory");
+    __builtin_amdgcn_s_barrier();
+    auto load_iteration = [&](const int st) __attribute__((always_inline)) {
+      asm volatile("s_waitcnt vmcnt(%0)" ::"n"((S - 2) * LOADS) : "memory");
+      __builtin_amdgcn_s_barrier();
+      __builtin_amdgcn_sched_barrier(0);
+      request(st);
+      __builtin_amdgcn_sched_barrier(0);
+    };
+    int kt = 0;
+    for (; kt + S <= nk; kt += S) {
+#pragma unroll
+      for (int st = 0; st < S; ++st) load_iteration(st);
+    }
+#pragma unroll
+    for (int st = 0; st < S - 1; ++st)
+      if (kt + st < nk) load_iteration(st);
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // nothing lands in LDS once the epilogue stages through it
+    __syncthreads();
+    return;
+  }
+  i32x16_t acc[MI][NJ];
+#pragma unroll
+  for (int i = 0; i < MI; ++i)
+#pragma unroll
+    for (int j = 0; j < NJ; ++j) acc[i][j] = i32x16_t{};
+  i32x4_t xa[MI], xb[NJ], ya[MI], yb[NJ];
+  const char* const fa = smem + wm * MI * 4096 + lane * 16;
+  const char* const fb = smem + C::A_BYTES + wn * NJ * 4096 + lane * 16;
+  constexpr int NFRAG = MI + NJ, NMMA = MI * NJ;
+  auto read = [&](int st, int ks, int q, i32x4_t(&a)[MI], i32x4_t(&b)[NJ]) __attribute__((always_inline)) {   // order a0, b0, b1, .., a1, ..
+    if (q == 0) a[0] = *reinterpret_cast<const i32x4_t*>(fa + st * STAGE + ks * 1024);
+    else if (q <= NJ) b[q - 1] = *reinterpret_cast<const i32x4_t*>(fb + st * STAGE + (q - 1) * 4096 + ks * 1024);
+    else a[q - NJ] = *reinterpret_cast<const i32x4_t*>(fa + st * STAGE + (q - NJ) * 4096 + ks * 1024);
+  };
+  auto kstep = [&](int st, int ks_next, i32x4_t(&a)[MI], i32x4_t(&b)[NJ], i32x4_t(&na)[MI], i32x4_t(&nb)[NJ]) __attribute__((always_inline)) {
+#pragma unroll
+    for (int u = 0; u < NMMA; ++u) {
+#pragma unroll
+      for (int q = u * NFRAG / NMMA; q < (u + 1) * NFRAG / NMMA; ++q) read(st, ks_next, q, na, nb);
+      acc[u / NJ][u % NJ] = __builtin_amdgcn_mfma_i32_32x32x32_i8(b[u % NJ], a[u / NJ], acc[u / NJ][u % NJ], 0, 0, 0);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+  };
+  __builtin_amdgcn_s_barrier();
+  __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+  for (int q = 0; q < NFRAG; ++q) read(0, 0, q, xa, xb);
+  // One barrier a K tile, before its last k-step: the load wavefronts have seen the next tile land, the others have read the last of this.
+  auto stage_iteration = [&](const int st) __attribute__((always_inline)) {
+    kstep(st, 1, xa, xb, ya, yb);
+    kstep(st, 2, ya, yb, xa, xb);
+    kstep(st, 3, xa, xb, ya, yb);
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    __builtin_amdgcn_s_barrier();
+    __builtin_amdgcn_sched_barrier(0);
+    kstep((st + 1) % S, 0, ya, yb, xa, xb);
+  };
+  int kt = 0;
+  for (; kt + S <= nk; kt += S) {
+#pragma unroll
+    for (int st = 0; st < S; ++st) stage_iteration(st);
+  }
+#pragma unroll
+  for (int st = 0; st < S - 1; ++st)
+    if (kt + st < nk) stage_iteration(st);
+  __syncthreads();
+  Out::run(p, acc, smem + wave * Out::BYTES, m0 + wm * MI * 32, n0 + wn * NJ * 32, lane);
+}
+
+typedef Tiling<2, 2, 2, 2, 4, 4> Tile128;       // 128 x 128, 128 KB of LDS
+typedef Tiling<2, 1, 2, 2, 6, 4> Tile128x64;    // 144 KB
+
+template <class C>
+hipError_t launch(const QuantGemmArgs& a, hipStream_t s) {
+  const int grid = ((a.M + C::TM - 1) / C::TM) * ((a.N + C::TN - 1) / C::TN);
+  if (a.y) gemm_int8_kernel<false, C><<<grid, (C::WAVES + C::LW) * 64, 0, s>>>(a);
+  else gemm_int8_kernel<true, C><<<grid, (C::WAVES + C::LW) * 64, 0, s>>>(a);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t stem_quant_gemm_launch(stem_ctx* ctx, int kid, const QuantGemmArgs& a, hipStream_t s) {
+  ProfScope prof(ctx, kid, s);
+  const int t256 = ((a.M + 255) / 256) * ((a.N + 255) / 256), t128 = ((a.M + 127) / 128) * ((a.N + 127) / 128);
+  if (t256 >= 192) {
+    if (a.y) gemm_int8_256_kernel<false><<<t256, 256, 0, s>>>(a);
+    else gemm_int8_256_kernel<true><<<t256, 256, 0, s>>>(a);
+    return hipGetLastError();
+  }
+  return t128 >= 192 ? launch<Tile128>(a, s) : launch<Tile128x64>(a, s);
+}

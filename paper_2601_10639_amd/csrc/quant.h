@@ -1,4 +1,4 @@
-// 8-bit integer products: layout, arguments and launches (quant.hip), called by their entry points (api_block.hip).
+// 8-bit integer products: layout, arguments and launches (quant.hip, gemm_int8.hip), called by their entry points (api_block.hip).
 //
 // Layout.  A matrix [rows, K] is kept as blocks of 32 rows x 32 k, 1 KB each: chunk h of row r, 16 bytes of k = 16 h .. 16 h + 15, lies at
 // (32 h + r) * 16, so that a block is one operand of v_mfma_i32_32x32x32_i8 with lane l's 16 bytes at 16 l, and a load of it is 1 KB in a

@@ -1,4 +1,4 @@
-// Products in 8-bit integers with a scale for each token and each channel, for serving.
+// Rows to 8-bit integers, for products with a scale for each token and each channel (gemm_int8.hip).
 //
 //     s_t = max_k |x_tk| / 127,  q_tk = rint(x_tk / s_t);   y_tn = s_t s_n sum_k q_tk q_nk
 //
@@ -8,13 +8,8 @@
 #include "quant.h"
 
 typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8_t;
-typedef __attribute__((ext_vector_type(4))) __bf16 bf16x4_t;
-typedef __attribute__((ext_vector_type(4))) int i32x4_t;
-typedef __attribute__((ext_vector_type(16))) int i32x16_t;
 
 namespace {
-
-__device__ __forceinline__ float sigmoidf(float z) { return 1.0f / (1.0f + __expf(-z)); }
 
 // ---- rows to integers -------------------------------------------------------------------------------------
 // 16 elements of a row from p on, of which `left` are the row's; the others read as zero.  VEC: rows are multiples of 8 elements.
@@ -155,50 +150,6 @@ __global__ __launch_bounds__(256) void quant_rows_kernel(QuantRowsArgs p) {
   }
 }
 
-// ---- the product ----------------------------------------------------------------------------------------------
-// A wavefront has 32 tokens x 32 channels and reads its blocks from memory.  With the weights as the first operand a lane holds, for one
-// token, groups of four neighbouring channels.
-template <bool GATE>
-__global__ __launch_bounds__(256) void quant_gemm_kernel(QuantGemmArgs p) {
-  const int lane = threadIdx.x & 63;
-  const int mt = (p.M + 31) / 32, nt = (p.N + 31) / 32;
-  const int64_t tile = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-  if (tile >= (int64_t)mt * nt) return;
-  const int tm = (int)(tile % mt), tn = (int)(tile / mt);
-  const i32x4_t* a = reinterpret_cast<const i32x4_t*>(p.A + (int64_t)tm * 32 * p.K) + lane;
-  const i32x4_t* b = reinterpret_cast<const i32x4_t*>(p.B + (int64_t)tn * 32 * p.K) + lane;
-  i32x16_t acc = {};
-  for (int k = 0; k < p.K / 32; ++k) acc = __builtin_amdgcn_mfma_i32_32x32x32_i8(b[k * 64], a[k * 64], acc, 0, 0, 0);
-  const int m = tm * 32 + (lane & 31);
-  if (m >= p.M) return;
-  const float sa = p.scale_a[m];
-  int id = 0;
-  if (GATE) {
-    id = p.ids[m];
-    if ((unsigned)id >= (unsigned)p.E_rows) {
-      *p.flag = 1;
-      id = id < 0 ? 0 : p.E_rows - 1;
-    }
-  }
-#pragma unroll
-  for (int g = 0; g < 4; ++g) {
-    const int n = tn * 32 + 8 * g + 4 * (lane >> 5);
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      if (n + e >= p.N) break;
-      const float z = (float)acc[4 * g + e] * (sa * p.scale_b[n + e]);
-      const size_t at = (size_t)m * p.N + n + e;
-      if (GATE) {
-        const float u = __uint_as_float((uint32_t)p.E[(size_t)id * p.N + n + e] << 16);
-        p.h[at] = z * sigmoidf(z) * u;
-      } else {
-        const float o = p.residual ? z + __uint_as_float((uint32_t)p.residual[at] << 16) : z;
-        reinterpret_cast<__bf16*>(p.y)[at] = (__bf16)o;
-      }
-    }
-  }
-}
-
 template <class E, bool VEC>
 hipError_t rows(const QuantRowsArgs& a, hipStream_t s) {
   const unsigned grid = (unsigned)(a.pad_rows ? (a.rows + 31) / 32 * 32 : a.rows);
@@ -215,13 +166,4 @@ hipError_t stem_quant_rows_launch(stem_ctx* ctx, int kid, int is_bf16, const Qua
   const bool vec = a.K % 8 == 0;
   if (is_bf16) return vec ? rows<bf16_t, true>(a, s) : rows<bf16_t, false>(a, s);
   return vec ? rows<float, true>(a, s) : rows<float, false>(a, s);
-}
-
-hipError_t stem_quant_gemm_launch(stem_ctx* ctx, int kid, const QuantGemmArgs& a, hipStream_t s) {
-  ProfScope prof(ctx, kid, s);
-  const int64_t tiles = (int64_t)((a.M + 31) / 32) * ((a.N + 31) / 32);
-  const unsigned grid = (unsigned)((tiles + 3) / 4);
-  if (a.y) quant_gemm_kernel<false><<<grid, 256, 0, s>>>(a);
-  else quant_gemm_kernel<true><<<grid, 256, 0, s>>>(a);
-  return hipGetLastError();
 }
