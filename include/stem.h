@@ -86,7 +86,7 @@ stem_status stem_create(stem_ctx** out, const stem_layer_desc* desc, int64_t max
  *   STEM_RESERVE_UP    one more [max_tokens, d_ff] activation and one more [d_ff, d_model] weight buffer,
  *                      for stem_ffn_up_forward / stem_ffn_up_backward (bf16 contexts);
  *   STEM_RESERVE_EDIT  index lists and 64 replacement rows for stem_edit_rows;
- *   STEM_RESERVE_QUANT 8-bit copies of [max_tokens, max(d_model, d_ff)] and of 4096 tokens' hidden values, these in fp32 too, for
+ *   STEM_RESERVE_QUANT 8-bit copies of [max_tokens, max(d_model, d_ff)] activations and of [max_tokens, d_ff] hidden values, for
  *                      stem_quant_linear / stem_quant_ffn_forward (bf16 contexts).
  * Those entry points return STEM_ERR_WORKSPACE until their scratch has been reserved. */
 #define STEM_RESERVE_UP 1u

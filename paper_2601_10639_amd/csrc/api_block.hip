@@ -99,14 +99,14 @@ size_t gate_bytes(const stem_ctx* c, int kind, int64_t T, size_t es) {
 
 stem_status check_quant(stem_ctx* c, const char* who) {
   if (c->desc.dtype != STEM_BF16) return stem_fail(c, STEM_ERR_UNSUPPORTED, "%s: needs a bf16 context", who);
-  if (!c->quant_hidden) return stem_fail(c, STEM_ERR_WORKSPACE, "%s: needs stem_reserve(ctx, STEM_RESERVE_QUANT)", who);
+  if (!c->quant_sync) return stem_fail(c, STEM_ERR_WORKSPACE, "%s: needs stem_reserve(ctx, STEM_RESERVE_QUANT)", who);
   return STEM_OK;
 }
 
-hipError_t quant_rows(stem_ctx* c, int kid, int is_bf16, const void* x, int64_t rows, int64_t K, const stem_norm* norm, bool pad, int8_t* q,
-                      float* scale, hipStream_t s) {
-  QuantRowsArgs a = {x, rows, (int)K, pad, norm ? *norm : stem_norm{STEM_NORM_NONE, 0.f, nullptr}, q, scale};
-  return stem_quant_rows_launch(c, kid, is_bf16, a, s);
+hipError_t quant_rows(stem_ctx* c, int kid, const void* x, int64_t rows, int64_t K, const stem_norm* norm, bool pad, int8_t* q, float* scale,
+                      uint32_t* clear, int64_t words, hipStream_t s) {
+  const QuantRowsArgs a = {static_cast<const bf16_t*>(x), rows, (int)K, pad, norm ? *norm : stem_norm{STEM_NORM_NONE, 0.f, nullptr}, q, scale, clear, words};
+  return stem_quant_rows_launch(c, kid, a, s);
 }
 
 }  // namespace
@@ -226,7 +226,7 @@ stem_status stem_quant_weights(stem_ctx* c, const void* W, int64_t N, int64_t K,
     return stem_fail(c, STEM_ERR_SHAPE, "%s: a matrix [%lld, %lld]; K is up to 131072 and the 8-bit form below 2^31 bytes", who, (long long)N, (long long)K);
   if (!W || !q || !scale) return stem_fail(c, STEM_ERR_INVALID_ARG, "%s: null pointer argument", who);
   STEM_TRY(check_buffers(c, who, {{W, (size_t)(N * K * 2)}}, {{q, (size_t)stem_quant_size(N, K)}, {scale, (size_t)N * 4}}, false));
-  HIP_TRY(c, quant_rows(c, K_QUANT_WEIGHTS, 1, W, N, K, nullptr, true, static_cast<int8_t*>(q), scale, static_cast<hipStream_t>(stream)));
+  HIP_TRY(c, quant_rows(c, K_QUANT_WEIGHTS, W, N, K, nullptr, true, static_cast<int8_t*>(q), scale, nullptr, 0, static_cast<hipStream_t>(stream)));
   return STEM_OK;
 }
 
@@ -248,7 +248,7 @@ stem_status stem_quant_linear(stem_ctx* c, const void* x, int64_t T, int64_t K, 
                          {{y, yb}}, false));
   STEM_TRY(check_buffers(c, who, {{x, xb}}, {}, false));
   hipStream_t s = static_cast<hipStream_t>(stream);
-  HIP_TRY(c, quant_rows(c, K_QUANT_ROWS, 1, x, T, K, norm, false, c->quant_x, c->quant_sx, s));
+  HIP_TRY(c, quant_rows(c, K_QUANT_ROWS, x, T, K, norm, false, c->quant_x, c->quant_sx, nullptr, 0, s));
   QuantGemmArgs g = {};
   g.A = c->quant_x; g.scale_a = c->quant_sx;
   g.B = static_cast<const int8_t*>(q); g.scale_b = scale;
@@ -278,25 +278,20 @@ stem_status stem_quant_ffn_forward(stem_ctx* c, const void* x, const int32_t* id
   if (reinterpret_cast<uintptr_t>(ids) & 3u) return stem_fail(c, STEM_ERR_INVALID_ARG, "%s: ids must be 4-byte aligned", who);
   if (overlap({ids, (size_t)T * 4}, {y, xb})) return stem_fail(c, STEM_ERR_INVALID_ARG, "%s: an output lies over an input", who);
   hipStream_t s = static_cast<hipStream_t>(stream);
-  // The hidden values of all tokens in fp32 would be read back from HBM; those of a chunk are still in the memory-side cache.
-  for (int64_t t0 = 0; t0 < T; t0 += STEM_QUANT_CHUNK) {
-    const int64_t n = std::min<int64_t>(STEM_QUANT_CHUNK, T - t0);
-    HIP_TRY(c, quant_rows(c, K_QUANT_ROWS, 1, static_cast<const bf16_t*>(x) + t0 * d, n, d, norm, false, c->quant_x, c->quant_sx, s));
-    QuantGemmArgs g = {};
-    g.A = c->quant_x; g.scale_a = c->quant_sx;
-    g.B = static_cast<const int8_t*>(gate_q); g.scale_b = gate_scale;
-    g.M = (int)n; g.N = (int)F; g.K = (int)stem_quant_pitch(d);
-    g.h = c->quant_hidden; g.ids = ids + t0; g.E = static_cast<const bf16_t*>(E); g.E_rows = (int)E_rows; g.flag = c->flag;
-    HIP_TRY(c, stem_quant_gemm_launch(c, K_QUANT_GATE, g, s));
-    HIP_TRY(c, quant_rows(c, K_QUANT_HIDDEN, 0, c->quant_hidden, n, F, nullptr, false, c->quant_h, c->quant_sh, s));
-    QuantGemmArgs b = {};
-    b.A = c->quant_h; b.scale_a = c->quant_sh;
-    b.B = static_cast<const int8_t*>(down_q); b.scale_b = down_scale;
-    b.M = (int)n; b.N = (int)d; b.K = (int)stem_quant_pitch(F);
-    b.y = static_cast<bf16_t*>(y) + t0 * d;
-    if (residual) b.residual = static_cast<const bf16_t*>(residual) + t0 * d;
-    HIP_TRY(c, stem_quant_gemm_launch(c, K_QUANT_DOWN, b, s));
-  }
+  HIP_TRY(c, quant_rows(c, K_QUANT_ROWS, x, T, d, norm, false, c->quant_x, c->quant_sx, c->quant_sync, stem_quant_words(T, F), s));
+  QuantGemmArgs g = {};
+  g.A = c->quant_x; g.scale_a = c->quant_sx;
+  g.B = static_cast<const int8_t*>(gate_q); g.scale_b = gate_scale;
+  g.M = (int)T; g.N = (int)F; g.K = (int)stem_quant_pitch(d);
+  g.hq = c->quant_h; g.scale_h = c->quant_sh; g.amax = c->quant_sync; g.panels = c->quant_sync + T; g.polls = c->polls;
+  g.ids = ids; g.E = static_cast<const bf16_t*>(E); g.E_rows = (int)E_rows; g.flag = c->flag;
+  HIP_TRY(c, stem_quant_gemm_launch(c, K_QUANT_GATE, g, s));
+  QuantGemmArgs b = {};
+  b.A = c->quant_h; b.scale_a = c->quant_sh;
+  b.B = static_cast<const int8_t*>(down_q); b.scale_b = down_scale;
+  b.M = (int)T; b.N = (int)d; b.K = (int)stem_quant_pitch(F);
+  b.y = static_cast<bf16_t*>(y); b.residual = static_cast<const bf16_t*>(residual);
+  HIP_TRY(c, stem_quant_gemm_launch(c, K_QUANT_DOWN, b, s));
   return STEM_OK;
 }
 

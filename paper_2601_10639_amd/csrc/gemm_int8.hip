@@ -64,27 +64,40 @@ struct Loader {
   }
 };
 
-// ---- epilogue: a wavefront's 32 MI x 32 NJ results, 32 rows at a time through LDS ------------------------------------------
+// ---- epilogue of a product: a wavefront's 32 MI x 32 NJ results, 32 rows at a time through LDS ---------------------------------
 // acc[i][j]: token block i, channel block j; a lane holds token lane & 31 and channels 8 g + 4 (lane >> 5) + 0..3 of each.
-template <bool GATE, int MI, int NJ>
-struct Epilogue {
-  static constexpr int COLS = 32 * NJ;
-  static constexpr int PITCH = COLS + 4;                  // of a staged row, in words
-  static constexpr int BYTES = 32 * PITCH * 4;            // of LDS, for each wavefront
-  static constexpr int CPL = GATE ? 4 : 8;                // columns of a lane: 16 bytes of fp32 or of bf16
-  static constexpr int LPR = COLS / CPL, RPP = 64 / LPR, PASSES = 32 / RPP;
+template <int MI, int NJ>
+struct Output {
+  static constexpr int COLS = 32 * NJ, PITCH = COLS + 4;       // of a staged row, in words
+  static constexpr int BYTES = 32 * PITCH * 4;                 // of LDS, for each wavefront
+  static constexpr int LPR = COLS / 8, RPP = 64 / LPR, PASSES = 32 / RPP;   // 8 columns a lane
 
   static __device__ __forceinline__ void run(const QuantGemmArgs& p, const i32x16_t (&acc)[MI][NJ], char* stg, int m0, int n0, int lane) {
     int* const st = reinterpret_cast<int*>(stg);
-    const int srow = lane / LPR, scol = (lane % LPR) * CPL, n = n0 + scol;
-    const bool whole = p.N % 8 == 0;                      // rows of y and h are 16-byte aligned
-    float sb[CPL];
+    if (m0 >= p.M || n0 >= p.N) return;
+    const int srow = lane / LPR, scol = (lane % LPR) * 8, n = n0 + scol;
+    const bool whole = p.N % 8 == 0;                           // rows of y are 16-byte aligned
+    float sb[8], sa_row[MI];
 #pragma unroll
-    for (int q = 0; q < CPL; ++q) sb[q] = n + q < p.N ? p.scale_b[n + q] : 0.f;
+    for (int q = 0; q < 8; ++q) sb[q] = n + q < p.N ? p.scale_b[n + q] : 0.f;
+#pragma unroll
+    for (int i = 0; i < MI; ++i) sa_row[i] = p.scale_a[m0 + i * 32 + (lane & 31) < p.M ? m0 + i * 32 + (lane & 31) : p.M - 1];
+    // A lane outside the matrix is given an offset beyond the buffer: its loads read zero and its stores are dropped.
+    const int rows = p.M - m0 < 32 * MI ? p.M - m0 : 32 * MI;
+    const rsrc_t ry = resource(p.y + (size_t)m0 * p.N, rows * p.N * 2);
+    const rsrc_t rr = resource(p.residual ? p.residual + (size_t)m0 * p.N : nullptr, p.residual ? rows * p.N * 2 : 0);
 #pragma unroll
     for (int i = 0; i < MI; ++i) {
-      const int mi = m0 + i * 32;
-      if (mi >= p.M) break;
+      uint32_t off[PASSES];
+      u32x4_t res[PASSES];
+      if (whole) {
+#pragma unroll
+        for (int pass = 0; pass < PASSES; ++pass) {
+          const int r = i * 32 + pass * RPP + srow;
+          off[pass] = n < p.N && r < rows ? (uint32_t)(r * p.N + n) * 2u : OOB;
+          if (p.residual) res[pass] = __builtin_amdgcn_raw_buffer_load_b128(rr, off[pass], 0, 0);
+        }
+      }
 #pragma unroll
       for (int j = 0; j < NJ; ++j)
 #pragma unroll
@@ -92,68 +105,36 @@ struct Epilogue {
           const i32x4_t w = {acc[i][j][4 * g], acc[i][j][4 * g + 1], acc[i][j][4 * g + 2], acc[i][j][4 * g + 3]};
           *reinterpret_cast<i32x4_t*>(st + (lane & 31) * PITCH + j * 32 + g * 8 + (lane >> 5) * 4) = w;
         }
-      // scale, and for the gate product the table row, of the row that lane & 31 names
-      const int mr = mi + (lane & 31) < p.M ? mi + (lane & 31) : p.M - 1;
-      const float sa_row = p.scale_a[mr];
-      int id_row = 0;
-      if (GATE) {
-        id_row = p.ids[mr];
-        if ((unsigned)id_row >= (unsigned)p.E_rows) {
-          *p.flag = 1;
-          id_row = id_row < 0 ? 0 : p.E_rows - 1;
-        }
-      }
       __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
       __builtin_amdgcn_wave_barrier();
       __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
-      if (GATE || whole) {
+      if (whole) {
 #pragma unroll
         for (int pass = 0; pass < PASSES; ++pass) {
-          const int r = pass * RPP + srow, m = mi + r;
-          const float sa = __shfl(sa_row, r);
-          const int id = GATE ? __shfl(id_row, r) : 0;
-          if (m >= p.M || n >= p.N) continue;
+          const int r = pass * RPP + srow;
+          const float sa = __shfl(sa_row[i], r);
           const int* const src = st + r * PITCH + scol;
-          float z[CPL];
+          const i32x4_t c0 = *reinterpret_cast<const i32x4_t*>(src), c1 = *reinterpret_cast<const i32x4_t*>(src + 4);
+          bf16x8_t o;
 #pragma unroll
-          for (int h = 0; h < CPL; h += 4) {
-            const i32x4_t c = *reinterpret_cast<const i32x4_t*>(src + h);
-#pragma unroll
-            for (int q = 0; q < 4; ++q) z[h + q] = (float)c[q] * (sa * sb[h + q]);
+          for (int q = 0; q < 8; ++q) {
+            float z = (float)(q < 4 ? c0[q & 3] : c1[q & 3]) * (sa * sb[q]);
+            if (p.residual) z += __uint_as_float(q & 1 ? res[pass][q >> 1] & 0xffff0000u : res[pass][q >> 1] << 16);
+            o[q] = (__bf16)z;
           }
-          const size_t at = (size_t)m * p.N + n;
-          if constexpr (GATE) {
-            const u32x2_t e = *reinterpret_cast<const u32x2_t*>(p.E + (size_t)id * p.N + n);
-            const float u[4] = {__uint_as_float(e[0] << 16), __uint_as_float(e[0] & 0xffff0000u), __uint_as_float(e[1] << 16),
-                                __uint_as_float(e[1] & 0xffff0000u)};
-            f32x4_t o;
-#pragma unroll
-            for (int q = 0; q < 4; ++q) o[q] = z[q] * sigmoidf_fast(z[q]) * u[q];
-            *reinterpret_cast<f32x4_t*>(p.h + at) = o;
-          } else {
-            bf16x8_t o;
-            if (p.residual) {
-              const bf16x8_t rz = *reinterpret_cast<const bf16x8_t*>(p.residual + at);
-#pragma unroll
-              for (int q = 0; q < 8; ++q) z[q] += (float)rz[q];
-            }
-#pragma unroll
-            for (int q = 0; q < 8; ++q) o[q] = (__bf16)z[q];
-            *reinterpret_cast<bf16x8_t*>(p.y + at) = o;
-          }
+          __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4_t, o), ry, off[pass], 0, 0);
         }
       } else {
         // rows of y at any 2-byte address: neighbouring lanes have neighbouring columns
         for (int r = 0; r < 32; ++r) {
-          const float sa = __shfl(sa_row, r);
-          const int m = mi + r;
-          if (m >= p.M) break;
+          const float sa = __shfl(sa_row[i], r);
+          if (i * 32 + r >= rows) break;
 #pragma unroll
           for (int c = 0; c < COLS; c += 64) {
             const int col = c + lane;
             if (col >= COLS || n0 + col >= p.N) continue;
             float z = (float)st[r * PITCH + col] * (sa * p.scale_b[n0 + col]);
-            const size_t at = (size_t)m * p.N + n0 + col;
+            const size_t at = (size_t)(m0 + i * 32 + r) * p.N + n0 + col;
             if (p.residual) z += __uint_as_float((uint32_t)p.residual[at] << 16);
             reinterpret_cast<__bf16*>(p.y)[at] = (__bf16)z;
           }
@@ -166,6 +147,165 @@ struct Epilogue {
   }
 };
 
+// ---- epilogue of the gate product: hidden values SiLU(z) * E[ids], as 8-bit integers -------------------------------------------------
+// A token's scale is the largest of all its hidden values, which lie in as many workgroups as there are tiles of d_ff.  These exchange
+// their maxima and then quantise what they still hold in registers: the hidden values never reach memory otherwise.  (Stored in fp32 and
+// quantised by another kernel they are 9 bytes of traffic each instead of 1; rounded to bf16 on the way, one integer in a hundred differs.)
+//
+// The lanes' own layout is kept throughout: a lane has one token, so its maximum is over its registers and one other lane, and after a swap
+// of half rows (v_permlane32_swap) the 16 values of a block that are one chunk lie in one lane, in the order of the lanes, so a block of the
+// next product's operand is one store of 1 KB.  The table rows are what moves: they go to LDS as they are gathered, 16 bytes a lane,
+// chunk c of row r at chunk c ^ f(r) so that 16 rows' reads fall into 16 chunk columns.
+//
+// The wait.  Tiles of the same tokens are neighbours in the order of dispatch, so the ones that are waited for run or have run unless other
+// streams' kernels hold the compute units; a workgroup that has looked `polls` times without seeing all of them computes the missing
+// maxima itself, tile by tile, then its own tile again.  Nobody depends on anybody.
+template <int MI, int NJ, int WM, int WN>
+struct Hidden {
+  static constexpr int CH = 4 * NJ;                            // 16-byte chunks of a row of the table, of this wavefront's columns
+  static constexpr int E_BYTES = 32 * MI * CH * 16;            // of LDS, for each wavefront
+  static constexpr int TM = 32 * MI * WM;
+  static constexpr int MAX_BYTES = WN * TM * 4 + 16;           // and for the workgroup
+  static __device__ __forceinline__ int swz(int r) { return NJ == 4 ? r & 15 : NJ == 2 ? r >> 1 & 7 : r >> 2 & 3; }
+
+  static __device__ __forceinline__ void fetch_rows(const QuantGemmArgs& p, const int (&row_id)[(MI + 1) / 2], char* lds, int n0, int lane) {
+#pragma unroll
+    for (int q = 0; q < MI * CH / 2; ++q) {
+      const int r = q * (64 / CH) + lane / CH, col = n0 + ((lane % CH) ^ swz(r)) * 8;
+      const int id = __builtin_amdgcn_ds_bpermute((r & 63) * 4, row_id[(q * (64 / CH)) >> 6]);
+      const bf16_t* const at = p.E + (size_t)id * p.N + (col < p.N ? col : 0);
+      __builtin_amdgcn_global_load_lds(const_cast<bf16_t*>(at), (lds_ptr_t)(lds + q * 1024), 16, 0, 0);
+    }
+  }
+  // acc: sums -> hidden values (fp32 bits); top: the largest magnitude's bits of this lane's token in each block
+  static __device__ __forceinline__ void values(const QuantGemmArgs& p, i32x16_t (&acc)[MI][NJ], uint32_t (&top)[MI], const float (&sa)[MI],
+                                                const char* lds, int n0, int lane) {
+#pragma unroll
+    for (int i = 0; i < MI; ++i) top[i] = 0;
+#pragma unroll
+    for (int j = 0; j < NJ; ++j) {
+      const int n = n0 + 32 * j;
+      if (n >= p.N) {                                          // (d_ff is whole blocks)
+#pragma unroll
+        for (int i = 0; i < MI; ++i) acc[i][j] = i32x16_t{};
+        continue;
+      }
+#pragma unroll
+      for (int g = 0; g < 4; ++g) {
+        const f32x4_t sb = *reinterpret_cast<const f32x4_t*>(p.scale_b + n + 8 * g + 4 * (lane >> 5));
+#pragma unroll
+        for (int i = 0; i < MI; ++i) {
+          const int m = i * 32 + (lane & 31);
+          const u32x2_t e = *reinterpret_cast<const u32x2_t*>(lds + m * (CH * 16) + (((4 * j + g) ^ swz(m)) << 4) + (lane >> 5) * 8);
+          const float u[4] = {__uint_as_float(e[0] << 16), __uint_as_float(e[0] & 0xffff0000u), __uint_as_float(e[1] << 16),
+                              __uint_as_float(e[1] & 0xffff0000u)};
+#pragma unroll
+          for (int q = 0; q < 4; ++q) {
+            const float z = (float)acc[i][j][4 * g + q] * (sa[i] * sb[q]), h = z * sigmoidf_fast(z) * u[q];
+            acc[i][j][4 * g + q] = __float_as_int(h);
+            top[i] = max(top[i], __float_as_uint(h) & 0x7fffffffu);
+          }
+        }
+        __builtin_amdgcn_sched_barrier(0);                     // (all steps' reads at once would not fit the registers)
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < MI; ++i) top[i] = max(top[i], (uint32_t)__shfl_xor((int)top[i], 32));
+  }
+  // the integers of a row whose largest magnitude has the bits `top`
+  static __device__ __forceinline__ void store(const QuantGemmArgs& p, const i32x16_t (&acc)[MI][NJ], int m0, int n0, bool first, int lane) {
+    const int pitch = (p.N + 127) / 128 * 128;
+#pragma unroll
+    for (int i = 0; i < MI; ++i) {
+      const int mb = m0 + 32 * i, m = mb + (lane & 31);
+      if (mb >= p.M) break;
+      const uint32_t top = __hip_atomic_load(p.amax + (m < p.M ? m : p.M - 1), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      const bool finite = top < 0x7f800000u;
+      const float s = fmaxf(__uint_as_float(top) / 127.0f, 0x1p-126f), inv = finite ? 1.0f / s : 0.f;
+      if (first && lane < 32 && m < p.M) p.scale_h[m] = finite ? s : __uint_as_float(0x7fc00000u);
+      int8_t* const out = p.hq + (size_t)mb * pitch + (n0 >> 5) * 1024 + lane * 16;
+#pragma unroll
+      for (int j = 0; j < NJ; ++j) {
+        if (n0 + 32 * j >= pitch) continue;
+        uint32_t w[4];
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+          // |h inv| is at most 127 and a rounding: next to 1.5 x 2^23 a float's last digit is 1, and the low byte the integer's
+          uint32_t b[4];
+#pragma unroll
+          for (int q = 0; q < 4; ++q) b[q] = __float_as_uint(__builtin_fmaf(__int_as_float(acc[i][j][4 * g + q]), inv, 12582912.f));
+          w[g] = __builtin_amdgcn_perm(__builtin_amdgcn_perm(b[3], b[2], 0x0c0c0400), __builtin_amdgcn_perm(b[1], b[0], 0x0c0c0400), 0x05040100);
+        }
+        const u32x2_t lo = __builtin_amdgcn_permlane32_swap(w[0], w[2], false, false);
+        const u32x2_t hi = __builtin_amdgcn_permlane32_swap(w[1], w[3], false, false);
+        *reinterpret_cast<u32x4_t*>(out + j * 1024) = u32x4_t{lo[0], lo[1], hi[0], hi[1]};
+      }
+    }
+  }
+  // What a workgroup does next: -1 its values can be quantised, else a column of tiles whose maxima it has to compute (its own: the last).
+  // By all threads; `at` is the column just computed, `own` this workgroup's.  max_lds: [WN][TM] maxima and a word.
+  static __device__ __forceinline__ int exchange(const QuantGemmArgs& p, uint32_t* max_lds, int tm, int at, int own, int ntn) {
+    const int tid = threadIdx.x;
+    uint32_t* const counter = p.panels + tm;
+    uint32_t* const flags = p.panels + (p.M + TM - 1) / TM + (size_t)tm * ntn;
+    int* const verdict = reinterpret_cast<int*>(max_lds + WN * TM);
+    __syncthreads();
+    if (tid < TM && tm * TM + tid < p.M) {
+      uint32_t v = max_lds[tid];
+#pragma unroll
+      for (int w = 1; w < WN; ++w) v = max(v, max_lds[w * TM + tid]);
+      __hip_atomic_fetch_max(p.amax + tm * TM + tid, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    }
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();
+    if (tid == 0) {
+      int next = own, from = 0;
+      if (at == own) {
+        __hip_atomic_store(flags + own, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        bool all = __hip_atomic_fetch_add(counter, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) + 1 == (uint32_t)ntn;
+        for (int i = 0; i < p.polls && !all; ++i) {
+          __builtin_amdgcn_s_sleep(1);
+          all = __hip_atomic_load(counter, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == (uint32_t)ntn;
+        }
+        if (all) next = -1;
+      } else {
+        from = at + 1;
+      }
+      if (next >= 0)
+        for (; from < ntn; ++from)
+          if (from != own && !__hip_atomic_load(flags + from, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT)) { next = from; break; }
+      *verdict = next;
+    }
+    __syncthreads();
+    return __builtin_amdgcn_readfirstlane(*verdict);
+  }
+};
+
+// Workgroup -> tile of the gate product: all of a row of tiles before the next, and with more than 8 in a row each XCD the same columns of
+// every row (ntn8 of them, the rest empty), which also is 8 token panels by 4 of weights for the 32 workgroups of an XCD.
+__device__ __forceinline__ int row_of_tiles(int ntn) { return ntn > 8 ? (ntn + 7) & ~7 : ntn; }
+
+// Scales of a wavefront's tokens, lane & 31 of each block of 32, and the ids of their table rows, lane l having rows l and 64 + l
+template <int MI, bool GATE>
+struct Rows {
+  float scale[MI];
+  int id[(MI + 1) / 2];
+  __device__ __forceinline__ void init(const QuantGemmArgs& p, int m0, int lane) {
+#pragma unroll
+    for (int i = 0; i < MI; ++i) scale[i] = p.scale_a[min(m0 + i * 32 + (lane & 31), p.M - 1)];
+#pragma unroll
+    for (int h = 0; h < (MI + 1) / 2; ++h) {
+      int v = p.ids[min(m0 + h * 64 + lane, p.M - 1)];
+      if ((unsigned)v >= (unsigned)p.E_rows) {   // reported to the host, clamped so no access leaves the table
+        *p.flag = 1;
+        v = v < 0 ? 0 : p.E_rows - 1;
+      }
+      id[h] = v;
+    }
+  }
+};
+
 // ---- 256 x 256 ----------------------------------------------------------------------------------------------------------------
 constexpr int SLOT = 32768;   // an operand tile: 256 rows x 128 k
 
@@ -174,9 +314,21 @@ __global__ __launch_bounds__(256) void gemm_int8_256_kernel(QuantGemmArgs p) {
   __shared__ __attribute__((aligned(16))) char smem[5 * SLOT];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wm = wave >> 1, wn = wave & 1;
-  int tm, tn;
-  tile_of(blockIdx.x, gridDim.x, (p.M + 255) / 256, (p.N + 255) / 256, tm, tn);
-  const int m0 = tm * 256, n0 = tn * 256;
+  const int ntn = (p.N + 255) / 256;
+  int tm, own;
+  if (GATE) {
+    tm = blockIdx.x / row_of_tiles(ntn);
+    own = blockIdx.x % row_of_tiles(ntn);
+    if (own >= ntn) return;
+  } else {
+    tile_of(blockIdx.x, gridDim.x, (p.M + 255) / 256, ntn, tm, own);
+  }
+  const int m0 = tm * 256;
+  typedef Hidden<4, 4, 2, 2> Hid;
+  Rows<4, GATE> rows;
+  if (GATE) rows.init(p, m0 + wm * 128, lane);
+  for (int tn = own, last = 0;;) {
+  const int n0 = tn * 256;
   Loader<256, 4> la, lb;
   la.init(p.A, p.M, p.K, m0, wave, lane);
   lb.init(p.B, p.N, p.K, n0, wave, lane);
@@ -281,9 +433,35 @@ __global__ __launch_bounds__(256) void gemm_int8_256_kernel(QuantGemmArgs p) {
   if (kt + 3 < nk) ring_iteration(3);
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
   __syncthreads();
-  typedef Epilogue<GATE, 4, 4> Out;
-  static_assert(4 * Out::BYTES <= 5 * SLOT, "staging");
-  Out::run(p, acc, smem + wave * Out::BYTES, m0 + wm * 128, n0 + wn * 128, lane);
+  if constexpr (!GATE) {
+    typedef Output<4, 4> Out;
+    static_assert(4 * Out::BYTES <= 5 * SLOT, "staging");
+    Out::run(p, acc, smem + wave * Out::BYTES, m0 + wm * 128, n0 + wn * 128, lane);
+    return;
+  } else {
+    static_assert(4 * Hid::E_BYTES + Hid::MAX_BYTES <= 5 * SLOT, "room for the rows of the table");
+    char* const lds = smem + wave * Hid::E_BYTES;
+    uint32_t* const max_lds = reinterpret_cast<uint32_t*>(smem + 4 * Hid::E_BYTES);
+    uint32_t top[4];
+    Hid::fetch_rows(p, rows.id, lds, n0 + wn * 128, lane);
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    Hid::values(p, acc, top, rows.scale, lds, n0 + wn * 128, lane);
+    if (!last) {
+      if (lane < 32)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) max_lds[wn * 256 + wm * 128 + i * 32 + lane] = top[i];
+      const int next = Hid::exchange(p, max_lds, tm, tn, own, ntn);
+      if (next >= 0) {
+        last = next == own;
+        tn = next;
+        __syncthreads();
+        continue;
+      }
+    }
+    Hid::store(p, acc, m0 + wm * 128, own * 256 + wn * 128, own == 0 && wn == 0, lane);
+    return;
+  }
+  }
 }
 
 // ---- smaller tiles: STAGES whole K tiles in LDS, filled by LW wavefronts of their own ---------------------------------------------
@@ -297,16 +475,30 @@ struct Tiling {
 template <bool GATE, class C>
 __global__ __launch_bounds__((C::WAVES + C::LW) * 64) void gemm_int8_kernel(QuantGemmArgs p) {
   constexpr int MI = C::MI, NJ = C::NJ, S = C::STAGES, STAGE = C::STAGE;
-  typedef Epilogue<GATE, MI, NJ> Out;
-  constexpr int LDS = S * STAGE > C::WAVES * Out::BYTES ? S * STAGE : C::WAVES * Out::BYTES;
+  typedef Output<MI, NJ> Out;
+  typedef Hidden<MI, NJ, C::WM, C::WN> Hid;
+  constexpr int EPI = GATE ? C::WAVES * Hid::E_BYTES + Hid::MAX_BYTES : C::WAVES * Out::BYTES;
+  constexpr int LDS = S * STAGE > EPI ? S * STAGE : EPI;
   __shared__ __attribute__((aligned(16))) char smem[LDS];
   const int lane = threadIdx.x & 63, wave_id = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const bool load_wave = wave_id >= C::WAVES;
   const int wave = load_wave ? wave_id - C::WAVES : wave_id, wm = wave / C::WN, wn = wave % C::WN;
-  int tm, tn;
-  tile_of(blockIdx.x, gridDim.x, (p.M + C::TM - 1) / C::TM, (p.N + C::TN - 1) / C::TN, tm, tn);
-  const int m0 = tm * C::TM, n0 = tn * C::TN;
+  const int ntn = (p.N + C::TN - 1) / C::TN;
+  int tm, own;
+  if (GATE) {
+    tm = blockIdx.x / row_of_tiles(ntn);
+    own = blockIdx.x % row_of_tiles(ntn);
+    if (own >= ntn) return;
+  } else {
+    tile_of(blockIdx.x, gridDim.x, (p.M + C::TM - 1) / C::TM, ntn, tm, own);
+  }
+  const int m0 = tm * C::TM;
   const int nk = p.K / 128, kbytes = nk * 4096;
+  uint32_t* const max_lds = reinterpret_cast<uint32_t*>(smem + C::WAVES * Hid::E_BYTES);
+  Rows<MI, GATE> rows;
+  if (GATE && !load_wave) rows.init(p, m0 + wm * MI * 32, lane);
+  for (int tn = own, last = 0;;) {
+  const int n0 = tn * C::TN;
   if (load_wave) {
     Loader<C::TM, C::LW> la;
     Loader<C::TN, C::LW> lb;
@@ -342,9 +534,15 @@ __global__ __launch_bounds__((C::WAVES + C::LW) * 64) void gemm_int8_kernel(Quan
 #pragma unroll
     for (int st = 0; st < S - 1; ++st)
       if (kt + st < nk) load_iteration(st);
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // nothing lands in LDS once the epilogue stages through it
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // nothing lands in LDS once the epilogue uses it
     __syncthreads();
-    return;
+    if (!GATE || last) return;
+    const int next = Hid::exchange(p, max_lds, tm, tn, own, ntn);
+    if (next < 0) return;
+    last = next == own;
+    tn = next;
+    __syncthreads();
+    continue;
   }
   i32x16_t acc[MI][NJ];
 #pragma unroll
@@ -392,7 +590,31 @@ __global__ __launch_bounds__((C::WAVES + C::LW) * 64) void gemm_int8_kernel(Quan
   for (int st = 0; st < S - 1; ++st)
     if (kt + st < nk) stage_iteration(st);
   __syncthreads();
-  Out::run(p, acc, smem + wave * Out::BYTES, m0 + wm * MI * 32, n0 + wn * NJ * 32, lane);
+  if constexpr (!GATE) {
+    Out::run(p, acc, smem + wave * Out::BYTES, m0 + wm * MI * 32, n0 + wn * NJ * 32, lane);
+    return;
+  } else {
+    char* const lds = smem + wave * Hid::E_BYTES;
+    uint32_t top[MI];
+    Hid::fetch_rows(p, rows.id, lds, n0 + wn * NJ * 32, lane);
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    Hid::values(p, acc, top, rows.scale, lds, n0 + wn * NJ * 32, lane);
+    if (!last) {
+      if (lane < 32)
+#pragma unroll
+        for (int i = 0; i < MI; ++i) max_lds[wn * C::TM + (wm * MI + i) * 32 + lane] = top[i];
+      const int next = Hid::exchange(p, max_lds, tm, tn, own, ntn);
+      if (next >= 0) {
+        last = next == own;
+        tn = next;
+        __syncthreads();
+        continue;
+      }
+    }
+    Hid::store(p, acc, m0 + wm * MI * 32, own * C::TN + wn * NJ * 32, own == 0 && wn == 0, lane);
+    return;
+  }
+  }
 }
 
 typedef Tiling<2, 2, 2, 2, 4, 4> Tile128;       // 128 x 128, 128 KB of LDS
@@ -400,9 +622,9 @@ typedef Tiling<2, 1, 2, 2, 6, 4> Tile128x64;    // 144 KB
 
 template <class C>
 hipError_t launch(const QuantGemmArgs& a, hipStream_t s) {
-  const int grid = ((a.M + C::TM - 1) / C::TM) * ((a.N + C::TN - 1) / C::TN);
-  if (a.y) gemm_int8_kernel<false, C><<<grid, (C::WAVES + C::LW) * 64, 0, s>>>(a);
-  else gemm_int8_kernel<true, C><<<grid, (C::WAVES + C::LW) * 64, 0, s>>>(a);
+  const int ntm = (a.M + C::TM - 1) / C::TM, ntn = (a.N + C::TN - 1) / C::TN;
+  if (a.y) gemm_int8_kernel<false, C><<<ntm * ntn, (C::WAVES + C::LW) * 64, 0, s>>>(a);
+  else gemm_int8_kernel<true, C><<<ntm * (ntn > 8 ? (ntn + 7) & ~7 : ntn), (C::WAVES + C::LW) * 64, 0, s>>>(a);
   return hipGetLastError();
 }
 
@@ -410,10 +632,10 @@ hipError_t launch(const QuantGemmArgs& a, hipStream_t s) {
 
 hipError_t stem_quant_gemm_launch(stem_ctx* ctx, int kid, const QuantGemmArgs& a, hipStream_t s) {
   ProfScope prof(ctx, kid, s);
-  const int t256 = ((a.M + 255) / 256) * ((a.N + 255) / 256), t128 = ((a.M + 127) / 128) * ((a.N + 127) / 128);
-  if (t256 >= 192) {
-    if (a.y) gemm_int8_256_kernel<false><<<t256, 256, 0, s>>>(a);
-    else gemm_int8_256_kernel<true><<<t256, 256, 0, s>>>(a);
+  const int ntm = (a.M + 255) / 256, ntn = (a.N + 255) / 256, t128 = ((a.M + 127) / 128) * ((a.N + 127) / 128);
+  if (ntm * ntn >= 192) {
+    if (a.y) gemm_int8_256_kernel<false><<<ntm * ntn, 256, 0, s>>>(a);
+    else gemm_int8_256_kernel<true><<<ntm * (ntn > 8 ? (ntn + 7) & ~7 : ntn), 256, 0, s>>>(a);
     return hipGetLastError();
   }
   return t128 >= 192 ? launch<Tile128>(a, s) : launch<Tile128x64>(a, s);

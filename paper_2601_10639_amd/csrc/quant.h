@@ -7,29 +7,35 @@
 #pragma once
 #include "stem_internal.h"
 
-#define STEM_QUANT_CHUNK 4096   // tokens whose hidden values a layer call has in fp32 at a time
-
 inline int64_t stem_quant_pitch(int64_t K) { return (K + 127) / 128 * 128; }
 inline int64_t stem_quant_size(int64_t rows, int64_t K) { return (rows + 31) / 32 * 32 * stem_quant_pitch(K); }
+// Words that the tiles of a gate product exchange: the largest magnitude of each token's hidden values, how many tiles of a row of tiles
+// are done, and which (tiles of at least 128 tokens x 64 channels).
+inline int64_t stem_quant_words(int64_t T, int64_t F) { return T + (T + 127) / 128 * (1 + (F + 63) / 64); }
 
 struct QuantRowsArgs {
-  const void* x;       // [rows, K], bf16 or fp32
+  const bf16_t* x;     // [rows, K]
   int64_t rows;
   int K;
   int pad_rows;        // write zeros for the rows that fill the last block
   stem_norm norm;      // of a row, before it is quantised (bf16 weight)
   int8_t* q;
   float* scale;        // [rows]
+  uint32_t* clear;     // set to zero besides; may be null
+  int64_t clear_words;
 };
-hipError_t stem_quant_rows_launch(stem_ctx* ctx, int kid, int is_bf16, const QuantRowsArgs& a, hipStream_t s);
+hipError_t stem_quant_rows_launch(stem_ctx* ctx, int kid, const QuantRowsArgs& a, hipStream_t s);
 
 struct QuantGemmArgs {
   const int8_t *A, *B;              // tokens [M, K] and weights [N, K], in the layout above
   const float *scale_a, *scale_b;
   int M, N, K;                      // K: padded
-  bf16_t* y;                        // [M, N], or null:
+  bf16_t* y;                        // [M, N], or null: a gate product
   const bf16_t* residual;           // [M, N], may be null
-  float* h;                         // [M, N] = SiLU(product) * E[ids]
+  int8_t* hq;                       // SiLU(product) * E[ids] as the tokens of the next product, [M, N] in the layout above
+  float* scale_h;
+  uint32_t *amax, *panels;          // stem_quant_words, zero: M maxima, and the rest
+  int polls;                        // how often a tile looks for the others
   const int32_t* ids;
   const bf16_t* E;
   int E_rows;

@@ -28,20 +28,6 @@ __device__ __forceinline__ void load16(const bf16_t* p, int left, float (&v)[16]
     }
   }
 }
-template <bool VEC>
-__device__ __forceinline__ void load16(const float* p, int left, float (&v)[16]) {
-#pragma unroll
-  for (int h = 0; h < 4; ++h) {
-    if (VEC) {
-      const float4 u = left > 4 * h ? *reinterpret_cast<const float4*>(p + 4 * h) : make_float4(0.f, 0.f, 0.f, 0.f);
-      v[4 * h] = u.x; v[4 * h + 1] = u.y; v[4 * h + 2] = u.z; v[4 * h + 3] = u.w;
-    } else {
-#pragma unroll
-      for (int q = 4 * h; q < 4 * h + 4; ++q) v[q] = q < left ? p[q] : 0.f;
-    }
-  }
-}
-
 __device__ __forceinline__ float block_sum(float v, float* red) {
 #pragma unroll
   for (int o = 1; o < 64; o <<= 1) v += __shfl_xor(v, o);
@@ -60,17 +46,19 @@ __device__ __forceinline__ uint32_t block_max(uint32_t v, uint32_t* red) {
 }
 
 // A workgroup has a row.  VPT: chunks of 16 elements a thread holds; 0: the row is longer than that and is read again for each step.
-template <class E, bool VEC, int VPT>
+template <bool VEC, int VPT>
 __global__ __launch_bounds__(256) void quant_rows_kernel(QuantRowsArgs p) {
   __shared__ float red[4];
   __shared__ uint32_t redm[4];
   const int64_t row = blockIdx.x;
   const int chunks = (int)((p.K + 127) / 128 * 8);
   int8_t* const out = p.q + (row >> 5) * 32 * (int64_t)chunks * 16 + (row & 31) * 16;
-  const E* const x = static_cast<const E*>(p.x) + row * p.K;
+  const bf16_t* const x = p.x + row * p.K;
   constexpr int HELD = VPT ? VPT : 1;
   float v[HELD][16];
   const bool live = row < p.rows;
+  if (p.clear)
+    for (int64_t i = row * 256 + threadIdx.x; i < p.clear_words; i += (int64_t)gridDim.x * 256) p.clear[i] = 0;
   const int steps = VPT ? VPT : (chunks + 255) / 256;
   auto fetch = [&](int t, float (&u)[16]) {
     const int c = t * 256 + threadIdx.x;
@@ -150,20 +138,18 @@ __global__ __launch_bounds__(256) void quant_rows_kernel(QuantRowsArgs p) {
   }
 }
 
-template <class E, bool VEC>
+template <bool VEC>
 hipError_t rows(const QuantRowsArgs& a, hipStream_t s) {
   const unsigned grid = (unsigned)(a.pad_rows ? (a.rows + 31) / 32 * 32 : a.rows);
-  if (a.K <= 4096) quant_rows_kernel<E, VEC, 1><<<grid, 256, 0, s>>>(a);
-  else if (a.K <= 8192) quant_rows_kernel<E, VEC, 2><<<grid, 256, 0, s>>>(a);
-  else quant_rows_kernel<E, VEC, 0><<<grid, 256, 0, s>>>(a);
+  if (a.K <= 4096) quant_rows_kernel<VEC, 1><<<grid, 256, 0, s>>>(a);
+  else if (a.K <= 8192) quant_rows_kernel<VEC, 2><<<grid, 256, 0, s>>>(a);
+  else quant_rows_kernel<VEC, 0><<<grid, 256, 0, s>>>(a);
   return hipGetLastError();
 }
 
 }  // namespace
 
-hipError_t stem_quant_rows_launch(stem_ctx* ctx, int kid, int is_bf16, const QuantRowsArgs& a, hipStream_t s) {
+hipError_t stem_quant_rows_launch(stem_ctx* ctx, int kid, const QuantRowsArgs& a, hipStream_t s) {
   ProfScope prof(ctx, kid, s);
-  const bool vec = a.K % 8 == 0;
-  if (is_bf16) return vec ? rows<bf16_t, true>(a, s) : rows<bf16_t, false>(a, s);
-  return vec ? rows<float, true>(a, s) : rows<float, false>(a, s);
+  return a.K % 8 == 0 ? rows<true>(a, s) : rows<false>(a, s);
 }

@@ -41,8 +41,7 @@ enum StemKernelId {
   K_DROPOUT,
   K_QUANT_WEIGHTS,   // bf16 weights to 8-bit integers
   K_QUANT_ROWS,      // (normed) activations to 8-bit integers
-  K_QUANT_HIDDEN,    // hidden values to 8-bit integers
-  K_QUANT_GATE,      // 8-bit gate product with SiLU*gather
+  K_QUANT_GATE,      // 8-bit gate product with SiLU*gather, as 8-bit integers
   K_QUANT_DOWN,      // 8-bit product
   K_COUNT_
 };
@@ -122,9 +121,9 @@ struct stem_ctx {
   float* block_part;
 
   // 8-bit products (STEM_RESERVE_QUANT)
-  int8_t *quant_x, *quant_h;      // rows of a call; hidden values of STEM_QUANT_CHUNK tokens
+  int8_t *quant_x, *quant_h;      // rows of a call; their hidden values
   float *quant_sx, *quant_sh;     // their scales
-  float* quant_hidden;            // those hidden values in fp32
+  uint32_t* quant_sync;           // what the gate product's tiles exchange
 
   // profiling
   int prof_on;
