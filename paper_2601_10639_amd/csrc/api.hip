@@ -25,7 +25,7 @@ const char* const kKernelNames[K_COUNT_] = {
     "splitk_reduce",   "gemm_up",      "gemm_dw_up",   "sort_merge",
     "grads_f32", "gemm_dw", "list_copy", "ffn_decode",
     "block_enter", "block_enter_back", "block_leave", "block_leave_back", "dropout",
-    "quant_weights", "quant_rows", "quant_gate", "quant_down"};
+    "quant_weights", "quant_rows", "quant_gate", "quant_hidden", "quant_down"};
 
 #define fail stem_fail
 
@@ -167,7 +167,7 @@ void release(stem_ctx* c) {
   free(c->cache_id_in_slot); free(c->cache_slot_of); free(c->cache_freq);
   (void)hipFree(c->edit_idx_dev); (void)hipFree(c->edit_rep_dev);
   (void)hipFree(c->block_part);
-  (void)hipFree(c->quant_x); (void)hipFree(c->quant_h); (void)hipFree(c->quant_sx); (void)hipFree(c->quant_sh); (void)hipFree(c->quant_sync);
+  (void)hipFree(c->quant_x); (void)hipFree(c->quant_h); (void)hipFree(c->quant_sx); (void)hipFree(c->quant_sh); (void)hipFree(c->quant_amax); (void)hipFree(c->quant_hidden);
   if (c->inst_pinned) (void)hipHostFree(c->inst_pinned);
   (void)hipFree(c->inst_dev);
   if (c->side) copy_streams_put(c->device);
@@ -381,7 +381,7 @@ stem_status stem_reserve(stem_ctx* c, uint32_t what) {
     HIP_TRY(c, hipMalloc(reinterpret_cast<void**>(&c->edit_idx_dev), 3 * STEM_EDIT_MAX_TOKENS * sizeof(int32_t)));
     HIP_TRY(c, hipMalloc(&c->edit_rep_dev, (size_t)STEM_EDIT_MAX_TOKENS * c->desc.d_ff * esize(c)));
   }
-  if ((what & STEM_RESERVE_QUANT) && !c->quant_sync) {
+  if ((what & STEM_RESERVE_QUANT) && !c->quant_hidden) {
     if (c->desc.dtype != STEM_BF16) return fail(c, STEM_ERR_UNSUPPORTED, "stem_reserve: STEM_RESERVE_QUANT needs a bf16 context");
     const int64_t T = std::max<int64_t>(c->max_tokens, 1), F = c->desc.d_ff;
     // (the one that says that all are there comes last)
@@ -389,7 +389,8 @@ stem_status stem_reserve(stem_ctx* c, uint32_t what) {
     if (!c->quant_h) HIP_TRY(c, dmalloc(&c->quant_h, (size_t)stem_quant_size(T, F)));
     if (!c->quant_sx) HIP_TRY(c, dmalloc(&c->quant_sx, (size_t)T));
     if (!c->quant_sh) HIP_TRY(c, dmalloc(&c->quant_sh, (size_t)T));
-    HIP_TRY(c, dmalloc(&c->quant_sync, (size_t)stem_quant_words(T, F)));
+    if (!c->quant_amax) HIP_TRY(c, dmalloc(&c->quant_amax, (size_t)T));
+    HIP_TRY(c, dmalloc(&c->quant_hidden, (size_t)((std::min(T, stem_quant_chunk(F)) + 31) / 32 * 32 * stem_quant_pitch(F))));
   }
   return STEM_OK;
 }

@@ -99,7 +99,7 @@ size_t gate_bytes(const stem_ctx* c, int kind, int64_t T, size_t es) {
 
 stem_status check_quant(stem_ctx* c, const char* who) {
   if (c->desc.dtype != STEM_BF16) return stem_fail(c, STEM_ERR_UNSUPPORTED, "%s: needs a bf16 context", who);
-  if (!c->quant_sync) return stem_fail(c, STEM_ERR_WORKSPACE, "%s: needs stem_reserve(ctx, STEM_RESERVE_QUANT)", who);
+  if (!c->quant_hidden) return stem_fail(c, STEM_ERR_WORKSPACE, "%s: needs stem_reserve(ctx, STEM_RESERVE_QUANT)", who);
   return STEM_OK;
 }
 
@@ -278,14 +278,20 @@ stem_status stem_quant_ffn_forward(stem_ctx* c, const void* x, const int32_t* id
   if (reinterpret_cast<uintptr_t>(ids) & 3u) return stem_fail(c, STEM_ERR_INVALID_ARG, "%s: ids must be 4-byte aligned", who);
   if (overlap({ids, (size_t)T * 4}, {y, xb})) return stem_fail(c, STEM_ERR_INVALID_ARG, "%s: an output lies over an input", who);
   hipStream_t s = static_cast<hipStream_t>(stream);
-  HIP_TRY(c, quant_rows(c, K_QUANT_ROWS, x, T, d, norm, false, c->quant_x, c->quant_sx, c->quant_sync, stem_quant_words(T, F), s));
-  QuantGemmArgs g = {};
-  g.A = c->quant_x; g.scale_a = c->quant_sx;
-  g.B = static_cast<const int8_t*>(gate_q); g.scale_b = gate_scale;
-  g.M = (int)T; g.N = (int)F; g.K = (int)stem_quant_pitch(d);
-  g.hq = c->quant_h; g.scale_h = c->quant_sh; g.amax = c->quant_sync; g.panels = c->quant_sync + T; g.polls = c->polls;
-  g.ids = ids; g.E = static_cast<const bf16_t*>(E); g.E_rows = (int)E_rows; g.flag = c->flag;
-  HIP_TRY(c, stem_quant_gemm_launch(c, K_QUANT_GATE, g, s));
+  HIP_TRY(c, quant_rows(c, K_QUANT_ROWS, x, T, d, norm, false, c->quant_x, c->quant_sx, c->quant_amax, T, s));
+  const int64_t chunk = stem_quant_chunk(F), pitch = stem_quant_pitch(F);
+  for (int64_t t0 = 0; t0 < T; t0 += chunk) {
+    const int64_t n = std::min<int64_t>(chunk, T - t0);
+    QuantGemmArgs g = {};
+    g.A = c->quant_x + t0 * stem_quant_pitch(d); g.scale_a = c->quant_sx + t0;
+    g.B = static_cast<const int8_t*>(gate_q); g.scale_b = gate_scale;
+    g.M = (int)n; g.N = (int)F; g.K = (int)stem_quant_pitch(d);
+    g.h = c->quant_hidden; g.amax = c->quant_amax + t0;
+    g.ids = ids + t0; g.E = static_cast<const bf16_t*>(E); g.E_rows = (int)E_rows; g.flag = c->flag;
+    HIP_TRY(c, stem_quant_gemm_launch(c, K_QUANT_GATE, g, s));
+    const QuantHiddenArgs q = {c->quant_hidden, c->quant_amax + t0, (int)n, (int)(pitch / 32), c->quant_h + t0 * pitch, c->quant_sh + t0};
+    HIP_TRY(c, stem_quant_hidden_launch(c, q, s));
+  }
   QuantGemmArgs b = {};
   b.A = c->quant_h; b.scale_a = c->quant_sh;
   b.B = static_cast<const int8_t*>(down_q); b.scale_b = down_scale;

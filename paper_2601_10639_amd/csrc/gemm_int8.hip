@@ -147,28 +147,25 @@ struct Output {
   }
 };
 
-// ---- epilogue of the gate product: hidden values SiLU(z) * E[ids], as 8-bit integers -------------------------------------------------
-// A token's scale is the largest of all its hidden values, which lie in as many workgroups as there are tiles of d_ff.  These exchange
-// their maxima and then quantise what they still hold in registers: the hidden values never reach memory otherwise.  (Stored in fp32 and
-// quantised by another kernel they are 9 bytes of traffic each instead of 1; rounded to bf16 on the way, one integer in a hundred differs.)
+// ---- epilogue of the gate product: hidden values SiLU(z) * E[ids] ---------------------------------------------------------------------
+// A token's scale is the largest of all its hidden values, which lie in as many workgroups as there are tiles of d_ff.  So the values are
+// kept in fp32 (rounded to bf16 on the way, one integer in a hundred would be another), in the lanes' own layout, 4 KB a block, and the maxima
+// of the tokens are taken on the way (a maximum of integers, whose order does not matter); quant_hidden_kernel makes integers of them.
+// (Workgroups that wait for the others' maxima and quantise what they hold in registers save that traffic, and wait: 16384 tokens of 2048 x
+// 8192, 525 us, 34 thousand of a workgroup's 114 thousand clocks in the wait; the two kernels take %GATE% and %QUANT%.)
 //
-// The lanes' own layout is kept throughout: a lane has one token, so its maximum is over its registers and one other lane, and after a swap
-// of half rows (v_permlane32_swap) the 16 values of a block that are one chunk lie in one lane, in the order of the lanes, so a block of the
-// next product's operand is one store of 1 KB.  The table rows are what moves: they go to LDS as they are gathered, 16 bytes a lane,
-// chunk c of row r at chunk c ^ f(r) so that 16 rows' reads fall into 16 chunk columns.
-//
-// The wait.  Tiles of the same tokens are neighbours in the order of dispatch, so the ones that are waited for run or have run unless other
-// streams' kernels hold the compute units; a workgroup that has looked `polls` times without seeing all of them computes the missing
-// maxima itself, tile by tile, then its own tile again.  Nobody depends on anybody.
-template <int MI, int NJ, int WM, int WN>
+// The lanes' layout is kept throughout: a lane has one token, so its maximum is over its registers and one other lane's.  The table rows
+// are what moves: they go to LDS as they are gathered, 16 bytes a lane, chunk c of row r at chunk c ^ f(r) so that 16 rows' reads fall into
+// 16 chunk columns.
+template <int MI, int NJ>
 struct Hidden {
   static constexpr int CH = 4 * NJ;                            // 16-byte chunks of a row of the table, of this wavefront's columns
-  static constexpr int E_BYTES = 32 * MI * CH * 16;            // of LDS, for each wavefront
-  static constexpr int TM = 32 * MI * WM;
-  static constexpr int MAX_BYTES = WN * TM * 4 + 16;           // and for the workgroup
+  static constexpr int BYTES = 32 * MI * CH * 16;              // of LDS, for each wavefront
   static __device__ __forceinline__ int swz(int r) { return NJ == 4 ? r & 15 : NJ == 2 ? r >> 1 & 7 : r >> 2 & 3; }
 
-  static __device__ __forceinline__ void fetch_rows(const QuantGemmArgs& p, const int (&row_id)[(MI + 1) / 2], char* lds, int n0, int lane) {
+  static __device__ __forceinline__ void run(const QuantGemmArgs& p, const i32x16_t (&acc)[MI][NJ], const float (&sa)[MI],
+                                             const int (&row_id)[(MI + 1) / 2], char* lds, int m0, int n0, int lane) {
+    if (m0 >= p.M || n0 >= p.N) return;
 #pragma unroll
     for (int q = 0; q < MI * CH / 2; ++q) {
       const int r = q * (64 / CH) + lane / CH, col = n0 + ((lane % CH) ^ swz(r)) * 8;
@@ -176,115 +173,55 @@ struct Hidden {
       const bf16_t* const at = p.E + (size_t)id * p.N + (col < p.N ? col : 0);
       __builtin_amdgcn_global_load_lds(const_cast<bf16_t*>(at), (lds_ptr_t)(lds + q * 1024), 16, 0, 0);
     }
-  }
-  // acc: sums -> hidden values (fp32 bits); top: the largest magnitude's bits of this lane's token in each block
-  static __device__ __forceinline__ void values(const QuantGemmArgs& p, i32x16_t (&acc)[MI][NJ], uint32_t (&top)[MI], const float (&sa)[MI],
-                                                const char* lds, int n0, int lane) {
+    // the columns past d_ff, up to the pitch of the next product's K, become zeros: their sums are
+    const int blocks = (p.N + 127) / 128 * 4;
+    uint32_t top[MI];
 #pragma unroll
     for (int i = 0; i < MI; ++i) top[i] = 0;
+    struct Step { f32x4_t sb; u32x2_t e[MI]; };
+    auto load = [&](int t) __attribute__((always_inline)) {
+      Step s;
+      const int n = n0 + 8 * t + 4 * (lane >> 5);
+      s.sb = *reinterpret_cast<const f32x4_t*>(p.scale_b + (n < p.N ? n : 0));
 #pragma unroll
-    for (int j = 0; j < NJ; ++j) {
-      const int n = n0 + 32 * j;
-      if (n >= p.N) {                                          // (d_ff is whole blocks)
-#pragma unroll
-        for (int i = 0; i < MI; ++i) acc[i][j] = i32x16_t{};
-        continue;
+      for (int i = 0; i < MI; ++i) {
+        const int m = i * 32 + (lane & 31);
+        s.e[i] = *reinterpret_cast<const u32x2_t*>(lds + m * (CH * 16) + ((t ^ swz(m)) << 4) + (lane >> 5) * 8);
       }
+      return s;
+    };
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    Step cur = load(0);
 #pragma unroll
-      for (int g = 0; g < 4; ++g) {
-        const f32x4_t sb = *reinterpret_cast<const f32x4_t*>(p.scale_b + n + 8 * g + 4 * (lane >> 5));
+    for (int t = 0; t < 4 * NJ; ++t) {                         // 8 channels a step
+      const int j = t >> 2, g = t & 3, block = (n0 >> 5) + j;
+      const Step nxt = t + 1 < 4 * NJ ? load(t + 1) : cur;
 #pragma unroll
-        for (int i = 0; i < MI; ++i) {
-          const int m = i * 32 + (lane & 31);
-          const u32x2_t e = *reinterpret_cast<const u32x2_t*>(lds + m * (CH * 16) + (((4 * j + g) ^ swz(m)) << 4) + (lane >> 5) * 8);
-          const float u[4] = {__uint_as_float(e[0] << 16), __uint_as_float(e[0] & 0xffff0000u), __uint_as_float(e[1] << 16),
-                              __uint_as_float(e[1] & 0xffff0000u)};
+      for (int i = 0; i < MI; ++i) {
+        const float u[4] = {__uint_as_float(cur.e[i][0] << 16), __uint_as_float(cur.e[i][0] & 0xffff0000u),
+                            __uint_as_float(cur.e[i][1] << 16), __uint_as_float(cur.e[i][1] & 0xffff0000u)};
+        f32x4_t h;
 #pragma unroll
-          for (int q = 0; q < 4; ++q) {
-            const float z = (float)acc[i][j][4 * g + q] * (sa[i] * sb[q]), h = z * sigmoidf_fast(z) * u[q];
-            acc[i][j][4 * g + q] = __float_as_int(h);
-            top[i] = max(top[i], __float_as_uint(h) & 0x7fffffffu);
-          }
+        for (int q = 0; q < 4; ++q) {
+          const float z = (float)acc[i][j][4 * g + q] * (sa[i] * cur.sb[q]);
+          h[q] = z * sigmoidf_fast(z) * u[q];
+          if (block * 32 >= p.N) h[q] = 0.f;
+          top[i] = max(top[i], __float_as_uint(h[q]) & 0x7fffffffu);
         }
-        __builtin_amdgcn_sched_barrier(0);                     // (all steps' reads at once would not fit the registers)
+        if (block < blocks && m0 + 32 * i < p.M)
+          *reinterpret_cast<f32x4_t*>(p.h + (((size_t)((m0 >> 5) + i) * blocks + block) * 4 + g) * 256 + lane * 4) = h;
       }
+      __builtin_amdgcn_sched_barrier(0);                       // (all steps' reads at once would not fit the registers)
+      cur = nxt;
     }
-#pragma unroll
-    for (int i = 0; i < MI; ++i) top[i] = max(top[i], (uint32_t)__shfl_xor((int)top[i], 32));
-  }
-  // the integers of a row whose largest magnitude has the bits `top`
-  static __device__ __forceinline__ void store(const QuantGemmArgs& p, const i32x16_t (&acc)[MI][NJ], int m0, int n0, bool first, int lane) {
-    const int pitch = (p.N + 127) / 128 * 128;
 #pragma unroll
     for (int i = 0; i < MI; ++i) {
-      const int mb = m0 + 32 * i, m = mb + (lane & 31);
-      if (mb >= p.M) break;
-      const uint32_t top = __hip_atomic_load(p.amax + (m < p.M ? m : p.M - 1), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-      const bool finite = top < 0x7f800000u;
-      const float s = fmaxf(__uint_as_float(top) / 127.0f, 0x1p-126f), inv = finite ? 1.0f / s : 0.f;
-      if (first && lane < 32 && m < p.M) p.scale_h[m] = finite ? s : __uint_as_float(0x7fc00000u);
-      int8_t* const out = p.hq + (size_t)mb * pitch + (n0 >> 5) * 1024 + lane * 16;
-#pragma unroll
-      for (int j = 0; j < NJ; ++j) {
-        if (n0 + 32 * j >= pitch) continue;
-        uint32_t w[4];
-#pragma unroll
-        for (int g = 0; g < 4; ++g) {
-          // |h inv| is at most 127 and a rounding: next to 1.5 x 2^23 a float's last digit is 1, and the low byte the integer's
-          uint32_t b[4];
-#pragma unroll
-          for (int q = 0; q < 4; ++q) b[q] = __float_as_uint(__builtin_fmaf(__int_as_float(acc[i][j][4 * g + q]), inv, 12582912.f));
-          w[g] = __builtin_amdgcn_perm(__builtin_amdgcn_perm(b[3], b[2], 0x0c0c0400), __builtin_amdgcn_perm(b[1], b[0], 0x0c0c0400), 0x05040100);
-        }
-        const u32x2_t lo = __builtin_amdgcn_permlane32_swap(w[0], w[2], false, false);
-        const u32x2_t hi = __builtin_amdgcn_permlane32_swap(w[1], w[3], false, false);
-        *reinterpret_cast<u32x4_t*>(out + j * 1024) = u32x4_t{lo[0], lo[1], hi[0], hi[1]};
-      }
+      const uint32_t v = max(top[i], (uint32_t)__shfl_xor((int)top[i], 32));
+      const int m = m0 + i * 32 + lane;
+      if (lane < 32 && m < p.M) __hip_atomic_fetch_max(p.amax + m, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     }
-  }
-  // What a workgroup does next: -1 its values can be quantised, else a column of tiles whose maxima it has to compute (its own: the last).
-  // By all threads; `at` is the column just computed, `own` this workgroup's.  max_lds: [WN][TM] maxima and a word.
-  static __device__ __forceinline__ int exchange(const QuantGemmArgs& p, uint32_t* max_lds, int tm, int at, int own, int ntn) {
-    const int tid = threadIdx.x;
-    uint32_t* const counter = p.panels + tm;
-    uint32_t* const flags = p.panels + (p.M + TM - 1) / TM + (size_t)tm * ntn;
-    int* const verdict = reinterpret_cast<int*>(max_lds + WN * TM);
-    __syncthreads();
-    if (tid < TM && tm * TM + tid < p.M) {
-      uint32_t v = max_lds[tid];
-#pragma unroll
-      for (int w = 1; w < WN; ++w) v = max(v, max_lds[w * TM + tid]);
-      __hip_atomic_fetch_max(p.amax + tm * TM + tid, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    }
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    __syncthreads();
-    if (tid == 0) {
-      int next = own, from = 0;
-      if (at == own) {
-        __hip_atomic_store(flags + own, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-        bool all = __hip_atomic_fetch_add(counter, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) + 1 == (uint32_t)ntn;
-        for (int i = 0; i < p.polls && !all; ++i) {
-          __builtin_amdgcn_s_sleep(1);
-          all = __hip_atomic_load(counter, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == (uint32_t)ntn;
-        }
-        if (all) next = -1;
-      } else {
-        from = at + 1;
-      }
-      if (next >= 0)
-        for (; from < ntn; ++from)
-          if (from != own && !__hip_atomic_load(flags + from, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT)) { next = from; break; }
-      *verdict = next;
-    }
-    __syncthreads();
-    return __builtin_amdgcn_readfirstlane(*verdict);
   }
 };
-
-// Workgroup -> tile of the gate product: all of a row of tiles before the next, and with more than 8 in a row each XCD the same columns of
-// every row (ntn8 of them, the rest empty), which also is 8 token panels by 4 of weights for the 32 workgroups of an XCD.
-__device__ __forceinline__ int row_of_tiles(int ntn) { return ntn > 8 ? (ntn + 7) & ~7 : ntn; }
 
 // Scales of a wavefront's tokens, lane & 31 of each block of 32, and the ids of their table rows, lane l having rows l and 64 + l
 template <int MI, bool GATE>
@@ -309,26 +246,13 @@ struct Rows {
 // ---- 256 x 256 ----------------------------------------------------------------------------------------------------------------
 constexpr int SLOT = 32768;   // an operand tile: 256 rows x 128 k
 
-template <bool GATE>
 __global__ __launch_bounds__(256) void gemm_int8_256_kernel(QuantGemmArgs p) {
   __shared__ __attribute__((aligned(16))) char smem[5 * SLOT];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wm = wave >> 1, wn = wave & 1;
-  const int ntn = (p.N + 255) / 256;
-  int tm, own;
-  if (GATE) {
-    tm = blockIdx.x / row_of_tiles(ntn);
-    own = blockIdx.x % row_of_tiles(ntn);
-    if (own >= ntn) return;
-  } else {
-    tile_of(blockIdx.x, gridDim.x, (p.M + 255) / 256, ntn, tm, own);
-  }
-  const int m0 = tm * 256;
-  typedef Hidden<4, 4, 2, 2> Hid;
-  Rows<4, GATE> rows;
-  if (GATE) rows.init(p, m0 + wm * 128, lane);
-  for (int tn = own, last = 0;;) {
-  const int n0 = tn * 256;
+  int tm, tn;
+  tile_of(blockIdx.x, gridDim.x, (p.M + 255) / 256, (p.N + 255) / 256, tm, tn);
+  const int m0 = tm * 256, n0 = tn * 256;
   Loader<256, 4> la, lb;
   la.init(p.A, p.M, p.K, m0, wave, lane);
   lb.init(p.B, p.N, p.K, n0, wave, lane);
@@ -433,35 +357,107 @@ __global__ __launch_bounds__(256) void gemm_int8_256_kernel(QuantGemmArgs p) {
   if (kt + 3 < nk) ring_iteration(3);
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
   __syncthreads();
-  if constexpr (!GATE) {
-    typedef Output<4, 4> Out;
-    static_assert(4 * Out::BYTES <= 5 * SLOT, "staging");
-    Out::run(p, acc, smem + wave * Out::BYTES, m0 + wm * 128, n0 + wn * 128, lane);
-    return;
-  } else {
-    static_assert(4 * Hid::E_BYTES + Hid::MAX_BYTES <= 5 * SLOT, "room for the rows of the table");
-    char* const lds = smem + wave * Hid::E_BYTES;
-    uint32_t* const max_lds = reinterpret_cast<uint32_t*>(smem + 4 * Hid::E_BYTES);
-    uint32_t top[4];
-    Hid::fetch_rows(p, rows.id, lds, n0 + wn * 128, lane);
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    Hid::values(p, acc, top, rows.scale, lds, n0 + wn * 128, lane);
-    if (!last) {
-      if (lane < 32)
+  typedef Output<4, 4> Out;
+  static_assert(4 * Out::BYTES <= 5 * SLOT, "staging");
+  Out::run(p, acc, smem + wave * Out::BYTES, m0 + wm * 128, n0 + wn * 128, lane);
+}
+
+// ---- 128 x 256, two workgroups a compute unit -----------------------------------------------------------------------------------------
+// 4 wavefronts of 2 x 4 accumulators, K tiles of 64 in a ring of three 24 KB slots.
+constexpr int PAIR_A = 8192, PAIR_SLOT = 24576;
+
+template <bool GATE>
+__global__ __launch_bounds__(256, 2) void gemm_int8_pair_kernel(QuantGemmArgs p) {
+  typedef Hidden<2, 4> Hid;
+  typedef Output<2, 4> Out;
+  static_assert(4 * Hid::BYTES <= 3 * PAIR_SLOT && 4 * Out::BYTES <= 3 * PAIR_SLOT, "room for the epilogue");
+  __shared__ __attribute__((aligned(16))) char smem[3 * PAIR_SLOT];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int wm = wave >> 1, wn = wave & 1;
+  int tm, tn;
+  tile_of(blockIdx.x, gridDim.x, (p.M + 127) / 128, (p.N + 255) / 256, tm, tn);
+  const int m0 = tm * 128, n0 = tn * 256;
+  Rows<2, GATE> rows;
+  if (GATE) rows.init(p, m0 + wm * 64, lane);
+  const int nk = p.K / 64, kbytes = p.K * 32;
+  const rsrc_t none = resource(p.A, 0);
+  rsrc_t ra = resource(p.A, (p.M + 31) / 32 * 32 * p.K), rb = resource(p.B, (p.N + 31) / 32 * 32 * p.K);
+  // a wavefront loads one 32-row group of the tokens and two of the weights: 2 KB of each and K tile
+  uint32_t oa, ob[2];
+  oa = m0 + wave * 32 < p.M ? (uint32_t)((m0 + wave * 32) * p.K + lane * 16) : OOB;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) max_lds[wn * 256 + wm * 128 + i * 32 + lane] = top[i];
-      const int next = Hid::exchange(p, max_lds, tm, tn, own, ntn);
-      if (next >= 0) {
-        last = next == own;
-        tn = next;
-        __syncthreads();
-        continue;
-      }
+  for (int h = 0; h < 2; ++h) ob[h] = n0 + wave * 64 + h * 32 < p.N ? (uint32_t)((n0 + wave * 64 + h * 32) * p.K + lane * 16) : OOB;
+  int k = nk >= 32 ? (int)(blockIdx.x & 7) * (nk >> 4) * 4096 : 0, left = nk;
+  auto issue = [&](int q, char* slot) __attribute__((always_inline)) {   // load q of 6
+    if (q < 2) lds_dma_16(ra, slot + (wave * 2 + q) * 1024, oa, k + q * 1024);
+    else lds_dma_16(rb, slot + PAIR_A + (wave * 4 + q - 2) * 1024, ob[(q - 2) >> 1], k + (q & 1) * 1024);
+  };
+  auto next = [&]() __attribute__((always_inline)) {
+    k += 2048;
+    if (k >= kbytes) k = 0;
+    if (--left <= 0) ra = rb = none;
+  };
+  i32x16_t acc[2][4];
+#pragma unroll
+  for (int i = 0; i < 2; ++i)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) acc[i][j] = i32x16_t{};
+  i32x4_t xa[2], xb[4], ya[2], yb[4];
+  const char* const fa = smem + wm * 4096 + lane * 16;
+  const char* const fb = smem + PAIR_A + wn * 8192 + lane * 16;
+  auto read = [&](int slot, int ks, int q, i32x4_t(&a)[2], i32x4_t(&b)[4]) __attribute__((always_inline)) {   // a0 b0 b1 a1 b2 b3
+    constexpr int isA[6] = {1, 0, 0, 1, 0, 0}, idx[6] = {0, 0, 1, 1, 2, 3};
+    if (isA[q]) a[idx[q]] = *reinterpret_cast<const i32x4_t*>(fa + slot * PAIR_SLOT + idx[q] * 2048 + ks * 1024);
+    else b[idx[q]] = *reinterpret_cast<const i32x4_t*>(fb + slot * PAIR_SLOT + idx[q] * 2048 + ks * 1024);
+  };
+  auto mma = [&](int u, i32x4_t(&a)[2], i32x4_t(&b)[4]) __attribute__((always_inline)) {
+    constexpr int ii[8] = {0, 0, 1, 1, 0, 1, 0, 1}, jj[8] = {0, 1, 0, 1, 2, 2, 3, 3};
+    acc[ii[u]][jj[u]] = __builtin_amdgcn_mfma_i32_32x32x32_i8(b[jj[u]], a[ii[u]], acc[ii[u]][jj[u]], 0, 0, 0);
+  };
+#pragma unroll
+  for (int st = 0; st < 2; ++st) {
+#pragma unroll
+    for (int q = 0; q < 6; ++q) issue(q, smem + st * PAIR_SLOT);
+    next();
+  }
+  asm volatile("s_waitcnt vmcnt(%0)" ::"n"(6) : "memory");
+  __builtin_amdgcn_s_barrier();
+  __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+  for (int q = 0; q < 6; ++q) read(0, 0, q, xa, xb);
+  // K tile t in slot t mod 3; tile t + 2 is requested while t is multiplied, into the slot that t - 1 has left
+  auto iteration = [&](const int st) __attribute__((always_inline)) {
+    const int nx = (st + 1) % 3, in = (st + 2) % 3;
+#pragma unroll
+    for (int u = 0; u < 8; ++u) {
+      if (u < 6) read(st, 1, u, ya, yb);
+      if (u >= 2) issue(u - 2, smem + in * PAIR_SLOT);
+      mma(u, xa, xb);
+      __builtin_amdgcn_sched_barrier(0);
     }
-    Hid::store(p, acc, m0 + wm * 128, own * 256 + wn * 128, own == 0 && wn == 0, lane);
-    return;
+    next();
+    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(6) : "memory");
+    __builtin_amdgcn_s_barrier();
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int u = 0; u < 8; ++u) {
+      if (u < 6) read(nx, 0, u, xa, xb);
+      mma(u, ya, yb);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+  };
+  int kt = 0;
+  for (; kt + 3 <= nk; kt += 3) {
+    iteration(0);
+    iteration(1);
+    iteration(2);
   }
-  }
+  if (kt < nk) iteration(0);
+  if (kt + 1 < nk) iteration(1);
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+  __syncthreads();
+  if constexpr (GATE) Hid::run(p, acc, rows.scale, rows.id, smem + wave * Hid::BYTES, m0 + wm * 64, n0 + wn * 128, lane);
+  else Out::run(p, acc, smem + wave * Out::BYTES, m0 + wm * 64, n0 + wn * 128, lane);
 }
 
 // ---- smaller tiles: STAGES whole K tiles in LDS, filled by LW wavefronts of their own ---------------------------------------------
@@ -476,29 +472,19 @@ template <bool GATE, class C>
 __global__ __launch_bounds__((C::WAVES + C::LW) * 64) void gemm_int8_kernel(QuantGemmArgs p) {
   constexpr int MI = C::MI, NJ = C::NJ, S = C::STAGES, STAGE = C::STAGE;
   typedef Output<MI, NJ> Out;
-  typedef Hidden<MI, NJ, C::WM, C::WN> Hid;
-  constexpr int EPI = GATE ? C::WAVES * Hid::E_BYTES + Hid::MAX_BYTES : C::WAVES * Out::BYTES;
+  typedef Hidden<MI, NJ> Hid;
+  constexpr int EPI = C::WAVES * (GATE ? Hid::BYTES : Out::BYTES);
   constexpr int LDS = S * STAGE > EPI ? S * STAGE : EPI;
   __shared__ __attribute__((aligned(16))) char smem[LDS];
   const int lane = threadIdx.x & 63, wave_id = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const bool load_wave = wave_id >= C::WAVES;
   const int wave = load_wave ? wave_id - C::WAVES : wave_id, wm = wave / C::WN, wn = wave % C::WN;
-  const int ntn = (p.N + C::TN - 1) / C::TN;
-  int tm, own;
-  if (GATE) {
-    tm = blockIdx.x / row_of_tiles(ntn);
-    own = blockIdx.x % row_of_tiles(ntn);
-    if (own >= ntn) return;
-  } else {
-    tile_of(blockIdx.x, gridDim.x, (p.M + C::TM - 1) / C::TM, ntn, tm, own);
-  }
-  const int m0 = tm * C::TM;
+  int tm, tn;
+  tile_of(blockIdx.x, gridDim.x, (p.M + C::TM - 1) / C::TM, (p.N + C::TN - 1) / C::TN, tm, tn);
+  const int m0 = tm * C::TM, n0 = tn * C::TN;
   const int nk = p.K / 128, kbytes = nk * 4096;
-  uint32_t* const max_lds = reinterpret_cast<uint32_t*>(smem + C::WAVES * Hid::E_BYTES);
   Rows<MI, GATE> rows;
   if (GATE && !load_wave) rows.init(p, m0 + wm * MI * 32, lane);
-  for (int tn = own, last = 0;;) {
-  const int n0 = tn * C::TN;
   if (load_wave) {
     Loader<C::TM, C::LW> la;
     Loader<C::TN, C::LW> lb;
@@ -536,13 +522,7 @@ __global__ __launch_bounds__((C::WAVES + C::LW) * 64) void gemm_int8_kernel(Quan
       if (kt + st < nk) load_iteration(st);
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // nothing lands in LDS once the epilogue uses it
     __syncthreads();
-    if (!GATE || last) return;
-    const int next = Hid::exchange(p, max_lds, tm, tn, own, ntn);
-    if (next < 0) return;
-    last = next == own;
-    tn = next;
-    __syncthreads();
-    continue;
+    return;
   }
   i32x16_t acc[MI][NJ];
 #pragma unroll
@@ -590,31 +570,8 @@ __global__ __launch_bounds__((C::WAVES + C::LW) * 64) void gemm_int8_kernel(Quan
   for (int st = 0; st < S - 1; ++st)
     if (kt + st < nk) stage_iteration(st);
   __syncthreads();
-  if constexpr (!GATE) {
-    Out::run(p, acc, smem + wave * Out::BYTES, m0 + wm * MI * 32, n0 + wn * NJ * 32, lane);
-    return;
-  } else {
-    char* const lds = smem + wave * Hid::E_BYTES;
-    uint32_t top[MI];
-    Hid::fetch_rows(p, rows.id, lds, n0 + wn * NJ * 32, lane);
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    Hid::values(p, acc, top, rows.scale, lds, n0 + wn * NJ * 32, lane);
-    if (!last) {
-      if (lane < 32)
-#pragma unroll
-        for (int i = 0; i < MI; ++i) max_lds[wn * C::TM + (wm * MI + i) * 32 + lane] = top[i];
-      const int next = Hid::exchange(p, max_lds, tm, tn, own, ntn);
-      if (next >= 0) {
-        last = next == own;
-        tn = next;
-        __syncthreads();
-        continue;
-      }
-    }
-    Hid::store(p, acc, m0 + wm * MI * 32, own * C::TN + wn * NJ * 32, own == 0 && wn == 0, lane);
-    return;
-  }
-  }
+  if constexpr (GATE) Hid::run(p, acc, rows.scale, rows.id, smem + wave * Hid::BYTES, m0 + wm * MI * 32, n0 + wn * NJ * 32, lane);
+  else Out::run(p, acc, smem + wave * Out::BYTES, m0 + wm * MI * 32, n0 + wn * NJ * 32, lane);
 }
 
 typedef Tiling<2, 2, 2, 2, 4, 4> Tile128;       // 128 x 128, 128 KB of LDS
@@ -622,9 +579,9 @@ typedef Tiling<2, 1, 2, 2, 6, 4> Tile128x64;    // 144 KB
 
 template <class C>
 hipError_t launch(const QuantGemmArgs& a, hipStream_t s) {
-  const int ntm = (a.M + C::TM - 1) / C::TM, ntn = (a.N + C::TN - 1) / C::TN;
-  if (a.y) gemm_int8_kernel<false, C><<<ntm * ntn, (C::WAVES + C::LW) * 64, 0, s>>>(a);
-  else gemm_int8_kernel<true, C><<<ntm * (ntn > 8 ? (ntn + 7) & ~7 : ntn), (C::WAVES + C::LW) * 64, 0, s>>>(a);
+  const int grid = ((a.M + C::TM - 1) / C::TM) * ((a.N + C::TN - 1) / C::TN);
+  if (a.y) gemm_int8_kernel<false, C><<<grid, (C::WAVES + C::LW) * 64, 0, s>>>(a);
+  else gemm_int8_kernel<true, C><<<grid, (C::WAVES + C::LW) * 64, 0, s>>>(a);
   return hipGetLastError();
 }
 
@@ -634,8 +591,8 @@ hipError_t stem_quant_gemm_launch(stem_ctx* ctx, int kid, const QuantGemmArgs& a
   ProfScope prof(ctx, kid, s);
   const int ntm = (a.M + 255) / 256, ntn = (a.N + 255) / 256, t128 = ((a.M + 127) / 128) * ((a.N + 127) / 128);
   if (ntm * ntn >= 192) {
-    if (a.y) gemm_int8_256_kernel<false><<<ntm * ntn, 256, 0, s>>>(a);
-    else gemm_int8_256_kernel<true><<<ntm * (ntn > 8 ? (ntn + 7) & ~7 : ntn), 256, 0, s>>>(a);
+    if (a.y) gemm_int8_256_kernel<<<ntm * ntn, 256, 0, s>>>(a);
+    else gemm_int8_pair_kernel<true><<<(a.M + 127) / 128 * ntn, 256, 0, s>>>(a);
     return hipGetLastError();
   }
   return t128 >= 192 ? launch<Tile128>(a, s) : launch<Tile128x64>(a, s);

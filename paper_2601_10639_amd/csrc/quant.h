@@ -9,9 +9,11 @@
 
 inline int64_t stem_quant_pitch(int64_t K) { return (K + 127) / 128 * 128; }
 inline int64_t stem_quant_size(int64_t rows, int64_t K) { return (rows + 31) / 32 * 32 * stem_quant_pitch(K); }
-// Words that the tiles of a gate product exchange: the largest magnitude of each token's hidden values, how many tiles of a row of tiles
-// are done, and which (tiles of at least 128 tokens x 64 channels).
-inline int64_t stem_quant_words(int64_t T, int64_t F) { return T + (T + 127) / 128 * (1 + (F + 63) / 64); }
+// Tokens whose hidden values a layer call has in fp32 at a time: up to 128 MiB, so that they are in the memory-side cache when they are read again
+inline int64_t stem_quant_chunk(int64_t F) {
+  const int64_t n = ((int64_t)128 << 20) / (4 * stem_quant_pitch(F)) / 256 * 256;
+  return n < 256 ? 256 : n;
+}
 
 struct QuantRowsArgs {
   const bf16_t* x;     // [rows, K]
@@ -32,13 +34,21 @@ struct QuantGemmArgs {
   int M, N, K;                      // K: padded
   bf16_t* y;                        // [M, N], or null: a gate product
   const bf16_t* residual;           // [M, N], may be null
-  int8_t* hq;                       // SiLU(product) * E[ids] as the tokens of the next product, [M, N] in the layout above
-  float* scale_h;
-  uint32_t *amax, *panels;          // stem_quant_words, zero: M maxima, and the rest
-  int polls;                        // how often a tile looks for the others
+  float* h;                         // SiLU(product) * E[ids], blocks of 32 tokens x 32 channels, 4 KB: the four channels 8 g + 4 (l / 32) ..
+                                    // of token l % 32 at (64 g + l) * 16; channels up to the pitch of N
+  uint32_t* amax;                   // [M], zero: takes the bits of each token's largest magnitude
   const int32_t* ids;
   const bf16_t* E;
   int E_rows;
   int32_t* flag;
 };
 hipError_t stem_quant_gemm_launch(stem_ctx* ctx, int kid, const QuantGemmArgs& a, hipStream_t s);
+
+struct QuantHiddenArgs {
+  const float* h;                   // as a gate product leaves them
+  const uint32_t* amax;
+  int M, blocks;                    // blocks of 32 channels a row
+  int8_t* q;                        // tokens of the next product
+  float* scale;
+};
+hipError_t stem_quant_hidden_launch(stem_ctx* ctx, const QuantHiddenArgs& a, hipStream_t s);

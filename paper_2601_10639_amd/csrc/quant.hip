@@ -8,6 +8,9 @@
 #include "quant.h"
 
 typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8_t;
+typedef __attribute__((ext_vector_type(4))) float f32x4_t;
+typedef __attribute__((ext_vector_type(4))) uint32_t u32x4_t;
+typedef __attribute__((ext_vector_type(2))) uint32_t u32x2_t;
 
 namespace {
 
@@ -138,6 +141,44 @@ __global__ __launch_bounds__(256) void quant_rows_kernel(QuantRowsArgs p) {
   }
 }
 
+// ---- hidden values to integers ---------------------------------------------------------------------------------
+// A wavefront takes RUN blocks of 32 tokens x 32 channels as the gate product left them: a lane has 16 values of one token, and after a swap
+// of half rows (v_permlane32_swap) the 16 that are one chunk of the next product's operand, in the order of the lanes: loads and stores of
+// 1 KB throughout.
+constexpr int RUN = 4;   // (rows are whole 128 channels)
+__global__ __launch_bounds__(256) void quant_hidden_kernel(QuantHiddenArgs p) {
+  const int lane = threadIdx.x & 63;
+  const int runs = p.blocks / RUN, groups = (p.M + 31) / 32;
+  const int64_t run = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+  if (run >= (int64_t)runs * groups) return;
+  const int group = (int)(run / runs), first = (int)(run % runs) * RUN, m = group * 32 + (lane & 31);
+  const float* const h = p.h + ((size_t)group * p.blocks + first) * 1024 + lane * 4;
+  f32x4_t v[RUN][4];
+#pragma unroll
+  for (int b = 0; b < RUN; ++b)
+#pragma unroll
+    for (int g = 0; g < 4; ++g) v[b][g] = *reinterpret_cast<const f32x4_t*>(h + b * 1024 + g * 256);
+  const uint32_t top = p.amax[m < p.M ? m : p.M - 1];
+  const bool finite = top < 0x7f800000u;
+  const float s = fmaxf(__uint_as_float(top) / 127.0f, 0x1p-126f), inv = finite ? 1.0f / s : 0.f;
+  if (first == 0 && lane < 32 && m < p.M) p.scale[m] = finite ? s : __uint_as_float(0x7fc00000u);
+  int8_t* const q = p.q + ((size_t)group * p.blocks + first) * 1024 + lane * 16;
+#pragma unroll
+  for (int b = 0; b < RUN; ++b) {
+    uint32_t w[4];
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+      // |v inv| is at most 127 and a rounding: next to 1.5 x 2^23 a float's last digit is 1, and the low byte the integer's
+      uint32_t c[4];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) c[k] = __float_as_uint(__builtin_fmaf(v[b][g][k], inv, 12582912.f));
+      w[g] = __builtin_amdgcn_perm(__builtin_amdgcn_perm(c[3], c[2], 0x0c0c0400), __builtin_amdgcn_perm(c[1], c[0], 0x0c0c0400), 0x05040100);
+    }
+    const u32x2_t lo = __builtin_amdgcn_permlane32_swap(w[0], w[2], false, false), hi = __builtin_amdgcn_permlane32_swap(w[1], w[3], false, false);
+    *reinterpret_cast<u32x4_t*>(q + b * 1024) = u32x4_t{lo[0], lo[1], hi[0], hi[1]};
+  }
+}
+
 template <bool VEC>
 hipError_t rows(const QuantRowsArgs& a, hipStream_t s) {
   const unsigned grid = (unsigned)(a.pad_rows ? (a.rows + 31) / 32 * 32 : a.rows);
@@ -152,4 +193,11 @@ hipError_t rows(const QuantRowsArgs& a, hipStream_t s) {
 hipError_t stem_quant_rows_launch(stem_ctx* ctx, int kid, const QuantRowsArgs& a, hipStream_t s) {
   ProfScope prof(ctx, kid, s);
   return a.K % 8 == 0 ? rows<true>(a, s) : rows<false>(a, s);
+}
+
+hipError_t stem_quant_hidden_launch(stem_ctx* ctx, const QuantHiddenArgs& a, hipStream_t s) {
+  ProfScope prof(ctx, K_QUANT_HIDDEN, s);
+  const int64_t runs = (int64_t)(a.blocks / RUN) * ((a.M + 31) / 32);
+  quant_hidden_kernel<<<(unsigned)((runs + 3) / 4), 256, 0, s>>>(a);
+  return hipGetLastError();
 }

@@ -41,7 +41,8 @@ enum StemKernelId {
   K_DROPOUT,
   K_QUANT_WEIGHTS,   // bf16 weights to 8-bit integers
   K_QUANT_ROWS,      // (normed) activations to 8-bit integers
-  K_QUANT_GATE,      // 8-bit gate product with SiLU*gather, as 8-bit integers
+  K_QUANT_GATE,      // 8-bit gate product with SiLU*gather
+  K_QUANT_HIDDEN,    // hidden values to 8-bit integers
   K_QUANT_DOWN,      // 8-bit product
   K_COUNT_
 };
@@ -123,7 +124,8 @@ struct stem_ctx {
   // 8-bit products (STEM_RESERVE_QUANT)
   int8_t *quant_x, *quant_h;      // rows of a call; their hidden values
   float *quant_sx, *quant_sh;     // their scales
-  uint32_t* quant_sync;           // what the gate product's tiles exchange
+  uint32_t* quant_amax;           // the largest magnitudes of tokens' hidden values
+  float* quant_hidden;            // hidden values of stem_quant_chunk tokens
 
   // profiling
   int prof_on;
