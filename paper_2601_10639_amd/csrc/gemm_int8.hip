@@ -160,7 +160,8 @@ struct Output {
 template <int MI, int NJ>
 struct Hidden {
   static constexpr int CH = 4 * NJ;                            // 16-byte chunks of a row of the table, of this wavefront's columns
-  static constexpr int BYTES = 32 * MI * CH * 16;              // of LDS, for each wavefront
+  static constexpr int ROWS = 32 * MI * CH * 16;               // of LDS, for each wavefront, and 128 NJ for the channels' scales
+  static constexpr int BYTES = ROWS + 128 * NJ;
   static __device__ __forceinline__ int swz(int r) { return NJ == 4 ? r & 15 : NJ == 2 ? r >> 1 & 7 : r >> 2 & 3; }
 
   static __device__ __forceinline__ void run(const QuantGemmArgs& p, const i32x16_t (&acc)[MI][NJ], const float (&sa)[MI],
@@ -173,16 +174,22 @@ struct Hidden {
       const bf16_t* const at = p.E + (size_t)id * p.N + (col < p.N ? col : 0);
       __builtin_amdgcn_global_load_lds(const_cast<bf16_t*>(at), (lds_ptr_t)(lds + q * 1024), 16, 0, 0);
     }
-    // the columns past d_ff, up to the pitch of the next product's K, become zeros: their sums are
-    const int blocks = (p.N + 127) / 128 * 4;
-    uint32_t top[MI];
+    float* const scales = reinterpret_cast<float*>(lds + ROWS);
 #pragma unroll
-    for (int i = 0; i < MI; ++i) top[i] = 0;
+    for (int c = lane; c < 32 * NJ; c += 64) scales[c] = p.scale_b[n0 + c < p.N ? n0 + c : 0];
+    // Columns past d_ff, up to the pitch of the next product's K, have sums of zero, and a row's first columns of the table: they become
+    // zeros, or NaN where the row's own first columns are no numbers either.
+    const int blocks = (p.N + 127) / 128 * 4, first = n0 >> 5;
+    const rsrc_t rh = resource(p.h, (p.M + 31) / 32 * blocks * 4096);
+    // largest positive value as an integer, and as an unsigned one the largest negative: NaN are above all numbers in both
+    int top_pos[MI];
+    uint32_t top_neg[MI];
+#pragma unroll
+    for (int i = 0; i < MI; ++i) { top_pos[i] = 0; top_neg[i] = 0; }
     struct Step { f32x4_t sb; u32x2_t e[MI]; };
     auto load = [&](int t) __attribute__((always_inline)) {
       Step s;
-      const int n = n0 + 8 * t + 4 * (lane >> 5);
-      s.sb = *reinterpret_cast<const f32x4_t*>(p.scale_b + (n < p.N ? n : 0));
+      s.sb = *reinterpret_cast<const f32x4_t*>(scales + 8 * t + 4 * (lane >> 5));
 #pragma unroll
       for (int i = 0; i < MI; ++i) {
         const int m = i * 32 + (lane & 31);
@@ -190,33 +197,36 @@ struct Hidden {
       }
       return s;
     };
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
     Step cur = load(0);
 #pragma unroll
     for (int t = 0; t < 4 * NJ; ++t) {                         // 8 channels a step
-      const int j = t >> 2, g = t & 3, block = (n0 >> 5) + j;
+      const int j = t >> 2, g = t & 3;
       const Step nxt = t + 1 < 4 * NJ ? load(t + 1) : cur;
 #pragma unroll
       for (int i = 0; i < MI; ++i) {
         const float u[4] = {__uint_as_float(cur.e[i][0] << 16), __uint_as_float(cur.e[i][0] & 0xffff0000u),
                             __uint_as_float(cur.e[i][1] << 16), __uint_as_float(cur.e[i][1] & 0xffff0000u)};
-        f32x4_t h;
+        u32x4_t h;
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
           const float z = (float)acc[i][j][4 * g + q] * (sa[i] * cur.sb[q]);
-          h[q] = z * sigmoidf_fast(z) * u[q];
-          if (block * 32 >= p.N) h[q] = 0.f;
-          top[i] = max(top[i], __float_as_uint(h[q]) & 0x7fffffffu);
+          h[q] = __float_as_uint(z * sigmoidf_fast(z) * u[q]);
         }
-        if (block < blocks && m0 + 32 * i < p.M)
-          *reinterpret_cast<f32x4_t*>(p.h + (((size_t)((m0 >> 5) + i) * blocks + block) * 4 + g) * 256 + lane * 4) = h;
+        top_pos[i] = max(max(top_pos[i], (int)h[0]), (int)h[1]);
+        top_pos[i] = max(max(top_pos[i], (int)h[2]), (int)h[3]);
+        top_neg[i] = max(max(top_neg[i], h[0]), h[1]);
+        top_neg[i] = max(max(top_neg[i], h[2]), h[3]);
+        const bool out = first + j >= blocks || m0 + 32 * i >= p.M;
+        __builtin_amdgcn_raw_buffer_store_b128(h, rh, out ? OOB : lane * 16, ((((m0 >> 5) + i) * blocks + first + j) * 4 + g) * 1024, 0);
       }
       __builtin_amdgcn_sched_barrier(0);                       // (all steps' reads at once would not fit the registers)
       cur = nxt;
     }
 #pragma unroll
     for (int i = 0; i < MI; ++i) {
-      const uint32_t v = max(top[i], (uint32_t)__shfl_xor((int)top[i], 32));
+      uint32_t v = max((uint32_t)top_pos[i], top_neg[i] & 0x7fffffffu);
+      v = max(v, (uint32_t)__shfl_xor((int)v, 32));
       const int m = m0 + i * 32 + lane;
       if (lane < 32 && m < p.M) __hip_atomic_fetch_max(p.amax + m, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     }
