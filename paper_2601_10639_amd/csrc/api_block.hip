@@ -105,8 +105,29 @@ stem_status check_quant(stem_ctx* c, const char* who) {
 
 hipError_t quant_rows(stem_ctx* c, int kid, const void* x, int64_t rows, int64_t K, const stem_norm* norm, bool pad, int8_t* q, float* scale,
                       uint32_t* clear, int64_t words, hipStream_t s) {
-  const QuantRowsArgs a = {static_cast<const bf16_t*>(x), rows, (int)K, pad, norm ? *norm : stem_norm{STEM_NORM_NONE, 0.f, nullptr}, q, scale, clear, words};
+  const QuantRowsArgs a = {static_cast<const bf16_t*>(x), rows, (int)K, pad, norm ? *norm : stem_norm{STEM_NORM_NONE, 0.f, nullptr}, q, scale, clear, words, 0};
   return stem_quant_rows_launch(c, kid, a, s);
+}
+
+QuantDecodeArgs decode_args(const stem_ctx* c, int64_t T, int64_t N, int64_t K, const void* q, const float* scale) {
+  QuantDecodeArgs a = {};
+  a.B = static_cast<const int8_t*>(q); a.scale_b = scale;
+  a.M = (int)T; a.N = (int)N; a.K = (int)K;
+  a.ksplit = stem_quant_decode_slices((int)N, (int)K, c->splitk_bytes, (int)T);
+  a.ws = reinterpret_cast<int*>(c->splitk_ws); a.tickets = c->tickets;
+  return a;
+}
+
+// The tokens of a decode product from rows x: in place, or quantised by a kernel before it (which clears `words` words too)
+hipError_t decode_tokens(stem_ctx* c, const void* x, int64_t K, const stem_norm* norm, uint32_t* clear, int64_t words, QuantDecodeArgs& a, hipStream_t s) {
+  if (stem_quant_decode_inline(a.M, K)) {
+    a.x = static_cast<const bf16_t*>(x);
+    a.row_K = (int)K;
+    a.norm = norm ? *norm : stem_norm{STEM_NORM_NONE, 0.f, nullptr};
+    return hipSuccess;
+  }
+  a.A = c->quant_x; a.scale_a = c->quant_sx;
+  return quant_rows(c, K_QUANT_ROWS, x, a.M, K, norm, false, c->quant_x, c->quant_sx, clear, words, s);
 }
 
 }  // namespace
@@ -248,6 +269,13 @@ stem_status stem_quant_linear(stem_ctx* c, const void* x, int64_t T, int64_t K, 
                          {{y, yb}}, false));
   STEM_TRY(check_buffers(c, who, {{x, xb}}, {}, false));
   hipStream_t s = static_cast<hipStream_t>(stream);
+  if (T <= STEM_QUANT_DECODE_TOKENS) {
+    QuantDecodeArgs a = decode_args(c, T, N, stem_quant_pitch(K), q, scale);
+    a.y = static_cast<bf16_t*>(y); a.residual = static_cast<const bf16_t*>(residual);
+    HIP_TRY(c, decode_tokens(c, x, K, norm, nullptr, 0, a, s));
+    HIP_TRY(c, stem_quant_decode_launch(c, K_QUANT_DOWN, a, s));
+    return STEM_OK;
+  }
   HIP_TRY(c, quant_rows(c, K_QUANT_ROWS, x, T, K, norm, false, c->quant_x, c->quant_sx, nullptr, 0, s));
   QuantGemmArgs g = {};
   g.A = c->quant_x; g.scale_a = c->quant_sx;
@@ -278,8 +306,30 @@ stem_status stem_quant_ffn_forward(stem_ctx* c, const void* x, const int32_t* id
   if (reinterpret_cast<uintptr_t>(ids) & 3u) return stem_fail(c, STEM_ERR_INVALID_ARG, "%s: ids must be 4-byte aligned", who);
   if (overlap({ids, (size_t)T * 4}, {y, xb})) return stem_fail(c, STEM_ERR_INVALID_ARG, "%s: an output lies over an input", who);
   hipStream_t s = static_cast<hipStream_t>(stream);
-  HIP_TRY(c, quant_rows(c, K_QUANT_ROWS, x, T, d, norm, false, c->quant_x, c->quant_sx, c->quant_amax, T, s));
   const int64_t chunk = stem_quant_chunk(F), pitch = stem_quant_pitch(F);
+  if (T <= STEM_QUANT_DECODE_TOKENS) {
+    QuantDecodeArgs g = decode_args(c, T, F, stem_quant_pitch(d), gate_q, gate_scale);
+    g.h_out = c->quant_hidden;
+    g.ids = ids; g.E = static_cast<const bf16_t*>(E); g.E_rows = (int)E_rows; g.flag = c->flag;
+    QuantDecodeArgs b = decode_args(c, T, d, pitch, down_q, down_scale);
+    b.y = static_cast<bf16_t*>(y); b.residual = static_cast<const bf16_t*>(residual);
+    // (a slice of the hidden values is quantised in place, by what all of them come to)
+    const bool hidden = T <= 8 && stem_quant_decode_inline(T, (pitch / 128 + b.ksplit - 1) / b.ksplit * 128);
+    if (hidden) g.max_out = c->quant_max; else g.amax = c->quant_amax;
+    HIP_TRY(c, decode_tokens(c, x, d, norm, hidden ? nullptr : c->quant_amax, T * QUANT_AMAX_STRIDE, g, s));
+    if (!hidden && g.x) HIP_TRY(c, stem_fill_zero(c->quant_amax, T * QUANT_AMAX_STRIDE * 4, s));
+    HIP_TRY(c, stem_quant_decode_launch(c, K_QUANT_GATE, g, s));
+    if (hidden) {
+      b.h = c->quant_hidden; b.max_in = c->quant_max; b.maxima = (int)(F / 32);
+    } else {
+      const QuantHiddenArgs q = {c->quant_hidden, c->quant_amax, QUANT_AMAX_STRIDE, (int)T, (int)(pitch / 32), c->quant_h, c->quant_sh};
+      HIP_TRY(c, stem_quant_hidden_launch(c, q, s));
+      b.A = c->quant_h; b.scale_a = c->quant_sh;
+    }
+    HIP_TRY(c, stem_quant_decode_launch(c, K_QUANT_DOWN, b, s));
+    return STEM_OK;
+  }
+  HIP_TRY(c, quant_rows(c, K_QUANT_ROWS, x, T, d, norm, false, c->quant_x, c->quant_sx, c->quant_amax, T, s));
   for (int64_t t0 = 0; t0 < T; t0 += chunk) {
     const int64_t n = std::min<int64_t>(chunk, T - t0);
     QuantGemmArgs g = {};
@@ -289,7 +339,7 @@ stem_status stem_quant_ffn_forward(stem_ctx* c, const void* x, const int32_t* id
     g.h = c->quant_hidden; g.amax = c->quant_amax + t0;
     g.ids = ids + t0; g.E = static_cast<const bf16_t*>(E); g.E_rows = (int)E_rows; g.flag = c->flag;
     HIP_TRY(c, stem_quant_gemm_launch(c, K_QUANT_GATE, g, s));
-    const QuantHiddenArgs q = {c->quant_hidden, c->quant_amax + t0, (int)n, (int)(pitch / 32), c->quant_h + t0 * pitch, c->quant_sh + t0};
+    const QuantHiddenArgs q = {c->quant_hidden, c->quant_amax + t0, 1, (int)n, (int)(pitch / 32), c->quant_h + t0 * pitch, c->quant_sh + t0};
     HIP_TRY(c, stem_quant_hidden_launch(c, q, s));
   }
   QuantGemmArgs b = {};

@@ -2,12 +2,9 @@
 //
 //     s_t = max_k |x_tk| / 127,  q_tk = rint(x_tk / s_t);   y_tn = s_t s_n sum_k q_tk q_nk
 //
-// The sums are exact in 32 bits up to K = 133 000 (127^2 K < 2^31).  A row that holds a NaN or an infinity has no scale: its
-// integers are zero and its scale NaN, so that what is made of it is NaN and nothing else is.  A row of zeros, or of values so small that
-// their scale would be subnormal, has the scale 2^-126.
+// The sums are exact in 32 bits up to K = 133 000 (127^2 K < 2^31).
 #include "quant.h"
 
-typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8_t;
 typedef __attribute__((ext_vector_type(4))) float f32x4_t;
 typedef __attribute__((ext_vector_type(4))) uint32_t u32x4_t;
 typedef __attribute__((ext_vector_type(2))) uint32_t u32x2_t;
@@ -15,130 +12,153 @@ typedef __attribute__((ext_vector_type(2))) uint32_t u32x2_t;
 namespace {
 
 // ---- rows to integers -------------------------------------------------------------------------------------
-// 16 elements of a row from p on, of which `left` are the row's; the others read as zero.  VEC: rows are multiples of 8 elements.
-template <bool VEC>
-__device__ __forceinline__ void load16(const bf16_t* p, int left, float (&v)[16]) {
-#pragma unroll
-  for (int h = 0; h < 2; ++h) {
-    if (VEC) {
-      bf16x8_t u = {};
-      if (left > 8 * h) u = *reinterpret_cast<const bf16x8_t*>(p + 8 * h);
-#pragma unroll
-      for (int q = 0; q < 8; ++q) v[8 * h + q] = (float)u[q];
-    } else {
-#pragma unroll
-      for (int q = 8 * h; q < 8 * h + 8; ++q) v[q] = q < left ? __uint_as_float((uint32_t)p[q] << 16) : 0.f;
-    }
+template <int CTRL>
+__device__ __forceinline__ uint32_t dpp(uint32_t v) { return __builtin_amdgcn_update_dpp(0, v, CTRL, 0xf, 0xf, true); }
+
+// LPR neighbouring lanes have a row (256: the workgroup).  f: of two values in each lane's place, given and taken as bits.
+template <int LPR, class F>
+__device__ __forceinline__ uint32_t over_row(uint32_t v, uint32_t* red, F f) {
+  v = f(v, dpp<0xb1>(v));                                   // quad_perm 1 0 3 2
+  v = f(v, dpp<0x4e>(v));                                   // quad_perm 2 3 0 1
+  v = f(v, dpp<0x141>(v));                                  // row_half_mirror
+  if (LPR > 8) v = f(v, dpp<0x140>(v));                     // row_mirror
+  if (LPR > 16) v = f(v, (uint32_t)__shfl_xor((int)v, 16));
+  if (LPR > 32) v = f(v, (uint32_t)__shfl_xor((int)v, 32));
+  if (LPR > 64) {
+    __syncthreads();
+    if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
+    __syncthreads();
+    v = f(f(red[0], red[1]), f(red[2], red[3]));
   }
+  return v;
 }
-__device__ __forceinline__ float block_sum(float v, float* red) {
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1) v += __shfl_xor(v, o);
-  __syncthreads();
-  if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
-  __syncthreads();
-  return (red[0] + red[1]) + (red[2] + red[3]);
-}
-__device__ __forceinline__ uint32_t block_max(uint32_t v, uint32_t* red) {
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1) v = max(v, (uint32_t)__shfl_xor((int)v, o));
-  __syncthreads();
-  if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
-  __syncthreads();
-  return max(max(red[0], red[1]), max(red[2], red[3]));
+template <int LPR>
+__device__ __forceinline__ float sum_row(float v, uint32_t* red) {
+  return __uint_as_float(over_row<LPR>(__float_as_uint(v), red, [](uint32_t a, uint32_t b) { return __float_as_uint(__uint_as_float(a) + __uint_as_float(b)); }));
 }
 
-// A workgroup has a row.  VPT: chunks of 16 elements a thread holds; 0: the row is longer than that and is read again for each step.
-template <bool VEC, int VPT>
+// A row's chunks lie 512 bytes apart in its block row, and 8 neighbouring rows' chunks in a line.  With few lanes a
+// row a wavefront stores longer pieces of a line, and waits for more of its loads before it has a row.  us, 16 / 32 / 64 / 256 lanes a row, behind a
+// norm: 16384 x 2048 32 / 28 / 32 / 46, 1000 x 2048 12 / 9 / 8 / 9; without one, 16384 x 4096 - / 47 / 59 / 75, 8192 x 8192 - / - / 61 / 77.
+// CPT: chunks a lane holds, in fp32; 0: the row is longer and is read again for each step.
+template <int LPR, int CPT>
 __global__ __launch_bounds__(256) void quant_rows_kernel(QuantRowsArgs p) {
-  __shared__ float red[4];
-  __shared__ uint32_t redm[4];
-  const int64_t row = blockIdx.x;
-  const int chunks = (int)((p.K + 127) / 128 * 8);
-  int8_t* const out = p.q + (row >> 5) * 32 * (int64_t)chunks * 16 + (row & 31) * 16;
-  const bf16_t* const x = p.x + row * p.K;
-  constexpr int HELD = VPT ? VPT : 1;
-  float v[HELD][16];
-  const bool live = row < p.rows;
+  __shared__ uint32_t red[4];
+  constexpr int ROWS = 256 / LPR, HELD = CPT ? CPT : 1;
+  // a norm's weight, read by every row: from LDS where a workgroup has several
+  constexpr bool SHARED = LPR <= 64;
+  __shared__ QuantChunk weight[SHARED ? LPR * HELD : 1];
+  const int l = threadIdx.x % LPR;
+  const int64_t row = (int64_t)blockIdx.x * ROWS + threadIdx.x / LPR;
   if (p.clear)
-    for (int64_t i = row * 256 + threadIdx.x; i < p.clear_words; i += (int64_t)gridDim.x * 256) p.clear[i] = 0;
-  const int steps = VPT ? VPT : (chunks + 255) / 256;
-  auto fetch = [&](int t, float (&u)[16]) {
-    const int c = t * 256 + threadIdx.x;
-    if (live && c * 16 < p.K) load16<VEC>(x + c * 16, p.K - c * 16, u);
-    else
-#pragma unroll
-      for (int q = 0; q < 16; ++q) u[q] = 0.f;
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < p.clear_words; i += (int64_t)gridDim.x * 256) p.clear[i] = 0;
+  const int chunks = (p.K + 127) / 128 * 8;
+  const bool live = row < p.rows;
+  const bf16_t* const x = p.x + (live ? row : 0) * p.K;
+  auto fetch = [&](int t) __attribute__((always_inline)) {
+    const int c = t * LPR + l;
+    return live && c * 16 < p.K ? quant_load_chunk(x + c * 16, p.K - c * 16) : QuantChunk{};
   };
-  if (VPT) {
+  QuantChunk raw[HELD] = {};
+  if constexpr (CPT > 0) {
 #pragma unroll
-    for (int t = 0; t < HELD; ++t) fetch(t, v[t]);
+    for (int t = 0; t < CPT; ++t)
+      if (t * LPR < chunks) raw[t] = fetch(t);
   }
-  // what the row's values are before they are quantised: a norm's mean and factor, and its weight
+  if (SHARED && p.norm.weight) {
+    for (int c = threadIdx.x; c * 16 < p.K; c += 256) weight[c] = quant_load_chunk(static_cast<const bf16_t*>(p.norm.weight) + c * 16, p.K - c * 16);
+    __syncthreads();
+  }
+  if (LPR <= 64 && row >= p.all_rows) return;               // (whole groups of lanes that exchange nothing with others)
+  // f on each step's values, which it may change where the lane holds them; otherwise they are made again
+  float v[HELD][16];
+  auto elements = [&](const QuantChunk& c, float (&u)[16]) __attribute__((always_inline)) {
+#pragma unroll
+    for (int q = 0; q < 16; ++q) u[q] = quant_element(c, q);
+  };
+  if constexpr (CPT > 0) {
+#pragma unroll
+    for (int t = 0; t < CPT; ++t) elements(raw[t], v[t]);
+  }
+  // zeros behind the row's end
+  auto cut = [&](int t, float (&u)[16]) __attribute__((always_inline)) {
+    const int left = p.K - (t * LPR + l) * 16;
+    if (left < 16)
+#pragma unroll
+      for (int q = 0; q < 16; ++q) u[q] = q < left ? u[q] : 0.f;
+  };
   float mean = 0.f, r = 1.f;
-  if (p.norm.kind != STEM_NORM_NONE) {
-    if (p.norm.kind == STEM_NORM_LAYER) {
-      float s = 0.f;
-      for (int t = 0; t < steps; ++t) {
-        if (!VPT) fetch(t, v[0]);
+  // the values a step has after its norm so far (stage 1: centred, 2: normed and weighted)
+  auto advance = [&](int stage, int t, float (&u)[16]) __attribute__((always_inline)) {
+    if (stage == 1) {
 #pragma unroll
-        for (int q = 0; q < 16; ++q) s += v[VPT ? t : 0][q];
-      }
-      mean = block_sum(s, red) / (float)p.K;
-    }
-    float s = 0.f;
-    for (int t = 0; t < steps; ++t) {
-      if (!VPT) fetch(t, v[0]);
-      const int left = p.K - (t * 256 + (int)threadIdx.x) * 16;
+      for (int q = 0; q < 16; ++q) u[q] -= mean;
+    } else {
+      const int at = t * LPR + l;
+      if (p.norm.weight) {
+        const QuantChunk w = at * 16 >= p.K ? QuantChunk{} : SHARED ? weight[at] : quant_load_chunk(static_cast<const bf16_t*>(p.norm.weight) + at * 16, p.K - at * 16);
 #pragma unroll
-      for (int q = 0; q < 16; ++q) {
-        const float c = q < left ? v[VPT ? t : 0][q] - mean : 0.f;
-        s += c * c;
+        for (int q = 0; q < 16; ++q) u[q] = u[q] * r * quant_element(w, q);
+      } else {
+#pragma unroll
+        for (int q = 0; q < 16; ++q) u[q] *= r;
       }
     }
-    r = 1.0f / sqrtf(block_sum(s, red) / (float)p.K + p.norm.eps);
-  }
-  auto finish = [&](int t, float (&u)[16]) {
-    if (p.norm.kind == STEM_NORM_NONE) return;
-    const int c = t * 256 + threadIdx.x, left = p.K - c * 16;
-    float w[16];
-    if (p.norm.weight && left > 0) load16<VEC>(static_cast<const bf16_t*>(p.norm.weight) + c * 16, left, w);
-#pragma unroll
-    for (int q = 0; q < 16; ++q) u[q] = q < left ? (u[q] - mean) * r * (p.norm.weight ? w[q] : 1.f) : 0.f;
+    cut(t, u);
   };
-  uint32_t top = 0;
-  for (int t = 0; t < steps; ++t) {
-    if (!VPT) fetch(t, v[0]);
-    float (&u)[16] = v[VPT ? t : 0];
-    finish(t, u);
+  const bool centred = p.norm.kind == STEM_NORM_LAYER, normed = p.norm.kind != STEM_NORM_NONE || p.norm.weight;
+  // f(t, values) for every step, after `stage` steps of the norm, the last of them taken now
+  auto each_step = [&](int stage, auto f) __attribute__((always_inline)) {
+    if constexpr (CPT > 0) {
 #pragma unroll
-    for (int q = 0; q < 16; ++q) top = max(top, __float_as_uint(u[q]) & 0x7fffffffu);
-  }
-  top = block_max(top, redm);
-  const bool finite = top < 0x7f800000u;
-  const float s = fmaxf(__uint_as_float(top) / 127.0f, 0x1p-126f), inv = finite ? 1.0f / s : 0.f;
-  if (threadIdx.x == 0 && live) p.scale[row] = finite ? s : __uint_as_float(0x7fc00000u);
-  for (int t = 0; t < steps; ++t) {
-    const int c = t * 256 + threadIdx.x;
-    if (c >= chunks) break;
-    float (&u)[16] = v[VPT ? t : 0];
-    if (!VPT) {
-      fetch(t, u);
-      finish(t, u);
+      for (int t = 0; t < CPT; ++t)
+        if (t * LPR < chunks) {
+          if (stage == 1 && centred) advance(1, t, v[t]);
+          if (stage == 2 && normed) advance(2, t, v[t]);
+          f(t, v[t]);
+        }
+    } else {
+      for (int t = 0; t * LPR < chunks; ++t) {
+        elements(fetch(t), v[0]);
+        if (stage >= 1 && centred) advance(1, t, v[0]);
+        if (stage >= 2 && normed) advance(2, t, v[0]);
+        f(t, v[0]);
+      }
     }
+  };
+  if (p.norm.kind != STEM_NORM_NONE) {
+    float s = 0.f;
+    if (centred) {
+      each_step(0, [&](int, float (&u)[16]) {
+#pragma unroll
+        for (int q = 0; q < 16; ++q) s += u[q];
+      });
+      mean = sum_row<LPR>(s, red) / (float)p.K;
+      s = 0.f;
+    }
+    each_step(1, [&](int, float (&u)[16]) {
+#pragma unroll
+      for (int q = 0; q < 16; ++q) s += u[q] * u[q];
+    });
+    r = 1.0f / sqrtf(sum_row<LPR>(s, red) / (float)p.K + p.norm.eps);
+  }
+  uint32_t top = 0;
+  each_step(2, [&](int, float (&u)[16]) {
+#pragma unroll
+    for (int q = 0; q < 16; q += 2) top = max(max(top, __float_as_uint(u[q]) & 0x7fffffffu), __float_as_uint(u[q + 1]) & 0x7fffffffu);
+  });
+  top = over_row<LPR>(top, red, [](uint32_t a, uint32_t b) { return max(a, b); });
+  const QuantScale s = quant_scale(top);
+  if (l == 0 && live) p.scale[row] = s.scale;
+  int8_t* const out = p.q + (row >> 5) * 32 * (int64_t)chunks * 16 + (row & 31) * 16;
+  each_step(CPT ? 3 : 2, [&](int t, float (&u)[16]) {
+    const int c = t * LPR + l;
     uint32_t w[4];
 #pragma unroll
-    for (int q = 0; q < 4; ++q) {
-      w[q] = 0;
-#pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        // |u / s| is at most 127 and a rounding
-        const int i = finite ? (int)fminf(fmaxf(rintf(u[4 * q + k] * inv), -127.f), 127.f) : 0;
-        w[q] |= (uint32_t)(i & 0xff) << (8 * k);
-      }
-    }
-    *reinterpret_cast<uint4*>(out + (int64_t)(c >> 1) * 1024 + (c & 1) * 512) = make_uint4(w[0], w[1], w[2], w[3]);
-  }
+    for (int q = 0; q < 4; ++q)
+      w[q] = quant_four_bytes(quant_integer(u[4 * q], s.inv), quant_integer(u[4 * q + 1], s.inv), quant_integer(u[4 * q + 2], s.inv), quant_integer(u[4 * q + 3], s.inv)) & s.mask;
+    if (c < chunks) *reinterpret_cast<u32x4_t*>(out + (int64_t)(c >> 1) * 1024 + (c & 1) * 512) = u32x4_t{w[0], w[1], w[2], w[3]};
+  });
 }
 
 // ---- hidden values to integers ---------------------------------------------------------------------------------
@@ -158,41 +178,36 @@ __global__ __launch_bounds__(256) void quant_hidden_kernel(QuantHiddenArgs p) {
   for (int b = 0; b < RUN; ++b)
 #pragma unroll
     for (int g = 0; g < 4; ++g) v[b][g] = *reinterpret_cast<const f32x4_t*>(h + b * 1024 + g * 256);
-  const uint32_t top = p.amax[m < p.M ? m : p.M - 1];
-  const bool finite = top < 0x7f800000u;
-  const float s = fmaxf(__uint_as_float(top) / 127.0f, 0x1p-126f), inv = finite ? 1.0f / s : 0.f;
-  if (first == 0 && lane < 32 && m < p.M) p.scale[m] = finite ? s : __uint_as_float(0x7fc00000u);
+  const QuantScale s = quant_scale(p.amax[(m < p.M ? m : p.M - 1) * p.stride]);
+  if (first == 0 && lane < 32 && m < p.M) p.scale[m] = s.scale;
   int8_t* const q = p.q + ((size_t)group * p.blocks + first) * 1024 + lane * 16;
 #pragma unroll
   for (int b = 0; b < RUN; ++b) {
     uint32_t w[4];
 #pragma unroll
-    for (int g = 0; g < 4; ++g) {
-      // |v inv| is at most 127 and a rounding: next to 1.5 x 2^23 a float's last digit is 1, and the low byte the integer's
-      uint32_t c[4];
-#pragma unroll
-      for (int k = 0; k < 4; ++k) c[k] = __float_as_uint(__builtin_fmaf(v[b][g][k], inv, 12582912.f));
-      w[g] = __builtin_amdgcn_perm(__builtin_amdgcn_perm(c[3], c[2], 0x0c0c0400), __builtin_amdgcn_perm(c[1], c[0], 0x0c0c0400), 0x05040100);
-    }
+    for (int g = 0; g < 4; ++g)
+      w[g] = quant_four_bytes(quant_integer(v[b][g][0], s.inv), quant_integer(v[b][g][1], s.inv), quant_integer(v[b][g][2], s.inv), quant_integer(v[b][g][3], s.inv)) & s.mask;
     const u32x2_t lo = __builtin_amdgcn_permlane32_swap(w[0], w[2], false, false), hi = __builtin_amdgcn_permlane32_swap(w[1], w[3], false, false);
     *reinterpret_cast<u32x4_t*>(q + b * 1024) = u32x4_t{lo[0], lo[1], hi[0], hi[1]};
   }
 }
 
-template <bool VEC>
-hipError_t rows(const QuantRowsArgs& a, hipStream_t s) {
-  const unsigned grid = (unsigned)(a.pad_rows ? (a.rows + 31) / 32 * 32 : a.rows);
-  if (a.K <= 4096) quant_rows_kernel<VEC, 1><<<grid, 256, 0, s>>>(a);
-  else if (a.K <= 8192) quant_rows_kernel<VEC, 2><<<grid, 256, 0, s>>>(a);
-  else quant_rows_kernel<VEC, 0><<<grid, 256, 0, s>>>(a);
-  return hipGetLastError();
+template <int LPR, int CPT>
+void launch_rows(const QuantRowsArgs& a, hipStream_t s) {
+  quant_rows_kernel<LPR, CPT><<<(unsigned)((a.all_rows * LPR + 255) / 256), 256, 0, s>>>(a);
 }
 
 }  // namespace
 
-hipError_t stem_quant_rows_launch(stem_ctx* ctx, int kid, const QuantRowsArgs& a, hipStream_t s) {
+hipError_t stem_quant_rows_launch(stem_ctx* ctx, int kid, const QuantRowsArgs& p, hipStream_t s) {
   ProfScope prof(ctx, kid, s);
-  return a.K % 8 == 0 ? rows<true>(a, s) : rows<false>(a, s);
+  QuantRowsArgs a = p;
+  a.all_rows = a.pad_rows ? (a.rows + 31) / 32 * 32 : a.rows;
+  if (a.K <= 2048) a.all_rows >= 2048 ? launch_rows<32, 4>(a, s) : launch_rows<64, 2>(a, s);
+  else if (a.K <= 4096) a.all_rows >= 2048 ? launch_rows<32, 8>(a, s) : launch_rows<256, 1>(a, s);
+  else if (a.K <= 8192) a.all_rows >= 1024 ? launch_rows<64, 8>(a, s) : launch_rows<256, 2>(a, s);
+  else launch_rows<256, 0>(a, s);
+  return hipGetLastError();
 }
 
 hipError_t stem_quant_hidden_launch(stem_ctx* ctx, const QuantHiddenArgs& a, hipStream_t s) {

@@ -125,6 +125,7 @@ struct stem_ctx {
   int8_t *quant_x, *quant_h;      // rows of a call; their hidden values
   float *quant_sx, *quant_sh;     // their scales
   uint32_t* quant_amax;           // the largest magnitudes of tokens' hidden values
+  uint32_t* quant_max;            // those of up to 8 tokens, in each tile of 32 channels
   float* quant_hidden;            // hidden values of stem_quant_chunk tokens
 
   // profiling
