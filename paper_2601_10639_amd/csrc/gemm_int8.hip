@@ -69,7 +69,7 @@ struct Loader {
 template <int MI, int NJ>
 struct Output {
   static constexpr int COLS = 32 * NJ, PITCH = COLS + 4;       // of a staged row, in words
-  static constexpr int BYTES = 32 * PITCH * 4;                 // of LDS, for each wavefront
+  static constexpr int BYTES = 32 * PITCH * 4 + (COLS + 32) * 4;   // of LDS, for each wavefront: the rows, the channels' scales and the rows'
   static constexpr int LPR = COLS / 8, RPP = 64 / LPR, PASSES = 32 / RPP;   // 8 columns a lane
 
   static __device__ __forceinline__ void run(const QuantGemmArgs& p, const i32x16_t (&acc)[MI][NJ], char* stg, int m0, int n0, int lane) {
@@ -80,6 +80,10 @@ struct Output {
     float sb[8], sa_row[MI];
 #pragma unroll
     for (int q = 0; q < 8; ++q) sb[q] = n + q < p.N ? p.scale_b[n + q] : 0.f;
+    float* const scales = reinterpret_cast<float*>(st + 32 * PITCH);
+    float* const scales_a = scales + COLS;
+    if (!whole)
+      for (int c = lane; c < COLS; c += 64) scales[c] = n0 + c < p.N ? p.scale_b[n0 + c] : 0.f;
 #pragma unroll
     for (int i = 0; i < MI; ++i) sa_row[i] = p.scale_a[m0 + i * 32 + (lane & 31) < p.M ? m0 + i * 32 + (lane & 31) : p.M - 1];
     // A lane outside the matrix is given an offset beyond the buffer: its loads read zero and its stores are dropped.
@@ -125,19 +129,60 @@ struct Output {
           __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4_t, o), ry, off[pass], 0, 0);
         }
       } else {
-        // rows of y at any 2-byte address: neighbouring lanes have neighbouring columns
-        for (int r = 0; r < 32; ++r) {
-          const float sa = __shfl(sa_row[i], r);
-          if (i * 32 + r >= rows) break;
+        // Rows of y at any 2-byte address: 16 bytes at a time where all of them are the tile's, and the ends of each row, up to 7 columns on
+        // either side, one by one.  (One by one throughout: 4000 x 5001, K 1999, 191 us instead of %ODD%, against 67 at 5000 columns.)
+        constexpr int GROUPS = COLS / 8 + 1, UNITS = (32 * GROUPS + 63) / 64;
+        const int lim = p.N - n0 < COLS ? p.N - n0 : COLS;
+        auto head = [&](int r) __attribute__((always_inline)) {   // columns in front of row r's first 16-byte boundary
+          return (8 - (((m0 + i * 32 + r) & 7) * (p.N & 7) + n0 & 7)) & 7;
+        };
+        if (lane < 32) scales_a[lane] = sa_row[i];
+        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+        __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+        // offsets from the boundary in front of row m0 (the buffers are aligned to it)
+        const size_t first = (size_t)m0 * p.N & ~(size_t)7;
+        const int skip = (int)((size_t)m0 * p.N & 7), size = (skip + rows * p.N) * 2;
+        const rsrc_t uy = resource(p.y + first, size), ur = resource(p.residual ? p.residual + first : nullptr, p.residual ? size : 0);
+        auto at = [&](int r, int col, bool ok) __attribute__((always_inline)) {
+          return ok ? (uint32_t)(skip + (i * 32 + r) * p.N + n0 + col) * 2u : OOB;
+        };
+        uint32_t whole_at[UNITS], end_at[8];
+        int whole_st[UNITS], end_st[8];   // where in the staged rows; channel and row are made of it
+        u32x4_t rz[UNITS] = {};
+        uint16_t re[8] = {};
 #pragma unroll
-          for (int c = 0; c < COLS; c += 64) {
-            const int col = c + lane;
-            if (col >= COLS || n0 + col >= p.N) continue;
-            float z = (float)st[r * PITCH + col] * (sa * p.scale_b[n0 + col]);
-            const size_t at = (size_t)(m0 + i * 32 + r) * p.N + n0 + col;
-            if (p.residual) z += __uint_as_float((uint32_t)p.residual[at] << 16);
-            reinterpret_cast<__bf16*>(p.y)[at] = (__bf16)z;
-          }
+        for (int u = 0; u < UNITS; ++u) {
+          const int e = u * 64 + lane, r = e / GROUPS < 32 ? e / GROUPS : 31, h = head(r), col = (e % GROUPS) * 8 + (h ? h - 8 : 0);
+          const bool ok = e / GROUPS < 32 && i * 32 + r < rows && col >= 0 && col + 8 <= lim;
+          whole_at[u] = at(r, col, ok);
+          whole_st[u] = ok ? r * PITCH + col : 0;
+          if (p.residual) rz[u] = __builtin_amdgcn_raw_buffer_load_b128(ur, whole_at[u], 0, 0);
+        }
+#pragma unroll
+        for (int u = 0; u < 8; ++u) {   // column q of up to 7 in front, or q - 8 behind
+          const int e = u * 64 + lane, r = e >> 4, q = e & 15, h = head(r);
+          const int col = q < 8 ? q : (lim > h ? h + ((lim - h) & ~7) : 0) + q - 8;
+          const bool ok = i * 32 + r < rows && (q < 8 ? col < h && col < lim : lim > h && col < lim);
+          end_at[u] = at(r, col, ok);
+          end_st[u] = ok ? r * PITCH + col : 0;
+          if (p.residual) re[u] = __builtin_amdgcn_raw_buffer_load_b16(ur, end_at[u], 0, 0);
+        }
+#pragma unroll
+        for (int u = 0; u < UNITS; ++u) {
+          const int r = whole_st[u] / PITCH, col = whole_st[u] % PITCH;
+          const float sa = scales_a[r];
+          bf16x8_t o;
+#pragma unroll
+          for (int q = 0; q < 8; ++q)
+            o[q] = (__bf16)((float)st[whole_st[u] + q] * (sa * scales[col + q]) + __uint_as_float(q & 1 ? rz[u][q >> 1] & 0xffff0000u : rz[u][q >> 1] << 16));
+          __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4_t, o), uy, whole_at[u], 0, 0);
+        }
+#pragma unroll
+        for (int u = 0; u < 8; ++u) {
+          const int r = end_st[u] / PITCH, col = end_st[u] % PITCH;
+          const float z = (float)st[end_st[u]] * (scales_a[r] * scales[col]) + __uint_as_float((uint32_t)re[u] << 16);
+          __builtin_amdgcn_raw_buffer_store_b16(__builtin_bit_cast(uint16_t, (__bf16)z), uy, end_at[u], 0, 0);
         }
       }
       __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
