@@ -109,6 +109,12 @@ hipError_t quant_rows(stem_ctx* c, int kid, const void* x, int64_t rows, int64_t
   return stem_quant_rows_launch(c, kid, a, s);
 }
 
+QuantGemmArgs gemm_args(const stem_ctx* c) {
+  QuantGemmArgs a = {};
+  a.ws = reinterpret_cast<int*>(c->splitk_ws); a.ws_bytes = c->splitk_bytes; a.tickets = c->tickets;
+  return a;
+}
+
 QuantDecodeArgs decode_args(const stem_ctx* c, int64_t T, int64_t N, int64_t K, const void* q, const float* scale) {
   QuantDecodeArgs a = {};
   a.B = static_cast<const int8_t*>(q); a.scale_b = scale;
@@ -277,7 +283,7 @@ stem_status stem_quant_linear(stem_ctx* c, const void* x, int64_t T, int64_t K, 
     return STEM_OK;
   }
   HIP_TRY(c, quant_rows(c, K_QUANT_ROWS, x, T, K, norm, false, c->quant_x, c->quant_sx, nullptr, 0, s));
-  QuantGemmArgs g = {};
+  QuantGemmArgs g = gemm_args(c);
   g.A = c->quant_x; g.scale_a = c->quant_sx;
   g.B = static_cast<const int8_t*>(q); g.scale_b = scale;
   g.M = (int)T; g.N = (int)N; g.K = (int)stem_quant_pitch(K);
@@ -332,7 +338,7 @@ stem_status stem_quant_ffn_forward(stem_ctx* c, const void* x, const int32_t* id
   HIP_TRY(c, quant_rows(c, K_QUANT_ROWS, x, T, d, norm, false, c->quant_x, c->quant_sx, c->quant_amax, T, s));
   for (int64_t t0 = 0; t0 < T; t0 += chunk) {
     const int64_t n = std::min<int64_t>(chunk, T - t0);
-    QuantGemmArgs g = {};
+    QuantGemmArgs g = gemm_args(c);
     g.A = c->quant_x + t0 * stem_quant_pitch(d); g.scale_a = c->quant_sx + t0;
     g.B = static_cast<const int8_t*>(gate_q); g.scale_b = gate_scale;
     g.M = (int)n; g.N = (int)F; g.K = (int)stem_quant_pitch(d);
@@ -342,7 +348,7 @@ stem_status stem_quant_ffn_forward(stem_ctx* c, const void* x, const int32_t* id
     const QuantHiddenArgs q = {c->quant_hidden, c->quant_amax + t0, 1, (int)n, (int)(pitch / 32), c->quant_h + t0 * pitch, c->quant_sh + t0};
     HIP_TRY(c, stem_quant_hidden_launch(c, q, s));
   }
-  QuantGemmArgs b = {};
+  QuantGemmArgs b = gemm_args(c);
   b.A = c->quant_h; b.scale_a = c->quant_sh;
   b.B = static_cast<const int8_t*>(down_q); b.scale_b = down_scale;
   b.M = (int)T; b.N = (int)d; b.K = (int)stem_quant_pitch(F);

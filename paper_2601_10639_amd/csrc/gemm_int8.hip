@@ -6,6 +6,8 @@
 //
 // The instruction multiplies twice as many k as the bf16 one of the same shape in the same 32 clocks on operands of the same bytes, so
 // the large tile is that product's (gemm_bf16.hip): 256 x 256, 4 wavefronts of 4 x 4 accumulators, a ring of five 32 KB slots.
+#include <algorithm>
+
 #include "quant.h"
 
 typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8_t;
@@ -21,6 +23,8 @@ typedef __amdgpu_buffer_rsrc_t rsrc_t;
 namespace {
 
 constexpr uint32_t OOB = 0x80000000u;   // a buffer offset beyond any operand: reads as zero, is not stored
+constexpr int SC1 = 16;                 // cache policy bit of the buffer instructions: device scope
+constexpr int MAX_SLICES = 8;
 
 __device__ __forceinline__ float sigmoidf_fast(float z) { return __builtin_amdgcn_rcpf(1.0f + __expf(-z)); }
 __device__ __forceinline__ void lds_dma_16(rsrc_t rs, char* lds_dst, uint32_t off, int soff) {
@@ -130,7 +134,7 @@ struct Output {
         }
       } else {
         // Rows of y at any 2-byte address: 16 bytes at a time where all of them are the tile's, and the ends of each row, up to 7 columns on
-        // either side, one by one.  (One by one throughout: 4000 x 5001, K 1999, 191 us instead of %ODD%, against 67 at 5000 columns.)
+        // either side, one by one.  (One by one throughout: 4000 x 5001, K 1999, 191 us instead of 91, against 61 at 5000 columns.)
         constexpr int GROUPS = COLS / 8 + 1, UNITS = (32 * GROUPS + 63) / 64;
         const int lim = p.N - n0 < COLS ? p.N - n0 : COLS;
         auto head = [&](int r) __attribute__((always_inline)) {   // columns in front of row r's first 16-byte boundary
@@ -523,6 +527,50 @@ struct Tiling {
   static constexpr int A_BYTES = TM * 128, STAGE = (TM + TN) * 128;
 };
 
+// Split K (few tiles): every slice writes its sums in the lanes' layout and takes a ticket of its tile; the workgroup that takes the last one
+// adds the others' to its own, in any order: they are integers.  Nobody waits for anybody.  The slices run on different XCDs, whose L2s don't
+// see each other's lines: stores and loads carry the device scope bit, and a wavefront's stores are there for the device when they
+// leave its counter, which is before the workgroup's ticket is taken.  `at`: this wavefront's place among all of a slice's, `stride` apart.
+template <int MI, int NJ>
+__device__ __forceinline__ bool last_slice(const QuantGemmArgs& p, i32x16_t (&acc)[MI][NJ], char* smem, int at, int stride, int slice, int tile, int lane) {
+  constexpr int BYTES = MI * NJ * 4096;
+  const rsrc_t rw = resource(p.ws, p.ksplit * stride * BYTES);
+#pragma unroll
+  for (int i = 0; i < MI; ++i)
+#pragma unroll
+    for (int j = 0; j < NJ; ++j)
+#pragma unroll
+      for (int g = 0; g < 4; ++g) {
+        const i32x4_t v = {acc[i][j][4 * g], acc[i][j][4 * g + 1], acc[i][j][4 * g + 2], acc[i][j][4 * g + 3]};
+        __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4_t, v), rw, lane * 16, at * BYTES + ((i * NJ + j) * 4 + g) * 1024, SC1);
+      }
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+  __syncthreads();
+  int* const ticket = reinterpret_cast<int*>(smem);
+  if (threadIdx.x == 0) *ticket = __hip_atomic_fetch_add(p.tickets + tile, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  __syncthreads();
+  const bool last = *ticket == p.ksplit - 1;
+  if (!last) return false;
+  if (threadIdx.x == 0) __hip_atomic_store(p.tickets + tile, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);   // for the next launch
+  asm volatile("" ::: "memory");
+  for (int s = 0; s < p.ksplit; ++s) {
+    if (s == slice) continue;
+    const int from = (at + (s - slice) * stride) * BYTES;
+#pragma unroll
+    for (int i = 0; i < MI; ++i)
+#pragma unroll
+      for (int j = 0; j < NJ; ++j)
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+          const i32x4_t v = __builtin_bit_cast(i32x4_t, __builtin_amdgcn_raw_buffer_load_b128(rw, lane * 16, from + ((i * NJ + j) * 4 + g) * 1024, SC1));
+#pragma unroll
+          for (int q = 0; q < 4; ++q) acc[i][j][4 * g + q] += v[q];
+        }
+  }
+  __syncthreads();   // the ticket has been read: LDS may be used again
+  return true;
+}
+
 template <bool GATE, class C>
 __global__ __launch_bounds__((C::WAVES + C::LW) * 64) void gemm_int8_kernel(QuantGemmArgs p) {
   constexpr int MI = C::MI, NJ = C::NJ, S = C::STAGES, STAGE = C::STAGE;
@@ -535,9 +583,11 @@ __global__ __launch_bounds__((C::WAVES + C::LW) * 64) void gemm_int8_kernel(Quan
   const bool load_wave = wave_id >= C::WAVES;
   const int wave = load_wave ? wave_id - C::WAVES : wave_id, wm = wave / C::WN, wn = wave % C::WN;
   int tm, tn;
-  tile_of(blockIdx.x, gridDim.x, (p.M + C::TM - 1) / C::TM, (p.N + C::TN - 1) / C::TN, tm, tn);
+  const int ntm = (p.M + C::TM - 1) / C::TM, ntn = (p.N + C::TN - 1) / C::TN, tiles = ntm * ntn;
+  const int slice = blockIdx.x / tiles;
+  tile_of(blockIdx.x - slice * tiles, tiles, ntm, ntn, tm, tn);
   const int m0 = tm * C::TM, n0 = tn * C::TN;
-  const int nk = p.K / 128, kbytes = nk * 4096;
+  const int nk_all = p.K / 128, per = (nk_all + p.ksplit - 1) / p.ksplit, k0 = slice * per, nk = nk_all - k0 < per ? nk_all - k0 : per;
   Rows<MI, GATE> rows;
   if (GATE && !load_wave) rows.init(p, m0 + wm * MI * 32, lane);
   if (load_wave) {
@@ -546,14 +596,14 @@ __global__ __launch_bounds__((C::WAVES + C::LW) * 64) void gemm_int8_kernel(Quan
     constexpr int LOADS = la.LOADS + lb.LOADS;
     la.init(p.A, p.M, p.K, m0, wave, lane);
     lb.init(p.B, p.N, p.K, n0, wave, lane);
-    int k = nk >= 16 ? (int)(blockIdx.x & 7) * nk / 8 * 4096 : 0, left = nk;
+    int k = (k0 + (nk >= 16 ? (int)(blockIdx.x & 7) * nk / 8 : 0)) * 4096, left = nk;
     auto request = [&](const int st) __attribute__((always_inline)) {
 #pragma unroll
       for (int q = 0; q < la.LOADS; ++q) la.issue(q, smem + st * STAGE, wave, k);
 #pragma unroll
       for (int q = 0; q < lb.LOADS; ++q) lb.issue(q, smem + st * STAGE + C::A_BYTES, wave, k);
       k += 4096;
-      if (k >= kbytes) k = 0;
+      if (k >= (k0 + nk) * 4096) k = k0 * 4096;
       if (--left <= 0) { la.r = resource(p.A, 0); lb.r = resource(p.B, 0); }
     };
 #pragma unroll
@@ -625,6 +675,7 @@ __global__ __launch_bounds__((C::WAVES + C::LW) * 64) void gemm_int8_kernel(Quan
   for (int st = 0; st < S - 1; ++st)
     if (kt + st < nk) stage_iteration(st);
   __syncthreads();
+  if (p.ksplit > 1 && !last_slice<MI, NJ>(p, acc, smem, (slice * tiles + tn * ntm + tm) * C::WAVES + wave, tiles * C::WAVES, slice, tn * ntm + tm, lane)) return;
   if constexpr (GATE) Hid::run(p, acc, rows.scale, rows.id, smem + wave * Hid::BYTES, m0 + wm * MI * 32, n0 + wn * NJ * 32, lane);
   else Out::run(p, acc, smem + wave * Out::BYTES, m0 + wm * MI * 32, n0 + wn * NJ * 32, lane);
 }
@@ -634,7 +685,7 @@ typedef Tiling<2, 1, 2, 2, 6, 4> Tile128x64;    // 144 KB
 
 template <class C>
 hipError_t launch(const QuantGemmArgs& a, hipStream_t s) {
-  const int grid = ((a.M + C::TM - 1) / C::TM) * ((a.N + C::TN - 1) / C::TN);
+  const int grid = ((a.M + C::TM - 1) / C::TM) * ((a.N + C::TN - 1) / C::TN) * a.ksplit;
   if (a.y) gemm_int8_kernel<false, C><<<grid, (C::WAVES + C::LW) * 64, 0, s>>>(a);
   else gemm_int8_kernel<true, C><<<grid, (C::WAVES + C::LW) * 64, 0, s>>>(a);
   return hipGetLastError();
@@ -642,13 +693,49 @@ hipError_t launch(const QuantGemmArgs& a, hipStream_t s) {
 
 }  // namespace
 
-hipError_t stem_quant_gemm_launch(stem_ctx* ctx, int kid, const QuantGemmArgs& a, hipStream_t s) {
-  ProfScope prof(ctx, kid, s);
-  const int ntm = (a.M + 255) / 256, ntn = (a.N + 255) / 256, t128 = ((a.M + 127) / 128) * ((a.N + 127) / 128);
-  if (ntm * ntn >= 192) {
-    if (a.y) gemm_int8_256_kernel<<<ntm * ntn, 256, 0, s>>>(a);
-    else gemm_int8_pair_kernel<true><<<(a.M + 127) / 128 * ntn, 256, 0, s>>>(a);
-    return hipGetLastError();
+// ---- choice of the tile and of the K slices ----------------------------------------------------------------------------------------
+// One round of workgroups with as many bytes in flight as may be: the smallest tile whose grid is at most one workgroup a compute unit, and
+// beyond 256 tiles of 128 x 128 the large ones.  us, products without / with SiLU * gather, 128 x 64 / 128 x 128 / 128 x 256 / 256 x 256:
+//   N 8192, K 2048, gate: 80 tokens 15.4 / 14.9 / 20, 256 17.6 / 16.1 / 21, 400 23 / 18 / 22, 700 32 / 27 / 24.5, 4096 155 / 121 / 83
+//   N 4096, K 1024, gate: 256 tokens 11.7 / 11.7 / 15, 700 17 / 14 / 17, 1500 24 / 23 / 18
+//   N 2048, K 8192: 700 tokens 24 / 28 / 47 / 73, 1500 44 / 31 / 50 / 76, 4096 94 / 72 / 66 / 89, 16384 - / - / 241 / 218
+// K is cut where tiles are few and slices long, in up to 4 (a slice of 8 K tiles or more, 240 workgroups or fewer; in two slices 256, from 48
+// K tiles): N 2048, K 8192, 1 / 2 / 3 / 4 slices of 128 x 64 tiles: 80 tokens 19 / 15.5 / 14.1 / 14.2, 256 20.6 / 17.1 / 15.6 / 16.6, 400 21.5 / 18.2 / 24 / 23;
+// N 1024, K 4096: 128 tokens 13.3 / 12.5 / 12.0 / 12.1, 1024 14.6 / 15.5; N 448, K 1472: 256 tokens 9.4 / 10.2 / 10.4.
+// Cut gate products were slower throughout (256 tokens of N 8192, K 2048 17.6 / 23.1).
+extern "C" void stem_route_quant(int M, int N, int K, int gate, int64_t ws_bytes, int32_t* route) {
+  auto tiles = [&](int tm, int tn) { return (int64_t)((M + tm - 1) / tm) * ((N + tn - 1) / tn); };
+  const int64_t t64 = tiles(128, 64), t128 = tiles(128, 128), pair = tiles(128, 256), t256 = tiles(256, 256);
+  const int nk = K / 128;
+  int rows = 128, cols = 64, slices = 1;
+  if (t64 > 256 || (gate && nk > 8 && t128 >= 64)) cols = 128;
+  if (cols == 128 && t128 > 256) {
+    cols = 256;
+    // rounds of 256 x 256, and of 128 x 256 in their terms: two of these a compute unit, and the last round's alone are faster
+    const int64_t last = pair % 512;
+    const double few = 1.1 * (double)(pair / 512) + (last == 0 ? 0 : last <= 256 ? 0.72 : 1.1);
+    if (!gate && (double)((t256 + 255) / 256) <= few) rows = 256;
   }
-  return t128 >= 192 ? launch<Tile128>(a, s) : launch<Tile128x64>(a, s);
+  if (!gate && cols == 64) {
+    slices = (int)std::min<int64_t>({4, nk / 8, 240 / t64});
+    if (slices < 2 && t64 <= 128 && nk >= 48) slices = 2;
+    while (slices > 1 && (int64_t)slices * t64 * 128 * 64 * 4 > ws_bytes) --slices;
+    while (slices > 1 && (nk + slices - 1) / slices * (slices - 1) >= nk) --slices;   // every slice has a part of K
+    if (slices < 1) slices = 1;
+  }
+  route[0] = rows; route[1] = cols; route[2] = slices;
+}
+
+hipError_t stem_quant_gemm_launch(stem_ctx* ctx, int kid, const QuantGemmArgs& p, hipStream_t s) {
+  ProfScope prof(ctx, kid, s);
+  QuantGemmArgs a = p;
+  int32_t route[3];
+  stem_route_quant(a.M, a.N, a.K, !a.y, (int64_t)a.ws_bytes, route);
+  a.ksplit = route[2];
+  const int grid = ((a.M + route[0] - 1) / route[0]) * ((a.N + route[1] - 1) / route[1]);
+  if (route[0] == 256) gemm_int8_256_kernel<<<grid, 256, 0, s>>>(a);
+  else if (route[1] == 256 && a.y) gemm_int8_pair_kernel<false><<<grid, 256, 0, s>>>(a);
+  else if (route[1] == 256) gemm_int8_pair_kernel<true><<<grid, 256, 0, s>>>(a);
+  else return route[1] == 128 ? launch<Tile128>(a, s) : launch<Tile128x64>(a, s);
+  return hipGetLastError();
 }

@@ -33,6 +33,10 @@ struct QuantGemmArgs {
   const int8_t *A, *B;              // tokens [M, K] and weights [N, K], in the layout above
   const float *scale_a, *scale_b;
   int M, N, K;                      // K: padded
+  int* ws;                          // room for the sums of K slices
+  size_t ws_bytes;
+  int32_t* tickets;                 // the context's
+  int ksplit;                       // by the launcher
   bf16_t* y;                        // [M, N], or null: a gate product
   const bf16_t* residual;           // [M, N], may be null
   float* h;                         // SiLU(product) * E[ids], blocks of 32 tokens x 32 channels, 4 KB: the four channels 8 g + 4 (l / 32) ..

@@ -276,6 +276,8 @@ int stem_route_touch_bytes(int d_model, int d_ff, int64_t T);   // of W_down, to
 // 124 / 146; fp32, 256 x 1024, 8192 tokens (0.9) 212 / 203 / 197, 512 x 2048, vocabulary 8000, 2000 tokens (1.5) 156 / 131 / 149.  On two contexts two in
 // turn are within 1 % of a stream for each, and of one but at 8192 tokens of 1024 x 4096 (381 / 393) and 4096 of 2048 x 8192 (470 / 510).
 int stem_route_copy_streams(int d_model, int d_ff, int dtype, int64_t T, int64_t rows);
+// the tile and K slices of an 8-bit product of more than 64 tokens: {tile rows, tile columns, K slices}
+void stem_route_quant(int M, int N, int K, int gate, int64_t ws_bytes, int32_t* route);
 void stem_exchange_two_launches(stem_ctx* c, int on);   // no layer in one launch on this context
 uint32_t stem_next_launch(uint32_t last);           // stem_launch_after, and
 int stem_exchange_launch(stem_ctx* c, uint32_t last);   // all flags of the layer in one launch as launch `last` left them (waits for the device)
