@@ -71,6 +71,11 @@ __device__ __forceinline__ uint64_t offset_of(const DropArgs& d) { return d.offs
 // ---- sums over a row ---------------------------------------------------------------------------------
 // LPR neighbouring lanes hold a row (a power of two; more than 64: whole wavefronts).  Every lane gets every sum.  `red` has
 // room for two sets of partial sums, taken in turn, so that one barrier a reduction is enough.
+template <int CTRL>
+__device__ __forceinline__ float add_dpp(float v) {
+  return v + __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(v), CTRL, 0xf, 0xf, true));
+}
+typedef __attribute__((ext_vector_type(2))) uint32_t u32x2_t;
 template <int LPR>
 struct RowSum {
   static constexpr int WPR = LPR > 64 ? LPR / 64 : 1;   // wavefronts that share a row
@@ -80,9 +85,20 @@ struct RowSum {
   __device__ __forceinline__ void operator()(float (&v)[N]) {
     static_assert(N <= 2, "room in red");
 #pragma unroll
-    for (int o = 1; o < (LPR < 64 ? LPR : 64); o <<= 1)
-#pragma unroll
-      for (int k = 0; k < N; ++k) v[k] += __shfl_xor(v[k], o);
+    for (int k = 0; k < N; ++k) {
+      v[k] = add_dpp<0xb1>(v[k]);                      // quad_perm 1 0 3 2
+      v[k] = add_dpp<0x4e>(v[k]);                      // quad_perm 2 3 0 1
+      v[k] = add_dpp<0x141>(v[k]);                     // row_half_mirror
+      if (LPR > 8) v[k] = add_dpp<0x140>(v[k]);        // row_mirror
+      if (LPR > 16) {                                  // rows 0, 1 and 2, 3 against each other, then the halves
+        const u32x2_t w = __builtin_amdgcn_permlane16_swap(__float_as_uint(v[k]), __float_as_uint(v[k]), false, false);
+        v[k] = __uint_as_float(w[0]) + __uint_as_float(w[1]);
+      }
+      if (LPR > 32) {
+        const u32x2_t w = __builtin_amdgcn_permlane32_swap(__float_as_uint(v[k]), __float_as_uint(v[k]), false, false);
+        v[k] = __uint_as_float(w[0]) + __uint_as_float(w[1]);
+      }
+    }
     if (WPR > 1) {
       const int wave = (threadIdx.x >> 6) % WPR;
       if ((threadIdx.x & 63) == 0)
@@ -101,137 +117,160 @@ struct RowSum {
   }
 };
 
-template <int LPR, int VPT>
+// THREADS of a workgroup: several rows of up to 64 lanes, or of 256 (two in the backward pass, whose sums over tokens then take half
+// as many partial sums)
+template <class E, int LPR, int VPT, bool BACK>
 struct Shape {
-  static constexpr int THREADS = LPR > 256 ? LPR : 256;
+  static constexpr int THREADS = LPR > 256 ? LPR : BACK ? 512 : 256;
   static constexpr int SLOTS = THREADS / LPR;             // rows a workgroup has in hand
   static constexpr int WPR = RowSum<LPR>::WPR;
+  static constexpr bool WHOLE = sizeof(E) == 2;           // rows are whole vectors of 8
 };
 
-// v <- N(v), and 1 / sqrt(...).  Elements past the row's end are zero and stay zero.  The variance is of the centred values: the
-// difference of two sums of squares would lose what a large mean shifts out.
-template <int LPR, int VPT>
-__device__ __forceinline__ float normalise(float (&v)[VPT][8], const bool (&in)[VPT], const int (&left)[VPT], int kind, float eps, float inv_d,
-                                           RowSum<LPR>& row_sum) {
-  if (kind == STEM_NORM_NONE) return 1.f;
-  if (kind == STEM_NORM_LAYER) {
-    float s[1] = {0.f};
+// This lane's vectors of a row
+template <class E, int LPR, int VPT, bool BACK>
+struct Columns {
+  bool in[VPT];
+  int col[VPT], left[VPT];
+  __device__ __forceinline__ Columns(int lane, int d) {
 #pragma unroll
-    for (int t = 0; t < VPT; ++t)
-#pragma unroll
-      for (int q = 0; q < 8; ++q) s[0] += v[t][q];
-    row_sum(s);
-    const float mean = s[0] * inv_d;
-#pragma unroll
-    for (int t = 0; t < VPT; ++t)
-#pragma unroll
-      for (int q = 0; q < 8; ++q) v[t][q] = in[t] && q < left[t] ? v[t][q] - mean : 0.f;
+    for (int t = 0; t < VPT; ++t) {
+      col[t] = (t * LPR + lane) * 8;
+      in[t] = col[t] < d;
+      left[t] = d - col[t];
+    }
   }
-  float s[1] = {0.f};
+  // whether element q of vector t is the row's
+  __device__ __forceinline__ bool has(int t, int q) const { return in[t] && (Shape<E, LPR, VPT, BACK>::WHOLE || q < left[t]); }
+  __device__ __forceinline__ void load(const void* p, size_t at, float (&v)[VPT][8], float otherwise = 0.f) const {
+#pragma unroll
+    for (int t = 0; t < VPT; ++t) {
+#pragma unroll
+      for (int q = 0; q < 8; ++q) v[t][q] = otherwise;
+      if (p && in[t]) load8(static_cast<const E*>(p) + at + col[t], left[t], v[t]);
+    }
+  }
+  __device__ __forceinline__ void store(void* p, size_t at, int t, const float (&v)[8]) const {
+    if (in[t]) store8(static_cast<E*>(p) + at + col[t], left[t], v);
+  }
+  // v <- v - mean of a row whose sum this is; elements past the row's end are zero and stay zero
+  __device__ __forceinline__ void centre(float (&v)[VPT][8], float mean) const {
+#pragma unroll
+    for (int t = 0; t < VPT; ++t)
+#pragma unroll
+      for (int q = 0; q < 8; ++q) v[t][q] = has(t, q) ? v[t][q] - mean : 0.f;
+  }
+};
+
+template <int VPT>
+__device__ __forceinline__ float sum(const float (&v)[VPT][8]) {
+  float s = 0.f;
 #pragma unroll
   for (int t = 0; t < VPT; ++t)
 #pragma unroll
-    for (int q = 0; q < 8; ++q) s[0] += v[t][q] * v[t][q];
-  row_sum(s);
-  const float r = 1.0f / sqrtf(s[0] * inv_d + eps);
+    for (int q = 0; q < 8; ++q) s += v[t][q];
+  return s;
+}
+template <int VPT>
+__device__ __forceinline__ float dot(const float (&v)[VPT][8], const float (&w)[VPT][8]) {
+  float s = 0.f;
+#pragma unroll
+  for (int t = 0; t < VPT; ++t)
+#pragma unroll
+    for (int q = 0; q < 8; ++q) s += v[t][q] * w[t][q];
+  return s;
+}
+template <int VPT>
+__device__ __forceinline__ void scale_by(float (&v)[VPT][8], float r) {
 #pragma unroll
   for (int t = 0; t < VPT; ++t)
 #pragma unroll
     for (int q = 0; q < 8; ++q) v[t][q] *= r;
-  return r;
 }
 
-// h <- the gradient of N's input, h being that of its output v^ (past the row's end zero, and again afterwards)
-template <int LPR, int VPT>
-__device__ __forceinline__ void normalise_back(float (&h)[VPT][8], const float (&v)[VPT][8], const bool (&in)[VPT], const int (&left)[VPT], float r,
-                                               int kind, float inv_d, RowSum<LPR>& row_sum) {
-  if (kind == STEM_NORM_NONE) return;
-  float s[2] = {0.f, 0.f};
-#pragma unroll
-  for (int t = 0; t < VPT; ++t)
-#pragma unroll
-    for (int q = 0; q < 8; ++q) {
-      s[0] += h[t][q] * v[t][q];
-      s[1] += h[t][q];
-    }
+// 1 / sqrt(mean of squares + eps), v centred before for the second kind.  The variance is of the centred values: the difference of two sums
+// of squares would lose what a large mean shifts out.
+template <class C, int LPR, int VPT>
+__device__ __forceinline__ float factor(const C& c, float (&v)[VPT][8], const stem_norm& n, float inv_d, RowSum<LPR>& row_sum) {
+  if (n.kind == STEM_NORM_LAYER) {
+    float s[1] = {sum(v)};
+    row_sum(s);
+    c.centre(v, s[0] * inv_d);
+  }
+  float s[1] = {dot(v, v)};
   row_sum(s);
-  const float along = s[0] * inv_d, mean = kind == STEM_NORM_LAYER ? s[1] * inv_d : 0.f;
-#pragma unroll
-  for (int t = 0; t < VPT; ++t)
-#pragma unroll
-    for (int q = 0; q < 8; ++q) h[t][q] = in[t] && q < left[t] ? r * (h[t][q] - mean - v[t][q] * along) : 0.f;
+  return 1.0f / sqrtf(s[0] * inv_d + n.eps);
 }
 
 // ---- forward -------------------------------------------------------------------------------------------
 // BRANCH: the end of a block; without it y is x and only n is written.  One pass: a row's values stay in registers from its loads
-// to its stores.
+// to its stores.  A workgroup keeps what is the same for all rows (w_out times a gate a channel, w_next) in registers and takes as many rows
+// as leave 8 workgroups to a compute unit.
 template <class E, int LPR, int VPT, bool BRANCH>
-__global__ __launch_bounds__((Shape<LPR, VPT>::THREADS)) void block_forward_kernel(BlockArgs p) {
-  typedef Shape<LPR, VPT> S;
+__global__ __launch_bounds__((Shape<E, LPR, VPT, false>::THREADS)) void block_forward_kernel(BlockArgs p) {
+  typedef Shape<E, LPR, VPT, false> S;
   __shared__ float red[S::SLOTS][2][S::WPR][2];
   const int slot = threadIdx.x / LPR, lane = threadIdx.x % LPR;
   RowSum<LPR> row_sum{red[slot], 0};
-  bool in[VPT];
-  int col[VPT], left[VPT];
-#pragma unroll
-  for (int t = 0; t < VPT; ++t) {
-    col[t] = (t * LPR + lane) * 8;
-    in[t] = col[t] < p.d;
-    left[t] = p.d - col[t];
-  }
+  const Columns<E, LPR, VPT, false> c(lane, p.d);
   const uint64_t offset = BRANCH && p.drop.threshold ? offset_of(p.drop) : 0;
-  for (int64_t base = (int64_t)blockIdx.x * S::SLOTS; base < p.T; base += (int64_t)gridDim.x * S::SLOTS) {
-    const int64_t row = base + slot;
-    const bool live = row < p.T;
-    const size_t at = (size_t)(live ? row : p.T - 1) * p.d;
-    float y[VPT][8], f[VPT][8];
+  const bool by_channel = p.gate_kind == STEM_GATE_CHANNEL, by_element = p.gate_kind == STEM_GATE_FULL, by_token = p.gate_kind == STEM_GATE_TOKEN;
+  float branch[VPT][8], after[VPT][8];
+  if (BRANCH) {
+    c.load(p.out.weight, 0, branch, 1.f);
+    if (by_channel) {
+      float g[VPT][8];
+      c.load(p.gate, 0, g);
 #pragma unroll
-    for (int t = 0; t < VPT; ++t) {
+      for (int t = 0; t < VPT; ++t)
 #pragma unroll
-      for (int q = 0; q < 8; ++q) y[t][q] = f[t][q] = 0.f;
-      if (in[t]) load8(static_cast<const E*>(p.x) + at + col[t], left[t], y[t]);
-      if (BRANCH && in[t]) load8(static_cast<const E*>(p.f) + at + col[t], left[t], f[t]);
+        for (int q = 0; q < 8; ++q) branch[t][q] *= g[t][q];
     }
+  }
+  c.load(p.next.weight, 0, after, 1.f);
+  const float of_branch = p.branch_scale * (p.drop.threshold ? p.drop.scale : 1.f);
+  for (int64_t base = (int64_t)blockIdx.x * S::SLOTS; base < p.T; base += (int64_t)gridDim.x * S::SLOTS) {
+    const bool live = base + slot < p.T;
+    const int64_t row = live ? base + slot : p.T - 1;
+    const size_t at = (size_t)row * p.d;
+    float y[VPT][8];
+    c.load(p.x, at, y);
     if (BRANCH) {
-      normalise<LPR, VPT>(f, in, left, p.out.kind, p.out.eps, p.inv_d, row_sum);
-      const float of_token = p.gate_kind == STEM_GATE_TOKEN ? load1(static_cast<const E*>(p.gate) + (live ? row : p.T - 1)) : 1.f;
+      float f[VPT][8];
+      c.load(p.f, at, f);
+      float r = of_branch;
+      if (by_token) r *= load1(static_cast<const E*>(p.gate) + row);
+      if (by_element) {
+        float g[VPT][8];
+        c.load(p.gate, at, g);
+        if (p.out.kind != STEM_NORM_NONE) r *= factor(c, f, p.out, p.inv_d, row_sum);
+#pragma unroll
+        for (int t = 0; t < VPT; ++t)
+#pragma unroll
+          for (int q = 0; q < 8; ++q) f[t][q] *= g[t][q];
+      } else if (p.out.kind != STEM_NORM_NONE) {
+        r *= factor(c, f, p.out, p.inv_d, row_sum);
+      }
 #pragma unroll
       for (int t = 0; t < VPT; ++t) {
-        if (!in[t]) continue;
-        if (p.out.weight) {
-          float w[8];
-          load8(static_cast<const E*>(p.out.weight) + col[t], left[t], w);
-#pragma unroll
-          for (int q = 0; q < 8; ++q) f[t][q] *= w[q];
-        }
         if (p.drop.threshold) {
-          const Bits r = philox((uint32_t)(col[t] >> 3), (uint32_t)row, offset, p.drop.seed);
+          const Bits b = philox((uint32_t)(c.col[t] >> 3), (uint32_t)row, offset, p.drop.seed);
 #pragma unroll
-          for (int q = 0; q < 8; ++q) f[t][q] = kept(r, q, p.drop.threshold) ? f[t][q] * p.drop.scale : 0.f;
+          for (int q = 0; q < 8; ++q) y[t][q] = p.residual_scale * y[t][q] + (kept(b, q, p.drop.threshold) ? f[t][q] * branch[t][q] * r : 0.f);
+        } else {
+#pragma unroll
+          for (int q = 0; q < 8; ++q) y[t][q] = p.residual_scale * y[t][q] + f[t][q] * branch[t][q] * r;
         }
-        if (p.gate_kind == STEM_GATE_CHANNEL || p.gate_kind == STEM_GATE_FULL) {
-          float g[8];
-          load8(static_cast<const E*>(p.gate) + (p.gate_kind == STEM_GATE_FULL ? at : 0) + col[t], left[t], g);
-#pragma unroll
-          for (int q = 0; q < 8; ++q) f[t][q] *= g[q];
-        }
-#pragma unroll
-        for (int q = 0; q < 8; ++q) y[t][q] = p.residual_scale * y[t][q] + p.branch_scale * (f[t][q] * of_token);
-        if (live) store8(static_cast<E*>(p.y) + at + col[t], left[t], y[t]);
+        if (live) c.store(p.y, at, t, y[t]);
       }
     }
     if (p.n) {
-      normalise<LPR, VPT>(y, in, left, p.next.kind, p.next.eps, p.inv_d, row_sum);
+      if (p.next.kind != STEM_NORM_NONE) scale_by(y, factor(c, y, p.next, p.inv_d, row_sum));
 #pragma unroll
       for (int t = 0; t < VPT; ++t) {
-        if (!in[t]) continue;
-        if (p.next.weight) {
-          float w[8];
-          load8(static_cast<const E*>(p.next.weight) + col[t], left[t], w);
 #pragma unroll
-          for (int q = 0; q < 8; ++q) y[t][q] *= w[q];
-        }
-        if (live) store8(static_cast<E*>(p.n) + at + col[t], left[t], y[t]);
+        for (int q = 0; q < 8; ++q) y[t][q] *= after[t][q];
+        if (live) c.store(p.n, at, t, y[t]);
       }
     }
   }
@@ -239,133 +278,115 @@ __global__ __launch_bounds__((Shape<LPR, VPT>::THREADS)) void block_forward_kern
 
 // ---- backward ------------------------------------------------------------------------------------------
 // Sums over tokens (of dw_next, dw_out and a gate a channel) are held in registers over a workgroup's rows and written as one partial
-// sum a workgroup, [sum][workgroup][d]; block_sums_kernel adds those in order.  No atomics: the same bits on every run.
+// sum a workgroup, [sum][workgroup][d]; block_sums_kernel adds those in order.  No atomics: the same bits on every run.  All of a row is
+// requested before its first reduction.
 template <class E, int LPR, int VPT, bool BRANCH>
-__global__ __launch_bounds__((Shape<LPR, VPT>::THREADS)) void block_backward_kernel(BlockArgs p) {
-  typedef Shape<LPR, VPT> S;
+__global__ __launch_bounds__((Shape<E, LPR, VPT, true>::THREADS)) void block_backward_kernel(BlockArgs p) {
+  typedef Shape<E, LPR, VPT, true> S;
   __shared__ float red[S::SLOTS][2][S::WPR][2];
   __shared__ float sums[S::SLOTS > 1 ? S::THREADS * VPT * 8 : 1];
   const int slot = threadIdx.x / LPR, lane = threadIdx.x % LPR;
   RowSum<LPR> row_sum{red[slot], 0};
-  bool in[VPT];
-  int col[VPT], left[VPT];
-#pragma unroll
-  for (int t = 0; t < VPT; ++t) {
-    col[t] = (t * LPR + lane) * 8;
-    in[t] = col[t] < p.d;
-    left[t] = p.d - col[t];
-  }
+  const Columns<E, LPR, VPT, true> c(lane, p.d);
   const uint64_t offset = BRANCH && p.drop.threshold ? offset_of(p.drop) : 0;
+  const bool by_channel = p.gate_kind == STEM_GATE_CHANNEL, by_element = p.gate_kind == STEM_GATE_FULL, by_token = p.gate_kind == STEM_GATE_TOKEN;
   float sum_next[VPT][8], sum_out[VPT][8], sum_gate[VPT][8];
 #pragma unroll
   for (int t = 0; t < VPT; ++t)
 #pragma unroll
     for (int q = 0; q < 8; ++q) sum_next[t][q] = sum_out[t][q] = sum_gate[t][q] = 0.f;
+  const float of_branch = p.branch_scale * (p.drop.threshold ? p.drop.scale : 1.f);
   for (int64_t base = (int64_t)blockIdx.x * S::SLOTS; base < p.T; base += (int64_t)gridDim.x * S::SLOTS) {
-    const int64_t row = base + slot;
-    const bool live = row < p.T;
-    const size_t at = (size_t)(live ? row : p.T - 1) * p.d;
-    float G[VPT][8];
-#pragma unroll
-    for (int t = 0; t < VPT; ++t) {
-#pragma unroll
-      for (int q = 0; q < 8; ++q) G[t][q] = 0.f;
-      if (p.dy && in[t]) load8(static_cast<const E*>(p.dy) + at + col[t], left[t], G[t]);
-    }
+    const bool live = base + slot < p.T;
+    const int64_t row = live ? base + slot : p.T - 1;
+    const size_t at = (size_t)row * p.d;
+    float G[VPT][8], f[VPT][8];
+    c.load(p.dy, at, G);
+    if (BRANCH) c.load(p.f, at, f);
     if (p.dn) {
-      float y[VPT][8], h[VPT][8];
-#pragma unroll
-      for (int t = 0; t < VPT; ++t) {
-#pragma unroll
-        for (int q = 0; q < 8; ++q) y[t][q] = h[t][q] = 0.f;
-        if (in[t]) {
-          load8(static_cast<const E*>(p.x) + at + col[t], left[t], y[t]);
-          load8(static_cast<const E*>(p.dn) + at + col[t], left[t], h[t]);
-        }
-      }
-      const float r = normalise<LPR, VPT>(y, in, left, p.next.kind, p.next.eps, p.inv_d, row_sum);
-#pragma unroll
-      for (int t = 0; t < VPT; ++t) {
-        if (live)
-#pragma unroll
-          for (int q = 0; q < 8; ++q) sum_next[t][q] += h[t][q] * y[t][q];
-        if (p.next.weight && in[t]) {
-          float w[8];
-          load8(static_cast<const E*>(p.next.weight) + col[t], left[t], w);
-#pragma unroll
-          for (int q = 0; q < 8; ++q) h[t][q] *= w[q];
-        }
-      }
-      normalise_back<LPR, VPT>(h, y, in, left, r, p.next.kind, p.inv_d, row_sum);
+      float y[VPT][8], h[VPT][8], w[VPT][8];
+      c.load(p.x, at, y);
+      c.load(p.dn, at, h);
+      c.load(p.next.weight, 0, w, 1.f);
+      const float r = factor(c, y, p.next, p.inv_d, row_sum);
+      scale_by(y, r);
 #pragma unroll
       for (int t = 0; t < VPT; ++t)
 #pragma unroll
-        for (int q = 0; q < 8; ++q) G[t][q] += h[t][q];
+        for (int q = 0; q < 8; ++q) {
+          sum_next[t][q] += live ? h[t][q] * y[t][q] : 0.f;
+          h[t][q] *= w[t][q];
+        }
+      float s[2] = {dot(h, y), p.next.kind == STEM_NORM_LAYER ? sum(h) : 0.f};
+      row_sum(s);
+      const float along = s[0] * p.inv_d, mean = s[1] * p.inv_d;
+#pragma unroll
+      for (int t = 0; t < VPT; ++t)
+#pragma unroll
+        for (int q = 0; q < 8; ++q) G[t][q] += c.has(t, q) ? r * (h[t][q] - mean - y[t][q] * along) : 0.f;
     }
-    auto store_dx = [&](int t) {   // of a vector whose inputs have all been read: dx may be any of them
+    auto store_dx = [&](int t) __attribute__((always_inline)) {   // of a vector whose inputs have all been read: dx may be any of them
       if (!p.dx || !live) return;
       float o[8];
 #pragma unroll
       for (int q = 0; q < 8; ++q) o[q] = p.residual_scale * G[t][q];
-      store8(static_cast<E*>(p.dx) + at + col[t], left[t], o);
+      c.store(p.dx, at, t, o);
     };
     if (!BRANCH) {
 #pragma unroll
-      for (int t = 0; t < VPT; ++t)
-        if (in[t]) store_dx(t);
+      for (int t = 0; t < VPT; ++t) store_dx(t);
       continue;
     }
-    float f[VPT][8];
-#pragma unroll
-    for (int t = 0; t < VPT; ++t) {
-#pragma unroll
-      for (int q = 0; q < 8; ++q) f[t][q] = 0.f;
-      if (p.f && in[t]) load8(static_cast<const E*>(p.f) + at + col[t], left[t], f[t]);
+    // (f stays as the norm leaves it: f^ without what follows)
+    float r = 1.f;
+    if (p.f && p.out.kind != STEM_NORM_NONE) {
+      r = factor(c, f, p.out, p.inv_d, row_sum);
+      scale_by(f, r);
     }
-    const float r = normalise<LPR, VPT>(f, in, left, p.out.kind, p.out.eps, p.inv_d, row_sum);
-    const float of_token = p.gate_kind == STEM_GATE_TOKEN ? load1(static_cast<const E*>(p.gate) + (live ? row : p.T - 1)) : 1.f;
-    float of_gate[1] = {0.f};
+    const float of_token = by_token ? load1(static_cast<const E*>(p.gate) + row) : 1.f;
+    float token_gate = 0.f;
 #pragma unroll
     for (int t = 0; t < VPT; ++t) {
-      if (!in[t]) continue;
-      float w[8], g[8], keep[8];
+      if (!c.in[t]) continue;
+      float w[8], g[8], dg[8];
 #pragma unroll
-      for (int q = 0; q < 8; ++q) { w[q] = 1.f; g[q] = of_token; keep[q] = 1.f; }
-      if (p.out.weight) load8(static_cast<const E*>(p.out.weight) + col[t], left[t], w);
-      if (p.gate_kind == STEM_GATE_CHANNEL || p.gate_kind == STEM_GATE_FULL)
-        load8(static_cast<const E*>(p.gate) + (p.gate_kind == STEM_GATE_FULL ? at : 0) + col[t], left[t], g);
-      if (p.drop.threshold) {
-        const Bits b = philox((uint32_t)(col[t] >> 3), (uint32_t)row, offset, p.drop.seed);
-#pragma unroll
-        for (int q = 0; q < 8; ++q) keep[q] = kept(b, q, p.drop.threshold) ? p.drop.scale : 0.f;
-      }
+      for (int q = 0; q < 8; ++q) { w[q] = 1.f; g[q] = of_token; }
+      if (p.out.weight) load8(static_cast<const E*>(p.out.weight) + c.col[t], c.left[t], w);
+      if (by_channel || by_element) load8(static_cast<const E*>(p.gate) + (by_element ? at : 0) + c.col[t], c.left[t], g);
       store_dx(t);
-      float dg[8];
+      Bits b = {};
+      if (p.drop.threshold) b = philox((uint32_t)(c.col[t] >> 3), (uint32_t)row, offset, p.drop.seed);
 #pragma unroll
       for (int q = 0; q < 8; ++q) {
-        const float h = p.branch_scale * G[t][q];
         // (what is dropped counts for nothing, whatever f holds there)
-        const float u = keep[q] != 0.f ? f[t][q] * w[q] * keep[q] : 0.f, du = keep[q] != 0.f ? h * g[q] * keep[q] : 0.f;
-        dg[q] = h * u;
-        if (live) {
-          sum_out[t][q] += du * f[t][q];
-          sum_gate[t][q] += dg[q];
-        }
-        of_gate[0] += q < left[t] ? dg[q] : 0.f;
-        G[t][q] = du * w[q];
+        const bool keep = kept(b, q, p.drop.threshold) && live;
+        const float h = keep ? of_branch * G[t][q] : 0.f, u = keep ? f[t][q] : 0.f, du = h * g[q];
+        dg[q] = h * (u * w[q]);
+        sum_out[t][q] += du * u;
+        sum_gate[t][q] += dg[q];
+        if (c.has(t, q)) token_gate += dg[q];
+        G[t][q] = c.has(t, q) ? du * w[q] : 0.f;
       }
-      if (p.gate_kind == STEM_GATE_FULL && p.dgate && live) store8(static_cast<E*>(p.dgate) + at + col[t], left[t], dg);
+      if (by_element && p.dgate && live) c.store(p.dgate, at, t, dg);
     }
-    if (p.gate_kind == STEM_GATE_TOKEN && p.dgate) {
-      row_sum(of_gate);
-      if (live && lane == 0) store1(static_cast<E*>(p.dgate) + row, of_gate[0]);
+    if (by_token && p.dgate) {
+      float s[1] = {token_gate};
+      row_sum(s);
+      if (live && lane == 0) store1(static_cast<E*>(p.dgate) + row, s[0]);
     }
     if (p.df) {
-      normalise_back<LPR, VPT>(G, f, in, left, r, p.out.kind, p.inv_d, row_sum);
-      if (live)
+      if (p.out.kind != STEM_NORM_NONE) {
+        float s[2] = {dot(G, f), p.out.kind == STEM_NORM_LAYER ? sum(G) : 0.f};
+        row_sum(s);
+        const float along = s[0] * p.inv_d, mean = s[1] * p.inv_d;
 #pragma unroll
         for (int t = 0; t < VPT; ++t)
-          if (in[t]) store8(static_cast<E*>(p.df) + at + col[t], left[t], G[t]);
+#pragma unroll
+          for (int q = 0; q < 8; ++q) G[t][q] = r * (G[t][q] - mean - f[t][q] * along);
+      }
+      if (live)
+#pragma unroll
+        for (int t = 0; t < VPT; ++t) c.store(p.df, at, t, G[t]);
     }
   }
   auto write = [&](float (&sum)[VPT][8], float* part) {
@@ -374,7 +395,7 @@ __global__ __launch_bounds__((Shape<LPR, VPT>::THREADS)) void block_backward_ker
     if (S::SLOTS == 1) {
 #pragma unroll
       for (int t = 0; t < VPT; ++t)
-        if (in[t]) store8(to + col[t], left[t], sum[t]);
+        if (c.in[t]) store8(to + c.col[t], c.left[t], sum[t]);
       return;
     }
     __syncthreads();
@@ -383,11 +404,11 @@ __global__ __launch_bounds__((Shape<LPR, VPT>::THREADS)) void block_backward_ker
 #pragma unroll
       for (int q = 0; q < 8; ++q) sums[(slot * VPT + t) * LPR * 8 + lane * 8 + q] = sum[t][q];
     __syncthreads();
-    for (int c = threadIdx.x; c < p.d; c += S::THREADS) {
+    for (int k = threadIdx.x; k < p.d; k += S::THREADS) {
       float s = 0.f;
 #pragma unroll
-      for (int k = 0; k < S::SLOTS; ++k) s += sums[k * VPT * LPR * 8 + c];
-      to[c] = s;
+      for (int n = 0; n < S::SLOTS; ++n) s += sums[n * VPT * LPR * 8 + k];
+      to[k] = s;
     }
   };
   write(sum_next, p.part[0]);
@@ -397,21 +418,26 @@ __global__ __launch_bounds__((Shape<LPR, VPT>::THREADS)) void block_backward_ker
   }
 }
 
-// out[c] (+)= sum of part[k][c] over k < n, for up to three sums: four stretches of k, each in order, these in order
+// out[c] (+)= sum of part[k][c] over k < n, for up to three sums: a thread has every 32nd k, in order, and 32 threads a column, in order
 struct SumArgs { const float* part[3]; float* out[3]; int n, d, accumulate; };
-__global__ __launch_bounds__(256) void block_sums_kernel(SumArgs p) {
-  __shared__ float s[4][64];
-  const int c = blockIdx.x * 64 + (threadIdx.x & 63), k = threadIdx.x >> 6, which = blockIdx.y;
+__global__ __launch_bounds__(1024) void block_sums_kernel(SumArgs p) {
+  __shared__ float s[32][33];
+  const int x = threadIdx.x & 31, k = threadIdx.x >> 5, c = blockIdx.x * 32 + x, which = blockIdx.y;
   const float* const part = which == 0 ? p.part[0] : which == 1 ? p.part[1] : p.part[2];
   float* const out = which == 0 ? p.out[0] : which == 1 ? p.out[1] : p.out[2];
-  float v = 0.f;
-  if (c < p.d)
-    for (int i = k * p.n / 4; i < (k + 1) * p.n / 4; ++i) v += part[(size_t)i * p.d + c];
-  s[k][threadIdx.x & 63] = v;
+  float v[STEM_BLOCK_GRID / 32];   // all in flight together
+#pragma unroll
+  for (int i = 0; i < STEM_BLOCK_GRID / 32; ++i) v[i] = c < p.d && i * 32 + k < p.n ? part[(size_t)(i * 32 + k) * p.d + c] : 0.f;
+  float sum = 0.f;
+#pragma unroll
+  for (int i = 0; i < STEM_BLOCK_GRID / 32; ++i) sum += v[i];
+  s[k][x] = sum;
   __syncthreads();
   if (k == 0 && c < p.d) {
-    v = (s[0][threadIdx.x] + s[1][threadIdx.x]) + (s[2][threadIdx.x] + s[3][threadIdx.x]);
-    out[c] = p.accumulate ? out[c] + v : v;
+    sum = 0.f;
+#pragma unroll
+    for (int i = 0; i < 32; ++i) sum += s[i][x];
+    out[c] = p.accumulate ? out[c] + sum : sum;
   }
 }
 
@@ -443,47 +469,40 @@ __global__ __launch_bounds__(256) void dropout_kernel(const E* x, E* y, int64_t 
 
 // ---- launches ------------------------------------------------------------------------------------------------
 template <class E, int LPR, int VPT, bool BRANCH, bool BACK>
-hipError_t launch(const BlockArgs& a, int64_t most, hipStream_t s, int* grid_out) {
-  typedef Shape<LPR, VPT> S;
-  const int64_t groups = (a.T + S::SLOTS - 1) / S::SLOTS;
+hipError_t launch(const BlockArgs& a, hipStream_t s) {
+  typedef Shape<E, LPR, VPT, BACK> S;
+  const int64_t groups = (a.T + S::SLOTS - 1) / S::SLOTS, most = BACK ? STEM_BLOCK_GRID : 2048 * 256 / S::THREADS;
   const int grid = (int)(groups < most ? groups : most);
-  if (grid_out) *grid_out = grid;
-  BlockArgs p = a;
-  if (BACK) {
-    float* to = a.part[0];
-    const bool want[3] = {a.part_of[0] != nullptr, a.part_of[1] != nullptr, a.part_of[2] != nullptr};
+  if constexpr (BACK) {
+    BlockArgs p = a;
+    SumArgs q = {};
+    int n = 0;
     for (int k = 0; k < 3; ++k) {
-      p.part[k] = want[k] ? to : nullptr;
-      if (want[k]) to += (size_t)grid * a.d;
+      p.part[k] = a.part_of[k] ? a.part[0] + (size_t)n * grid * a.d : nullptr;
+      if (a.part_of[k]) { q.part[n] = p.part[k]; q.out[n++] = a.part_of[k]; }
     }
     block_backward_kernel<E, LPR, VPT, BRANCH><<<grid, S::THREADS, 0, s>>>(p);
     const hipError_t e = hipGetLastError();
-    if (e != hipSuccess) return e;
-    SumArgs q = {};
-    int n = 0;
-    for (int k = 0; k < 3; ++k)
-      if (want[k]) { q.part[n] = p.part[k]; q.out[n++] = a.part_of[k]; }
-    if (n == 0) return hipSuccess;
+    if (e != hipSuccess || n == 0) return e;
     q.n = grid; q.d = a.d; q.accumulate = a.accumulate;
-    block_sums_kernel<<<dim3((a.d + 63) / 64, n), 256, 0, s>>>(q);
+    block_sums_kernel<<<dim3((a.d + 31) / 32, n), 1024, 0, s>>>(q);
   } else {
-    block_forward_kernel<E, LPR, VPT, BRANCH><<<grid, S::THREADS, 0, s>>>(p);
+    block_forward_kernel<E, LPR, VPT, BRANCH><<<grid, S::THREADS, 0, s>>>(a);
   }
   return hipGetLastError();
 }
 
 template <class E, bool BRANCH, bool BACK>
 hipError_t by_width(const BlockArgs& a, hipStream_t s) {
-  const int most = STEM_BLOCK_GRID;
-  if (a.d <= 64) return launch<E, 8, 1, BRANCH, BACK>(a, most, s, nullptr);
-  if (a.d <= 128) return launch<E, 16, 1, BRANCH, BACK>(a, most, s, nullptr);
-  if (a.d <= 256) return launch<E, 32, 1, BRANCH, BACK>(a, most, s, nullptr);
-  if (a.d <= 512) return launch<E, 64, 1, BRANCH, BACK>(a, most, s, nullptr);
-  if (a.d <= 1024) return launch<E, 64, 2, BRANCH, BACK>(a, most, s, nullptr);
-  if (a.d <= 2048) return launch<E, 256, 1, BRANCH, BACK>(a, most, s, nullptr);
-  if (a.d <= 4096) return launch<E, 256, 2, BRANCH, BACK>(a, most, s, nullptr);
-  if (a.d <= 8192) return launch<E, 1024, 1, BRANCH, BACK>(a, most, s, nullptr);
-  return launch<E, 1024, 2, BRANCH, BACK>(a, most, s, nullptr);
+  if (a.d <= 64) return launch<E, 8, 1, BRANCH, BACK>(a, s);
+  if (a.d <= 128) return launch<E, 16, 1, BRANCH, BACK>(a, s);
+  if (a.d <= 256) return launch<E, 32, 1, BRANCH, BACK>(a, s);
+  if (a.d <= 512) return launch<E, 64, 1, BRANCH, BACK>(a, s);
+  if (a.d <= 1024) return launch<E, 64, 2, BRANCH, BACK>(a, s);
+  if (a.d <= 2048) return launch<E, 256, 1, BRANCH, BACK>(a, s);
+  if (a.d <= 4096) return launch<E, 256, 2, BRANCH, BACK>(a, s);
+  if (a.d <= 8192) return launch<E, 1024, 1, BRANCH, BACK>(a, s);
+  return launch<E, 1024, 2, BRANCH, BACK>(a, s);
 }
 
 }  // namespace
