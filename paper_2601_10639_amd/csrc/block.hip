@@ -127,41 +127,6 @@ struct Shape {
   static constexpr bool WHOLE = sizeof(E) == 2;           // rows are whole vectors of 8
 };
 
-// This lane's vectors of a row
-template <class E, int LPR, int VPT, bool BACK>
-struct Columns {
-  bool in[VPT];
-  int col[VPT], left[VPT];
-  __device__ __forceinline__ Columns(int lane, int d) {
-#pragma unroll
-    for (int t = 0; t < VPT; ++t) {
-      col[t] = (t * LPR + lane) * 8;
-      in[t] = col[t] < d;
-      left[t] = d - col[t];
-    }
-  }
-  // whether element q of vector t is the row's
-  __device__ __forceinline__ bool has(int t, int q) const { return in[t] && (Shape<E, LPR, VPT, BACK>::WHOLE || q < left[t]); }
-  __device__ __forceinline__ void load(const void* p, size_t at, float (&v)[VPT][8], float otherwise = 0.f) const {
-#pragma unroll
-    for (int t = 0; t < VPT; ++t) {
-#pragma unroll
-      for (int q = 0; q < 8; ++q) v[t][q] = otherwise;
-      if (p && in[t]) load8(static_cast<const E*>(p) + at + col[t], left[t], v[t]);
-    }
-  }
-  __device__ __forceinline__ void store(void* p, size_t at, int t, const float (&v)[8]) const {
-    if (in[t]) store8(static_cast<E*>(p) + at + col[t], left[t], v);
-  }
-  // v <- v - mean of a row whose sum this is; elements past the row's end are zero and stay zero
-  __device__ __forceinline__ void centre(float (&v)[VPT][8], float mean) const {
-#pragma unroll
-    for (int t = 0; t < VPT; ++t)
-#pragma unroll
-      for (int q = 0; q < 8; ++q) v[t][q] = has(t, q) ? v[t][q] - mean : 0.f;
-  }
-};
-
 template <int VPT>
 __device__ __forceinline__ float sum(const float (&v)[VPT][8]) {
   float s = 0.f;
@@ -180,6 +145,68 @@ __device__ __forceinline__ float dot(const float (&v)[VPT][8], const float (&w)[
     for (int q = 0; q < 8; ++q) s += v[t][q] * w[t][q];
   return s;
 }
+// This lane's vectors of a row
+template <class E, int LPR, int VPT, bool BACK>
+struct Columns {
+  bool in[VPT];
+  int col[VPT], left[VPT];
+  __device__ __forceinline__ Columns(int lane, int d) {
+#pragma unroll
+    for (int t = 0; t < VPT; ++t) {
+      col[t] = (t * LPR + lane) * 8;
+      in[t] = col[t] < d;
+      left[t] = d - col[t];
+    }
+  }
+  // v where the first or second four elements of vector t are the row's, else 0
+  __device__ __forceinline__ float where(int t, int half, float v) const { return in[t] && (Shape<E, LPR, VPT, BACK>::WHOLE || !half || left[t] > 4) ? v : 0.f; }
+  __device__ __forceinline__ void load(const void* p, size_t at, float (&v)[VPT][8], float otherwise = 0.f, bool wanted = true) const {
+#pragma unroll
+    for (int t = 0; t < VPT; ++t) {
+#pragma unroll
+      for (int q = 0; q < 8; ++q) v[t][q] = otherwise;
+      if (p && in[t] && wanted) load8(static_cast<const E*>(p) + at + col[t], left[t], v[t]);
+    }
+  }
+  __device__ __forceinline__ void store(void* p, size_t at, int t, const float (&v)[8]) const {
+    if (in[t]) store8(static_cast<E*>(p) + at + col[t], left[t], v);
+  }
+  // v <- v - mean of a row whose sum this is; elements past the row's end are zero and stay zero
+  __device__ __forceinline__ void centre(float (&v)[VPT][8], float mean) const {
+#pragma unroll
+    for (int t = 0; t < VPT; ++t) {
+      const float m[2] = {where(t, 0, mean), where(t, 1, mean)};
+#pragma unroll
+      for (int q = 0; q < 8; ++q) v[t][q] -= m[q >> 2];
+    }
+  }
+  // G += the gradient of N's input for the gradient h of its output v^; r = 1 / sqrt(...)
+  __device__ __forceinline__ void add_back(float (&G)[VPT][8], const float (&h)[VPT][8], const float (&v)[VPT][8], float r, int kind, float inv_d,
+                                           RowSum<LPR>& row_sum) const {
+    float s[2] = {dot(h, v), 0.f};
+    if (kind == STEM_NORM_LAYER) {
+      s[1] = sum(h);
+      row_sum(s);
+      const float mean = r * s[1] * inv_d;
+#pragma unroll
+      for (int t = 0; t < VPT; ++t) {
+        const float m[2] = {where(t, 0, mean), where(t, 1, mean)};
+#pragma unroll
+        for (int q = 0; q < 8; ++q) G[t][q] -= m[q >> 2];
+      }
+    } else {
+      float one[1] = {s[0]};
+      row_sum(one);
+      s[0] = one[0];
+    }
+    const float along = -r * s[0] * inv_d;
+#pragma unroll
+    for (int t = 0; t < VPT; ++t)
+#pragma unroll
+      for (int q = 0; q < 8; ++q) G[t][q] = __builtin_fmaf(along, v[t][q], __builtin_fmaf(r, h[t][q], G[t][q]));
+  }
+};
+
 template <int VPT>
 __device__ __forceinline__ void scale_by(float (&v)[VPT][8], float r) {
 #pragma unroll
@@ -277,9 +304,9 @@ __global__ __launch_bounds__((Shape<E, LPR, VPT, false>::THREADS)) void block_fo
 }
 
 // ---- backward ------------------------------------------------------------------------------------------
-// Sums over tokens (of dw_next, dw_out and a gate a channel) are held in registers over a workgroup's rows and written as one partial
-// sum a workgroup, [sum][workgroup][d]; block_sums_kernel adds those in order.  No atomics: the same bits on every run.  All of a row is
-// requested before its first reduction.
+// Sums over tokens are held in registers over a workgroup's rows and written as one partial sum a workgroup, [sum][workgroup][d];
+// block_sums_kernel adds those in order.  No atomics: the same bits on every run.  dw_out and the gradient of a gate a channel are the same
+// sum, of h times the kept N_out(f), times the gate and times w_out: it is held once.  All of a row is requested before its first reduction.
 template <class E, int LPR, int VPT, bool BRANCH>
 __global__ __launch_bounds__((Shape<E, LPR, VPT, true>::THREADS)) void block_backward_kernel(BlockArgs p) {
   typedef Shape<E, LPR, VPT, true> S;
@@ -290,40 +317,43 @@ __global__ __launch_bounds__((Shape<E, LPR, VPT, true>::THREADS)) void block_bac
   const Columns<E, LPR, VPT, true> c(lane, p.d);
   const uint64_t offset = BRANCH && p.drop.threshold ? offset_of(p.drop) : 0;
   const bool by_channel = p.gate_kind == STEM_GATE_CHANNEL, by_element = p.gate_kind == STEM_GATE_FULL, by_token = p.gate_kind == STEM_GATE_TOKEN;
-  float sum_next[VPT][8], sum_out[VPT][8], sum_gate[VPT][8];
+  float sum_next[VPT][8] = {}, sum_branch[VPT][8] = {};
+  float after[VPT][8], branch[VPT][8];      // w_next; w_out times a gate a channel
+  c.load(p.next.weight, 0, after, 1.f);
+  auto branch_weight = [&](float (&w)[VPT][8], bool weight, bool gate) __attribute__((always_inline)) {
+    c.load(weight ? p.out.weight : nullptr, 0, w, 1.f);
+    if (gate && by_channel) {
+      float g[VPT][8];
+      c.load(p.gate, 0, g);
 #pragma unroll
-  for (int t = 0; t < VPT; ++t)
+      for (int t = 0; t < VPT; ++t)
 #pragma unroll
-    for (int q = 0; q < 8; ++q) sum_next[t][q] = sum_out[t][q] = sum_gate[t][q] = 0.f;
+        for (int q = 0; q < 8; ++q) w[t][q] *= g[t][q];
+    }
+  };
+  if (BRANCH) branch_weight(branch, true, true);
   const float of_branch = p.branch_scale * (p.drop.threshold ? p.drop.scale : 1.f);
   for (int64_t base = (int64_t)blockIdx.x * S::SLOTS; base < p.T; base += (int64_t)gridDim.x * S::SLOTS) {
-    const bool live = base + slot < p.T;
+    const bool live = base + slot < p.T;    // a slot without a row has zeros in all places, and adds zeros
     const int64_t row = live ? base + slot : p.T - 1;
     const size_t at = (size_t)row * p.d;
     float G[VPT][8], f[VPT][8];
-    c.load(p.dy, at, G);
-    if (BRANCH) c.load(p.f, at, f);
+    c.load(p.dy, at, G, 0.f, live);
+    if (BRANCH) c.load(p.f, at, f, 0.f, live);
     if (p.dn) {
-      float y[VPT][8], h[VPT][8], w[VPT][8];
-      c.load(p.x, at, y);
-      c.load(p.dn, at, h);
-      c.load(p.next.weight, 0, w, 1.f);
-      const float r = factor(c, y, p.next, p.inv_d, row_sum);
-      scale_by(y, r);
+      float y[VPT][8], h[VPT][8];
+      c.load(p.x, at, y, 0.f, live);
+      c.load(p.dn, at, h, 0.f, live);
+      const float r = factor(c, y, p.next, p.inv_d, row_sum), r_live = live ? r : 0.f;
+      scale_by(y, r_live);
 #pragma unroll
       for (int t = 0; t < VPT; ++t)
 #pragma unroll
         for (int q = 0; q < 8; ++q) {
-          sum_next[t][q] += live ? h[t][q] * y[t][q] : 0.f;
-          h[t][q] *= w[t][q];
+          sum_next[t][q] = __builtin_fmaf(h[t][q], y[t][q], sum_next[t][q]);
+          h[t][q] *= after[t][q];
         }
-      float s[2] = {dot(h, y), p.next.kind == STEM_NORM_LAYER ? sum(h) : 0.f};
-      row_sum(s);
-      const float along = s[0] * p.inv_d, mean = s[1] * p.inv_d;
-#pragma unroll
-      for (int t = 0; t < VPT; ++t)
-#pragma unroll
-        for (int q = 0; q < 8; ++q) G[t][q] += c.has(t, q) ? r * (h[t][q] - mean - y[t][q] * along) : 0.f;
+      c.add_back(G, h, y, r_live, p.next.kind, p.inv_d, row_sum);
     }
     auto store_dx = [&](int t) __attribute__((always_inline)) {   // of a vector whose inputs have all been read: dx may be any of them
       if (!p.dx || !live) return;
@@ -341,33 +371,49 @@ __global__ __launch_bounds__((Shape<E, LPR, VPT, true>::THREADS)) void block_bac
     float r = 1.f;
     if (p.f && p.out.kind != STEM_NORM_NONE) {
       r = factor(c, f, p.out, p.inv_d, row_sum);
+      if (!live) r = 0.f;
       scale_by(f, r);
     }
-    const float of_token = by_token ? load1(static_cast<const E*>(p.gate) + row) : 1.f;
+    const float of_row = by_token ? load1(static_cast<const E*>(p.gate) + row) : 1.f;
     float token_gate = 0.f;
 #pragma unroll
     for (int t = 0; t < VPT; ++t) {
-      if (!c.in[t]) continue;
-      float w[8], g[8], dg[8];
+      float g[8], dg[8];
+      if (by_element) {
 #pragma unroll
-      for (int q = 0; q < 8; ++q) { w[q] = 1.f; g[q] = of_token; }
-      if (p.out.weight) load8(static_cast<const E*>(p.out.weight) + c.col[t], c.left[t], w);
-      if (by_channel || by_element) load8(static_cast<const E*>(p.gate) + (by_element ? at : 0) + c.col[t], c.left[t], g);
+        for (int q = 0; q < 8; ++q) g[q] = 0.f;
+        if (c.in[t] && live) load8(static_cast<const E*>(p.gate) + at + c.col[t], c.left[t], g);
+      }
       store_dx(t);
-      Bits b = {};
-      if (p.drop.threshold) b = philox((uint32_t)(c.col[t] >> 3), (uint32_t)row, offset, p.drop.seed);
+#pragma unroll
+      for (int q = 0; q < 8; ++q) G[t][q] *= of_branch;
+      // (what is dropped counts for nothing, whatever f holds there)
+      float u[8];
+#pragma unroll
+      for (int q = 0; q < 8; ++q) u[q] = f[t][q];
+      if (p.drop.threshold) {
+        const Bits b = philox((uint32_t)(c.col[t] >> 3), (uint32_t)row, offset, p.drop.seed);
+#pragma unroll
+        for (int q = 0; q < 8; ++q) {
+          const bool keep = kept(b, q, p.drop.threshold);
+          G[t][q] = keep ? G[t][q] : 0.f;
+          u[q] = keep ? u[q] : 0.f;
+        }
+      }
+      if (by_token || by_element) {          // (branch is w_out alone)
+#pragma unroll
+        for (int q = 0; q < 8; ++q) {
+          dg[q] = G[t][q] * (u[q] * branch[t][q]);
+          token_gate += dg[q];
+          G[t][q] *= by_element ? g[q] : of_row;
+        }
+        if (by_element && p.dgate && live) c.store(p.dgate, at, t, dg);
+      }
 #pragma unroll
       for (int q = 0; q < 8; ++q) {
-        // (what is dropped counts for nothing, whatever f holds there)
-        const bool keep = kept(b, q, p.drop.threshold) && live;
-        const float h = keep ? of_branch * G[t][q] : 0.f, u = keep ? f[t][q] : 0.f, du = h * g[q];
-        dg[q] = h * (u * w[q]);
-        sum_out[t][q] += du * u;
-        sum_gate[t][q] += dg[q];
-        if (c.has(t, q)) token_gate += dg[q];
-        G[t][q] = c.has(t, q) ? du * w[q] : 0.f;
+        sum_branch[t][q] = __builtin_fmaf(G[t][q], u[q], sum_branch[t][q]);
+        G[t][q] *= branch[t][q];
       }
-      if (by_element && p.dgate && live) c.store(p.dgate, at, t, dg);
     }
     if (by_token && p.dgate) {
       float s[1] = {token_gate};
@@ -376,21 +422,18 @@ __global__ __launch_bounds__((Shape<E, LPR, VPT, true>::THREADS)) void block_bac
     }
     if (p.df) {
       if (p.out.kind != STEM_NORM_NONE) {
-        float s[2] = {dot(G, f), p.out.kind == STEM_NORM_LAYER ? sum(G) : 0.f};
-        row_sum(s);
-        const float along = s[0] * p.inv_d, mean = s[1] * p.inv_d;
+        float o[VPT][8] = {};
+        c.add_back(o, G, f, r, p.out.kind, p.inv_d, row_sum);
+        if (live)
 #pragma unroll
-        for (int t = 0; t < VPT; ++t)
-#pragma unroll
-          for (int q = 0; q < 8; ++q) G[t][q] = r * (G[t][q] - mean - f[t][q] * along);
-      }
-      if (live)
+          for (int t = 0; t < VPT; ++t) c.store(p.df, at, t, o[t]);
+      } else if (live) {
 #pragma unroll
         for (int t = 0; t < VPT; ++t) c.store(p.df, at, t, G[t]);
+      }
     }
   }
-  auto write = [&](float (&sum)[VPT][8], float* part) {
-    if (!part) return;
+  auto write = [&](const float (&sum)[VPT][8], float* part) __attribute__((always_inline)) {
     float* const to = part + (size_t)blockIdx.x * p.d;
     if (S::SLOTS == 1) {
 #pragma unroll
@@ -411,10 +454,19 @@ __global__ __launch_bounds__((Shape<E, LPR, VPT, true>::THREADS)) void block_bac
       to[k] = s;
     }
   };
-  write(sum_next, p.part[0]);
+  if (p.part[0]) write(sum_next, p.part[0]);
   if (BRANCH) {
-    write(sum_out, p.part[1]);
-    write(sum_gate, p.part[2]);
+#pragma unroll 1
+    for (int which = 1; which < 3; ++which) {
+      if (!p.part[which]) continue;
+      float w[VPT][8];
+      branch_weight(w, which == 2, which == 1);
+#pragma unroll
+      for (int t = 0; t < VPT; ++t)
+#pragma unroll
+        for (int q = 0; q < 8; ++q) w[t][q] *= sum_branch[t][q];
+      write(w, p.part[which]);
+    }
   }
 }
 
@@ -498,9 +550,9 @@ hipError_t by_width(const BlockArgs& a, hipStream_t s) {
   if (a.d <= 128) return launch<E, 16, 1, BRANCH, BACK>(a, s);
   if (a.d <= 256) return launch<E, 32, 1, BRANCH, BACK>(a, s);
   if (a.d <= 512) return launch<E, 64, 1, BRANCH, BACK>(a, s);
-  if (a.d <= 1024) return launch<E, 64, 2, BRANCH, BACK>(a, s);
+  if (a.d <= 1024) return launch<E, BACK ? 128 : 64, BACK ? 1 : 2, BRANCH, BACK>(a, s);
   if (a.d <= 2048) return launch<E, 256, 1, BRANCH, BACK>(a, s);
-  if (a.d <= 4096) return launch<E, 256, 2, BRANCH, BACK>(a, s);
+  if (a.d <= 4096) return launch<E, BACK ? 512 : 256, BACK ? 1 : 2, BRANCH, BACK>(a, s);
   if (a.d <= 8192) return launch<E, 1024, 1, BRANCH, BACK>(a, s);
   return launch<E, 1024, 2, BRANCH, BACK>(a, s);
 }
