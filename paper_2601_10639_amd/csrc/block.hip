@@ -13,8 +13,13 @@
 #include "block.h"
 
 typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8_t;
+typedef __attribute__((ext_vector_type(4))) uint32_t u32x4_t;
+typedef __attribute__((ext_vector_type(2))) uint32_t u32x2_t;
+typedef __amdgpu_buffer_rsrc_t rsrc_t;
 
 namespace {
+
+constexpr uint32_t OOB = 0x80000000u;   // a buffer offset beyond any row: reads as zero, is not stored
 
 // ---- eight consecutive elements of a row, in fp32 --------------------------------------------------
 // `left`: elements of the row from p on, 4 or more (an fp32 row ends on a multiple of 4, a bf16 row on one of 64)
@@ -75,7 +80,6 @@ template <int CTRL>
 __device__ __forceinline__ float add_dpp(float v) {
   return v + __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(v), CTRL, 0xf, 0xf, true));
 }
-typedef __attribute__((ext_vector_type(2))) uint32_t u32x2_t;
 template <int LPR>
 struct RowSum {
   static constexpr int WPR = LPR > 64 ? LPR / 64 : 1;   // wavefronts that share a row
@@ -145,31 +149,68 @@ __device__ __forceinline__ float dot(const float (&v)[VPT][8], const float (&w)[
     for (int q = 0; q < 8; ++q) s += v[t][q] * w[t][q];
   return s;
 }
+// The rows that a workgroup has in hand, of one tensor: a buffer that ends behind them and behind the tensor, so that a slot without a row
+// reads zeros and stores nothing, as do lanes behind a row's end, and all of a tensor that is not there.  No branches.
+template <class E>
+__device__ __forceinline__ rsrc_t rows_of(const void* p, int64_t base, int slots, const BlockArgs& a) {
+  const int64_t left = a.T - base;
+  return __builtin_amdgcn_make_buffer_rsrc(const_cast<E*>(static_cast<const E*>(p)) + base * a.d, 0,
+                                           p ? (int)((left < slots ? left : slots) * a.d * sizeof(E)) : 0, 0x00020000);
+}
+
 // This lane's vectors of a row
 template <class E, int LPR, int VPT, bool BACK>
 struct Columns {
   bool in[VPT];
   int col[VPT], left[VPT];
-  __device__ __forceinline__ Columns(int lane, int d) {
+  uint32_t off[VPT], off2[VPT];     // of the vector in rows_of(), and of its second half
+  __device__ __forceinline__ Columns(int slot, int lane, int d) {
 #pragma unroll
     for (int t = 0; t < VPT; ++t) {
       col[t] = (t * LPR + lane) * 8;
       in[t] = col[t] < d;
       left[t] = d - col[t];
+      off[t] = in[t] ? (uint32_t)((slot * d + col[t]) * sizeof(E)) : OOB;
+      off2[t] = left[t] > 4 ? off[t] + 16 : OOB;
     }
   }
   // v where the first or second four elements of vector t are the row's, else 0
   __device__ __forceinline__ float where(int t, int half, float v) const { return in[t] && (Shape<E, LPR, VPT, BACK>::WHOLE || !half || left[t] > 4) ? v : 0.f; }
-  __device__ __forceinline__ void load(const void* p, size_t at, float (&v)[VPT][8], float otherwise = 0.f, bool wanted = true) const {
+  __device__ __forceinline__ void load1(rsrc_t r, int t, float (&v)[8]) const {
+    const u32x4_t a = __builtin_amdgcn_raw_buffer_load_b128(r, off[t], 0, 0);
+    if (sizeof(E) == 2) {
+#pragma unroll
+      for (int q = 0; q < 8; ++q) v[q] = __uint_as_float(q & 1 ? a[q >> 1] & 0xffff0000u : a[q >> 1] << 16);
+    } else {
+      const u32x4_t b = __builtin_amdgcn_raw_buffer_load_b128(r, off2[t], 0, 0);
+#pragma unroll
+      for (int q = 0; q < 8; ++q) v[q] = __uint_as_float(q < 4 ? a[q] : b[q - 4]);
+    }
+  }
+  __device__ __forceinline__ void load(rsrc_t r, float (&v)[VPT][8]) const {
+#pragma unroll
+    for (int t = 0; t < VPT; ++t) load1(r, t, v[t]);
+  }
+  __device__ __forceinline__ void store(rsrc_t r, int t, const float (&v)[8]) const {
+    if (sizeof(E) == 2) {
+      bf16x8_t u;
+#pragma unroll
+      for (int q = 0; q < 8; ++q) u[q] = (__bf16)v[q];
+      __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4_t, u), r, off[t], 0, 0);
+    } else {
+      const float4 a = make_float4(v[0], v[1], v[2], v[3]), b = make_float4(v[4], v[5], v[6], v[7]);
+      __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4_t, a), r, off[t], 0, 0);
+      __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4_t, b), r, off2[t], 0, 0);
+    }
+  }
+  // a weight of each channel, 1 where there is none
+  __device__ __forceinline__ void weight(const void* p, float (&v)[VPT][8]) const {
 #pragma unroll
     for (int t = 0; t < VPT; ++t) {
 #pragma unroll
-      for (int q = 0; q < 8; ++q) v[t][q] = otherwise;
-      if (p && in[t] && wanted) load8(static_cast<const E*>(p) + at + col[t], left[t], v[t]);
+      for (int q = 0; q < 8; ++q) v[t][q] = 1.f;
+      if (p && in[t]) load8(static_cast<const E*>(p) + col[t], left[t], v[t]);
     }
-  }
-  __device__ __forceinline__ void store(void* p, size_t at, int t, const float (&v)[8]) const {
-    if (in[t]) store8(static_cast<E*>(p) + at + col[t], left[t], v);
   }
   // v <- v - mean of a row whose sum this is; elements past the row's end are zero and stay zero
   __device__ __forceinline__ void centre(float (&v)[VPT][8], float mean) const {
@@ -239,37 +280,35 @@ __global__ __launch_bounds__((Shape<E, LPR, VPT, false>::THREADS)) void block_fo
   __shared__ float red[S::SLOTS][2][S::WPR][2];
   const int slot = threadIdx.x / LPR, lane = threadIdx.x % LPR;
   RowSum<LPR> row_sum{red[slot], 0};
-  const Columns<E, LPR, VPT, false> c(lane, p.d);
+  const Columns<E, LPR, VPT, false> c(slot, lane, p.d);
   const uint64_t offset = BRANCH && p.drop.threshold ? offset_of(p.drop) : 0;
   const bool by_channel = p.gate_kind == STEM_GATE_CHANNEL, by_element = p.gate_kind == STEM_GATE_FULL, by_token = p.gate_kind == STEM_GATE_TOKEN;
   float branch[VPT][8], after[VPT][8];
   if (BRANCH) {
-    c.load(p.out.weight, 0, branch, 1.f);
+    c.weight(p.out.weight, branch);
     if (by_channel) {
       float g[VPT][8];
-      c.load(p.gate, 0, g);
+      c.weight(p.gate, g);
 #pragma unroll
       for (int t = 0; t < VPT; ++t)
 #pragma unroll
         for (int q = 0; q < 8; ++q) branch[t][q] *= g[t][q];
     }
   }
-  c.load(p.next.weight, 0, after, 1.f);
+  c.weight(p.next.weight, after);
   const float of_branch = p.branch_scale * (p.drop.threshold ? p.drop.scale : 1.f);
   for (int64_t base = (int64_t)blockIdx.x * S::SLOTS; base < p.T; base += (int64_t)gridDim.x * S::SLOTS) {
-    const bool live = base + slot < p.T;
-    const int64_t row = live ? base + slot : p.T - 1;
-    const size_t at = (size_t)row * p.d;
+    const int64_t row = base + slot;
     float y[VPT][8];
-    c.load(p.x, at, y);
+    c.load(rows_of<E>(p.x, base, S::SLOTS, p), y);
     if (BRANCH) {
       float f[VPT][8];
-      c.load(p.f, at, f);
+      c.load(rows_of<E>(p.f, base, S::SLOTS, p), f);
       float r = of_branch;
-      if (by_token) r *= load1(static_cast<const E*>(p.gate) + row);
+      if (by_token) r *= load1(static_cast<const E*>(p.gate) + (row < p.T ? row : p.T - 1));
       if (by_element) {
         float g[VPT][8];
-        c.load(p.gate, at, g);
+        c.load(rows_of<E>(p.gate, base, S::SLOTS, p), g);
         if (p.out.kind != STEM_NORM_NONE) r *= factor(c, f, p.out, p.inv_d, row_sum);
 #pragma unroll
         for (int t = 0; t < VPT; ++t)
@@ -278,6 +317,7 @@ __global__ __launch_bounds__((Shape<E, LPR, VPT, false>::THREADS)) void block_fo
       } else if (p.out.kind != STEM_NORM_NONE) {
         r *= factor(c, f, p.out, p.inv_d, row_sum);
       }
+      const rsrc_t ry = rows_of<E>(p.y, base, S::SLOTS, p);
 #pragma unroll
       for (int t = 0; t < VPT; ++t) {
         if (p.drop.threshold) {
@@ -288,16 +328,17 @@ __global__ __launch_bounds__((Shape<E, LPR, VPT, false>::THREADS)) void block_fo
 #pragma unroll
           for (int q = 0; q < 8; ++q) y[t][q] = p.residual_scale * y[t][q] + f[t][q] * branch[t][q] * r;
         }
-        if (live) c.store(p.y, at, t, y[t]);
+        c.store(ry, t, y[t]);
       }
     }
     if (p.n) {
       if (p.next.kind != STEM_NORM_NONE) scale_by(y, factor(c, y, p.next, p.inv_d, row_sum));
+      const rsrc_t rn = rows_of<E>(p.n, base, S::SLOTS, p);
 #pragma unroll
       for (int t = 0; t < VPT; ++t) {
 #pragma unroll
         for (int q = 0; q < 8; ++q) y[t][q] *= after[t][q];
-        if (live) c.store(p.n, at, t, y[t]);
+        c.store(rn, t, y[t]);
       }
     }
   }
@@ -314,17 +355,17 @@ __global__ __launch_bounds__((Shape<E, LPR, VPT, true>::THREADS)) void block_bac
   __shared__ float sums[S::SLOTS > 1 ? S::THREADS * VPT * 8 : 1];
   const int slot = threadIdx.x / LPR, lane = threadIdx.x % LPR;
   RowSum<LPR> row_sum{red[slot], 0};
-  const Columns<E, LPR, VPT, true> c(lane, p.d);
+  const Columns<E, LPR, VPT, true> c(slot, lane, p.d);
   const uint64_t offset = BRANCH && p.drop.threshold ? offset_of(p.drop) : 0;
   const bool by_channel = p.gate_kind == STEM_GATE_CHANNEL, by_element = p.gate_kind == STEM_GATE_FULL, by_token = p.gate_kind == STEM_GATE_TOKEN;
   float sum_next[VPT][8] = {}, sum_branch[VPT][8] = {};
   float after[VPT][8], branch[VPT][8];      // w_next; w_out times a gate a channel
-  c.load(p.next.weight, 0, after, 1.f);
+  c.weight(p.next.weight, after);
   auto branch_weight = [&](float (&w)[VPT][8], bool weight, bool gate) __attribute__((always_inline)) {
-    c.load(weight ? p.out.weight : nullptr, 0, w, 1.f);
+    c.weight(weight ? p.out.weight : nullptr, w);
     if (gate && by_channel) {
       float g[VPT][8];
-      c.load(p.gate, 0, g);
+      c.weight(p.gate, g);
 #pragma unroll
       for (int t = 0; t < VPT; ++t)
 #pragma unroll
@@ -334,16 +375,16 @@ __global__ __launch_bounds__((Shape<E, LPR, VPT, true>::THREADS)) void block_bac
   if (BRANCH) branch_weight(branch, true, true);
   const float of_branch = p.branch_scale * (p.drop.threshold ? p.drop.scale : 1.f);
   for (int64_t base = (int64_t)blockIdx.x * S::SLOTS; base < p.T; base += (int64_t)gridDim.x * S::SLOTS) {
-    const bool live = base + slot < p.T;    // a slot without a row has zeros in all places, and adds zeros
-    const int64_t row = live ? base + slot : p.T - 1;
-    const size_t at = (size_t)row * p.d;
+    const int64_t row = base + slot;
+    const bool live = row < p.T;            // a slot without a row has zeros in all places, and adds zeros
+    auto rows = [&](const void* t) __attribute__((always_inline)) { return rows_of<E>(t, base, S::SLOTS, p); };
     float G[VPT][8], f[VPT][8];
-    c.load(p.dy, at, G, 0.f, live);
-    if (BRANCH) c.load(p.f, at, f, 0.f, live);
+    c.load(rows(p.dy), G);
+    if (BRANCH) c.load(rows(p.f), f);
     if (p.dn) {
       float y[VPT][8], h[VPT][8];
-      c.load(p.x, at, y, 0.f, live);
-      c.load(p.dn, at, h, 0.f, live);
+      c.load(rows(p.x), y);
+      c.load(rows(p.dn), h);
       const float r = factor(c, y, p.next, p.inv_d, row_sum), r_live = live ? r : 0.f;
       scale_by(y, r_live);
 #pragma unroll
@@ -355,12 +396,12 @@ __global__ __launch_bounds__((Shape<E, LPR, VPT, true>::THREADS)) void block_bac
         }
       c.add_back(G, h, y, r_live, p.next.kind, p.inv_d, row_sum);
     }
+    const rsrc_t rdx = rows(p.dx);
     auto store_dx = [&](int t) __attribute__((always_inline)) {   // of a vector whose inputs have all been read: dx may be any of them
-      if (!p.dx || !live) return;
       float o[8];
 #pragma unroll
       for (int q = 0; q < 8; ++q) o[q] = p.residual_scale * G[t][q];
-      c.store(p.dx, at, t, o);
+      c.store(rdx, t, o);
     };
     if (!BRANCH) {
 #pragma unroll
@@ -374,16 +415,12 @@ __global__ __launch_bounds__((Shape<E, LPR, VPT, true>::THREADS)) void block_bac
       if (!live) r = 0.f;
       scale_by(f, r);
     }
-    const float of_row = by_token ? load1(static_cast<const E*>(p.gate) + row) : 1.f;
+    const float of_row = by_token ? load1(static_cast<const E*>(p.gate) + (live ? row : p.T - 1)) : 1.f;
     float token_gate = 0.f;
 #pragma unroll
     for (int t = 0; t < VPT; ++t) {
       float g[8], dg[8];
-      if (by_element) {
-#pragma unroll
-        for (int q = 0; q < 8; ++q) g[q] = 0.f;
-        if (c.in[t] && live) load8(static_cast<const E*>(p.gate) + at + c.col[t], c.left[t], g);
-      }
+      if (by_element) c.load1(rows(p.gate), t, g);
       store_dx(t);
 #pragma unroll
       for (int q = 0; q < 8; ++q) G[t][q] *= of_branch;
@@ -407,7 +444,7 @@ __global__ __launch_bounds__((Shape<E, LPR, VPT, true>::THREADS)) void block_bac
           token_gate += dg[q];
           G[t][q] *= by_element ? g[q] : of_row;
         }
-        if (by_element && p.dgate && live) c.store(p.dgate, at, t, dg);
+        if (by_element) c.store(rows(p.dgate), t, dg);
       }
 #pragma unroll
       for (int q = 0; q < 8; ++q) {
@@ -424,12 +461,11 @@ __global__ __launch_bounds__((Shape<E, LPR, VPT, true>::THREADS)) void block_bac
       if (p.out.kind != STEM_NORM_NONE) {
         float o[VPT][8] = {};
         c.add_back(o, G, f, r, p.out.kind, p.inv_d, row_sum);
-        if (live)
 #pragma unroll
-          for (int t = 0; t < VPT; ++t) c.store(p.df, at, t, o[t]);
-      } else if (live) {
+        for (int t = 0; t < VPT; ++t) c.store(rows(p.df), t, o[t]);
+      } else {
 #pragma unroll
-        for (int t = 0; t < VPT; ++t) c.store(p.df, at, t, G[t]);
+        for (int t = 0; t < VPT; ++t) c.store(rows(p.df), t, G[t]);
       }
     }
   }
