@@ -18,6 +18,7 @@
 namespace {
 
 PyObject *g_ctx_type, *g_get_device, *g_raw_stream, *g_handle, *g_value, *g_dtype, *g_cuda_stream;   // set by setup()
+PyObject *g_norm_type, *g_leave_type, *g_quant_type, *g_facts, *g_d_model, *g_d_ff, *g_q, *g_scale, *g_N, *g_K;
 bool g_off = true;                                        // before setup(), and in a forked process
 
 struct Unusual {};
@@ -30,27 +31,87 @@ struct Hold {                  // a new reference, or Unusual
   ~Hold() { Py_DECREF(o); }
 };
 
-enum Kind { ACT, F32, I32 };   // ACT: the context's type
+enum Kind { ACT, F32, I32, I64, I8 };   // ACT: the context's type
+
+// The memory of one of stemlib.py's ctypes structures, of exactly this type
+template <class T>
+const T* structure(PyObject* o, PyObject* type) {
+  if (reinterpret_cast<PyObject*>(Py_TYPE(o)) != type) throw Unusual();
+  Py_buffer b;
+  if (PyObject_GetBuffer(o, &b, PyBUF_SIMPLE) < 0) {
+    PyErr_Clear();
+    throw Unusual();
+  }
+  void* const p = b.buf;
+  const bool whole = b.len == (Py_ssize_t)sizeof(T);
+  PyBuffer_Release(&b);        // (the object, which the caller's arguments hold, keeps its memory)
+  if (!whole) throw Unusual();
+  return static_cast<const T*>(p);
+}
 
 // The arguments of one call
 struct Args {
   PyObject* const* v;
+  PyObject* ctx;
   int dtype;
   mutable bool device_seen;    // a device tensor is among them: the runtime is up
 
   template <class T = void>
-  T* ptr(int i, Kind kind) const {
-    PyObject* const o = v[i];
+  T* ptr(int i, Kind kind) const { return static_cast<T*>(pointer_of(v[i], kind, -1, -1)); }
+  // of this shape: [rows, cols], or [rows] where cols is -1
+  template <class T = void>
+  T* shaped(int i, Kind kind, int64_t rows, int64_t cols = -1) const { return static_cast<T*>(pointer_of(v[i], kind, rows, cols)); }
+
+  void* pointer_of(PyObject* o, Kind kind, int64_t rows, int64_t cols) const {
     if (o == Py_None) return nullptr;
     if (!THPVariable_CheckExact(o)) throw Unusual();
     const at::Tensor& t = THPVariable_Unpack(o);
-    const at::ScalarType want = kind == I32 ? at::kInt : kind == ACT && dtype == STEM_BF16 ? at::kBFloat16 : at::kFloat;
+    if (rows >= 0 && (t.dim() != (cols < 0 ? 1 : 2) || t.size(0) != rows || (cols >= 0 && t.size(1) != cols))) throw Unusual();
+    const at::ScalarType want = kind == I32 ? at::kInt : kind == I64 ? at::kLong : kind == I8 ? at::kChar
+                                : kind == ACT && dtype == STEM_BF16 ? at::kBFloat16 : at::kFloat;
     if (t.layout() != at::kStrided || t.scalar_type() != want || !t.is_cuda() || !t.is_contiguous()) throw Unusual();
     device_seen = true;
     // (as data_ptr() in Python: a tensor that shares its storage with another until one is written gets its own first.  Inputs too, as a
     // call may write to the same tensor)
-    return static_cast<T*>(t.mutable_data_ptr());
+    return t.mutable_data_ptr();
   }
+
+  int64_t attribute(PyObject* o, PyObject* name) const { return as_integer(Hold(PyObject_GetAttr(o, name)).o); }
+  // what a structure's tensors were when it was made
+  template <int N>
+  void facts(PyObject* o, int64_t (&f)[N]) const {
+    const Hold t(PyObject_GetAttr(o, g_facts));
+    if (!PyTuple_CheckExact(t.o) || PyTuple_GET_SIZE(t.o) != N) throw Unusual();
+    for (int k = 0; k < N; ++k) f[k] = as_integer(PyTuple_GET_ITEM(t.o, k));
+  }
+  // a norm of rows of `width` (None: none)
+  const stem_norm* norm(int i, int64_t width) const {
+    if (v[i] == Py_None) return nullptr;
+    const stem_norm* const n = structure<stem_norm>(v[i], g_norm_type);
+    int64_t f[2];              // elements of the weight (-1: none) and its type
+    facts(v[i], f);
+    if (f[0] >= 0 && (f[0] != width || f[1] != dtype)) throw Unusual();
+    return n;
+  }
+  const stem_leave* leave(int i, int64_t T, int64_t d) const {
+    const stem_leave* const L = structure<stem_leave>(v[i], g_leave_type);
+    int64_t f[5];              // elements of w_out and w_next, the gate's sides, the type of all that is there
+    facts(v[i], f);
+    const int64_t g0 = L->gate_kind == STEM_GATE_CHANNEL ? d : T, g1 = L->gate_kind == STEM_GATE_FULL ? d : -1;
+    if ((f[0] >= 0 && f[0] != d) || (f[1] >= 0 && f[1] != d) || (f[2] >= 0 && (f[2] != g0 || f[3] != g1)) || (f[4] != -1 && f[4] != dtype))
+      throw Unusual();
+    return L;
+  }
+  // weights in 8 bits
+  struct Quant { const void* q; const float* scale; int64_t N, K; };
+  Quant quant(int i) const {
+    if (reinterpret_cast<PyObject*>(Py_TYPE(v[i])) != g_quant_type) throw Unusual();
+    const int64_t N = attribute(v[i], g_N), K = attribute(v[i], g_K);
+    const Hold q(PyObject_GetAttr(v[i], g_q)), scale(PyObject_GetAttr(v[i], g_scale));
+    return {pointer_of(q.o, I8, stem_quant_bytes(N, K), -1), static_cast<const float*>(pointer_of(scale.o, F32, N, -1)), N, K};
+  }
+  int64_t d_model() const { return attribute(ctx, g_d_model); }
+  int64_t d_ff() const { return attribute(ctx, g_d_ff); }
 
   static int64_t as_integer(PyObject* o) {
     if (!PyLong_CheckExact(o)) throw Unusual();
@@ -70,9 +131,9 @@ struct Args {
   }
   void* pointer(int i) const { return v[i] == Py_None ? nullptr : reinterpret_cast<void*>(integer(i)); }
 
-  // argument i, or where it is None the rows of tensor t (0 where that is None and may be)
+  // argument i (-1: there is none), or where it is None the rows of tensor t (0 where that is None and may be)
   int64_t rows(int i, int t, bool none_is_0 = false) const {
-    if (v[i] != Py_None) return integer(i);
+    if (i >= 0 && v[i] != Py_None) return integer(i);
     if (v[t] == Py_None && none_is_0) return 0;
     if (!THPVariable_CheckExact(v[t])) throw Unusual();
     const at::Tensor& x = THPVariable_Unpack(v[t]);
@@ -98,7 +159,7 @@ PyObject* enter(PyObject* const* args, Py_ssize_t n, Py_ssize_t want, F f) {
   try {
     const Hold handle(PyObject_GetAttr(args[0], g_handle)), value(PyObject_GetAttr(handle.o, g_value)), dtype(PyObject_GetAttr(args[0], g_dtype));
     stem_ctx* const c = reinterpret_cast<stem_ctx*>(Args::as_integer(value.o));   // (closed: None)
-    const Args a{args + 1, (int)Args::as_integer(dtype.o), false};
+    const Args a{args + 1, args[0], (int)Args::as_integer(dtype.o), false};
     auto call = f(a, c);
     stem_status st;
     Py_BEGIN_ALLOW_THREADS
@@ -194,10 +255,90 @@ PyObject* embed_sparse_adamw(PyObject*, PyObject* const* args, Py_ssize_t n) {
   });
 }
 
-// (StemCtx, torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream)
+PyObject* block_enter_forward(PyObject*, PyObject* const* args, Py_ssize_t n) {
+  return enter(args, n, 4, [](const Args& a, stem_ctx* c) {
+    const int64_t T = a.rows(-1, 0), d = a.d_model();
+    auto x = a.shaped(0, ACT, T, d); auto norm = a.norm(1, d); auto to = a.shaped(2, ACT, T, d); auto s = a.stream(3);
+    return [=] { return stem_block_enter_forward(c, x, T, norm, to, s); };
+  });
+}
+
+PyObject* block_enter_backward(PyObject*, PyObject* const* args, Py_ssize_t n) {
+  return enter(args, n, 8, [](const Args& a, stem_ctx* c) {
+    const int64_t T = a.rows(-1, 1), d = a.d_model();
+    auto dn = a.shaped(0, ACT, T, d); auto x = a.shaped(1, ACT, T, d); auto norm = a.norm(2, d); auto dx = a.shaped(3, ACT, T, d);
+    auto dw = a.shaped<float>(4, F32, d); auto dres = a.shaped(5, ACT, T, d); const int accumulate = a.flag(6); auto s = a.stream(7);
+    return [=] { return stem_block_enter_backward(c, dn, x, T, norm, dres, dx, dw, accumulate, s); };
+  });
+}
+
+PyObject* block_leave_forward(PyObject*, PyObject* const* args, Py_ssize_t n) {
+  return enter(args, n, 6, [](const Args& a, stem_ctx* c) {
+    const int64_t T = a.rows(-1, 1), d = a.d_model();
+    auto f = a.shaped(0, ACT, T, d); auto x = a.shaped(1, ACT, T, d); auto L = a.leave(2, T, d); auto y = a.shaped(3, ACT, T, d);
+    auto to = a.shaped(4, ACT, T, d); auto s = a.stream(5);
+    return [=] { return stem_block_leave_forward(c, f, x, T, L, y, to, s); };
+  });
+}
+
+PyObject* block_leave_backward(PyObject*, PyObject* const* args, Py_ssize_t n) {
+  return enter(args, n, 12, [](const Args& a, stem_ctx* c) {
+    const int64_t T = a.rows(-1, a.v[0] == Py_None ? 1 : 0), d = a.d_model();
+    auto dy = a.shaped(0, ACT, T, d); auto dn = a.shaped(1, ACT, T, d); auto f = a.shaped(2, ACT, T, d); auto y = a.shaped(3, ACT, T, d);
+    auto L = a.leave(4, T, d); auto dx = a.shaped(5, ACT, T, d); auto df = a.shaped(6, ACT, T, d);
+    auto dg = L->gate_kind == STEM_GATE_CHANNEL ? a.shaped(7, F32, d) : L->gate_kind == STEM_GATE_TOKEN ? a.shaped(7, ACT, T) : a.shaped(7, ACT, T, d);
+    auto dwo = a.shaped<float>(8, F32, d); auto dwn = a.shaped<float>(9, F32, d); const int accumulate = a.flag(10); auto s = a.stream(11);
+    return [=] { return stem_block_leave_backward(c, dy, dn, f, y, T, L, dx, df, dg, dwo, dwn, accumulate, s); };
+  });
+}
+
+PyObject* dropout(PyObject*, PyObject* const* args, Py_ssize_t n) {
+  return enter(args, n, 7, [](const Args& a, stem_ctx* c) {
+    if (!THPVariable_CheckExact(a.v[0])) throw Unusual();
+    const at::Tensor& t = THPVariable_Unpack(a.v[0]);
+    if (t.dim() != 2) throw Unusual();
+    const int64_t T = t.size(0), width = t.size(1), seed = a.integer(3), offset = a.integer(4);
+    if (seed < 0 || offset < 0) throw Unusual();
+    auto x = a.shaped(0, ACT, T, width); auto y = a.shaped(1, ACT, T, width);
+    const stem_drop drop = {a.number(2), (uint64_t)seed, (uint64_t)offset, a.ptr<const uint64_t>(5, I64)};
+    auto s = a.stream(6);
+    return [=] { return stem_dropout(c, x, T, width, &drop, y, s); };
+  });
+}
+
+PyObject* quant_linear(PyObject*, PyObject* const* args, Py_ssize_t n) {
+  return enter(args, n, 6, [](const Args& a, stem_ctx* c) {
+    const int64_t T = a.rows(-1, 0);
+    const Args::Quant w = a.quant(1);
+    auto x = a.shaped(0, ACT, T, w.K); auto y = a.shaped(2, ACT, T, w.N); auto r = a.shaped(3, ACT, T, w.N); auto norm = a.norm(4, w.K);
+    auto s = a.stream(5);
+    return [=] { return stem_quant_linear(c, x, T, w.K, norm, w.q, w.scale, w.N, r, y, s); };
+  });
+}
+
+PyObject* quant_ffn_forward(PyObject*, PyObject* const* args, Py_ssize_t n) {
+  return enter(args, n, 10, [](const Args& a, stem_ctx* c) {
+    const int64_t T = a.rows(-1, 0), d = a.d_model(), F = a.d_ff(), rows = a.rows(-1, 4), E_rows = a.rows(9, 4);
+    const Args::Quant g = a.quant(2), w = a.quant(3);
+    if (g.N != F || g.K != d || w.N != d || w.K != F) throw Unusual();
+    auto x = a.shaped(0, ACT, T, d); auto ids = a.shaped<int32_t>(1, I32, T); auto E = a.shaped(4, ACT, rows, F); auto y = a.shaped(5, ACT, T, d);
+    auto r = a.shaped(6, ACT, T, d); auto norm = a.norm(7, d); auto s = a.stream(8);
+    return [=] { return stem_quant_ffn_forward(c, x, ids, T, norm, g.q, g.scale, w.q, w.scale, E, E_rows, r, y, s); };
+  });
+}
+
+// (StemCtx, torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream, stem_norm, stem_leave, StemQuant)
 PyObject* setup(PyObject*, PyObject* args) {
-  if (!PyArg_ParseTuple(args, "OOO", &g_ctx_type, &g_get_device, &g_raw_stream)) return nullptr;
-  for (PyObject* o : {g_ctx_type, g_get_device, g_raw_stream}) Py_INCREF(o);
+  if (!PyArg_ParseTuple(args, "OOOOOO", &g_ctx_type, &g_get_device, &g_raw_stream, &g_norm_type, &g_leave_type, &g_quant_type)) return nullptr;
+  for (PyObject* o : {g_ctx_type, g_get_device, g_raw_stream, g_norm_type, g_leave_type, g_quant_type}) Py_INCREF(o);
+  g_facts = PyUnicode_InternFromString("facts");
+  g_d_model = PyUnicode_InternFromString("d_model");
+  g_d_ff = PyUnicode_InternFromString("d_ff");
+  g_q = PyUnicode_InternFromString("q");
+  g_scale = PyUnicode_InternFromString("scale");
+  g_N = PyUnicode_InternFromString("N");
+  g_K = PyUnicode_InternFromString("K");
+  if (!g_facts || !g_d_model || !g_d_ff || !g_q || !g_scale || !g_N || !g_K) return nullptr;
   g_handle = PyUnicode_InternFromString("handle");
   g_value = PyUnicode_InternFromString("value");
   g_dtype = PyUnicode_InternFromString("dtype");
@@ -215,6 +356,8 @@ PyObject* off(PyObject*, PyObject*) {
 #define FAST(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(name)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {FAST(ffn_forward), FAST(ffn_forward_residual), FAST(ffn_backward), FAST(ffn_up_forward), FAST(ffn_up_backward),
                          FAST(embed_grad), FAST(embed_grad_presorted), FAST(embed_sparse_adamw),
+                         FAST(block_enter_forward), FAST(block_enter_backward), FAST(block_leave_forward), FAST(block_leave_backward), FAST(dropout),
+                         FAST(quant_linear), FAST(quant_ffn_forward),
                          {"setup", setup, METH_VARARGS, nullptr}, {"off", off, METH_NOARGS, nullptr}, {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_bind", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

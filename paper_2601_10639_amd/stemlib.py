@@ -49,6 +49,10 @@ STEM_NORM_NONE, STEM_NORM_RMS, STEM_NORM_LAYER = range(3)
 STEM_GATE_NONE, STEM_GATE_CHANNEL, STEM_GATE_TOKEN, STEM_GATE_FULL = range(4)
 
 
+def _code(t) -> int:
+    return {torch.float32: STEM_F32, torch.bfloat16: STEM_BF16}.get(t.dtype, -2)
+
+
 class stem_norm(ctypes.Structure):
     """A norm and its weight, a device tensor [d] or None.  Made once and passed to every call."""
 
@@ -57,6 +61,8 @@ class stem_norm(ctypes.Structure):
     def __init__(self, kind: int = STEM_NORM_NONE, eps: float = 1e-6, weight=None):
         super().__init__(kind, eps, _ptr(weight, name="weight"))
         self.tensor = weight   # kept alive
+        # for the native binding: elements of the weight and its type (0 elements: not of one side, which no call takes)
+        self.facts = (-1, -1) if weight is None else (weight.numel() if weight.dim() == 1 else 0, _code(weight))
 
     def _check(self, ctx, width: int, name: str):
         if self.tensor is not None:
@@ -84,6 +90,10 @@ class stem_leave(ctypes.Structure):
         self.norms = (out or stem_norm(), next or stem_norm())
         super().__init__(*self.norms, residual_scale, branch_scale, gate_kind, _ptr(gate, name="gate"), stem_drop(p, seed, offset, step))
         self.gate_tensor, self.step_tensor = gate, step
+        # for the native binding: elements of both weights, the gate's sides, and the type of all of them (-1: none is there, -2: several)
+        codes = {_code(t) for t in (self.norms[0].tensor, self.norms[1].tensor, gate) if t is not None}
+        sides = (-1, -1) if gate is None else (*gate.shape, -1)[:2] if 0 < gate.dim() < 3 else (0, 0)
+        self.facts = (self.norms[0].facts[0], self.norms[1].facts[0], *sides, -1 if not codes else codes.pop() if len(codes) == 1 else -2)
 
     def _check(self, ctx, T: int):
         d = ctx.d_model
@@ -213,7 +223,7 @@ def _load_bind():
                       "`python -m paper_2601_10639_amd.build` builds it", RuntimeWarning, stacklevel=3)
         _bind = _NoBind()
         return _bind
-    native.setup(StemCtx, torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream)
+    native.setup(StemCtx, torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream, stem_norm, stem_leave, StemQuant)
     os.register_at_fork(after_in_child=native.off)   # torch refuses the device there
     _bind = native
     return native
@@ -532,31 +542,37 @@ def stem_edit_rows(ctx: StemCtx, E, src_ids, tgt_ids, mode: int, pad_id: int = 0
 
 def stem_block_enter_forward(ctx: StemCtx, x, norm: stem_norm, n, stream=None):
     """n = N(x) * w."""
-    dt, shape = ctx.torch_dtype, (x.shape[0], ctx.d_model)
-    norm._check(ctx, ctx.d_model, "norm")
-    st = lib().stem_block_enter_forward(ctx.handle, _shaped(x, dt, shape, "x"), shape[0], norm, _shaped(n, dt, shape, "n"), _stream(stream))
+    st = (_bind or _load_bind()).block_enter_forward(ctx, x, norm, n, stream)
+    if st is None:   # not the ordinary call
+        dt, shape = ctx.torch_dtype, (x.shape[0], ctx.d_model)
+        norm._check(ctx, ctx.d_model, "norm")
+        st = lib().stem_block_enter_forward(ctx.handle, _shaped(x, dt, shape, "x"), shape[0], norm, _shaped(n, dt, shape, "n"), _stream(stream))
     if st != STEM_OK:
         _check(ctx, st, "stem_block_enter_forward")
 
 
 def stem_block_enter_backward(ctx: StemCtx, dn, x, norm: stem_norm, dx, dw=None, dres=None, accumulate: bool = False, stream=None):
     """dx = dres + the gradient of x; dw fp32."""
-    dt, d = ctx.torch_dtype, ctx.d_model
-    shape = (x.shape[0], d)
-    norm._check(ctx, d, "norm")
-    st = lib().stem_block_enter_backward(ctx.handle, _shaped(dn, dt, shape, "dn"), _shaped(x, dt, shape, "x"), shape[0], norm,
-                                         _shaped(dres, dt, shape, "dres"), _shaped(dx, dt, shape, "dx"),
-                                         _shaped(dw, torch.float32, (d,), "dw"), 1 if accumulate else 0, _stream(stream))
+    st = (_bind or _load_bind()).block_enter_backward(ctx, dn, x, norm, dx, dw, dres, accumulate, stream)
+    if st is None:   # not the ordinary call
+        dt, d = ctx.torch_dtype, ctx.d_model
+        shape = (x.shape[0], d)
+        norm._check(ctx, d, "norm")
+        st = lib().stem_block_enter_backward(ctx.handle, _shaped(dn, dt, shape, "dn"), _shaped(x, dt, shape, "x"), shape[0], norm,
+                                             _shaped(dres, dt, shape, "dres"), _shaped(dx, dt, shape, "dx"),
+                                             _shaped(dw, torch.float32, (d,), "dw"), 1 if accumulate else 0, _stream(stream))
     if st != STEM_OK:
         _check(ctx, st, "stem_block_enter_backward")
 
 
 def stem_block_leave_forward(ctx: StemCtx, f, x, leave: stem_leave, y, n=None, stream=None):
     """y = residual_scale x + branch_scale gate * drop(N_out(f) * w_out), n = N_next(y) * w_next; y may be x."""
-    dt, shape = ctx.torch_dtype, (x.shape[0], ctx.d_model)
-    leave._check(ctx, shape[0])
-    st = lib().stem_block_leave_forward(ctx.handle, _shaped(f, dt, shape, "f"), _shaped(x, dt, shape, "x"), shape[0], leave,
-                                        _shaped(y, dt, shape, "y"), _shaped(n, dt, shape, "n"), _stream(stream))
+    st = (_bind or _load_bind()).block_leave_forward(ctx, f, x, leave, y, n, stream)
+    if st is None:   # not the ordinary call
+        dt, shape = ctx.torch_dtype, (x.shape[0], ctx.d_model)
+        leave._check(ctx, shape[0])
+        st = lib().stem_block_leave_forward(ctx.handle, _shaped(f, dt, shape, "f"), _shaped(x, dt, shape, "x"), shape[0], leave,
+                                            _shaped(y, dt, shape, "y"), _shaped(n, dt, shape, "n"), _stream(stream))
     if st != STEM_OK:
         _check(ctx, st, "stem_block_leave_forward")
 
@@ -564,25 +580,29 @@ def stem_block_leave_forward(ctx: StemCtx, f, x, leave: stem_leave, y, n=None, s
 def stem_block_leave_backward(ctx: StemCtx, dy, dn, f, y, leave: stem_leave, dx, df, dgate=None, dw_out=None, dw_next=None,
                               accumulate: bool = False, stream=None):
     """Gradients of stem_block_leave_forward; dy or dn may be None, and so may every output."""
-    dt, d, f32 = ctx.torch_dtype, ctx.d_model, torch.float32
-    shape = ((dy if dy is not None else dn).shape[0], d)
-    leave._check(ctx, shape[0])
-    gate_shape = {STEM_GATE_CHANNEL: (d,), STEM_GATE_TOKEN: shape[:1]}.get(leave.gate_kind, shape)
-    st = lib().stem_block_leave_backward(ctx.handle, _shaped(dy, dt, shape, "dy"), _shaped(dn, dt, shape, "dn"), _shaped(f, dt, shape, "f"),
-                                         _shaped(y, dt, shape, "y"), shape[0], leave, _shaped(dx, dt, shape, "dx"),
-                                         _shaped(df, dt, shape, "df"),
-                                         _shaped(dgate, f32 if leave.gate_kind == STEM_GATE_CHANNEL else dt, gate_shape, "dgate"),
-                                         _shaped(dw_out, f32, (d,), "dw_out"), _shaped(dw_next, f32, (d,), "dw_next"),
-                                         1 if accumulate else 0, _stream(stream))
+    st = (_bind or _load_bind()).block_leave_backward(ctx, dy, dn, f, y, leave, dx, df, dgate, dw_out, dw_next, accumulate, stream)
+    if st is None:   # not the ordinary call
+        dt, d, f32 = ctx.torch_dtype, ctx.d_model, torch.float32
+        shape = ((dy if dy is not None else dn).shape[0], d)
+        leave._check(ctx, shape[0])
+        gate_shape = {STEM_GATE_CHANNEL: (d,), STEM_GATE_TOKEN: shape[:1]}.get(leave.gate_kind, shape)
+        st = lib().stem_block_leave_backward(ctx.handle, _shaped(dy, dt, shape, "dy"), _shaped(dn, dt, shape, "dn"), _shaped(f, dt, shape, "f"),
+                                             _shaped(y, dt, shape, "y"), shape[0], leave, _shaped(dx, dt, shape, "dx"),
+                                             _shaped(df, dt, shape, "df"),
+                                             _shaped(dgate, f32 if leave.gate_kind == STEM_GATE_CHANNEL else dt, gate_shape, "dgate"),
+                                             _shaped(dw_out, f32, (d,), "dw_out"), _shaped(dw_next, f32, (d,), "dw_next"),
+                                             1 if accumulate else 0, _stream(stream))
     if st != STEM_OK:
         _check(ctx, st, "stem_block_leave_backward")
 
 
 def stem_dropout(ctx: StemCtx, x, y, p: float, seed: int, offset: int = 0, step=None, stream=None):
     """y = D(x), rows of any width; on the gradient the same call is the backward pass.  y may be x."""
-    shape = (x.shape[0], x.shape[1])
-    st = lib().stem_dropout(ctx.handle, _shaped(x, ctx.torch_dtype, shape, "x"), *shape, stem_drop(p, seed, offset, step),
-                            _shaped(y, ctx.torch_dtype, shape, "y"), _stream(stream))
+    st = (_bind or _load_bind()).dropout(ctx, x, y, p, seed, offset, step, stream)
+    if st is None:   # not the ordinary call
+        shape = (x.shape[0], x.shape[1])
+        st = lib().stem_dropout(ctx.handle, _shaped(x, ctx.torch_dtype, shape, "x"), *shape, stem_drop(p, seed, offset, step),
+                                _shaped(y, ctx.torch_dtype, shape, "y"), _stream(stream))
     if st != STEM_OK:
         _check(ctx, st, "stem_dropout")
 
@@ -619,12 +639,14 @@ def _quant(w: StemQuant, N: int, K: int, name: str):
 
 def stem_quant_linear(ctx: StemCtx, x, W: StemQuant, y, residual=None, norm: stem_norm | None = None, stream=None):
     """y = Q(N(x)) W^T (+ residual)."""
-    dt, T = ctx.torch_dtype, x.shape[0]
-    q, scale = _quant(W, W.N, W.K, "W")
-    if norm is not None:
-        norm._check(ctx, W.K, "norm")
-    st = lib().stem_quant_linear(ctx.handle, _shaped(x, dt, (T, W.K), "x"), T, W.K, norm, q, scale, W.N,
-                                 _shaped(residual, dt, (T, W.N), "residual"), _shaped(y, dt, (T, W.N), "y"), _stream(stream))
+    st = (_bind or _load_bind()).quant_linear(ctx, x, W, y, residual, norm, stream)
+    if st is None:   # not the ordinary call
+        dt, T = ctx.torch_dtype, x.shape[0]
+        q, scale = _quant(W, W.N, W.K, "W")
+        if norm is not None:
+            norm._check(ctx, W.K, "norm")
+        st = lib().stem_quant_linear(ctx.handle, _shaped(x, dt, (T, W.K), "x"), T, W.K, norm, q, scale, W.N,
+                                     _shaped(residual, dt, (T, W.N), "residual"), _shaped(y, dt, (T, W.N), "y"), _stream(stream))
     if st != STEM_OK:
         _check(ctx, st, "stem_quant_linear")
 
@@ -632,15 +654,17 @@ def stem_quant_linear(ctx: StemCtx, x, W: StemQuant, y, residual=None, norm: ste
 def stem_quant_ffn_forward(ctx: StemCtx, x, ids, gate: StemQuant, down: StemQuant, E, y, residual=None, norm: stem_norm | None = None,
                            stream=None, E_rows=None):
     """y = Q(SiLU(Q(N(x)) gate^T) * E[ids]) down^T (+ residual); y may be x and residual."""
-    dt, T, d, F = ctx.torch_dtype, x.shape[0], ctx.d_model, ctx.d_ff
-    gq, gs = _quant(gate, F, d, "gate")
-    dq, ds = _quant(down, d, F, "down")
-    if norm is not None:
-        norm._check(ctx, d, "norm")
-    E_rows = E.shape[0] if E_rows is None else E_rows
-    st = lib().stem_quant_ffn_forward(ctx.handle, _shaped(x, dt, (T, d), "x"), _shaped(ids, torch.int32, (T,), "ids"), T, norm, gq, gs, dq, ds,
-                                      _shaped(E, dt, (E.shape[0], F), "E"), E_rows, _shaped(residual, dt, (T, d), "residual"),
-                                      _shaped(y, dt, (T, d), "y"), _stream(stream))
+    st = (_bind or _load_bind()).quant_ffn_forward(ctx, x, ids, gate, down, E, y, residual, norm, stream, E_rows)
+    if st is None:   # not the ordinary call
+        dt, T, d, F = ctx.torch_dtype, x.shape[0], ctx.d_model, ctx.d_ff
+        gq, gs = _quant(gate, F, d, "gate")
+        dq, ds = _quant(down, d, F, "down")
+        if norm is not None:
+            norm._check(ctx, d, "norm")
+        E_rows = E.shape[0] if E_rows is None else E_rows
+        st = lib().stem_quant_ffn_forward(ctx.handle, _shaped(x, dt, (T, d), "x"), _shaped(ids, torch.int32, (T,), "ids"), T, norm, gq, gs, dq, ds,
+                                          _shaped(E, dt, (E.shape[0], F), "E"), E_rows, _shaped(residual, dt, (T, d), "residual"),
+                                          _shaped(y, dt, (T, d), "y"), _stream(stream))
     if st != STEM_OK:
         _check(ctx, st, "stem_quant_ffn_forward")
 
