@@ -24,7 +24,7 @@ namespace {
 
 constexpr uint32_t OOB = 0x80000000u;   // a buffer offset beyond any operand: reads as zero, is not stored
 constexpr int SC1 = 16;                 // cache policy bit of the buffer instructions: device scope
-constexpr int MAX_SLICES = 8;
+constexpr int MAX_SLICES = 4;
 
 __device__ __forceinline__ float sigmoidf_fast(float z) { return __builtin_amdgcn_rcpf(1.0f + __expf(-z)); }
 __device__ __forceinline__ void lds_dma_16(rsrc_t rs, char* lds_dst, uint32_t off, int soff) {
@@ -69,130 +69,136 @@ struct Loader {
 };
 
 // ---- epilogue of a product: a wavefront's 32 MI x 32 NJ results, 32 rows at a time through LDS ---------------------------------
-// acc[i][j]: token block i, channel block j; a lane holds token lane & 31 and channels 8 g + 4 (lane >> 5) + 0..3 of each.
+// acc[i][j]: token block i, channel block j; a lane holds token lane & 31 and channels 8 g + 4 (lane >> 5) + 0..3 of each.  They are scaled
+// on their way into LDS.
 template <int MI, int NJ>
 struct Output {
   static constexpr int COLS = 32 * NJ, PITCH = COLS + 4;       // of a staged row, in words
-  static constexpr int BYTES = 32 * PITCH * 4 + (COLS + 32) * 4;   // of LDS, for each wavefront: the rows, the channels' scales and the rows'
+  static constexpr int BYTES = (32 * PITCH + COLS) * 4;        // of LDS, for each wavefront: the rows, and the channels' scales
   static constexpr int LPR = COLS / 8, RPP = 64 / LPR, PASSES = 32 / RPP;   // 8 columns a lane
 
   static __device__ __forceinline__ void run(const QuantGemmArgs& p, const i32x16_t (&acc)[MI][NJ], char* stg, int m0, int n0, int lane) {
-    int* const st = reinterpret_cast<int*>(stg);
+    float* const st = reinterpret_cast<float*>(stg);
     if (m0 >= p.M || n0 >= p.N) return;
-    const int srow = lane / LPR, scol = (lane % LPR) * 8, n = n0 + scol;
-    const bool whole = p.N % 8 == 0;                           // rows of y are 16-byte aligned
-    float sb[8], sa_row[MI];
+    float* const scales = st + 32 * PITCH;
 #pragma unroll
-    for (int q = 0; q < 8; ++q) sb[q] = n + q < p.N ? p.scale_b[n + q] : 0.f;
-    float* const scales = reinterpret_cast<float*>(st + 32 * PITCH);
-    float* const scales_a = scales + COLS;
-    if (!whole)
-      for (int c = lane; c < COLS; c += 64) scales[c] = n0 + c < p.N ? p.scale_b[n0 + c] : 0.f;
+    for (int c = lane; c < COLS; c += 64) scales[c] = p.scale_b[n0 + c < p.N ? n0 + c : 0];
+    float sa[MI];
 #pragma unroll
-    for (int i = 0; i < MI; ++i) sa_row[i] = p.scale_a[m0 + i * 32 + (lane & 31) < p.M ? m0 + i * 32 + (lane & 31) : p.M - 1];
-    // A lane outside the matrix is given an offset beyond the buffer: its loads read zero and its stores are dropped.
-    const int rows = p.M - m0 < 32 * MI ? p.M - m0 : 32 * MI;
-    const rsrc_t ry = resource(p.y + (size_t)m0 * p.N, rows * p.N * 2);
-    const rsrc_t rr = resource(p.residual ? p.residual + (size_t)m0 * p.N : nullptr, p.residual ? rows * p.N * 2 : 0);
-#pragma unroll
-    for (int i = 0; i < MI; ++i) {
-      uint32_t off[PASSES];
-      u32x4_t res[PASSES];
-      if (whole) {
-#pragma unroll
-        for (int pass = 0; pass < PASSES; ++pass) {
-          const int r = i * 32 + pass * RPP + srow;
-          off[pass] = n < p.N && r < rows ? (uint32_t)(r * p.N + n) * 2u : OOB;
-          if (p.residual) res[pass] = __builtin_amdgcn_raw_buffer_load_b128(rr, off[pass], 0, 0);
-        }
-      }
+    for (int i = 0; i < MI; ++i) sa[i] = p.scale_a[min(m0 + i * 32 + (lane & 31), p.M - 1)];
+    // A lane outside the matrix is given an offset beyond the buffer: its loads read zero and its stores are dropped.  The buffers begin at the
+    // 16-byte boundary in front of row m0.
+    const bool whole = p.N % 8 == 0;                           // all rows begin at one
+    const int rows = p.M - m0 < 32 * MI ? p.M - m0 : 32 * MI, lim = p.N - n0 < COLS ? p.N - n0 : COLS;
+    const size_t first = (size_t)m0 * p.N & ~(size_t)7;
+    const int skip = (int)((size_t)m0 * p.N & 7), size = (skip + rows * p.N) * 2;
+    const rsrc_t ry = resource(p.y + first, size), rr = resource(p.residual ? p.residual + first : nullptr, p.residual ? size : 0);
+    auto at = [&](int r, int col, bool ok) __attribute__((always_inline)) { return ok ? (uint32_t)(skip + r * p.N + n0 + col) * 2u : OOB; };
+    auto to_lds = [&](int i) __attribute__((always_inline)) {
 #pragma unroll
       for (int j = 0; j < NJ; ++j)
 #pragma unroll
         for (int g = 0; g < 4; ++g) {
-          const i32x4_t w = {acc[i][j][4 * g], acc[i][j][4 * g + 1], acc[i][j][4 * g + 2], acc[i][j][4 * g + 3]};
-          *reinterpret_cast<i32x4_t*>(st + (lane & 31) * PITCH + j * 32 + g * 8 + (lane >> 5) * 4) = w;
+          const int col = j * 32 + g * 8 + (lane >> 5) * 4;
+          const f32x4_t sb = *reinterpret_cast<const f32x4_t*>(scales + col);
+          f32x4_t w;
+#pragma unroll
+          for (int q = 0; q < 4; ++q) w[q] = (float)acc[i][j][4 * g + q] * (sa[i] * sb[q]);
+          *reinterpret_cast<f32x4_t*>(st + (lane & 31) * PITCH + col) = w;
         }
-      __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-      __builtin_amdgcn_wave_barrier();
-      __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
-      if (whole) {
+      in_order();
+    };
+    auto add_and_store = [&](const float* from, uint32_t off, u32x4_t res) __attribute__((always_inline)) {
+      float z[8];
+      __builtin_memcpy(z, from, 32);
+      bf16x8_t o;
+#pragma unroll
+      for (int q = 0; q < 8; ++q) o[q] = (__bf16)(z[q] + __uint_as_float(q & 1 ? res[q >> 1] & 0xffff0000u : res[q >> 1] << 16));
+      __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4_t, o), ry, off, 0, 0);
+    };
+    // what the rows of a block are added to: requested for all blocks at once where registers allow
+    constexpr int AHEAD = MI * NJ <= 4 ? MI : 1;
+    if (whole) {
+      const int srow = lane / LPR, scol = (lane % LPR) * 8;
+      uint32_t off[AHEAD][PASSES];
+      u32x4_t res[AHEAD][PASSES];
+      auto fetch = [&](int i) __attribute__((always_inline)) {
 #pragma unroll
         for (int pass = 0; pass < PASSES; ++pass) {
-          const int r = pass * RPP + srow;
-          const float sa = __shfl(sa_row[i], r);
-          const int* const src = st + r * PITCH + scol;
-          const i32x4_t c0 = *reinterpret_cast<const i32x4_t*>(src), c1 = *reinterpret_cast<const i32x4_t*>(src + 4);
-          bf16x8_t o;
-#pragma unroll
-          for (int q = 0; q < 8; ++q) {
-            float z = (float)(q < 4 ? c0[q & 3] : c1[q & 3]) * (sa * sb[q]);
-            if (p.residual) z += __uint_as_float(q & 1 ? res[pass][q >> 1] & 0xffff0000u : res[pass][q >> 1] << 16);
-            o[q] = (__bf16)z;
-          }
-          __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4_t, o), ry, off[pass], 0, 0);
+          const int r = i * 32 + pass * RPP + srow;
+          off[i % AHEAD][pass] = at(r, scol, scol < lim && r < rows);
+          res[i % AHEAD][pass] = u32x4_t{};
+          if (p.residual) res[i % AHEAD][pass] = __builtin_amdgcn_raw_buffer_load_b128(rr, off[i % AHEAD][pass], 0, 0);
         }
-      } else {
-        // Rows of y at any 2-byte address: 16 bytes at a time where all of them are the tile's, and the ends of each row, up to 7 columns on
-        // either side, one by one.  (One by one throughout: 4000 x 5001, K 1999, 191 us instead of 91, against 61 at 5000 columns.)
-        constexpr int GROUPS = COLS / 8 + 1, UNITS = (32 * GROUPS + 63) / 64;
-        const int lim = p.N - n0 < COLS ? p.N - n0 : COLS;
-        auto head = [&](int r) __attribute__((always_inline)) {   // columns in front of row r's first 16-byte boundary
-          return (8 - (((m0 + i * 32 + r) & 7) * (p.N & 7) + n0 & 7)) & 7;
-        };
-        if (lane < 32) scales_a[lane] = sa_row[i];
-        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-        __builtin_amdgcn_wave_barrier();
-        __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
-        // offsets from the boundary in front of row m0 (the buffers are aligned to it)
-        const size_t first = (size_t)m0 * p.N & ~(size_t)7;
-        const int skip = (int)((size_t)m0 * p.N & 7), size = (skip + rows * p.N) * 2;
-        const rsrc_t uy = resource(p.y + first, size), ur = resource(p.residual ? p.residual + first : nullptr, p.residual ? size : 0);
-        auto at = [&](int r, int col, bool ok) __attribute__((always_inline)) {
-          return ok ? (uint32_t)(skip + (i * 32 + r) * p.N + n0 + col) * 2u : OOB;
-        };
-        uint32_t whole_at[UNITS], end_at[8];
-        int whole_st[UNITS], end_st[8];   // where in the staged rows; channel and row are made of it
-        u32x4_t rz[UNITS] = {};
-        uint16_t re[8] = {};
+      };
+      if (AHEAD > 1)
 #pragma unroll
-        for (int u = 0; u < UNITS; ++u) {
-          const int e = u * 64 + lane, r = e / GROUPS < 32 ? e / GROUPS : 31, h = head(r), col = (e % GROUPS) * 8 + (h ? h - 8 : 0);
-          const bool ok = e / GROUPS < 32 && i * 32 + r < rows && col >= 0 && col + 8 <= lim;
-          whole_at[u] = at(r, col, ok);
-          whole_st[u] = ok ? r * PITCH + col : 0;
-          if (p.residual) rz[u] = __builtin_amdgcn_raw_buffer_load_b128(ur, whole_at[u], 0, 0);
-        }
+        for (int i = 0; i < MI; ++i) fetch(i);
 #pragma unroll
-        for (int u = 0; u < 8; ++u) {   // column q of up to 7 in front, or q - 8 behind
-          const int e = u * 64 + lane, r = e >> 4, q = e & 15, h = head(r);
-          const int col = q < 8 ? q : (lim > h ? h + ((lim - h) & ~7) : 0) + q - 8;
-          const bool ok = i * 32 + r < rows && (q < 8 ? col < h && col < lim : lim > h && col < lim);
-          end_at[u] = at(r, col, ok);
-          end_st[u] = ok ? r * PITCH + col : 0;
-          if (p.residual) re[u] = __builtin_amdgcn_raw_buffer_load_b16(ur, end_at[u], 0, 0);
-        }
+      for (int i = 0; i < MI; ++i) {
+        if (AHEAD == 1) fetch(i);
+        to_lds(i);
 #pragma unroll
-        for (int u = 0; u < UNITS; ++u) {
-          const int r = whole_st[u] / PITCH, col = whole_st[u] % PITCH;
-          const float sa = scales_a[r];
-          bf16x8_t o;
-#pragma unroll
-          for (int q = 0; q < 8; ++q)
-            o[q] = (__bf16)((float)st[whole_st[u] + q] * (sa * scales[col + q]) + __uint_as_float(q & 1 ? rz[u][q >> 1] & 0xffff0000u : rz[u][q >> 1] << 16));
-          __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4_t, o), uy, whole_at[u], 0, 0);
-        }
-#pragma unroll
-        for (int u = 0; u < 8; ++u) {
-          const int r = end_st[u] / PITCH, col = end_st[u] % PITCH;
-          const float z = (float)st[end_st[u]] * (scales_a[r] * scales[col]) + __uint_as_float((uint32_t)re[u] << 16);
-          __builtin_amdgcn_raw_buffer_store_b16(__builtin_bit_cast(uint16_t, (__bf16)z), uy, end_at[u], 0, 0);
-        }
+        for (int pass = 0; pass < PASSES; ++pass) add_and_store(st + (pass * RPP + srow) * PITCH + scol, off[i % AHEAD][pass], res[i % AHEAD][pass]);
+        in_order();   // all have read the rows before they are staged over
+        __builtin_amdgcn_sched_barrier(0);   // (all blocks' reads at once would not fit the registers)
       }
-      __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-      __builtin_amdgcn_wave_barrier();   // all have read the rows before they are staged over
-      __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+      return;
     }
+    // Rows of y at any 2-byte address: 16 bytes at a time where all of them are the tile's, and the ends of each row, up to 7 columns on
+    // either side, one by one.  (One by one throughout: 4000 x 5001, K 1999, 191 us instead of 67, against 48 at 5000 columns.)
+    constexpr int GROUPS = COLS / 8 + 1, UNITS = (32 * GROUPS + 63) / 64;
+    uint32_t whole_at[AHEAD][UNITS], end_at[AHEAD][8];
+    int whole_st[AHEAD][UNITS], end_st[AHEAD][8];   // where in the staged rows
+    u32x4_t rz[AHEAD][UNITS];
+    uint16_t re[AHEAD][8];
+    auto fetch = [&](int i) __attribute__((always_inline)) {
+      const int k = i % AHEAD;
+      auto head = [&](int r) __attribute__((always_inline)) {   // columns in front of row r's first 16-byte boundary
+        return (8 - (((m0 + i * 32 + r) & 7) * (p.N & 7) + n0 & 7)) & 7;
+      };
+#pragma unroll
+      for (int u = 0; u < UNITS; ++u) {
+        const int e = u * 64 + lane, r = e / GROUPS < 32 ? e / GROUPS : 31, h = head(r), col = (e % GROUPS) * 8 + (h ? h - 8 : 0);
+        const bool ok = e / GROUPS < 32 && i * 32 + r < rows && col >= 0 && col + 8 <= lim;
+        whole_at[k][u] = at(i * 32 + r, col, ok);
+        whole_st[k][u] = ok ? r * PITCH + col : 0;
+        rz[k][u] = u32x4_t{};
+        if (p.residual) rz[k][u] = __builtin_amdgcn_raw_buffer_load_b128(rr, whole_at[k][u], 0, 0);
+      }
+#pragma unroll
+      for (int u = 0; u < 8; ++u) {   // column q of up to 7 in front, or q - 8 behind
+        const int e = u * 64 + lane, r = e >> 4, q = e & 15, h = head(r);
+        const int col = q < 8 ? q : (lim > h ? h + ((lim - h) & ~7) : 0) + q - 8;
+        const bool ok = i * 32 + r < rows && (q < 8 ? col < h && col < lim : lim > h && col < lim);
+        end_at[k][u] = at(i * 32 + r, col, ok);
+        end_st[k][u] = ok ? r * PITCH + col : 0;
+        re[k][u] = 0;
+        if (p.residual) re[k][u] = __builtin_amdgcn_raw_buffer_load_b16(rr, end_at[k][u], 0, 0);
+      }
+    };
+    if (AHEAD > 1)
+#pragma unroll
+      for (int i = 0; i < MI; ++i) fetch(i);
+#pragma unroll
+    for (int i = 0; i < MI; ++i) {
+      const int k = i % AHEAD;
+      if (AHEAD == 1) fetch(i);
+      to_lds(i);
+#pragma unroll
+      for (int u = 0; u < UNITS; ++u) add_and_store(st + whole_st[k][u], whole_at[k][u], rz[k][u]);
+#pragma unroll
+      for (int u = 0; u < 8; ++u)
+        __builtin_amdgcn_raw_buffer_store_b16(__builtin_bit_cast(uint16_t, (__bf16)(st[end_st[k][u]] + __uint_as_float((uint32_t)re[k][u] << 16))), ry,
+                                              end_at[k][u], 0, 0);
+      in_order();
+      __builtin_amdgcn_sched_barrier(0);
+    }
+  }
+  static __device__ __forceinline__ void in_order() {   // of LDS, within the wavefront
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
   }
 };
 
@@ -553,20 +559,26 @@ __device__ __forceinline__ bool last_slice(const QuantGemmArgs& p, i32x16_t (&ac
   if (!last) return false;
   if (threadIdx.x == 0) __hip_atomic_store(p.tickets + tile, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);   // for the next launch
   asm volatile("" ::: "memory");
-  for (int s = 0; s < p.ksplit; ++s) {
-    if (s == slice) continue;
-    const int from = (at + (s - slice) * stride) * BYTES;
+  // the others' sums, all in flight together; what is beyond the last slice reads as zero
+  constexpr int N = MI * NJ * 4;
+  i32x4_t v[MAX_SLICES - 1][N];
+#pragma unroll
+  for (int o = 0; o < MAX_SLICES - 1; ++o) {
+    const int s = o + (o >= slice);
+#pragma unroll
+    for (int k = 0; k < N; ++k)
+      v[o][k] = __builtin_bit_cast(i32x4_t, __builtin_amdgcn_raw_buffer_load_b128(rw, s < p.ksplit ? lane * 16 : OOB, (at + (s - slice) * stride) * BYTES + k * 1024, SC1));
+  }
+#pragma unroll
+  for (int o = 0; o < MAX_SLICES - 1; ++o)
 #pragma unroll
     for (int i = 0; i < MI; ++i)
 #pragma unroll
       for (int j = 0; j < NJ; ++j)
 #pragma unroll
-        for (int g = 0; g < 4; ++g) {
-          const i32x4_t v = __builtin_bit_cast(i32x4_t, __builtin_amdgcn_raw_buffer_load_b128(rw, lane * 16, from + ((i * NJ + j) * 4 + g) * 1024, SC1));
+        for (int g = 0; g < 4; ++g)
 #pragma unroll
-          for (int q = 0; q < 4; ++q) acc[i][j][4 * g + q] += v[q];
-        }
-  }
+          for (int q = 0; q < 4; ++q) acc[i][j][4 * g + q] += v[o][(i * NJ + j) * 4 + g][q];
   __syncthreads();   // the ticket has been read: LDS may be used again
   return true;
 }
@@ -675,7 +687,8 @@ __global__ __launch_bounds__((C::WAVES + C::LW) * 64) void gemm_int8_kernel(Quan
   for (int st = 0; st < S - 1; ++st)
     if (kt + st < nk) stage_iteration(st);
   __syncthreads();
-  if (p.ksplit > 1 && !last_slice<MI, NJ>(p, acc, smem, (slice * tiles + tn * ntm + tm) * C::WAVES + wave, tiles * C::WAVES, slice, tn * ntm + tm, lane)) return;
+  if constexpr (!GATE && C::TN == 64)   // (only these are cut)
+    if (p.ksplit > 1 && !last_slice<MI, NJ>(p, acc, smem, (slice * tiles + tn * ntm + tm) * C::WAVES + wave, tiles * C::WAVES, slice, tn * ntm + tm, lane)) return;
   if constexpr (GATE) Hid::run(p, acc, rows.scale, rows.id, smem + wave * Hid::BYTES, m0 + wm * MI * 32, n0 + wn * NJ * 32, lane);
   else Out::run(p, acc, smem + wave * Out::BYTES, m0 + wm * MI * 32, n0 + wn * NJ * 32, lane);
 }
@@ -717,7 +730,7 @@ extern "C" void stem_route_quant(int M, int N, int K, int gate, int64_t ws_bytes
     if (!gate && (double)((t256 + 255) / 256) <= few) rows = 256;
   }
   if (!gate && cols == 64) {
-    slices = (int)std::min<int64_t>({4, nk / 8, 240 / t64});
+    slices = (int)std::min<int64_t>({MAX_SLICES, nk / 8, 240 / t64});
     if (slices < 2 && t64 <= 128 && nk >= 48) slices = 2;
     while (slices > 1 && (int64_t)slices * t64 * 128 * 64 * 4 > ws_bytes) --slices;
     while (slices > 1 && (nk + slices - 1) / slices * (slices - 1) >= nk) --slices;   // every slice has a part of K
