@@ -21,6 +21,8 @@ namespace {
     if (st_ != STEM_OK) return st_;                      \
   } while (0)
 
+constexpr int64_t QUANT_MAX_CHANNELS = 1 << 22;   // 256 rows of an output are addressed with 32 bits
+
 struct Buffer { const void* p; size_t bytes; };
 
 bool overlap(const Buffer& a, const Buffer& b) {
@@ -125,8 +127,9 @@ QuantDecodeArgs decode_args(const stem_ctx* c, int64_t T, int64_t N, int64_t K, 
 }
 
 // The tokens of a decode product from rows x: in place, or quantised by a kernel before it (which clears `words` words too)
-hipError_t decode_tokens(stem_ctx* c, const void* x, int64_t K, const stem_norm* norm, uint32_t* clear, int64_t words, QuantDecodeArgs& a, hipStream_t s) {
-  if (stem_quant_decode_inline(a.M, K)) {
+hipError_t decode_tokens(stem_ctx* c, const void* x, int64_t K, const stem_norm* norm, bool in_place, uint32_t* clear, int64_t words,
+                         QuantDecodeArgs& a, hipStream_t s) {
+  if (in_place && stem_quant_decode_inline(a.M, K)) {
     a.x = static_cast<const bf16_t*>(x);
     a.row_K = (int)K;
     a.norm = norm ? *norm : stem_norm{STEM_NORM_NONE, 0.f, nullptr};
@@ -263,9 +266,9 @@ stem_status stem_quant_linear(stem_ctx* c, const void* x, int64_t T, int64_t K, 
   STEM_TRY(stem_enter(c, T));
   STEM_TRY(check_quant(c, who));
   const int64_t most = std::max(c->desc.d_model, c->desc.d_ff);
-  if (N < 1 || K < 1 || K > most || stem_quant_size(N, K) > INT32_MAX || stem_quant_size(std::max<int64_t>(T, 1), K) > INT32_MAX)
-    return stem_fail(c, STEM_ERR_SHAPE, "%s: a product [%lld, %lld] x [%lld, %lld]^T; K is up to max(d_model, d_ff) = %lld and each operand's 8-bit "
-                     "form below 2^31 bytes", who, (long long)T, (long long)K, (long long)N, (long long)K, (long long)most);
+  if (N < 1 || N > QUANT_MAX_CHANNELS || K < 1 || K > most || stem_quant_size(N, K) > INT32_MAX || stem_quant_size(std::max<int64_t>(T, 1), K) > INT32_MAX)
+    return stem_fail(c, STEM_ERR_SHAPE, "%s: a product [%lld, %lld] x [%lld, %lld]^T; K is up to max(d_model, d_ff) = %lld, N up to 2^22 and each "
+                     "operand's 8-bit form below 2^31 bytes", who, (long long)T, (long long)K, (long long)N, (long long)K, (long long)most);
   if (T == 0) return STEM_OK;
   if (!x || !q || !scale || !y) return stem_fail(c, STEM_ERR_INVALID_ARG, "%s: null pointer argument", who);
   if (norm) STEM_TRY(check_norm(c, who, *norm));
@@ -278,7 +281,8 @@ stem_status stem_quant_linear(stem_ctx* c, const void* x, int64_t T, int64_t K, 
   if (T <= STEM_QUANT_DECODE_TOKENS) {
     QuantDecodeArgs a = decode_args(c, T, N, stem_quant_pitch(K), q, scale);
     a.y = static_cast<bf16_t*>(y); a.residual = static_cast<const bf16_t*>(residual);
-    HIP_TRY(c, decode_tokens(c, x, K, norm, nullptr, 0, a, s));
+    // (in place every workgroup reads x, also when others have written their part of y)
+    HIP_TRY(c, decode_tokens(c, x, K, norm, !overlap({x, xb}, {y, yb}), nullptr, 0, a, s));
     HIP_TRY(c, stem_quant_decode_launch(c, K_QUANT_DOWN, a, s));
     return STEM_OK;
   }
@@ -304,6 +308,8 @@ stem_status stem_quant_ffn_forward(stem_ctx* c, const void* x, const int32_t* id
   if (E_rows < 1 || E_rows > INT32_MAX) return stem_fail(c, STEM_ERR_SHAPE, "%s: E_rows = %lld", who, (long long)E_rows);
   if (norm) STEM_TRY(check_norm(c, who, *norm));
   const int64_t d = c->desc.d_model, F = c->desc.d_ff;
+  for (int64_t bytes : {stem_quant_size(T, d), stem_quant_size(T, F), stem_quant_size(F, d), stem_quant_size(d, F)})
+    if (bytes > INT32_MAX) return stem_fail(c, STEM_ERR_SHAPE, "%s: %lld tokens or the weights are %lld bytes in 8 bits, 2^31 or more", who, (long long)T, (long long)bytes);
   const size_t xb = (size_t)(T * d) * 2;
   STEM_TRY(check_buffers(c, who, {{x, xb}, {residual, xb}}, {{y, xb}}, true));
   STEM_TRY(check_buffers(c, who, {{gate_q, (size_t)stem_quant_size(F, d)}, {gate_scale, (size_t)F * 4}, {down_q, (size_t)stem_quant_size(d, F)},
@@ -322,7 +328,7 @@ stem_status stem_quant_ffn_forward(stem_ctx* c, const void* x, const int32_t* id
     // (a slice of the hidden values is quantised in place, by what all of them come to)
     const bool hidden = T <= 8 && stem_quant_decode_inline(T, (pitch / 128 + b.ksplit - 1) / b.ksplit * 128);
     if (hidden) g.max_out = c->quant_max; else g.amax = c->quant_amax;
-    HIP_TRY(c, decode_tokens(c, x, d, norm, hidden ? nullptr : c->quant_amax, T * QUANT_AMAX_STRIDE, g, s));
+    HIP_TRY(c, decode_tokens(c, x, d, norm, true, hidden ? nullptr : c->quant_amax, T * QUANT_AMAX_STRIDE, g, s));
     if (!hidden && g.x) HIP_TRY(c, stem_fill_zero(c->quant_amax, T * QUANT_AMAX_STRIDE * 4, s));
     HIP_TRY(c, stem_quant_decode_launch(c, K_QUANT_GATE, g, s));
     if (hidden) {

@@ -195,6 +195,64 @@ def test_graph_replays_and_another_stream():
         assert torch.equal(got, y) and torch.equal(gl, lin)
 
 
+@pytest.mark.parametrize("T,N,K", [(1, 512, 512), (5, 700, 700), (40, 96, 96), (100, 256, 256)])
+def test_linear_over_its_own_input(T, N, K):
+    ctx = make_ctx(T, 704)
+    x, w = draw(1, T, K), L.stem_quant_weights(ctx, draw(2, N, K, std=0.05))
+    y = torch.empty(T, N, dtype=bf, device=DEV)
+    L.stem_quant_linear(ctx, x, w, y)
+    L.stem_quant_linear(ctx, x, w, x)
+    assert torch.equal(x, y)
+
+
+@pytest.mark.parametrize("T,F", [(5, 192), (300, 320), (700, 4096)])
+def test_ids_outside_the_table_at_other_sizes(T, F):
+    d, V = 64, 10
+    ctx = make_ctx(T, d, F, V)
+    x, E = draw(1, T, d), draw(4, V, F)
+    g, d8 = L.stem_quant_weights(ctx, draw(2, F, d)), L.stem_quant_weights(ctx, draw(3, d, F))
+    ids = torch.zeros(T, dtype=torch.int32, device=DEV)
+    y, z = torch.empty_like(x), torch.empty_like(x)
+    L.stem_quant_ffn_forward(ctx, x, ids, g, d8, E, y)
+    ids[T - 2] = -7
+    L.stem_quant_ffn_forward(ctx, x, ids, g, d8, E, z)
+    with pytest.raises(L.StemError) as e:
+        L.stem_sync_status(ctx)
+    assert e.value.status == L.STEM_ERR_ID_RANGE
+    assert torch.equal(y, z)
+
+
+def test_a_table_row_that_is_no_number_spoils_its_tokens_only():
+    T, d, F, V = 200, 128, 320, 20
+    ctx = make_ctx(T, d, F, V)
+    x, E = draw(1, T, d), draw(4, V, F)
+    E[3, 0], E[5, F - 1], E[7, 100] = float("inf"), float("nan"), float("-inf")
+    g, d8 = L.stem_quant_weights(ctx, draw(2, F, d, std=0.09)), L.stem_quant_weights(ctx, draw(3, d, F, std=0.05))
+    ids = (torch.arange(T, dtype=torch.int32) % V).to(DEV)
+    for t in (T, 30, 4):
+        y = torch.empty_like(x)
+        L.stem_quant_ffn_forward(ctx, x[:t], ids[:t], g, d8, E, y[:t])
+        bad = torch.isnan(y[:t]).all(1)
+        assert torch.equal(bad, (ids[:t] == 3) | (ids[:t] == 5) | (ids[:t] == 7))
+        assert torch.isfinite(y[:t][~bad]).all()
+
+
+def test_cut_products_give_the_same_bits_whatever_else_the_context_does():
+    """K slices exchange through the context's tickets, which other kernels of the context use too."""
+    T, d, F, V = 200, 512, 8192, 20
+    ctx = make_ctx(T, d, F, V)
+    x, h, E = draw(1, T, d), draw(2, T, F), draw(4, V, F)
+    w = L.stem_quant_weights(ctx, draw(3, d, F, std=0.05))
+    Wg, Wd = draw(5, F, d, std=0.05), draw(6, d, F, std=0.05)
+    ids = torch.zeros(T, dtype=torch.int32, device=DEV)
+    y, z, o = torch.empty_like(x), torch.empty_like(x), torch.empty_like(x)
+    L.stem_quant_linear(ctx, h, w, y)
+    for t in (16, 1, T):
+        L.stem_ffn_forward(ctx, x[:t], ids[:t], Wg, Wd, E, o[:t])
+        L.stem_quant_linear(ctx, h, w, z)
+        assert torch.equal(y, z)
+
+
 def test_refusals():
     T, d, F = 8, 64, 128
     ctx = make_ctx(T, d, F, 10)
