@@ -56,7 +56,10 @@ enum { FROM_INTEGERS = 0, FROM_ROWS, FROM_HIDDEN };
 template <int FROM>
 struct Inline {
   float v[2][16];
-  int row[2], at[2];     // of the chunk that v holds: token, chunk of the row; token -1 for none
+  QuantChunk raw[2], weight[2];   // of x, of the norm's weight
+  uint32_t tops[4];               // of this wavefront's token: the first 256 tiles' maxima
+  int row[2], at[2];              // of the chunk that v holds: token, chunk of the row; token -1 for none
+  // In front of the weights' loads: loads return in order, and all this is there before the first weights are.
   __device__ __forceinline__ void load(const QuantDecodeArgs& p, int k0, int chunks, int tid) {   // chunks of a row
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
@@ -68,9 +71,8 @@ struct Inline {
       if (row[h] < 0) continue;
       if (FROM == FROM_ROWS) {
         const int left = p.row_K - at[h] * 16;
-        const QuantChunk c = left > 0 ? quant_load_chunk(p.x + (size_t)r * p.row_K + at[h] * 16, left) : QuantChunk{};
-#pragma unroll
-        for (int q = 0; q < 16; ++q) v[h][q] = quant_element(c, q);
+        raw[h] = left > 0 ? quant_load_chunk(p.x + (size_t)r * p.row_K + at[h] * 16, left) : QuantChunk{};
+        if (p.norm.weight) weight[h] = left > 0 ? quant_load_chunk(static_cast<const bf16_t*>(p.norm.weight) + at[h] * 16, left) : QuantChunk{};
       } else {
         // two groups of 8 channels, four of each in lanes r and r + 32 of the gate product's layout
         const int c = k0 / 16 + at[h];
@@ -82,6 +84,11 @@ struct Inline {
           for (int k = 0; k < 4; ++k) v[h][4 * q + k] = u[k];
         }
       }
+    }
+    if (FROM == FROM_HIDDEN) {
+      const int t = tid >> 6, lane = tid & 63;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) tops[i] = t < p.M && i * 64 + lane < p.maxima ? p.max_in[(i * 64 + lane) * 8 + t] : 0;
     }
   }
   // a figure of each token, from one of each chunk: part[] in LDS takes them, wavefront t adds up token t's, stat[t] is the result
@@ -98,6 +105,12 @@ struct Inline {
   __device__ __forceinline__ void quantise(const QuantDecodeArgs& p, int k0, int K, int chunks, int tid, float* part, float* stat, char* q, int rows_log,
                                            float* scale) {
     const int lane = tid & 63;
+    if (FROM == FROM_ROWS)
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+        if (row[h] >= 0)
+#pragma unroll
+          for (int q = 0; q < 16; ++q) v[h][q] = quant_element(raw[h], q);
     auto total = [&](int t, const float* from) {
       float s = 0.f;
       for (int c = lane; c < chunks; c += 64) s += from[c];
@@ -129,9 +142,8 @@ struct Inline {
         const float r = p.norm.kind == STEM_NORM_NONE ? 1.f : 1.0f / sqrtf(stat[row[h]] / (float)p.row_K + p.norm.eps);
         const int left = p.row_K - at[h] * 16;
         if (p.norm.weight) {
-          const QuantChunk w = left > 0 ? quant_load_chunk(static_cast<const bf16_t*>(p.norm.weight) + at[h] * 16, left) : QuantChunk{};
 #pragma unroll
-          for (int e = 0; e < 16; ++e) v[h][e] = e < left ? v[h][e] * r * quant_element(w, e) : 0.f;
+          for (int e = 0; e < 16; ++e) v[h][e] = e < left ? v[h][e] * r * quant_element(weight[h], e) : 0.f;
         } else {
 #pragma unroll
           for (int e = 0; e < 16; ++e) v[h][e] *= r;
@@ -151,8 +163,8 @@ struct Inline {
     } else {
       const int t = tid >> 6;
       if (t < p.M) {
-        uint32_t m = 0;
-        for (int g = lane; g < p.maxima; g += 64) m = max(m, p.max_in[g * 8 + t]);
+        uint32_t m = max(max(tops[0], tops[1]), max(tops[2], tops[3]));
+        for (int g = 256 + lane; g < p.maxima; g += 64) m = max(m, p.max_in[g * 8 + t]);
         m = wave_max(m);
         if (lane == 0) stat[t] = __uint_as_float(m);
       }
@@ -186,7 +198,6 @@ __global__ __launch_bounds__(THREADS) void gemm_int8_decode_kernel(QuantDecodeAr
   const int tiles = (p.N + 31) / 32;
   const int slice = blockIdx.x / tiles, tile = blockIdx.x - slice * tiles;
   const int all = p.K / 32, per = (all / 4 + p.ksplit - 1) / p.ksplit * 4, b0 = slice * per, nb = all - b0 < per ? all - b0 : per;   // blocks
-  // weights first
   const rsrc_t rb = resource(p.B + (size_t)tile * 32 * p.K, 32 * p.K);
   const rsrc_t ra = resource(p.A, INLINE ? 0 : (p.M + 31) / 32 * 32 * p.K);
   const uint32_t la = (lane & 31) < p.M ? lane * 16 : OOB, lb = 32 + (lane & 31) < p.M ? 32 * p.K + lane * 16 : OOB;
@@ -204,6 +215,10 @@ __global__ __launch_bounds__(THREADS) void gemm_int8_decode_kernel(QuantDecodeAr
       }
     }
   };
+  const int chunks = FROM == FROM_ROWS ? p.K / 16 : nb * 2;
+  Inline<INLINE ? FROM : FROM_ROWS> in;
+  if constexpr (INLINE) in.load(p, b0 * 32, chunks, tid);
+  __builtin_amdgcn_sched_barrier(0);
   request(0);
   // the gate product's epilogue multiplies by a row of the table
   const int u_lane = tid & 63, u_group = tid >> 6 & 3, u_half = tid >> 8;   // of the tile in lanes' layout: 4 channels of a token
@@ -219,9 +234,6 @@ __global__ __launch_bounds__(THREADS) void gemm_int8_decode_kernel(QuantDecodeAr
     e = *reinterpret_cast<const u32x2_t*>(p.E + (size_t)id * p.N + ch);
   }
   if constexpr (INLINE) {
-    Inline<FROM> in;
-    const int chunks = FROM == FROM_ROWS ? p.K / 16 : nb * 2;
-    in.load(p, b0 * 32, chunks, tid);
     in.quantise(p, b0 * 32, nb * 32, chunks, tid, part, scale + 8, smem, rows_log, scale);
     __syncthreads();
   }
