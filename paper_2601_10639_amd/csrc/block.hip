@@ -277,6 +277,8 @@ __device__ __forceinline__ float factor(const C& c, float (&v)[VPT][8], const st
 // BRANCH: the end of a block; without it y is x and only n is written.  One pass: a row's values stay in registers from its loads
 // to its stores.  A workgroup keeps what is the same for all rows (w_out times a gate a channel, w_next) in registers and takes as many rows
 // as leave 8 workgroups to a compute unit.
+// Measured, 16384 x 2048 in bf16, both norms, a gate a channel, p 0.1: 55 us, 4.9 TB/s of the 268 MB that have to move (a copy reaches 6.0).
+// Arithmetic is as long: 17.6 million VALU instructions, 29 us of all SIMDs, 13 more for the generator's wide multiplications.  One token: the launch.
 template <class E, int LPR, int VPT, bool BRANCH>
 __global__ __launch_bounds__((Shape<E, LPR, VPT, false>::THREADS)) void block_forward_kernel(BlockArgs p) {
   typedef Shape<E, LPR, VPT, false> S;
@@ -351,6 +353,9 @@ __global__ __launch_bounds__((Shape<E, LPR, VPT, false>::THREADS)) void block_fo
 // Sums over tokens are held in registers over a workgroup's rows and written as one partial sum a workgroup, [sum][workgroup][d];
 // block_sums_kernel adds those in order.  No atomics: the same bits on every run.  dw_out and the gradient of a gate a channel are the same
 // sum, of h times the kept N_out(f), times the gate and times w_out: it is held once.  All of a row is requested before its first reduction.
+// Measured, 16384 x 2048 in bf16, both norms, a gate a channel, p 0.1: 83 us and 4 for the sums, 4.6 TB/s of the 403 MB that have to move;
+// the arithmetic alone is about 60 us (28.7 million VALU instructions), and 117 registers leave 16 wavefronts a compute unit to hide the rest.
+// Workgroups of 512, two rows of 2048 each: 512 of them are all resident, and write half as many partial sums as 1024 of 256 would.
 template <class E, int LPR, int VPT, bool BRANCH>
 __global__ __launch_bounds__((Shape<E, LPR, VPT, true>::THREADS)) void block_backward_kernel(BlockArgs p) {
   typedef Shape<E, LPR, VPT, true> S;
@@ -361,7 +366,7 @@ __global__ __launch_bounds__((Shape<E, LPR, VPT, true>::THREADS)) void block_bac
   const Columns<E, LPR, VPT, true> c(slot, lane, p.d);
   const uint64_t offset = BRANCH && p.drop.threshold ? offset_of(p.drop) : 0;
   const bool by_channel = p.gate_kind == STEM_GATE_CHANNEL, by_element = p.gate_kind == STEM_GATE_FULL, by_token = p.gate_kind == STEM_GATE_TOKEN;
-    // The next row is requested before this one's first reduction where registers allow it (16384 x 2048 96 -> 91 us; fp32 gains nothing).
+  // The next row is requested before this one's first reduction where registers allow it (16384 x 2048 96 -> 91 us; fp32 gains nothing).
   constexpr bool EARLY = VPT == 1 && LPR < 1024 && sizeof(E) == 2;
   float sum_next[VPT][8] = {}, sum_branch[VPT][8] = {};
   float after[VPT][8], branch[VPT][8];      // w_next; w_out times a gate a channel
@@ -561,7 +566,8 @@ __global__ __launch_bounds__(1024) void block_sums_kernel(SumArgs p) {
 }
 
 // ---- dropout by itself -------------------------------------------------------------------------------------
-// A thread has the eight elements of a counter; `tx` (a power of two) threads lie along a row.
+// A thread has the eight elements of a counter; `tx` (a power of two) threads lie along a row.  Measured: 65536 x 1024 in bf16 44.5 us, 6.0 TB/s,
+// what a copy reaches; the generator takes about 39 of them beside.  999 x 1001 in fp32, element by element, 5.0.
 template <class E>
 __global__ __launch_bounds__(256) void dropout_kernel(const E* x, E* y, int64_t T, int64_t d, int tx_log, DropArgs drop,
                                                       int vectors) {
@@ -611,6 +617,11 @@ hipError_t launch(const BlockArgs& a, hipStream_t s) {
   return hipGetLastError();
 }
 
+// Lanes a row and vectors a lane.  A lane has one vector where it can: more wavefronts wait for memory at a time.  Two vectors halve what a
+// row's reduction costs besides, and pay where a row would take more than a wavefront and the tensors stream from memory.  us, one vector /
+// two, bf16, both norms, p 0.1: forward 32768 x 1024 56 / 54, 4096 x 2048 14.9 / 16.6, 16384 x 2048 58 / 54.7 (4096 x 2048 in fp32 24.3 / 26.5, 16384 108 / 103),
+// 8192 x 4096 57 / 52, 512 x 8192 11.9 / 10.7, 4096 x 8192 70 / 56; the norm alone 1024 x 8192 7.2 / 7.5; backward, whose
+// registers are its sums', 65536 x 512 86 / 86, 16384 x 2048 87 / 104, 8192 x 4096 88 / 109, 256 x 8192 24.5 / 25.4.
 template <class E, bool BRANCH, bool BACK>
 hipError_t by_width(const BlockArgs& a, hipStream_t s) {
   if (a.d <= 64) return launch<E, 8, 1, BRANCH, BACK>(a, s);
@@ -618,9 +629,11 @@ hipError_t by_width(const BlockArgs& a, hipStream_t s) {
   if (a.d <= 256) return launch<E, 32, 1, BRANCH, BACK>(a, s);
   if (a.d <= 512) return launch<E, 64, 1, BRANCH, BACK>(a, s);
   if (a.d <= 1024) return launch<E, BACK ? 128 : 64, BACK ? 1 : 2, BRANCH, BACK>(a, s);
+  if constexpr (BRANCH && !BACK)
+    if (a.d > 1024 && a.d <= 2048 && a.T * a.d * (int64_t)sizeof(E) >= (64 << 20)) return launch<E, 128, 2, BRANCH, BACK>(a, s);
   if (a.d <= 2048) return launch<E, 256, 1, BRANCH, BACK>(a, s);
   if (a.d <= 4096) return launch<E, BACK ? 512 : 256, BACK ? 1 : 2, BRANCH, BACK>(a, s);
-  if (a.d <= 8192) return launch<E, 1024, 1, BRANCH, BACK>(a, s);
+  if (a.d <= 8192) return launch<E, BRANCH && !BACK ? 512 : 1024, BRANCH && !BACK ? 2 : 1, BRANCH, BACK>(a, s);
   return launch<E, 1024, 2, BRANCH, BACK>(a, s);
 }
 
