@@ -355,7 +355,8 @@ __global__ __launch_bounds__((Shape<E, LPR, VPT, false>::THREADS)) void block_fo
 // sum, of h times the kept N_out(f), times the gate and times w_out: it is held once.  All of a row is requested before its first reduction.
 // Measured, 16384 x 2048 in bf16, both norms, a gate a channel, p 0.1: 83 us and 4 for the sums, 4.6 TB/s of the 403 MB that have to move;
 // the arithmetic alone is about 60 us (28.7 million VALU instructions), and 117 registers leave 16 wavefronts a compute unit to hide the rest.
-// Workgroups of 512, two rows of 2048 each: 512 of them are all resident, and write half as many partial sums as 1024 of 256 would.
+// Workgroups of 512, two rows of 2048 each: 512 of them are all resident, and write half as many partial sums as 1024 of 256 would.  Of 1024
+// a compute unit holds one: 256 (512 take two turns: 4096 x 8192 119 us instead of 112, 1024 x 8192 46.7 / 37.2, 2048 x 16384 157 / 139).
 template <class E, int LPR, int VPT, bool BRANCH>
 __global__ __launch_bounds__((Shape<E, LPR, VPT, true>::THREADS)) void block_backward_kernel(BlockArgs p) {
   typedef Shape<E, LPR, VPT, true> S;
@@ -368,9 +369,29 @@ __global__ __launch_bounds__((Shape<E, LPR, VPT, true>::THREADS)) void block_bac
   const bool by_channel = p.gate_kind == STEM_GATE_CHANNEL, by_element = p.gate_kind == STEM_GATE_FULL, by_token = p.gate_kind == STEM_GATE_TOKEN;
   // The next row is requested before this one's first reduction where registers allow it (16384 x 2048 96 -> 91 us; fp32 gains nothing).
   constexpr bool EARLY = VPT == 1 && LPR < 1024 && sizeof(E) == 2;
-  float sum_next[VPT][8] = {}, sum_branch[VPT][8] = {};
-  float after[VPT][8], branch[VPT][8];      // w_next; w_out times a gate a channel
-  c.weight(p.next.weight, after);
+  // Rows of two vectors a lane (1024 lanes, 128 registers): the weights are read again for each row, and the sums over tokens lie in LDS
+  // where there are two, each lane's own (2048 x 16384 in bf16 306 us with all in registers and scratch memory, 157 so).
+  constexpr bool AGAIN = VPT == 2, IN_LDS = AGAIN && BRANCH;
+  __shared__ float4 lds_sum[IN_LDS ? 4 * VPT * S::THREADS : 1];
+  enum { NEXT, OUT };
+  float sum[2][VPT][8] = {};
+  auto place = [&](int which, int t, int half) __attribute__((always_inline)) {
+    return lds_sum + (IN_LDS ? ((which * VPT + t) * 2 + half) * S::THREADS + threadIdx.x : 0);
+  };
+  auto add = [&](int which, int t, const float (&a)[8], const float (&b)[8]) __attribute__((always_inline)) {
+    float(&v)[8] = sum[which][t];
+    float4 w[2];
+    if (IN_LDS) { w[0] = *place(which, t, 0); w[1] = *place(which, t, 1); memcpy(v, w, 32); }
+#pragma unroll
+    for (int q = 0; q < 8; ++q) v[q] = __builtin_fmaf(a[q], b[q], v[q]);
+    if (IN_LDS) { memcpy(w, v, 32); *place(which, t, 0) = w[0]; *place(which, t, 1) = w[1]; }
+  };
+  if (IN_LDS)
+#pragma unroll
+    for (int k = 0; k < 4 * VPT; ++k) lds_sum[k * S::THREADS + threadIdx.x] = make_float4(0.f, 0.f, 0.f, 0.f);
+  // w_next; w_out times a gate a channel
+  float after[VPT][8], branch[VPT][8];
+  if (!AGAIN) c.weight(p.next.weight, after);
   auto branch_weight = [&](float (&w)[VPT][8], bool weight, bool gate) __attribute__((always_inline)) {
     c.weight(weight ? p.out.weight : nullptr, w);
     if (gate && by_channel) {
@@ -382,7 +403,7 @@ __global__ __launch_bounds__((Shape<E, LPR, VPT, true>::THREADS)) void block_bac
         for (int q = 0; q < 8; ++q) w[t][q] *= g[t][q];
     }
   };
-  if (BRANCH) branch_weight(branch, true, true);
+  if (BRANCH && !AGAIN) branch_weight(branch, true, true);
   const float of_branch = p.branch_scale * (p.drop.threshold ? p.drop.scale : 1.f);
   typedef typename Columns<E, LPR, VPT, true>::Raw Raw;
   struct Row { Raw dy[VPT], f[VPT], y[VPT], dn[VPT]; };
@@ -421,13 +442,13 @@ __global__ __launch_bounds__((Shape<E, LPR, VPT, true>::THREADS)) void block_bac
       }
       const float r = factor(c, y, p.next, p.inv_d, row_sum), r_live = live ? r : 0.f;
       scale_by(y, r_live);
+      if (AGAIN) c.weight(p.next.weight, after);
 #pragma unroll
-      for (int t = 0; t < VPT; ++t)
+      for (int t = 0; t < VPT; ++t) {
+        add(NEXT, t, h[t], y[t]);
 #pragma unroll
-        for (int q = 0; q < 8; ++q) {
-          sum_next[t][q] = __builtin_fmaf(h[t][q], y[t][q], sum_next[t][q]);
-          h[t][q] *= after[t][q];
-        }
+        for (int q = 0; q < 8; ++q) h[t][q] *= after[t][q];
+      }
       c.add_back(G, h, y, r_live, p.next.kind, p.inv_d, row_sum);
     }
     const rsrc_t rdx = rows(p.dx);
@@ -452,6 +473,7 @@ __global__ __launch_bounds__((Shape<E, LPR, VPT, true>::THREADS)) void block_bac
     }
     const float of_row = by_token ? load1(static_cast<const E*>(p.gate) + (live ? row : p.T - 1)) : 1.f;
     float token_gate = 0.f;
+    if (AGAIN) branch_weight(branch, true, true);
 #pragma unroll
     for (int t = 0; t < VPT; ++t) {
       float g[8], dg[8];
@@ -481,11 +503,9 @@ __global__ __launch_bounds__((Shape<E, LPR, VPT, true>::THREADS)) void block_bac
         }
         if (by_element) c.store(rows(p.dgate), t, dg);
       }
+      add(OUT, t, G[t], u);
 #pragma unroll
-      for (int q = 0; q < 8; ++q) {
-        sum_branch[t][q] = __builtin_fmaf(G[t][q], u[q], sum_branch[t][q]);
-        G[t][q] *= branch[t][q];
-      }
+      for (int q = 0; q < 8; ++q) G[t][q] *= branch[t][q];
     }
     if (by_token && p.dgate) {
       float s[1] = {token_gate};
@@ -526,7 +546,13 @@ __global__ __launch_bounds__((Shape<E, LPR, VPT, true>::THREADS)) void block_bac
       to[k] = s;
     }
   };
-  if (p.part[0]) write(sum_next, p.part[0]);
+  if (IN_LDS)
+#pragma unroll
+    for (int k = 0; k < 2 * VPT; ++k) {
+      const float4 w[2] = {*place(k / VPT, k % VPT, 0), *place(k / VPT, k % VPT, 1)};
+      memcpy(sum[k / VPT][k % VPT], w, 32);
+    }
+  if (p.part[0]) write(sum[NEXT], p.part[0]);
   if (BRANCH) {
 #pragma unroll 1
     for (int which = 1; which < 3; ++which) {
@@ -536,7 +562,7 @@ __global__ __launch_bounds__((Shape<E, LPR, VPT, true>::THREADS)) void block_bac
 #pragma unroll
       for (int t = 0; t < VPT; ++t)
 #pragma unroll
-        for (int q = 0; q < 8; ++q) w[t][q] *= sum_branch[t][q];
+        for (int q = 0; q < 8; ++q) w[t][q] *= sum[OUT][t][q];
       write(w, p.part[which]);
     }
   }
@@ -596,7 +622,7 @@ __global__ __launch_bounds__(256) void dropout_kernel(const E* x, E* y, int64_t 
 template <class E, int LPR, int VPT, bool BRANCH, bool BACK>
 hipError_t launch(const BlockArgs& a, hipStream_t s) {
   typedef Shape<E, LPR, VPT, BACK> S;
-  const int64_t groups = (a.T + S::SLOTS - 1) / S::SLOTS, most = BACK ? STEM_BLOCK_GRID : 2048 * 256 / S::THREADS;
+  const int64_t groups = (a.T + S::SLOTS - 1) / S::SLOTS, most = BACK ? STEM_BLOCK_GRID / (LPR == 1024 ? 2 : 1) : 2048 * 256 / S::THREADS;
   const int grid = (int)(groups < most ? groups : most);
   if constexpr (BACK) {
     BlockArgs p = a;

@@ -129,6 +129,31 @@ def test_leave(dtype, T, d, out, next, gate, p):
     assert torch.equal(x, y)
 
 
+# a workgroup takes several rows, of which each lane has two vectors
+@pytest.mark.parametrize("dtype,T,d,out,next,gate,p", [("bf16", 600, 8256, "rms", "layer", "channel", 0.1), ("f32", 530, 9004, "layer", "rms", "token", 0.1),
+                                                       ("bf16", 300, 16384, "none", "rms", "full", 0.0), ("f32", 257, 16384, "rms", "none", "channel", 0.0),
+                                                       ("bf16", 700, 8192, "rms", "rms", "channel", 0.1)])
+def test_leave_of_many_wide_rows(dtype, T, d, out, next, gate, p):
+    test_leave(dtype, T, d, out, next, gate, p)
+
+
+@pytest.mark.parametrize("dtype,T,d", [("bf16", 300, 12032), ("f32", 515, 9004), ("bf16", 515, 8192)])
+@pytest.mark.parametrize("kind", ["rms", "layer"])
+def test_enter_of_many_wide_rows(dtype, T, d, kind):
+    test_enter(dtype, T, d, kind)
+
+
+@pytest.mark.parametrize("dtype,T,d", [("bf16", 16500, 2048), ("bf16", 33000, 1088), ("f32", 8300, 2044)])
+def test_leave_forward_of_64_mib(dtype, T, d):
+    ctx = make_ctx(dtype, T, d)
+    f, x, g, leave, ref = leave_case(dtype, T, d, "rms", "layer", "channel", 0.1)
+    y, n = empty_like(x), empty_like(x)
+    L.stem_block_leave_forward(ctx, f, x, leave, y, n)
+    for rows in (slice(0, 40), slice(T // 2, T // 2 + 40), slice(T - 40, T)):
+        wy, wn = B.leave_forward(num(f[rows]), num(x[rows]), **dict(ref, factor=ref["factor"][rows]))
+        assert max_rel(num(y[rows]), wy) <= TOL[dtype] and max_rel(num(n[rows]), wn) <= TOL[dtype]
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_leave_with_one_gradient_or_few_outputs(dtype):
     T, d = 37, 192
