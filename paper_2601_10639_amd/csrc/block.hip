@@ -623,7 +623,10 @@ template <class E, int LPR, int VPT, bool BRANCH, bool BACK>
 hipError_t launch(const BlockArgs& a, hipStream_t s) {
   typedef Shape<E, LPR, VPT, BACK> S;
   const int64_t groups = (a.T + S::SLOTS - 1) / S::SLOTS, most = BACK ? STEM_BLOCK_GRID / (LPR == 1024 ? 2 : 1) : 2048 * 256 / S::THREADS;
-  const int grid = (int)(groups < most ? groups : most);
+  // Up to 512 workgroups of the backward pass are done in one round either way: about as many take two rows in turn, and write half as many
+  // partial sums (us, 1024 x 2048 19.2 -> 16.4, its fp32 19.3 -> 19.8, 512 x 4096 22.8 -> 20.0; fewer gain nothing: 512 x 2048 12.9 / 13.5).
+  const bool in_turn = BACK && groups > 384 && groups <= STEM_BLOCK_GRID;
+  const int grid = (int)(in_turn ? (groups + 1) / 2 : groups < most ? groups : most);
   if constexpr (BACK) {
     BlockArgs p = a;
     SumArgs q = {};
