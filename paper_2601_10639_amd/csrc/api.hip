@@ -167,6 +167,7 @@ void release(stem_ctx* c) {
   free(c->cache_id_in_slot); free(c->cache_slot_of); free(c->cache_freq);
   (void)hipFree(c->edit_idx_dev); (void)hipFree(c->edit_rep_dev);
   (void)hipFree(c->block_part);
+  if (c->quant_ws != reinterpret_cast<int*>(c->splitk_ws)) (void)hipFree(c->quant_ws);
   (void)hipFree(c->quant_x); (void)hipFree(c->quant_h); (void)hipFree(c->quant_sx); (void)hipFree(c->quant_sh); (void)hipFree(c->quant_amax); (void)hipFree(c->quant_max); (void)hipFree(c->quant_hidden);
   if (c->inst_pinned) (void)hipHostFree(c->inst_pinned);
   (void)hipFree(c->inst_dev);
@@ -391,6 +392,10 @@ stem_status stem_reserve(stem_ctx* c, uint32_t what) {
     if (!c->quant_sh) HIP_TRY(c, dmalloc(&c->quant_sh, (size_t)T));
     if (!c->quant_amax) HIP_TRY(c, dmalloc(&c->quant_amax, (size_t)std::max<int64_t>(T, std::min<int64_t>(T, STEM_QUANT_DECODE_TOKENS) * QUANT_AMAX_STRIDE)));
     if (!c->quant_max) HIP_TRY(c, dmalloc(&c->quant_max, (size_t)(F / 32 * 8)));
+    if (!c->quant_ws) {
+      if (c->splitk_bytes >= QUANT_WS) c->quant_ws = reinterpret_cast<int*>(c->splitk_ws);
+      else HIP_TRY(c, dmalloc(&c->quant_ws, (size_t)QUANT_WS / sizeof(int)));
+    }
     HIP_TRY(c, dmalloc(&c->quant_hidden, (size_t)((std::min(T, stem_quant_chunk(F)) + 31) / 32 * 32 * stem_quant_pitch(F))));
   }
   return STEM_OK;

@@ -113,7 +113,7 @@ hipError_t quant_rows(stem_ctx* c, int kid, const void* x, int64_t rows, int64_t
 
 QuantGemmArgs gemm_args(const stem_ctx* c) {
   QuantGemmArgs a = {};
-  a.ws = reinterpret_cast<int*>(c->splitk_ws); a.ws_bytes = c->splitk_bytes; a.tickets = c->tickets;
+  a.ws = c->quant_ws; a.ws_bytes = QUANT_WS; a.tickets = c->tickets;
   return a;
 }
 
@@ -121,8 +121,8 @@ QuantDecodeArgs decode_args(const stem_ctx* c, int64_t T, int64_t N, int64_t K, 
   QuantDecodeArgs a = {};
   a.B = static_cast<const int8_t*>(q); a.scale_b = scale;
   a.M = (int)T; a.N = (int)N; a.K = (int)K;
-  a.ksplit = stem_quant_decode_slices((int)N, (int)K, c->splitk_bytes, (int)T);
-  a.ws = reinterpret_cast<int*>(c->splitk_ws); a.tickets = c->tickets;
+  a.ksplit = stem_quant_decode_slices((int)N, (int)K, QUANT_WS, (int)T);
+  a.ws = c->quant_ws; a.tickets = c->tickets;
   return a;
 }
 

@@ -716,9 +716,9 @@ hipError_t launch(const QuantGemmArgs& a, hipStream_t s) {
 //   N 8192, K 2048, gate: 80 tokens 15.4 / 14.9 / 20, 256 17.6 / 16.1 / 21, 400 23 / 18 / 22, 700 32 / 27 / 24.5, 4096 155 / 121 / 83
 //   N 4096, K 1024, gate: 256 tokens 11.7 / 11.7 / 15, 700 17 / 14 / 17, 1500 24 / 23 / 18
 //   N 2048, K 8192: 700 tokens 24 / 28 / 47 / 73, 1500 44 / 31 / 50 / 76, 4096 94 / 72 / 66 / 89, 16384 - / - / 241 / 218
-// K is cut where tiles are few and slices long, in up to 4 (a slice of 8 K tiles or more, 240 workgroups or fewer; in two slices 256, from 48
-// K tiles): N 2048, K 8192, 1 / 2 / 3 / 4 slices of 128 x 64 tiles: 80 tokens 19 / 15.5 / 14.1 / 14.2, 256 20.6 / 17.1 / 15.6 / 16.6, 400 21.5 / 18.2 / 24 / 23;
-// N 1024, K 4096: 128 tokens 13.3 / 12.5 / 12.0 / 12.1, 1024 14.6 / 15.5; N 448, K 1472: 256 tokens 9.4 / 10.2 / 10.4.
+// K is cut where tiles are few and slices long, in up to 4 (from 32 K tiles on, a slice of 10 or more, 240 workgroups or fewer; in two slices 256, from 48
+// K tiles): K 2048, 1 / 2 / 3 slices of 128 x 64 tiles: 700 tokens of N 1000 13.1 / 14.6 / -, 256 of N 1024 11.2 / 12.0 / 11.7; K 4096, 1024 of N 512 20.5 / 19.7 / 19.2; N 2048, K 8192, 1 / 2 / 3 / 4 slices of 128 x 64 tiles: 80 tokens 19 / 15.5 / 14.1 / 14.2, 256 20.6 / 17.1 / 15.6 / 16.6, 400 21.5 / 18.2 / 24 / 23;
+// N 1024, K 4096: 128 tokens 13.3 / 12.5 / 12.0 / 12.1, 1024 14.6 / 15.5.
 // Cut gate products were slower throughout (256 tokens of N 8192, K 2048 17.6 / 23.1).
 extern "C" void stem_route_quant(int M, int N, int K, int gate, int64_t ws_bytes, int32_t* route) {
   auto tiles = [&](int tm, int tn) { return (int64_t)((M + tm - 1) / tm) * ((N + tn - 1) / tn); };
@@ -734,7 +734,7 @@ extern "C" void stem_route_quant(int M, int N, int K, int gate, int64_t ws_bytes
     if (!gate && (double)((t256 + 255) / 256) <= few) rows = 256;
   }
   if (!gate && cols == 64) {
-    slices = (int)std::min<int64_t>({MAX_SLICES, nk / 8, 240 / t64});
+    slices = nk < 32 ? 1 : (int)std::min<int64_t>({MAX_SLICES, nk / 10, 240 / t64});
     if (slices < 2 && t64 <= 128 && nk >= 48) slices = 2;
     while (slices > 1 && (int64_t)slices * t64 * 128 * 64 * 4 > ws_bytes) --slices;
     while (slices > 1 && (nk + slices - 1) / slices * (slices - 1) >= nk) --slices;   // every slice has a part of K

@@ -60,6 +60,7 @@ struct QuantHiddenArgs {
 hipError_t stem_quant_hidden_launch(stem_ctx* ctx, const QuantHiddenArgs& a, hipStream_t s);
 
 #define STEM_QUANT_DECODE_TOKENS 64
+#define QUANT_WS (256 * 128 * 64 * 4)   // bytes: a product is cut into 256 workgroups at most, of tiles of up to 128 x 64
 // Every workgroup of a few tokens' product has all of them: their maxima lie in lines of their own, or the atomics of 256 workgroups on one line
 // take longer than the product (16 tokens of 2048 x 8192: the gate product 65 us instead of 10)
 #define QUANT_AMAX_STRIDE 32

@@ -127,6 +127,7 @@ struct stem_ctx {
   uint32_t* quant_amax;           // the largest magnitudes of tokens' hidden values
   uint32_t* quant_max;            // those of up to 8 tokens, in each tile of 32 channels
   float* quant_hidden;            // hidden values of stem_quant_chunk tokens
+  int* quant_ws;         // sums of the 8-bit products' K slices: the room above where that has QUANT_WS bytes, else its own
 
   // profiling
   int prof_on;

@@ -36,3 +36,8 @@ def test_every_slice_has_a_part_of_k_and_room():
                                              (4096, 2048, 8192, False, (128, 256, 1)), (16384, 2048, 8192, False, (256, 256, 1)), (4096, 8192, 2048, True, (128, 256, 1))])
 def test_measured_choices(M, N, K, gate, want):
     assert route(M, N, K, gate, 64 << 20) == want
+
+
+@pytest.mark.parametrize("M,N,K,slices", [(700, 1001, 2048, 1), (256, 1024, 2048, 1), (512, 1024, 2944, 1), (128, 1024, 4096, 3), (1024, 512, 4096, 3), (80, 2048, 8192, 4)])
+def test_short_products_are_not_cut(M, N, K, slices):
+    assert route(M, N, K, False, 64 << 20) == (128, 64, slices)
