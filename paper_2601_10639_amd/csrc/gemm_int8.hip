@@ -147,52 +147,60 @@ struct Output {
       }
       return;
     }
-    // Rows of y at any 2-byte address: 16 bytes at a time where all of them are the tile's, and the ends of each row, up to 7 columns on
-    // either side, one by one.  (One by one throughout: 4000 x 5001, K 1999, 191 us instead of 67, against 48 at 5000 columns.)
-    constexpr int GROUPS = COLS / 8 + 1, UNITS = (32 * GROUPS + 63) / 64;
-    uint32_t whole_at[AHEAD][UNITS], end_at[AHEAD][8];
-    int whole_st[AHEAD][UNITS], end_st[AHEAD][8];   // where in the staged rows
-    u32x4_t rz[AHEAD][UNITS];
-    uint16_t re[AHEAD][8];
+    // Rows of y at any 2-byte address: the same lanes store the same 8 columns, as global stores, which take any address; the last ones of the
+    // matrix's rows that are fewer go one by one, eight rows at a time.  (4000 x 5001, K 1999, with residual: 62 us, against 56 at 5000 columns; 191 with
+    // all columns one by one, 77 with 16-byte boundaries sought in each row.)
+    const int srow = lane / LPR, scol = (lane % LPR) * 8, left = lim - scol;
+    const bool edge = lim % 8 != 0;                            // of the matrix, in this tile
+    bf16_t* const y = p.y + (size_t)m0 * p.N + n0 + scol;
+    const bf16_t* const res = p.residual ? p.residual + (size_t)m0 * p.N + n0 + scol : nullptr;
+    u32x4_t rz[AHEAD][PASSES];
+    uint32_t end_at[AHEAD][4];
+    uint16_t re[AHEAD][4];
+    const int end_col = (lim & ~7) + (lane & 7);
     auto fetch = [&](int i) __attribute__((always_inline)) {
-      const int k = i % AHEAD;
-      auto head = [&](int r) __attribute__((always_inline)) {   // columns in front of row r's first 16-byte boundary
-        return (8 - (((m0 + i * 32 + r) & 7) * (p.N & 7) + n0 & 7)) & 7;
-      };
 #pragma unroll
-      for (int u = 0; u < UNITS; ++u) {
-        const int e = u * 64 + lane, r = e / GROUPS < 32 ? e / GROUPS : 31, h = head(r), col = (e % GROUPS) * 8 + (h ? h - 8 : 0);
-        const bool ok = e / GROUPS < 32 && i * 32 + r < rows && col >= 0 && col + 8 <= lim;
-        whole_at[k][u] = at(i * 32 + r, col, ok);
-        whole_st[k][u] = ok ? r * PITCH + col : 0;
-        rz[k][u] = u32x4_t{};
-        if (p.residual) rz[k][u] = __builtin_amdgcn_raw_buffer_load_b128(rr, whole_at[k][u], 0, 0);
+      for (int pass = 0; pass < PASSES; ++pass) {
+        const int r = i * 32 + pass * RPP + srow;
+        u32x4_t& v = rz[i % AHEAD][pass];
+        v = u32x4_t{};
+        if (res && left >= 8 && r < rows) __builtin_memcpy(&v, res + (size_t)r * p.N, 16);
       }
+      if (edge)
 #pragma unroll
-      for (int u = 0; u < 8; ++u) {   // column q of up to 7 in front, or q - 8 behind
-        const int e = u * 64 + lane, r = e >> 4, q = e & 15, h = head(r);
-        const int col = q < 8 ? q : (lim > h ? h + ((lim - h) & ~7) : 0) + q - 8;
-        const bool ok = i * 32 + r < rows && (q < 8 ? col < h && col < lim : lim > h && col < lim);
-        end_at[k][u] = at(i * 32 + r, col, ok);
-        end_st[k][u] = ok ? r * PITCH + col : 0;
-        re[k][u] = 0;
-        if (p.residual) re[k][u] = __builtin_amdgcn_raw_buffer_load_b16(rr, end_at[k][u], 0, 0);
-      }
+        for (int u = 0; u < 4; ++u) {
+          const int r = i * 32 + u * 8 + (lane >> 3);
+          end_at[i % AHEAD][u] = at(r, end_col, end_col < lim && r < rows);
+          re[i % AHEAD][u] = p.residual ? __builtin_amdgcn_raw_buffer_load_b16(rr, end_at[i % AHEAD][u], 0, 0) : 0;
+        }
     };
     if (AHEAD > 1)
 #pragma unroll
       for (int i = 0; i < MI; ++i) fetch(i);
 #pragma unroll
     for (int i = 0; i < MI; ++i) {
-      const int k = i % AHEAD;
       if (AHEAD == 1) fetch(i);
       to_lds(i);
 #pragma unroll
-      for (int u = 0; u < UNITS; ++u) add_and_store(st + whole_st[k][u], whole_at[k][u], rz[k][u]);
+      for (int pass = 0; pass < PASSES; ++pass) {
+        const int r = i * 32 + pass * RPP + srow;
+        float z[8];
+        __builtin_memcpy(z, st + (pass * RPP + srow) * PITCH + scol, 32);
+        if (left >= 8 && r < rows) {
+          const u32x4_t v = rz[i % AHEAD][pass];
+          bf16x8_t o;
 #pragma unroll
-      for (int u = 0; u < 8; ++u)
-        __builtin_amdgcn_raw_buffer_store_b16(__builtin_bit_cast(uint16_t, (__bf16)(st[end_st[k][u]] + __uint_as_float((uint32_t)re[k][u] << 16))), ry,
-                                              end_at[k][u], 0, 0);
+          for (int q = 0; q < 8; ++q) o[q] = (__bf16)(z[q] + __uint_as_float(q & 1 ? v[q >> 1] & 0xffff0000u : v[q >> 1] << 16));
+          __builtin_memcpy(y + (size_t)r * p.N, &o, 16);
+        }
+      }
+      if (edge)
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+          const float z = st[(u * 8 + (lane >> 3)) * PITCH + end_col];
+          __builtin_amdgcn_raw_buffer_store_b16(__builtin_bit_cast(uint16_t, (__bf16)(z + __uint_as_float((uint32_t)re[i % AHEAD][u] << 16))), ry,
+                                                end_at[i % AHEAD][u], 0, 0);
+        }
       in_order();
       __builtin_amdgcn_sched_barrier(0);
     }
