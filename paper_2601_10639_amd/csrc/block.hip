@@ -277,8 +277,8 @@ __device__ __forceinline__ float factor(const C& c, float (&v)[VPT][8], const st
 // BRANCH: the end of a block; without it y is x and only n is written.  One pass: a row's values stay in registers from its loads
 // to its stores.  A workgroup keeps what is the same for all rows (w_out times a gate a channel, w_next) in registers and takes as many rows
 // as leave 8 workgroups to a compute unit.
-// Measured, 16384 x 2048 in bf16, both norms, a gate a channel, p 0.1: 55 us, 4.9 TB/s of the 268 MB that have to move (a copy reaches 6.0).
-// Arithmetic is as long: 17.6 million VALU instructions, 29 us of all SIMDs, 13 more for the generator's wide multiplications.  One token: the launch.
+// Measured, 16384 x 2048 in bf16, both norms, a gate a channel, p 0.1: 53 to 55 us, 5 TB/s of the 268 MB that have to move (a copy reaches 6.0).
+// Arithmetic is nearly as long: about 17 million VALU instructions, 29 us of all SIMDs, 13 more for the generator's wide multiplications.  One token: the launch.
 template <class E, int LPR, int VPT, bool BRANCH>
 __global__ __launch_bounds__((Shape<E, LPR, VPT, false>::THREADS)) void block_forward_kernel(BlockArgs p) {
   typedef Shape<E, LPR, VPT, false> S;
