@@ -271,7 +271,8 @@ typedef struct {
 } stem_leave;
 
 /* For all of these: d is the context's d_model, up to 16384; sums and statistics in fp32, every output rounded once; in the calls of this
- * section an output [T,d] may be one of the inputs [T,d] (the same address), and overlaps nothing otherwise. */
+ * section an output [T,d] may be one of the inputs [T,d] (the same address), and overlaps nothing otherwise.  T == 0: sums over tokens
+ * are zero (or left as they are when accumulate != 0), nothing else is read or written. */
 
 /* n = N(x) * w: the norm in front of a block.  norm (host): not STEM_NORM_NONE. */
 stem_status stem_block_enter_forward(stem_ctx* ctx, const void* x, int64_t T, const stem_norm* norm, void* n, void* stream);

@@ -94,6 +94,16 @@ stem_status check_leave(stem_ctx* c, const char* who, const stem_leave& L, Block
   return STEM_OK;
 }
 
+// Sums over no tokens: zero, unless they are added to what is there.
+stem_status no_tokens(stem_ctx* c, const char* who, std::initializer_list<float*> sums, int accumulate, void* stream) {
+  const size_t sum = (size_t)c->desc.d_model * 4;
+  for (float* p : sums) {
+    STEM_TRY(check_buffers(c, who, {}, {{p, sum}}, false));
+    if (p && !accumulate) HIP_TRY(c, stem_fill_zero(p, sum, static_cast<hipStream_t>(stream)));
+  }
+  return STEM_OK;
+}
+
 size_t gate_bytes(const stem_ctx* c, int kind, int64_t T, size_t es) {
   const size_t d = c->desc.d_model;
   return kind == STEM_GATE_CHANNEL ? d * es : kind == STEM_GATE_TOKEN ? T * es : kind == STEM_GATE_FULL ? T * d * es : 0;
@@ -163,7 +173,7 @@ stem_status stem_block_enter_backward(stem_ctx* c, const void* dn, const void* x
                                       float* dw, int accumulate, void* stream) {
   static const char who[] = "stem_block_enter_backward";
   STEM_TRY(stem_enter(c, T));
-  if (T == 0) return STEM_OK;
+  if (T == 0) return no_tokens(c, who, {dw}, accumulate, stream);
   if (!dn || !x || !norm || !dx) return stem_fail(c, STEM_ERR_INVALID_ARG, "%s: null pointer argument", who);
   STEM_TRY(check_width(c, who));
   STEM_TRY(check_norm(c, who, *norm));
@@ -202,7 +212,8 @@ stem_status stem_block_leave_backward(stem_ctx* c, const void* dy, const void* d
                                       void* dx, void* df, void* dgate, float* dw_out, float* dw_next, int accumulate, void* stream) {
   static const char who[] = "stem_block_leave_backward";
   STEM_TRY(stem_enter(c, T));
-  if (T == 0) return STEM_OK;
+  if (T == 0)
+    return no_tokens(c, who, {dw_out, dw_next, L && L->gate_kind == STEM_GATE_CHANNEL ? static_cast<float*>(dgate) : nullptr}, accumulate, stream);
   if (!L || (!dy && !dn)) return stem_fail(c, STEM_ERR_INVALID_ARG, "%s: null pointer argument", who);
   STEM_TRY(check_width(c, who));
   BlockArgs a = block_args(c, T);
