@@ -378,12 +378,12 @@ __global__ __launch_bounds__((Shape<E, LPR, VPT, true>::THREADS)) void block_bac
   auto place = [&](int which, int t, int half) __attribute__((always_inline)) {
     return lds_sum + (IN_LDS ? ((which * VPT + t) * 2 + half) * S::THREADS + threadIdx.x : 0);
   };
-  auto add = [&](int which, int t, const float (&a)[8], const float (&b)[8]) __attribute__((always_inline)) {
+  auto add = [&](int which, int t, auto product) __attribute__((always_inline)) {
     float(&v)[8] = sum[which][t];
     float4 w[2];
     if (IN_LDS) { w[0] = *place(which, t, 0); w[1] = *place(which, t, 1); memcpy(v, w, 32); }
 #pragma unroll
-    for (int q = 0; q < 8; ++q) v[q] = __builtin_fmaf(a[q], b[q], v[q]);
+    for (int q = 0; q < 8; ++q) v[q] = product(q, v[q]);
     if (IN_LDS) { memcpy(w, v, 32); *place(which, t, 0) = w[0]; *place(which, t, 1) = w[1]; }
   };
   if (IN_LDS)
@@ -445,7 +445,7 @@ __global__ __launch_bounds__((Shape<E, LPR, VPT, true>::THREADS)) void block_bac
       if (AGAIN) c.weight(p.next.weight, after);
 #pragma unroll
       for (int t = 0; t < VPT; ++t) {
-        add(NEXT, t, h[t], y[t]);
+        add(NEXT, t, [&](int q, float v) __attribute__((always_inline)) { return __builtin_fmaf(h[t][q], y[t][q], v); });
 #pragma unroll
         for (int q = 0; q < 8; ++q) h[t][q] *= after[t][q];
       }
@@ -471,7 +471,7 @@ __global__ __launch_bounds__((Shape<E, LPR, VPT, true>::THREADS)) void block_bac
       if (!live) r = 0.f;
       scale_by(f, r);
     }
-    const float of_row = by_token ? load1(static_cast<const E*>(p.gate) + (live ? row : p.T - 1)) : 1.f;
+    const float gate_of_row = by_token ? load1(static_cast<const E*>(p.gate) + (live ? row : p.T - 1)) : 1.f, of_row = live ? gate_of_row : 1.f;
     float token_gate = 0.f;
     if (AGAIN) branch_weight(branch, true, true);
 #pragma unroll
@@ -481,31 +481,25 @@ __global__ __launch_bounds__((Shape<E, LPR, VPT, true>::THREADS)) void block_bac
       store_dx(t);
 #pragma unroll
       for (int q = 0; q < 8; ++q) G[t][q] *= of_branch;
-      // (what is dropped counts for nothing, whatever f holds there)
-      float u[8];
-#pragma unroll
-      for (int q = 0; q < 8; ++q) u[q] = f[t][q];
-      if (p.drop.threshold) {
-        const Bits b = philox((uint32_t)(c.col[t] >> 3), (uint32_t)row, offset, p.drop.seed);
-#pragma unroll
-        for (int q = 0; q < 8; ++q) {
-          const bool keep = kept(b, q, p.drop.threshold);
-          G[t][q] = keep ? G[t][q] : 0.f;
-          u[q] = keep ? u[q] : 0.f;
-        }
-      }
+      // What is dropped counts for nothing, whatever h, f, the gate or w_out hold there: each product is cut where it is complete.  (Without
+      // dropout the threshold is 0 and all is kept.)
+      Bits bits = {};
+      if (p.drop.threshold) bits = philox((uint32_t)(c.col[t] >> 3), (uint32_t)row, offset, p.drop.seed);
       if (by_token || by_element) {          // (branch is w_out alone)
 #pragma unroll
         for (int q = 0; q < 8; ++q) {
-          dg[q] = G[t][q] * (u[q] * branch[t][q]);
+          dg[q] = kept(bits, q, p.drop.threshold) ? G[t][q] * (f[t][q] * branch[t][q]) : 0.f;
           token_gate += dg[q];
           G[t][q] *= by_element ? g[q] : of_row;
         }
         if (by_element) c.store(rows(p.dgate), t, dg);
       }
-      add(OUT, t, G[t], u);
+      add(OUT, t, [&](int q, float v) __attribute__((always_inline)) {
+        const float sum = __builtin_fmaf(G[t][q], f[t][q], v);
+        return kept(bits, q, p.drop.threshold) ? sum : v;
+      });
 #pragma unroll
-      for (int q = 0; q < 8; ++q) G[t][q] *= branch[t][q];
+      for (int q = 0; q < 8; ++q) G[t][q] = kept(bits, q, p.drop.threshold) ? G[t][q] * branch[t][q] : 0.f;
     }
     if (by_token && p.dgate) {
       float s[1] = {token_gate};

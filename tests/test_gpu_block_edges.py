@@ -2,6 +2,7 @@
 import pytest
 import torch
 
+from oracle import block_oracle as B
 from paper_2601_10639_amd import stemlib as L
 
 pytestmark = pytest.mark.gpu
@@ -39,3 +40,54 @@ def test_sums_over_no_tokens_are_zero(dtype):
     # a gate's gradient for each token or element has no element; sums that are not asked for
     for kind, gate in ((L.STEM_GATE_TOKEN, none[:, 0].contiguous()), (L.STEM_GATE_FULL, none)):
         L.stem_block_leave_backward(ctx, none, none, none, none, L.stem_leave(next=norm, gate_kind=kind, gate=gate), None, None, gate)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("where,out", [("full", "none"), ("full", "rms"), ("channel", "none"), ("channel", "layer"), ("token", "none"), ("w_out", "rms")])
+def test_what_is_dropped_counts_for_nothing(dtype, where, out):
+    """An infinity or a NaN in the gate or the norm's weight reaches nothing where the element that it multiplies is dropped."""
+    T, d, p, seed, offset = 40, 192, 0.3, 5, 6
+    ctx = make_ctx(dtype, T, d)
+    dropped = torch.from_numpy(B.drop_factor(T, d, p, seed, offset) == 0).to(DEV)
+    f, x, dy = draw(dtype, 1, T, d), draw(dtype, 2, T, d), draw(dtype, 3, T, d)
+    kind = {"none": L.STEM_NORM_NONE, "rms": L.STEM_NORM_RMS, "layer": L.STEM_NORM_LAYER}[out]
+    gate_kind, shape = {"full": (L.STEM_GATE_FULL, (T, d)), "channel": (L.STEM_GATE_CHANNEL, (d,)), "token": (L.STEM_GATE_TOKEN, (T,)),
+                        "w_out": (L.STEM_GATE_TOKEN, (T,))}[where]
+    w, g = draw(dtype, 4, d), draw(dtype, 5, *shape)
+    wild, wild_f = (w if where == "w_out" else g).clone(), f.clone()
+    if where == "full":
+        wild[dropped] = float("inf")
+        wild[0][dropped[0]] = float("nan")
+        same = torch.ones_like(dropped)
+    elif where == "token":
+        wild[::2] = float("inf")
+        same = dropped.clone()
+        same[1::2] = True
+    else:
+        wild[7], wild[100] = float("inf"), float("nan")
+        same = (dropped[:, [7, 100]].all(1, keepdim=True)).expand(T, d).clone()   # rows that neither reaches
+        assert same[:, 0].sum() > 0
+    if out == "none":
+        wild_f[dropped] = float("nan")
+
+    def run(f, w, g):
+        norm = L.stem_norm(kind, 1e-5, w if out != "none" else None)
+        leave = L.stem_leave(out=norm, gate_kind=gate_kind, gate=g, p=p, seed=seed, offset=offset)
+        y, dx, df = torch.empty_like(x), torch.empty_like(x), torch.empty_like(x)
+        dg, dw = torch.empty_like(g, dtype=torch.float32 if where == "channel" else g.dtype), torch.empty(d, device=DEV)
+        L.stem_block_leave_forward(ctx, f, x, leave, y)
+        L.stem_block_leave_backward(ctx, dy, None, f, None, leave, dx, df, dg, dw)
+        return y, dx, df, dg, dw
+
+    clean = run(f, w, g)
+    got = run(wild_f, wild if where == "w_out" else w, g if where == "w_out" else wild)
+    for a, b in zip(clean[:3], got[:3]):
+        assert torch.equal(a[same], b[same])
+    assert (got[2][dropped & same] == 0).all() or out != "none"
+    if where == "full":
+        assert torch.equal(clean[3], got[3]) and (got[3][dropped] == 0).all() and torch.equal(clean[4], got[4])
+    elif where == "w_out":
+        rows = same[:, 0]
+        assert torch.equal(clean[3][rows], got[3][rows])
+    else:
+        assert torch.equal(clean[3], got[3])      # (a gate's own gradient does not hold the gate)
