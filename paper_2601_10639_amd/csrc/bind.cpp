@@ -18,7 +18,7 @@
 namespace {
 
 PyObject *g_ctx_type, *g_get_device, *g_raw_stream, *g_handle, *g_value, *g_dtype, *g_cuda_stream;   // set by setup()
-PyObject *g_norm_type, *g_leave_type, *g_quant_type, *g_facts, *g_d_model, *g_d_ff, *g_q, *g_scale, *g_N, *g_K;
+PyObject *g_norm_type, *g_leave_type, *g_quant_type, *g_tensor, *g_norms, *g_gate_tensor, *g_step_tensor, *g_d_model, *g_d_ff, *g_q, *g_scale, *g_N, *g_K;
 bool g_off = true;                                        // before setup(), and in a forked process
 
 struct Unusual {};
@@ -77,29 +77,32 @@ struct Args {
   }
 
   int64_t attribute(PyObject* o, PyObject* name) const { return as_integer(Hold(PyObject_GetAttr(o, name)).o); }
-  // what a structure's tensors were when it was made
-  template <int N>
-  void facts(PyObject* o, int64_t (&f)[N]) const {
-    const Hold t(PyObject_GetAttr(o, g_facts));
-    if (!PyTuple_CheckExact(t.o) || PyTuple_GET_SIZE(t.o) != N) throw Unusual();
-    for (int k = 0; k < N; ++k) f[k] = as_integer(PyTuple_GET_ITEM(t.o, k));
+  // The structures with the pointers that their tensors have now
+  struct Norm {
+    stem_norm norm;
+    bool given;
+    const stem_norm* get() const { return given ? &norm : nullptr; }
+  };
+  const void* weight(PyObject* norm, const void* as_is, int64_t width) const {
+    const Hold t(PyObject_GetAttr(norm, g_tensor));
+    return t.o == Py_None ? as_is : pointer_of(t.o, ACT, width, -1);
   }
   // a norm of rows of `width` (None: none)
-  const stem_norm* norm(int i, int64_t width) const {
-    if (v[i] == Py_None) return nullptr;
-    const stem_norm* const n = structure<stem_norm>(v[i], g_norm_type);
-    int64_t f[2];              // elements of the weight (-1: none) and its type
-    facts(v[i], f);
-    if (f[0] >= 0 && (f[0] != width || f[1] != dtype)) throw Unusual();
+  Norm norm(int i, int64_t width) const {
+    if (v[i] == Py_None) return {{}, false};
+    Norm n = {*structure<stem_norm>(v[i], g_norm_type), true};
+    n.norm.weight = weight(v[i], n.norm.weight, width);
     return n;
   }
-  const stem_leave* leave(int i, int64_t T, int64_t d) const {
-    const stem_leave* const L = structure<stem_leave>(v[i], g_leave_type);
-    int64_t f[5];              // elements of w_out and w_next, the gate's sides, the type of all that is there
-    facts(v[i], f);
-    const int64_t g0 = L->gate_kind == STEM_GATE_CHANNEL ? d : T, g1 = L->gate_kind == STEM_GATE_FULL ? d : -1;
-    if ((f[0] >= 0 && f[0] != d) || (f[1] >= 0 && f[1] != d) || (f[2] >= 0 && (f[2] != g0 || f[3] != g1)) || (f[4] != -1 && f[4] != dtype))
-      throw Unusual();
+  stem_leave leave(int i, int64_t T, int64_t d) const {
+    stem_leave L = *structure<stem_leave>(v[i], g_leave_type);
+    const Hold norms(PyObject_GetAttr(v[i], g_norms)), gate(PyObject_GetAttr(v[i], g_gate_tensor)), step(PyObject_GetAttr(v[i], g_step_tensor));
+    if (!PyTuple_CheckExact(norms.o) || PyTuple_GET_SIZE(norms.o) != 2) throw Unusual();
+    L.out.weight = weight(PyTuple_GET_ITEM(norms.o, 0), L.out.weight, d);
+    L.next.weight = weight(PyTuple_GET_ITEM(norms.o, 1), L.next.weight, d);
+    if (gate.o != Py_None)
+      L.gate = pointer_of(gate.o, ACT, L.gate_kind == STEM_GATE_CHANNEL ? d : T, L.gate_kind == STEM_GATE_FULL ? d : -1);
+    if (step.o != Py_None && L.drop.step) L.drop.step = static_cast<const uint64_t*>(pointer_of(step.o, I64, -1, -1));
     return L;
   }
   // weights in 8 bits
@@ -259,7 +262,7 @@ PyObject* block_enter_forward(PyObject*, PyObject* const* args, Py_ssize_t n) {
   return enter(args, n, 4, [](const Args& a, stem_ctx* c) {
     const int64_t T = a.rows(-1, 0), d = a.d_model();
     auto x = a.shaped(0, ACT, T, d); auto norm = a.norm(1, d); auto to = a.shaped(2, ACT, T, d); auto s = a.stream(3);
-    return [=] { return stem_block_enter_forward(c, x, T, norm, to, s); };
+    return [=] { return stem_block_enter_forward(c, x, T, norm.get(), to, s); };
   });
 }
 
@@ -268,7 +271,7 @@ PyObject* block_enter_backward(PyObject*, PyObject* const* args, Py_ssize_t n) {
     const int64_t T = a.rows(-1, 1), d = a.d_model();
     auto dn = a.shaped(0, ACT, T, d); auto x = a.shaped(1, ACT, T, d); auto norm = a.norm(2, d); auto dx = a.shaped(3, ACT, T, d);
     auto dw = a.shaped<float>(4, F32, d); auto dres = a.shaped(5, ACT, T, d); const int accumulate = a.flag(6); auto s = a.stream(7);
-    return [=] { return stem_block_enter_backward(c, dn, x, T, norm, dres, dx, dw, accumulate, s); };
+    return [=] { return stem_block_enter_backward(c, dn, x, T, norm.get(), dres, dx, dw, accumulate, s); };
   });
 }
 
@@ -277,7 +280,7 @@ PyObject* block_leave_forward(PyObject*, PyObject* const* args, Py_ssize_t n) {
     const int64_t T = a.rows(-1, 1), d = a.d_model();
     auto f = a.shaped(0, ACT, T, d); auto x = a.shaped(1, ACT, T, d); auto L = a.leave(2, T, d); auto y = a.shaped(3, ACT, T, d);
     auto to = a.shaped(4, ACT, T, d); auto s = a.stream(5);
-    return [=] { return stem_block_leave_forward(c, f, x, T, L, y, to, s); };
+    return [=] { return stem_block_leave_forward(c, f, x, T, &L, y, to, s); };
   });
 }
 
@@ -286,9 +289,9 @@ PyObject* block_leave_backward(PyObject*, PyObject* const* args, Py_ssize_t n) {
     const int64_t T = a.rows(-1, a.v[0] == Py_None ? 1 : 0), d = a.d_model();
     auto dy = a.shaped(0, ACT, T, d); auto dn = a.shaped(1, ACT, T, d); auto f = a.shaped(2, ACT, T, d); auto y = a.shaped(3, ACT, T, d);
     auto L = a.leave(4, T, d); auto dx = a.shaped(5, ACT, T, d); auto df = a.shaped(6, ACT, T, d);
-    auto dg = L->gate_kind == STEM_GATE_CHANNEL ? a.shaped(7, F32, d) : L->gate_kind == STEM_GATE_TOKEN ? a.shaped(7, ACT, T) : a.shaped(7, ACT, T, d);
+    auto dg = L.gate_kind == STEM_GATE_CHANNEL ? a.shaped(7, F32, d) : L.gate_kind == STEM_GATE_TOKEN ? a.shaped(7, ACT, T) : a.shaped(7, ACT, T, d);
     auto dwo = a.shaped<float>(8, F32, d); auto dwn = a.shaped<float>(9, F32, d); const int accumulate = a.flag(10); auto s = a.stream(11);
-    return [=] { return stem_block_leave_backward(c, dy, dn, f, y, T, L, dx, df, dg, dwo, dwn, accumulate, s); };
+    return [=] { return stem_block_leave_backward(c, dy, dn, f, y, T, &L, dx, df, dg, dwo, dwn, accumulate, s); };
   });
 }
 
@@ -312,7 +315,7 @@ PyObject* quant_linear(PyObject*, PyObject* const* args, Py_ssize_t n) {
     const Args::Quant w = a.quant(1);
     auto x = a.shaped(0, ACT, T, w.K); auto y = a.shaped(2, ACT, T, w.N); auto r = a.shaped(3, ACT, T, w.N); auto norm = a.norm(4, w.K);
     auto s = a.stream(5);
-    return [=] { return stem_quant_linear(c, x, T, w.K, norm, w.q, w.scale, w.N, r, y, s); };
+    return [=] { return stem_quant_linear(c, x, T, w.K, norm.get(), w.q, w.scale, w.N, r, y, s); };
   });
 }
 
@@ -323,7 +326,7 @@ PyObject* quant_ffn_forward(PyObject*, PyObject* const* args, Py_ssize_t n) {
     if (g.N != F || g.K != d || w.N != d || w.K != F) throw Unusual();
     auto x = a.shaped(0, ACT, T, d); auto ids = a.shaped<int32_t>(1, I32, T); auto E = a.shaped(4, ACT, rows, F); auto y = a.shaped(5, ACT, T, d);
     auto r = a.shaped(6, ACT, T, d); auto norm = a.norm(7, d); auto s = a.stream(8);
-    return [=] { return stem_quant_ffn_forward(c, x, ids, T, norm, g.q, g.scale, w.q, w.scale, E, E_rows, r, y, s); };
+    return [=] { return stem_quant_ffn_forward(c, x, ids, T, norm.get(), g.q, g.scale, w.q, w.scale, E, E_rows, r, y, s); };
   });
 }
 
@@ -331,14 +334,17 @@ PyObject* quant_ffn_forward(PyObject*, PyObject* const* args, Py_ssize_t n) {
 PyObject* setup(PyObject*, PyObject* args) {
   if (!PyArg_ParseTuple(args, "OOOOOO", &g_ctx_type, &g_get_device, &g_raw_stream, &g_norm_type, &g_leave_type, &g_quant_type)) return nullptr;
   for (PyObject* o : {g_ctx_type, g_get_device, g_raw_stream, g_norm_type, g_leave_type, g_quant_type}) Py_INCREF(o);
-  g_facts = PyUnicode_InternFromString("facts");
+  g_tensor = PyUnicode_InternFromString("tensor");
+  g_norms = PyUnicode_InternFromString("norms");
+  g_gate_tensor = PyUnicode_InternFromString("gate_tensor");
+  g_step_tensor = PyUnicode_InternFromString("step_tensor");
   g_d_model = PyUnicode_InternFromString("d_model");
   g_d_ff = PyUnicode_InternFromString("d_ff");
   g_q = PyUnicode_InternFromString("q");
   g_scale = PyUnicode_InternFromString("scale");
   g_N = PyUnicode_InternFromString("N");
   g_K = PyUnicode_InternFromString("K");
-  if (!g_facts || !g_d_model || !g_d_ff || !g_q || !g_scale || !g_N || !g_K) return nullptr;
+  if (!g_tensor || !g_norms || !g_gate_tensor || !g_step_tensor || !g_d_model || !g_d_ff || !g_q || !g_scale || !g_N || !g_K) return nullptr;
   g_handle = PyUnicode_InternFromString("handle");
   g_value = PyUnicode_InternFromString("value");
   g_dtype = PyUnicode_InternFromString("dtype");

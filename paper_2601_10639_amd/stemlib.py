@@ -49,30 +49,27 @@ STEM_NORM_NONE, STEM_NORM_RMS, STEM_NORM_LAYER = range(3)
 STEM_GATE_NONE, STEM_GATE_CHANNEL, STEM_GATE_TOKEN, STEM_GATE_FULL = range(4)
 
 
-def _code(t) -> int:
-    return {torch.float32: STEM_F32, torch.bfloat16: STEM_BF16}.get(t.dtype, -2)
-
-
+# A structure's tensors are kept alive with it, and where their memory is is asked when a call is made: a tensor may get other memory in between.
 class stem_norm(ctypes.Structure):
     """A norm and its weight, a device tensor [d] or None.  Made once and passed to every call."""
 
     _fields_ = [("kind", ctypes.c_int32), ("eps", ctypes.c_float), ("weight", ctypes.c_void_p)]
+    tensor = None
 
     def __init__(self, kind: int = STEM_NORM_NONE, eps: float = 1e-6, weight=None):
         super().__init__(kind, eps, _ptr(weight, name="weight"))
-        self.tensor = weight   # kept alive
-        # for the native binding: elements of the weight and its type (0 elements: not of one side, which no call takes)
-        self.facts = (-1, -1) if weight is None else (weight.numel() if weight.dim() == 1 else 0, _code(weight))
+        self.tensor = weight
 
     def _check(self, ctx, width: int, name: str):
         if self.tensor is not None:
-            _shaped(self.tensor, ctx.torch_dtype, (width,), name + ".weight")
+            self.weight = _shaped(self.tensor, ctx.torch_dtype, (width,), name + ".weight")
 
 
 class stem_drop(ctypes.Structure):
     """step: a device int64 tensor of one element that is added to offset when the kernel runs, or None."""
 
     _fields_ = [("p", ctypes.c_float), ("seed", ctypes.c_uint64), ("offset", ctypes.c_uint64), ("step", ctypes.c_void_p)]
+    step_tensor = None
 
     def __init__(self, p: float = 0.0, seed: int = 0, offset: int = 0, step=None):
         super().__init__(p, seed, offset, _ptr(step, torch.int64, name="step"))
@@ -80,7 +77,8 @@ class stem_drop(ctypes.Structure):
 
 
 class stem_leave(ctypes.Structure):
-    """What the end of a block consists of (include/stem.h).  Made once and passed to every call; `drop` may be changed in between."""
+    """What the end of a block consists of (include/stem.h).  Made once and passed to every call; `drop`, `out` and `next` may be given anew in between,
+    and so may the numbers in them."""
 
     _fields_ = [("out", stem_norm), ("next", stem_norm), ("residual_scale", ctypes.c_float), ("branch_scale", ctypes.c_float),
                 ("gate_kind", ctypes.c_int32), ("gate", ctypes.c_void_p), ("drop", stem_drop)]
@@ -89,20 +87,27 @@ class stem_leave(ctypes.Structure):
                  p: float = 0.0, seed: int = 0, offset: int = 0, step=None):
         self.norms = (out or stem_norm(), next or stem_norm())
         super().__init__(*self.norms, residual_scale, branch_scale, gate_kind, _ptr(gate, name="gate"), stem_drop(p, seed, offset, step))
-        self.gate_tensor, self.step_tensor = gate, step
-        # for the native binding: elements of both weights, the gate's sides, and the type of all of them (-1: none is there, -2: several)
-        codes = {_code(t) for t in (self.norms[0].tensor, self.norms[1].tensor, gate) if t is not None}
-        sides = (-1, -1) if gate is None else (*gate.shape, -1)[:2] if 0 < gate.dim() < 3 else (0, 0)
-        self.facts = (self.norms[0].facts[0], self.norms[1].facts[0], *sides, -1 if not codes else codes.pop() if len(codes) == 1 else -2)
+        self.gate_tensor = gate
+
+    def __setattr__(self, name, value):
+        super().__setattr__(name, value)
+        if name == "drop":
+            self.step_tensor = value.step_tensor
+        elif name == "out":
+            self.norms = (value, self.norms[1])
+        elif name == "next":
+            self.norms = (self.norms[0], value)
 
     def _check(self, ctx, T: int):
         d = ctx.d_model
-        self.norms[0]._check(ctx, d, "out")
-        self.norms[1]._check(ctx, d, "next")
+        for norm, mine, name in ((self.norms[0], self.out, "out"), (self.norms[1], self.next, "next")):
+            if norm.tensor is not None:
+                mine.weight = _shaped(norm.tensor, ctx.torch_dtype, (d,), name + ".weight")
         if self.gate_tensor is not None:
-            shape = {STEM_GATE_CHANNEL: (d,), STEM_GATE_TOKEN: (T,), STEM_GATE_FULL: (T, d)}.get(self.gate_kind)
-            if shape:
-                _shaped(self.gate_tensor, ctx.torch_dtype, shape, "gate")
+            shape = {STEM_GATE_CHANNEL: (d,), STEM_GATE_TOKEN: (T,), STEM_GATE_FULL: (T, d)}.get(self.gate_kind, self.gate_tensor.shape)
+            self.gate = _shaped(self.gate_tensor, ctx.torch_dtype, shape, "gate")
+        if self.step_tensor is not None and self.drop.step:
+            self.drop.step = _ptr(self.step_tensor, torch.int64, name="step")
 
 
 class StemError(RuntimeError):

@@ -91,3 +91,48 @@ def test_what_is_dropped_counts_for_nothing(dtype, where, out):
         assert torch.equal(clean[3][rows], got[3][rows])
     else:
         assert torch.equal(clean[3], got[3])      # (a gate's own gradient does not hold the gate)
+
+
+@pytest.mark.parametrize("way", ["native", "python"])
+def test_tensors_that_get_other_memory(way, monkeypatch):
+    """A norm, a gate and a step are read where their tensors are when a call is made."""
+    if way == "python":
+        monkeypatch.setattr(L, "_bind", L._NoBind())
+    T, d = 5, 128
+    ctx = make_ctx("bf16", T, d)
+    f, x = draw("bf16", 1, T, d), draw("bf16", 2, T, d)
+    w_out, w_next, gate, step = draw("bf16", 3, d), draw("bf16", 4, d), draw("bf16", 5, d), torch.zeros(1, dtype=torch.int64, device=DEV)
+    held = [t.data for t in (w_out, w_next, gate, step)]      # (the memory of before stays allocated)
+
+    def parts():
+        norm = L.stem_norm(L.STEM_NORM_RMS, 1e-5, w_next)
+        return norm, L.stem_leave(out=L.stem_norm(L.STEM_NORM_RMS, 1e-5, w_out), next=norm, gate_kind=L.STEM_GATE_CHANNEL, gate=gate, p=0.5, seed=1, step=step)
+
+    def run(norm, leave):
+        m, y, n, dx, df = (torch.empty_like(x) for _ in range(5))
+        sums = [torch.empty(d, device=DEV) for _ in range(3)]
+        L.stem_block_enter_forward(ctx, x, norm, m)
+        L.stem_block_leave_forward(ctx, f, x, leave, y, n)
+        L.stem_block_leave_backward(ctx, x, f, f, y, leave, dx, df, *sums)
+        return [m, y, n, dx, df, *sums]
+
+    early = parts()
+    before = run(*early)
+    w_out.data, w_next.data, gate.data = draw("bf16", 13, d), draw("bf16", 14, d), draw("bf16", 15, d)
+    step.data = torch.full((1,), 3, dtype=torch.int64, device=DEV)
+    after, want = run(*early), run(*parts())
+    assert all(torch.equal(a, b) for a, b in zip(after, want))
+    assert not any(torch.equal(a, b) for a, b in zip(before, want))
+    # other norms and another dropout in a structure's places
+    norm, leave = parts()
+    leave.drop = L.stem_drop(0.25, 7, 8, step=step)
+    leave.out = L.stem_norm(L.STEM_NORM_LAYER, 1e-5, held[0])
+    leave.next = L.stem_norm(L.STEM_NORM_LAYER, 1e-5, held[1])
+    want = L.stem_leave(out=L.stem_norm(L.STEM_NORM_LAYER, 1e-5, held[0]), next=L.stem_norm(L.STEM_NORM_LAYER, 1e-5, held[1]),
+                        gate_kind=L.STEM_GATE_CHANNEL, gate=gate, p=0.25, seed=7, offset=8 + 3)
+    assert all(torch.equal(a, b) for a, b in zip(run(norm, leave), run(norm, want)))
+    # a weight that is not of one row any more
+    w_out.data = draw("bf16", 3, d + 1)
+    with pytest.raises(ValueError):
+        run(*early)
+    assert len(held) == 4
