@@ -162,7 +162,8 @@ stem_status stem_block_enter_forward(stem_ctx* c, const void* x, int64_t T, cons
   STEM_TRY(check_norm(c, who, *norm));
   if (norm->kind == STEM_NORM_NONE) return stem_fail(c, STEM_ERR_INVALID_ARG, "%s: no norm", who);
   const size_t es = type_bytes(c), row = c->desc.d_model * es;
-  STEM_TRY(check_buffers(c, who, {{x, T * row}, {norm->weight, row}}, {{n, T * row}}, true));
+  STEM_TRY(check_buffers(c, who, {{x, T * row}}, {{n, T * row}}, true));
+  STEM_TRY(check_buffers(c, who, {{norm->weight, row}}, {{n, T * row}}, false));
   BlockArgs a = block_args(c, T);
   a.x = x; a.n = n; a.next = *norm;
   HIP_TRY(c, stem_block_forward_launch(c, c->desc.dtype == STEM_BF16, false, a, static_cast<hipStream_t>(stream)));
@@ -179,8 +180,9 @@ stem_status stem_block_enter_backward(stem_ctx* c, const void* dn, const void* x
   STEM_TRY(check_norm(c, who, *norm));
   if (norm->kind == STEM_NORM_NONE) return stem_fail(c, STEM_ERR_INVALID_ARG, "%s: no norm", who);
   const size_t es = type_bytes(c), row = c->desc.d_model * es, sum = c->desc.d_model * 4;
-  STEM_TRY(check_buffers(c, who, {{dn, T * row}, {x, T * row}, {dres, T * row}, {norm->weight, row}}, {{dx, T * row}}, true));
-  STEM_TRY(check_buffers(c, who, {{dn, T * row}, {x, T * row}, {dres, T * row}, {norm->weight, row}}, {{dx, 0}, {dw, sum}}, false));
+  STEM_TRY(check_buffers(c, who, {{dn, T * row}, {x, T * row}, {dres, T * row}}, {{dx, T * row}}, true));
+  STEM_TRY(check_buffers(c, who, {{dn, T * row}, {x, T * row}, {dres, T * row}}, {{dw, sum}}, false));
+  STEM_TRY(check_buffers(c, who, {{norm->weight, row}}, {{dx, T * row}, {dw, sum}}, false));
   BlockArgs a = block_args(c, T);
   a.dy = dres; a.dn = dn; a.x = x; a.dx = dx; a.next = *norm;
   a.part_of[0] = dw; a.accumulate = accumulate;

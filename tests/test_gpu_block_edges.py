@@ -136,3 +136,39 @@ def test_tensors_that_get_other_memory(way, monkeypatch):
     with pytest.raises(ValueError):
         run(*early)
     assert len(held) == 4
+
+
+def refused(call, *a, **k):
+    with pytest.raises(L.StemError) as e:
+        call(*a, **k)
+    assert e.value.status == L.STEM_ERR_INVALID_ARG
+
+
+@pytest.mark.parametrize("at", [0, 16, 1024, 8192 - 256, 8192 - 16])
+def test_a_sum_over_another_output_is_refused(at):
+    T, d = 64, 64
+    ctx = make_ctx("bf16", T, d)
+    x, dn, w = draw("bf16", 1, T, d), draw("bf16", 2, T, d), draw("bf16", 3, d)
+    memory = torch.zeros(T * d * 2 + 256, dtype=torch.uint8, device=DEV)
+    dx, dw = memory[:T * d * 2].view(torch.bfloat16).view(T, d), memory[at:at + 4 * d].view(torch.float32)
+    norm = L.stem_norm(L.STEM_NORM_RMS, 1e-5, w)
+    refused(L.stem_block_enter_backward, ctx, dn, x, norm, dx, dw)
+    leave = L.stem_leave(out=norm, next=norm, gate_kind=L.STEM_GATE_CHANNEL, gate=w)
+    for k in range(3):
+        sums = [None] * 3
+        sums[k] = dw
+        refused(L.stem_block_leave_backward, ctx, x, dn, x, x, leave, dx, None, *sums)
+        refused(L.stem_block_leave_backward, ctx, x, dn, x, x, leave, None, dx, *sums)
+    torch.cuda.synchronize()
+    assert (memory == 0).all()
+
+
+def test_an_output_over_a_weight_is_refused():
+    d = 64
+    ctx = make_ctx("bf16", 1, d)
+    x, w = draw("bf16", 1, 1, d), draw("bf16", 2, d)
+    norm, over = L.stem_norm(L.STEM_NORM_RMS, 1e-5, w), w.view(1, d)
+    refused(L.stem_block_enter_forward, ctx, x, norm, over)
+    refused(L.stem_block_enter_backward, ctx, x, x, norm, over)
+    refused(L.stem_block_leave_forward, ctx, x, x, L.stem_leave(out=norm), over)
+    refused(L.stem_block_leave_backward, ctx, x, None, x, None, L.stem_leave(out=norm), over, None)
