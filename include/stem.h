@@ -250,7 +250,7 @@ typedef struct {
  * Element c of row r has 16 bits of the generator's output for the counter (c / 8, r, low and high word of o) and the key (low and high word
  * of seed), o = offset + *step: bits 16 (c % 2) .. of word (c % 8) / 2.  It is dropped, that is 0 whatever it was, where they are below
  * threshold = rint(65536 p), and is multiplied by 65536 / (65536 - threshold) otherwise.  p in [0, 1]; 0: nothing is dropped.
- * step (device, may be NULL) is read when the kernel runs: a captured graph draws another mask on every replay when it counts on. */
+ * step (device, may be NULL, under no output) is read when the kernel runs: a captured graph draws another mask on every replay when it counts on. */
 typedef struct {
   float p;
   uint64_t seed, offset;

@@ -53,9 +53,12 @@ stem_status check_norm(stem_ctx* c, const char* who, const stem_norm& n) {
   return STEM_OK;
 }
 
-stem_status check_drop(stem_ctx* c, const char* who, const stem_drop& d, DropArgs* out) {
+// (every workgroup reads the step, also when others have stored their part of an output)
+stem_status check_drop(stem_ctx* c, const char* who, const stem_drop& d, std::initializer_list<Buffer> outputs, DropArgs* out) {
   if (!(d.p >= 0.f && d.p <= 1.f)) return stem_fail(c, STEM_ERR_INVALID_ARG, "%s: p = %g is not in [0, 1]", who, (double)d.p);
   if (reinterpret_cast<uintptr_t>(d.step) & 7u) return stem_fail(c, STEM_ERR_INVALID_ARG, "%s: step must be 8-byte aligned", who);
+  for (const Buffer& o : outputs)
+    if (overlap(o, {d.step, sizeof *d.step})) return stem_fail(c, STEM_ERR_INVALID_ARG, "%s: an output lies over step", who);
   out->threshold = (uint32_t)lrint((double)d.p * 65536.0);
   out->scale = out->threshold < 65536 ? (float)(65536.0 / (65536 - out->threshold)) : 0.f;
   out->seed = d.seed; out->offset = d.offset; out->step = d.step;
@@ -80,10 +83,10 @@ BlockArgs block_args(const stem_ctx* c, int64_t T) {
   return a;
 }
 
-stem_status check_leave(stem_ctx* c, const char* who, const stem_leave& L, BlockArgs* a) {
+stem_status check_leave(stem_ctx* c, const char* who, const stem_leave& L, std::initializer_list<Buffer> outputs, BlockArgs* a) {
   STEM_TRY(check_norm(c, who, L.out));
   STEM_TRY(check_norm(c, who, L.next));
-  STEM_TRY(check_drop(c, who, L.drop, &a->drop));
+  STEM_TRY(check_drop(c, who, L.drop, outputs, &a->drop));
   if (L.gate_kind < STEM_GATE_NONE || L.gate_kind > STEM_GATE_FULL)
     return stem_fail(c, STEM_ERR_INVALID_ARG, "%s: %d is not a stem_gate_kind", who, L.gate_kind);
   if ((L.gate_kind != STEM_GATE_NONE) != (L.gate != nullptr))
@@ -197,9 +200,9 @@ stem_status stem_block_leave_forward(stem_ctx* c, const void* f, const void* x, 
   if (!f || !x || !L || !y) return stem_fail(c, STEM_ERR_INVALID_ARG, "%s: null pointer argument", who);
   STEM_TRY(check_width(c, who));
   BlockArgs a = block_args(c, T);
-  STEM_TRY(check_leave(c, who, *L, &a));
-  if ((L->next.kind != STEM_NORM_NONE) != (n != nullptr)) return stem_fail(c, STEM_ERR_INVALID_ARG, "%s: n and the next norm go together", who);
   const size_t es = type_bytes(c), row = c->desc.d_model * es;
+  STEM_TRY(check_leave(c, who, *L, {{y, T * row}, {n, T * row}}, &a));
+  if ((L->next.kind != STEM_NORM_NONE) != (n != nullptr)) return stem_fail(c, STEM_ERR_INVALID_ARG, "%s: n and the next norm go together", who);
   const Buffer gate = {L->gate, gate_bytes(c, L->gate_kind, T, es)};
   // (a gate of another kind than [T,d] is read for every row: no output lies over it, though it may be as long as one)
   STEM_TRY(check_buffers(c, who, {{f, T * row}, {x, T * row}, L->gate_kind == STEM_GATE_FULL ? gate : Buffer{}}, {{y, T * row}, {n, T * row}}, true));
@@ -219,17 +222,17 @@ stem_status stem_block_leave_backward(stem_ctx* c, const void* dy, const void* d
   if (!L || (!dy && !dn)) return stem_fail(c, STEM_ERR_INVALID_ARG, "%s: null pointer argument", who);
   STEM_TRY(check_width(c, who));
   BlockArgs a = block_args(c, T);
-  STEM_TRY(check_leave(c, who, *L, &a));
+  const size_t es = type_bytes(c), row = c->desc.d_model * es, sum = c->desc.d_model * 4;
+  const bool full = L->gate_kind == STEM_GATE_FULL;
+  const size_t gate_size = gate_bytes(c, L->gate_kind, T, es);
+  const Buffer gate = {L->gate, gate_size}, of_gate = {dgate, L->gate_kind == STEM_GATE_CHANNEL ? sum : gate_size};
+  STEM_TRY(check_leave(c, who, *L, {{dx, T * row}, {df, T * row}, of_gate, {dw_out, sum}, {dw_next, sum}}, &a));
   if (dn && L->next.kind == STEM_NORM_NONE) return stem_fail(c, STEM_ERR_INVALID_ARG, "%s: dn without a next norm", who);
   if ((dn && !y) || (dw_next && !dn)) return stem_fail(c, STEM_ERR_INVALID_ARG, "%s: the next norm's gradients need dn and y", who);
   if (dgate && L->gate_kind == STEM_GATE_NONE) return stem_fail(c, STEM_ERR_INVALID_ARG, "%s: dgate without a gate", who);
   // dw_out is asked for: of N_out(f), also where that is f
   const bool need_f = (df && L->out.kind != STEM_NORM_NONE) || dgate || dw_out;
   if (need_f && !f) return stem_fail(c, STEM_ERR_INVALID_ARG, "%s: these gradients need f", who);
-  const size_t es = type_bytes(c), row = c->desc.d_model * es, sum = c->desc.d_model * 4;
-  const bool full = L->gate_kind == STEM_GATE_FULL;
-  const size_t gate_size = gate_bytes(c, L->gate_kind, T, es);
-  const Buffer gate = {L->gate, gate_size}, of_gate = {dgate, L->gate_kind == STEM_GATE_CHANNEL ? sum : gate_size};
   const Buffer in_f = {need_f ? f : nullptr, T * row}, in_y = {dn ? y : nullptr, T * row}, in_dy = {dy, T * row}, in_dn = {dn, T * row};
   STEM_TRY(check_buffers(c, who, {in_dy, in_dn, in_f, in_y, full ? gate : Buffer{}}, {{dx, T * row}, {df, T * row}, full ? of_gate : Buffer{}}, true));
   STEM_TRY(check_buffers(c, who, {{L->out.weight, row}, {L->next.weight, row}, full ? Buffer{} : gate},
@@ -252,8 +255,8 @@ stem_status stem_dropout(stem_ctx* c, const void* x, int64_t T, int64_t width, c
   if (T == 0 || width == 0) return STEM_OK;
   if (!x || !drop || !y) return stem_fail(c, STEM_ERR_INVALID_ARG, "%s: null pointer argument", who);
   DropArgs d;
-  STEM_TRY(check_drop(c, who, *drop, &d));
   const size_t bytes = (size_t)T * width * type_bytes(c);
+  STEM_TRY(check_drop(c, who, *drop, {{y, bytes}}, &d));
   STEM_TRY(check_buffers(c, who, {{x, bytes}}, {{y, bytes}}, true));
   HIP_TRY(c, stem_dropout_launch(c, c->desc.dtype == STEM_BF16, x, T, width, d, y, static_cast<hipStream_t>(stream)));
   return STEM_OK;

@@ -172,3 +172,25 @@ def test_an_output_over_a_weight_is_refused():
     refused(L.stem_block_enter_backward, ctx, x, x, norm, over)
     refused(L.stem_block_leave_forward, ctx, x, x, L.stem_leave(out=norm), over)
     refused(L.stem_block_leave_backward, ctx, x, None, x, None, L.stem_leave(out=norm), over, None)
+
+
+@pytest.mark.parametrize("at", [0, 8, 64])
+def test_an_output_over_the_step_is_refused(at):
+    T, d = 4, 64
+    ctx = make_ctx("bf16", T, d)
+    x, w = draw("bf16", 1, T, d), draw("bf16", 2, d)
+    memory = torch.zeros(T * d * 2, dtype=torch.uint8, device=DEV)
+    y, step = memory.view(torch.bfloat16).view(T, d), memory[at:at + 8].view(torch.int64)
+    norm = L.stem_norm(L.STEM_NORM_RMS, 1e-5, w)
+    leave = L.stem_leave(out=norm, next=norm, gate_kind=L.STEM_GATE_CHANNEL, gate=w, p=0.1, seed=1, step=step)
+    refused(L.stem_dropout, ctx, x, y, 0.1, 1, step=step)
+    refused(L.stem_block_leave_forward, ctx, x, x, leave, y, torch.empty_like(x))
+    refused(L.stem_block_leave_forward, ctx, x, x, leave, torch.empty_like(x), y)
+    refused(L.stem_block_leave_backward, ctx, x, x, x, x, leave, y, None)
+    refused(L.stem_block_leave_backward, ctx, x, x, x, x, leave, None, y)
+    for k in range(3):
+        sums = [None] * 3
+        sums[k] = memory[:4 * d].view(torch.float32)
+        refused(L.stem_block_leave_backward, ctx, x, x, x, x, leave, None, None, *sums)
+    torch.cuda.synchronize()
+    assert (memory == 0).all()
