@@ -639,7 +639,7 @@ def stem_quant_weights(ctx: StemCtx, W, out: StemQuant | None = None, stream=Non
 def _quant(w: StemQuant, N: int, K: int, name: str):
     if (w.N, w.K) != (N, K):
         raise ValueError(f"{name}: expected weights of shape {(N, K)}, got {(w.N, w.K)}")
-    return _ptr(w.q, torch.int8, name=name + ".q"), _ptr(w.scale, torch.float32, name=name + ".scale")
+    return _shaped(w.q, torch.int8, (lib().stem_quant_bytes(N, K),), name + ".q"), _shaped(w.scale, torch.float32, (N,), name + ".scale")
 
 
 def stem_quant_linear(ctx: StemCtx, x, W: StemQuant, y, residual=None, norm: stem_norm | None = None, stream=None):

@@ -50,3 +50,13 @@ def test_what_is_given_anew_is_kept_alive():
     leave.out.eps = 0.5
     leave._check(Context, 3)
     assert leave.drop.step is None and leave.out.eps == 0.5
+
+
+@pytest.mark.parametrize("short", ["q", "scale"])
+def test_quantised_weights_of_another_size_are_refused(short):
+    N, K = 40, 100
+    q, scale = torch.zeros(L.stem_quant_bytes(N, K), dtype=torch.int8), torch.zeros(N)
+    assert L._quant(L.StemQuant(q, scale, N, K), N, K, "W") == (q.data_ptr(), scale.data_ptr())
+    bad = L.StemQuant(q[:-1], scale, N, K) if short == "q" else L.StemQuant(q, scale[:-1], N, K)
+    with pytest.raises(ValueError):
+        L._quant(bad, N, K, "W")
