@@ -77,6 +77,11 @@ struct Args {
   }
 
   int64_t attribute(PyObject* o, PyObject* name) const { return as_integer(Hold(PyObject_GetAttr(o, name)).o); }
+  // dropout's device counter, of one element
+  const uint64_t* counter(PyObject* o) const {
+    if (o != Py_None && THPVariable_CheckExact(o) && THPVariable_Unpack(o).numel() != 1) throw Unusual();
+    return static_cast<const uint64_t*>(pointer_of(o, I64, -1, -1));
+  }
   // The structures with the pointers that their tensors have now
   struct Norm {
     stem_norm norm;
@@ -102,7 +107,7 @@ struct Args {
     L.next.weight = weight(PyTuple_GET_ITEM(norms.o, 1), L.next.weight, d);
     if (gate.o != Py_None)
       L.gate = pointer_of(gate.o, ACT, L.gate_kind == STEM_GATE_CHANNEL ? d : T, L.gate_kind == STEM_GATE_FULL ? d : -1);
-    if (step.o != Py_None && L.drop.step) L.drop.step = static_cast<const uint64_t*>(pointer_of(step.o, I64, -1, -1));
+    if (step.o != Py_None && L.drop.step) L.drop.step = counter(step.o);
     return L;
   }
   // weights in 8 bits
@@ -303,7 +308,7 @@ PyObject* dropout(PyObject*, PyObject* const* args, Py_ssize_t n) {
     const int64_t T = t.size(0), width = t.size(1), seed = a.integer(3), offset = a.integer(4);
     if (seed < 0 || offset < 0) throw Unusual();
     auto x = a.shaped(0, ACT, T, width); auto y = a.shaped(1, ACT, T, width);
-    const stem_drop drop = {a.number(2), (uint64_t)seed, (uint64_t)offset, a.ptr<const uint64_t>(5, I64)};
+    const stem_drop drop = {a.number(2), (uint64_t)seed, (uint64_t)offset, a.counter(a.v[5])};
     auto s = a.stream(6);
     return [=] { return stem_dropout(c, x, T, width, &drop, y, s); };
   });

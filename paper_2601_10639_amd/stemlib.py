@@ -65,6 +65,13 @@ class stem_norm(ctypes.Structure):
             self.weight = _shaped(self.tensor, ctx.torch_dtype, (width,), name + ".weight")
 
 
+def _step(t):
+    """The pointer of a device counter (None stays None)."""
+    if t is not None and t.numel() != 1:
+        raise ValueError(f"step: expected one element, got {t.numel()}")
+    return _ptr(t, torch.int64, name="step")
+
+
 class stem_drop(ctypes.Structure):
     """step: a device int64 tensor of one element that is added to offset when the kernel runs, or None."""
 
@@ -72,7 +79,7 @@ class stem_drop(ctypes.Structure):
     step_tensor = None
 
     def __init__(self, p: float = 0.0, seed: int = 0, offset: int = 0, step=None):
-        super().__init__(p, seed, offset, _ptr(step, torch.int64, name="step"))
+        super().__init__(p, seed, offset, _step(step))
         self.step_tensor = step
 
 
@@ -107,7 +114,7 @@ class stem_leave(ctypes.Structure):
             shape = {STEM_GATE_CHANNEL: (d,), STEM_GATE_TOKEN: (T,), STEM_GATE_FULL: (T, d)}.get(self.gate_kind, self.gate_tensor.shape)
             self.gate = _shaped(self.gate_tensor, ctx.torch_dtype, shape, "gate")
         if self.step_tensor is not None and self.drop.step:
-            self.drop.step = _ptr(self.step_tensor, torch.int64, name="step")
+            self.drop.step = _step(self.step_tensor)
 
 
 class StemError(RuntimeError):

@@ -60,3 +60,17 @@ def test_quantised_weights_of_another_size_are_refused(short):
     bad = L.StemQuant(q[:-1], scale, N, K) if short == "q" else L.StemQuant(q, scale[:-1], N, K)
     with pytest.raises(ValueError):
         L._quant(bad, N, K, "W")
+
+
+@pytest.mark.parametrize("n", [0, 2])
+def test_a_step_is_one_element(n):
+    step = torch.zeros(n, dtype=torch.int64)
+    with pytest.raises(ValueError):
+        L.stem_drop(0.1, 1, 2, step=step)
+    with pytest.raises(ValueError):
+        L.stem_leave(p=0.1, step=step)
+    one = torch.zeros(1, dtype=torch.int64)
+    leave = L.stem_leave(p=0.1, step=one)
+    one.data = step
+    with pytest.raises(ValueError):
+        leave._check(Context, 3)

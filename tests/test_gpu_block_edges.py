@@ -194,3 +194,18 @@ def test_an_output_over_the_step_is_refused(at):
         refused(L.stem_block_leave_backward, ctx, x, x, x, x, leave, None, None, *sums)
     torch.cuda.synchronize()
     assert (memory == 0).all()
+
+
+@pytest.mark.parametrize("n", [0, 2])
+def test_a_step_of_another_size_is_refused(n):
+    """A counter of no elements has no address, which would be none at all: the same mask in every replay."""
+    T, d = 4, 64
+    ctx = make_ctx("bf16", T, d)
+    x, step = draw("bf16", 1, T, d), torch.zeros(n, dtype=torch.int64, device=DEV)
+    with pytest.raises(ValueError):
+        L.stem_dropout(ctx, x, torch.empty_like(x), 0.1, 1, step=step)
+    one = torch.zeros(1, dtype=torch.int64, device=DEV)
+    leave = L.stem_leave(p=0.1, step=one)
+    one.data = step
+    with pytest.raises(ValueError):
+        L.stem_block_leave_forward(ctx, x, x, leave, torch.empty_like(x))
