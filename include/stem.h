@@ -312,7 +312,7 @@ int64_t stem_quant_bytes(int64_t N, int64_t K);
 /* W [N,K] (bf16) -> q (stem_quant_bytes(N, K) bytes) and scale [N] fp32.  N, K >= 1, K <= 131072; W is only read here. */
 stem_status stem_quant_weights(stem_ctx* ctx, const void* W, int64_t N, int64_t K, void* q, float* scale, void* stream);
 
-/* y = Q(N(x)) Q(W)^T (+ residual): x [T,K], y and residual [T,N] bf16, 1 <= N <= 2^22 and 1 <= K <= max(d_model, d_ff); q, scale: of
+/* y = Q(N(x)) Q(W)^T (+ residual): x [T,K], y and residual [T,N] bf16, 1 <= N <= 2^22 and 1 <= K <= min(max(d_model, d_ff), 131072); q, scale: of
  * stem_quant_weights.  norm (host) may be NULL: none.  residual may be NULL, and may be y; y may lie over x.  8-bit forms of x and of W
  * are below 2^31 bytes.  Needs stem_reserve(ctx, STEM_RESERVE_QUANT). */
 stem_status stem_quant_linear(stem_ctx* ctx, const void* x, int64_t T, int64_t K, const stem_norm* norm, const void* q, const float* scale,
@@ -320,7 +320,7 @@ stem_status stem_quant_linear(stem_ctx* ctx, const void* x, int64_t T, int64_t K
 
 /* The layer on Q of both weight matrices: y = Q(SiLU(Q(N(x)) Q(W_gate)^T) * E[ids]) Q(W_down)^T (+ residual); ids and the bf16 table as in
  * stem_ffn_forward.  The hidden values stay in fp32 until they are quantised: rounded to bf16 first, one in a hundred would become
- * another integer (which moves y by 1 %).  norm and residual may be NULL; y may be x and residual.  Needs stem_reserve(ctx, STEM_RESERVE_QUANT). */
+ * another integer (which moves y by 1 %).  d_model and d_ff are up to 131072.  norm and residual may be NULL; y may be x and residual.  Needs stem_reserve(ctx, STEM_RESERVE_QUANT). */
 stem_status stem_quant_ffn_forward(stem_ctx* ctx, const void* x, const int32_t* ids, int64_t T, const stem_norm* norm, const void* gate_q,
                                    const float* gate_scale, const void* down_q, const float* down_scale, const void* E, int64_t E_rows,
                                    const void* residual, void* y, void* stream);

@@ -22,6 +22,7 @@ namespace {
   } while (0)
 
 constexpr int64_t QUANT_MAX_CHANNELS = 1 << 22;   // 256 rows of an output are addressed with 32 bits
+constexpr int64_t QUANT_MAX_K = 131072;           // up to here a sum of products of two bytes, 127 x 127 at most, fits 32 bits
 
 struct Buffer { const void* p; size_t bytes; };
 
@@ -268,8 +269,9 @@ stem_status stem_quant_weights(stem_ctx* c, const void* W, int64_t N, int64_t K,
   static const char who[] = "stem_quant_weights";
   STEM_TRY(stem_enter(c, 0));
   if (c->desc.dtype != STEM_BF16) return stem_fail(c, STEM_ERR_UNSUPPORTED, "%s: needs a bf16 context", who);
-  if (N < 1 || K < 1 || K > 131072 || stem_quant_size(N, K) > INT32_MAX)
-    return stem_fail(c, STEM_ERR_SHAPE, "%s: a matrix [%lld, %lld]; K is up to 131072 and the 8-bit form below 2^31 bytes", who, (long long)N, (long long)K);
+  if (N < 1 || K < 1 || K > QUANT_MAX_K || stem_quant_size(N, K) > INT32_MAX)
+    return stem_fail(c, STEM_ERR_SHAPE, "%s: a matrix [%lld, %lld]; K is up to %lld and the 8-bit form below 2^31 bytes", who, (long long)N, (long long)K,
+                     (long long)QUANT_MAX_K);
   if (!W || !q || !scale) return stem_fail(c, STEM_ERR_INVALID_ARG, "%s: null pointer argument", who);
   STEM_TRY(check_buffers(c, who, {{W, (size_t)(N * K * 2)}}, {{q, (size_t)stem_quant_size(N, K)}, {scale, (size_t)N * 4}}, false));
   HIP_TRY(c, quant_rows(c, K_QUANT_WEIGHTS, W, N, K, nullptr, true, static_cast<int8_t*>(q), scale, nullptr, 0, static_cast<hipStream_t>(stream)));
@@ -281,9 +283,9 @@ stem_status stem_quant_linear(stem_ctx* c, const void* x, int64_t T, int64_t K, 
   static const char who[] = "stem_quant_linear";
   STEM_TRY(stem_enter(c, T));
   STEM_TRY(check_quant(c, who));
-  const int64_t most = std::max(c->desc.d_model, c->desc.d_ff);
+  const int64_t most = std::min<int64_t>(std::max(c->desc.d_model, c->desc.d_ff), QUANT_MAX_K);
   if (N < 1 || N > QUANT_MAX_CHANNELS || K < 1 || K > most || stem_quant_size(N, K) > INT32_MAX || stem_quant_size(std::max<int64_t>(T, 1), K) > INT32_MAX)
-    return stem_fail(c, STEM_ERR_SHAPE, "%s: a product [%lld, %lld] x [%lld, %lld]^T; K is up to max(d_model, d_ff) = %lld, N up to 2^22 and each "
+    return stem_fail(c, STEM_ERR_SHAPE, "%s: a product [%lld, %lld] x [%lld, %lld]^T; K is up to %lld here, N up to 2^22 and each "
                      "operand's 8-bit form below 2^31 bytes", who, (long long)T, (long long)K, (long long)N, (long long)K, (long long)most);
   if (T == 0) return STEM_OK;
   if (!x || !q || !scale || !y) return stem_fail(c, STEM_ERR_INVALID_ARG, "%s: null pointer argument", who);
@@ -324,6 +326,7 @@ stem_status stem_quant_ffn_forward(stem_ctx* c, const void* x, const int32_t* id
   if (E_rows < 1 || E_rows > INT32_MAX) return stem_fail(c, STEM_ERR_SHAPE, "%s: E_rows = %lld", who, (long long)E_rows);
   if (norm) STEM_TRY(check_norm(c, who, *norm));
   const int64_t d = c->desc.d_model, F = c->desc.d_ff;
+  if (std::max(d, F) > QUANT_MAX_K) return stem_fail(c, STEM_ERR_SHAPE, "%s: d_model or d_ff is over %lld", who, (long long)QUANT_MAX_K);
   for (int64_t bytes : {stem_quant_size(T, d), stem_quant_size(T, F), stem_quant_size(F, d), stem_quant_size(d, F)})
     if (bytes > INT32_MAX) return stem_fail(c, STEM_ERR_SHAPE, "%s: %lld tokens or the weights are %lld bytes in 8 bits, 2^31 or more", who, (long long)T, (long long)bytes);
   const size_t xb = (size_t)(T * d) * 2;
