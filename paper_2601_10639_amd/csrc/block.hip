@@ -589,12 +589,12 @@ __global__ __launch_bounds__(1024) void block_sums_kernel(SumArgs p) {
 // A thread has the eight elements of a counter; `tx` (a power of two) threads lie along a row.  Measured: 65536 x 1024 in bf16 44.5 us, 6.0 TB/s,
 // what a copy reaches; the generator takes about 39 of them beside.  999 x 1001 in fp32, element by element, 5.0.
 template <class E>
-__global__ __launch_bounds__(256) void dropout_kernel(const E* x, E* y, int64_t T, int64_t d, int tx_log, DropArgs drop,
+__global__ __launch_bounds__(256) void dropout_kernel(const E* x, E* y, int64_t T, int64_t d, int64_t row0, int tx_log, DropArgs drop,
                                                       int vectors) {
   const int tx = 1 << tx_log;
   const int64_t columns = (d + 7) / 8;
   const int64_t tiles = (columns + tx - 1) >> tx_log;
-  const int64_t row = (int64_t)(blockIdx.x / tiles) * (256 >> tx_log) + (threadIdx.x >> tx_log);
+  const int64_t row = row0 + (int64_t)(blockIdx.x / tiles) * (256 >> tx_log) + (threadIdx.x >> tx_log);
   const int64_t c = ((int64_t)(blockIdx.x % tiles) << tx_log) + (threadIdx.x & (tx - 1));
   if (row >= T || c >= columns) return;
   const Bits r = philox((uint32_t)c, (uint32_t)row, offset_of(drop), drop.seed);
@@ -674,16 +674,24 @@ hipError_t stem_block_backward_launch(stem_ctx* ctx, int is_bf16, bool branch, c
   return branch ? by_width<float, true, true>(a, s) : by_width<float, false, true>(a, s);
 }
 
+// A launch has fewer than 2^32 threads: longer tensors are done in several, of as many rows each.
+constexpr int64_t DROPOUT_GRID = 1 << 23;
 hipError_t stem_dropout_launch(stem_ctx* ctx, int is_bf16, const void* x, int64_t T, int64_t d, const DropArgs& drop, void* y, hipStream_t s) {
   ProfScope prof(ctx, K_DROPOUT, s);
   const int64_t columns = (d + 7) / 8;
   int tx_log = 0;
   while (tx_log < 8 && ((int64_t)1 << tx_log) < columns) ++tx_log;
-  const int64_t tiles = (columns + (1 << tx_log) - 1) >> tx_log, rows = (T + (256 >> tx_log) - 1) / (256 >> tx_log);
+  const int64_t tiles = (columns + (1 << tx_log) - 1) >> tx_log, rows = 256 >> tx_log;   // workgroups along a row, rows of a workgroup
   const int vectors = d % 8 == 0;
-  if (is_bf16)
-    dropout_kernel<bf16_t><<<(unsigned)(tiles * rows), 256, 0, s>>>(static_cast<const bf16_t*>(x), static_cast<bf16_t*>(y), T, d, tx_log, drop, vectors);
-  else
-    dropout_kernel<float><<<(unsigned)(tiles * rows), 256, 0, s>>>(static_cast<const float*>(x), static_cast<float*>(y), T, d, tx_log, drop, vectors);
-  return hipGetLastError();
+  const int64_t most = DROPOUT_GRID / tiles * rows;   // rows of a launch
+  for (int64_t row0 = 0; row0 < T; row0 += most) {
+    const unsigned grid = (unsigned)(tiles * (((T - row0 < most ? T - row0 : most) + rows - 1) / rows));
+    if (is_bf16)
+      dropout_kernel<bf16_t><<<grid, 256, 0, s>>>(static_cast<const bf16_t*>(x), static_cast<bf16_t*>(y), T, d, row0, tx_log, drop, vectors);
+    else
+      dropout_kernel<float><<<grid, 256, 0, s>>>(static_cast<const float*>(x), static_cast<float*>(y), T, d, row0, tx_log, drop, vectors);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
 }

@@ -1,4 +1,5 @@
 """The block's calls at the edges of their range: no tokens, gates that are no numbers where an element is dropped, tensors that get other memory."""
+import numpy as np
 import pytest
 import torch
 
@@ -209,3 +210,20 @@ def test_a_step_of_another_size_is_refused(n):
     one.data = step
     with pytest.raises(ValueError):
         L.stem_block_leave_forward(ctx, x, x, leave, torch.empty_like(x))
+
+
+def test_dropout_of_more_than_a_launch_holds():
+    """More than 2^32 threads: rows of 2056 take 512 each."""
+    T, d, p, seed, offset = (1 << 23) + 9, 2056, 0.25, 11, 12
+    ctx = make_ctx("bf16", T, 64)
+    x = torch.ones(T, d, dtype=torch.bfloat16, device=DEV)
+    L.stem_dropout(ctx, x, x, p, seed, offset)
+    rows = [0, 1, (1 << 22) - 1, 1 << 22, (1 << 22) + 1, (1 << 23) - 1, 1 << 23, T - 1]
+    c = np.zeros((len(rows), d // 8, 4), np.uint64)
+    c[..., 0], c[..., 1], c[..., 2] = np.arange(d // 8), np.array(rows)[:, None], offset
+    words = B.philox(c, (seed, 0))
+    bits = np.stack([words & np.uint64(0xFFFF), words >> np.uint64(16)], -1).reshape(len(rows), d)
+    want = torch.from_numpy(np.where(bits >= 16384, 4.0 / 3.0, 0.0)).to(torch.bfloat16)
+    assert torch.equal(x[rows].cpu(), want)
+    del x
+    torch.cuda.empty_cache()
