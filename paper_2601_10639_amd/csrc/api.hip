@@ -166,7 +166,7 @@ void release(stem_ctx* c) {
   free(c->slot);
   free(c->cache_id_in_slot); free(c->cache_slot_of); free(c->cache_freq);
   (void)hipFree(c->edit_idx_dev); (void)hipFree(c->edit_rep_dev);
-  (void)hipFree(c->block_part);
+  (void)hipFree(c->block_own);
   if (c->quant_ws != reinterpret_cast<int*>(c->splitk_ws)) (void)hipFree(c->quant_ws);
   (void)hipFree(c->quant_x); (void)hipFree(c->quant_h); (void)hipFree(c->quant_sx); (void)hipFree(c->quant_sh); (void)hipFree(c->quant_amax); (void)hipFree(c->quant_max); (void)hipFree(c->quant_hidden);
   if (c->inst_pinned) (void)hipHostFree(c->inst_pinned);
@@ -219,6 +219,14 @@ extern "C" {
 int64_t stem_route_splitk_bytes(int d_model, int d_ff, int64_t max_tokens) {
   // partial products of up to 8 K slices of a [T,d] or [d,F] output
   return std::min<int64_t>(STEM_SPLITK_WS_MAX, (int64_t)8 * 4 * d_model * std::max<int64_t>({max_tokens, d_ff, 1}));
+}
+
+int stem_route_block_scratch(int d, int F, int dtype, int64_t max_tokens, int64_t* bytes) {
+  // The partial sums of the block's gradients lie in scratch that a context has for the layer, which no call keeps anything in for the
+  // next: in that of the products' K slices (bf16), else in that of the hidden values, else in their own.
+  *bytes = d <= STEM_BLOCK_MAX_WIDTH ? std::min<int64_t>(max_tokens, stem_block_grid(d)) * 3 * d * 4 : 0;
+  if (dtype == STEM_BF16 && stem_route_splitk_bytes(d, F, max_tokens) >= *bytes) return 0;
+  return max_tokens * F * (dtype == STEM_BF16 ? 2 : 4) >= *bytes ? 1 : 2;
 }
 
 void stem_route_forward(int d, int F, int64_t T, int32_t* route) {
@@ -337,8 +345,12 @@ stem_status stem_create(stem_ctx** out, const stem_layer_desc* desc, int64_t max
   ok(dmalloc(&c->sort_counts, (size_t)stem_sort_count_entries(std::max<int64_t>(max_tokens, 1))));
   ok(dmalloc(&c->seg_of, (size_t)max_tokens));
   ok(dmalloc(&c->seg_part, (size_t)stem_seg_chunks(std::max<int64_t>(max_tokens, 1)) * 2 * desc->d_ff));
-  if (desc->d_model <= STEM_BLOCK_MAX_WIDTH)
-    ok(dmalloc(&c->block_part, (size_t)std::min<int64_t>(max_tokens, STEM_BLOCK_GRID) * 3 * desc->d_model));
+  int64_t block_bytes;
+  switch (stem_route_block_scratch(desc->d_model, desc->d_ff, desc->dtype, max_tokens, &block_bytes)) {
+    case 0: c->block_part = c->splitk_ws; break;
+    case 1: c->block_part = static_cast<float*>(c->H_ws); break;
+    default: ok(hipMalloc(reinterpret_cast<void**>(&c->block_own), block_bytes)); c->block_part = c->block_own;
+  }
   ok(dmalloc(&c->uniq_dev, (size_t)max_tokens));
   ok(dmalloc(&c->order_dev, 2 * (size_t)max_tokens));
   ok(hipHostMalloc(reinterpret_cast<void**>(&c->order_pinned), std::max<size_t>(max_tokens, 1) * 8, hipHostMallocDefault));

@@ -3,7 +3,10 @@
 #include "stem_internal.h"
 
 #define STEM_BLOCK_MAX_WIDTH 16384   // a row's values stay in a workgroup's registers
-#define STEM_BLOCK_GRID 512          // workgroups of a launch, and so partial sums of a gradient that is a sum over tokens
+#define STEM_BLOCK_WIDE 4096         // longer rows take workgroups of 1024 lanes in the backward pass, of which a compute unit holds one
+// Workgroups of a launch of the backward pass, and so partial sums of a gradient that is a sum over tokens
+inline int stem_block_grid(int d) { return d > STEM_BLOCK_WIDE ? 256 : 512; }
+#define STEM_BLOCK_GRID 512          // at most
 
 struct DropArgs {
   uint32_t threshold;   // of 65536: dropped below it; 0 = nothing is

@@ -616,7 +616,7 @@ __global__ __launch_bounds__(256) void dropout_kernel(const E* x, E* y, int64_t 
 template <class E, int LPR, int VPT, bool BRANCH, bool BACK>
 hipError_t launch(const BlockArgs& a, hipStream_t s) {
   typedef Shape<E, LPR, VPT, BACK> S;
-  const int64_t groups = (a.T + S::SLOTS - 1) / S::SLOTS, most = BACK ? STEM_BLOCK_GRID / (LPR == 1024 ? 2 : 1) : 2048 * 256 / S::THREADS;
+  const int64_t groups = (a.T + S::SLOTS - 1) / S::SLOTS, most = BACK ? stem_block_grid(a.d) : 2048 * 256 / S::THREADS;
   // Up to 512 workgroups of the backward pass are done in one round either way: about as many take two rows in turn, and write half as many
   // partial sums (us, 1024 x 2048 19.2 -> 16.4, its fp32 19.3 -> 19.8, 512 x 4096 22.8 -> 20.0; fewer gain nothing: 512 x 2048 12.9 / 13.5).
   const bool in_turn = BACK && groups > 384 && groups <= STEM_BLOCK_GRID;
@@ -655,7 +655,7 @@ hipError_t by_width(const BlockArgs& a, hipStream_t s) {
   if constexpr (BRANCH && !BACK)
     if (a.d > 1024 && a.d <= 2048 && a.T * a.d * (int64_t)sizeof(E) >= (64 << 20)) return launch<E, 128, 2, BRANCH, BACK>(a, s);
   if (a.d <= 2048) return launch<E, 256, 1, BRANCH, BACK>(a, s);
-  if (a.d <= 4096) return launch<E, BACK ? 512 : 256, BACK ? 1 : 2, BRANCH, BACK>(a, s);
+  if (a.d <= STEM_BLOCK_WIDE) return launch<E, BACK ? 512 : 256, BACK ? 1 : 2, BRANCH, BACK>(a, s);
   if (a.d <= 8192) return launch<E, BRANCH && !BACK ? 512 : 1024, BRANCH && !BACK ? 2 : 1, BRANCH, BACK>(a, s);
   return launch<E, 1024, 2, BRANCH, BACK>(a, s);
 }

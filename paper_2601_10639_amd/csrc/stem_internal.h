@@ -119,7 +119,7 @@ struct stem_ctx {
   void* edit_rep_dev;        // [STEM_EDIT_MAX_TOKENS, F] replacement rows
 
   // gradients of the block around the layer that are sums over tokens: partial sums, [3][workgroups][d_model]
-  float* block_part;
+  float *block_part, *block_own;   // where they lie (stem_route_block_scratch), and what is freed
 
   // 8-bit products (STEM_RESERVE_QUANT)
   int8_t *quant_x, *quant_h;      // rows of a call; their hidden values
@@ -277,6 +277,8 @@ int stem_route_touch_bytes(int d_model, int d_ff, int64_t T);   // of W_down, to
 // 124 / 146; fp32, 256 x 1024, 8192 tokens (0.9) 212 / 203 / 197, 512 x 2048, vocabulary 8000, 2000 tokens (1.5) 156 / 131 / 149.  On two contexts two in
 // turn are within 1 % of a stream for each, and of one but at 8192 tokens of 1024 x 4096 (381 / 393) and 4096 of 2048 x 8192 (470 / 510).
 int stem_route_copy_streams(int d_model, int d_ff, int dtype, int64_t T, int64_t rows);
+// bytes of the partial sums of a block's gradients, and where they lie: 0 with the K slices' sums, 1 with the hidden values, 2 in memory of their own
+int stem_route_block_scratch(int d_model, int d_ff, int dtype, int64_t max_tokens, int64_t* bytes);
 // the tile and K slices of an 8-bit product of more than 64 tokens: {tile rows, tile columns, K slices}
 void stem_route_quant(int M, int N, int K, int gate, int64_t ws_bytes, int32_t* route);
 void stem_exchange_two_launches(stem_ctx* c, int on);   // no layer in one launch on this context
