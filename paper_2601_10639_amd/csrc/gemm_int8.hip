@@ -35,6 +35,13 @@ __device__ __forceinline__ void lds_dma_16(rsrc_t rs, char* lds_dst, uint32_t of
 __device__ __forceinline__ rsrc_t resource(const void* p, int bytes) {
   return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(p), 0, bytes, 0x00020000);
 }
+// 16 bytes to a buffer, all of the address in the vector offset.  With a scalar register as the other offset the compiler has been seen to let the
+// next vector instruction write one of the data's registers (it keeps two apart only where that offset is a constant), and the last 4 lanes of
+// each 16 stored what that had written: hidden values of zero in the gate product's second workgroup of a compute unit.
+template <int POLICY = 0>
+__device__ __forceinline__ void store_16(u32x4_t v, rsrc_t r, uint32_t off) {
+  __builtin_amdgcn_raw_buffer_store_b128(v, r, off, 0, POLICY);
+}
 
 // Workgroup -> tile, as the bf16 products do it: the workgroups of an XCD take a contiguous run of tiles, walked in bands of 4 token tiles.
 __device__ __forceinline__ void tile_of(int b, int nb, int ntm, int ntn, int& tm, int& tn) {
@@ -283,7 +290,7 @@ struct Hidden {
         top_neg[i] = max(max(top_neg[i], h[0]), h[1]);
         top_neg[i] = max(max(top_neg[i], h[2]), h[3]);
         const bool out = first + j >= blocks || m0 + 32 * i >= p.M;
-        __builtin_amdgcn_raw_buffer_store_b128(h, rh, out ? OOB : lane * 16, ((((m0 >> 5) + i) * blocks + first + j) * 4 + g) * 1024, 0);
+        store_16(h, rh, (out ? OOB : (uint32_t)(((m0 >> 5) + i) * blocks + first + j) * 4096u + lane * 16u) + g * 1024u);
       }
       __builtin_amdgcn_sched_barrier(0);                       // (all steps' reads at once would not fit the registers)
       cur = nxt;
@@ -560,7 +567,7 @@ __device__ __forceinline__ bool last_slice(const QuantGemmArgs& p, i32x16_t (&ac
 #pragma unroll
       for (int g = 0; g < 4; ++g) {
         const i32x4_t v = {acc[i][j][4 * g], acc[i][j][4 * g + 1], acc[i][j][4 * g + 2], acc[i][j][4 * g + 3]};
-        __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4_t, v), rw, lane * 16, at * BYTES + ((i * NJ + j) * 4 + g) * 1024, SC1);
+        store_16<SC1>(__builtin_bit_cast(u32x4_t, v), rw, (uint32_t)(at * BYTES + lane * 16) + ((i * NJ + j) * 4 + g) * 1024u);
       }
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
   __syncthreads();
