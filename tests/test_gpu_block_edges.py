@@ -5,6 +5,7 @@ import torch
 
 from oracle import block_oracle as B
 from paper_2601_10639_amd import stemlib as L
+from tests import test_gpu_block as M
 
 pytestmark = pytest.mark.gpu
 DEV = "cuda:0"
@@ -227,3 +228,59 @@ def test_dropout_of_more_than_a_launch_holds():
     assert torch.equal(x[rows].cpu(), want)
     del x
     torch.cuda.empty_cache()
+
+
+# 385 to 512 workgroups of the backward pass take two rows, or two sets of rows, in turn: at both ends, one more, and an odd number of them
+@pytest.mark.parametrize("dtype,T,d", [("bf16", 769, 2048), ("bf16", 801, 2048), ("bf16", 1024, 2048), ("bf16", 1025, 2048), ("bf16", 385, 4096), ("bf16", 511, 2112), ("bf16", 401, 8192),
+                                       ("f32", 770, 2044), ("f32", 1023, 1028), ("f32", 387, 4096), ("f32", 512, 2052), ("f32", 3201, 260), ("f32", 390, 5000)])
+def test_rows_in_turn(dtype, T, d):
+    M.test_leave(dtype, T, d, "rms", "layer", "channel", 0.1)
+    M.test_leave(dtype, T, d, "layer", "rms", "token", 0.0)
+    M.test_enter(dtype, T, d, "rms")
+
+
+@pytest.mark.parametrize("dtype,T,d", [("bf16", 37, 192), ("f32", 700, 260), ("bf16", 300, 2048), ("bf16", 5, 8256)])
+def test_outputs_in_the_place_of_any_input(dtype, T, d):
+    """Every [T,d] output over every [T,d] input, against the same call with memory of its own for each."""
+    ctx = make_ctx(dtype, T, d)
+    (f, x, dy, dn, gate), w = (draw(dtype, s, T, d) for s in range(5)), draw(dtype, 9, d)
+    norm = L.stem_norm(L.STEM_NORM_RMS, 1e-5, w)
+
+    def leave(g):
+        return L.stem_leave(out=norm, next=norm, residual_scale=0.5, branch_scale=2.0, gate_kind=L.STEM_GATE_FULL, gate=g, p=0.2, seed=3, offset=4)
+
+    def forward(y_over=None, n_over=None):
+        t = dict(f=f.clone(), x=x.clone(), gate=gate.clone())
+        y, n = t.get(y_over, torch.empty_like(x)), t.get(n_over, torch.empty_like(x))
+        L.stem_block_leave_forward(ctx, t["f"], t["x"], leave(t["gate"]), y, n)
+        return y, n
+
+    y, n = forward()
+    for a in ("f", "x", "gate", None):
+        for b in ("f", "x", "gate", None):
+            if a != b or a is None:
+                assert all(torch.equal(p, q) for p, q in zip((y, n), forward(a, b)))
+
+    def backward(**over):
+        t = dict(dy=dy.clone(), dn=dn.clone(), f=f.clone(), y=y.clone(), gate=gate.clone())
+        out = [t.get(over.get(k), torch.empty_like(x)) for k in ("dx", "df", "dgate")]
+        sums = [torch.empty(d, device=DEV) for _ in range(2)]
+        L.stem_block_leave_backward(ctx, t["dy"], t["dn"], t["f"], t["y"], leave(t["gate"]), *out, *sums)
+        return out + sums
+
+    want = backward()
+    inputs = ("dy", "dn", "f", "y", "gate")
+    for i, a in enumerate(inputs):
+        places = {"dx": a, "df": inputs[(i + 1) % 5], "dgate": inputs[(i + 2) % 5]}
+        for one in [places, {"dx": inputs[(i + 2) % 5], "df": a, "dgate": inputs[(i + 1) % 5]}] + [{k: a} for k in places]:
+            assert all(torch.equal(p, q) for p, q in zip(want, backward(**one)))
+
+    def enter(over=None):
+        t = dict(dn=dn.clone(), x=x.clone(), dres=dy.clone())
+        dx, dw = t.get(over, torch.empty_like(x)), torch.empty(d, device=DEV)
+        L.stem_block_enter_backward(ctx, t["dn"], t["x"], norm, dx, dw, dres=t["dres"])
+        return dx, dw
+
+    want = enter()
+    for a in ("dn", "x", "dres"):
+        assert all(torch.equal(p, q) for p, q in zip(want, enter(a)))
