@@ -305,7 +305,12 @@ stem_status stem_dropout(stem_ctx* ctx, const void* x, int64_t T, int64_t width,
 
 /* Q(v) of a row: s = max |v| / 127 and the integers rint(v / s).  A product is s_t s_n (sum over k of q_tk q_nk), its sum exact: a scale for
  * each token, taken from the row within the call, and one for each channel of the weights, which are quantised once.
- * A row with a NaN or an infinity makes NaN of all that depends on it, and of nothing else. */
+ * A row with a NaN or an infinity makes NaN of all that depends on it, and of nothing else.
+ *
+ * The weights take half the bytes.  Time is saved from some tokens on: the bf16 layer, behind stem_block_enter_forward, is as fast or faster up to
+ * about 32 tokens of d_model 2048, d_ff 8192 and of 1536, 5120, up to 256 of 1024, 4096; from 512 tokens of each on 8 bits are ahead, at 4096 by 11 to
+ * 23 %.  (us, bf16 / 8 bits, weights of 16 layers in turn: 2048 x 8192 17.5 / 18.8 at one token, 20.5 / 24.8 at 16, 30.3 / 28.3 at 64, 45 / 40 at 256,
+ * 244 / 200 at 4096; 1024 x 4096 10.1 / 12.9, 11.1 / 17.8, 16.3 / 20.6, 24 / 27, 85 / 75.) */
 
 /* Bytes of the 8-bit form of a weight matrix [N,K], which only these calls read (blocks of 32 rows by 32 k, padded). */
 int64_t stem_quant_bytes(int64_t N, int64_t K);

@@ -278,7 +278,7 @@ __device__ __forceinline__ float factor(const C& c, float (&v)[VPT][8], const st
 // to its stores.  A workgroup keeps what is the same for all rows (w_out times a gate a channel, w_next) in registers and takes as many rows
 // as leave 8 workgroups to a compute unit.
 // Measured, 16384 x 2048 in bf16, both norms, a gate a channel, p 0.1: 53 to 55 us, 5 TB/s of the 268 MB that have to move (a copy reaches 6.0).
-// Arithmetic is nearly as long: about 17 million VALU instructions, 29 us of all SIMDs, 13 more for the generator's wide multiplications.  One token: the launch.
+// Arithmetic is nearly as long: about 15 million VALU instructions, 26 us of all SIMDs, 13 more for the generator's wide multiplications.  One token: the launch.
 template <class E, int LPR, int VPT, bool BRANCH>
 __global__ __launch_bounds__((Shape<E, LPR, VPT, false>::THREADS)) void block_forward_kernel(BlockArgs p) {
   typedef Shape<E, LPR, VPT, false> S;
@@ -354,7 +354,8 @@ __global__ __launch_bounds__((Shape<E, LPR, VPT, false>::THREADS)) void block_fo
 // block_sums_kernel adds those in order.  No atomics: the same bits on every run.  dw_out and the gradient of a gate a channel are the same
 // sum, of h times the kept N_out(f), times the gate and times w_out: it is held once.  All of a row is requested before its first reduction.
 // Measured, 16384 x 2048 in bf16, both norms, a gate a channel, p 0.1: 83 us and 4 for the sums, 4.6 TB/s of the 403 MB that have to move;
-// the arithmetic alone is about 60 us (28.7 million VALU instructions), and 117 registers leave 16 wavefronts a compute unit to hide the rest.
+// the arithmetic alone is about 60 us (29.3 million VALU instructions), and 115 registers leave 16 wavefronts a compute unit to hide the rest.
+// Without BRANCH, the same shape: 56 us, 4.8 TB/s; 16384 x 2048 in fp32 100 us, with BRANCH 158.
 // Workgroups of 512, two rows of 2048 each: 512 of them are all resident, and write half as many partial sums as 1024 of 256 would.  Of 1024
 // a compute unit holds one: 256 (512 take two turns: 4096 x 8192 119 us instead of 112, 1024 x 8192 46.7 / 37.2, 2048 x 16384 157 / 139).
 template <class E, int LPR, int VPT, bool BRANCH>
@@ -587,7 +588,7 @@ __global__ __launch_bounds__(1024) void block_sums_kernel(SumArgs p) {
 
 // ---- dropout by itself -------------------------------------------------------------------------------------
 // A thread has the eight elements of a counter; `tx` (a power of two) threads lie along a row.  Measured: 65536 x 1024 in bf16 44.5 us, 6.0 TB/s,
-// what a copy reaches; the generator takes about 39 of them beside.  999 x 1001 in fp32, element by element, 5.0.
+// what a copy reaches; the generator takes about 39 of them beside.  999 x 1001 in fp32, element by element, 5.0 to 5.2.
 template <class E>
 __global__ __launch_bounds__(256) void dropout_kernel(const E* x, E* y, int64_t T, int64_t d, int64_t row0, int tx_log, DropArgs drop,
                                                       int vectors) {
@@ -617,8 +618,10 @@ template <class E, int LPR, int VPT, bool BRANCH, bool BACK>
 hipError_t launch(const BlockArgs& a, hipStream_t s) {
   typedef Shape<E, LPR, VPT, BACK> S;
   const int64_t groups = (a.T + S::SLOTS - 1) / S::SLOTS, most = BACK ? stem_block_grid(a.d) : 2048 * 256 / S::THREADS;
-  // Up to 512 workgroups of the backward pass are done in one round either way: about as many take two rows in turn, and write half as many
-  // partial sums (us, 1024 x 2048 19.2 -> 16.4, its fp32 19.3 -> 19.8, 512 x 4096 22.8 -> 20.0; fewer gain nothing: 512 x 2048 12.9 / 13.5).
+  // Up to 512 workgroups of the backward pass are done in one round either way: 385 and more take two rows in turn, and write half as many partial
+  // sums.  us, one each / two in turn, with BRANCH: bf16 4000 x 512 12.6 / 12.1, 2000 x 1024 14.4 / 13.7, 1024 x 2048 17.4 / 15.2, 512 x 4096 22.0 / 19.2;
+  // fp32 4000 x 512 15.2 / 14.4, 2000 x 1024 17.1 / 18.0, 800 x 2048 17.8 / 16.6, 1024 x 2048 19.0 / 19.1, 512 x 4096 21.3 / 20.4.  Without: bf16 512 x 4096
+  // 11.3 / 10.1, fp32 13.3 / 11.4, the others within 0.5 of each other.  (Fewer workgroups gain nothing: 512 x 2048 12.9 / 13.5.)
   const bool in_turn = BACK && groups > 384 && groups <= STEM_BLOCK_GRID;
   const int grid = (int)(in_turn ? (groups + 1) / 2 : groups < most ? groups : most);
   if constexpr (BACK) {

@@ -249,8 +249,8 @@ struct Hidden {
     float* const scales = reinterpret_cast<float*>(lds + ROWS);
 #pragma unroll
     for (int c = lane; c < 32 * NJ; c += 64) scales[c] = p.scale_b[n0 + c < p.N ? n0 + c : 0];
-    // Columns past d_ff, up to the pitch of the next product's K, have sums of zero, and a row's first columns of the table: they become
-    // zeros, or NaN where the row's own first columns are no numbers either.
+    // Columns past d_ff that a wavefront has have sums of zero, and a row's first columns of the table: they become zeros, or NaN where the
+    // row's own first columns are no numbers either.  Blocks past d_ff that no wavefront has are not written (quant.h).
     const int blocks = (p.N + 127) / 128 * 4, first = n0 >> 5;
     const rsrc_t rh = resource(p.h, (p.M + 31) / 32 * blocks * 4096);
     // largest positive value as an integer, and as an unsigned one the largest negative: NaN are above all numbers in both

@@ -2,8 +2,9 @@
 //
 // Layout.  A matrix [rows, K] is kept as blocks of 32 rows x 32 k, 1 KB each: chunk h of row r, 16 bytes of k = 16 h .. 16 h + 15, lies at
 // (32 h + r) * 16, so that a block is one operand of v_mfma_i32_32x32x32_i8 with lane l's 16 bytes at 16 l, and a load of it is 1 KB in a
-// row wherever it is made from.  The blocks of 32 rows follow each other along k; k is padded with zeros to a multiple of 128 and the
-// rows to one of 32.
+// row wherever it is made from.  The blocks of 32 rows follow each other along k; k is padded to a multiple of 128 and the rows to one of
+// 32.  Weights are padded with zeros.  What tokens have there is any integer, of hidden values in blocks that no kernel wrote too: behind a row's
+// end in k it meets the weights' zeros, and rows past the last one are in no output.
 #pragma once
 #include "stem_internal.h"
 
@@ -40,7 +41,7 @@ struct QuantGemmArgs {
   bf16_t* y;                        // [M, N], or null: a gate product
   const bf16_t* residual;           // [M, N], may be null
   float* h;                         // SiLU(product) * E[ids], blocks of 32 tokens x 32 channels, 4 KB: the four channels 8 g + 4 (l / 32) ..
-                                    // of token l % 32 at (64 g + l) * 16; channels up to the pitch of N
+                                    // of token l % 32 at (64 g + l) * 16; blocks of a row: up to the pitch of N
   uint32_t* amax;                   // [M], zero: takes the bits of each token's largest magnitude
   const int32_t* ids;
   const bf16_t* E;
