@@ -167,7 +167,7 @@ def _context(d, F, V, dtype, T, groups=0, backward=False):
     if key not in _contexts:
         _contexts[key] = L.stem_create(d, F, V, dtype, T)
         if groups:
-            L.stem_fp8_reserve(_contexts[key], groups=groups, backward=backward)
+            L.stem_qfloat_reserve(_contexts[key], groups=groups, backward=backward)
     return _contexts[key]
 
 
@@ -192,14 +192,14 @@ def prepare(case, seed):
         K, N, G = c["K"], c["N"], c["groups"]
         m = -(-max(K, N) // 64) * 64
         s["ctx"] = _context(64, m, 1000, code, T, G, op == "grad")
-        s["pW"] = L.stem_fp8_weights(s["ctx"], s["W"], backward=op == "grad")
+        s["pW"] = L.stem_qfloat_weights(s["ctx"], s["W"], backward=op == "grad")
         if op == "grad":
             s.update(dx=empty(T, K), dW=empty(G, N, K, dtype=F32))
         else:
             s.update(y=empty(T, N), norm=None if c["norm"] == "none" else L.stem_norm(kinds[c["norm"]], EPS, s["w"]))
     elif op == "ffn":
         s["ctx"] = _context(c["d"], c["F"], c["V"], code, T, c["groups"])
-        s["pWg"], s["pWd"] = L.stem_fp8_weights(s["ctx"], s["Wg"]), L.stem_fp8_weights(s["ctx"], s["Wd"])
+        s["pWg"], s["pWd"] = L.stem_qfloat_weights(s["ctx"], s["Wg"]), L.stem_qfloat_weights(s["ctx"], s["Wd"])
         s.update(norm=L.stem_norm(L.STEM_NORM_RMS, EPS, s["w"]), y=empty(T, c["d"]))
     else:
         k, d = c["k"], c["d"]
@@ -308,13 +308,13 @@ def _own(s):
     from paper_2601_10639_amd import stemlib as L
     c, op = s["case"], s["case"]["op"]
     if op == "linear":
-        L.stem_fp8_linear(s["ctx"], s["x"], s["pW"], s["y"], residual=s["res"], norm=s["norm"], offsets=s["offsets"])
+        L.stem_qfloat_linear(s["ctx"], s["x"], s["pW"], s["y"], residual=s["res"], norm=s["norm"], offsets=s["offsets"])
         return s["y"]
     if op == "grad":
-        L.stem_fp8_linear_backward(s["ctx"], s["dy"], s["x"], s["pW"], s["dx"], s["dW"], offsets=s["offsets"])
+        L.stem_qfloat_linear_backward(s["ctx"], s["dy"], s["x"], s["pW"], s["dx"], s["dW"], offsets=s["offsets"])
         return s["dx"], s["dW"]
     if op == "ffn":
-        L.stem_fp8_ffn_forward(s["ctx"], s["x"], s["ids"], s["pWg"], s["pWd"], s["E"], s["y"], residual=s["x"], norm=s["norm"], offsets=s["offsets"])
+        L.stem_qfloat_ffn_forward(s["ctx"], s["x"], s["ids"], s["pWg"], s["pWd"], s["E"], s["y"], residual=s["x"], norm=s["norm"], offsets=s["offsets"])
         return s["y"]
     if op == "dispatch":
         L.stem_experts_sort(s["ctx"], s["experts"], s["src"], s["place"], s["offsets"])
