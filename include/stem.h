@@ -330,6 +330,39 @@ stem_status stem_quant_ffn_forward(stem_ctx* ctx, const void* x, const int32_t* 
                                    const float* gate_scale, const void* down_q, const float* down_scale, const void* E, int64_t E_rows,
                                    const void* residual, void* y, void* stream);
 
+/* ---- tokens to experts and back ------------------------------------------------------ */
+
+/* A token has k choices (1 to 16), each an expert 0 .. n_experts - 1 (up to 512) or, negative, none (padding, a choice that is dropped).  The
+ * (token, choice) pair t k + j is its place in experts [T,k].  Rows of an expert stand together once they are sorted, which is what
+ * stem_qfloat_linear and stem_qfloat_ffn_forward read with `offsets`; weights are the router's, fp32.  Rows have any width, in the context's
+ * dtype; sums are in fp32 and rounded once.  No atomics: the same bits on every run.  Arrays of integers and fp32 weights may begin at any 4 bytes. */
+#define STEM_EXPERTS_MAX 512
+#define STEM_EXPERTS_MAX_CHOICES 16
+
+/* Sorts the pairs by expert, those of one in their own order.  place [T,k]: the row of each pair, -1 where it has no expert; src [T k]: the pair
+ * of each row, -1 in the rows behind the last pair that has one; offsets [n_experts + 1]: the first row of each expert, and the end.  An expert
+ * of n_experts or more counts as none and raises the id-range flag.  T == 0: offsets are zero. */
+stem_status stem_experts_sort(stem_ctx* ctx, const int32_t* experts, int64_t T, int k, int n_experts, int32_t* src, int32_t* place,
+                              int32_t* offsets, void* stream);
+
+/* xs[r] = x[src[r] / k] for x [T,width], xs [rows,width]; and ids_out[r] = ids[src[r] / k], for the layer on the rows, where ids [T] and
+ * ids_out [rows] are not NULL.  Rows whose src is negative are left as they were.  Its backward pass: stem_experts_combine without weights
+ * (dxs in, dx out, residual: the gradient that reaches x otherwise). */
+stem_status stem_experts_dispatch(stem_ctx* ctx, const void* x, int64_t T, int64_t width, const int32_t* src, int64_t rows, int k,
+                                  const int32_t* ids, void* xs, int32_t* ids_out, void* stream);
+
+/* y_t = residual_t + sum over j of weights[t,j] ys[place[t,j]], in the order of j; choices whose place is negative add nothing, whatever their weight.
+ * weights NULL: ones.  residual [T,width] may be NULL, and may be y.  ys [rows,width]; nothing else overlaps y. */
+stem_status stem_experts_combine(stem_ctx* ctx, const void* ys, int64_t rows, int64_t width, const int32_t* place, const float* weights,
+                                 int64_t T, int k, const void* residual, void* y, void* stream);
+
+/* Its backward pass for dy [T,width]: dys[place[t,j]] = weights[t,j] dy_t, other rows of dys [rows,width] left as they were; dweights[t,j] =
+ * sum over the row of dy_t ys[place[t,j]], 0 where there is no place.  Either may be NULL, and so may ys without dweights.  place names a
+ * row at most once.  (The residual's gradient is dy.)  Places beyond the rows raise the id-range flag: such a pair reads the last row in stem_experts_combine, and
+ * here gives nothing but a dweights of 0. */
+stem_status stem_experts_combine_backward(stem_ctx* ctx, const void* dy, const void* ys, int64_t rows, int64_t width, const int32_t* place,
+                                          const float* weights, int64_t T, int k, void* dys, float* dweights, void* stream);
+
 /* ---- host-resident table (System Implementation: CPU offloading, asynchronous
  *      prefetch, token de-duplication) ------------------------------------------- */
 

@@ -12,6 +12,7 @@
 #include <vector>
 
 #include "block.h"
+#include "experts.h"
 #include "quant.h"
 
 namespace {
@@ -25,7 +26,9 @@ const char* const kKernelNames[K_COUNT_] = {
     "splitk_reduce",   "gemm_up",      "gemm_dw_up",   "sort_merge",
     "grads_f32", "gemm_dw", "list_copy", "ffn_decode",
     "block_enter", "block_enter_back", "block_leave", "block_leave_back", "dropout",
-    "quant_weights", "quant_rows", "quant_gate", "quant_hidden", "quant_down"};
+    "quant_weights", "quant_rows", "quant_gate", "quant_hidden", "quant_down",
+    "experts_sort", "experts_dispatch", "experts_combine", "experts_combine_back", "qfloat_weights", "qfloat_rows", "qfloat_tiles", "qfloat_gate",
+    "qfloat_linear", "qfloat_dx", "qfloat_dw"};
 
 #define fail stem_fail
 
@@ -169,6 +172,8 @@ void release(stem_ctx* c) {
   (void)hipFree(c->block_own);
   if (c->quant_ws != reinterpret_cast<int*>(c->splitk_ws)) (void)hipFree(c->quant_ws);
   (void)hipFree(c->quant_x); (void)hipFree(c->quant_h); (void)hipFree(c->quant_sx); (void)hipFree(c->quant_sh); (void)hipFree(c->quant_amax); (void)hipFree(c->quant_max); (void)hipFree(c->quant_hidden);
+  (void)hipFree(c->experts_counts);
+  (void)hipFree(c->qfloat_x); (void)hipFree(c->qfloat_h); (void)hipFree(c->qfloat_dyt); (void)hipFree(c->qfloat_xt); (void)hipFree(c->qfloat_ws);
   if (c->inst_pinned) (void)hipHostFree(c->inst_pinned);
   (void)hipFree(c->inst_dev);
   if (c->side) copy_streams_put(c->device);
@@ -344,6 +349,7 @@ stem_status stem_create(stem_ctx** out, const stem_layer_desc* desc, int64_t max
   }
   ok(dmalloc(&c->sort_counts, (size_t)stem_sort_count_entries(std::max<int64_t>(max_tokens, 1))));
   ok(dmalloc(&c->seg_of, (size_t)max_tokens));
+  ok(dmalloc(&c->experts_counts, (size_t)(max_tokens * STEM_EXPERTS_MAX_CHOICES / EXPERTS_SEGMENT + 1) * (STEM_EXPERTS_MAX + 1)));
   ok(dmalloc(&c->seg_part, (size_t)stem_seg_chunks(std::max<int64_t>(max_tokens, 1)) * 2 * desc->d_ff));
   int64_t block_bytes;
   switch (stem_route_block_scratch(desc->d_model, desc->d_ff, desc->dtype, max_tokens, &block_bytes)) {

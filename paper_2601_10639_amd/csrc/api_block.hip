@@ -5,54 +5,13 @@
 #include <algorithm>
 
 #include "block.h"
+#include "checks.h"
 #include "quant.h"
 
 namespace {
 
-#define HIP_TRY(c, expr)                                                                                                       \
-  do {                                                                                                                         \
-    hipError_t e_ = (expr);                                                                                                    \
-    if (e_ != hipSuccess)                                                                                                      \
-      return stem_fail((c), STEM_ERR_HIP, "%s failed: %s (%s:%d)", #expr, hipGetErrorString(e_), __FILE__, __LINE__);          \
-  } while (0)
-#define STEM_TRY(expr)                                   \
-  do {                                                   \
-    const stem_status st_ = (expr);                      \
-    if (st_ != STEM_OK) return st_;                      \
-  } while (0)
-
 constexpr int64_t QUANT_MAX_CHANNELS = 1 << 22;   // 256 rows of an output are addressed with 32 bits
 constexpr int64_t QUANT_MAX_K = 131072;           // up to here a sum of products of two bytes, 127 x 127 at most, fits 32 bits
-
-struct Buffer { const void* p; size_t bytes; };
-
-bool overlap(const Buffer& a, const Buffer& b) {
-  const uintptr_t x = reinterpret_cast<uintptr_t>(a.p), y = reinterpret_cast<uintptr_t>(b.p);
-  return a.p && b.p && x < y + b.bytes && y < x + a.bytes;
-}
-
-// Alignment of all buffers; no output over another, nor over an input unless `in_place` and it is that input.
-stem_status check_buffers(stem_ctx* c, const char* who, std::initializer_list<Buffer> in, std::initializer_list<Buffer> out, bool in_place) {
-  for (auto& list : {in, out})
-    for (const Buffer& b : list)
-      if (reinterpret_cast<uintptr_t>(b.p) & 15u) return stem_fail(c, STEM_ERR_INVALID_ARG, "%s: pointers must be 16-byte aligned", who);
-  for (const Buffer* o = out.begin(); o != out.end(); ++o) {
-    for (const Buffer& i : in)
-      if (overlap(*o, i) && !(in_place && o->p == i.p && o->bytes == i.bytes))
-        return stem_fail(c, STEM_ERR_INVALID_ARG, "%s: an output lies over an input", who);
-    for (const Buffer* other = out.begin(); other != o; ++other)
-      if (overlap(*o, *other)) return stem_fail(c, STEM_ERR_INVALID_ARG, "%s: an output lies over another", who);
-  }
-  return STEM_OK;
-}
-
-stem_status check_norm(stem_ctx* c, const char* who, const stem_norm& n) {
-  if (n.kind != STEM_NORM_NONE && n.kind != STEM_NORM_RMS && n.kind != STEM_NORM_LAYER)
-    return stem_fail(c, STEM_ERR_INVALID_ARG, "%s: %d is not a stem_norm_kind", who, n.kind);
-  if (n.kind != STEM_NORM_NONE && !(n.eps >= 0.f && n.eps < INFINITY))
-    return stem_fail(c, STEM_ERR_INVALID_ARG, "%s: eps = %g", who, (double)n.eps);
-  return STEM_OK;
-}
 
 // (every workgroup reads the step, also when others have stored their part of an output)
 stem_status check_drop(stem_ctx* c, const char* who, const stem_drop& d, std::initializer_list<Buffer> outputs, DropArgs* out) {

@@ -44,6 +44,17 @@ enum StemKernelId {
   K_QUANT_GATE,      // 8-bit gate product with SiLU*gather
   K_QUANT_HIDDEN,    // hidden values to 8-bit integers
   K_QUANT_DOWN,      // 8-bit product
+  K_EXPERTS_SORT,    // (token, choice) pairs by expert
+  K_EXPERTS_DISPATCH,
+  K_EXPERTS_COMBINE,
+  K_EXPERTS_COMBINE_BACK,
+  K_QFLOAT_WEIGHTS,  // bf16 weights to 8-bit floating point
+  K_QFLOAT_ROWS,     // (normed) activations
+  K_QFLOAT_TILES,    // gradients and activations, by rows and by columns
+  K_QFLOAT_GATE,     // gate product with SiLU*gather and its result's 8-bit form
+  K_QFLOAT_LINEAR,
+  K_QFLOAT_DX,
+  K_QFLOAT_DW,
   K_COUNT_
 };
 
@@ -128,6 +139,14 @@ struct stem_ctx {
   uint32_t* quant_max;            // those of up to 8 tokens, in each tile of 32 channels
   float* quant_hidden;            // hidden values of stem_quant_chunk tokens
   int* quant_ws;         // sums of the 8-bit products' K slices: the room above where that has QUANT_WS bytes, else its own
+
+  int32_t* experts_counts;        // each expert's pairs in every segment of a sort
+
+  // 8-bit floating point products (stem_qfloat_reserve): room for rows of a call, their hidden values, and for the backward pass dy and x by columns
+  int qfloat_groups;              // of weights, that it is sized for; 0: not reserved
+  int qfloat_backward;
+  uint8_t *qfloat_x, *qfloat_h, *qfloat_dyt, *qfloat_xt;
+  float* qfloat_ws;               // partial sums of K slices, and hidden values of few tokens
 
   // profiling
   int prof_on;

@@ -29,6 +29,7 @@ SYMBOLS = [
     "stem_embed_grad", "stem_embed_grad_presorted", "stem_embed_grad_noalloc", "stem_embed_sparse_adamw",
     "stem_block_enter_forward", "stem_block_enter_backward", "stem_block_leave_forward", "stem_block_leave_backward", "stem_dropout",
     "stem_quant_bytes", "stem_quant_weights", "stem_quant_linear", "stem_quant_ffn_forward",
+    "stem_experts_sort", "stem_experts_dispatch", "stem_experts_combine", "stem_experts_combine_backward",
     "stem_prefetch_rows", "stem_cache_init", "stem_prefetch_rows_cached", "stem_cache_state",
     "stem_edit_rows", "stem_profile_enable", "stem_profile_kernels", "stem_profile_read",
     "stem_profile_reset", "stem_measure_peak",
@@ -200,6 +201,14 @@ def lib() -> ctypes.CDLL:
         L.stem_quant_linear.restype = i32
         L.stem_quant_ffn_forward.argtypes = [vp, vp, vp, i64, norm, vp, vp, vp, vp, vp, i64, vp, vp, vp]
         L.stem_quant_ffn_forward.restype = i32
+        L.stem_experts_sort.argtypes = [vp, vp, i64, i32, i32, vp, vp, vp, vp]
+        L.stem_experts_sort.restype = i32
+        L.stem_experts_dispatch.argtypes = [vp, vp, i64, i64, vp, i64, i32, vp, vp, vp, vp]
+        L.stem_experts_dispatch.restype = i32
+        L.stem_experts_combine.argtypes = [vp, vp, i64, i64, vp, vp, i64, i32, vp, vp, vp]
+        L.stem_experts_combine.restype = i32
+        L.stem_experts_combine_backward.argtypes = [vp, vp, vp, i64, i64, vp, vp, i64, i32, vp, vp, vp]
+        L.stem_experts_combine_backward.restype = i32
         L.stem_profile_enable.argtypes = [vp, i32]
         L.stem_profile_enable.restype = i32
         L.stem_profile_kernels.argtypes = []
@@ -679,6 +688,42 @@ def stem_quant_ffn_forward(ctx: StemCtx, x, ids, gate: StemQuant, down: StemQuan
                                           _shaped(y, dt, (T, d), "y"), _stream(stream))
     if st != STEM_OK:
         _check(ctx, st, "stem_quant_ffn_forward")
+
+
+def stem_experts_sort(ctx: StemCtx, experts, src, place, offsets, stream=None):
+    """experts [T, k] -> place [T, k], src [T * k], offsets [n_experts + 1]; n_experts is what offsets has room for."""
+    i32, (T, k) = torch.int32, experts.shape
+    st = lib().stem_experts_sort(ctx.handle, _shaped(experts, i32, (T, k), "experts"), T, k, offsets.shape[0] - 1, _shaped(src, i32, (T * k,), "src"),
+                                 _shaped(place, i32, (T, k), "place"), _shaped(offsets, i32, (offsets.shape[0],), "offsets"), _stream(stream))
+    _check(ctx, st, "stem_experts_sort")
+
+
+def stem_experts_dispatch(ctx: StemCtx, x, src, xs, choices: int, ids=None, ids_out=None, stream=None):
+    """xs[r] = x[src[r] // choices], ids_out[r] = ids[src[r] // choices]; rows of a negative src are left as they were."""
+    i32, (T, width), rows = torch.int32, x.shape, src.shape[0]
+    st = lib().stem_experts_dispatch(ctx.handle, _shaped(x, ctx.torch_dtype, (T, width), "x"), T, width, _shaped(src, i32, (rows,), "src"), rows, choices,
+                                     _shaped(ids, i32, (T,), "ids"), _shaped(xs, ctx.torch_dtype, (rows, width), "xs"),
+                                     _shaped(ids_out, i32, (rows,), "ids_out"), _stream(stream))
+    _check(ctx, st, "stem_experts_dispatch")
+
+
+def stem_experts_combine(ctx: StemCtx, ys, place, y, weights=None, residual=None, stream=None):
+    """y_t = residual_t + sum_j weights[t, j] ys[place[t, j]]; y may be residual."""
+    dt, (T, k), (rows, width) = ctx.torch_dtype, place.shape, ys.shape
+    st = lib().stem_experts_combine(ctx.handle, _shaped(ys, dt, (rows, width), "ys"), rows, width, _shaped(place, torch.int32, (T, k), "place"),
+                                    _shaped(weights, torch.float32, (T, k), "weights"), T, k, _shaped(residual, dt, (T, width), "residual"),
+                                    _shaped(y, dt, (T, width), "y"), _stream(stream))
+    _check(ctx, st, "stem_experts_combine")
+
+
+def stem_experts_combine_backward(ctx: StemCtx, dy, place, dys=None, ys=None, weights=None, dweights=None, stream=None):
+    """dys[place[t, j]] = weights[t, j] dy_t, dweights[t, j] = <dy_t, ys[place[t, j]]>; either may be None."""
+    dt, (T, k), width = ctx.torch_dtype, place.shape, dy.shape[1]
+    rows = next((t.shape[0] for t in (dys, ys) if t is not None), 0)
+    st = lib().stem_experts_combine_backward(ctx.handle, _shaped(dy, dt, (T, width), "dy"), _shaped(ys, dt, (rows, width), "ys"), rows, width,
+                                             _shaped(place, torch.int32, (T, k), "place"), _shaped(weights, torch.float32, (T, k), "weights"), T, k,
+                                             _shaped(dys, dt, (rows, width), "dys"), _shaped(dweights, torch.float32, (T, k), "dweights"), _stream(stream))
+    _check(ctx, st, "stem_experts_combine_backward")
 
 
 def stem_profile_enable(ctx: StemCtx, on: bool):
