@@ -330,6 +330,48 @@ stem_status stem_quant_ffn_forward(stem_ctx* ctx, const void* x, const int32_t* 
                                    const float* gate_scale, const void* down_q, const float* down_scale, const void* E, int64_t E_rows,
                                    const void* residual, void* y, void* stream);
 
+/* ---- products and the layer in 8-bit floating point, for training and serving, by groups of rows (bf16 contexts) ------ */
+
+/* Q(v) of a block of 128 values: e is the least integer with max |v| <= 448 2^e (at least -126), and Q the values of 8-bit floating point (e4m3, to
+ * nearest even) of v 2^-e, times 2^e.  Blocks are 128 values in a row of activations and gradients, counted from the row's first (or, where a product runs over
+ * the rows, 128 rows of a column, counted from the first row of the group) and 128 x 128 of a matrix of weights, whose Q is therefore the same
+ * whichever way it is read.  Sums are in fp32 and rounded once.  A NaN or an infinity makes NaN of what depends on it and of nothing else;
+ * the blocks' largest magnitude is that of their finite values.
+ *
+ * Groups.  Weights are groups matrices (1 to 512), one behind another, and rows offsets[g] .. offsets[g + 1] of the activations meet the g-th: offsets
+ * [groups + 1], device, as stem_experts_sort leaves them.  Rows in front of offsets[0] and behind offsets[groups] belong to no group: they are not
+ * read, and what would be their output is left as it was.  Offsets that are below those before them, negative or beyond T are taken as the nearest that
+ * are not.  offsets NULL: one group of all T rows. */
+
+/* Scratch for the calls below (a set-up call: it allocates, enqueues nothing): 8-bit forms of max_tokens rows in up to `groups` groups, each of which may take
+ * up to 127 rows more, and with backward != 0 those of stem_qfloat_linear_backward.  The first call names the most groups; a later one may add backward. */
+stem_status stem_qfloat_reserve(stem_ctx* ctx, int groups, int backward);
+
+/* Bytes of the 8-bit form of a matrix [N,K], which only these calls read; that of [K,N] has as many. */
+int64_t stem_qfloat_bytes(int64_t N, int64_t K);
+/* W [groups,N,K] (bf16) -> q, what the forward calls read, and qt, its transpose for the backward pass: groups * stem_qfloat_bytes(N, K) bytes each; either may
+ * be NULL.  N, K are up to 2^22 and a form below 2^31 bytes.  W is only read here. */
+stem_status stem_qfloat_weights(stem_ctx* ctx, const void* W, int groups, int64_t N, int64_t K, void* q, void* qt, void* stream);
+
+/* y = Q(N(x)) Q(W_g)^T (+ residual): x [T,K], y and residual [T,N] bf16, 1 <= N <= 2^22, 1 <= K <= max(d_model, d_ff).  norm (host) and residual may be
+ * NULL; y may be residual, and may lie over x.  8-bit forms of x (with the groups' padding) and of a W are below 2^31 bytes. */
+stem_status stem_qfloat_linear(stem_ctx* ctx, const void* x, int64_t T, int64_t K, const stem_norm* norm, const void* q, int64_t N, int groups,
+                               const int32_t* offsets, const void* residual, void* y, void* stream);
+
+/* Its backward pass (without norm and residual, Q's own gradient taken as 1): dx [T,K] bf16 = Q(dy) Q(W_g), blocks of 128 along the row of dy; dW [groups,N,K]
+ * fp32 = dy^T x over the group's rows, of the bf16 values as they are, in fp32 sums (a gradient that is added up over steps keeps what 8 bits would lose), overwritten, or
+ * added to when accumulate != 0; a group without rows has a gradient of zero.  Either output may be NULL, x without dW and qt without dx; dx may lie over dy or x.  N, K up to max(d_model, d_ff).  T == 0: dW is
+ * zero (or left as it is). */
+stem_status stem_qfloat_linear_backward(stem_ctx* ctx, const void* dy, const void* x, int64_t T, int64_t K, const void* qt, int64_t N, int groups,
+                                        const int32_t* offsets, void* dx, float* dW, int accumulate, void* stream);
+
+/* The layer: y = Q(SiLU(Q(N(x)) Q(W_gate)^T) * E[ids]) Q(W_down)^T (+ residual), W_gate and W_down those of the row's group; ids and the bf16 table (one for all
+ * groups) as in stem_ffn_forward.  The hidden values are quantised as the gate product leaves them, not rounded before.  norm and residual may be NULL; y may be x and
+ * residual. */
+stem_status stem_qfloat_ffn_forward(stem_ctx* ctx, const void* x, const int32_t* ids, int64_t T, const stem_norm* norm, const void* gate_q,
+                                    const void* down_q, int groups, const int32_t* offsets, const void* E, int64_t E_rows, const void* residual,
+                                    void* y, void* stream);
+
 /* ---- tokens to experts and back ------------------------------------------------------ */
 
 /* A token has k choices (1 to 16), each an expert 0 .. n_experts - 1 (up to 512) or, negative, none (padding, a choice that is dropped).  The

@@ -27,7 +27,7 @@ const char* const kKernelNames[K_COUNT_] = {
     "grads_f32", "gemm_dw", "list_copy", "ffn_decode",
     "block_enter", "block_enter_back", "block_leave", "block_leave_back", "dropout",
     "quant_weights", "quant_rows", "quant_gate", "quant_hidden", "quant_down",
-    "experts_sort", "experts_dispatch", "experts_combine", "experts_combine_back", "qfloat_weights", "qfloat_rows", "qfloat_tiles", "qfloat_gate",
+    "experts_sort", "experts_dispatch", "experts_combine", "experts_combine_back", "qfloat_weights", "qfloat_rows", "qfloat_turn", "qfloat_gate",
     "qfloat_linear", "qfloat_dx", "qfloat_dw"};
 
 #define fail stem_fail

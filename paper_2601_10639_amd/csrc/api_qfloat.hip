@@ -1,0 +1,221 @@
+// Entry points of the products in 8-bit floating point: argument checks and launch sequences (qfloat.hip, gemm_qfloat.hip).
+#include <algorithm>
+
+#include "checks.h"
+#include "qfloat.h"
+
+namespace {
+
+constexpr int64_t MAX_CHANNELS = 1 << 22;
+constexpr int64_t MAX_FORM = INT32_MAX;   // elements of a form, which kernels address with 32 bits
+
+int64_t widest(const stem_ctx* c) { return std::max(c->desc.d_model, c->desc.d_ff); }
+
+stem_status check_context(stem_ctx* c, const char* who, int groups, bool backward) {
+  if (c->desc.dtype != STEM_BF16) return stem_fail(c, STEM_ERR_UNSUPPORTED, "%s: needs a bf16 context", who);
+  if (groups < 1 || groups > STEM_EXPERTS_MAX) return stem_fail(c, STEM_ERR_SHAPE, "%s: %d groups; 1 to %d", who, groups, STEM_EXPERTS_MAX);
+  if (groups > c->qfloat_groups || (backward && !c->qfloat_backward))
+    return stem_fail(c, STEM_ERR_WORKSPACE, "%s: needs stem_qfloat_reserve(ctx, %d or more, %d)", who, groups, backward ? 1 : 0);
+  return STEM_OK;
+}
+
+stem_status check_form(stem_ctx* c, const char* who, int64_t rows, int64_t K) {
+  if (stem_qfloat_size(rows, K) > MAX_FORM)
+    return stem_fail(c, STEM_ERR_SHAPE, "%s: an operand of %lld rows (padded) by %lld is 2^31 bytes or more in 8 bits", who, (long long)rows, (long long)K);
+  return STEM_OK;
+}
+
+stem_status check_groups(stem_ctx* c, const char* who, const int32_t* offsets, int groups) {
+  if (!offsets && groups != 1) return stem_fail(c, STEM_ERR_INVALID_ARG, "%s: %d groups without offsets", who, groups);
+  return check_words(c, who, {offsets});
+}
+
+struct Form { uint8_t *q, *scale; int64_t bytes; };
+Form form(const void* p, int64_t rows, int64_t K) {
+  uint8_t* const q = static_cast<uint8_t*>(const_cast<void*>(p));
+  const int64_t bytes = stem_qfloat_size(rows, K);
+  return {q, q + bytes, bytes};
+}
+
+QfloatGemmArgs gemm_args(const stem_ctx* c, const Form& a, const Form& b, int64_t stride_b, int64_t M, int64_t N, int64_t K, const QfloatGroups& g) {
+  QfloatGemmArgs r = {};
+  r.A = a.q; r.sa = a.scale; r.a_bytes = a.bytes;
+  r.B = b.q; r.sb = b.scale; r.stride_b = stride_b;
+  r.M = (int)M; r.N = (int)N; r.K = (int)stem_qfloat_pitch(K);
+  r.groups = g;
+  r.ws = c->qfloat_ws; r.ws_bytes = QFLOAT_WS; r.tickets = c->tickets;
+  return r;
+}
+
+hipError_t rows_form(stem_ctx* c, const void* x, const QfloatGroups& g, int64_t K, const stem_norm* norm, const Form& f, hipStream_t s) {
+  const QfloatRowsArgs a = {static_cast<const bf16_t*>(x), g, (int)K, norm ? *norm : stem_norm{STEM_NORM_NONE, 0.f, nullptr}, f.q, f.scale};
+  return stem_qfloat_rows_launch(c, a, s);
+}
+
+}  // namespace
+
+extern "C" {
+
+int64_t stem_qfloat_bytes(int64_t N, int64_t K) { return N < 1 || K < 1 ? 0 : stem_qfloat_form(N, K); }
+
+stem_status stem_qfloat_reserve(stem_ctx* c, int groups, int backward) {
+  static const char who[] = "stem_qfloat_reserve";
+  STEM_TRY(stem_enter(c, 0));
+  if (c->desc.dtype != STEM_BF16) return stem_fail(c, STEM_ERR_UNSUPPORTED, "%s: needs a bf16 context", who);
+  if (groups < 1 || groups > STEM_EXPERTS_MAX) return stem_fail(c, STEM_ERR_SHAPE, "%s: %d groups; 1 to %d", who, groups, STEM_EXPERTS_MAX);
+  if (c->qfloat_groups && groups > c->qfloat_groups)
+    return stem_fail(c, STEM_ERR_INVALID_ARG, "%s: reserved for %d groups before; the first call names the most", who, c->qfloat_groups);
+  HIP_TRY(c, hipSetDevice(c->device));
+  const int most = c->qfloat_groups ? c->qfloat_groups : groups;
+  const int64_t T = std::max<int64_t>(c->max_tokens, 1), rows = stem_qfloat_rows(T, most), F = c->desc.d_ff, wide = widest(c);
+  auto need = [&](uint8_t** p, int64_t bytes) { return *p ? hipSuccess : hipMalloc(reinterpret_cast<void**>(p), (size_t)bytes); };
+  HIP_TRY(c, need(&c->qfloat_x, stem_qfloat_form(rows, wide)));
+  HIP_TRY(c, need(&c->qfloat_h, stem_qfloat_form(rows, F)));
+  if (!c->qfloat_ws) HIP_TRY(c, hipMalloc(reinterpret_cast<void**>(&c->qfloat_ws), QFLOAT_WS));
+  c->qfloat_groups = most;
+  if (backward) {
+    HIP_TRY(c, need(&c->qfloat_dyt, stem_qfloat_size(wide, rows) * 2));
+    HIP_TRY(c, need(&c->qfloat_xt, stem_qfloat_size(wide, rows) * 2));
+    c->qfloat_backward = 1;
+  }
+  return STEM_OK;
+}
+
+stem_status stem_qfloat_weights(stem_ctx* c, const void* W, int groups, int64_t N, int64_t K, void* q, void* qt, void* stream) {
+  static const char who[] = "stem_qfloat_weights";
+  STEM_TRY(stem_enter(c, 0));
+  if (c->desc.dtype != STEM_BF16) return stem_fail(c, STEM_ERR_UNSUPPORTED, "%s: needs a bf16 context", who);
+  if (groups < 1 || groups > STEM_EXPERTS_MAX) return stem_fail(c, STEM_ERR_SHAPE, "%s: %d groups; 1 to %d", who, groups, STEM_EXPERTS_MAX);
+  if (N < 1 || K < 1 || N > MAX_CHANNELS || K > MAX_CHANNELS) return stem_fail(c, STEM_ERR_SHAPE, "%s: matrices [%lld, %lld]", who, (long long)N, (long long)K);
+  STEM_TRY(check_form(c, who, N, K));
+  if (!W || (!q && !qt)) return stem_fail(c, STEM_ERR_INVALID_ARG, "%s: null pointer argument", who);
+  const size_t bytes = (size_t)groups * stem_qfloat_form(N, K);
+  STEM_TRY(check_buffers(c, who, {{W, (size_t)groups * N * K * 2}}, {{q, bytes}, {qt, bytes}}, false));
+  const QfloatTilesArgs a = {static_cast<const bf16_t*>(W), (int)N, (int)K, groups, static_cast<uint8_t*>(q), static_cast<uint8_t*>(qt)};
+  HIP_TRY(c, stem_qfloat_weights_launch(c, a, static_cast<hipStream_t>(stream)));
+  return STEM_OK;
+}
+
+stem_status stem_qfloat_linear(stem_ctx* c, const void* x, int64_t T, int64_t K, const stem_norm* norm, const void* q, int64_t N, int groups,
+                               const int32_t* offsets, const void* residual, void* y, void* stream) {
+  static const char who[] = "stem_qfloat_linear";
+  STEM_TRY(stem_enter(c, T));
+  STEM_TRY(check_context(c, who, groups, false));
+  if (N < 1 || N > MAX_CHANNELS || K < 1 || K > widest(c))
+    return stem_fail(c, STEM_ERR_SHAPE, "%s: a product [%lld, %lld] x [%lld, %lld]^T; K is up to %lld here, N up to 2^22", who, (long long)T, (long long)K,
+                     (long long)N, (long long)K, (long long)widest(c));
+  const int64_t rows = stem_qfloat_rows(T, groups);
+  STEM_TRY(check_form(c, who, rows, K));
+  STEM_TRY(check_form(c, who, N, K));
+  if (T == 0) return STEM_OK;
+  if (!x || !q || !y) return stem_fail(c, STEM_ERR_INVALID_ARG, "%s: null pointer argument", who);
+  STEM_TRY(check_groups(c, who, offsets, groups));
+  if (norm) STEM_TRY(check_norm(c, who, *norm));
+  const size_t xb = (size_t)T * K * 2, yb = (size_t)T * N * 2;
+  STEM_TRY(check_buffers(c, who, {{residual, yb}}, {{y, yb}}, true));
+  STEM_TRY(check_buffers(c, who, {{q, (size_t)groups * stem_qfloat_form(N, K)}, {norm ? norm->weight : nullptr, (size_t)K * 2}}, {{y, yb}}, false));
+  STEM_TRY(check_buffers(c, who, {{x, xb}}, {}, false));
+  STEM_TRY(check_apart(c, who, {{offsets, (size_t)(groups + 1) * 4}}, {{y, yb}}));
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  const QfloatGroups g = {offsets, groups, (int)T};
+  const Form f = form(c->qfloat_x, rows, K);
+  HIP_TRY(c, rows_form(c, x, g, K, norm, f, s));
+  QfloatGemmArgs a = gemm_args(c, f, form(q, N, K), stem_qfloat_form(N, K), T, N, K, g);
+  a.y = static_cast<bf16_t*>(y); a.residual = static_cast<const bf16_t*>(residual);
+  HIP_TRY(c, stem_qfloat_gemm_launch(c, K_QFLOAT_LINEAR, QFLOAT_BF16, a, s));
+  return STEM_OK;
+}
+
+stem_status stem_qfloat_linear_backward(stem_ctx* c, const void* dy, const void* x, int64_t T, int64_t K, const void* qt, int64_t N, int groups,
+                                        const int32_t* offsets, void* dx, float* dW, int accumulate, void* stream) {
+  static const char who[] = "stem_qfloat_linear_backward";
+  STEM_TRY(stem_enter(c, T));
+  STEM_TRY(check_context(c, who, groups, true));
+  if (N < 1 || N > widest(c) || K < 1 || K > widest(c))
+    return stem_fail(c, STEM_ERR_SHAPE, "%s: gradients of [%lld, %lld] x [%lld, %lld]^T; K and N are up to %lld here", who, (long long)T, (long long)K,
+                     (long long)N, (long long)K, (long long)widest(c));
+  const int64_t rows = stem_qfloat_rows(T, groups);
+  STEM_TRY(check_form(c, who, rows * 2, std::max(N, K)));   // (dy and x are transposed in bf16)
+  STEM_TRY(check_form(c, who, N, K));
+  const size_t xb = (size_t)T * K * 2, yb = (size_t)T * N * 2, wb = (size_t)groups * N * K * 4;
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  if (T == 0) {
+    STEM_TRY(check_buffers(c, who, {}, {{dW, wb}}, false));
+    if (dW && !accumulate) HIP_TRY(c, stem_fill_zero(dW, wb, s));
+    return STEM_OK;
+  }
+  if (!dy || (dx && !qt) || (dW && !x)) return stem_fail(c, STEM_ERR_INVALID_ARG, "%s: null pointer argument", who);
+  if (!dx && !dW) return STEM_OK;
+  STEM_TRY(check_groups(c, who, offsets, groups));
+  const Buffer in_x = {dW ? x : nullptr, xb}, in_q = {dx ? qt : nullptr, (size_t)groups * stem_qfloat_form(K, N)};
+  STEM_TRY(check_buffers(c, who, {{dy, yb}, in_x, in_q}, {{dW, wb}}, false));
+  STEM_TRY(check_buffers(c, who, {in_q}, {{dx, xb}, {dW, wb}}, false));
+  STEM_TRY(check_apart(c, who, {{offsets, (size_t)(groups + 1) * 4}}, {{dx, xb}, {dW, wb}}));
+  const QfloatGroups g = {offsets, groups, (int)T};
+  const Form f = form(c->qfloat_x, rows, N);
+  const auto *g_in = static_cast<const bf16_t*>(dy), *x_in = static_cast<const bf16_t*>(x);
+  // Whole matrices of aligned rows are read as they lie; others are transposed first (of dy, together with its 8-bit form)
+  const bool as_stored = groups == 1 && !offsets && N % 64 == 0 && K % 64 == 0 && wb <= INT32_MAX;
+  if (dW && !as_stored) {
+    HIP_TRY(c, stem_qfloat_turn_launch(c, {g_in, g, (int)N, c->qfloat_dyt, (int)rows * 2, dx ? f.q : nullptr, f.scale}, s));
+    HIP_TRY(c, stem_qfloat_turn_launch(c, {x_in, g, (int)K, c->qfloat_xt, (int)rows * 2, nullptr, nullptr}, s));
+  } else if (dx) {
+    HIP_TRY(c, rows_form(c, dy, g, N, nullptr, f, s));
+  }
+  if (dW && as_stored) {
+    GemmArgs a = {};
+    a.A = g_in; a.lda = (int)N;
+    a.B = x_in; a.ldb = (int)K;
+    a.M = (int)N; a.N = (int)K; a.K = (int)T;
+    a.C = dW; a.accumulate = accumulate;
+    a.ws = c->splitk_ws; a.ws_bytes = c->splitk_bytes; a.tickets = c->tickets;
+    HIP_TRY(c, stem_gemm_bf16(c, K_QFLOAT_DW, OP_MC, OP_MC, EPI_F32, a, s));
+  } else if (dW) {
+    QfloatGemmArgs a = gemm_args(c, {c->qfloat_dyt, nullptr, stem_qfloat_pitch(N) * rows * 2}, {c->qfloat_xt, nullptr, 0}, 0, N, K, rows * 2, g);
+    a.c = dW; a.accumulate = accumulate;
+    HIP_TRY(c, stem_qfloat_gemm_launch(c, K_QFLOAT_DW, QFLOAT_F32, a, s));
+  }
+  if (dx) {
+    QfloatGemmArgs a = gemm_args(c, f, form(qt, K, N), stem_qfloat_form(K, N), T, K, N, g);
+    a.y = static_cast<bf16_t*>(dx);
+    HIP_TRY(c, stem_qfloat_gemm_launch(c, K_QFLOAT_DX, QFLOAT_BF16, a, s));
+  }
+  return STEM_OK;
+}
+
+stem_status stem_qfloat_ffn_forward(stem_ctx* c, const void* x, const int32_t* ids, int64_t T, const stem_norm* norm, const void* gate_q,
+                                    const void* down_q, int groups, const int32_t* offsets, const void* E, int64_t E_rows, const void* residual,
+                                    void* y, void* stream) {
+  static const char who[] = "stem_qfloat_ffn_forward";
+  STEM_TRY(stem_enter(c, T));
+  STEM_TRY(check_context(c, who, groups, false));
+  if (T == 0) return STEM_OK;
+  if (!x || !ids || !gate_q || !down_q || !E || !y) return stem_fail(c, STEM_ERR_INVALID_ARG, "%s: null pointer argument", who);
+  if (E_rows < 1 || E_rows > INT32_MAX) return stem_fail(c, STEM_ERR_SHAPE, "%s: E_rows = %lld", who, (long long)E_rows);
+  if (norm) STEM_TRY(check_norm(c, who, *norm));
+  const int64_t d = c->desc.d_model, F = c->desc.d_ff, rows = stem_qfloat_rows(T, groups);
+  STEM_TRY(check_form(c, who, rows, std::max(d, F)));
+  STEM_TRY(check_form(c, who, F, d));
+  STEM_TRY(check_form(c, who, d, F));
+  STEM_TRY(check_groups(c, who, offsets, groups));
+  const size_t xb = (size_t)(T * d) * 2;
+  STEM_TRY(check_buffers(c, who, {{x, xb}, {residual, xb}}, {{y, xb}}, true));
+  STEM_TRY(check_buffers(c, who, {{gate_q, (size_t)groups * stem_qfloat_form(F, d)}, {down_q, (size_t)groups * stem_qfloat_form(d, F)},
+                                  {norm ? norm->weight : nullptr, (size_t)d * 2}, {E, (size_t)(E_rows * F) * 2}}, {{y, xb}}, false));
+  STEM_TRY(check_words(c, who, {ids}));
+  STEM_TRY(check_apart(c, who, {{ids, (size_t)T * 4}, {offsets, (size_t)(groups + 1) * 4}}, {{y, xb}}));
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  const QfloatGroups g = {offsets, groups, (int)T};
+  const Form f = form(c->qfloat_x, rows, d), h = form(c->qfloat_h, rows, F);
+  HIP_TRY(c, rows_form(c, x, g, d, norm, f, s));
+  QfloatGemmArgs a = gemm_args(c, f, form(gate_q, F, d), stem_qfloat_form(F, d), T, F, d, g);
+  a.hq = h.q; a.hs = h.scale;
+  a.ids = ids; a.E = static_cast<const bf16_t*>(E); a.E_rows = (int)E_rows; a.flag = c->flag;
+  HIP_TRY(c, stem_qfloat_gemm_launch(c, K_QFLOAT_GATE, QFLOAT_HIDDEN, a, s));
+  a = gemm_args(c, h, form(down_q, d, F), stem_qfloat_form(d, F), T, d, F, g);
+  a.y = static_cast<bf16_t*>(y); a.residual = static_cast<const bf16_t*>(residual);
+  HIP_TRY(c, stem_qfloat_gemm_launch(c, K_QFLOAT_LINEAR, QFLOAT_BF16, a, s));
+  return STEM_OK;
+}
+
+}  // extern "C"

@@ -1,0 +1,514 @@
+// 8-bit floating point MFMA products for gfx950: C[m,n] = sum_k a_mk b_nk of two forms (qfloat.h), the scales of their blocks of 128 multiplied in by
+// the matrix instruction.
+//
+// A weight gradient's products are of bf16 values (qfloat.h says why), in blocks of the same bytes, and go through the same loops with the bf16 instruction.
+//
+// A form's blocks lie in memory as the instruction takes them, so a tile of an operand is 4 KB for each 32 rows and 128 k, in a row; it goes to LDS as it
+// is (buffer_load ... lds), a fragment is the 32 bytes of two blocks at 16 x lane: no swizzle, no bank conflict.  The scales of a K tile are a word a
+// lane for each 128 rows of an operand, which goes straight to a register some K tiles ahead.
+#include <algorithm>
+#include <utility>
+
+#include "qfloat.h"
+
+typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8_t;
+typedef __attribute__((ext_vector_type(4))) int i32x4_t;
+typedef __attribute__((ext_vector_type(8))) int i32x8_t;
+typedef __attribute__((ext_vector_type(16))) float f32x16_t;
+typedef __attribute__((ext_vector_type(4))) float f32x4_t;
+typedef __attribute__((ext_vector_type(4))) uint32_t u32x4_t;
+typedef __attribute__((ext_vector_type(2))) uint32_t u32x2_t;
+typedef __attribute__((address_space(3))) void* lds_ptr_t;
+typedef __amdgpu_buffer_rsrc_t rsrc_t;
+
+namespace {
+
+constexpr uint32_t OOB = 0x80000000u;   // a buffer offset beyond any operand: reads as zero, is not stored
+constexpr int SC1 = 16;                 // cache policy bit of the buffer instructions: device scope
+constexpr int MAX_SLICES = 4;
+
+__device__ __forceinline__ float sigmoidf_fast(float z) { return __builtin_amdgcn_rcpf(1.0f + __expf(-z)); }
+__device__ __forceinline__ void lds_dma_16(rsrc_t rs, char* lds_dst, uint32_t off, int soff) {
+  __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (lds_ptr_t)lds_dst, 16, off, soff, 0, 0);
+}
+__device__ __forceinline__ rsrc_t resource(const void* p, int64_t bytes) {
+  return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(p), 0, (int)bytes, 0x00020000);
+}
+// 16 bytes to a buffer, all of the address in the vector offset (with a scalar register as the other one the compiler has let the next vector
+// instruction write the data's registers)
+template <int POLICY = 0>
+__device__ __forceinline__ void store_16(u32x4_t v, rsrc_t r, uint32_t off) {
+  __builtin_amdgcn_raw_buffer_store_b128(v, r, off, 0, POLICY);
+}
+__device__ __forceinline__ void in_order() {   // of LDS, within the wavefront
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
+__device__ __forceinline__ i32x8_t join(i32x4_t lo, i32x4_t hi) { return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7); }
+__device__ __forceinline__ f32x16_t mma_bf16(i32x8_t a, i32x8_t b, f32x16_t c) {   // 32 k
+  c = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, __builtin_shufflevector(a, a, 0, 1, 2, 3)),
+                                              __builtin_bit_cast(bf16x8_t, __builtin_shufflevector(b, b, 0, 1, 2, 3)), c, 0, 0, 0);
+  return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, __builtin_shufflevector(a, a, 4, 5, 6, 7)),
+                                                 __builtin_bit_cast(bf16x8_t, __builtin_shufflevector(b, b, 4, 5, 6, 7)), c, 0, 0, 0);
+}
+// 32 channels (a) x 32 tokens (b) x 64 k; the scales are byte A and byte B of their words
+template <int A, int B>
+__device__ __forceinline__ f32x16_t mma(i32x8_t a, i32x8_t b, f32x16_t c, uint32_t sa, uint32_t sb) {
+  return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a, b, c, 0, 0, A, (int)sa, B, (int)sb);
+}
+
+template <class F, int... U>
+__device__ __forceinline__ void each(F f, std::integer_sequence<int, U...>) { (f(std::integral_constant<int, U>{}), ...); }
+
+// Workgroup -> tile: the workgroups of an XCD take a contiguous run of tiles, walked in bands of 4 row tiles.
+__device__ __forceinline__ void tile_of(int b, int nb, int ntm, int ntn, int& tm, int& tn) {
+  const int q = nb >> 3, r = nb & 7, xcd = b & 7;
+  const int L = xcd * q + (xcd < r ? xcd : r) + (b >> 3);
+  const int per = 4 * ntn, group = L / per, first = group * 4, rows = ntm - first < 4 ? ntm - first : 4, in = L - group * per;
+  tm = first + in % rows;
+  tn = in / rows;
+}
+
+// What a workgroup computes
+struct Work {
+  int m0, rows;        // first row of the output, and how many there are from it on (in the group)
+  int pa;              // the same in the form of A
+  int n0;
+  int k0, nk;          // K tiles
+  int group;
+  int tile, tiles, slice;   // of the output, of K slices
+};
+template <int TM, int TN, bool BY_K>
+__device__ __forceinline__ bool find_work(const QfloatGemmArgs& p, int lane, Work& w) {
+  const int ntn = (p.N + TN - 1) / TN, nk_all = p.K / 128;
+  int b = blockIdx.x;
+  w.slice = 0; w.k0 = 0; w.nk = nk_all;
+  int tm, tn;
+  if constexpr (BY_K) {                                     // all of the output for each group of K
+    const int ntm = (p.M + TM - 1) / TM;
+    w.tiles = ntm * ntn;
+    const int part = b / w.tiles;
+    w.group = p.groups.offsets ? part : 0;
+    b -= part * w.tiles;
+    tile_of(b, w.tiles, ntm, ntn, tm, tn);
+    w.m0 = w.pa = tm * TM;
+    w.rows = p.M - w.m0;
+    if (p.groups.offsets) {
+      int k0 = 0, nk = 0;
+      qfloat_scan<128>(p.groups, lane, [&](int i, int, int rows, int, int, int padded) {
+        const uint64_t mine = __ballot(i == w.group);
+        if (!mine) return false;
+        const int l = __builtin_ctzll(mine);
+        k0 = __builtin_amdgcn_readlane(padded, l) / 64;     // (bf16: 64 rows a K tile)
+        nk = (__builtin_amdgcn_readlane(rows, l) + 63) / 64;
+        return true;
+      });
+      w.k0 = k0; w.nk = nk;
+    } else {
+      w.slice = part;
+    }
+  } else if (p.groups.offsets) {
+    w.tiles = qfloat_tiles<TM>(p.groups, lane) * ntn;
+    if (b >= w.tiles) return false;
+    tile_of(b, w.tiles, w.tiles / ntn, ntn, tm, tn);
+    QfloatTile t;
+    if (!qfloat_tile<TM>(p.groups, tm, lane, t)) return false;
+    w.group = t.group; w.m0 = t.row; w.rows = t.rows; w.pa = t.padded;
+  } else {
+    const int ntm = (p.M + TM - 1) / TM;
+    w.tiles = ntm * ntn;
+    w.slice = b / w.tiles;
+    b -= w.slice * w.tiles;
+    tile_of(b, w.tiles, ntm, ntn, tm, tn);
+    w.group = 0;
+    w.m0 = w.pa = tm * TM;
+    w.rows = p.M - w.m0;
+  }
+  w.tile = tm * ntn + tn;
+  w.n0 = tn * TN;
+  if (p.ksplit > 1) {
+    const int per = (nk_all + p.ksplit - 1) / p.ksplit;
+    w.k0 = w.slice * per;
+    w.nk = nk_all - w.k0 < per ? nk_all - w.k0 : per;
+  }
+  return true;
+}
+
+// The operand tiles of a workgroup: EDGE rows x 128 k, LOADS loads of 1 KB for each of LOADERS wavefronts
+template <int EDGE, int LOADERS>
+struct Loader {
+  static constexpr int LOADS = EDGE * 128 / 1024 / LOADERS;
+  rsrc_t r;
+  uint32_t off[(LOADS + 3) / 4];   // of the 32-row groups this wavefront loads from
+  // rows from row0 on, `rows` of them
+  __device__ __forceinline__ void init(const uint8_t* p, int64_t bytes, int rows, int K, int row0, int wave, int lane) {
+    r = resource(p, bytes);
+#pragma unroll
+    for (int i = 0; i < (LOADS + 3) / 4; ++i) {
+      const int group = (wave * LOADS + i * 4) / 4;
+      off[i] = group * 32 < rows ? (uint32_t)((row0 + group * 32) * K + lane * 16) : OOB;
+    }
+  }
+  // load i of the K tile at byte `k` of a group
+  __device__ __forceinline__ void issue(int i, char* tile, int wave, int k) const {
+    const int piece = wave * LOADS + i;
+    lds_dma_16(r, tile + piece * 1024, off[LOADS < 4 ? 0 : i / 4], k + (piece & 3) * 1024);
+  }
+};
+
+// The scale words of ROWS rows from `row` on (within 128), one K tile after another; byte 0 is the first 32 rows'
+struct Scales {
+  rsrc_t r;
+  uint32_t off;
+  int shift;
+  __device__ __forceinline__ void init(const uint8_t* p, int64_t bytes, int row, int nkb, int lane) {
+    r = resource(p, bytes);
+    off = (uint32_t)(((row >> 7) * nkb * 32 + (lane & 31)) * 4);
+    shift = (row >> 5 & 3) * 8;
+  }
+  __device__ __forceinline__ uint32_t load(int kt) const { return __builtin_amdgcn_raw_buffer_load_b32(r, off, kt * 128, 0); }
+};
+
+// ---- epilogue: a wavefront's 32 MI x 32 NJ results, 32 rows at a time through LDS ------------------------------------------------------
+// acc[i][j]: row block i, column block j; a lane holds row lane & 31 and columns 8 g + 4 (lane >> 5) + 0..3 of each.
+template <int MI, int NJ, bool F32>
+struct Output {
+  static constexpr int COLS = 32 * NJ, PITCH = COLS + 4;       // of a staged row, in words
+  static constexpr int BYTES = 32 * PITCH * 4;                 // of LDS, for each wavefront
+  static constexpr int V = F32 ? 4 : 8, LPR = COLS / V, RPP = 64 / LPR, PASSES = 32 / RPP;
+
+  // out: row m0, column n0 of it; rows and cols: how many there are
+  static __device__ __forceinline__ void run(const QfloatGemmArgs& p, const f32x16_t (&acc)[MI][NJ], char* stg, int64_t m0, int n0, int rows, int64_t base, int lane) {
+    const int lim = p.N - n0;
+    if (rows <= 0 || lim <= 0) return;
+    float* const st = reinterpret_cast<float*>(stg);
+    const int srow = lane / LPR, scol = (lane % LPR) * V, left = lim - scol;
+    const int64_t at = base + m0 * p.N + n0 + scol;
+#pragma unroll
+    for (int i = 0; i < MI; ++i) {
+      if (i * 32 >= rows) return;
+#pragma unroll
+      for (int j = 0; j < NJ; ++j)
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+          const f32x4_t w = {acc[i][j][4 * g], acc[i][j][4 * g + 1], acc[i][j][4 * g + 2], acc[i][j][4 * g + 3]};
+          *reinterpret_cast<f32x4_t*>(st + (lane & 31) * PITCH + j * 32 + g * 8 + (lane >> 5) * 4) = w;
+        }
+      in_order();
+#pragma unroll
+      for (int pass = 0; pass < PASSES; ++pass) {
+        const int r = i * 32 + pass * RPP + srow;
+        float z[V];
+        __builtin_memcpy(z, st + (pass * RPP + srow) * PITCH + scol, sizeof z);
+        if (r >= rows) continue;
+        const int64_t to = at + (int64_t)r * p.N;
+        if (left >= V) {
+          if constexpr (F32) {
+            if (p.accumulate) {
+              float c[4];
+              __builtin_memcpy(c, p.c + to, 16);
+#pragma unroll
+              for (int q = 0; q < 4; ++q) z[q] += c[q];
+            }
+            __builtin_memcpy(p.c + to, z, 16);
+          } else {
+            u32x4_t v = {};
+            if (p.residual) __builtin_memcpy(&v, p.residual + to, 16);
+            bf16x8_t o;
+#pragma unroll
+            for (int q = 0; q < 8; ++q) o[q] = (__bf16)(z[q] + __uint_as_float(q & 1 ? v[q >> 1] & 0xffff0000u : v[q >> 1] << 16));
+            __builtin_memcpy(p.y + to, &o, 16);
+          }
+        } else {
+#pragma unroll
+          for (int q = 0; q < V; ++q)
+            if (q < left) {
+              if constexpr (F32) p.c[to + q] = p.accumulate ? p.c[to + q] + z[q] : z[q];
+              else p.y[to + q] = __builtin_bit_cast(uint16_t, (__bf16)(z[q] + (p.residual ? __uint_as_float((uint32_t)p.residual[to + q] << 16) : 0.f)));
+            }
+        }
+      }
+      in_order();   // all have read the rows before they are staged over
+      __builtin_amdgcn_sched_barrier(0);
+    }
+  }
+};
+
+// ---- epilogue of the gate product: the form of SiLU(z) * E[ids] ----------------------------------------------------------------------------
+// A wavefront has 128 channels, a block of each of its tokens: the magnitude is over a lane's registers and one other lane's, and the
+// values go to the next product's operand from here; nothing is rounded before they are.  The table rows are what moves: they go to LDS as they
+// are gathered, 16 bytes a lane, chunk c of row r at chunk c ^ r % 16 so that 16 rows' reads fall into 16 chunk columns.
+template <int MI>
+struct Hidden {
+  static constexpr int NJ = 4, CH = 16;
+  static constexpr int BYTES = 32 * MI * CH * 16;              // of LDS, for each wavefront
+  static __device__ __forceinline__ void run(const QfloatGemmArgs& p, f32x16_t (&acc)[MI][NJ], const int (&row_id)[(MI + 1) / 2], char* lds, int pa, int n0,
+                                             int rows, int lane) {
+    if (rows <= 0 || n0 >= p.N) return;
+#pragma unroll
+    for (int q = 0; q < MI * CH / 2; ++q) {
+      const int r = q * 4 + lane / CH, col = n0 + ((lane % CH) ^ (r & 15)) * 8;
+      const int id = __builtin_amdgcn_ds_bpermute((r & 63) * 4, row_id[(q * 4) >> 6]);
+      const bf16_t* const at = p.E + (size_t)id * p.N + (col < p.N ? col : 0);
+      __builtin_amdgcn_global_load_lds(const_cast<bf16_t*>(at), (lds_ptr_t)(lds + q * 1024), 16, 0, 0);
+    }
+    const int pitch = (p.N + 127) / 128 * 128, nkb = pitch / 128;
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+#pragma unroll
+    for (int i = 0; i < MI; ++i) {
+      const int m = i * 32 + (lane & 31);
+      uint32_t top = 0;
+#pragma unroll
+      for (int t = 0; t < 4 * NJ; ++t) {                       // 8 channels a step
+        const int j = t >> 2, g = t & 3;
+        const u32x2_t e = *reinterpret_cast<const u32x2_t*>(lds + m * (CH * 16) + ((t ^ (m & 15)) << 4) + (lane >> 5) * 8);
+        const float u[4] = {__uint_as_float(e[0] << 16), __uint_as_float(e[0] & 0xffff0000u), __uint_as_float(e[1] << 16), __uint_as_float(e[1] & 0xffff0000u)};
+        const bool inside = n0 + 32 * j < p.N;                 // d_ff is a multiple of 64; what is behind it counts as zero
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          const float z = acc[i][j][4 * g + q], h = inside ? z * sigmoidf_fast(z) * u[q] : 0.f;
+          acc[i][j][4 * g + q] = h;
+          top = max(top, qfloat_magnitude(h));
+        }
+        __builtin_amdgcn_sched_barrier(0);                     // (all steps' reads at once would not fit the registers)
+      }
+      const auto both = __builtin_amdgcn_permlane32_swap(top, top, false, false);
+      const QfloatScale s = qfloat_scale(max((uint32_t)both[0], (uint32_t)both[1]));
+      if (i * 32 >= rows) return;                              // (the next rows of the form are another group's)
+      uint8_t* const out = p.hq + ((int64_t)((pa >> 5) + i) * (pitch / 32) + (n0 >> 5)) * 1024 + lane * 16;
+#pragma unroll
+      for (int j = 0; j < NJ; ++j) {
+        uint32_t w[4];
+#pragma unroll
+        for (int g = 0; g < 4; ++g)
+          w[g] = qfloat_four(acc[i][j][4 * g] * s.inv, acc[i][j][4 * g + 1] * s.inv, acc[i][j][4 * g + 2] * s.inv, acc[i][j][4 * g + 3] * s.inv);
+        // halves of the lanes have halves of 8 channels: they exchange, and have 16 in a row
+        const auto lo = __builtin_amdgcn_permlane32_swap(w[0], w[2], false, false), hi = __builtin_amdgcn_permlane32_swap(w[1], w[3], false, false);
+        *reinterpret_cast<u32x4_t*>(out + j * 1024) = u32x4_t{(uint32_t)lo[0], (uint32_t)lo[1], (uint32_t)hi[0], (uint32_t)hi[1]};
+      }
+      if (lane < 32) p.hs[qfloat_scale_at(pa + m, n0 >> 7, nkb)] = (uint8_t)s.byte;
+    }
+  }
+};
+
+// ids of the table rows of a wavefront's tokens, lane l having rows l and 64 + l
+template <int MI>
+__device__ __forceinline__ void load_ids(const QfloatGemmArgs& p, int m0, int rows, int lane, int (&id)[(MI + 1) / 2]) {
+#pragma unroll
+  for (int h = 0; h < (MI + 1) / 2; ++h) {
+    const int at = h * 64 + lane;
+    int v = p.ids[m0 + (at < rows ? at : rows - 1)];   // (none: the last row of the group)
+    if ((unsigned)v >= (unsigned)p.E_rows) {   // reported to the host, clamped so no access leaves the table
+      *p.flag = 1;
+      v = v < 0 ? 0 : p.E_rows - 1;
+    }
+    id[h] = v;
+  }
+}
+
+// ---- tiles with wavefronts that load: STAGES whole K tiles in LDS ----------------------------------------------------------------------
+template <int MI_, int NJ_, int WM_, int WN_, int STAGES_, int LW_>
+struct Tiling {
+  static constexpr int MI = MI_, NJ = NJ_, WM = WM_, WN = WN_, STAGES = STAGES_, LW = LW_, WAVES = WM * WN;
+  static constexpr int TM = 32 * MI * WM, TN = 32 * NJ * WN;
+  static constexpr int A_BYTES = TM * 128, STAGE = (TM + TN) * 128;
+};
+
+// Split K (few tiles): every slice writes its sums in the lanes' layout and takes a ticket of its tile; the workgroup that takes the last one adds them in
+// the order of the slices, so that the result does not depend on who is last.  Nobody waits for anybody.  The slices run on different XCDs, whose L2s
+// don't see each other's lines: stores and loads carry the device scope bit, and a wavefront's stores are there for the device when they
+// leave its counter, which is before the workgroup's ticket is taken.  `at`: this wavefront's place among all of a slice's, `stride` apart.
+template <int MI, int NJ>
+__device__ __forceinline__ bool last_slice(const QfloatGemmArgs& p, f32x16_t (&acc)[MI][NJ], char* smem, int at, int stride, int slice, int tile, int lane) {
+  constexpr int BYTES = MI * NJ * 4096, N = MI * NJ * 4;
+  const rsrc_t rw = resource(p.ws, (int64_t)p.ksplit * stride * BYTES);
+#pragma unroll
+  for (int k = 0; k < N; ++k) {
+    const f32x16_t& a = acc[k / 4 / NJ][k / 4 % NJ];
+    const f32x4_t v = {a[4 * (k % 4)], a[4 * (k % 4) + 1], a[4 * (k % 4) + 2], a[4 * (k % 4) + 3]};
+    store_16<SC1>(__builtin_bit_cast(u32x4_t, v), rw, (uint32_t)((at + slice * stride) * BYTES + lane * 16) + k * 1024u);
+  }
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+  __syncthreads();
+  int* const ticket = reinterpret_cast<int*>(smem);
+  if (threadIdx.x == 0) *ticket = __hip_atomic_fetch_add(p.tickets + tile, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  __syncthreads();
+  const bool last = *ticket == p.ksplit - 1;
+  if (!last) return false;
+  if (threadIdx.x == 0) __hip_atomic_store(p.tickets + tile, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);   // for the next launch
+  asm volatile("" ::: "memory");
+#pragma unroll
+  for (int i = 0; i < MI; ++i)
+#pragma unroll
+    for (int j = 0; j < NJ; ++j) acc[i][j] = f32x16_t{};
+  for (int s = 0; s < p.ksplit; ++s) {
+    f32x4_t v[N];
+#pragma unroll
+    for (int k = 0; k < N; ++k)
+      v[k] = __builtin_bit_cast(f32x4_t, __builtin_amdgcn_raw_buffer_load_b128(rw, (uint32_t)(lane * 16), (at + s * stride) * BYTES + k * 1024, SC1));
+#pragma unroll
+    for (int k = 0; k < N; ++k)
+#pragma unroll
+      for (int q = 0; q < 4; ++q) acc[k / 4 / NJ][k / 4 % NJ][4 * (k % 4) + q] += v[k][q];
+  }
+  __syncthreads();   // the ticket has been read: LDS may be used again
+  return true;
+}
+
+template <QfloatOut OUT, class C>
+__global__ __launch_bounds__((C::WAVES + C::LW) * 64) void tile_kernel(QfloatGemmArgs p) {
+  constexpr int MI = C::MI, NJ = C::NJ, S = C::STAGES, STAGE = C::STAGE;
+  typedef Output<MI, NJ, OUT == QFLOAT_F32> Out;
+  typedef Hidden<MI> Hid;
+  constexpr int EPI = C::WAVES * (OUT == QFLOAT_HIDDEN ? Hid::BYTES : Out::BYTES);
+  constexpr int LDS = S * STAGE > EPI ? S * STAGE : EPI;
+  __shared__ __attribute__((aligned(16))) char smem[LDS];
+  const int lane = threadIdx.x & 63, wave_id = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const bool load_wave = wave_id >= C::WAVES;
+  const int wave = load_wave ? wave_id - C::WAVES : wave_id, wm = wave / C::WN, wn = wave % C::WN;
+  Work w;
+  constexpr bool HALF = OUT == QFLOAT_F32;
+  if (!find_work<C::TM, C::TN, HALF>(p, lane, w)) return;
+  const int nk = w.nk, k0 = w.k0, nkb = p.K / 128;
+  const int64_t b_bytes = stem_qfloat_pitch(p.N) * p.K;
+  const uint8_t *const B = p.B + (HALF ? 0 : w.group * p.stride_b), *const sb = p.sb + (HALF ? 0 : w.group * p.stride_b);
+  if (load_wave) {
+    Loader<C::TM, C::LW> la;
+    Loader<C::TN, C::LW> lb;
+    constexpr int LOADS = la.LOADS + lb.LOADS;
+    la.init(p.A, p.a_bytes, w.rows, p.K, w.pa, wave, lane);
+    lb.init(B, b_bytes, p.N - w.n0, p.K, w.n0, wave, lane);
+    int k = k0 * 4096, left = nk;
+    auto request = [&](const int st) __attribute__((always_inline)) {
+      if (left <= 0) { la.r = resource(p.A, 0); lb.r = resource(p.A, 0); }
+#pragma unroll
+      for (int q = 0; q < la.LOADS; ++q) la.issue(q, smem + st * STAGE, wave, k);
+#pragma unroll
+      for (int q = 0; q < lb.LOADS; ++q) lb.issue(q, smem + st * STAGE + C::A_BYTES, wave, k);
+      k += 4096;
+      --left;
+    };
+#pragma unroll
+    for (int st = 0; st < S; ++st) request(st);
+    asm volatile("s_waitcnt vmcnt(%0)" ::"n"((S - 1) * LOADS) : "memory");
+    __builtin_amdgcn_s_barrier();
+    auto load_iteration = [&](const int st) __attribute__((always_inline)) {
+      asm volatile("s_waitcnt vmcnt(%0)" ::"n"((S - 2) * LOADS) : "memory");
+      __builtin_amdgcn_s_barrier();
+      __builtin_amdgcn_sched_barrier(0);
+      request(st);
+      __builtin_amdgcn_sched_barrier(0);
+    };
+    int kt = 0;
+    for (; kt + S <= nk; kt += S) {
+#pragma unroll
+      for (int st = 0; st < S; ++st) load_iteration(st);
+    }
+#pragma unroll
+    for (int st = 0; st < S - 1; ++st)
+      if (kt + st < nk) load_iteration(st);
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // nothing lands in LDS once the epilogue uses it
+    __syncthreads();
+    return;                                            // (barriers are of the wavefronts that are left)
+  }
+  int id[(MI + 1) / 2];
+  if (OUT == QFLOAT_HIDDEN) load_ids<MI>(p, w.m0 + wm * MI * 32, w.rows - wm * MI * 32, lane, id);
+  Scales ca, cb;
+  uint32_t sca[S], scb[S];
+  if constexpr (!HALF) {
+    ca.init(p.sa, p.a_bytes / 128, w.pa + wm * MI * 32, nkb, lane);
+    cb.init(sb, b_bytes / 128, w.n0 + wn * NJ * 32, nkb, lane);
+#pragma unroll
+    for (int st = 0; st < S; ++st) {
+      sca[st] = ca.load(k0 + st);
+      scb[st] = cb.load(k0 + st);
+    }
+  }
+  f32x16_t acc[MI][NJ];
+#pragma unroll
+  for (int i = 0; i < MI; ++i)
+#pragma unroll
+    for (int j = 0; j < NJ; ++j) acc[i][j] = f32x16_t{};
+  i32x8_t xa[MI], xb[NJ], ya[MI], yb[NJ];
+  const char* const fa = smem + wm * MI * 4096 + lane * 16;
+  const char* const fb = smem + C::A_BYTES + wn * NJ * 4096 + lane * 16;
+  constexpr int NFRAG = MI + NJ, NMMA = MI * NJ;
+  auto frag = [&](const char* f) __attribute__((always_inline)) {
+    return join(*reinterpret_cast<const i32x4_t*>(f), *reinterpret_cast<const i32x4_t*>(f + 1024));
+  };
+  auto read = [&](int st, int ks, int q, i32x8_t(&a)[MI], i32x8_t(&b)[NJ]) __attribute__((always_inline)) {   // order a0, b0, b1, .., a1, ..
+    if (q == 0) a[0] = frag(fa + st * STAGE + ks * 2048);
+    else if (q <= NJ) b[q - 1] = frag(fb + st * STAGE + (q - 1) * 4096 + ks * 2048);
+    else a[q - NJ] = frag(fa + st * STAGE + (q - NJ) * 4096 + ks * 2048);
+  };
+  auto kstep = [&](int st, int ks_next, i32x8_t(&a)[MI], i32x8_t(&b)[NJ], i32x8_t(&na)[MI], i32x8_t(&nb)[NJ], uint32_t sa, uint32_t sb) __attribute__((always_inline)) {
+    auto one = [&](auto U) __attribute__((always_inline)) {
+      constexpr int u = decltype(U)::value;
+#pragma unroll
+      for (int q = u * NFRAG / NMMA; q < (u + 1) * NFRAG / NMMA; ++q) read(st, ks_next, q, na, nb);
+      if constexpr (HALF) acc[u / NJ][u % NJ] = mma_bf16(b[u % NJ], a[u / NJ], acc[u / NJ][u % NJ]);
+      else acc[u / NJ][u % NJ] = mma<u % NJ, u / NJ>(b[u % NJ], a[u / NJ], acc[u / NJ][u % NJ], sb, sa);
+      __builtin_amdgcn_sched_barrier(0);
+    };
+    each(one, std::make_integer_sequence<int, NMMA>{});
+  };
+  __builtin_amdgcn_s_barrier();
+  __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+  for (int q = 0; q < NFRAG; ++q) read(0, 0, q, xa, xb);
+  // One barrier a K tile, before its last k-step: the load wavefronts have seen the next tile land, the others have read the last of this.
+  int kt = 0;
+  auto stage_iteration = [&](const int st) __attribute__((always_inline)) {
+    uint32_t sa = 0, sb = 0;
+    if constexpr (!HALF) {
+      sa = sca[st] >> ca.shift;
+      sb = scb[st] >> cb.shift;
+      sca[st] = ca.load(k0 + kt + st + S);
+      scb[st] = cb.load(k0 + kt + st + S);
+    }
+    kstep(st, 1, xa, xb, ya, yb, sa, sb);
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    __builtin_amdgcn_s_barrier();
+    __builtin_amdgcn_sched_barrier(0);
+    kstep((st + 1) % S, 0, ya, yb, xa, xb, sa, sb);
+  };
+  for (; kt + S <= nk; kt += S) {
+#pragma unroll
+    for (int st = 0; st < S; ++st) stage_iteration(st);
+  }
+#pragma unroll
+  for (int st = 0; st < S - 1; ++st)
+    if (kt + st < nk) stage_iteration(st);
+  __syncthreads();
+  if constexpr (OUT != QFLOAT_HIDDEN)
+    if (p.ksplit > 1 && !last_slice<MI, NJ>(p, acc, smem, w.tile * C::WAVES + wave, w.tiles * C::WAVES, w.slice, w.tile, lane)) return;
+  if constexpr (OUT == QFLOAT_HIDDEN) Hid::run(p, acc, id, smem + wave * Hid::BYTES, w.pa + wm * MI * 32, w.n0 + wn * NJ * 32, w.rows - wm * MI * 32, lane);
+  else Out::run(p, acc, smem + wave * Out::BYTES, w.m0 + wm * MI * 32, w.n0 + wn * NJ * 32, w.rows - wm * MI * 32, HALF ? (int64_t)w.group * p.M * p.N : 0, lane);
+}
+
+typedef Tiling<2, 2, 2, 2, 4, 4> Tile128;       // 128 x 128, 128 KB of LDS
+typedef Tiling<2, 1, 2, 2, 6, 4> Tile128x64;    // 144 KB
+typedef Tiling<1, 4, 4, 1, 4, 4> Hidden128;     // 128 x 128, a wavefront with whole blocks of 128 channels
+
+template <QfloatOut OUT, class C>
+hipError_t launch(const QfloatGemmArgs& a, hipStream_t s) {
+  const int64_t ntn = (a.N + C::TN - 1) / C::TN;
+  int64_t tiles;
+  if (OUT == QFLOAT_F32) tiles = (a.M + C::TM - 1) / C::TM * ntn * (a.groups.offsets ? a.groups.n : a.ksplit);
+  else if (a.groups.offsets) tiles = ((a.groups.T + C::TM - 1) / C::TM + std::min(a.groups.n, a.groups.T) - 1) * ntn;   // at most: each group may have a tile not full
+  else tiles = (a.M + C::TM - 1) / C::TM * ntn * a.ksplit;
+  tile_kernel<OUT, C><<<(unsigned)tiles, (C::WAVES + C::LW) * 64, 0, s>>>(a);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t stem_qfloat_gemm_launch(stem_ctx* ctx, int kid, QfloatOut out, const QfloatGemmArgs& p, hipStream_t s) {
+  ProfScope prof(ctx, kid, s);
+  QfloatGemmArgs a = p;
+  a.ksplit = 1;
+  if (out == QFLOAT_HIDDEN) return launch<QFLOAT_HIDDEN, Hidden128>(a, s);
+  if (out == QFLOAT_F32) return launch<QFLOAT_F32, Tile128>(a, s);
+  return launch<QFLOAT_BF16, Tile128>(a, s);
+}

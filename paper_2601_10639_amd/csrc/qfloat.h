@@ -1,0 +1,179 @@
+// Products in 8-bit floating point with a scale for each block of 128: layout, arguments and launches (qfloat.hip, gemm_qfloat.hip,
+// gemm_qfloat_decode.hip), called by their entry points (api_qfloat.hip).
+//
+// Sums.  The matrix instruction of this format adds eight products at a time, cut (towards zero) 13 binary digits below the largest of their exponents'
+// sums, and adds the result to its fp32 accumulator: measured, for normal values, 1.5e-5 of the result's norm whatever its length (instructions of 16, 64 and 128
+// k alike; the bf16 instruction: 1e-8).  Rounded to bf16, or to 8 bits again, an output does not know it.  An fp32 weight gradient would, whose sums go on over
+// steps; so that product is made of the bf16 values themselves, exact products and fp32 sums, and nothing of it is quantised.
+//
+// Numbers.  A block of 128 values v (1 x 128 of a row or a column, 128 x 128 of a matrix of weights) has a scale 2^e, e the least integer with max |v| <=
+// 448 2^e, at least -126, and the e4m3 values rne(v 2^-e).  v_mfma_scale_f32_32x32x64_f8f6f4 takes such exponents, a byte e + 127 for each row and
+// 32 k, and multiplies by them itself: a product of blocks needs no arithmetic but the matrix units', and sums stay in their fp32 accumulators
+// over all of K.  (A power of two costs a floating point format nothing but up to one of its 15 binades above the subnormal numbers; a scale that is
+// no power of two would cost 16 FMAs for every two matrix instructions.)
+// The magnitude of a block is that of its finite values.  NaN and infinities become NaN, and what they meet becomes NaN by itself.
+//
+// Layout.  The form of a matrix [rows, K] is blocks of 32 rows x 32 k, 1 KB each, that follow each other along k: chunk h of row r, 16 bytes of k = 16 h ..,
+// at (32 h + r) * 16.  Rows and k are padded to multiples of 128; what is behind K is zero, what is behind the rows is anything and reaches no output.
+// Two blocks side by side are an operand of the instruction, 32 bytes a lane: the order in which it takes the 64 k is the same in both
+// operands, and the scale is the same over all of a block of 128.  The scales follow the elements: for 128 rows and 128 k 32 words, word i with the
+// bytes of rows i, 32 + i, 64 + i, 96 + i, so that a wavefront of 128 rows has all it needs for 128 k in a word a lane.
+//
+// Groups.  Rows offsets[g] .. offsets[g + 1] belong to group g and its weights.  Offsets are taken as they would be if each were at least those
+// before it and at most T; so no two groups share a row whatever they hold.  In a form every group's rows begin at a multiple of 128.
+#pragma once
+#include "stem_internal.h"
+
+__host__ __device__ inline int64_t stem_qfloat_pitch(int64_t K) { return (K + 127) / 128 * 128; }
+inline int64_t stem_qfloat_size(int64_t rows, int64_t K) { return stem_qfloat_pitch(rows) * stem_qfloat_pitch(K); }          // elements
+inline int64_t stem_qfloat_form(int64_t rows, int64_t K) { return stem_qfloat_size(rows, K) / 128 * 129; }                   // and scales
+// padded rows of T rows in groups: each but one may need 127 more than its own
+inline int64_t stem_qfloat_rows(int64_t T, int64_t groups) { return stem_qfloat_pitch(T) + 128 * ((groups < T ? groups : T < 1 ? 1 : T) - 1); }
+
+struct QfloatGroups {
+  const int32_t* offsets;   // [n + 1] device; null: one group of all rows
+  int n, T;
+};
+
+// Rows of x, behind a norm, to the form
+struct QfloatRowsArgs {
+  const bf16_t* x;          // [T, K]
+  QfloatGroups groups;
+  int K;
+  stem_norm norm;
+  uint8_t *q, *scale;
+};
+hipError_t stem_qfloat_rows_launch(stem_ctx* ctx, const QfloatRowsArgs& a, hipStream_t s);
+
+// Weights x [rows, cols] with one scale for 128 x 128: their form, that of their transpose, or both
+struct QfloatTilesArgs {
+  const bf16_t* x;
+  int rows, cols;
+  int batch;                // matrices, one behind another
+  uint8_t *q, *qt;          // either may be null
+};
+hipError_t stem_qfloat_weights_launch(stem_ctx* ctx, const QfloatTilesArgs& a, hipStream_t s);
+
+// The transpose of x [T, cols] in bf16, as a weight gradient's product reads it: blocks of 32 columns x 16 rows, 1 KB, chunk h of column c, rows 8 h .., at
+// (32 h + c) * 16, one behind another along the rows; each group's rows begin at a multiple of 128 and are followed by zeros up to the next multiple of 64
+// at least.  And the form of x besides.
+struct QfloatTurnArgs {
+  const bf16_t* x;
+  QfloatGroups groups;
+  int cols;
+  uint8_t* turned;
+  int pitch;                // bytes of a row of it
+  uint8_t *q, *scale;       // may be null
+};
+hipError_t stem_qfloat_turn_launch(stem_ctx* ctx, const QfloatTurnArgs& a, hipStream_t s);
+
+enum QfloatOut { QFLOAT_BF16 = 0, QFLOAT_F32, QFLOAT_HIDDEN };
+struct QfloatGemmArgs {
+  const uint8_t *A, *sa;    // [rows, K]: tokens; QFLOAT_F32: two operands of a weight gradient, turned, and no scales
+  const uint8_t *B, *sb;    // [N, K]: weights
+  int64_t a_bytes;          // of A's elements
+  int64_t stride_b;         // from one group's weights to the next's
+  int M, N, K;              // K: bytes of a row of both
+  QfloatGroups groups;      // of rows of A; QFLOAT_F32: of K
+  float* ws;                // room for K slices
+  int64_t ws_bytes;
+  int32_t* tickets;
+  int ksplit;               // by the launcher
+  bf16_t* y;                // QFLOAT_BF16: [M, N]
+  const bf16_t* residual;
+  float* c;                 // QFLOAT_F32: [groups][M, N]
+  int accumulate;
+  uint8_t *hq, *hs;         // QFLOAT_HIDDEN: the form of SiLU(product) * E[ids], [rows, N]
+  const int32_t* ids;
+  const bf16_t* E;
+  int E_rows;
+  int32_t* flag;
+};
+hipError_t stem_qfloat_gemm_launch(stem_ctx* ctx, int kid, QfloatOut out, const QfloatGemmArgs& a, hipStream_t s);
+
+#define QFLOAT_WS (256ll * 128 * 128 * 4)   // bytes: a product is cut into 256 workgroups at most
+
+// ---- device code ------------------------------------------------------------------------------------------------------------
+__device__ __forceinline__ int64_t qfloat_scale_at(int row, int kb, int nkb) { return ((int64_t)(row >> 7) * nkb + kb) * 128 + (row & 31) * 4 + (row >> 5 & 3); }
+
+// the bits of a magnitude; of no number's: 0
+__device__ __forceinline__ uint32_t qfloat_magnitude(float v) {
+  const uint32_t b = __float_as_uint(v) & 0x7fffffffu;
+  return b < 0x7f800000u ? b : 0u;
+}
+struct QfloatScale { uint32_t byte; float inv; };
+__device__ __forceinline__ QfloatScale qfloat_scale(uint32_t top) {   // 448 = 1.75 x 2^8
+  int e = (int)(top >> 23) - 127 - 8 + ((top & 0x7fffffu) > 0x600000u ? 1 : 0);
+  e = e < -126 ? -126 : e;
+  return {(uint32_t)(e + 127), __uint_as_float((uint32_t)(127 - e) << 23)};
+}
+__device__ __forceinline__ uint32_t qfloat_four(float a, float b, float c, float d) {
+  int w = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false);
+  w = __builtin_amdgcn_cvt_pk_fp8_f32(c, d, w, true);
+  return (uint32_t)w;
+}
+
+// ---- groups: every lane of a wavefront takes part -------------------------------------------------------------------------
+// f(group, first row, rows, tiles in front of its, its tiles, padded rows in front of its) for 64 groups at a time, a lane each; ends when f
+// says so (one answer for all lanes).  Returns the tiles of all groups that were seen.
+template <int TM, class F>
+__device__ __forceinline__ int qfloat_scan(const QfloatGroups& G, int lane, F f) {
+  auto at = [&](int i) __attribute__((always_inline)) {
+    const int v = G.offsets[i];
+    return v < 0 ? 0 : v > G.T ? G.T : v;
+  };
+  int last = at(0), tiles = 0, padded = 0;
+  for (int c = 0; c < G.n; c += 64) {
+    const int i = c + lane;
+    int hi = i < G.n ? at(i + 1) : 0;
+    hi = hi > last ? hi : last;
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+      const int up = __shfl_up(hi, d);
+      hi = lane >= d && up > hi ? up : hi;
+    }
+    int lo = __shfl_up(hi, 1);
+    if (lane == 0) lo = last;
+    const int rows = hi - lo, nt = (rows + TM - 1) / TM, np = (rows + 127) / 128;
+    int st = nt, sp = np;
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+      const int a = __shfl_up(st, d), b = __shfl_up(sp, d);
+      if (lane >= d) { st += a; sp += b; }
+    }
+    if (f(i, lo, rows, tiles + st - nt, nt, (padded + sp - np) * 128)) return tiles;
+    tiles += __builtin_amdgcn_readlane(st, 63);
+    padded += __builtin_amdgcn_readlane(sp, 63);
+    last = __builtin_amdgcn_readlane(hi, 63);
+  }
+  return tiles;
+}
+
+struct QfloatTile { int group, row, rows, padded; };   // first row, rows of the group from it on, its place in a form
+// Tile t of TM rows, the groups' tiles one behind another; false: there are not as many
+template <int TM>
+__device__ __forceinline__ bool qfloat_tile(const QfloatGroups& G, int t, int lane, QfloatTile& out) {
+  if (!G.offsets) {
+    out = {0, t * TM, G.T - t * TM, t * TM};
+    return t * TM < G.T;
+  }
+  bool found = false;
+  qfloat_scan<TM>(G, lane, [&](int i, int lo, int rows, int before, int nt, int padded) {
+    const uint64_t mine = __ballot(t >= before && t < before + nt);
+    if (!mine) return false;
+    const int l = __builtin_ctzll(mine), in = (t - __builtin_amdgcn_readlane(before, l)) * TM;
+    out.group = __builtin_amdgcn_readlane(i, l);
+    out.row = __builtin_amdgcn_readlane(lo, l) + in;
+    out.rows = __builtin_amdgcn_readlane(rows, l) - in;
+    out.padded = __builtin_amdgcn_readlane(padded, l) + in;
+    found = true;
+    return true;
+  });
+  return found;
+}
+// tiles of TM rows of all groups
+template <int TM>
+__device__ __forceinline__ int qfloat_tiles(const QfloatGroups& G, int lane) {
+  if (!G.offsets) return (G.T + TM - 1) / TM;
+  return qfloat_scan<TM>(G, lane, [](int, int, int, int, int, int) { return false; });
+}

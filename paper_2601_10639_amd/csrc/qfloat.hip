@@ -1,0 +1,296 @@
+// bf16 rows and tiles to 8-bit floating point with a scale for each block of 128 (qfloat.h).
+//
+// A block's scale depends on nothing but the block, so a kernel reads each value once: a row's 128 values are eight neighbouring lanes', a tile of
+// 128 x 128 is a workgroup's.  Bound by memory: 2 bytes read and 1 (or 2) written a value.
+#include "qfloat.h"
+#include "quant.h"   // chunks of a bf16 row
+
+typedef __attribute__((ext_vector_type(4))) uint32_t u32x4_t;
+
+namespace {
+
+template <int CTRL>
+__device__ __forceinline__ uint32_t dpp(uint32_t v) { return __builtin_amdgcn_update_dpp(0, v, CTRL, 0xf, 0xf, true); }
+__device__ __forceinline__ uint32_t max_of_eight(uint32_t v) {   // neighbouring lanes
+  v = max(v, dpp<0xb1>(v));    // quad_perm 1 0 3 2
+  v = max(v, dpp<0x4e>(v));    // quad_perm 2 3 0 1
+  return max(v, dpp<0x141>(v));   // row_half_mirror
+}
+template <int LPR>
+__device__ __forceinline__ float sum_row(float v, float* red) {
+#pragma unroll
+  for (int d = 1; d < (LPR < 64 ? LPR : 64); d <<= 1) v += __shfl_xor(v, d);
+  if (LPR > 64) {
+    __syncthreads();
+    if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
+    __syncthreads();
+    v = (red[0] + red[1]) + (red[2] + red[3]);
+  }
+  return v;
+}
+
+// ---- rows, with or without a norm ---------------------------------------------------------------------------------------------
+// LPR neighbouring lanes have a row (256: the workgroup), CPT chunks of 16 values each (0: as many as there are, read again for each use).
+template <int LPR, int CPT>
+__global__ __launch_bounds__(256) void rows_kernel(QfloatRowsArgs p) {
+  __shared__ float red[4];
+  constexpr int ROWS = 256 / LPR, HELD = CPT ? CPT : 1;
+  const int l = threadIdx.x % LPR, lane = threadIdx.x & 63;
+  const int row = blockIdx.x * ROWS + threadIdx.x / LPR;
+  const int chunks = (p.K + 127) / 128 * 8, nkb = chunks / 8;
+  const bool live = row < p.groups.T;
+  const bf16_t* const x = p.x + (int64_t)(live ? row : 0) * p.K;
+  auto fetch = [&](int t) __attribute__((always_inline)) {
+    const int c = t * LPR + l;
+    return live && c * 16 < p.K ? quant_load_chunk(x + c * 16, p.K - c * 16) : QuantChunk{};
+  };
+  QuantChunk raw[HELD] = {};
+  if constexpr (CPT > 0) {
+#pragma unroll
+    for (int t = 0; t < CPT; ++t)
+      if (t * LPR < chunks) raw[t] = fetch(t);
+  }
+  // its place in the form: the rows of a wavefront find theirs one after another
+  int place = live ? row : -1;
+  if (p.groups.offsets) {
+    place = -1;
+    qfloat_scan<128>(p.groups, lane, [&](int, int lo, int rows, int, int, int padded) {
+#pragma unroll
+      for (int h = 0; h < 64; h += (LPR < 64 ? LPR : 64)) {
+        const int r = __builtin_amdgcn_readlane(row, h);
+        const uint64_t mine = __ballot(r >= lo && r < lo + rows);
+        if (mine) {
+          const int at = __builtin_ctzll(mine);
+          if ((LPR < 64 ? lane / LPR * LPR : 0) == h) place = __builtin_amdgcn_readlane(padded, at) + r - __builtin_amdgcn_readlane(lo, at);
+        }
+      }
+      return false;
+    });
+  }
+  float v[HELD][16];
+  auto elements = [&](const QuantChunk& c, float (&u)[16]) __attribute__((always_inline)) {
+#pragma unroll
+    for (int q = 0; q < 16; ++q) u[q] = quant_element(c, q);
+  };
+  if constexpr (CPT > 0) {
+#pragma unroll
+    for (int t = 0; t < CPT; ++t) elements(raw[t], v[t]);
+  }
+  float mean = 0.f, r = 1.f;
+  const bool centred = p.norm.kind == STEM_NORM_LAYER, normed = p.norm.kind != STEM_NORM_NONE || p.norm.weight;
+  auto cut = [&](int t, float (&u)[16]) __attribute__((always_inline)) {   // zeros behind the row's end
+    const int left = p.K - (t * LPR + l) * 16;
+    if (left < 16)
+#pragma unroll
+      for (int q = 0; q < 16; ++q) u[q] = q < left ? u[q] : 0.f;
+  };
+  auto advance = [&](int stage, int t, float (&u)[16]) __attribute__((always_inline)) {   // 1: centred, 2: normed and weighted
+    if (stage == 1) {
+#pragma unroll
+      for (int q = 0; q < 16; ++q) u[q] -= mean;
+    } else {
+      const int at = t * LPR + l;
+#pragma unroll
+      for (int q = 0; q < 16; ++q) u[q] *= r;
+      if (p.norm.weight && at * 16 < p.K) {
+        const QuantChunk w = quant_load_chunk(static_cast<const bf16_t*>(p.norm.weight) + at * 16, p.K - at * 16);
+#pragma unroll
+        for (int q = 0; q < 16; ++q) u[q] *= quant_element(w, q);
+      }
+    }
+    cut(t, u);
+  };
+  auto each_step = [&](int stage, auto f) __attribute__((always_inline)) {
+    if constexpr (CPT > 0) {
+#pragma unroll
+      for (int t = 0; t < CPT; ++t)
+        if (t * LPR < chunks) {
+          if (stage == 1 && centred) advance(1, t, v[t]);
+          if (stage == 2 && normed) advance(2, t, v[t]);
+          f(t, v[t]);
+        }
+    } else {
+      for (int t = 0; t * LPR < chunks; ++t) {
+        elements(fetch(t), v[0]);
+        if (stage >= 1 && centred) advance(1, t, v[0]);
+        if (stage >= 2 && normed) advance(2, t, v[0]);
+        f(t, v[0]);
+      }
+    }
+  };
+  if (p.norm.kind != STEM_NORM_NONE) {
+    float s = 0.f;
+    if (centred) {
+      each_step(0, [&](int, float (&u)[16]) {
+#pragma unroll
+        for (int q = 0; q < 16; ++q) s += u[q];
+      });
+      mean = sum_row<LPR>(s, red) / (float)p.K;
+      s = 0.f;
+    }
+    each_step(1, [&](int, float (&u)[16]) {
+#pragma unroll
+      for (int q = 0; q < 16; ++q) s = __builtin_fmaf(u[q], u[q], s);
+    });
+    r = 1.0f / sqrtf(sum_row<LPR>(s, red) / (float)p.K + p.norm.eps);
+  }
+  uint8_t* const out = p.q + (int64_t)(place >> 5) * 32 * chunks * 16 + (place & 31) * 16;
+  each_step(2, [&](int t, float (&u)[16]) {
+    const int c = t * LPR + l;
+    uint32_t top = 0;
+#pragma unroll
+    for (int q = 0; q < 16; ++q) top = max(top, qfloat_magnitude(u[q]));
+    const QfloatScale s = qfloat_scale(max_of_eight(top));
+    uint32_t w[4];
+#pragma unroll
+    for (int q = 0; q < 4; ++q) w[q] = qfloat_four(u[4 * q] * s.inv, u[4 * q + 1] * s.inv, u[4 * q + 2] * s.inv, u[4 * q + 3] * s.inv);
+    if (c >= chunks || place < 0) return;
+    *reinterpret_cast<u32x4_t*>(out + (int64_t)(c >> 1) * 1024 + (c & 1) * 512) = u32x4_t{w[0], w[1], w[2], w[3]};
+    if ((c & 7) == 0) p.scale[qfloat_scale_at(place, c >> 3, nkb)] = (uint8_t)s.byte;
+  });
+}
+
+// ---- tiles of 128 x 128 -----------------------------------------------------------------------------------------------------------
+// Lane t of the workgroup has rows 4 (t / 8) .. + 3 and columns 16 (t % 8) .. + 15: a row's magnitudes are eight neighbouring lanes'.  Four rows of a
+// column are a word (8 bits) or two (bf16) of the transpose, which goes through LDS to lie as that form does.  Columns' words are a pitch apart that keeps
+// 16-byte pieces whole, and some more every 16 columns, so that the lanes' stores fall into different banks.
+__device__ __forceinline__ void load_tile(const bf16_t* x, int cols, int rows, int quad, int col, QuantChunk (&raw)[4]) {
+#pragma unroll
+  for (int r = 0; r < 4; ++r) {
+    const int in = quad * 4 + r;
+    raw[r] = in < rows && col < cols ? quant_load_chunk(x + (int64_t)in * cols + col, cols - col) : QuantChunk{};
+  }
+}
+// a lane's four rows of a form whose rows have nkb blocks
+__device__ __forceinline__ void store_rows(uint8_t* q, uint8_t* scale, int nkb, int row0, int kb, int c, const float (&v)[4][16], const QfloatScale (&s)[4]) {
+#pragma unroll
+  for (int r = 0; r < 4; ++r) {
+    const int row = row0 + r;
+    uint32_t w[4];
+#pragma unroll
+    for (int g = 0; g < 4; ++g) w[g] = qfloat_four(v[r][4 * g] * s[r].inv, v[r][4 * g + 1] * s[r].inv, v[r][4 * g + 2] * s[r].inv, v[r][4 * g + 3] * s[r].inv);
+    *reinterpret_cast<u32x4_t*>(q + ((int64_t)(row >> 5) * (nkb * 4) + (kb * 4 + (c >> 1))) * 1024 + (c & 1) * 512 + (row & 31) * 16) = u32x4_t{w[0], w[1], w[2], w[3]};
+    if (c == 0) scale[qfloat_scale_at(row, kb, nkb)] = (uint8_t)s[r].byte;
+  }
+}
+
+__global__ __launch_bounds__(256) void weights_kernel(QfloatTilesArgs p) {
+  constexpr int PITCH = 36;
+  __shared__ uint32_t tops[4];
+  __shared__ __attribute__((aligned(16))) uint32_t words[128 * PITCH + 64];
+  const int t = threadIdx.x, lane = t & 63, wave = t >> 6, quad = t >> 3, c = t & 7;
+  const int nkb = (p.cols + 127) / 128, nkb_t = (p.rows + 127) / 128, tr = blockIdx.x / nkb, tc = blockIdx.x - tr * nkb;
+  const int64_t form = (int64_t)nkb * nkb_t * (16384 + 128), elements = (int64_t)nkb * nkb_t * 16384;
+  float v[4][16];
+  {
+    QuantChunk raw[4];
+    load_tile(p.x + ((int64_t)blockIdx.y * p.rows + tr * 128) * p.cols, p.cols, p.rows - tr * 128, quad, tc * 128 + c * 16, raw);
+#pragma unroll
+    for (int r = 0; r < 4; ++r)
+#pragma unroll
+      for (int q = 0; q < 16; ++q) v[r][q] = quant_element(raw[r], q);
+  }
+  uint32_t m = 0;
+#pragma unroll
+  for (int r = 0; r < 4; ++r)
+#pragma unroll
+    for (int q = 0; q < 16; ++q) m = max(m, qfloat_magnitude(v[r][q]));
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) m = max(m, (uint32_t)__shfl_xor((int)m, d));
+  if (lane == 0) tops[wave] = m;
+  __syncthreads();
+  const QfloatScale one = qfloat_scale(max(max(tops[0], tops[1]), max(tops[2], tops[3])));
+  if (p.q) {
+    const QfloatScale s[4] = {one, one, one, one};
+    uint8_t* const q = p.q + blockIdx.y * form;
+    store_rows(q, q + elements, nkb, tr * 128 + quad * 4, tc, c, v, s);
+  }
+  if (!p.qt) return;
+  uint8_t* const qt = p.qt + blockIdx.y * form;
+#pragma unroll
+  for (int q = 0; q < 16; ++q) {
+    const int at = c * 16 + q;
+    words[at * PITCH + c * 8 + quad] = qfloat_four(v[0][q] * one.inv, v[1][q] * one.inv, v[2][q] * one.inv, v[3][q] * one.inv);
+    if (quad == 0) qt[elements + qfloat_scale_at(tc * 128 + at, tr, nkb_t)] = (uint8_t)one.byte;
+  }
+  __syncthreads();
+#pragma unroll
+  for (int u = 0; u < 4; ++u) {                             // column block u, row block `wave`
+    const int at = u * 32 + (lane & 31);
+    *reinterpret_cast<u32x4_t*>(qt + ((int64_t)(tc * 4 + u) * (nkb_t * 4) + tr * 4 + wave) * 1024 + lane * 16) =
+        *reinterpret_cast<const u32x4_t*>(words + at * PITCH + (at >> 4) * 8 + (wave * 2 + (lane >> 5)) * 4);
+  }
+}
+
+__global__ __launch_bounds__(256) void turn_kernel(QfloatTurnArgs p) {
+  constexpr int PITCH = 68;
+  __shared__ __attribute__((aligned(16))) uint32_t words[128 * PITCH + 128];
+  const int t = threadIdx.x, lane = t & 63, wave = t >> 6, quad = t >> 3, c = t & 7;
+  const int nkb = (p.cols + 127) / 128, tr = blockIdx.x / nkb, tc = blockIdx.x - tr * nkb;
+  QfloatTile tile;
+  if (!qfloat_tile<128>(p.groups, tr, lane, tile)) return;
+  QuantChunk raw[4];
+  load_tile(p.x + (int64_t)tile.row * p.cols, p.cols, tile.rows, quad, tc * 128 + c * 16, raw);
+#pragma unroll
+  for (int w = 0; w < 8; ++w) {                             // two columns at a time
+    const int at = c * 16 + 2 * w;
+    uint32_t* const to = words + at * PITCH + c * 16 + quad * 2;
+    to[0] = __builtin_amdgcn_perm(raw[1].w[w], raw[0].w[w], 0x05040100);
+    to[1] = __builtin_amdgcn_perm(raw[3].w[w], raw[2].w[w], 0x05040100);
+    to[PITCH] = __builtin_amdgcn_perm(raw[1].w[w], raw[0].w[w], 0x07060302);
+    to[PITCH + 1] = __builtin_amdgcn_perm(raw[3].w[w], raw[2].w[w], 0x07060302);
+  }
+  if (p.q) {
+    float v[4][16];
+    QfloatScale s[4];
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      uint32_t top = 0;
+#pragma unroll
+      for (int q = 0; q < 16; ++q) {
+        v[r][q] = quant_element(raw[r], q);
+        top = max(top, qfloat_magnitude(v[r][q]));
+      }
+      s[r] = qfloat_scale(max_of_eight(top));
+    }
+    store_rows(p.q, p.scale, nkb, tile.padded + quad * 4, tc, c, v, s);
+  }
+  __syncthreads();
+#pragma unroll
+  for (int u = 0; u < 8; ++u) {                             // column block u / 2, 16 rows 2 wave + (u & 1)
+    const int at = (u >> 1) * 32 + (lane & 31), rows = wave * 2 + (u & 1);
+    *reinterpret_cast<u32x4_t*>(p.turned + ((int64_t)(tc * 4 + (u >> 1)) * (p.pitch / 32) + (tile.padded >> 4) + rows) * 1024 + lane * 16) =
+        *reinterpret_cast<const u32x4_t*>(words + at * PITCH + (at >> 4) * 16 + (rows * 2 + (lane >> 5)) * 4);
+  }
+}
+
+template <int LPR, int CPT>
+void launch_rows(const QfloatRowsArgs& a, hipStream_t s) {
+  rows_kernel<LPR, CPT><<<(unsigned)(((int64_t)a.groups.T * LPR + 255) / 256), 256, 0, s>>>(a);
+}
+
+}  // namespace
+
+hipError_t stem_qfloat_rows_launch(stem_ctx* ctx, const QfloatRowsArgs& a, hipStream_t s) {
+  ProfScope prof(ctx, K_QFLOAT_ROWS, s);
+  const int rows = a.groups.T;
+  if (a.K <= 2048) rows >= 2048 ? launch_rows<32, 4>(a, s) : launch_rows<64, 2>(a, s);
+  else if (a.K <= 4096) rows >= 2048 ? launch_rows<32, 8>(a, s) : launch_rows<256, 1>(a, s);
+  else if (a.K <= 8192) rows >= 1024 ? launch_rows<64, 8>(a, s) : launch_rows<256, 2>(a, s);
+  else launch_rows<256, 0>(a, s);
+  return hipGetLastError();
+}
+
+hipError_t stem_qfloat_weights_launch(stem_ctx* ctx, const QfloatTilesArgs& a, hipStream_t s) {
+  ProfScope prof(ctx, K_QFLOAT_WEIGHTS, s);
+  const dim3 grid((unsigned)(stem_qfloat_size(a.rows, a.cols) / 16384), a.batch);
+  weights_kernel<<<grid, 256, 0, s>>>(a);
+  return hipGetLastError();
+}
+
+hipError_t stem_qfloat_turn_launch(stem_ctx* ctx, const QfloatTurnArgs& a, hipStream_t s) {
+  ProfScope prof(ctx, K_QFLOAT_TURN, s);
+  const int64_t rows = stem_qfloat_rows(a.groups.T, a.groups.n);
+  turn_kernel<<<(unsigned)(rows / 128 * ((a.cols + 127) / 128)), 256, 0, s>>>(a);
+  return hipGetLastError();
+}

@@ -50,7 +50,7 @@ enum StemKernelId {
   K_EXPERTS_COMBINE_BACK,
   K_QFLOAT_WEIGHTS,  // bf16 weights to 8-bit floating point
   K_QFLOAT_ROWS,     // (normed) activations
-  K_QFLOAT_TILES,    // gradients and activations, by rows and by columns
+  K_QFLOAT_TURN,     // gradients and activations transposed for a weight gradient
   K_QFLOAT_GATE,     // gate product with SiLU*gather and its result's 8-bit form
   K_QFLOAT_LINEAR,
   K_QFLOAT_DX,
@@ -145,8 +145,8 @@ struct stem_ctx {
   // 8-bit floating point products (stem_qfloat_reserve): room for rows of a call, their hidden values, and for the backward pass dy and x by columns
   int qfloat_groups;              // of weights, that it is sized for; 0: not reserved
   int qfloat_backward;
-  uint8_t *qfloat_x, *qfloat_h, *qfloat_dyt, *qfloat_xt;
-  float* qfloat_ws;               // partial sums of K slices, and hidden values of few tokens
+  uint8_t *qfloat_x, *qfloat_h, *qfloat_dyt, *qfloat_xt;   // (the last two: dy and x transposed)
+  float* qfloat_ws;               // partial sums of K slices
 
   // profiling
   int prof_on;

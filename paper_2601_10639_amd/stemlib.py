@@ -29,6 +29,7 @@ SYMBOLS = [
     "stem_embed_grad", "stem_embed_grad_presorted", "stem_embed_grad_noalloc", "stem_embed_sparse_adamw",
     "stem_block_enter_forward", "stem_block_enter_backward", "stem_block_leave_forward", "stem_block_leave_backward", "stem_dropout",
     "stem_quant_bytes", "stem_quant_weights", "stem_quant_linear", "stem_quant_ffn_forward",
+    "stem_qfloat_reserve", "stem_qfloat_bytes", "stem_qfloat_weights", "stem_qfloat_linear", "stem_qfloat_linear_backward", "stem_qfloat_ffn_forward",
     "stem_experts_sort", "stem_experts_dispatch", "stem_experts_combine", "stem_experts_combine_backward",
     "stem_prefetch_rows", "stem_cache_init", "stem_prefetch_rows_cached", "stem_cache_state",
     "stem_edit_rows", "stem_profile_enable", "stem_profile_kernels", "stem_profile_read",
@@ -201,6 +202,18 @@ def lib() -> ctypes.CDLL:
         L.stem_quant_linear.restype = i32
         L.stem_quant_ffn_forward.argtypes = [vp, vp, vp, i64, norm, vp, vp, vp, vp, vp, i64, vp, vp, vp]
         L.stem_quant_ffn_forward.restype = i32
+        L.stem_qfloat_reserve.argtypes = [vp, i32, i32]
+        L.stem_qfloat_reserve.restype = i32
+        L.stem_qfloat_bytes.argtypes = [i64, i64]
+        L.stem_qfloat_bytes.restype = i64
+        L.stem_qfloat_weights.argtypes = [vp, vp, i32, i64, i64, vp, vp, vp]
+        L.stem_qfloat_weights.restype = i32
+        L.stem_qfloat_linear.argtypes = [vp, vp, i64, i64, norm, vp, i64, i32, vp, vp, vp, vp]
+        L.stem_qfloat_linear.restype = i32
+        L.stem_qfloat_linear_backward.argtypes = [vp, vp, vp, i64, i64, vp, i64, i32, vp, vp, vp, i32, vp]
+        L.stem_qfloat_linear_backward.restype = i32
+        L.stem_qfloat_ffn_forward.argtypes = [vp, vp, vp, i64, norm, vp, vp, i32, vp, vp, i64, vp, vp, vp]
+        L.stem_qfloat_ffn_forward.restype = i32
         L.stem_experts_sort.argtypes = [vp, vp, i64, i32, i32, vp, vp, vp, vp]
         L.stem_experts_sort.restype = i32
         L.stem_experts_dispatch.argtypes = [vp, vp, i64, i64, vp, i64, i32, vp, vp, vp, vp]
@@ -688,6 +701,84 @@ def stem_quant_ffn_forward(ctx: StemCtx, x, ids, gate: StemQuant, down: StemQuan
                                           _shaped(y, dt, (T, d), "y"), _stream(stream))
     if st != STEM_OK:
         _check(ctx, st, "stem_quant_ffn_forward")
+
+
+class StemQfloat:
+    """Weights [groups, N, K] in 8-bit floating point: q for the forward calls, qt for the backward pass (or None)."""
+
+    def __init__(self, q, qt, groups: int, N: int, K: int):
+        self.q, self.qt, self.groups, self.N, self.K = q, qt, groups, N, K
+
+
+def stem_qfloat_reserve(ctx: StemCtx, groups: int = 1, backward: bool = False):
+    """Scratch for the stem_qfloat calls of up to this many groups."""
+    _check(ctx, lib().stem_qfloat_reserve(ctx.handle, groups, 1 if backward else 0), "stem_qfloat_reserve")
+
+
+def stem_qfloat_bytes(N: int, K: int) -> int:
+    return lib().stem_qfloat_bytes(N, K)
+
+
+def stem_qfloat_weights(ctx: StemCtx, W, backward: bool = False, out: StemQfloat | None = None, stream=None) -> StemQfloat:
+    """W [N, K] or [groups, N, K] in 8-bit floating point, into `out` or new buffers; backward: its transpose too."""
+    groups, (N, K) = (1 if W.dim() == 2 else W.shape[0]), W.shape[-2:]
+    if out is None:
+        new = lambda: torch.empty(groups * lib().stem_qfloat_bytes(N, K), dtype=torch.uint8, device=W.device)
+        out = StemQfloat(new(), new() if backward else None, groups, N, K)
+    shape = (out.N, out.K) if W.dim() == 2 and out.groups == 1 else (out.groups, out.N, out.K)
+    st = lib().stem_qfloat_weights(ctx.handle, _shaped(W, ctx.torch_dtype, shape, "W"), groups, N, K, *_qfloat(out, N, K, "out"), _stream(stream))
+    _check(ctx, st, "stem_qfloat_weights")
+    return out
+
+
+def _qfloat(w: StemQfloat, N: int, K: int, name: str):
+    if (w.N, w.K) != (N, K):
+        raise ValueError(f"{name}: expected weights of shape {(N, K)}, got {(w.N, w.K)}")
+    size = (w.groups * lib().stem_qfloat_bytes(N, K),)
+    return _shaped(w.q, torch.uint8, size, name + ".q"), _shaped(w.qt, torch.uint8, size, name + ".qt")
+
+
+def _offsets(offsets, groups: int):
+    return _shaped(offsets, torch.int32, (groups + 1,), "offsets")
+
+
+def stem_qfloat_linear(ctx: StemCtx, x, W: StemQfloat, y, residual=None, norm: stem_norm | None = None, offsets=None, stream=None):
+    """y = Q(N(x)) W_g^T (+ residual), rows offsets[g] .. offsets[g + 1] with the g-th weights; y may be residual."""
+    dt, T = ctx.torch_dtype, x.shape[0]
+    q, _ = _qfloat(W, W.N, W.K, "W")
+    if norm is not None:
+        norm._check(ctx, W.K, "norm")
+    st = lib().stem_qfloat_linear(ctx.handle, _shaped(x, dt, (T, W.K), "x"), T, W.K, norm, q, W.N, W.groups, _offsets(offsets, W.groups),
+                                  _shaped(residual, dt, (T, W.N), "residual"), _shaped(y, dt, (T, W.N), "y"), _stream(stream))
+    _check(ctx, st, "stem_qfloat_linear")
+
+
+def stem_qfloat_linear_backward(ctx: StemCtx, dy, x, W: StemQfloat, dx=None, dW=None, offsets=None, accumulate: bool = False, stream=None):
+    """dx = Q(dy) W_g; dW [groups, N, K] (or [N, K] of one) fp32 = dy^T x over each group's rows.  Either may be None, x without dW."""
+    dt, T = ctx.torch_dtype, dy.shape[0]
+    _, qt = _qfloat(W, W.N, W.K, "W")
+    if dW is not None and W.groups == 1 and dW.dim() == 2:
+        dW = dW.unsqueeze(0)
+    st = lib().stem_qfloat_linear_backward(ctx.handle, _shaped(dy, dt, (T, W.N), "dy"), _shaped(x, dt, (T, W.K), "x"), T, W.K, qt, W.N, W.groups,
+                                           _offsets(offsets, W.groups), _shaped(dx, dt, (T, W.K), "dx"),
+                                           _shaped(dW, torch.float32, (W.groups, W.N, W.K), "dW"), 1 if accumulate else 0, _stream(stream))
+    _check(ctx, st, "stem_qfloat_linear_backward")
+
+
+def stem_qfloat_ffn_forward(ctx: StemCtx, x, ids, gate: StemQfloat, down: StemQfloat, E, y, residual=None, norm: stem_norm | None = None, offsets=None,
+                            stream=None, E_rows=None):
+    """y = Q(SiLU(Q(N(x)) gate_g^T) * E[ids]) down_g^T (+ residual); y may be x and residual."""
+    dt, T, d, F = ctx.torch_dtype, x.shape[0], ctx.d_model, ctx.d_ff
+    if gate.groups != down.groups:
+        raise ValueError(f"down: expected {gate.groups} groups, got {down.groups}")
+    gq, dq = _qfloat(gate, F, d, "gate")[0], _qfloat(down, d, F, "down")[0]
+    if norm is not None:
+        norm._check(ctx, d, "norm")
+    E_rows = E.shape[0] if E_rows is None else E_rows
+    st = lib().stem_qfloat_ffn_forward(ctx.handle, _shaped(x, dt, (T, d), "x"), _shaped(ids, torch.int32, (T,), "ids"), T, norm, gq, dq, gate.groups,
+                                       _offsets(offsets, gate.groups), _shaped(E, dt, (E.shape[0], F), "E"), E_rows,
+                                       _shaped(residual, dt, (T, d), "residual"), _shaped(y, dt, (T, d), "y"), _stream(stream))
+    _check(ctx, st, "stem_qfloat_ffn_forward")
 
 
 def stem_experts_sort(ctx: StemCtx, experts, src, place, offsets, stream=None):
