@@ -96,7 +96,7 @@ __device__ __forceinline__ bool find_work(const QfloatGemmArgs& p, int lane, Wor
     w.rows = p.M - w.m0;
     if (p.groups.offsets) {
       int k0 = 0, nk = 0;
-      qfloat_scan<128>(p.groups, lane, [&](int i, int, int rows, int, int, int padded) {
+      qfloat_scan<128>(p.groups, lane, [&](int i, int, int rows, int, int, int padded) __attribute__((always_inline)) {
         const uint64_t mine = __ballot(i == w.group);
         if (!mine) return false;
         const int l = __builtin_ctzll(mine);
@@ -307,6 +307,134 @@ __device__ __forceinline__ void load_ids(const QfloatGemmArgs& p, int m0, int ro
   }
 }
 
+// ---- 256 x 256 ----------------------------------------------------------------------------------------------------------------
+// 4 wavefronts of 4 x 4 accumulators, a ring of five 32 KB slots of one operand tile each: the loop of the 8-bit integer products (gemm_int8.hip), whose
+// instruction takes as long for the same bytes.
+constexpr int SLOT = 32768;
+
+template <QfloatOut OUT>
+__global__ __launch_bounds__(256) void ring_kernel(QfloatGemmArgs p) {
+  typedef Output<4, 4, false> Out;
+  typedef Hidden<4> Hid;
+  static_assert(4 * Out::BYTES <= 5 * SLOT && 4 * Hid::BYTES <= 5 * SLOT, "room for the epilogue");
+  __shared__ __attribute__((aligned(16))) char smem[5 * SLOT];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int wm = wave >> 1, wn = wave & 1;
+  Work w;
+  if (!find_work<256, 256, false>(p, lane, w)) return;
+  const int nk = p.K / 128, kbytes = nk * 4096;
+  const int64_t b_bytes = stem_qfloat_pitch(p.N) * p.K;
+  const uint8_t *const B = p.B + w.group * p.stride_b, *const sb = p.sb + w.group * p.stride_b;
+  int id[2];
+  if (OUT == QFLOAT_HIDDEN) load_ids<4>(p, w.m0 + wm * 128, w.rows - wm * 128, lane, id);
+  Loader<256, 4> la, lb;
+  la.init(p.A, p.a_bytes, w.rows, p.K, w.pa, wave, lane);
+  lb.init(B, b_bytes, p.N - w.n0, p.K, w.n0, wave, lane);
+  const rsrc_t none = resource(p.A, 0);
+  Scales ca, cb;
+  ca.init(p.sa, p.a_bytes / 128, w.pa + wm * 128, nk, lane);
+  cb.init(sb, b_bytes / 128, w.n0 + wn * 128, nk, lane);
+  // every XCD starts at another eighth of K: the rows' groups are a power of two apart where K is, and so their blocks at one k in the
+  // same few memory channels
+  const int start = nk >= 16 ? (int)(blockIdx.x & 7) * nk / 8 : 0;
+  int ka = start * 4096, kb = ka, ks = start;
+  int left_a = nk, left_b = nk;   // tiles still to be requested; requests beyond the last one read nothing
+  auto next = [&](int& k, int& left, auto& l) __attribute__((always_inline)) {
+    k += 4096;
+    if (k >= kbytes) k = 0;
+    if (--left <= 0) l.r = none;
+  };
+  f32x16_t acc[4][4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) acc[i][j] = f32x16_t{};
+  i32x8_t xa[4], xb[4], ya[4], yb[4];
+  const uint32_t fa = wm * 16384 + lane * 16, fb = wn * 16384 + lane * 16;
+  auto frag = [&](int slot, uint32_t f, int ks, int i) __attribute__((always_inline)) {
+    const char* const at = smem + slot * SLOT + f + i * 4096 + ks * 2048;
+    return join(*reinterpret_cast<const i32x4_t*>(at), *reinterpret_cast<const i32x4_t*>(at + 1024));
+  };
+  uint32_t sa, sb_, na_, nb_;
+  // order of a k-step's fragments and of the products that use them, two a fragment
+  auto mma2 = [&](auto Q, i32x8_t(&a)[4], i32x8_t(&b)[4]) __attribute__((always_inline)) {
+    constexpr int ii[16] = {0, 0, 1, 1, 0, 1, 0, 1, 2, 2, 2, 2, 3, 3, 3, 3};
+    constexpr int jj[16] = {0, 1, 0, 1, 2, 2, 3, 3, 0, 1, 2, 3, 0, 1, 2, 3};
+    constexpr int h = 2 * decltype(Q)::value;
+    acc[ii[h]][jj[h]] = mma<jj[h], ii[h]>(b[jj[h]], a[ii[h]], acc[ii[h]][jj[h]], sb_, sa);
+    acc[ii[h + 1]][jj[h + 1]] = mma<jj[h + 1], ii[h + 1]>(b[jj[h + 1]], a[ii[h + 1]], acc[ii[h + 1]][jj[h + 1]], sb_, sa);
+  };
+  auto read = [&](int sa, int sb, int ks, int q, i32x8_t(&a)[4], i32x8_t(&b)[4]) __attribute__((always_inline)) {
+    constexpr int isA[8] = {1, 0, 0, 1, 0, 0, 1, 1};
+    constexpr int idx[8] = {0, 0, 1, 1, 2, 3, 2, 3};
+    if (isA[q]) a[idx[q]] = frag(sa, fa, ks, idx[q]);
+    else b[idx[q]] = frag(sb, fb, ks, idx[q]);
+  };
+  // Operand tiles alternate through the slots: A of K tile t in slot 2t mod 5, B in 2t+1 mod 5.  A(t+2) is requested during the first
+  // k-step of tile t, behind the scales of t+1, and B(t+2) behind the barrier before its last: whole K tiles before they are needed, and the wait in front
+  // of the barrier leaves the youngest 8 loads in flight.
+  sa = ca.load(ks);
+  sb_ = cb.load(ks);
+#pragma unroll
+  for (int h = 0; h < 4; ++h) {
+#pragma unroll
+    for (int q = 0; q < 8; ++q) {
+      if (h & 1) lb.issue(q, smem + h * SLOT, wave, kb);
+      else la.issue(q, smem + h * SLOT, wave, ka);
+    }
+    if (h & 1) next(kb, left_b, lb); else next(ka, left_a, la);
+  }
+  asm volatile("s_waitcnt vmcnt(%0)" ::"n"(16) : "memory");
+  __builtin_amdgcn_s_barrier();
+  __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+  for (int q = 0; q < 8; ++q) read(0, 1, 0, q, xa, xb);
+  auto ring_iteration = [&](const int tmod) __attribute__((always_inline)) {
+    const int s0 = (2 * tmod) % 5, s1 = (2 * tmod + 1) % 5, n0 = (2 * tmod + 2) % 5, n1 = (2 * tmod + 3) % 5, in = (2 * tmod + 4) % 5;
+    if (++ks >= nk) ks = 0;
+    na_ = ca.load(ks);
+    nb_ = cb.load(ks);
+    __builtin_amdgcn_sched_barrier(0);
+    each([&](auto Q) __attribute__((always_inline)) {
+      constexpr int q = decltype(Q)::value;
+      read(s0, s1, 1, q, ya, yb);
+      la.issue(q, smem + in * SLOT, wave, ka);
+      mma2(Q, xa, xb);
+      __builtin_amdgcn_sched_barrier(0);
+    }, std::make_integer_sequence<int, 8>{});
+    next(ka, left_a, la);
+    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(8) : "memory");
+    __builtin_amdgcn_s_barrier();
+    __builtin_amdgcn_sched_barrier(0);
+    each([&](auto Q) __attribute__((always_inline)) {
+      constexpr int q = decltype(Q)::value;
+      read(n0, n1, 0, q, xa, xb);
+      lb.issue(q, smem + s0 * SLOT, wave, kb);
+      mma2(Q, ya, yb);
+      __builtin_amdgcn_sched_barrier(0);
+    }, std::make_integer_sequence<int, 8>{});
+    next(kb, left_b, lb);
+    sa = na_;
+    sb_ = nb_;
+  };
+  int kt = 0;
+  for (; kt + 5 <= nk; kt += 5) {
+    ring_iteration(0);
+    ring_iteration(1);
+    ring_iteration(2);
+    ring_iteration(3);
+    ring_iteration(4);
+  }
+  if (kt < nk) ring_iteration(0);
+  if (kt + 1 < nk) ring_iteration(1);
+  if (kt + 2 < nk) ring_iteration(2);
+  if (kt + 3 < nk) ring_iteration(3);
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+  __syncthreads();
+  if constexpr (OUT == QFLOAT_HIDDEN) Hid::run(p, acc, id, smem + wave * Hid::BYTES, w.pa + wm * 128, w.n0 + wn * 128, w.rows - wm * 128, lane);
+  else Out::run(p, acc, smem + wave * Out::BYTES, w.m0 + wm * 128, w.n0 + wn * 128, w.rows - wm * 128, 0, lane);
+}
+
 // ---- tiles with wavefronts that load: STAGES whole K tiles in LDS ----------------------------------------------------------------------
 template <int MI_, int NJ_, int WM_, int WN_, int STAGES_, int LW_>
 struct Tiling {
@@ -491,14 +619,18 @@ typedef Tiling<2, 2, 2, 2, 4, 4> Tile128;       // 128 x 128, 128 KB of LDS
 typedef Tiling<2, 1, 2, 2, 6, 4> Tile128x64;    // 144 KB
 typedef Tiling<1, 4, 4, 1, 4, 4> Hidden128;     // 128 x 128, a wavefront with whole blocks of 128 channels
 
+template <QfloatOut OUT>
+unsigned grid_of(const QfloatGemmArgs& a, int tm, int tn) {
+  const int64_t ntn = (a.N + tn - 1) / tn, ntm = (a.M + tm - 1) / tm;
+  if (OUT == QFLOAT_F32) return (unsigned)(ntm * ntn * (a.groups.offsets ? a.groups.n : a.ksplit));
+  if (a.groups.offsets) return (unsigned)(((a.groups.T + tm - 1) / tm + std::min(a.groups.n, a.groups.T) - 1) * ntn);   // at most: each group may have a tile not full
+  return (unsigned)(ntm * ntn * a.ksplit);
+}
+
 template <QfloatOut OUT, class C>
 hipError_t launch(const QfloatGemmArgs& a, hipStream_t s) {
-  const int64_t ntn = (a.N + C::TN - 1) / C::TN;
-  int64_t tiles;
-  if (OUT == QFLOAT_F32) tiles = (a.M + C::TM - 1) / C::TM * ntn * (a.groups.offsets ? a.groups.n : a.ksplit);
-  else if (a.groups.offsets) tiles = ((a.groups.T + C::TM - 1) / C::TM + std::min(a.groups.n, a.groups.T) - 1) * ntn;   // at most: each group may have a tile not full
-  else tiles = (a.M + C::TM - 1) / C::TM * ntn * a.ksplit;
-  tile_kernel<OUT, C><<<(unsigned)tiles, (C::WAVES + C::LW) * 64, 0, s>>>(a);
+  const unsigned tiles = grid_of<OUT>(a, C::TM, C::TN);
+  tile_kernel<OUT, C><<<tiles, (C::WAVES + C::LW) * 64, 0, s>>>(a);
   return hipGetLastError();
 }
 
@@ -508,7 +640,14 @@ hipError_t stem_qfloat_gemm_launch(stem_ctx* ctx, int kid, QfloatOut out, const 
   ProfScope prof(ctx, kid, s);
   QfloatGemmArgs a = p;
   a.ksplit = 1;
-  if (out == QFLOAT_HIDDEN) return launch<QFLOAT_HIDDEN, Hidden128>(a, s);
   if (out == QFLOAT_F32) return launch<QFLOAT_F32, Tile128>(a, s);
+  // of an average group, which is all that is known here
+  const int64_t rows = (a.groups.T + a.groups.n - 1) / a.groups.n, tiles = (rows + 255) / 256 * a.groups.n * ((a.N + 255) / 256);
+  if (tiles > 128 && rows >= 256) {
+    if (out == QFLOAT_HIDDEN) ring_kernel<QFLOAT_HIDDEN><<<grid_of<QFLOAT_HIDDEN>(a, 256, 256), 256, 0, s>>>(a);
+    else ring_kernel<QFLOAT_BF16><<<grid_of<QFLOAT_BF16>(a, 256, 256), 256, 0, s>>>(a);
+    return hipGetLastError();
+  }
+  if (out == QFLOAT_HIDDEN) return launch<QFLOAT_HIDDEN, Hidden128>(a, s);
   return launch<QFLOAT_BF16, Tile128>(a, s);
 }

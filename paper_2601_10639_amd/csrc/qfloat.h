@@ -158,7 +158,7 @@ __device__ __forceinline__ bool qfloat_tile(const QfloatGroups& G, int t, int la
     return t * TM < G.T;
   }
   bool found = false;
-  qfloat_scan<TM>(G, lane, [&](int i, int lo, int rows, int before, int nt, int padded) {
+  qfloat_scan<TM>(G, lane, [&](int i, int lo, int rows, int before, int nt, int padded) __attribute__((always_inline)) {
     const uint64_t mine = __ballot(t >= before && t < before + nt);
     if (!mine) return false;
     const int l = __builtin_ctzll(mine), in = (t - __builtin_amdgcn_readlane(before, l)) * TM;
@@ -175,5 +175,5 @@ __device__ __forceinline__ bool qfloat_tile(const QfloatGroups& G, int t, int la
 template <int TM>
 __device__ __forceinline__ int qfloat_tiles(const QfloatGroups& G, int lane) {
   if (!G.offsets) return (G.T + TM - 1) / TM;
-  return qfloat_scan<TM>(G, lane, [](int, int, int, int, int, int) { return false; });
+  return qfloat_scan<TM>(G, lane, [](int, int, int, int, int, int) __attribute__((always_inline)) { return false; });
 }

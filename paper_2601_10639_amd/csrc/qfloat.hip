@@ -54,14 +54,15 @@ __global__ __launch_bounds__(256) void rows_kernel(QfloatRowsArgs p) {
   int place = live ? row : -1;
   if (p.groups.offsets) {
     place = -1;
-    qfloat_scan<128>(p.groups, lane, [&](int, int lo, int rows, int, int, int padded) {
+    qfloat_scan<128>(p.groups, lane, [&](int, int lo, int rows, int, int, int padded) __attribute__((always_inline)) {
 #pragma unroll
       for (int h = 0; h < 64; h += (LPR < 64 ? LPR : 64)) {
         const int r = __builtin_amdgcn_readlane(row, h);
         const uint64_t mine = __ballot(r >= lo && r < lo + rows);
         if (mine) {
           const int at = __builtin_ctzll(mine);
-          if ((LPR < 64 ? lane / LPR * LPR : 0) == h) place = __builtin_amdgcn_readlane(padded, at) + r - __builtin_amdgcn_readlane(lo, at);
+          const int found = __builtin_amdgcn_readlane(padded, at) + r - __builtin_amdgcn_readlane(lo, at);   // (of all lanes: not in the branch)
+          if ((LPR < 64 ? lane / LPR * LPR : 0) == h) place = found;
         }
       }
       return false;

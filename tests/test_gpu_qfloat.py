@@ -174,6 +174,18 @@ def test_linear_by_groups(T, groups, N, K, residual):
     check_linear(ctx, T, N, K, groups, offsets_of(T + 1, T, groups, T // 7, T - T // 5), norm_kind=L.STEM_NORM_RMS)   # rows in front of and behind the groups
 
 
+@pytest.mark.parametrize("T,groups,N,K", [(4500, 1, 2100, 200), (4500, 1, 2104, 2048), (2100, 1, 4097, 300), (9000, 3, 3001, 130), (6000, 2, 2304, 2200)])
+def test_linear_of_many_rows(T, groups, N, K):
+    """Large tiles: of odd columns, K tiles in all of the ring's places, and groups that end inside a tile."""
+    ctx = make_ctx(T, 64, wide(K), groups=groups)
+    check_linear(ctx, T, N, K, groups, None if groups == 1 else offsets_of(T, T, groups, 5, T - 77), residual=True)
+
+
+@pytest.mark.parametrize("T,groups,d,F", [(4200, 1, 192, 2240), (4400, 3, 128, 3264)])
+def test_ffn_of_many_rows(T, groups, d, F):
+    check_ffn(make_ctx(T, d, F, groups=groups), T, d, F, groups=groups, offsets=None if groups == 1 else offsets_of(3, T, groups, 9, T - 70))
+
+
 def test_offsets_that_are_none():
     """Descending, negative, beyond the rows: as the oracle takes them, and nothing outside is touched."""
     T, N, K = 300, 130, 200
