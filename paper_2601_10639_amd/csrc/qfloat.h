@@ -177,3 +177,22 @@ __device__ __forceinline__ int qfloat_tiles(const QfloatGroups& G, int lane) {
   if (!G.offsets) return (G.T + TM - 1) / TM;
   return qfloat_scan<TM>(G, lane, [](int, int, int, int, int, int) __attribute__((always_inline)) { return false; });
 }
+// The place in a form of each lane's row, which LANES neighbouring lanes share; -1: it belongs to no group.  One after another.
+template <int LANES>
+__device__ __forceinline__ int qfloat_place(const QfloatGroups& G, int row, int lane) {
+  int place = -1;
+  qfloat_scan<128>(G, lane, [&](int, int lo, int rows, int, int, int padded) __attribute__((always_inline)) {
+#pragma unroll
+    for (int h = 0; h < 64; h += LANES) {
+      const int r = __builtin_amdgcn_readlane(row, h);
+      const uint64_t mine = __ballot(r >= lo && r < lo + rows);
+      if (mine) {
+        const int at = __builtin_ctzll(mine);
+        const int found = __builtin_amdgcn_readlane(padded, at) + r - __builtin_amdgcn_readlane(lo, at);   // (of all lanes: not in the branch)
+        if (lane / LANES * LANES == h) place = found;
+      }
+    }
+    return false;
+  });
+  return place;
+}

@@ -29,7 +29,43 @@ __device__ __forceinline__ float sum_row(float v, float* red) {
   return v;
 }
 
-// ---- rows, with or without a norm ---------------------------------------------------------------------------------------------
+// ---- rows without a norm ----------------------------------------------------------------------------------------------------------
+// A workgroup has 32 rows and up to 4 blocks of each: a lane the 16 values of row t / 8, chunk t % 8, so that eight lanes read 256 bytes of a row and store, with
+// the seven other rows of their wavefront, whole lines of the form.  16384 x 8192: 123 us with a wavefront a row, whose 16-byte stores are 512 apart.
+constexpr int BLOCKS = 4;
+__global__ __launch_bounds__(256) void chunks_kernel(QfloatRowsArgs p) {
+  const int lane = threadIdx.x & 63, c = threadIdx.x & 7, nkb = (p.K + 127) / 128, parts = (nkb + BLOCKS - 1) / BLOCKS;
+  const int group = blockIdx.x / parts, kb0 = (blockIdx.x - group * parts) * BLOCKS, row = group * 32 + (threadIdx.x >> 3);
+  const bool live = row < p.groups.T;
+  const bf16_t* const x = p.x + (int64_t)(live ? row : 0) * p.K;
+  QuantChunk raw[BLOCKS];
+#pragma unroll
+  for (int u = 0; u < BLOCKS; ++u) {
+    const int at = (kb0 + u) * 128 + c * 16;
+    raw[u] = live && at < p.K ? quant_load_chunk(x + at, p.K - at) : QuantChunk{};
+  }
+  int place = live ? row : -1;
+  if (p.groups.offsets) place = qfloat_place<8>(p.groups, row, lane);
+  uint8_t* const out = p.q + ((int64_t)(place >> 5) * nkb * 4 + (c >> 1)) * 1024 + (c & 1) * 512 + (place & 31) * 16;
+#pragma unroll
+  for (int u = 0; u < BLOCKS; ++u) {
+    const int kb = kb0 + u;
+    uint32_t top = 0;
+#pragma unroll
+    for (int q = 0; q < 16; ++q) top = max(top, qfloat_magnitude(quant_element(raw[u], q)));
+    const QfloatScale s = qfloat_scale(max_of_eight(top));
+    uint32_t w[4];
+#pragma unroll
+    for (int q = 0; q < 4; ++q)
+      w[q] = qfloat_four(quant_element(raw[u], 4 * q) * s.inv, quant_element(raw[u], 4 * q + 1) * s.inv, quant_element(raw[u], 4 * q + 2) * s.inv,
+                         quant_element(raw[u], 4 * q + 3) * s.inv);
+    if (place < 0 || kb >= nkb) continue;
+    *reinterpret_cast<u32x4_t*>(out + (int64_t)kb * 4096) = u32x4_t{w[0], w[1], w[2], w[3]};
+    if (c == 0) p.scale[qfloat_scale_at(place, kb, nkb)] = (uint8_t)s.byte;
+  }
+}
+
+// ---- rows behind a norm ---------------------------------------------------------------------------------------------
 // LPR neighbouring lanes have a row (256: the workgroup), CPT chunks of 16 values each (0: as many as there are, read again for each use).
 template <int LPR, int CPT>
 __global__ __launch_bounds__(256) void rows_kernel(QfloatRowsArgs p) {
@@ -50,24 +86,8 @@ __global__ __launch_bounds__(256) void rows_kernel(QfloatRowsArgs p) {
     for (int t = 0; t < CPT; ++t)
       if (t * LPR < chunks) raw[t] = fetch(t);
   }
-  // its place in the form: the rows of a wavefront find theirs one after another
   int place = live ? row : -1;
-  if (p.groups.offsets) {
-    place = -1;
-    qfloat_scan<128>(p.groups, lane, [&](int, int lo, int rows, int, int, int padded) __attribute__((always_inline)) {
-#pragma unroll
-      for (int h = 0; h < 64; h += (LPR < 64 ? LPR : 64)) {
-        const int r = __builtin_amdgcn_readlane(row, h);
-        const uint64_t mine = __ballot(r >= lo && r < lo + rows);
-        if (mine) {
-          const int at = __builtin_ctzll(mine);
-          const int found = __builtin_amdgcn_readlane(padded, at) + r - __builtin_amdgcn_readlane(lo, at);   // (of all lanes: not in the branch)
-          if ((LPR < 64 ? lane / LPR * LPR : 0) == h) place = found;
-        }
-      }
-      return false;
-    });
-  }
+  if (p.groups.offsets) place = qfloat_place<(LPR < 64 ? LPR : 64)>(p.groups, row, lane);
   float v[HELD][16];
   auto elements = [&](const QuantChunk& c, float (&u)[16]) __attribute__((always_inline)) {
 #pragma unroll
@@ -275,7 +295,10 @@ void launch_rows(const QfloatRowsArgs& a, hipStream_t s) {
 hipError_t stem_qfloat_rows_launch(stem_ctx* ctx, const QfloatRowsArgs& a, hipStream_t s) {
   ProfScope prof(ctx, K_QFLOAT_ROWS, s);
   const int rows = a.groups.T;
-  if (a.K <= 2048) rows >= 2048 ? launch_rows<32, 4>(a, s) : launch_rows<64, 2>(a, s);
+  if (a.norm.kind == STEM_NORM_NONE && !a.norm.weight) {
+    const int64_t nkb = (a.K + 127) / 128;
+    chunks_kernel<<<(unsigned)((rows + 31) / 32 * ((nkb + BLOCKS - 1) / BLOCKS)), 256, 0, s>>>(a);
+  } else if (a.K <= 2048) rows >= 2048 ? launch_rows<32, 4>(a, s) : launch_rows<64, 2>(a, s);
   else if (a.K <= 4096) rows >= 2048 ? launch_rows<32, 8>(a, s) : launch_rows<256, 1>(a, s);
   else if (a.K <= 8192) rows >= 1024 ? launch_rows<64, 8>(a, s) : launch_rows<256, 2>(a, s);
   else launch_rows<256, 0>(a, s);
