@@ -13,7 +13,7 @@ BIND = os.path.join(HERE, "_bind.so")   # the hot calls' binding, a Python modul
 OBJ_DIR = os.path.join(HERE, "_build")
 SOURCES = ["api.hip", "gemm_bf16.hip", "gemm_skinny_bf16.hip", "gemm_decode_bf16.hip", "ffn_decode_bf16.hip", "kernels_f32.hip", "embed_grad.hip", "embed_grad_static.hip", "adamw.hip", "prefetch.hip", "edit.hip", "calibrate.hip",
            "api_block.hip", "block.hip", "quant.hip", "gemm_int8.hip", "gemm_int8_decode.hip", "api_experts.hip", "experts.hip",
-           "api_qfloat.hip", "qfloat.hip", "gemm_qfloat.hip"]
+           "api_qfloat.hip", "qfloat.hip", "gemm_qfloat.hip", "gemm_qfloat_decode.hip"]
 FLAGS = ["-O3", "--offload-arch=gfx950", "-fPIC", "-std=c++17",
          # keep the compiler from forming packed-fp32 instructions
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops"]

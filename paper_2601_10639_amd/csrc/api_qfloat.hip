@@ -7,6 +7,7 @@
 namespace {
 
 constexpr int64_t MAX_CHANNELS = 1 << 22;
+constexpr int64_t QFLOAT_HIDDEN_INLINE = 4;   // rows whose fp32 hidden values every workgroup of the down product makes its operands of
 constexpr int64_t MAX_FORM = INT32_MAX;   // elements of a form, which kernels address with 32 bits
 
 int64_t widest(const stem_ctx* c) { return std::max(c->desc.d_model, c->desc.d_ff); }
@@ -48,8 +49,30 @@ QfloatGemmArgs gemm_args(const stem_ctx* c, const Form& a, const Form& b, int64_
 }
 
 hipError_t rows_form(stem_ctx* c, const void* x, const QfloatGroups& g, int64_t K, const stem_norm* norm, const Form& f, hipStream_t s) {
-  const QfloatRowsArgs a = {static_cast<const bf16_t*>(x), g, (int)K, norm ? *norm : stem_norm{STEM_NORM_NONE, 0.f, nullptr}, f.q, f.scale};
+  const QfloatRowsArgs a = {static_cast<const bf16_t*>(x), nullptr, g, (int)K, norm ? *norm : stem_norm{STEM_NORM_NONE, 0.f, nullptr}, f.q, f.scale};
   return stem_qfloat_rows_launch(c, a, s);
+}
+
+QfloatDecodeArgs decode_args(const Form& b, int64_t stride_b, int64_t N, int64_t K, const QfloatGroups& g) {
+  QfloatDecodeArgs r = {};
+  r.B = b.q; r.sb = b.scale; r.stride_b = stride_b;
+  r.N = (int)N; r.K = (int)stem_qfloat_pitch(K); r.row_K = (int)K;
+  r.groups = g;
+  const int rows = (g.T + g.n - 1) / g.n;   // of an average group
+  r.nt = rows <= 16 ? 1 : rows <= 32 ? 2 : 4;
+  return r;
+}
+bool few_rows(const QfloatGroups& g) { return (g.T + g.n - 1) / g.n <= QFLOAT_DECODE_ROWS; }
+
+// The rows of a decode product: in place, or their form, which a kernel makes before it
+hipError_t decode_rows(stem_ctx* c, const void* x, int64_t K, const stem_norm* norm, bool in_place, const Form& f, QfloatDecodeArgs& a, hipStream_t s) {
+  if (in_place && a.nt == 1 && stem_qfloat_decode_inline(a.groups.T, K, norm && norm->kind != STEM_NORM_NONE)) {
+    a.x = static_cast<const bf16_t*>(x);
+    a.norm = norm ? *norm : stem_norm{STEM_NORM_NONE, 0.f, nullptr};
+    return hipSuccess;
+  }
+  a.A = f.q; a.sa = f.scale; a.a_bytes = f.bytes;
+  return rows_form(c, x, a.groups, K, norm, f, s);
 }
 
 }  // namespace
@@ -119,6 +142,14 @@ stem_status stem_qfloat_linear(stem_ctx* c, const void* x, int64_t T, int64_t K,
   hipStream_t s = static_cast<hipStream_t>(stream);
   const QfloatGroups g = {offsets, groups, (int)T};
   const Form f = form(c->qfloat_x, rows, K);
+  if (few_rows(g)) {
+    QfloatDecodeArgs a = decode_args(form(q, N, K), stem_qfloat_form(N, K), N, K, g);
+    a.y = static_cast<bf16_t*>(y); a.residual = static_cast<const bf16_t*>(residual);
+    // (in place every workgroup reads x, also when others have written their part of y)
+    HIP_TRY(c, decode_rows(c, x, K, norm, !overlap({x, xb}, {y, yb}), f, a, s));
+    HIP_TRY(c, stem_qfloat_decode_launch(c, K_QFLOAT_LINEAR, a, s));
+    return STEM_OK;
+  }
   HIP_TRY(c, rows_form(c, x, g, K, norm, f, s));
   QfloatGemmArgs a = gemm_args(c, f, form(q, N, K), stem_qfloat_form(N, K), T, N, K, g);
   a.y = static_cast<bf16_t*>(y); a.residual = static_cast<const bf16_t*>(residual);
@@ -207,6 +238,23 @@ stem_status stem_qfloat_ffn_forward(stem_ctx* c, const void* x, const int32_t* i
   hipStream_t s = static_cast<hipStream_t>(stream);
   const QfloatGroups g = {offsets, groups, (int)T};
   const Form f = form(c->qfloat_x, rows, d), h = form(c->qfloat_h, rows, F);
+  if (few_rows(g) && T * F * 4 <= QFLOAT_WS) {
+    QfloatDecodeArgs a = decode_args(form(gate_q, F, d), stem_qfloat_form(F, d), F, d, g);
+    a.h_out = c->qfloat_ws;
+    a.ids = ids; a.E = static_cast<const bf16_t*>(E); a.E_rows = (int)E_rows; a.flag = c->flag;
+    HIP_TRY(c, decode_rows(c, x, d, norm, true, f, a, s));
+    HIP_TRY(c, stem_qfloat_decode_launch(c, K_QFLOAT_GATE, a, s));
+    QfloatDecodeArgs b = decode_args(form(down_q, d, F), stem_qfloat_form(d, F), d, F, g);
+    b.y = static_cast<bf16_t*>(y); b.residual = static_cast<const bf16_t*>(residual);
+    if (T <= QFLOAT_HIDDEN_INLINE) {
+      b.h = c->qfloat_ws;
+    } else {
+      HIP_TRY(c, stem_qfloat_rows_launch(c, {nullptr, c->qfloat_ws, g, (int)F, {STEM_NORM_NONE, 0.f, nullptr}, h.q, h.scale}, s));
+      b.A = h.q; b.sa = h.scale; b.a_bytes = h.bytes;
+    }
+    HIP_TRY(c, stem_qfloat_decode_launch(c, K_QFLOAT_LINEAR, b, s));
+    return STEM_OK;
+  }
   HIP_TRY(c, rows_form(c, x, g, d, norm, f, s));
   QfloatGemmArgs a = gemm_args(c, f, form(gate_q, F, d), stem_qfloat_form(F, d), T, F, d, g);
   a.hq = h.q; a.hs = h.scale;

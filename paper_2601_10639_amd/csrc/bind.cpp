@@ -18,7 +18,7 @@
 namespace {
 
 PyObject *g_ctx_type, *g_get_device, *g_raw_stream, *g_handle, *g_value, *g_dtype, *g_cuda_stream;   // set by setup()
-PyObject *g_norm_type, *g_leave_type, *g_quant_type, *g_tensor, *g_norms, *g_gate_tensor, *g_step_tensor, *g_d_model, *g_d_ff, *g_q, *g_scale, *g_N, *g_K;
+PyObject *g_norm_type, *g_leave_type, *g_quant_type, *g_qfloat_type, *g_qt, *g_groups, *g_tensor, *g_norms, *g_gate_tensor, *g_step_tensor, *g_d_model, *g_d_ff, *g_q, *g_scale, *g_N, *g_K;
 bool g_off = true;                                        // before setup(), and in a forked process
 
 struct Unusual {};
@@ -31,7 +31,7 @@ struct Hold {                  // a new reference, or Unusual
   ~Hold() { Py_DECREF(o); }
 };
 
-enum Kind { ACT, F32, I32, I64, I8 };   // ACT: the context's type
+enum Kind { ACT, F32, I32, I64, I8, U8 };   // ACT: the context's type
 
 // The memory of one of stemlib.py's ctypes structures, of exactly this type
 template <class T>
@@ -67,7 +67,7 @@ struct Args {
     if (!THPVariable_CheckExact(o)) throw Unusual();
     const at::Tensor& t = THPVariable_Unpack(o);
     if (rows >= 0 && (t.dim() != (cols < 0 ? 1 : 2) || t.size(0) != rows || (cols >= 0 && t.size(1) != cols))) throw Unusual();
-    const at::ScalarType want = kind == I32 ? at::kInt : kind == I64 ? at::kLong : kind == I8 ? at::kChar
+    const at::ScalarType want = kind == I32 ? at::kInt : kind == I64 ? at::kLong : kind == I8 ? at::kChar : kind == U8 ? at::kByte
                                 : kind == ACT && dtype == STEM_BF16 ? at::kBFloat16 : at::kFloat;
     if (t.layout() != at::kStrided || t.scalar_type() != want || !t.is_cuda() || !t.is_contiguous()) throw Unusual();
     device_seen = true;
@@ -117,6 +117,30 @@ struct Args {
     const int64_t N = attribute(v[i], g_N), K = attribute(v[i], g_K);
     const Hold q(PyObject_GetAttr(v[i], g_q)), scale(PyObject_GetAttr(v[i], g_scale));
     return {pointer_of(q.o, I8, stem_quant_bytes(N, K), -1), static_cast<const float*>(pointer_of(scale.o, F32, N, -1)), N, K};
+  }
+  // weights in 8-bit floating point
+  struct Qfloat { const void *q, *qt; int64_t groups, N, K; };
+  Qfloat qfloat(int i) const {
+    if (reinterpret_cast<PyObject*>(Py_TYPE(v[i])) != g_qfloat_type) throw Unusual();
+    const int64_t groups = attribute(v[i], g_groups), N = attribute(v[i], g_N), K = attribute(v[i], g_K), bytes = groups * stem_qfloat_bytes(N, K);
+    const Hold q(PyObject_GetAttr(v[i], g_q)), qt(PyObject_GetAttr(v[i], g_qt));
+    return {pointer_of(q.o, U8, bytes, -1), pointer_of(qt.o, U8, bytes, -1), groups, N, K};
+  }
+  // [groups, N, K], or [N, K] of one
+  float* cube(int i, int64_t groups, int64_t N, int64_t K) const {
+    if (v[i] == Py_None) return nullptr;
+    if (!THPVariable_CheckExact(v[i])) throw Unusual();
+    const at::Tensor& t = THPVariable_Unpack(v[i]);
+    const int64_t d = t.dim();
+    if (d < 2 || d > 3 || t.size(d - 2) != N || t.size(d - 1) != K || (d == 3 ? t.size(0) : 1) != groups) throw Unusual();
+    return static_cast<float*>(pointer_of(v[i], F32, -1, -1));
+  }
+  // columns of tensor t
+  int64_t columns(int t) const {
+    if (!THPVariable_CheckExact(v[t])) throw Unusual();
+    const at::Tensor& x = THPVariable_Unpack(v[t]);
+    if (x.dim() != 2) throw Unusual();
+    return x.size(1);
   }
   int64_t d_model() const { return attribute(ctx, g_d_model); }
   int64_t d_ff() const { return attribute(ctx, g_d_ff); }
@@ -335,10 +359,81 @@ PyObject* quant_ffn_forward(PyObject*, PyObject* const* args, Py_ssize_t n) {
   });
 }
 
-// (StemCtx, torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream, stem_norm, stem_leave, StemQuant)
+PyObject* qfloat_linear(PyObject*, PyObject* const* args, Py_ssize_t n) {
+  return enter(args, n, 7, [](const Args& a, stem_ctx* c) {
+    const int64_t T = a.rows(-1, 0);
+    const Args::Qfloat w = a.qfloat(1);
+    auto x = a.shaped(0, ACT, T, w.K); auto y = a.shaped(2, ACT, T, w.N); auto r = a.shaped(3, ACT, T, w.N); auto norm = a.norm(4, w.K);
+    auto o = a.shaped<int32_t>(5, I32, w.groups + 1); auto s = a.stream(6);
+    return [=] { return stem_qfloat_linear(c, x, T, w.K, norm.get(), w.q, w.N, (int)w.groups, o, r, y, s); };
+  });
+}
+
+PyObject* qfloat_linear_backward(PyObject*, PyObject* const* args, Py_ssize_t n) {
+  return enter(args, n, 8, [](const Args& a, stem_ctx* c) {
+    const int64_t T = a.rows(-1, 0);
+    const Args::Qfloat w = a.qfloat(2);
+    auto dy = a.shaped(0, ACT, T, w.N); auto x = a.shaped(1, ACT, T, w.K); auto dx = a.shaped(3, ACT, T, w.K);
+    auto dW = a.cube(4, w.groups, w.N, w.K); auto o = a.shaped<int32_t>(5, I32, w.groups + 1); const int accumulate = a.flag(6); auto s = a.stream(7);
+    return [=] { return stem_qfloat_linear_backward(c, dy, x, T, w.K, w.qt, w.N, (int)w.groups, o, dx, dW, accumulate, s); };
+  });
+}
+
+PyObject* qfloat_ffn_forward(PyObject*, PyObject* const* args, Py_ssize_t n) {
+  return enter(args, n, 11, [](const Args& a, stem_ctx* c) {
+    const int64_t T = a.rows(-1, 0), d = a.d_model(), F = a.d_ff(), rows = a.rows(-1, 4), E_rows = a.rows(10, 4);
+    const Args::Qfloat g = a.qfloat(2), w = a.qfloat(3);
+    if (g.N != F || g.K != d || w.N != d || w.K != F || g.groups != w.groups) throw Unusual();
+    auto x = a.shaped(0, ACT, T, d); auto ids = a.shaped<int32_t>(1, I32, T); auto E = a.shaped(4, ACT, rows, F); auto y = a.shaped(5, ACT, T, d);
+    auto r = a.shaped(6, ACT, T, d); auto norm = a.norm(7, d); auto o = a.shaped<int32_t>(8, I32, g.groups + 1); auto s = a.stream(9);
+    return [=] { return stem_qfloat_ffn_forward(c, x, ids, T, norm.get(), g.q, w.q, (int)g.groups, o, E, E_rows, r, y, s); };
+  });
+}
+
+PyObject* experts_sort(PyObject*, PyObject* const* args, Py_ssize_t n) {
+  return enter(args, n, 5, [](const Args& a, stem_ctx* c) {
+    const int64_t T = a.rows(-1, 0), k = a.columns(0), experts = a.rows(-1, 3) - 1;
+    auto e = a.shaped<int32_t>(0, I32, T, k); auto src = a.shaped<int32_t>(1, I32, T * k); auto place = a.shaped<int32_t>(2, I32, T, k);
+    auto o = a.shaped<int32_t>(3, I32, experts + 1); auto s = a.stream(4);
+    if (k > INT32_MAX || experts > INT32_MAX) throw Unusual();
+    return [=] { return stem_experts_sort(c, e, T, (int)k, (int)experts, src, place, o, s); };
+  });
+}
+
+PyObject* experts_dispatch(PyObject*, PyObject* const* args, Py_ssize_t n) {
+  return enter(args, n, 7, [](const Args& a, stem_ctx* c) {
+    const int64_t T = a.rows(-1, 0), width = a.columns(0), rows = a.rows(-1, 1), k = a.integer(3);
+    auto x = a.shaped(0, ACT, T, width); auto src = a.shaped<int32_t>(1, I32, rows); auto xs = a.shaped(2, ACT, rows, width);
+    auto ids = a.shaped<int32_t>(4, I32, T); auto out = a.shaped<int32_t>(5, I32, rows); auto s = a.stream(6);
+    if (k < INT32_MIN || k > INT32_MAX) throw Unusual();
+    return [=] { return stem_experts_dispatch(c, x, T, width, src, rows, (int)k, ids, xs, out, s); };
+  });
+}
+
+PyObject* experts_combine(PyObject*, PyObject* const* args, Py_ssize_t n) {
+  return enter(args, n, 6, [](const Args& a, stem_ctx* c) {
+    const int64_t rows = a.rows(-1, 0), width = a.columns(0), T = a.rows(-1, 1), k = a.columns(1);
+    auto ys = a.shaped(0, ACT, rows, width); auto place = a.shaped<int32_t>(1, I32, T, k); auto y = a.shaped(2, ACT, T, width);
+    auto w = a.shaped<float>(3, F32, T, k); auto r = a.shaped(4, ACT, T, width); auto s = a.stream(5);
+    if (k > INT32_MAX) throw Unusual();
+    return [=] { return stem_experts_combine(c, ys, rows, width, place, w, T, (int)k, r, y, s); };
+  });
+}
+
+PyObject* experts_combine_backward(PyObject*, PyObject* const* args, Py_ssize_t n) {
+  return enter(args, n, 7, [](const Args& a, stem_ctx* c) {
+    const int64_t T = a.rows(-1, 1), k = a.columns(1), width = a.columns(0), rows = a.v[2] != Py_None ? a.rows(-1, 2) : a.v[3] != Py_None ? a.rows(-1, 3) : 0;
+    auto dy = a.shaped(0, ACT, T, width); auto place = a.shaped<int32_t>(1, I32, T, k); auto dys = a.shaped(2, ACT, rows, width);
+    auto ys = a.shaped(3, ACT, rows, width); auto w = a.shaped<float>(4, F32, T, k); auto dw = a.shaped<float>(5, F32, T, k); auto s = a.stream(6);
+    if (k > INT32_MAX) throw Unusual();
+    return [=] { return stem_experts_combine_backward(c, dy, ys, rows, width, place, w, T, (int)k, dys, dw, s); };
+  });
+}
+
+// (StemCtx, torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream, stem_norm, stem_leave, StemQuant, StemQfloat)
 PyObject* setup(PyObject*, PyObject* args) {
-  if (!PyArg_ParseTuple(args, "OOOOOO", &g_ctx_type, &g_get_device, &g_raw_stream, &g_norm_type, &g_leave_type, &g_quant_type)) return nullptr;
-  for (PyObject* o : {g_ctx_type, g_get_device, g_raw_stream, g_norm_type, g_leave_type, g_quant_type}) Py_INCREF(o);
+  if (!PyArg_ParseTuple(args, "OOOOOOO", &g_ctx_type, &g_get_device, &g_raw_stream, &g_norm_type, &g_leave_type, &g_quant_type, &g_qfloat_type)) return nullptr;
+  for (PyObject* o : {g_ctx_type, g_get_device, g_raw_stream, g_norm_type, g_leave_type, g_quant_type, g_qfloat_type}) Py_INCREF(o);
   g_tensor = PyUnicode_InternFromString("tensor");
   g_norms = PyUnicode_InternFromString("norms");
   g_gate_tensor = PyUnicode_InternFromString("gate_tensor");
@@ -349,6 +444,9 @@ PyObject* setup(PyObject*, PyObject* args) {
   g_scale = PyUnicode_InternFromString("scale");
   g_N = PyUnicode_InternFromString("N");
   g_K = PyUnicode_InternFromString("K");
+  g_qt = PyUnicode_InternFromString("qt");
+  g_groups = PyUnicode_InternFromString("groups");
+  if (!g_qt || !g_groups) return nullptr;
   if (!g_tensor || !g_norms || !g_gate_tensor || !g_step_tensor || !g_d_model || !g_d_ff || !g_q || !g_scale || !g_N || !g_K) return nullptr;
   g_handle = PyUnicode_InternFromString("handle");
   g_value = PyUnicode_InternFromString("value");
@@ -368,7 +466,8 @@ PyObject* off(PyObject*, PyObject*) {
 PyMethodDef methods[] = {FAST(ffn_forward), FAST(ffn_forward_residual), FAST(ffn_backward), FAST(ffn_up_forward), FAST(ffn_up_backward),
                          FAST(embed_grad), FAST(embed_grad_presorted), FAST(embed_sparse_adamw),
                          FAST(block_enter_forward), FAST(block_enter_backward), FAST(block_leave_forward), FAST(block_leave_backward), FAST(dropout),
-                         FAST(quant_linear), FAST(quant_ffn_forward),
+                         FAST(quant_linear), FAST(quant_ffn_forward), FAST(qfloat_linear), FAST(qfloat_linear_backward), FAST(qfloat_ffn_forward),
+                         FAST(experts_sort), FAST(experts_dispatch), FAST(experts_combine), FAST(experts_combine_backward),
                          {"setup", setup, METH_VARARGS, nullptr}, {"off", off, METH_NOARGS, nullptr}, {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_bind", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

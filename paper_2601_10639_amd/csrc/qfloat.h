@@ -37,7 +37,8 @@ struct QfloatGroups {
 
 // Rows of x, behind a norm, to the form
 struct QfloatRowsArgs {
-  const bf16_t* x;          // [T, K]
+  const bf16_t* x;          // [T, K], or null:
+  const float* h;           // fp32 hidden values (no norm)
   QfloatGroups groups;
   int K;
   stem_norm norm;
@@ -90,6 +91,31 @@ struct QfloatGemmArgs {
   int32_t* flag;
 };
 hipError_t stem_qfloat_gemm_launch(stem_ctx* ctx, int kid, QfloatOut out, const QfloatGemmArgs& a, hipStream_t s);
+
+// Products of few rows in each group.  Rows: a form (A, sa), or up to 16 that are made to operands in place: rows x of row_K values behind a norm, or fp32 hidden
+// values h.
+struct QfloatDecodeArgs {
+  const uint8_t *A, *sa;
+  const uint8_t *B, *sb;
+  int64_t a_bytes, stride_b;
+  int N, K;                 // K: padded
+  QfloatGroups groups;
+  int nt;                   // 16 nt rows of a form to a workgroup: 1, 2 or 4
+  const bf16_t* x;
+  int row_K;
+  stem_norm norm;
+  const float* h;           // [T, row_K]
+  bf16_t* y;                // [T, N], or null: a gate product
+  const bf16_t* residual;
+  float* h_out;             // [T, N]
+  const int32_t* ids;
+  const bf16_t* E;
+  int E_rows;
+  int32_t* flag;
+};
+bool stem_qfloat_decode_inline(int64_t rows, int64_t K, bool normed);
+hipError_t stem_qfloat_decode_launch(stem_ctx* ctx, int kid, const QfloatDecodeArgs& a, hipStream_t s);
+#define QFLOAT_DECODE_ROWS 64   // of a group, on average, up to which its products are those of few rows
 
 #define QFLOAT_WS (256ll * 128 * 128 * 4)   // bytes: a product is cut into 256 workgroups at most
 

@@ -6,6 +6,7 @@
 #include "quant.h"   // chunks of a bf16 row
 
 typedef __attribute__((ext_vector_type(4))) uint32_t u32x4_t;
+typedef __attribute__((ext_vector_type(4))) float f32x4_t;
 
 namespace {
 
@@ -33,17 +34,28 @@ __device__ __forceinline__ float sum_row(float v, float* red) {
 // A workgroup has 32 rows and up to 4 blocks of each: a lane the 16 values of row t / 8, chunk t % 8, so that eight lanes read 256 bytes of a row and store, with
 // the seven other rows of their wavefront, whole lines of the form.  16384 x 8192: 123 us with a wavefront a row, whose 16-byte stores are 512 apart.
 constexpr int BLOCKS = 4;
+template <bool HIDDEN>
 __global__ __launch_bounds__(256) void chunks_kernel(QfloatRowsArgs p) {
   const int lane = threadIdx.x & 63, c = threadIdx.x & 7, nkb = (p.K + 127) / 128, parts = (nkb + BLOCKS - 1) / BLOCKS;
   const int group = blockIdx.x / parts, kb0 = (blockIdx.x - group * parts) * BLOCKS, row = group * 32 + (threadIdx.x >> 3);
   const bool live = row < p.groups.T;
-  const bf16_t* const x = p.x + (int64_t)(live ? row : 0) * p.K;
-  QuantChunk raw[BLOCKS];
+  const int64_t first = (int64_t)(live ? row : 0) * p.K;
+  QuantChunk raw[HIDDEN ? 1 : BLOCKS];
+  f32x4_t hid[HIDDEN ? BLOCKS : 1][4];
 #pragma unroll
   for (int u = 0; u < BLOCKS; ++u) {
     const int at = (kb0 + u) * 128 + c * 16;
-    raw[u] = live && at < p.K ? quant_load_chunk(x + at, p.K - at) : QuantChunk{};
+    if constexpr (HIDDEN) {
+#pragma unroll
+      for (int g = 0; g < 4; ++g) hid[u][g] = live && at < p.K ? *reinterpret_cast<const f32x4_t*>(p.h + first + at + 4 * g) : f32x4_t{};   // (d_ff: multiples of 64)
+    } else {
+      raw[u] = live && at < p.K ? quant_load_chunk(p.x + first + at, p.K - at) : QuantChunk{};
+    }
   }
+  auto value = [&](int u, int q) __attribute__((always_inline)) {
+    if constexpr (HIDDEN) return hid[u][q >> 2][q & 3];
+    else return quant_element(raw[u], q);
+  };
   int place = live ? row : -1;
   if (p.groups.offsets) place = qfloat_place<8>(p.groups, row, lane);
   uint8_t* const out = p.q + ((int64_t)(place >> 5) * nkb * 4 + (c >> 1)) * 1024 + (c & 1) * 512 + (place & 31) * 16;
@@ -52,13 +64,11 @@ __global__ __launch_bounds__(256) void chunks_kernel(QfloatRowsArgs p) {
     const int kb = kb0 + u;
     uint32_t top = 0;
 #pragma unroll
-    for (int q = 0; q < 16; ++q) top = max(top, qfloat_magnitude(quant_element(raw[u], q)));
+    for (int q = 0; q < 16; ++q) top = max(top, qfloat_magnitude(value(u, q)));
     const QfloatScale s = qfloat_scale(max_of_eight(top));
     uint32_t w[4];
 #pragma unroll
-    for (int q = 0; q < 4; ++q)
-      w[q] = qfloat_four(quant_element(raw[u], 4 * q) * s.inv, quant_element(raw[u], 4 * q + 1) * s.inv, quant_element(raw[u], 4 * q + 2) * s.inv,
-                         quant_element(raw[u], 4 * q + 3) * s.inv);
+    for (int q = 0; q < 4; ++q) w[q] = qfloat_four(value(u, 4 * q) * s.inv, value(u, 4 * q + 1) * s.inv, value(u, 4 * q + 2) * s.inv, value(u, 4 * q + 3) * s.inv);
     if (place < 0 || kb >= nkb) continue;
     *reinterpret_cast<u32x4_t*>(out + (int64_t)kb * 4096) = u32x4_t{w[0], w[1], w[2], w[3]};
     if (c == 0) p.scale[qfloat_scale_at(place, kb, nkb)] = (uint8_t)s.byte;
@@ -297,7 +307,9 @@ hipError_t stem_qfloat_rows_launch(stem_ctx* ctx, const QfloatRowsArgs& a, hipSt
   const int rows = a.groups.T;
   if (a.norm.kind == STEM_NORM_NONE && !a.norm.weight) {
     const int64_t nkb = (a.K + 127) / 128;
-    chunks_kernel<<<(unsigned)((rows + 31) / 32 * ((nkb + BLOCKS - 1) / BLOCKS)), 256, 0, s>>>(a);
+    const unsigned grid = (unsigned)((rows + 31) / 32 * ((nkb + BLOCKS - 1) / BLOCKS));
+    if (a.h) chunks_kernel<true><<<grid, 256, 0, s>>>(a);
+    else chunks_kernel<false><<<grid, 256, 0, s>>>(a);
   } else if (a.K <= 2048) rows >= 2048 ? launch_rows<32, 4>(a, s) : launch_rows<64, 2>(a, s);
   else if (a.K <= 4096) rows >= 2048 ? launch_rows<32, 8>(a, s) : launch_rows<256, 1>(a, s);
   else if (a.K <= 8192) rows >= 1024 ? launch_rows<64, 8>(a, s) : launch_rows<256, 2>(a, s);

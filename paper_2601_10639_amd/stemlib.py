@@ -257,7 +257,7 @@ def _load_bind():
                       "`python -m paper_2601_10639_amd.build` builds it", RuntimeWarning, stacklevel=3)
         _bind = _NoBind()
         return _bind
-    native.setup(StemCtx, torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream, stem_norm, stem_leave, StemQuant)
+    native.setup(StemCtx, torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream, stem_norm, stem_leave, StemQuant, StemQfloat)
     os.register_at_fork(after_in_child=native.off)   # torch refuses the device there
     _bind = native
     return native
@@ -744,77 +744,98 @@ def _offsets(offsets, groups: int):
 
 def stem_qfloat_linear(ctx: StemCtx, x, W: StemQfloat, y, residual=None, norm: stem_norm | None = None, offsets=None, stream=None):
     """y = Q(N(x)) W_g^T (+ residual), rows offsets[g] .. offsets[g + 1] with the g-th weights; y may be residual."""
-    dt, T = ctx.torch_dtype, x.shape[0]
-    q, _ = _qfloat(W, W.N, W.K, "W")
-    if norm is not None:
-        norm._check(ctx, W.K, "norm")
-    st = lib().stem_qfloat_linear(ctx.handle, _shaped(x, dt, (T, W.K), "x"), T, W.K, norm, q, W.N, W.groups, _offsets(offsets, W.groups),
-                                  _shaped(residual, dt, (T, W.N), "residual"), _shaped(y, dt, (T, W.N), "y"), _stream(stream))
-    _check(ctx, st, "stem_qfloat_linear")
+    st = (_bind or _load_bind()).qfloat_linear(ctx, x, W, y, residual, norm, offsets, stream)
+    if st is None:   # not the ordinary call
+        dt, T = ctx.torch_dtype, x.shape[0]
+        q, _ = _qfloat(W, W.N, W.K, "W")
+        if norm is not None:
+            norm._check(ctx, W.K, "norm")
+        st = lib().stem_qfloat_linear(ctx.handle, _shaped(x, dt, (T, W.K), "x"), T, W.K, norm, q, W.N, W.groups, _offsets(offsets, W.groups),
+                                      _shaped(residual, dt, (T, W.N), "residual"), _shaped(y, dt, (T, W.N), "y"), _stream(stream))
+    if st != STEM_OK:
+        _check(ctx, st, "stem_qfloat_linear")
 
 
 def stem_qfloat_linear_backward(ctx: StemCtx, dy, x, W: StemQfloat, dx=None, dW=None, offsets=None, accumulate: bool = False, stream=None):
     """dx = Q(dy) W_g; dW [groups, N, K] (or [N, K] of one) fp32 = dy^T x over each group's rows.  Either may be None, x without dW."""
-    dt, T = ctx.torch_dtype, dy.shape[0]
-    _, qt = _qfloat(W, W.N, W.K, "W")
-    if dW is not None and W.groups == 1 and dW.dim() == 2:
-        dW = dW.unsqueeze(0)
-    st = lib().stem_qfloat_linear_backward(ctx.handle, _shaped(dy, dt, (T, W.N), "dy"), _shaped(x, dt, (T, W.K), "x"), T, W.K, qt, W.N, W.groups,
-                                           _offsets(offsets, W.groups), _shaped(dx, dt, (T, W.K), "dx"),
-                                           _shaped(dW, torch.float32, (W.groups, W.N, W.K), "dW"), 1 if accumulate else 0, _stream(stream))
-    _check(ctx, st, "stem_qfloat_linear_backward")
+    st = (_bind or _load_bind()).qfloat_linear_backward(ctx, dy, x, W, dx, dW, offsets, accumulate, stream)
+    if st is None:   # not the ordinary call
+        dt, T = ctx.torch_dtype, dy.shape[0]
+        _, qt = _qfloat(W, W.N, W.K, "W")
+        if dW is not None and W.groups == 1 and dW.dim() == 2:
+            dW = dW.unsqueeze(0)
+        st = lib().stem_qfloat_linear_backward(ctx.handle, _shaped(dy, dt, (T, W.N), "dy"), _shaped(x, dt, (T, W.K), "x"), T, W.K, qt, W.N, W.groups,
+                                               _offsets(offsets, W.groups), _shaped(dx, dt, (T, W.K), "dx"),
+                                               _shaped(dW, torch.float32, (W.groups, W.N, W.K), "dW"), 1 if accumulate else 0, _stream(stream))
+    if st != STEM_OK:
+        _check(ctx, st, "stem_qfloat_linear_backward")
 
 
 def stem_qfloat_ffn_forward(ctx: StemCtx, x, ids, gate: StemQfloat, down: StemQfloat, E, y, residual=None, norm: stem_norm | None = None, offsets=None,
                             stream=None, E_rows=None):
     """y = Q(SiLU(Q(N(x)) gate_g^T) * E[ids]) down_g^T (+ residual); y may be x and residual."""
-    dt, T, d, F = ctx.torch_dtype, x.shape[0], ctx.d_model, ctx.d_ff
-    if gate.groups != down.groups:
-        raise ValueError(f"down: expected {gate.groups} groups, got {down.groups}")
-    gq, dq = _qfloat(gate, F, d, "gate")[0], _qfloat(down, d, F, "down")[0]
-    if norm is not None:
-        norm._check(ctx, d, "norm")
-    E_rows = E.shape[0] if E_rows is None else E_rows
-    st = lib().stem_qfloat_ffn_forward(ctx.handle, _shaped(x, dt, (T, d), "x"), _shaped(ids, torch.int32, (T,), "ids"), T, norm, gq, dq, gate.groups,
-                                       _offsets(offsets, gate.groups), _shaped(E, dt, (E.shape[0], F), "E"), E_rows,
-                                       _shaped(residual, dt, (T, d), "residual"), _shaped(y, dt, (T, d), "y"), _stream(stream))
-    _check(ctx, st, "stem_qfloat_ffn_forward")
+    st = (_bind or _load_bind()).qfloat_ffn_forward(ctx, x, ids, gate, down, E, y, residual, norm, offsets, stream, E_rows)
+    if st is None:   # not the ordinary call
+        dt, T, d, F = ctx.torch_dtype, x.shape[0], ctx.d_model, ctx.d_ff
+        if gate.groups != down.groups:
+            raise ValueError(f"down: expected {gate.groups} groups, got {down.groups}")
+        gq, dq = _qfloat(gate, F, d, "gate")[0], _qfloat(down, d, F, "down")[0]
+        if norm is not None:
+            norm._check(ctx, d, "norm")
+        E_rows = E.shape[0] if E_rows is None else E_rows
+        st = lib().stem_qfloat_ffn_forward(ctx.handle, _shaped(x, dt, (T, d), "x"), _shaped(ids, torch.int32, (T,), "ids"), T, norm, gq, dq, gate.groups,
+                                           _offsets(offsets, gate.groups), _shaped(E, dt, (E.shape[0], F), "E"), E_rows,
+                                           _shaped(residual, dt, (T, d), "residual"), _shaped(y, dt, (T, d), "y"), _stream(stream))
+    if st != STEM_OK:
+        _check(ctx, st, "stem_qfloat_ffn_forward")
 
 
 def stem_experts_sort(ctx: StemCtx, experts, src, place, offsets, stream=None):
     """experts [T, k] -> place [T, k], src [T * k], offsets [n_experts + 1]; n_experts is what offsets has room for."""
-    i32, (T, k) = torch.int32, experts.shape
-    st = lib().stem_experts_sort(ctx.handle, _shaped(experts, i32, (T, k), "experts"), T, k, offsets.shape[0] - 1, _shaped(src, i32, (T * k,), "src"),
-                                 _shaped(place, i32, (T, k), "place"), _shaped(offsets, i32, (offsets.shape[0],), "offsets"), _stream(stream))
-    _check(ctx, st, "stem_experts_sort")
+    st = (_bind or _load_bind()).experts_sort(ctx, experts, src, place, offsets, stream)
+    if st is None:   # not the ordinary call
+        i32, (T, k) = torch.int32, experts.shape
+        st = lib().stem_experts_sort(ctx.handle, _shaped(experts, i32, (T, k), "experts"), T, k, offsets.shape[0] - 1, _shaped(src, i32, (T * k,), "src"),
+                                     _shaped(place, i32, (T, k), "place"), _shaped(offsets, i32, (offsets.shape[0],), "offsets"), _stream(stream))
+    if st != STEM_OK:
+        _check(ctx, st, "stem_experts_sort")
 
 
 def stem_experts_dispatch(ctx: StemCtx, x, src, xs, choices: int, ids=None, ids_out=None, stream=None):
     """xs[r] = x[src[r] // choices], ids_out[r] = ids[src[r] // choices]; rows of a negative src are left as they were."""
-    i32, (T, width), rows = torch.int32, x.shape, src.shape[0]
-    st = lib().stem_experts_dispatch(ctx.handle, _shaped(x, ctx.torch_dtype, (T, width), "x"), T, width, _shaped(src, i32, (rows,), "src"), rows, choices,
-                                     _shaped(ids, i32, (T,), "ids"), _shaped(xs, ctx.torch_dtype, (rows, width), "xs"),
-                                     _shaped(ids_out, i32, (rows,), "ids_out"), _stream(stream))
-    _check(ctx, st, "stem_experts_dispatch")
+    st = (_bind or _load_bind()).experts_dispatch(ctx, x, src, xs, choices, ids, ids_out, stream)
+    if st is None:   # not the ordinary call
+        i32, (T, width), rows = torch.int32, x.shape, src.shape[0]
+        st = lib().stem_experts_dispatch(ctx.handle, _shaped(x, ctx.torch_dtype, (T, width), "x"), T, width, _shaped(src, i32, (rows,), "src"), rows, choices,
+                                         _shaped(ids, i32, (T,), "ids"), _shaped(xs, ctx.torch_dtype, (rows, width), "xs"),
+                                         _shaped(ids_out, i32, (rows,), "ids_out"), _stream(stream))
+    if st != STEM_OK:
+        _check(ctx, st, "stem_experts_dispatch")
 
 
 def stem_experts_combine(ctx: StemCtx, ys, place, y, weights=None, residual=None, stream=None):
     """y_t = residual_t + sum_j weights[t, j] ys[place[t, j]]; y may be residual."""
-    dt, (T, k), (rows, width) = ctx.torch_dtype, place.shape, ys.shape
-    st = lib().stem_experts_combine(ctx.handle, _shaped(ys, dt, (rows, width), "ys"), rows, width, _shaped(place, torch.int32, (T, k), "place"),
-                                    _shaped(weights, torch.float32, (T, k), "weights"), T, k, _shaped(residual, dt, (T, width), "residual"),
-                                    _shaped(y, dt, (T, width), "y"), _stream(stream))
-    _check(ctx, st, "stem_experts_combine")
+    st = (_bind or _load_bind()).experts_combine(ctx, ys, place, y, weights, residual, stream)
+    if st is None:   # not the ordinary call
+        dt, (T, k), (rows, width) = ctx.torch_dtype, place.shape, ys.shape
+        st = lib().stem_experts_combine(ctx.handle, _shaped(ys, dt, (rows, width), "ys"), rows, width, _shaped(place, torch.int32, (T, k), "place"),
+                                        _shaped(weights, torch.float32, (T, k), "weights"), T, k, _shaped(residual, dt, (T, width), "residual"),
+                                        _shaped(y, dt, (T, width), "y"), _stream(stream))
+    if st != STEM_OK:
+        _check(ctx, st, "stem_experts_combine")
 
 
 def stem_experts_combine_backward(ctx: StemCtx, dy, place, dys=None, ys=None, weights=None, dweights=None, stream=None):
     """dys[place[t, j]] = weights[t, j] dy_t, dweights[t, j] = <dy_t, ys[place[t, j]]>; either may be None."""
-    dt, (T, k), width = ctx.torch_dtype, place.shape, dy.shape[1]
-    rows = next((t.shape[0] for t in (dys, ys) if t is not None), 0)
-    st = lib().stem_experts_combine_backward(ctx.handle, _shaped(dy, dt, (T, width), "dy"), _shaped(ys, dt, (rows, width), "ys"), rows, width,
-                                             _shaped(place, torch.int32, (T, k), "place"), _shaped(weights, torch.float32, (T, k), "weights"), T, k,
-                                             _shaped(dys, dt, (rows, width), "dys"), _shaped(dweights, torch.float32, (T, k), "dweights"), _stream(stream))
-    _check(ctx, st, "stem_experts_combine_backward")
+    st = (_bind or _load_bind()).experts_combine_backward(ctx, dy, place, dys, ys, weights, dweights, stream)
+    if st is None:   # not the ordinary call
+        dt, (T, k), width = ctx.torch_dtype, place.shape, dy.shape[1]
+        rows = next((t.shape[0] for t in (dys, ys) if t is not None), 0)
+        st = lib().stem_experts_combine_backward(ctx.handle, _shaped(dy, dt, (T, width), "dy"), _shaped(ys, dt, (rows, width), "ys"), rows, width,
+                                                 _shaped(place, torch.int32, (T, k), "place"), _shaped(weights, torch.float32, (T, k), "weights"), T, k,
+                                                 _shaped(dys, dt, (rows, width), "dys"), _shaped(dweights, torch.float32, (T, k), "dweights"), _stream(stream))
+    if st != STEM_OK:
+        _check(ctx, st, "stem_experts_combine_backward")
 
 
 def stem_profile_enable(ctx: StemCtx, on: bool):
