@@ -7,7 +7,10 @@
 namespace {
 
 constexpr int64_t MAX_CHANNELS = 1 << 22;
-constexpr int64_t QFLOAT_HIDDEN_INLINE = 4;   // rows whose fp32 hidden values every workgroup of the down product makes its operands of
+// The layer of up to 8 rows: its gate product leaves fp32 hidden values, of which every workgroup of the down product makes its operands where they are few, else a
+// kernel between the two.  More rows: tiles of the gate product leave 8 bits.  us, the whole layer, hidden values inline / by a kernel: 2048 x 8192, 1, 4, 8 rows
+// 13.5 / 17.4, 16.7 / 18.1, 20.1 / 18.1; 1024 x 4096 8.4 / 11.8 at one row, 11.5 / 12.3 at 8, 16.6 / 14.3 at 16.
+constexpr int64_t GATE_ROWS = 8, HIDDEN_INLINE = 32768;
 constexpr int64_t MAX_FORM = INT32_MAX;   // elements of a form, which kernels address with 32 bits
 
 int64_t widest(const stem_ctx* c) { return std::max(c->desc.d_model, c->desc.d_ff); }
@@ -58,15 +61,12 @@ QfloatDecodeArgs decode_args(const Form& b, int64_t stride_b, int64_t N, int64_t
   r.B = b.q; r.sb = b.scale; r.stride_b = stride_b;
   r.N = (int)N; r.K = (int)stem_qfloat_pitch(K); r.row_K = (int)K;
   r.groups = g;
-  const int rows = (g.T + g.n - 1) / g.n;   // of an average group
-  r.nt = rows <= 16 ? 1 : rows <= 32 ? 2 : 4;
   return r;
 }
-bool few_rows(const QfloatGroups& g) { return (g.T + g.n - 1) / g.n <= QFLOAT_DECODE_ROWS; }
 
 // The rows of a decode product: in place, or their form, which a kernel makes before it
 hipError_t decode_rows(stem_ctx* c, const void* x, int64_t K, const stem_norm* norm, bool in_place, const Form& f, QfloatDecodeArgs& a, hipStream_t s) {
-  if (in_place && a.nt == 1 && stem_qfloat_decode_inline(a.groups.T, K, norm && norm->kind != STEM_NORM_NONE)) {
+  if (in_place && stem_qfloat_decode_inline(a.groups.T, K)) {
     a.x = static_cast<const bf16_t*>(x);
     a.norm = norm ? *norm : stem_norm{STEM_NORM_NONE, 0.f, nullptr};
     return hipSuccess;
@@ -142,7 +142,7 @@ stem_status stem_qfloat_linear(stem_ctx* c, const void* x, int64_t T, int64_t K,
   hipStream_t s = static_cast<hipStream_t>(stream);
   const QfloatGroups g = {offsets, groups, (int)T};
   const Form f = form(c->qfloat_x, rows, K);
-  if (few_rows(g)) {
+  if (stem_route_qfloat_few(T, offsets != nullptr, (int)N, (int)K)) {
     QfloatDecodeArgs a = decode_args(form(q, N, K), stem_qfloat_form(N, K), N, K, g);
     a.y = static_cast<bf16_t*>(y); a.residual = static_cast<const bf16_t*>(residual);
     // (in place every workgroup reads x, also when others have written their part of y)
@@ -238,20 +238,17 @@ stem_status stem_qfloat_ffn_forward(stem_ctx* c, const void* x, const int32_t* i
   hipStream_t s = static_cast<hipStream_t>(stream);
   const QfloatGroups g = {offsets, groups, (int)T};
   const Form f = form(c->qfloat_x, rows, d), h = form(c->qfloat_h, rows, F);
-  if (few_rows(g) && T * F * 4 <= QFLOAT_WS) {
+  QfloatDecodeArgs b = decode_args(form(down_q, d, F), stem_qfloat_form(d, F), d, F, g);
+  b.y = static_cast<bf16_t*>(y); b.residual = static_cast<const bf16_t*>(residual);
+  b.A = h.q; b.sa = h.scale; b.a_bytes = h.bytes;
+  if (T <= GATE_ROWS && T * F * 4 <= QFLOAT_WS) {
     QfloatDecodeArgs a = decode_args(form(gate_q, F, d), stem_qfloat_form(F, d), F, d, g);
     a.h_out = c->qfloat_ws;
     a.ids = ids; a.E = static_cast<const bf16_t*>(E); a.E_rows = (int)E_rows; a.flag = c->flag;
     HIP_TRY(c, decode_rows(c, x, d, norm, true, f, a, s));
     HIP_TRY(c, stem_qfloat_decode_launch(c, K_QFLOAT_GATE, a, s));
-    QfloatDecodeArgs b = decode_args(form(down_q, d, F), stem_qfloat_form(d, F), d, F, g);
-    b.y = static_cast<bf16_t*>(y); b.residual = static_cast<const bf16_t*>(residual);
-    if (T <= QFLOAT_HIDDEN_INLINE) {
-      b.h = c->qfloat_ws;
-    } else {
-      HIP_TRY(c, stem_qfloat_rows_launch(c, {nullptr, c->qfloat_ws, g, (int)F, {STEM_NORM_NONE, 0.f, nullptr}, h.q, h.scale}, s));
-      b.A = h.q; b.sa = h.scale; b.a_bytes = h.bytes;
-    }
+    if (T * F <= HIDDEN_INLINE && stem_qfloat_decode_inline(T, F)) b.h = c->qfloat_ws;
+    else HIP_TRY(c, stem_qfloat_rows_launch(c, {nullptr, c->qfloat_ws, g, (int)F, {STEM_NORM_NONE, 0.f, nullptr}, h.q, h.scale}, s));
     HIP_TRY(c, stem_qfloat_decode_launch(c, K_QFLOAT_LINEAR, b, s));
     return STEM_OK;
   }
@@ -260,6 +257,10 @@ stem_status stem_qfloat_ffn_forward(stem_ctx* c, const void* x, const int32_t* i
   a.hq = h.q; a.hs = h.scale;
   a.ids = ids; a.E = static_cast<const bf16_t*>(E); a.E_rows = (int)E_rows; a.flag = c->flag;
   HIP_TRY(c, stem_qfloat_gemm_launch(c, K_QFLOAT_GATE, QFLOAT_HIDDEN, a, s));
+  if (stem_route_qfloat_few(T, offsets != nullptr, (int)d, (int)F)) {
+    HIP_TRY(c, stem_qfloat_decode_launch(c, K_QFLOAT_LINEAR, b, s));
+    return STEM_OK;
+  }
   a = gemm_args(c, h, form(down_q, d, F), stem_qfloat_form(d, F), T, d, F, g);
   a.y = static_cast<bf16_t*>(y); a.residual = static_cast<const bf16_t*>(residual);
   HIP_TRY(c, stem_qfloat_gemm_launch(c, K_QFLOAT_LINEAR, QFLOAT_BF16, a, s));

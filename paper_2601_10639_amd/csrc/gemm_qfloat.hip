@@ -81,57 +81,33 @@ struct Work {
 };
 template <int TM, int TN, bool BY_K>
 __device__ __forceinline__ bool find_work(const QfloatGemmArgs& p, int lane, Work& w) {
-  const int ntn = (p.N + TN - 1) / TN, nk_all = p.K / 128;
-  int b = blockIdx.x;
-  w.slice = 0; w.k0 = 0; w.nk = nk_all;
+  const int ntn = (p.N + TN - 1) / TN, nk_all = p.K / 128, all_rows = (p.M + TM - 1) / TM;
+  const bool grouped = p.groups.offsets != nullptr;
+  const int ntm = BY_K || !grouped ? all_rows : qfloat_tiles<TM>(p.groups, lane), tiles = ntm * ntn;
+  const int part = tiles ? blockIdx.x / tiles : 1, b = blockIdx.x - part * tiles;   // of K: a group, a slice
+  if (!BY_K && grouped && part > 0) return false;
   int tm, tn;
-  if constexpr (BY_K) {                                     // all of the output for each group of K
-    const int ntm = (p.M + TM - 1) / TM;
-    w.tiles = ntm * ntn;
-    const int part = b / w.tiles;
-    w.group = p.groups.offsets ? part : 0;
-    b -= part * w.tiles;
-    tile_of(b, w.tiles, ntm, ntn, tm, tn);
-    w.m0 = w.pa = tm * TM;
-    w.rows = p.M - w.m0;
-    if (p.groups.offsets) {
-      int k0 = 0, nk = 0;
-      qfloat_scan<128>(p.groups, lane, [&](int i, int, int rows, int, int, int padded) __attribute__((always_inline)) {
-        const uint64_t mine = __ballot(i == w.group);
-        if (!mine) return false;
-        const int l = __builtin_ctzll(mine);
-        k0 = __builtin_amdgcn_readlane(padded, l) / 64;     // (bf16: 64 rows a K tile)
-        nk = (__builtin_amdgcn_readlane(rows, l) + 63) / 64;
-        return true;
-      });
-      w.k0 = k0; w.nk = nk;
-    } else {
-      w.slice = part;
-    }
-  } else if (p.groups.offsets) {
-    w.tiles = qfloat_tiles<TM>(p.groups, lane) * ntn;
-    if (b >= w.tiles) return false;
-    tile_of(b, w.tiles, w.tiles / ntn, ntn, tm, tn);
-    QfloatTile t;
+  tile_of(b, tiles, ntm, ntn, tm, tn);
+  QfloatTile t = {0, tm * TM, p.M - tm * TM, tm * TM};
+  int k0 = 0, nk = nk_all;
+  if (BY_K && grouped) {                                     // all of the output for each group of K
+    t.group = part;
+    qfloat_scan<128>(p.groups, lane, [&](int i, int, int rows, int, int, int padded) __attribute__((always_inline)) {
+      const uint64_t mine = __ballot(i == part);
+      if (!mine) return false;
+      const int l = __builtin_ctzll(mine);
+      k0 = __builtin_amdgcn_readlane(padded, l) / 64;       // (bf16: 64 rows a K tile)
+      nk = (__builtin_amdgcn_readlane(rows, l) + 63) / 64;
+      return true;
+    });
+  } else if (grouped) {
     if (!qfloat_tile<TM>(p.groups, tm, lane, t)) return false;
-    w.group = t.group; w.m0 = t.row; w.rows = t.rows; w.pa = t.padded;
-  } else {
-    const int ntm = (p.M + TM - 1) / TM;
-    w.tiles = ntm * ntn;
-    w.slice = b / w.tiles;
-    b -= w.slice * w.tiles;
-    tile_of(b, w.tiles, ntm, ntn, tm, tn);
-    w.group = 0;
-    w.m0 = w.pa = tm * TM;
-    w.rows = p.M - w.m0;
-  }
-  w.tile = tm * ntn + tn;
-  w.n0 = tn * TN;
-  if (p.ksplit > 1) {
+  } else if (p.ksplit > 1) {
     const int per = (nk_all + p.ksplit - 1) / p.ksplit;
-    w.k0 = w.slice * per;
-    w.nk = nk_all - w.k0 < per ? nk_all - w.k0 : per;
+    k0 = part * per;
+    nk = nk_all - k0 < per ? nk_all - k0 : per;
   }
+  w = {t.row, t.rows, t.padded, tn * TN, k0, nk, t.group, tm * ntn + tn, tiles, grouped ? 0 : part};
   return true;
 }
 
@@ -312,11 +288,9 @@ __device__ __forceinline__ void load_ids(const QfloatGemmArgs& p, int m0, int ro
 // instruction takes as long for the same bytes.
 constexpr int SLOT = 32768;
 
-template <QfloatOut OUT>
 __global__ __launch_bounds__(256) void ring_kernel(QfloatGemmArgs p) {
   typedef Output<4, 4, false> Out;
-  typedef Hidden<4> Hid;
-  static_assert(4 * Out::BYTES <= 5 * SLOT && 4 * Hid::BYTES <= 5 * SLOT, "room for the epilogue");
+  static_assert(4 * Out::BYTES <= 5 * SLOT, "room for the epilogue");
   __shared__ __attribute__((aligned(16))) char smem[5 * SLOT];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wm = wave >> 1, wn = wave & 1;
@@ -325,8 +299,6 @@ __global__ __launch_bounds__(256) void ring_kernel(QfloatGemmArgs p) {
   const int nk = p.K / 128, kbytes = nk * 4096;
   const int64_t b_bytes = stem_qfloat_pitch(p.N) * p.K;
   const uint8_t *const B = p.B + w.group * p.stride_b, *const sb = p.sb + w.group * p.stride_b;
-  int id[2];
-  if (OUT == QFLOAT_HIDDEN) load_ids<4>(p, w.m0 + wm * 128, w.rows - wm * 128, lane, id);
   Loader<256, 4> la, lb;
   la.init(p.A, p.a_bytes, w.rows, p.K, w.pa, wave, lane);
   lb.init(B, b_bytes, p.N - w.n0, p.K, w.n0, wave, lane);
@@ -431,8 +403,122 @@ __global__ __launch_bounds__(256) void ring_kernel(QfloatGemmArgs p) {
   if (kt + 3 < nk) ring_iteration(3);
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
   __syncthreads();
-  if constexpr (OUT == QFLOAT_HIDDEN) Hid::run(p, acc, id, smem + wave * Hid::BYTES, w.pa + wm * 128, w.n0 + wn * 128, w.rows - wm * 128, lane);
-  else Out::run(p, acc, smem + wave * Out::BYTES, w.m0 + wm * 128, w.n0 + wn * 128, w.rows - wm * 128, 0, lane);
+  Out::run(p, acc, smem + wave * Out::BYTES, w.m0 + wm * 128, w.n0 + wn * 128, w.rows - wm * 128, 0, lane);
+}
+
+// ---- 128 x 256, two workgroups a compute unit -----------------------------------------------------------------------------------------
+// 4 wavefronts of 2 x 4 accumulators, K tiles of 64 in a ring of three 24 KB slots: one workgroup's first loads and epilogue, which the gate product has a long
+// one of, run beside the other's products.  A K tile is one k-step: its fragments are read while the one before is multiplied, and its slot is free then.
+constexpr int PAIR_A = 8192, PAIR_SLOT = 24576;
+
+template <QfloatOut OUT>
+__global__ __launch_bounds__(256, 2) void pair_kernel(QfloatGemmArgs p) {
+  typedef Output<2, 4, false> Out;
+  typedef Hidden<2> Hid;
+  static_assert(4 * Hid::BYTES <= 3 * PAIR_SLOT && 4 * Out::BYTES <= 3 * PAIR_SLOT, "room for the epilogue");
+  __shared__ __attribute__((aligned(16))) char smem[3 * PAIR_SLOT];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int wm = wave >> 1, wn = wave & 1;
+  Work w;
+  if (!find_work<128, 256, false>(p, lane, w)) return;
+  const int nk = p.K / 64, nkb = p.K / 128, kbytes = p.K * 32;
+  const int64_t b_bytes = stem_qfloat_pitch(p.N) * p.K;
+  const uint8_t *const B = p.B + w.group * p.stride_b, *const sb = p.sb + w.group * p.stride_b;
+  int id[1];
+  if (OUT == QFLOAT_HIDDEN) load_ids<2>(p, w.m0 + wm * 64, w.rows - wm * 64, lane, id);
+  const rsrc_t none = resource(p.A, 0);
+  rsrc_t ra = resource(p.A, p.a_bytes), rb = resource(B, b_bytes);
+  Scales ca, cb;
+  ca.init(p.sa, p.a_bytes / 128, w.pa + wm * 64, nkb, lane);
+  cb.init(sb, b_bytes / 128, w.n0 + wn * 128, nkb, lane);
+  // a wavefront loads one 32-row group of the tokens and two of the weights: 2 KB of each and K tile
+  const uint32_t oa = wave * 32 < w.rows ? (uint32_t)((w.pa + wave * 32) * p.K + lane * 16) : OOB;
+  uint32_t ob[2];
+#pragma unroll
+  for (int h = 0; h < 2; ++h) ob[h] = w.n0 + wave * 64 + h * 32 < p.N ? (uint32_t)((w.n0 + wave * 64 + h * 32) * p.K + lane * 16) : OOB;
+  int ks = nk >= 32 ? (int)(blockIdx.x & 7) * (nk >> 4) : 0, k = ks * 4096, left = nk;   // (blocks of 128)
+  auto issue = [&](int q, char* slot) __attribute__((always_inline)) {   // load q of 6
+    if (q < 2) lds_dma_16(ra, slot + (wave * 2 + q) * 1024, oa, k + q * 1024);
+    else lds_dma_16(rb, slot + PAIR_A + (wave * 4 + q - 2) * 1024, ob[(q - 2) >> 1], k + (q & 1) * 1024);
+  };
+  auto next = [&]() __attribute__((always_inline)) {
+    k += 2048;
+    if (k >= kbytes) k = 0;
+    if (--left <= 0) ra = rb = none;
+  };
+  f32x16_t acc[2][4];
+#pragma unroll
+  for (int i = 0; i < 2; ++i)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) acc[i][j] = f32x16_t{};
+  i32x8_t xa[2], xb[4], ya[2], yb[4];
+  const char* const fa = smem + wm * 4096 + lane * 16;
+  const char* const fb = smem + PAIR_A + wn * 8192 + lane * 16;
+  auto read = [&](int slot, int q, i32x8_t(&a)[2], i32x8_t(&b)[4]) __attribute__((always_inline)) {   // a0 b0 b1 a1 b2 b3
+    constexpr int isA[6] = {1, 0, 0, 1, 0, 0}, idx[6] = {0, 0, 1, 1, 2, 3};
+    const char* const at = (isA[q] ? fa : fb) + slot * PAIR_SLOT + idx[q] * 2048;
+    (isA[q] ? a[idx[q]] : b[idx[q]]) = join(*reinterpret_cast<const i32x4_t*>(at), *reinterpret_cast<const i32x4_t*>(at + 1024));
+  };
+  uint32_t sa = ca.load(ks) >> ca.shift, sb_ = cb.load(ks), na = 0, nb = 0;
+#pragma unroll
+  for (int st = 0; st < 3; ++st) {
+#pragma unroll
+    for (int q = 0; q < 6; ++q) issue(q, smem + st * PAIR_SLOT);
+    next();
+  }
+  asm volatile("s_waitcnt vmcnt(%0)" ::"n"(12) : "memory");
+  __builtin_amdgcn_s_barrier();
+  __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+  for (int q = 0; q < 6; ++q) read(0, q, xa, xb);
+  // K tile t in slot t mod 3.  Its turn begins when its fragments are in everybody's registers and t + 1 has landed: t + 3 is requested into its slot.
+  auto iteration = [&](const int st, const bool even, i32x8_t(&a)[2], i32x8_t(&b)[4], i32x8_t(&c)[2], i32x8_t(&d)[4]) __attribute__((always_inline)) {
+    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(6) : "memory");
+    __builtin_amdgcn_s_barrier();
+    __builtin_amdgcn_sched_barrier(0);
+    if (even) {
+      if (++ks >= nkb) ks = 0;
+      na = ca.load(ks);
+      nb = cb.load(ks);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    each([&](auto U) __attribute__((always_inline)) {
+      constexpr int u = decltype(U)::value;
+      constexpr int ii[8] = {0, 0, 1, 1, 0, 1, 0, 1}, jj[8] = {0, 1, 0, 1, 2, 2, 3, 3};
+      if (u < 6) {
+        read((st + 1) % 3, u, c, d);
+        issue(u, smem + st * PAIR_SLOT);
+      }
+      acc[ii[u]][jj[u]] = mma<jj[u], ii[u]>(b[jj[u]], a[ii[u]], acc[ii[u]][jj[u]], sb_, sa);
+      __builtin_amdgcn_sched_barrier(0);
+    }, std::make_integer_sequence<int, 8>{});
+    next();
+    if (!even) {
+      sa = na >> ca.shift;
+      sb_ = nb;
+    }
+  };
+  int kt = 0;
+  for (; kt + 6 <= nk; kt += 6) {
+    iteration(0, true, xa, xb, ya, yb);
+    iteration(1, false, ya, yb, xa, xb);
+    iteration(2, true, xa, xb, ya, yb);
+    iteration(0, false, ya, yb, xa, xb);
+    iteration(1, true, xa, xb, ya, yb);
+    iteration(2, false, ya, yb, xa, xb);
+  }
+  if (kt < nk) {                                               // (an even number is left)
+    iteration(0, true, xa, xb, ya, yb);
+    iteration(1, false, ya, yb, xa, xb);
+    if (kt + 2 < nk) {
+      iteration(2, true, xa, xb, ya, yb);
+      iteration(0, false, ya, yb, xa, xb);
+    }
+  }
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+  __syncthreads();
+  if constexpr (OUT == QFLOAT_HIDDEN) Hid::run(p, acc, id, smem + wave * Hid::BYTES, w.pa + wm * 64, w.n0 + wn * 128, w.rows - wm * 64, lane);
+  else Out::run(p, acc, smem + wave * Out::BYTES, w.m0 + wm * 64, w.n0 + wn * 128, w.rows - wm * 64, 0, lane);
 }
 
 // ---- tiles with wavefronts that load: STAGES whole K tiles in LDS ----------------------------------------------------------------------
@@ -618,6 +704,7 @@ __global__ __launch_bounds__((C::WAVES + C::LW) * 64) void tile_kernel(QfloatGem
 typedef Tiling<2, 2, 2, 2, 4, 4> Tile128;       // 128 x 128, 128 KB of LDS
 typedef Tiling<2, 1, 2, 2, 6, 4> Tile128x64;    // 144 KB
 typedef Tiling<1, 4, 4, 1, 4, 4> Hidden128;     // 128 x 128, a wavefront with whole blocks of 128 channels
+typedef Tiling<1, 4, 2, 1, 6, 4> Hidden64;      // 64 x 128
 
 template <QfloatOut OUT>
 unsigned grid_of(const QfloatGemmArgs& a, int tm, int tn) {
@@ -636,18 +723,46 @@ hipError_t launch(const QfloatGemmArgs& a, hipStream_t s) {
 
 }  // namespace
 
+// ---- choice of the tile and of the K slices ----------------------------------------------------------------------------------------
+extern "C" void stem_route_qfloat(int64_t T, int groups, int N, int K, int out, int64_t ws_bytes, int32_t* route) {
+  const int64_t per_group = (T + groups - 1) / groups;       // of an average group, which is all that is known here
+  auto tiles = [&](int tm, int tn) { return (per_group + tm - 1) / tm * groups * ((N + tn - 1) / tn); };
+  const int nk = K / 128;
+  int rows = 128, cols = 128, slices = 1;
+  if (out == QFLOAT_HIDDEN) {
+    if (tiles(64, 128) <= 256) rows = 64;
+    else if (tiles(128, 128) > 256) cols = 256;
+  } else if (out == QFLOAT_BF16) {
+    if (tiles(128, 64) <= 256) cols = 64;
+    else if (tiles(128, 128) > 256) cols = 256;
+    if (cols == 256 && nk >= 32) {
+      // rounds of 256 x 256, and of 128 x 256 in their terms: two of these a compute unit, and the last round's alone are faster
+      const int64_t pair = tiles(128, 256), last = pair % 512;
+      const double few = 1.1 * (double)(pair / 512) + (last == 0 ? 0 : last <= 256 ? 0.72 : 1.1);
+      if ((double)((tiles(256, 256) + 255) / 256) <= few) rows = 256;
+    }
+  }
+  if (out != QFLOAT_HIDDEN && cols <= 128 && groups == 1) {
+    slices = nk < 32 ? 1 : (int)std::min<int64_t>({MAX_SLICES, nk / 10, 240 / tiles(rows, cols)});
+    while (slices > 1 && (slices * tiles(rows, cols) * rows * cols * 4 > ws_bytes || tiles(rows, cols) > STEM_TICKETS)) --slices;
+    while (slices > 1 && (nk + slices - 1) / slices * (slices - 1) >= nk) --slices;   // every slice has a part of K
+    if (slices < 1) slices = 1;
+  }
+  route[0] = rows; route[1] = cols; route[2] = slices;
+}
+
 hipError_t stem_qfloat_gemm_launch(stem_ctx* ctx, int kid, QfloatOut out, const QfloatGemmArgs& p, hipStream_t s) {
   ProfScope prof(ctx, kid, s);
   QfloatGemmArgs a = p;
-  a.ksplit = 1;
+  int32_t route[3];
+  // (all of a weight gradient's output for each group)
+  stem_route_qfloat(a.M, out == QFLOAT_F32 ? 1 : a.groups.n, a.N, a.K, out, a.ws_bytes, route);
+  a.ksplit = a.groups.offsets ? 1 : route[2];
   if (out == QFLOAT_F32) return launch<QFLOAT_F32, Tile128>(a, s);
-  // of an average group, which is all that is known here
-  const int64_t rows = (a.groups.T + a.groups.n - 1) / a.groups.n, tiles = (rows + 255) / 256 * a.groups.n * ((a.N + 255) / 256);
-  if (tiles > 128 && rows >= 256) {
-    if (out == QFLOAT_HIDDEN) ring_kernel<QFLOAT_HIDDEN><<<grid_of<QFLOAT_HIDDEN>(a, 256, 256), 256, 0, s>>>(a);
-    else ring_kernel<QFLOAT_BF16><<<grid_of<QFLOAT_BF16>(a, 256, 256), 256, 0, s>>>(a);
-    return hipGetLastError();
-  }
-  if (out == QFLOAT_HIDDEN) return launch<QFLOAT_HIDDEN, Hidden128>(a, s);
-  return launch<QFLOAT_BF16, Tile128>(a, s);
+  if (route[0] == 256) ring_kernel<<<grid_of<QFLOAT_BF16>(a, 256, 256), 256, 0, s>>>(a);
+  else if (route[1] == 256 && out == QFLOAT_HIDDEN) pair_kernel<QFLOAT_HIDDEN><<<grid_of<QFLOAT_HIDDEN>(a, 128, 256), 256, 0, s>>>(a);
+  else if (route[1] == 256) pair_kernel<QFLOAT_BF16><<<grid_of<QFLOAT_BF16>(a, 128, 256), 256, 0, s>>>(a);
+  else if (out == QFLOAT_HIDDEN) return route[0] == 64 ? launch<QFLOAT_HIDDEN, Hidden64>(a, s) : launch<QFLOAT_HIDDEN, Hidden128>(a, s);
+  else return route[1] == 64 ? launch<QFLOAT_BF16, Tile128x64>(a, s) : launch<QFLOAT_BF16, Tile128>(a, s);
+  return hipGetLastError();
 }

@@ -100,7 +100,6 @@ struct QfloatDecodeArgs {
   int64_t a_bytes, stride_b;
   int N, K;                 // K: padded
   QfloatGroups groups;
-  int nt;                   // 16 nt rows of a form to a workgroup: 1, 2 or 4
   const bf16_t* x;
   int row_K;
   stem_norm norm;
@@ -113,9 +112,8 @@ struct QfloatDecodeArgs {
   int E_rows;
   int32_t* flag;
 };
-bool stem_qfloat_decode_inline(int64_t rows, int64_t K, bool normed);
+bool stem_qfloat_decode_inline(int64_t rows, int64_t K);
 hipError_t stem_qfloat_decode_launch(stem_ctx* ctx, int kid, const QfloatDecodeArgs& a, hipStream_t s);
-#define QFLOAT_DECODE_ROWS 64   // of a group, on average, up to which its products are those of few rows
 
 #define QFLOAT_WS (256ll * 128 * 128 * 4)   // bytes: a product is cut into 256 workgroups at most
 
@@ -183,19 +181,19 @@ __device__ __forceinline__ bool qfloat_tile(const QfloatGroups& G, int t, int la
     out = {0, t * TM, G.T - t * TM, t * TM};
     return t * TM < G.T;
   }
-  bool found = false;
+  int group = -1, row = 0, left = 0, place = 0;
   qfloat_scan<TM>(G, lane, [&](int i, int lo, int rows, int before, int nt, int padded) __attribute__((always_inline)) {
     const uint64_t mine = __ballot(t >= before && t < before + nt);
     if (!mine) return false;
     const int l = __builtin_ctzll(mine), in = (t - __builtin_amdgcn_readlane(before, l)) * TM;
-    out.group = __builtin_amdgcn_readlane(i, l);
-    out.row = __builtin_amdgcn_readlane(lo, l) + in;
-    out.rows = __builtin_amdgcn_readlane(rows, l) - in;
-    out.padded = __builtin_amdgcn_readlane(padded, l) + in;
-    found = true;
+    group = __builtin_amdgcn_readlane(i, l);
+    row = __builtin_amdgcn_readlane(lo, l) + in;
+    left = __builtin_amdgcn_readlane(rows, l) - in;
+    place = __builtin_amdgcn_readlane(padded, l) + in;
     return true;
   });
-  return found;
+  out = {group, row, left, place};
+  return group >= 0;
 }
 // tiles of TM rows of all groups
 template <int TM>
