@@ -349,7 +349,7 @@ stem_status stem_create(stem_ctx** out, const stem_layer_desc* desc, int64_t max
   }
   ok(dmalloc(&c->sort_counts, (size_t)stem_sort_count_entries(std::max<int64_t>(max_tokens, 1))));
   ok(dmalloc(&c->seg_of, (size_t)max_tokens));
-  ok(dmalloc(&c->experts_counts, (size_t)(max_tokens * STEM_EXPERTS_MAX_CHOICES / EXPERTS_SEGMENT + 1) * (STEM_EXPERTS_MAX + 1)));
+  ok(dmalloc(&c->experts_counts, (size_t)stem_experts_segments(max_tokens * STEM_EXPERTS_MAX_CHOICES) * (STEM_EXPERTS_MAX + 1)));
   ok(dmalloc(&c->seg_part, (size_t)stem_seg_chunks(std::max<int64_t>(max_tokens, 1)) * 2 * desc->d_ff));
   int64_t block_bytes;
   switch (stem_route_block_scratch(desc->d_model, desc->d_ff, desc->dtype, max_tokens, &block_bytes)) {

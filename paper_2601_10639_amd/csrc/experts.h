@@ -2,7 +2,9 @@
 #pragma once
 #include "stem_internal.h"
 
-#define EXPERTS_SEGMENT 4096   // (token, choice) pairs that a workgroup of the sort counts and places
+// (token, choice) pairs up to which a workgroup of the sort has 1024 of them, and 4096 beyond; and the most segments that sorts of up to this many have
+#define EXPERTS_SMALL 65536
+inline int64_t stem_experts_segments(int64_t pairs) { return EXPERTS_SMALL / 1024 + pairs / 4096; }
 
 struct ExpertsSortArgs {
   const int32_t* experts;   // [pairs]

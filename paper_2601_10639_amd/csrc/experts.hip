@@ -21,7 +21,7 @@ namespace {
 // atomics: the order is the pairs' own.  Pairs of no expert (negative, or none of the n, which is reported) are kept as expert n: they get
 // place -1, and the rows behind the last expert's get src -1.
 // PLACE: the counts are taken again and the pairs placed; otherwise they are stored for the kernel that does.
-constexpr int WAVES = EXPERTS_SEGMENT / 256, TURNS = EXPERTS_SEGMENT / 64 / WAVES;
+constexpr int TURNS = 4;
 
 __device__ __forceinline__ void in_order() {                // of LDS, within the wavefront
   __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
@@ -29,13 +29,13 @@ __device__ __forceinline__ void in_order() {                // of LDS, within th
   __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
 }
 
-template <bool PLACE>
+template <int WAVES, bool PLACE>
 __global__ __launch_bounds__(WAVES * 64) void sort_kernel(ExpertsSortArgs p, int segments, int bits) {
   extern __shared__ int32_t table[];                        // [WAVES][n + 1], then [n + 1] of first rows
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n = p.n, pitch = n + 1;
   int32_t* const mine = table + wave * pitch;
   int32_t* const first = table + WAVES * pitch;
-  const int at = blockIdx.x * EXPERTS_SEGMENT + wave * (64 * TURNS) + lane;
+  const int at = blockIdx.x * (WAVES * 64 * TURNS) + wave * (64 * TURNS) + lane;
   for (int e = threadIdx.x; e < WAVES * pitch; e += WAVES * 64) table[e] = 0;
   int expert[TURNS], rank[TURNS];
 #pragma unroll
@@ -80,10 +80,15 @@ __global__ __launch_bounds__(WAVES * 64) void sort_kernel(ExpertsSortArgs p, int
   if (segments > 1)
     for (int e = threadIdx.x; e <= n; e += WAVES * 64) {
       int all = 0, before = 0;
-      for (int s = 0; s < segments; ++s) {
-        const int c = p.counts[(int64_t)s * pitch + e];
-        before += s < (int)blockIdx.x ? c : 0;
-        all += c;
+      for (int s0 = 0; s0 < segments; s0 += 16) {              // 16 under way together
+        int c[16];
+#pragma unroll
+        for (int u = 0; u < 16; ++u) c[u] = p.counts[(int64_t)min(s0 + u, segments - 1) * pitch + e];
+#pragma unroll
+        for (int u = 0; u < 16; ++u) {
+          all += s0 + u < segments ? c[u] : 0;
+          before += s0 + u < (int)blockIdx.x ? c[u] : 0;
+        }
       }
       first[e] = all;
       for (int w = 0; w < WAVES; ++w) table[w * pitch + e] += before;
@@ -118,153 +123,249 @@ __global__ __launch_bounds__(WAVES * 64) void sort_kernel(ExpertsSortArgs p, int
 }
 
 // ---- rows ------------------------------------------------------------------------------------------------------------------
-// BYTES: 16 where rows are whole vectors, else one element
-template <class E>
-__device__ __forceinline__ float to_float(E v) {
-  if constexpr (sizeof(E) == 2) return __uint_as_float((uint32_t)v << 16);
-  else return v;
-}
-template <class E>
-__device__ __forceinline__ E from_float(float v) {
-  if constexpr (sizeof(E) == 2) return __builtin_bit_cast(uint16_t, (__bf16)v);
-  else return v;
+// LPR neighbouring lanes have a row or a token, pieces of V elements (16 bytes, at any element's address; rows of fewer elements: one) a lane at a time, and U of
+// them are under way together: loads behind a store that may lie over what they read would wait for it.  A row's last piece ends where the row does and
+// has elements of the one before it again where the row is no whole number of pieces; pieces beyond it are loaded as it is, so that no load has a branch, and
+// not stored.
+// (vectors, not arrays of elements: those the compiler keeps in LDS)
+template <int BYTES> struct RawOf;
+template <> struct RawOf<16> { typedef u32x4_t type; };
+template <> struct RawOf<4> { typedef uint32_t type; };
+template <> struct RawOf<2> { typedef uint16_t type; };
+template <class E, int V>
+using Raw = typename RawOf<V * sizeof(E)>::type;
+template <class E, int V>
+__device__ __forceinline__ float element(const Raw<E, V>& p, int q) {
+  uint32_t w;
+  if constexpr (V > 1) w = p[q * sizeof(E) / 4];
+  else w = p;
+  if constexpr (sizeof(E) == 2) return __uint_as_float(q & 1 ? w & 0xffff0000u : w << 16);
+  else return __uint_as_float(w);
 }
 template <class E, int V>
-struct Piece { E v[V]; };
-template <class E, int V>
-__device__ __forceinline__ Piece<E, V> load(const void* base, int64_t at) {   // V elements from element `at` on
-  Piece<E, V> p;
-  __builtin_memcpy(&p, __builtin_assume_aligned(static_cast<const E*>(base) + at, V * sizeof(E)), sizeof p);
+__device__ __forceinline__ Raw<E, V> pack(const float (&f)[V]) {
+  Raw<E, V> p;
+  if constexpr (sizeof(E) == 4) {
+    if constexpr (V == 1) p = __float_as_uint(f[0]);
+    else
+#pragma unroll
+      for (int q = 0; q < V; ++q) p[q] = __float_as_uint(f[q]);
+  } else if constexpr (V == 1) {
+    p = __builtin_bit_cast(uint16_t, (__bf16)f[0]);
+  } else {
+#pragma unroll
+    for (int q = 0; q < V; q += 2)
+      p[q / 2] = (uint32_t)__builtin_bit_cast(uint16_t, (__bf16)f[q]) | (uint32_t)__builtin_bit_cast(uint16_t, (__bf16)f[q + 1]) << 16;
+  }
   return p;
 }
-template <class E, int V>
-__device__ __forceinline__ void store(void* base, int64_t at, const Piece<E, V>& p) {
-  __builtin_memcpy(__builtin_assume_aligned(static_cast<E*>(base) + at, V * sizeof(E)), &p, sizeof p);
+// U pieces of a row from element c on, `step` apart
+template <class E, int V, int U>
+__device__ __forceinline__ void load(const void* base, int64_t row, int width, int c, int step, Raw<E, V> (&p)[U]) {
+  const E* const from = static_cast<const E*>(base) + row * width;
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    Raw<E, V> v;
+    __builtin_memcpy(&v, from + min(c + u * step, width - V), sizeof v);
+    p[u] = v;
+  }
+}
+template <class E, int V, int U>
+__device__ __forceinline__ void store(void* base, int64_t row, int width, int c, int step, const Raw<E, V> (&p)[U]) {
+  E* const to = static_cast<E*>(base) + row * width;
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    const Raw<E, V> v = p[u];
+    if (c + u * step < width) __builtin_memcpy(to + min(c + u * step, width - V), &v, sizeof v);
+  }
 }
 
-// a wavefront has a row
-template <class E, int V>
+template <class E, int V, int LPR>
 __global__ __launch_bounds__(256) void dispatch_kernel(ExpertsRowsArgs p) {
-  const int lane = threadIdx.x & 63;
-  const int64_t row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+  constexpr int STEP = LPR * V, U = 4;
+  const int l = threadIdx.x % LPR, width = (int)p.width;
+  const int64_t row = (int64_t)blockIdx.x * (256 / LPR) + threadIdx.x / LPR;
   if (row >= p.rows) return;
   const int pair = p.src[row];
   if (pair < 0) return;
   int64_t t = pair / p.k;
   if (t >= p.T) {
-    if (lane == 0) *p.flag = 1;
+    if (l == 0) *p.flag = 1;
     t = p.T - 1;
   }
-  if (p.ids && lane == 0) p.ids_out[row] = p.ids[t];
-  for (int64_t c = lane * V; c < p.width; c += 64 * V) store<E, V>(p.xs, row * p.width + c, load<E, V>(p.x, t * p.width + c));
+  if (p.ids && l == 0) p.ids_out[row] = p.ids[t];
+  for (int c = 0; c < width; c += U * STEP) {
+    Raw<E, V> v[U];
+    load<E, V, U>(p.x, t, width, c + l * V, STEP, v);
+    store<E, V, U>(p.xs, row, width, c + l * V, STEP, v);
+  }
 }
 
-// a wavefront has a token
-template <class E, int V>
-__global__ __launch_bounds__(256) void combine_kernel(ExpertsRowsArgs p) {
-  const int lane = threadIdx.x & 63;
-  const int64_t t = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-  if (t >= p.T) return;
-  for (int64_t c = lane * V; c < p.width; c += 64 * V) {
-    float sum[V] = {};
-    if (p.residual) {
-      const Piece<E, V> r = load<E, V>(p.residual, t * p.width + c);
+// Places and weights of a token's choices, lane j of its lanes having the j-th (and the LPR + j-th)
+template <int LPR>
+struct Choices {
+  static constexpr int N = LPR < STEM_EXPERTS_MAX_CHOICES ? 2 : 1;
+  int place[N];
+  float weight[N];
+  __device__ __forceinline__ void load(const ExpertsRowsArgs& p, int64_t t, int l) {
 #pragma unroll
-      for (int q = 0; q < V; ++q) sum[q] = to_float(r.v[q]);
+    for (int h = 0; h < N; ++h) {
+      const int j = h * LPR + l;
+      place[h] = j < p.k ? p.place[t * p.k + j] : -1;
+      weight[h] = j < p.k && p.weights ? p.weights[t * p.k + j] : 1.f;
+    }
+  }
+  __device__ __forceinline__ int row(int j) const { return __shfl(N > 1 && j >= LPR ? place[N - 1] : place[0], j % LPR, LPR); }
+  __device__ __forceinline__ float of(int j) const { return __shfl(N > 1 && j >= LPR ? weight[N - 1] : weight[0], j % LPR, LPR); }
+};
+
+template <class E, int V, int LPR>
+__global__ __launch_bounds__(256) void combine_kernel(ExpertsRowsArgs p) {
+  constexpr int STEP = LPR * V, U = 4;
+  const int l = threadIdx.x % LPR, width = (int)p.width;
+  const int64_t t = (int64_t)blockIdx.x * (256 / LPR) + threadIdx.x / LPR;
+  if (t >= p.T) return;
+  Choices<LPR> choices;
+  choices.load(p, t, l);
+  // (a place behind the rows is the last of them, and reported)
+#pragma unroll
+  for (int& place : choices.place)
+    if (place >= p.rows) {
+      *p.flag = 1;
+      place = (int)p.rows - 1;
+    }
+  for (int c0 = 0; c0 < width; c0 += U * STEP) {
+    const int c = c0 + l * V;
+    float sum[U][V];
+    if (p.residual) {
+      Raw<E, V> v[U];
+      load<E, V, U>(p.residual, t, width, c, STEP, v);
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+#pragma unroll
+        for (int q = 0; q < V; ++q) sum[u][q] = element<E, V>(v[u], q);
+    } else {
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+#pragma unroll
+        for (int q = 0; q < V; ++q) sum[u][q] = 0.f;
     }
     for (int j = 0; j < p.k; ++j) {
-      int64_t row = p.place[t * p.k + j];
+      const int row = choices.row(j);
+      const float w = choices.of(j);
       if (row < 0) continue;
-      if (row >= p.rows) {
-        if (lane == 0) *p.flag = 1;
-        if (p.rows == 0) continue;
-        row = p.rows - 1;
-      }
-      const float w = p.weights ? p.weights[t * p.k + j] : 1.f;
-      const Piece<E, V> v = load<E, V>(p.ys, row * p.width + c);
+      Raw<E, V> v[U];
+      load<E, V, U>(p.ys, row, width, c, STEP, v);
 #pragma unroll
-      for (int q = 0; q < V; ++q) sum[q] = __builtin_fmaf(w, to_float(v.v[q]), sum[q]);
+      for (int u = 0; u < U; ++u)
+#pragma unroll
+        for (int q = 0; q < V; ++q) sum[u][q] = __builtin_fmaf(w, element<E, V>(v[u], q), sum[u][q]);
     }
-    Piece<E, V> out;
+    Raw<E, V> out[U];
 #pragma unroll
-    for (int q = 0; q < V; ++q) out.v[q] = from_float<E>(sum[q]);
-    store<E, V>(p.y, t * p.width + c, out);
+    for (int u = 0; u < U; ++u) out[u] = pack<E, V>(sum[u]);
+    store<E, V, U>(p.y, t, width, c, STEP, out);
   }
 }
 
-// a wavefront has a token
-template <class E, int V>
+template <class E, int V, int LPR>
 __global__ __launch_bounds__(256) void combine_backward_kernel(ExpertsRowsArgs p) {
-  const int lane = threadIdx.x & 63;
-  const int64_t t = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+  constexpr int STEP = LPR * V, U = 4;
+  const int l = threadIdx.x % LPR, width = (int)p.width;
+  const int64_t t = (int64_t)blockIdx.x * (256 / LPR) + threadIdx.x / LPR;
   if (t >= p.T) return;
+  Choices<LPR> choices;
+  choices.load(p, t, l);
+  const bool whole = width <= U * STEP;                        // dy's row stays in registers
+  Raw<E, V> g[U];
+  if (whole && width > 0) load<E, V, U>(p.x, t, width, l * V, STEP, g);
   for (int j = 0; j < p.k; ++j) {
-    int64_t row = p.place[t * p.k + j];
-    if (row < 0) {
-      if (p.dweights && lane == 0) p.dweights[t * p.k + j] = 0.f;
-      continue;
+    int row = choices.row(j);
+    if (row >= p.rows) {                                       // reported, and none
+      if (l == 0) *p.flag = 1;
+      row = -1;
     }
-    if (row >= p.rows) {
-      if (lane == 0) {
-        *p.flag = 1;
-        if (p.dweights) p.dweights[t * p.k + j] = 0.f;
-      }
-      continue;
-    }
-    const float w = p.weights ? p.weights[t * p.k + j] : 1.f;
+    const float w = choices.of(j);
     float sum = 0.f;
-    for (int64_t c = lane * V; c < p.width; c += 64 * V) {
-      const Piece<E, V> g = load<E, V>(p.x, t * p.width + c);
-      if (p.dweights) {
-        const Piece<E, V> v = load<E, V>(p.ys, row * p.width + c);
+    if (row >= 0)
+      for (int c0 = 0; c0 < width; c0 += U * STEP) {
+        const int c = c0 + l * V;
+        Raw<E, V> v[U];
+        if (p.dweights) load<E, V, U>(p.ys, row, width, c, STEP, v);
+        if (!whole) load<E, V, U>(p.x, t, width, c, STEP, g);
+        if (p.dweights)
 #pragma unroll
-        for (int q = 0; q < V; ++q) sum = __builtin_fmaf(to_float(g.v[q]), to_float(v.v[q]), sum);
-      }
-      if (p.dys) {
-        Piece<E, V> out;
+          for (int u = 0; u < U; ++u) {
+            const int at = c + u * STEP, again = at - min(at, width - V);   // elements that other pieces have
 #pragma unroll
-        for (int q = 0; q < V; ++q) out.v[q] = from_float<E>(w * to_float(g.v[q]));
-        store<E, V>(p.dys, row * p.width + c, out);
+            for (int q = 0; q < V; ++q) sum = q >= again ? __builtin_fmaf(element<E, V>(g[u], q), element<E, V>(v[u], q), sum) : sum;
+          }
+        if (p.dys) {
+#pragma unroll
+          for (int u = 0; u < U; ++u) {
+            float f[V];
+#pragma unroll
+            for (int q = 0; q < V; ++q) f[q] = w * element<E, V>(g[u], q);
+            v[u] = pack<E, V>(f);
+          }
+          store<E, V, U>(p.dys, row, width, c, STEP, v);
+        }
       }
-    }
     if (!p.dweights) continue;
 #pragma unroll
-    for (int d = 1; d < 64; d <<= 1) sum += __shfl_xor(sum, d);
-    if (lane == 0) p.dweights[t * p.k + j] = sum;
+    for (int d = 1; d < LPR; d <<= 1) sum += __shfl_xor(sum, d);
+    if (l == 0) p.dweights[t * p.k + j] = sum;
   }
 }
 
+template <int N>
+using Int = std::integral_constant<int, N>;
+// alone: elements may not be stored twice (in place, an element that two pieces have would be read behind its store where they are not under way together)
 template <class F>
-hipError_t by_type(const ExpertsRowsArgs& a, int64_t waves, F f) {
-  const unsigned grid = (unsigned)((waves + 3) / 4);
-  const bool whole = a.width * a.es % 16 == 0;
-  if (a.es == 2) whole ? f(bf16_t{}, std::integral_constant<int, 8>{}, grid) : f(bf16_t{}, std::integral_constant<int, 1>{}, grid);
-  else whole ? f(float{}, std::integral_constant<int, 4>{}, grid) : f(float{}, std::integral_constant<int, 1>{}, grid);
+hipError_t by_type(const ExpertsRowsArgs& a, int64_t n, bool alone, F f) {
+  const int64_t pieces = (a.width * a.es + 15) / 16;
+  auto of = [&](auto e, auto v) {
+    if (pieces <= 8) f(e, v, Int<8>{}, (unsigned)((n + 31) / 32));
+    else if (pieces <= 64) f(e, v, Int<16>{}, (unsigned)((n + 15) / 16));
+    else f(e, v, Int<64>{}, (unsigned)((n + 3) / 4));
+  };
+  const bool one = a.width * a.es < 16 || (alone && a.width * a.es % 16 && pieces > 256);
+  if (a.es == 2) one ? of(bf16_t{}, Int<1>{}) : of(bf16_t{}, Int<8>{});
+  else one ? of(float{}, Int<1>{}) : of(float{}, Int<4>{});
   return hipGetLastError();
+}
+
+template <int WAVES>
+void launch_sort(const ExpertsSortArgs& a, hipStream_t s) {
+  constexpr int SEGMENT = WAVES * 64 * TURNS;
+  const int segments = a.pairs ? (a.pairs + SEGMENT - 1) / SEGMENT : 1;
+  int bits = 1;
+  while (a.n >> bits) ++bits;
+  const size_t lds = (size_t)(WAVES + 1) * (a.n + 1) * 4;
+  if (segments > 1) sort_kernel<WAVES, false><<<segments, WAVES * 64, lds, s>>>(a, segments, bits);
+  sort_kernel<WAVES, true><<<segments, WAVES * 64, lds, s>>>(a, segments, bits);
 }
 
 }  // namespace
 
 hipError_t stem_experts_sort_launch(stem_ctx* ctx, const ExpertsSortArgs& a, hipStream_t s) {
   ProfScope prof(ctx, K_EXPERTS_SORT, s);
-  const int segments = a.pairs ? (a.pairs + EXPERTS_SEGMENT - 1) / EXPERTS_SEGMENT : 1;
-  int bits = 1;
-  while (a.n >> bits) ++bits;
-  const size_t lds = (size_t)(WAVES + 1) * (a.n + 1) * 4;
-  if (segments > 1) sort_kernel<false><<<segments, WAVES * 64, lds, s>>>(a, segments, bits);
-  sort_kernel<true><<<segments, WAVES * 64, lds, s>>>(a, segments, bits);
+  // one workgroup where it is enough, then segments whose counts are few to add and whose pairs are few to rank
+  if (a.pairs <= 256) launch_sort<1>(a, s);
+  else if (a.pairs <= 1024 || (a.pairs > 4096 && a.pairs <= EXPERTS_SMALL)) launch_sort<4>(a, s);
+  else launch_sort<16>(a, s);
   return hipGetLastError();
 }
 
 hipError_t stem_experts_dispatch_launch(stem_ctx* ctx, const ExpertsRowsArgs& a, hipStream_t s) {
   ProfScope prof(ctx, K_EXPERTS_DISPATCH, s);
-  return by_type(a, a.rows, [&](auto e, auto v, unsigned grid) { dispatch_kernel<decltype(e), decltype(v)::value><<<grid, 256, 0, s>>>(a); });
+  return by_type(a, a.rows, false, [&](auto e, auto v, auto l, unsigned grid) { dispatch_kernel<decltype(e), decltype(v)::value, decltype(l)::value><<<grid, 256, 0, s>>>(a); });
 }
 hipError_t stem_experts_combine_launch(stem_ctx* ctx, const ExpertsRowsArgs& a, hipStream_t s) {
   ProfScope prof(ctx, K_EXPERTS_COMBINE, s);
-  return by_type(a, a.T, [&](auto e, auto v, unsigned grid) { combine_kernel<decltype(e), decltype(v)::value><<<grid, 256, 0, s>>>(a); });
+  return by_type(a, a.T, a.y == a.residual, [&](auto e, auto v, auto l, unsigned grid) { combine_kernel<decltype(e), decltype(v)::value, decltype(l)::value><<<grid, 256, 0, s>>>(a); });
 }
 hipError_t stem_experts_combine_backward_launch(stem_ctx* ctx, const ExpertsRowsArgs& a, hipStream_t s) {
   ProfScope prof(ctx, K_EXPERTS_COMBINE_BACK, s);
-  return by_type(a, a.T, [&](auto e, auto v, unsigned grid) { combine_backward_kernel<decltype(e), decltype(v)::value><<<grid, 256, 0, s>>>(a); });
+  return by_type(a, a.T, false, [&](auto e, auto v, auto l, unsigned grid) { combine_backward_kernel<decltype(e), decltype(v)::value, decltype(l)::value><<<grid, 256, 0, s>>>(a); });
 }
