@@ -188,8 +188,8 @@ stem_status stem_qfloat_linear_backward(stem_ctx* c, const void* dy, const void*
   // Whole matrices of aligned rows are read as they lie; others are transposed first (of dy, together with its 8-bit form)
   const bool as_stored = groups == 1 && !offsets && N % 64 == 0 && K % 64 == 0 && wb <= INT32_MAX;
   if (dW && !as_stored) {
-    HIP_TRY(c, stem_qfloat_turn_launch(c, {g_in, g, (int)N, c->qfloat_dyt, (int)rows * 2, dx ? f.q : nullptr, f.scale}, s));
-    HIP_TRY(c, stem_qfloat_turn_launch(c, {x_in, g, (int)K, c->qfloat_xt, (int)rows * 2, nullptr, nullptr}, s));
+    HIP_TRY(c, stem_qfloat_turn_launch(c, {g_in, g, (int)N, c->qfloat_dyt, (int)rows * 2, dx ? f.q : nullptr, f.scale},
+                                       {x_in, g, (int)K, c->qfloat_xt, (int)rows * 2, nullptr, nullptr}, s));
   } else if (dx) {
     HIP_TRY(c, rows_form(c, dy, g, N, nullptr, f, s));
   }

@@ -245,9 +245,16 @@ struct Hidden {
         for (int q = 0; q < 4; ++q) {
           const float z = acc[i][j][4 * g + q], h = inside ? z * sigmoidf_fast(z) * u[q] : 0.f;
           acc[i][j][4 * g + q] = h;
-          top = max(top, qfloat_magnitude(h));
+          top = max(top, __float_as_uint(h) & 0x7fffffffu);
         }
         __builtin_amdgcn_sched_barrier(0);                     // (all steps' reads at once would not fit the registers)
+      }
+      if (__ballot(top >= 0x7f800000u)) {                      // (seldom: numbers alone count)
+        top = 0;
+#pragma unroll
+        for (int j = 0; j < NJ; ++j)
+#pragma unroll
+          for (int q = 0; q < 16; ++q) top = max(top, qfloat_magnitude(acc[i][j][q]));
       }
       const auto both = __builtin_amdgcn_permlane32_swap(top, top, false, false);
       const QfloatScale s = qfloat_scale(max((uint32_t)both[0], (uint32_t)both[1]));
@@ -258,7 +265,7 @@ struct Hidden {
         uint32_t w[4];
 #pragma unroll
         for (int g = 0; g < 4; ++g)
-          w[g] = qfloat_four(acc[i][j][4 * g] * s.inv, acc[i][j][4 * g + 1] * s.inv, acc[i][j][4 * g + 2] * s.inv, acc[i][j][4 * g + 3] * s.inv);
+          w[g] = qfloat_four(acc[i][j][4 * g], acc[i][j][4 * g + 1], acc[i][j][4 * g + 2], acc[i][j][4 * g + 3], s);
         // halves of the lanes have halves of 8 channels: they exchange, and have 16 in a row
         const auto lo = __builtin_amdgcn_permlane32_swap(w[0], w[2], false, false), hi = __builtin_amdgcn_permlane32_swap(w[1], w[3], false, false);
         *reinterpret_cast<u32x4_t*>(out + j * 1024) = u32x4_t{(uint32_t)lo[0], (uint32_t)lo[1], (uint32_t)hi[0], (uint32_t)hi[1]};

@@ -111,13 +111,10 @@ __global__ __launch_bounds__(WAVES * 64, SRC == FORM && KPW <= 2 ? 4 : 2) void d
       }
     };
     auto keep = [&](int row, int chunk) __attribute__((always_inline)) {
-      uint32_t top = 0;
-#pragma unroll
-      for (int q = 0; q < 16; ++q) top = max(top, qfloat_magnitude(v[q]));
-      const QfloatScale s = qfloat_scale(max_of_eight(top));
+      const QfloatScale s = qfloat_scale(max_of_eight(qfloat_top(v)));
       u32x4_t o;
 #pragma unroll
-      for (int q = 0; q < 4; ++q) o[q] = qfloat_four(v[4 * q] * s.inv, v[4 * q + 1] * s.inv, v[4 * q + 2] * s.inv, v[4 * q + 3] * s.inv);
+      for (int q = 0; q < 4; ++q) o[q] = qfloat_four(v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3], s);
       if (chunk >= nkb * 8) return;
       *reinterpret_cast<u32x4_t*>(held + row * pitch + chunk * 16) = o;
       if ((lane & 7) == 0) scales[row * nkb + (chunk >> 3)] = (uint8_t)s.byte;

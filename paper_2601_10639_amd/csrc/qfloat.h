@@ -66,7 +66,7 @@ struct QfloatTurnArgs {
   int pitch;                // bytes of a row of it
   uint8_t *q, *scale;       // may be null
 };
-hipError_t stem_qfloat_turn_launch(stem_ctx* ctx, const QfloatTurnArgs& a, hipStream_t s);
+hipError_t stem_qfloat_turn_launch(stem_ctx* ctx, const QfloatTurnArgs& a, const QfloatTurnArgs& b, hipStream_t s);   // two of the same rows
 
 enum QfloatOut { QFLOAT_BF16 = 0, QFLOAT_F32, QFLOAT_HIDDEN };
 struct QfloatGemmArgs {
@@ -125,16 +125,32 @@ __device__ __forceinline__ uint32_t qfloat_magnitude(float v) {
   const uint32_t b = __float_as_uint(v) & 0x7fffffffu;
   return b < 0x7f800000u ? b : 0u;
 }
-struct QfloatScale { uint32_t byte; float inv; };
+// The largest of n values.  Numbers alone are compared where some lane has others, which is seldom: as integers those are above all numbers.
+template <int N>
+__device__ __forceinline__ uint32_t qfloat_top(const float (&v)[N]) {
+  uint32_t top = 0;
+#pragma unroll
+  for (int q = 0; q < N; q += 2) top = max(max(top, __float_as_uint(v[q]) & 0x7fffffffu), __float_as_uint(v[q + 1]) & 0x7fffffffu);
+  if (__ballot(top >= 0x7f800000u)) {
+    top = 0;
+#pragma unroll
+    for (int q = 0; q < N; ++q) top = max(top, qfloat_magnitude(v[q]));
+  }
+  return top;
+}
+struct QfloatScale { uint32_t byte; float scale; };
 __device__ __forceinline__ QfloatScale qfloat_scale(uint32_t top) {   // 448 = 1.75 x 2^8
   int e = (int)(top >> 23) - 127 - 8 + ((top & 0x7fffffu) > 0x600000u ? 1 : 0);
   e = e < -126 ? -126 : e;
-  return {(uint32_t)(e + 127), __uint_as_float((uint32_t)(127 - e) << 23)};
+  return {(uint32_t)(e + 127), __uint_as_float((uint32_t)(127 + e) << 23)};
 }
-__device__ __forceinline__ uint32_t qfloat_four(float a, float b, float c, float d) {
-  int w = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false);
-  w = __builtin_amdgcn_cvt_pk_fp8_f32(c, d, w, true);
-  return (uint32_t)w;
+// four values divided by the scale, to the nearest
+typedef __attribute__((ext_vector_type(2))) short qfloat_half_t;
+__device__ __forceinline__ uint32_t qfloat_four(float a, float b, float c, float d, const QfloatScale& s) {
+  qfloat_half_t w = {};
+  w = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(w, a, b, s.scale, false);
+  w = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(w, c, d, s.scale, true);
+  return __builtin_bit_cast(uint32_t, w);
 }
 
 // ---- groups: every lane of a wavefront takes part -------------------------------------------------------------------------

@@ -62,13 +62,13 @@ __global__ __launch_bounds__(256) void chunks_kernel(QfloatRowsArgs p) {
 #pragma unroll
   for (int u = 0; u < BLOCKS; ++u) {
     const int kb = kb0 + u;
-    uint32_t top = 0;
+    float v[16];
 #pragma unroll
-    for (int q = 0; q < 16; ++q) top = max(top, qfloat_magnitude(value(u, q)));
-    const QfloatScale s = qfloat_scale(max_of_eight(top));
+    for (int q = 0; q < 16; ++q) v[q] = value(u, q);
+    const QfloatScale s = qfloat_scale(max_of_eight(qfloat_top(v)));
     uint32_t w[4];
 #pragma unroll
-    for (int q = 0; q < 4; ++q) w[q] = qfloat_four(value(u, 4 * q) * s.inv, value(u, 4 * q + 1) * s.inv, value(u, 4 * q + 2) * s.inv, value(u, 4 * q + 3) * s.inv);
+    for (int q = 0; q < 4; ++q) w[q] = qfloat_four(v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3], s);
     if (place < 0 || kb >= nkb) continue;
     *reinterpret_cast<u32x4_t*>(out + (int64_t)kb * 4096) = u32x4_t{w[0], w[1], w[2], w[3]};
     if (c == 0) p.scale[qfloat_scale_at(place, kb, nkb)] = (uint8_t)s.byte;
@@ -98,83 +98,67 @@ __global__ __launch_bounds__(256) void rows_kernel(QfloatRowsArgs p) {
   }
   int place = live ? row : -1;
   if (p.groups.offsets) place = qfloat_place<(LPR < 64 ? LPR : 64)>(p.groups, row, lane);
-  float v[HELD][16];
-  auto elements = [&](const QuantChunk& c, float (&u)[16]) __attribute__((always_inline)) {
-#pragma unroll
-    for (int q = 0; q < 16; ++q) u[q] = quant_element(c, q);
+  // (values are made of the packed ones at each use: held as floats they would cost half of the wavefronts)
+  auto chunk = [&](int t) __attribute__((always_inline)) {
+    if constexpr (CPT > 0) return raw[t];
+    else return fetch(t);
   };
-  if constexpr (CPT > 0) {
-#pragma unroll
-    for (int t = 0; t < CPT; ++t) elements(raw[t], v[t]);
-  }
-  float mean = 0.f, r = 1.f;
-  const bool centred = p.norm.kind == STEM_NORM_LAYER, normed = p.norm.kind != STEM_NORM_NONE || p.norm.weight;
-  auto cut = [&](int t, float (&u)[16]) __attribute__((always_inline)) {   // zeros behind the row's end
-    const int left = p.K - (t * LPR + l) * 16;
-    if (left < 16)
-#pragma unroll
-      for (int q = 0; q < 16; ++q) u[q] = q < left ? u[q] : 0.f;
-  };
-  auto advance = [&](int stage, int t, float (&u)[16]) __attribute__((always_inline)) {   // 1: centred, 2: normed and weighted
-    if (stage == 1) {
-#pragma unroll
-      for (int q = 0; q < 16; ++q) u[q] -= mean;
-    } else {
-      const int at = t * LPR + l;
-#pragma unroll
-      for (int q = 0; q < 16; ++q) u[q] *= r;
-      if (p.norm.weight && at * 16 < p.K) {
-        const QuantChunk w = quant_load_chunk(static_cast<const bf16_t*>(p.norm.weight) + at * 16, p.K - at * 16);
-#pragma unroll
-        for (int q = 0; q < 16; ++q) u[q] *= quant_element(w, q);
-      }
-    }
-    cut(t, u);
-  };
-  auto each_step = [&](int stage, auto f) __attribute__((always_inline)) {
+  auto each_chunk = [&](auto f) __attribute__((always_inline)) {
     if constexpr (CPT > 0) {
 #pragma unroll
       for (int t = 0; t < CPT; ++t)
-        if (t * LPR < chunks) {
-          if (stage == 1 && centred) advance(1, t, v[t]);
-          if (stage == 2 && normed) advance(2, t, v[t]);
-          f(t, v[t]);
-        }
+        if (t * LPR < chunks) f(t);
     } else {
-      for (int t = 0; t * LPR < chunks; ++t) {
-        elements(fetch(t), v[0]);
-        if (stage >= 1 && centred) advance(1, t, v[0]);
-        if (stage >= 2 && normed) advance(2, t, v[0]);
-        f(t, v[0]);
-      }
+      for (int t = 0; t * LPR < chunks; ++t) f(t);
     }
   };
-  if (p.norm.kind != STEM_NORM_NONE) {
+  float mean = 0.f, r = 1.f;
+  auto total = [&](bool squares) __attribute__((always_inline)) {
     float s = 0.f;
-    if (centred) {
-      each_step(0, [&](int, float (&u)[16]) {
+    each_chunk([&](int t) __attribute__((always_inline)) {
+      const QuantChunk c = chunk(t);
+      const int in = p.K - (t * LPR + l) * 16;
+      float u[16];
 #pragma unroll
-        for (int q = 0; q < 16; ++q) s += u[q];
-      });
-      mean = sum_row<LPR>(s, red) / (float)p.K;
-      s = 0.f;
-    }
-    each_step(1, [&](int, float (&u)[16]) {
+      for (int q = 0; q < 16; ++q) u[q] = quant_element(c, q);
+      if (p.norm.kind == STEM_NORM_LAYER && squares) {
 #pragma unroll
-      for (int q = 0; q < 16; ++q) s = __builtin_fmaf(u[q], u[q], s);
+        for (int q = 0; q < 16; ++q) u[q] -= mean;
+        if (in < 16)
+#pragma unroll
+          for (int q = 0; q < 16; ++q) u[q] = q < in ? u[q] : 0.f;
+      }
+#pragma unroll
+      for (int q = 0; q < 16; ++q) s = squares ? __builtin_fmaf(u[q], u[q], s) : s + u[q];
     });
-    r = 1.0f / sqrtf(sum_row<LPR>(s, red) / (float)p.K + p.norm.eps);
-  }
+    return sum_row<LPR>(s, red) / (float)p.K;
+  };
+  if (p.norm.kind == STEM_NORM_LAYER) mean = total(false);
+  if (p.norm.kind != STEM_NORM_NONE) r = 1.0f / sqrtf(total(true) + p.norm.eps);
   uint8_t* const out = p.q + (int64_t)(place >> 5) * 32 * chunks * 16 + (place & 31) * 16;
-  each_step(2, [&](int t, float (&u)[16]) {
-    const int c = t * LPR + l;
-    uint32_t top = 0;
+  each_chunk([&](int t) __attribute__((always_inline)) {
+    const int c = t * LPR + l, in = p.K - c * 16;
+    const QuantChunk x = chunk(t);
+    QuantChunk g = {};
+    if (p.norm.weight && in > 0) g = quant_load_chunk(static_cast<const bf16_t*>(p.norm.weight) + c * 16, in);
+    float u[16];
 #pragma unroll
-    for (int q = 0; q < 16; ++q) top = max(top, qfloat_magnitude(u[q]));
-    const QfloatScale s = qfloat_scale(max_of_eight(top));
+    for (int q = 0; q < 16; ++q) u[q] = quant_element(x, q);
+    if (p.norm.kind == STEM_NORM_LAYER)
+#pragma unroll
+      for (int q = 0; q < 16; ++q) u[q] -= mean;
+#pragma unroll
+    for (int q = 0; q < 16; ++q) u[q] *= r;
+    if (p.norm.weight)
+#pragma unroll
+      for (int q = 0; q < 16; ++q) u[q] *= quant_element(g, q);
+    if (in < 16)                                               // zeros behind the row's end
+#pragma unroll
+      for (int q = 0; q < 16; ++q) u[q] = q < in ? u[q] : 0.f;
+    const QfloatScale s = qfloat_scale(max_of_eight(qfloat_top(u)));
     uint32_t w[4];
 #pragma unroll
-    for (int q = 0; q < 4; ++q) w[q] = qfloat_four(u[4 * q] * s.inv, u[4 * q + 1] * s.inv, u[4 * q + 2] * s.inv, u[4 * q + 3] * s.inv);
+    for (int q = 0; q < 4; ++q) w[q] = qfloat_four(u[4 * q], u[4 * q + 1], u[4 * q + 2], u[4 * q + 3], s);
     if (c >= chunks || place < 0) return;
     *reinterpret_cast<u32x4_t*>(out + (int64_t)(c >> 1) * 1024 + (c & 1) * 512) = u32x4_t{w[0], w[1], w[2], w[3]};
     if ((c & 7) == 0) p.scale[qfloat_scale_at(place, c >> 3, nkb)] = (uint8_t)s.byte;
@@ -199,7 +183,7 @@ __device__ __forceinline__ void store_rows(uint8_t* q, uint8_t* scale, int nkb, 
     const int row = row0 + r;
     uint32_t w[4];
 #pragma unroll
-    for (int g = 0; g < 4; ++g) w[g] = qfloat_four(v[r][4 * g] * s[r].inv, v[r][4 * g + 1] * s[r].inv, v[r][4 * g + 2] * s[r].inv, v[r][4 * g + 3] * s[r].inv);
+    for (int g = 0; g < 4; ++g) w[g] = qfloat_four(v[r][4 * g], v[r][4 * g + 1], v[r][4 * g + 2], v[r][4 * g + 3], s[r]);
     *reinterpret_cast<u32x4_t*>(q + ((int64_t)(row >> 5) * (nkb * 4) + (kb * 4 + (c >> 1))) * 1024 + (c & 1) * 512 + (row & 31) * 16) = u32x4_t{w[0], w[1], w[2], w[3]};
     if (c == 0) scale[qfloat_scale_at(row, kb, nkb)] = (uint8_t)s[r].byte;
   }
@@ -223,9 +207,7 @@ __global__ __launch_bounds__(256) void weights_kernel(QfloatTilesArgs p) {
   }
   uint32_t m = 0;
 #pragma unroll
-  for (int r = 0; r < 4; ++r)
-#pragma unroll
-    for (int q = 0; q < 16; ++q) m = max(m, qfloat_magnitude(v[r][q]));
+  for (int r = 0; r < 4; ++r) m = max(m, qfloat_top(v[r]));
 #pragma unroll
   for (int d = 1; d < 64; d <<= 1) m = max(m, (uint32_t)__shfl_xor((int)m, d));
   if (lane == 0) tops[wave] = m;
@@ -241,7 +223,7 @@ __global__ __launch_bounds__(256) void weights_kernel(QfloatTilesArgs p) {
 #pragma unroll
   for (int q = 0; q < 16; ++q) {
     const int at = c * 16 + q;
-    words[at * PITCH + c * 8 + quad] = qfloat_four(v[0][q] * one.inv, v[1][q] * one.inv, v[2][q] * one.inv, v[3][q] * one.inv);
+    words[at * PITCH + c * 8 + quad] = qfloat_four(v[0][q], v[1][q], v[2][q], v[3][q], one);
     if (quad == 0) qt[elements + qfloat_scale_at(tc * 128 + at, tr, nkb_t)] = (uint8_t)one.byte;
   }
   __syncthreads();
@@ -253,11 +235,13 @@ __global__ __launch_bounds__(256) void weights_kernel(QfloatTilesArgs p) {
   }
 }
 
-__global__ __launch_bounds__(256) void turn_kernel(QfloatTurnArgs p) {
+__global__ __launch_bounds__(256) void turn_kernel(QfloatTurnArgs first, QfloatTurnArgs second, int blocks) {
   constexpr int PITCH = 68;
   __shared__ __attribute__((aligned(16))) uint32_t words[128 * PITCH + 128];
   const int t = threadIdx.x, lane = t & 63, wave = t >> 6, quad = t >> 3, c = t & 7;
-  const int nkb = (p.cols + 127) / 128, tr = blockIdx.x / nkb, tc = blockIdx.x - tr * nkb;
+  const QfloatTurnArgs& p = (int)blockIdx.x < blocks ? first : second;
+  const int b = (int)blockIdx.x < blocks ? blockIdx.x : blockIdx.x - blocks;
+  const int nkb = (p.cols + 127) / 128, tr = b / nkb, tc = b - tr * nkb;
   QfloatTile tile;
   if (!qfloat_tile<128>(p.groups, tr, lane, tile)) return;
   QuantChunk raw[4];
@@ -276,13 +260,9 @@ __global__ __launch_bounds__(256) void turn_kernel(QfloatTurnArgs p) {
     QfloatScale s[4];
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
-      uint32_t top = 0;
 #pragma unroll
-      for (int q = 0; q < 16; ++q) {
-        v[r][q] = quant_element(raw[r], q);
-        top = max(top, qfloat_magnitude(v[r][q]));
-      }
-      s[r] = qfloat_scale(max_of_eight(top));
+      for (int q = 0; q < 16; ++q) v[r][q] = quant_element(raw[r], q);
+      s[r] = qfloat_scale(max_of_eight(qfloat_top(v[r])));
     }
     store_rows(p.q, p.scale, nkb, tile.padded + quad * 4, tc, c, v, s);
   }
@@ -324,9 +304,9 @@ hipError_t stem_qfloat_weights_launch(stem_ctx* ctx, const QfloatTilesArgs& a, h
   return hipGetLastError();
 }
 
-hipError_t stem_qfloat_turn_launch(stem_ctx* ctx, const QfloatTurnArgs& a, hipStream_t s) {
+hipError_t stem_qfloat_turn_launch(stem_ctx* ctx, const QfloatTurnArgs& a, const QfloatTurnArgs& b, hipStream_t s) {
   ProfScope prof(ctx, K_QFLOAT_TURN, s);
-  const int64_t rows = stem_qfloat_rows(a.groups.T, a.groups.n);
-  turn_kernel<<<(unsigned)(rows / 128 * ((a.cols + 127) / 128)), 256, 0, s>>>(a);
+  const int64_t rows = stem_qfloat_rows(a.groups.T, a.groups.n) / 128, first = rows * ((a.cols + 127) / 128), second = rows * ((b.cols + 127) / 128);
+  turn_kernel<<<(unsigned)(first + second), 256, 0, s>>>(a, b, (int)first);
   return hipGetLastError();
 }
