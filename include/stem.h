@@ -376,7 +376,7 @@ stem_status stem_qfloat_ffn_forward(stem_ctx* ctx, const void* x, const int32_t*
 
 /* A token has k choices (1 to 16), each an expert 0 .. n_experts - 1 (up to 512) or, negative, none (padding, a choice that is dropped).  The
  * (token, choice) pair t k + j is its place in experts [T,k].  Rows of an expert stand together once they are sorted, which is what
- * stem_qfloat_linear and stem_qfloat_ffn_forward read with `offsets`; weights are the router's, fp32.  Rows have any width, in the context's
+ * stem_qfloat_linear and stem_qfloat_ffn_forward read with `offsets`; weights are the router's, fp32.  Rows have any width up to 2^30, in the context's
  * dtype; sums are in fp32 and rounded once.  No atomics: the same bits on every run.  Arrays of integers and fp32 weights may begin at any 4 bytes. */
 #define STEM_EXPERTS_MAX 512
 #define STEM_EXPERTS_MAX_CHOICES 16

@@ -12,7 +12,7 @@ stem_status check_choices(stem_ctx* c, const char* who, int64_t T, int k) {
 
 stem_status check_rows(stem_ctx* c, const char* who, int64_t rows, int64_t width) {
   if (rows < 0 || rows > ((int64_t)1 << 30)) return stem_fail(c, STEM_ERR_SHAPE, "%s: %lld rows", who, (long long)rows);
-  if (width < 0 || width > INT32_MAX) return stem_fail(c, STEM_ERR_SHAPE, "%s: rows of %lld elements", who, (long long)width);
+  if (width < 0 || width > ((int64_t)1 << 30)) return stem_fail(c, STEM_ERR_SHAPE, "%s: rows of %lld elements", who, (long long)width);
   return STEM_OK;
 }
 

@@ -6,6 +6,7 @@
 
 namespace {
 
+constexpr stem_norm no_norm = {STEM_NORM_NONE, 0.f, nullptr};
 constexpr int64_t MAX_CHANNELS = 1 << 22;
 // The layer of up to 8 rows: its gate product leaves fp32 hidden values, of which every workgroup of the down product makes its operands where they are few, else a
 // kernel between the two.  More rows: tiles of the gate product leave 8 bits.  us, the whole layer, hidden values inline / by a kernel: 2048 x 8192, 1, 4, 8 rows
@@ -52,7 +53,7 @@ QfloatGemmArgs gemm_args(const stem_ctx* c, const Form& a, const Form& b, int64_
 }
 
 hipError_t rows_form(stem_ctx* c, const void* x, const QfloatGroups& g, int64_t K, const stem_norm* norm, const Form& f, hipStream_t s) {
-  const QfloatRowsArgs a = {static_cast<const bf16_t*>(x), nullptr, g, (int)K, norm ? *norm : stem_norm{STEM_NORM_NONE, 0.f, nullptr}, f.q, f.scale};
+  const QfloatRowsArgs a = {static_cast<const bf16_t*>(x), nullptr, g, (int)K, norm ? *norm : no_norm, f.q, f.scale};
   return stem_qfloat_rows_launch(c, a, s);
 }
 
@@ -68,7 +69,7 @@ QfloatDecodeArgs decode_args(const Form& b, int64_t stride_b, int64_t N, int64_t
 hipError_t decode_rows(stem_ctx* c, const void* x, int64_t K, const stem_norm* norm, bool in_place, const Form& f, QfloatDecodeArgs& a, hipStream_t s) {
   if (in_place && stem_qfloat_decode_inline(a.groups.T, K)) {
     a.x = static_cast<const bf16_t*>(x);
-    a.norm = norm ? *norm : stem_norm{STEM_NORM_NONE, 0.f, nullptr};
+    a.norm = norm ? *norm : no_norm;
     return hipSuccess;
   }
   a.A = f.q; a.sa = f.scale; a.a_bytes = f.bytes;
@@ -241,14 +242,15 @@ stem_status stem_qfloat_ffn_forward(stem_ctx* c, const void* x, const int32_t* i
   QfloatDecodeArgs b = decode_args(form(down_q, d, F), stem_qfloat_form(d, F), d, F, g);
   b.y = static_cast<bf16_t*>(y); b.residual = static_cast<const bf16_t*>(residual);
   b.A = h.q; b.sa = h.scale; b.a_bytes = h.bytes;
-  if (T <= GATE_ROWS && T * F * 4 <= QFLOAT_WS) {
+  if (T <= GATE_ROWS && stem_qfloat_decode_inline(T, d) && T * F * 4 <= QFLOAT_WS) {
     QfloatDecodeArgs a = decode_args(form(gate_q, F, d), stem_qfloat_form(F, d), F, d, g);
     a.h_out = c->qfloat_ws;
     a.ids = ids; a.E = static_cast<const bf16_t*>(E); a.E_rows = (int)E_rows; a.flag = c->flag;
-    HIP_TRY(c, decode_rows(c, x, d, norm, true, f, a, s));
+    a.x = static_cast<const bf16_t*>(x);
+    a.norm = norm ? *norm : no_norm;
     HIP_TRY(c, stem_qfloat_decode_launch(c, K_QFLOAT_GATE, a, s));
     if (T * F <= HIDDEN_INLINE && stem_qfloat_decode_inline(T, F)) b.h = c->qfloat_ws;
-    else HIP_TRY(c, stem_qfloat_rows_launch(c, {nullptr, c->qfloat_ws, g, (int)F, {STEM_NORM_NONE, 0.f, nullptr}, h.q, h.scale}, s));
+    else HIP_TRY(c, stem_qfloat_rows_launch(c, {nullptr, c->qfloat_ws, g, (int)F, no_norm, h.q, h.scale}, s));
     HIP_TRY(c, stem_qfloat_decode_launch(c, K_QFLOAT_LINEAR, b, s));
     return STEM_OK;
   }

@@ -702,7 +702,7 @@ __global__ __launch_bounds__((C::WAVES + C::LW) * 64) void tile_kernel(QfloatGem
   for (int st = 0; st < S - 1; ++st)
     if (kt + st < nk) stage_iteration(st);
   __syncthreads();
-  if constexpr (OUT != QFLOAT_HIDDEN)
+  if constexpr (OUT == QFLOAT_F32 || (OUT == QFLOAT_BF16 && C::TN == 64))   // (only these are cut)
     if (p.ksplit > 1 && !last_slice<MI, NJ>(p, acc, smem, w.tile * C::WAVES + wave, w.tiles * C::WAVES, w.slice, w.tile, lane)) return;
   if constexpr (OUT == QFLOAT_HIDDEN) Hid::run(p, acc, id, smem + wave * Hid::BYTES, w.pa + wm * MI * 32, w.n0 + wn * NJ * 32, w.rows - wm * MI * 32, lane);
   else Out::run(p, acc, smem + wave * Out::BYTES, w.m0 + wm * MI * 32, w.n0 + wn * NJ * 32, w.rows - wm * MI * 32, HALF ? (int64_t)w.group * p.M * p.N : 0, lane);
@@ -749,7 +749,7 @@ extern "C" void stem_route_qfloat(int64_t T, int groups, int N, int K, int out, 
       if ((double)((tiles(256, 256) + 255) / 256) <= few) rows = 256;
     }
   }
-  if (out != QFLOAT_HIDDEN && cols <= 128 && groups == 1) {
+  if ((out == QFLOAT_F32 || (out == QFLOAT_BF16 && cols == 64)) && groups == 1) {
     slices = nk < 32 ? 1 : (int)std::min<int64_t>({MAX_SLICES, nk / 10, 240 / tiles(rows, cols)});
     while (slices > 1 && (slices * tiles(rows, cols) * rows * cols * 4 > ws_bytes || tiles(rows, cols) > STEM_TICKETS)) --slices;
     while (slices > 1 && (nk + slices - 1) / slices * (slices - 1) >= nk) --slices;   // every slice has a part of K

@@ -247,23 +247,21 @@ __global__ __launch_bounds__(WAVES * 64, SRC == FORM && KPW <= 2 ? 4 : 2) void d
 }
 
 template <int CH, int NT, Source SRC, bool GATE>
-void by_depth(const QfloatDecodeArgs& a, int64_t tiles, hipStream_t s) {
-  const unsigned grid = (unsigned)(tiles * ((a.N + CH - 1) / CH));
-  const int per = (a.K / 128 + WAVES - 1) / WAVES;
+void by_depth(const QfloatDecodeArgs& a, int depth, unsigned grid, hipStream_t s) {
   const size_t lds = SRC == FORM ? 0 : 16 * (size_t)(a.K + 16 + a.K / 128);
-  if (per <= 1) decode_kernel<CH, NT, SRC, 1, GATE><<<grid, WAVES * 64, lds, s>>>(a);
-  else if (per <= 2) decode_kernel<CH, NT, SRC, 2, GATE><<<grid, WAVES * 64, lds, s>>>(a);
-  else if (per <= 4) decode_kernel<CH, NT, SRC, 4, GATE><<<grid, WAVES * 64, lds, s>>>(a);
+  if (depth == 1) decode_kernel<CH, NT, SRC, 1, GATE><<<grid, WAVES * 64, lds, s>>>(a);
+  else if (depth == 2) decode_kernel<CH, NT, SRC, 2, GATE><<<grid, WAVES * 64, lds, s>>>(a);
+  else if (depth == 4) decode_kernel<CH, NT, SRC, 4, GATE><<<grid, WAVES * 64, lds, s>>>(a);
   else decode_kernel<CH, NT, SRC, 8, GATE><<<grid, WAVES * 64, lds, s>>>(a);
 }
 
 template <int NT, Source SRC, bool GATE>
-void by_channels(const QfloatDecodeArgs& a, int64_t tiles, hipStream_t s) {
-  // about as many workgroups as compute units
-  const int64_t wgs = tiles * ((a.N + 15) / 16);
-  if (wgs <= 128) by_depth<8, NT, SRC, GATE>(a, tiles, s);
-  else if (wgs <= 256) by_depth<16, NT, SRC, GATE>(a, tiles, s);
-  else by_depth<32, NT, SRC, GATE>(a, tiles, s);
+void by_channels(const QfloatDecodeArgs& a, const int32_t* route, hipStream_t s) {
+  const int64_t n = a.groups.n < a.groups.T ? a.groups.n : a.groups.T, tiles = (a.groups.T + 16 * NT - 1) / (16 * NT) + (a.groups.offsets ? n - 1 : 0);
+  const unsigned grid = (unsigned)(tiles * ((a.N + route[0] - 1) / route[0]));
+  if (route[0] == 8) by_depth<8, NT, SRC, GATE>(a, route[2], grid, s);
+  else if (route[0] == 16) by_depth<16, NT, SRC, GATE>(a, route[2], grid, s);
+  else by_depth<32, NT, SRC, GATE>(a, route[2], grid, s);
 }
 
 }  // namespace
@@ -276,24 +274,29 @@ extern "C" int stem_route_qfloat_few(int64_t T, int grouped, int N, int K) {
   return T <= 16 || (T <= 256 && T * N * K <= (int64_t)1 << 30);
 }
 
+// {channels and 16-row tiles of a workgroup, blocks of K that a wavefront has under way}.  About as many workgroups as compute units, if need be of 8 channels, half of whose
+// products count; of 32 rows where there are more workgroups than that helps (us, 16 / 32 rows: 64 of N 8192, K 2048 9.9 / 8.2, 256 of 1024 x 4096 9.5 / 8.6, 64 of
+// 1024 x 4096 6.4 / 8.0).
+extern "C" void stem_route_qfloat_decode(int64_t T, int groups, int N, int K, int form, int32_t* route) {
+  const int64_t n16 = (N + 15) / 16;
+  route[1] = form && (T + 15) / 16 * n16 >= 1024 ? 2 : 1;
+  const int64_t tiles = (T + 16 * route[1] - 1) / (16 * route[1]) + (groups < T ? groups : T) - 1, wgs = tiles * n16;
+  route[0] = wgs <= 128 ? 8 : wgs <= 256 ? 16 : 32;
+  const int per = ((K + 127) / 128 + WAVES - 1) / WAVES;
+  route[2] = per <= 1 ? 1 : per <= 2 ? 2 : per <= 4 ? 4 : 8;
+}
+
 // LDS has room for 16 rows' values
 bool stem_qfloat_decode_inline(int64_t rows, int64_t K) { return rows <= 16 && K <= 8192; }
 
 hipError_t stem_qfloat_decode_launch(stem_ctx* ctx, int kid, const QfloatDecodeArgs& a, hipStream_t s) {
   ProfScope prof(ctx, kid, s);
-  const bool form = !a.x && !a.h;
-  // 16 rows a workgroup, or 32 where there are more workgroups than that helps
-  const int nt = form && (int64_t)((a.groups.T + 15) / 16) * ((a.N + 15) / 16) >= 1024 ? 2 : 1;
-  const int64_t tiles = (a.groups.T + 16 * nt - 1) / (16 * nt) + (a.groups.offsets ? (a.groups.n < a.groups.T ? a.groups.n : a.groups.T) - 1 : 0);
-  if (a.h_out) {
-    if (a.x) by_channels<1, ROWS, true>(a, tiles, s);
-    else if (nt == 1) by_channels<1, FORM, true>(a, tiles, s);
-    else by_channels<2, FORM, true>(a, tiles, s);
-  } else {
-    if (a.x) by_channels<1, ROWS, false>(a, tiles, s);
-    else if (a.h) by_channels<1, HIDDEN, false>(a, tiles, s);
-    else if (nt == 1) by_channels<1, FORM, false>(a, tiles, s);
-    else by_channels<2, FORM, false>(a, tiles, s);
-  }
+  int32_t route[3];
+  stem_route_qfloat_decode(a.groups.T, a.groups.offsets ? a.groups.n : 1, a.N, a.K, !a.x && !a.h, route);
+  if (a.h_out) by_channels<1, ROWS, true>(a, route, s);        // (a gate product of up to 8 rows)
+  else if (a.x) by_channels<1, ROWS, false>(a, route, s);
+  else if (a.h) by_channels<1, HIDDEN, false>(a, route, s);
+  else if (route[1] == 1) by_channels<1, FORM, false>(a, route, s);
+  else by_channels<2, FORM, false>(a, route, s);
   return hipGetLastError();
 }

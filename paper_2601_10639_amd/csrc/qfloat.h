@@ -92,8 +92,7 @@ struct QfloatGemmArgs {
 };
 hipError_t stem_qfloat_gemm_launch(stem_ctx* ctx, int kid, QfloatOut out, const QfloatGemmArgs& a, hipStream_t s);
 
-// Products of few rows in each group.  Rows: a form (A, sa), or up to 16 that are made to operands in place: rows x of row_K values behind a norm, or fp32 hidden
-// values h.
+// Products of few rows.  Rows: a form (A, sa), or up to 16 that are made to operands in place: rows x of row_K values behind a norm, or fp32 hidden values h.
 struct QfloatDecodeArgs {
   const uint8_t *A, *sa;
   const uint8_t *B, *sb;
@@ -104,9 +103,9 @@ struct QfloatDecodeArgs {
   int row_K;
   stem_norm norm;
   const float* h;           // [T, row_K]
-  bf16_t* y;                // [T, N], or null: a gate product
+  bf16_t* y;                // [T, N], or null: a gate product of rows x
   const bf16_t* residual;
-  float* h_out;             // [T, N]
+  float* h_out;             // [T, N] of a gate product
   const int32_t* ids;
   const bf16_t* E;
   int E_rows;
