@@ -81,31 +81,35 @@ struct Work {
 };
 template <int TM, int TN, bool BY_K>
 __device__ __forceinline__ bool find_work(const QfloatGemmArgs& p, int lane, Work& w) {
-  const int ntn = (p.N + TN - 1) / TN, nk_all = p.K / 128, all_rows = (p.M + TM - 1) / TM;
+  const int ntn = (p.N + TN - 1) / TN, nk_all = p.K / 128;
   const bool grouped = p.groups.offsets != nullptr;
-  const int ntm = BY_K || !grouped ? all_rows : qfloat_tiles<TM>(p.groups, lane), tiles = ntm * ntn;
-  const int part = tiles ? blockIdx.x / tiles : 1, b = blockIdx.x - part * tiles;   // of K: a group, a slice
-  if (!BY_K && grouped && part > 0) return false;
-  int tm, tn;
-  tile_of(b, tiles, ntm, ntn, tm, tn);
-  QfloatTile t = {0, tm * TM, p.M - tm * TM, tm * TM};
-  int k0 = 0, nk = nk_all;
-  if (BY_K && grouped) {                                     // all of the output for each group of K
-    t.group = part;
-    qfloat_scan<128>(p.groups, lane, [&](int i, int, int rows, int, int, int padded) __attribute__((always_inline)) {
-      const uint64_t mine = __ballot(i == part);
-      if (!mine) return false;
-      const int l = __builtin_ctzll(mine);
-      k0 = __builtin_amdgcn_readlane(padded, l) / 64;       // (bf16: 64 rows a K tile)
-      nk = (__builtin_amdgcn_readlane(rows, l) + 63) / 64;
-      return true;
-    });
-  } else if (grouped) {
-    if (!qfloat_tile<TM>(p.groups, tm, lane, t)) return false;
-  } else if (p.ksplit > 1) {
-    const int per = (nk_all + p.ksplit - 1) / p.ksplit;
-    k0 = part * per;
-    nk = nk_all - k0 < per ? nk_all - k0 : per;
+  int tm = 0, tn = 0, tiles = 0, part = 0, k0 = 0, nk = nk_all;   // part: of K, a group or a slice
+  QfloatTile t;
+  if (!BY_K && grouped) {
+    if (!qfloat_tile_of<TM>(p.groups, lane, t, [&](int ntm) __attribute__((always_inline)) {
+          tiles = ntm * ntn;
+          if ((int)blockIdx.x >= tiles) return -1;
+          tile_of(blockIdx.x, tiles, ntm, ntn, tm, tn);
+          return tm;
+        }))
+      return false;
+  } else {
+    const int ntm = (p.M + TM - 1) / TM;
+    tiles = ntm * ntn;
+    part = blockIdx.x / tiles;
+    tile_of(blockIdx.x - part * tiles, tiles, ntm, ntn, tm, tn);
+    t = {0, tm * TM, p.M - tm * TM, tm * TM};
+    if (BY_K && grouped) {                                   // all of the output for each group of K
+      int rows = 0;
+      qfloat_group(p.groups, part, lane, k0, rows);
+      t.group = part;
+      k0 /= 64;                                              // (bf16: 64 rows a K tile)
+      nk = (rows + 63) / 64;
+    } else if (p.ksplit > 1) {
+      const int per = (nk_all + p.ksplit - 1) / p.ksplit;
+      k0 = part * per;
+      nk = nk_all - k0 < per ? nk_all - k0 : per;
+    }
   }
   w = {t.row, t.rows, t.padded, tn * TN, k0, nk, t.group, tm * ntn + tn, tiles, grouped ? 0 : part};
   return true;

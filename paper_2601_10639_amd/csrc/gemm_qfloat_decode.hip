@@ -37,6 +37,7 @@ __global__ __launch_bounds__(WAVES * 64, SRC == FORM && KPW <= 2 ? 4 : 2) void d
   constexpr int TM = 16 * NT, CB = CH == 32 ? 2 : 1;
   static_assert(CB * NT <= WAVES, "a wavefront joins the sums of 16 x 16 results");
   __shared__ __attribute__((aligned(16))) f32x4_t part[WAVES][CB * NT][64];
+  __shared__ float sums[WAVES];
   extern __shared__ __attribute__((aligned(16))) uint8_t held[];   // [16][K + 16] values, then [16][blocks] scales
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15, c = lane >> 4;
   const int ntn = (p.N + CH - 1) / CH, nkb = p.K / 128, tm = blockIdx.x / ntn, n0 = (blockIdx.x - tm * ntn) * CH;
@@ -121,12 +122,15 @@ __global__ __launch_bounds__(WAVES * 64, SRC == FORM && KPW <= 2 ? 4 : 2) void d
     };
     const bool normed = SRC == ROWS && (p.norm.kind != STEM_NORM_NONE || p.norm.weight);
     if (normed) {
-      bool first = true;
-      for (int row = wave; row < rows; row += WAVES) {
+      // 8, 4, 2 wavefronts a row or one.  In loops: values that are read again from the nearest cache cost less than the instructions that would hold them, whose
+      // first fetch is what short kernels wait for (one row of K 2048 with all chunks held and unrolled: 10.2 us against 9.5).
+      const int share = p.share, turns = (rows * share + WAVES - 1) / WAVES, first = wave % share * 64 + lane;
+      for (int turn = 0; turn < turns; ++turn) {
+        const int at = turn * (WAVES / share) + wave / share, row = at < rows ? at : 0;
         float mean = 0.f, scale = 1.f;
         auto total = [&](bool squares) __attribute__((always_inline)) {
           float s = 0.f;
-          for (int chunk = lane; chunk * 16 < p.row_K; chunk += 64) {
+          for (int chunk = first; chunk * 16 < p.row_K; chunk += 64 * share) {
             load(row, chunk);
             const int in = p.row_K - chunk * 16;
 #pragma unroll
@@ -137,12 +141,19 @@ __global__ __launch_bounds__(WAVES * 64, SRC == FORM && KPW <= 2 ? 4 : 2) void d
           }
 #pragma unroll
           for (int d = 1; d < 64; d <<= 1) s += __shfl_xor(s, d);
+          if (share > 1) {
+            __syncthreads();
+            if (lane == 0) sums[wave] = s;
+            __syncthreads();
+            s = 0.f;
+            for (int u = 0; u < share; ++u) s += sums[wave / share * share + u];
+          }
           return s / (float)p.row_K;
         };
         if (p.norm.kind == STEM_NORM_LAYER) mean = total(false);
         if (p.norm.kind != STEM_NORM_NONE) scale = 1.0f / sqrtf(total(true) + p.norm.eps);
-        if (first) { weights(0); meeting(); first = false; }   // (behind the rows, which are waited for first)
-        for (int chunk = lane; chunk - lane < nkb * 8; chunk += 64) {
+        if (turn == 0) { weights(0); meeting(); }              // (behind the rows, which are waited for first)
+        for (int chunk = first; chunk - lane < nkb * 8; chunk += 64 * share) {
           load(row, chunk);
           const int in = p.row_K - chunk * 16;
           const QuantChunk g = p.norm.weight && in > 0 ? quant_load_chunk(static_cast<const bf16_t*>(p.norm.weight) + chunk * 16, in) : QuantChunk{};
@@ -154,10 +165,9 @@ __global__ __launch_bounds__(WAVES * 64, SRC == FORM && KPW <= 2 ? 4 : 2) void d
             if (p.norm.weight) x *= quant_element(g, q);
             v[q] = q < in ? x : 0.f;
           }
-          keep(row, chunk);
+          keep(row, at < rows ? chunk : nkb * 8);
         }
       }
-      if (first) { weights(0); meeting(); }
     } else {
       weights(0);
       meeting();
@@ -289,8 +299,10 @@ extern "C" void stem_route_qfloat_decode(int64_t T, int groups, int N, int K, in
 // LDS has room for 16 rows' values
 bool stem_qfloat_decode_inline(int64_t rows, int64_t K) { return rows <= 16 && K <= 8192; }
 
-hipError_t stem_qfloat_decode_launch(stem_ctx* ctx, int kid, const QfloatDecodeArgs& a, hipStream_t s) {
+hipError_t stem_qfloat_decode_launch(stem_ctx* ctx, int kid, const QfloatDecodeArgs& p, hipStream_t s) {
   ProfScope prof(ctx, kid, s);
+  QfloatDecodeArgs a = p;
+  a.share = a.groups.T > 4 ? 1 : a.groups.T > 2 ? 2 : a.groups.T > 1 ? 4 : 8;
   int32_t route[3];
   stem_route_qfloat_decode(a.groups.T, a.groups.offsets ? a.groups.n : 1, a.N, a.K, !a.x && !a.h, route);
   if (a.h_out) by_channels<1, ROWS, true>(a, route, s);        // (a gate product of up to 8 rows)

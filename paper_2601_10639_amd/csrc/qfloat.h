@@ -102,6 +102,7 @@ struct QfloatDecodeArgs {
   const bf16_t* x;
   int row_K;
   stem_norm norm;
+  int share;                // wavefronts that have a row of x behind a norm together, by the launcher
   const float* h;           // [T, row_K]
   bf16_t* y;                // [T, N], or null: a gate product of rows x
   const bf16_t* residual;
@@ -153,85 +154,106 @@ __device__ __forceinline__ uint32_t qfloat_four(float a, float b, float c, float
 }
 
 // ---- groups: every lane of a wavefront takes part -------------------------------------------------------------------------
-// f(group, first row, rows, tiles in front of its, its tiles, padded rows in front of its) for 64 groups at a time, a lane each; ends when f
-// says so (one answer for all lanes).  Returns the tiles of all groups that were seen.
-template <int TM, class F>
-__device__ __forceinline__ int qfloat_scan(const QfloatGroups& G, int lane, F f) {
-  auto at = [&](int i) __attribute__((always_inline)) {
-    const int v = G.offsets[i];
-    return v < 0 ? 0 : v > G.T ? G.T : v;
-  };
-  int last = at(0), tiles = 0, padded = 0;
-  for (int c = 0; c < G.n; c += 64) {
-    const int i = c + lane;
-    int hi = i < G.n ? at(i + 1) : 0;
-    hi = hi > last ? hi : last;
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) {
-      const int up = __shfl_up(hi, d);
-      hi = lane >= d && up > hi ? up : hi;
-    }
-    int lo = __shfl_up(hi, 1);
-    if (lane == 0) lo = last;
-    const int rows = hi - lo, nt = (rows + TM - 1) / TM, np = (rows + 127) / 128;
-    int st = nt, sp = np;
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) {
-      const int a = __shfl_up(st, d), b = __shfl_up(sp, d);
-      if (lane >= d) { st += a; sp += b; }
-    }
-    if (f(i, lo, rows, tiles + st - nt, nt, (padded + sp - np) * 128)) return tiles;
-    tiles += __builtin_amdgcn_readlane(st, 63);
-    padded += __builtin_amdgcn_readlane(sp, 63);
-    last = __builtin_amdgcn_readlane(hi, 63);
-  }
-  return tiles;
+// Over the lanes up to each, in registers: within rows of 16, then the last of the rows in front
+template <class F>
+__device__ __forceinline__ int qfloat_over_lanes(int v, F f) {       // f(0, v) = v
+  v = f(v, __builtin_amdgcn_update_dpp(0, v, 0x111, 0xf, 0xf, true));    // row_shr 1
+  v = f(v, __builtin_amdgcn_update_dpp(0, v, 0x112, 0xf, 0xf, true));
+  v = f(v, __builtin_amdgcn_update_dpp(0, v, 0x114, 0xf, 0xf, true));
+  v = f(v, __builtin_amdgcn_update_dpp(0, v, 0x118, 0xf, 0xf, true));
+  v = f(v, __builtin_amdgcn_update_dpp(0, v, 0x142, 0xa, 0xf, false));   // row_bcast 15 to rows 1 and 3
+  return f(v, __builtin_amdgcn_update_dpp(0, v, 0x143, 0xc, 0xf, false));   // row_bcast 31 to rows 2 and 3
 }
+// 64 groups, a lane each: first row, rows, tiles in front of its, its tiles, padded rows in front of its
+struct QfloatSpan { int lo, rows, before, tiles, padded; };
+struct QfloatSums { int last, tiles, blocks; };   // of the groups seen so far: the end, tiles, padded rows / 128
+__device__ __forceinline__ int qfloat_offset(const QfloatGroups& G, int i) {
+  const int v = G.offsets[i];
+  return v < 0 ? 0 : v > G.T ? G.T : v;
+}
+template <int TM>
+__device__ __forceinline__ QfloatSpan qfloat_span(const QfloatGroups& G, int first, int lane, QfloatSums& seen) {
+  const int i = first + lane;
+  int hi = i < G.n ? qfloat_offset(G, i + 1) : 0;
+  hi = hi > seen.last ? hi : seen.last;
+  hi = qfloat_over_lanes(hi, [](int a, int b) __attribute__((always_inline)) { return a > b ? a : b; });
+  int lo = __builtin_amdgcn_update_dpp(0, hi, 0x138, 0xf, 0xf, true);    // wave_shr 1
+  if (lane == 0) lo = seen.last;
+  auto add = [](int a, int b) __attribute__((always_inline)) { return a + b; };
+  const int rows = hi - lo, nt = (rows + TM - 1) / TM, np = (rows + 127) / 128;
+  const int st = qfloat_over_lanes(nt, add), sp = qfloat_over_lanes(np, add);
+  const QfloatSpan s = {lo, rows, seen.tiles + st - nt, nt, (seen.blocks + sp - np) * 128};
+  seen.last = __builtin_amdgcn_readlane(hi, 63);
+  seen.tiles += __builtin_amdgcn_readlane(st, 63);
+  seen.blocks += __builtin_amdgcn_readlane(sp, 63);
+  return s;
+}
+__device__ __forceinline__ QfloatSums qfloat_sums(const QfloatGroups& G) { return {qfloat_offset(G, 0), 0, 0}; }
 
 struct QfloatTile { int group, row, rows, padded; };   // first row, rows of the group from it on, its place in a form
-// Tile t of TM rows, the groups' tiles one behind another; false: there are not as many
+// whether tile t of TM rows is one of the 64 groups'
+template <int TM>
+__device__ __forceinline__ bool qfloat_in_span(const QfloatSpan& s, int first, int t, QfloatTile& out) {
+  const uint64_t mine = __ballot(t >= s.before && t < s.before + s.tiles);
+  if (!mine) return false;
+  const int l = __builtin_ctzll(mine), in = (t - __builtin_amdgcn_readlane(s.before, l)) * TM;
+  out = {first + l, __builtin_amdgcn_readlane(s.lo, l) + in, __builtin_amdgcn_readlane(s.rows, l) - in, __builtin_amdgcn_readlane(s.padded, l) + in};
+  return true;
+}
+// The tile that `which` names, given how many there are, the groups' tiles one behind another; false: it names none
+template <int TM, class F>
+__device__ __forceinline__ bool qfloat_tile_of(const QfloatGroups& G, int lane, QfloatTile& out, F which) {
+  if (!G.offsets) {
+    const int t = which((G.T + TM - 1) / TM);
+    out = {0, t * TM, G.T - t * TM, t * TM};
+    return t >= 0 && t * TM < G.T;
+  }
+  QfloatSums seen = qfloat_sums(G);
+  QfloatSpan s = qfloat_span<TM>(G, 0, lane, seen);
+  for (int c = 64; c < G.n; c += 64) (void)qfloat_span<TM>(G, c, lane, seen);
+  const int t = which(seen.tiles);
+  if (t < 0 || t >= seen.tiles) return false;
+  if (qfloat_in_span<TM>(s, 0, t, out)) return true;
+  seen = qfloat_sums(G);
+  for (int c = 0; c < G.n; c += 64) {
+    s = qfloat_span<TM>(G, c, lane, seen);
+    if (qfloat_in_span<TM>(s, c, t, out)) return true;
+  }
+  return false;
+}
 template <int TM>
 __device__ __forceinline__ bool qfloat_tile(const QfloatGroups& G, int t, int lane, QfloatTile& out) {
-  if (!G.offsets) {
-    out = {0, t * TM, G.T - t * TM, t * TM};
-    return t * TM < G.T;
-  }
-  int group = -1, row = 0, left = 0, place = 0;
-  qfloat_scan<TM>(G, lane, [&](int i, int lo, int rows, int before, int nt, int padded) __attribute__((always_inline)) {
-    const uint64_t mine = __ballot(t >= before && t < before + nt);
-    if (!mine) return false;
-    const int l = __builtin_ctzll(mine), in = (t - __builtin_amdgcn_readlane(before, l)) * TM;
-    group = __builtin_amdgcn_readlane(i, l);
-    row = __builtin_amdgcn_readlane(lo, l) + in;
-    left = __builtin_amdgcn_readlane(rows, l) - in;
-    place = __builtin_amdgcn_readlane(padded, l) + in;
-    return true;
-  });
-  out = {group, row, left, place};
-  return group >= 0;
+  return qfloat_tile_of<TM>(G, lane, out, [&](int) __attribute__((always_inline)) { return t; });
 }
-// tiles of TM rows of all groups
-template <int TM>
-__device__ __forceinline__ int qfloat_tiles(const QfloatGroups& G, int lane) {
-  if (!G.offsets) return (G.T + TM - 1) / TM;
-  return qfloat_scan<TM>(G, lane, [](int, int, int, int, int, int) __attribute__((always_inline)) { return false; });
+// A group's place in a form and its rows
+__device__ __forceinline__ void qfloat_group(const QfloatGroups& G, int g, int lane, int& padded, int& rows) {
+  QfloatSums seen = qfloat_sums(G);
+  for (int c = 0; c < G.n; c += 64) {
+    const QfloatSpan s = qfloat_span<128>(G, c, lane, seen);
+    if (g < c + 64) {
+      padded = __builtin_amdgcn_readlane(s.padded, g - c);
+      rows = __builtin_amdgcn_readlane(s.rows, g - c);
+      return;
+    }
+  }
 }
 // The place in a form of each lane's row, which LANES neighbouring lanes share; -1: it belongs to no group.  One after another.
 template <int LANES>
 __device__ __forceinline__ int qfloat_place(const QfloatGroups& G, int row, int lane) {
   int place = -1;
-  qfloat_scan<128>(G, lane, [&](int, int lo, int rows, int, int, int padded) __attribute__((always_inline)) {
+  QfloatSums seen = qfloat_sums(G);
+  for (int c = 0; c < G.n; c += 64) {
+    const QfloatSpan s = qfloat_span<128>(G, c, lane, seen);
 #pragma unroll
     for (int h = 0; h < 64; h += LANES) {
       const int r = __builtin_amdgcn_readlane(row, h);
-      const uint64_t mine = __ballot(r >= lo && r < lo + rows);
+      const uint64_t mine = __ballot(r >= s.lo && r < s.lo + s.rows);
       if (mine) {
         const int at = __builtin_ctzll(mine);
-        const int found = __builtin_amdgcn_readlane(padded, at) + r - __builtin_amdgcn_readlane(lo, at);   // (of all lanes: not in the branch)
+        const int found = __builtin_amdgcn_readlane(s.padded, at) + r - __builtin_amdgcn_readlane(s.lo, at);   // (of all lanes: not in the branch)
         if (lane / LANES * LANES == h) place = found;
       }
     }
-    return false;
-  });
+  }
   return place;
 }
