@@ -7,6 +7,7 @@
 // is (buffer_load ... lds), a fragment is the 32 bytes of two blocks at 16 x lane: no swizzle, no bank conflict.  The scales of a K tile are a word a
 // lane for each 128 rows of an operand, which goes straight to a register some K tiles ahead.
 #include <algorithm>
+#include <type_traits>
 #include <utility>
 
 #include "qfloat.h"
@@ -25,7 +26,7 @@ namespace {
 
 constexpr uint32_t OOB = 0x80000000u;   // a buffer offset beyond any operand: reads as zero, is not stored
 constexpr int SC1 = 16;                 // cache policy bit of the buffer instructions: device scope
-constexpr int MAX_SLICES = 4;
+constexpr int MAX_SLICES = 4, MAX_WEIGHT_SLICES = 16;
 
 __device__ __forceinline__ float sigmoidf_fast(float z) { return __builtin_amdgcn_rcpf(1.0f + __expf(-z)); }
 __device__ __forceinline__ void lds_dma_16(rsrc_t rs, char* lds_dst, uint32_t off, int soff) {
@@ -77,7 +78,7 @@ struct Work {
   int n0;
   int k0, nk;          // K tiles
   int group;
-  int tile, tiles, slice;   // of the output, of K slices
+  int tile, tiles, slice;   // of all outputs, of K slices
 };
 template <int TM, int TN, bool BY_K>
 __device__ __forceinline__ bool find_work(const QfloatGemmArgs& p, int lane, Work& w) {
@@ -100,18 +101,19 @@ __device__ __forceinline__ bool find_work(const QfloatGemmArgs& p, int lane, Wor
     tile_of(blockIdx.x - part * tiles, tiles, ntm, ntn, tm, tn);
     t = {0, tm * TM, p.M - tm * TM, tm * TM};
     if (BY_K && grouped) {                                   // all of the output for each group of K
-      int rows = 0;
-      qfloat_group(p.groups, part, lane, k0, rows);
-      t.group = part;
+      t.group = part / p.ksplit;
+      part -= t.group * p.ksplit;
+      qfloat_group(p.groups, t.group, lane, k0, nk);
       k0 /= 64;                                              // (bf16: 64 rows a K tile)
-      nk = (rows + 63) / 64;
-    } else if (p.ksplit > 1) {
-      const int per = (nk_all + p.ksplit - 1) / p.ksplit;
-      k0 = part * per;
-      nk = nk_all - k0 < per ? nk_all - k0 : per;
+      nk = (nk + 63) / 64;
+    }
+    if (p.ksplit > 1) {                                      // (a group's may be without any)
+      const int per = (nk + p.ksplit - 1) / p.ksplit;
+      k0 += part * per;
+      nk = min(max(nk - part * per, 0), per);
     }
   }
-  w = {t.row, t.rows, t.padded, tn * TN, k0, nk, t.group, tm * ntn + tn, tiles, grouped ? 0 : part};
+  w = {t.row, t.rows, t.padded, tn * TN, k0, nk, t.group, BY_K ? (t.group * tiles) + tm * ntn + tn : tm * ntn + tn, BY_K && grouped ? tiles * p.groups.n : tiles, part};
   return true;
 }
 
@@ -158,13 +160,45 @@ struct Output {
   static constexpr int BYTES = 32 * PITCH * 4;                 // of LDS, for each wavefront
   static constexpr int V = F32 ? 4 : 8, LPR = COLS / V, RPP = 64 / LPR, PASSES = 32 / RPP;
 
-  // out: row m0, column n0 of it; rows and cols: how many there are
+  // What a block of 32 rows is added to, requested before the block in front of it is stored: a load behind a store that may lie over it waits for it.
+  struct Before {
+    u32x4_t pass[PASSES], edge;
+  };
+  // 16 bytes of results z and of what they are added to
+  static __device__ __forceinline__ u32x4_t sum(const float (&z)[V], u32x4_t v) {
+    if constexpr (F32) {
+#pragma unroll
+      for (int q = 0; q < 4; ++q) v[q] = __float_as_uint(z[q] + __uint_as_float(v[q]));
+      return v;
+    } else {
+      bf16x8_t o;
+#pragma unroll
+      for (int q = 0; q < 8; ++q) o[q] = (__bf16)(z[q] + __uint_as_float(q & 1 ? v[q >> 1] & 0xffff0000u : v[q >> 1] << 16));
+      return __builtin_bit_cast(u32x4_t, o);
+    }
+  }
+
+  // rows from m0 on, how many there are of them, columns from n0 on
   static __device__ __forceinline__ void run(const QfloatGemmArgs& p, const f32x16_t (&acc)[MI][NJ], char* stg, int64_t m0, int n0, int rows, int64_t base, int lane) {
-    const int lim = p.N - n0;
+    typedef typename std::conditional<F32, float, bf16_t>::type E;
+    const int lim = p.N - n0 < COLS ? p.N - n0 : COLS;
     if (rows <= 0 || lim <= 0) return;
     float* const st = reinterpret_cast<float*>(stg);
-    const int srow = lane / LPR, scol = (lane % LPR) * V, left = lim - scol;
-    const int64_t at = base + m0 * p.N + n0 + scol;
+    const int srow = lane / LPR, scol = (lane % LPR) * V;
+    const bool adds = F32 ? p.accumulate != 0 : p.residual != nullptr;
+    // columns behind the last whole V: rows take one lane each, for the row's last V (some of them again), or one by one where there are fewer
+    const bool edge = lim % V != 0;
+    E* const out = (F32 ? reinterpret_cast<E*>(p.c) : reinterpret_cast<E*>(p.y)) + base + m0 * p.N + n0;
+    const E* const in = (F32 ? reinterpret_cast<const E*>(p.c) : reinterpret_cast<const E*>(p.residual)) + base + m0 * p.N + n0;
+    auto fetch = [&](int i, Before& b) __attribute__((always_inline)) {
+      if (!adds || lim < V) return;
+#pragma unroll
+      for (int pass = 0; pass < PASSES; ++pass)
+        __builtin_memcpy(&b.pass[pass], in + (int64_t)min(i * 32 + pass * RPP + srow, rows - 1) * p.N + min(scol, lim - V), 16);
+      if (edge) __builtin_memcpy(&b.edge, in + (int64_t)min(i * 32 + (lane & 31), rows - 1) * p.N + lim - V, 16);
+    };
+    Before before[2] = {};
+    fetch(0, before[0]);
 #pragma unroll
     for (int i = 0; i < MI; ++i) {
       if (i * 32 >= rows) return;
@@ -176,37 +210,31 @@ struct Output {
           *reinterpret_cast<f32x4_t*>(st + (lane & 31) * PITCH + j * 32 + g * 8 + (lane >> 5) * 4) = w;
         }
       in_order();
+      if (i + 1 < MI) fetch(i + 1, before[(i + 1) & 1]);
+      const Before& b = before[i & 1];
 #pragma unroll
       for (int pass = 0; pass < PASSES; ++pass) {
         const int r = i * 32 + pass * RPP + srow;
         float z[V];
         __builtin_memcpy(z, st + (pass * RPP + srow) * PITCH + scol, sizeof z);
-        if (r >= rows) continue;
-        const int64_t to = at + (int64_t)r * p.N;
-        if (left >= V) {
-          if constexpr (F32) {
-            if (p.accumulate) {
-              float c[4];
-              __builtin_memcpy(c, p.c + to, 16);
+        const u32x4_t v = sum(z, b.pass[pass]);
+        if (r < rows && scol + V <= lim) __builtin_memcpy(out + (int64_t)r * p.N + scol, &v, 16);
+      }
+      if (edge) {
+        const int r = i * 32 + (lane & 31);
+        const float* const from = st + (lane & 31) * PITCH;
+        if (lim >= V) {
+          float z[V];
 #pragma unroll
-              for (int q = 0; q < 4; ++q) z[q] += c[q];
-            }
-            __builtin_memcpy(p.c + to, z, 16);
-          } else {
-            u32x4_t v = {};
-            if (p.residual) __builtin_memcpy(&v, p.residual + to, 16);
-            bf16x8_t o;
-#pragma unroll
-            for (int q = 0; q < 8; ++q) o[q] = (__bf16)(z[q] + __uint_as_float(q & 1 ? v[q >> 1] & 0xffff0000u : v[q >> 1] << 16));
-            __builtin_memcpy(p.y + to, &o, 16);
+          for (int q = 0; q < V; ++q) z[q] = from[lim - V + q];
+          const u32x4_t v = sum(z, b.edge);
+          if (lane < 32 && r < rows) __builtin_memcpy(out + (int64_t)r * p.N + lim - V, &v, 16);
+        } else if (lane < 32 && r < rows) {
+          for (int q = 0; q < lim; ++q) {
+            const int64_t to = (int64_t)r * p.N + q;
+            if constexpr (F32) out[to] = adds ? in[to] + from[q] : from[q];
+            else out[to] = __builtin_bit_cast(uint16_t, (__bf16)(from[q] + (adds ? __uint_as_float((uint32_t)in[to] << 16) : 0.f)));
           }
-        } else {
-#pragma unroll
-          for (int q = 0; q < V; ++q)
-            if (q < left) {
-              if constexpr (F32) p.c[to + q] = p.accumulate ? p.c[to + q] + z[q] : z[q];
-              else p.y[to + q] = __builtin_bit_cast(uint16_t, (__bf16)(z[q] + (p.residual ? __uint_as_float((uint32_t)p.residual[to + q] << 16) : 0.f)));
-            }
         }
       }
       in_order();   // all have read the rows before they are staged over
@@ -424,30 +452,33 @@ constexpr int PAIR_A = 8192, PAIR_SLOT = 24576;
 
 template <QfloatOut OUT>
 __global__ __launch_bounds__(256, 2) void pair_kernel(QfloatGemmArgs p) {
-  typedef Output<2, 4, false> Out;
+  constexpr bool HALF = OUT == QFLOAT_F32;
+  typedef Output<2, 4, HALF> Out;
   typedef Hidden<2> Hid;
   static_assert(4 * Hid::BYTES <= 3 * PAIR_SLOT && 4 * Out::BYTES <= 3 * PAIR_SLOT, "room for the epilogue");
   __shared__ __attribute__((aligned(16))) char smem[3 * PAIR_SLOT];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wm = wave >> 1, wn = wave & 1;
   Work w;
-  if (!find_work<128, 256, false>(p, lane, w)) return;
-  const int nk = p.K / 64, nkb = p.K / 128, kbytes = p.K * 32;
+  if (!find_work<128, 256, HALF>(p, lane, w)) return;
+  const int nkb = p.K / 128, nk = w.nk * 2, kbytes = p.K * 32;
   const int64_t b_bytes = stem_qfloat_pitch(p.N) * p.K;
-  const uint8_t *const B = p.B + w.group * p.stride_b, *const sb = p.sb + w.group * p.stride_b;
+  const uint8_t *const B = p.B + (HALF ? 0 : w.group * p.stride_b), *const sb = p.sb + (HALF ? 0 : w.group * p.stride_b);
   int id[1];
   if (OUT == QFLOAT_HIDDEN) load_ids<2>(p, w.m0 + wm * 64, w.rows - wm * 64, lane, id);
   const rsrc_t none = resource(p.A, 0);
-  rsrc_t ra = resource(p.A, p.a_bytes), rb = resource(B, b_bytes);
+  rsrc_t ra = nk ? resource(p.A, p.a_bytes) : none, rb = nk ? resource(B, b_bytes) : none;
   Scales ca, cb;
-  ca.init(p.sa, p.a_bytes / 128, w.pa + wm * 64, nkb, lane);
-  cb.init(sb, b_bytes / 128, w.n0 + wn * 128, nkb, lane);
+  if constexpr (!HALF) {
+    ca.init(p.sa, p.a_bytes / 128, w.pa + wm * 64, nkb, lane);
+    cb.init(sb, b_bytes / 128, w.n0 + wn * 128, nkb, lane);
+  }
   // a wavefront loads one 32-row group of the tokens and two of the weights: 2 KB of each and K tile
   const uint32_t oa = wave * 32 < w.rows ? (uint32_t)((w.pa + wave * 32) * p.K + lane * 16) : OOB;
   uint32_t ob[2];
 #pragma unroll
   for (int h = 0; h < 2; ++h) ob[h] = w.n0 + wave * 64 + h * 32 < p.N ? (uint32_t)((w.n0 + wave * 64 + h * 32) * p.K + lane * 16) : OOB;
-  int ks = nk >= 32 ? (int)(blockIdx.x & 7) * (nk >> 4) : 0, k = ks * 4096, left = nk;   // (blocks of 128)
+  int ks = HALF ? w.k0 : nk >= 32 ? (int)(blockIdx.x & 7) * (nk >> 4) : 0, k = ks * 4096, left = nk;   // (blocks of 128)
   auto issue = [&](int q, char* slot) __attribute__((always_inline)) {   // load q of 6
     if (q < 2) lds_dma_16(ra, slot + (wave * 2 + q) * 1024, oa, k + q * 1024);
     else lds_dma_16(rb, slot + PAIR_A + (wave * 4 + q - 2) * 1024, ob[(q - 2) >> 1], k + (q & 1) * 1024);
@@ -470,7 +501,11 @@ __global__ __launch_bounds__(256, 2) void pair_kernel(QfloatGemmArgs p) {
     const char* const at = (isA[q] ? fa : fb) + slot * PAIR_SLOT + idx[q] * 2048;
     (isA[q] ? a[idx[q]] : b[idx[q]]) = join(*reinterpret_cast<const i32x4_t*>(at), *reinterpret_cast<const i32x4_t*>(at + 1024));
   };
-  uint32_t sa = ca.load(ks) >> ca.shift, sb_ = cb.load(ks), na = 0, nb = 0;
+  uint32_t sa = 0, sb_ = 0, na = 0, nb = 0;
+  if constexpr (!HALF) {
+    sa = ca.load(ks) >> ca.shift;
+    sb_ = cb.load(ks);
+  }
 #pragma unroll
   for (int st = 0; st < 3; ++st) {
 #pragma unroll
@@ -487,7 +522,7 @@ __global__ __launch_bounds__(256, 2) void pair_kernel(QfloatGemmArgs p) {
     asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(6) : "memory");
     __builtin_amdgcn_s_barrier();
     __builtin_amdgcn_sched_barrier(0);
-    if (even) {
+    if (!HALF && even) {
       if (++ks >= nkb) ks = 0;
       na = ca.load(ks);
       nb = cb.load(ks);
@@ -500,11 +535,12 @@ __global__ __launch_bounds__(256, 2) void pair_kernel(QfloatGemmArgs p) {
         read((st + 1) % 3, u, c, d);
         issue(u, smem + st * PAIR_SLOT);
       }
-      acc[ii[u]][jj[u]] = mma<jj[u], ii[u]>(b[jj[u]], a[ii[u]], acc[ii[u]][jj[u]], sb_, sa);
+      if constexpr (HALF) acc[ii[u]][jj[u]] = mma_bf16(b[jj[u]], a[ii[u]], acc[ii[u]][jj[u]]);
+      else acc[ii[u]][jj[u]] = mma<jj[u], ii[u]>(b[jj[u]], a[ii[u]], acc[ii[u]][jj[u]], sb_, sa);
       __builtin_amdgcn_sched_barrier(0);
     }, std::make_integer_sequence<int, 8>{});
     next();
-    if (!even) {
+    if (!HALF && !even) {
       sa = na >> ca.shift;
       sb_ = nb;
     }
@@ -529,7 +565,7 @@ __global__ __launch_bounds__(256, 2) void pair_kernel(QfloatGemmArgs p) {
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
   __syncthreads();
   if constexpr (OUT == QFLOAT_HIDDEN) Hid::run(p, acc, id, smem + wave * Hid::BYTES, w.pa + wm * 64, w.n0 + wn * 128, w.rows - wm * 64, lane);
-  else Out::run(p, acc, smem + wave * Out::BYTES, w.m0 + wm * 64, w.n0 + wn * 128, w.rows - wm * 64, 0, lane);
+  else Out::run(p, acc, smem + wave * Out::BYTES, w.m0 + wm * 64, w.n0 + wn * 128, w.rows - wm * 64, HALF ? (int64_t)w.group * p.M * p.N : 0, lane);
 }
 
 // ---- tiles with wavefronts that load: STAGES whole K tiles in LDS ----------------------------------------------------------------------
@@ -720,7 +756,7 @@ typedef Tiling<1, 4, 2, 1, 6, 4> Hidden64;      // 64 x 128
 template <QfloatOut OUT>
 unsigned grid_of(const QfloatGemmArgs& a, int tm, int tn) {
   const int64_t ntn = (a.N + tn - 1) / tn, ntm = (a.M + tm - 1) / tm;
-  if (OUT == QFLOAT_F32) return (unsigned)(ntm * ntn * (a.groups.offsets ? a.groups.n : a.ksplit));
+  if (OUT == QFLOAT_F32) return (unsigned)(ntm * ntn * (a.groups.offsets ? a.groups.n : 1) * a.ksplit);
   if (a.groups.offsets) return (unsigned)(((a.groups.T + tm - 1) / tm + std::min(a.groups.n, a.groups.T) - 1) * ntn);   // at most: each group may have a tile not full
   return (unsigned)(ntm * ntn * a.ksplit);
 }
@@ -737,7 +773,8 @@ hipError_t launch(const QfloatGemmArgs& a, hipStream_t s) {
 // ---- choice of the tile and of the K slices ----------------------------------------------------------------------------------------
 extern "C" void stem_route_qfloat(int64_t T, int groups, int N, int K, int out, int64_t ws_bytes, int32_t* route) {
   const int64_t per_group = (T + groups - 1) / groups;       // of an average group, which is all that is known here
-  auto tiles = [&](int tm, int tn) { return (per_group + tm - 1) / tm * groups * ((N + tn - 1) / tn); };
+  auto tiles_of = [&](int64_t rows, int tm, int tn) { return (rows + tm - 1) / tm * ((N + tn - 1) / tn); };
+  auto tiles = [&](int tm, int tn) { return tiles_of(per_group, tm, tn) * groups; };
   const int nk = K / 128;
   int rows = 128, cols = 128, slices = 1;
   if (out == QFLOAT_HIDDEN) {
@@ -753,12 +790,17 @@ extern "C" void stem_route_qfloat(int64_t T, int groups, int N, int K, int out, 
       if ((double)((tiles(256, 256) + 255) / 256) <= few) rows = 256;
     }
   }
-  if ((out == QFLOAT_F32 || (out == QFLOAT_BF16 && cols == 64)) && groups == 1) {
+  if (out == QFLOAT_F32) {
+    // T: rows of the output, all of it for each group; K: of an average group
+    const int64_t n = tiles_of(T, 128, 128) * groups;
+    if (n > 256) cols = 256;
+    else slices = (int)std::min<int64_t>({MAX_WEIGHT_SLICES, nk / 8, 256 / n});
+  } else if (out == QFLOAT_BF16 && cols == 64 && groups == 1) {
     slices = nk < 32 ? 1 : (int)std::min<int64_t>({MAX_SLICES, nk / 10, 240 / tiles(rows, cols)});
-    while (slices > 1 && (slices * tiles(rows, cols) * rows * cols * 4 > ws_bytes || tiles(rows, cols) > STEM_TICKETS)) --slices;
-    while (slices > 1 && (nk + slices - 1) / slices * (slices - 1) >= nk) --slices;   // every slice has a part of K
-    if (slices < 1) slices = 1;
   }
+  while (slices > 1 && slices * rows * cols * 4 * (out == QFLOAT_F32 ? tiles_of(T, 128, 128) * groups : tiles(rows, cols)) > ws_bytes) --slices;
+  while (slices > 1 && (nk + slices - 1) / slices * (slices - 1) >= nk) --slices;   // every slice has a part of K
+  if (slices < 1) slices = 1;
   route[0] = rows; route[1] = cols; route[2] = slices;
 }
 
@@ -766,11 +808,12 @@ hipError_t stem_qfloat_gemm_launch(stem_ctx* ctx, int kid, QfloatOut out, const 
   ProfScope prof(ctx, kid, s);
   QfloatGemmArgs a = p;
   int32_t route[3];
-  // (all of a weight gradient's output for each group)
-  stem_route_qfloat(a.M, out == QFLOAT_F32 ? 1 : a.groups.n, a.N, a.K, out, a.ws_bytes, route);
-  a.ksplit = a.groups.offsets ? 1 : route[2];
-  if (out == QFLOAT_F32) return launch<QFLOAT_F32, Tile128>(a, s);
-  if (route[0] == 256) ring_kernel<<<grid_of<QFLOAT_BF16>(a, 256, 256), 256, 0, s>>>(a);
+  const int nk = out == QFLOAT_F32 ? (int)(((int64_t)a.groups.T / a.groups.n + 63) / 64) : a.K / 128;
+  stem_route_qfloat(a.M, a.groups.n, a.N, nk * 128, out, a.ws_bytes, route);
+  a.ksplit = a.groups.offsets && out != QFLOAT_F32 ? 1 : route[2];
+  if (out == QFLOAT_F32 && route[1] == 256) pair_kernel<QFLOAT_F32><<<grid_of<QFLOAT_F32>(a, 128, 256), 256, 0, s>>>(a);
+  else if (out == QFLOAT_F32) return launch<QFLOAT_F32, Tile128>(a, s);
+  else if (route[0] == 256) ring_kernel<<<grid_of<QFLOAT_BF16>(a, 256, 256), 256, 0, s>>>(a);
   else if (route[1] == 256 && out == QFLOAT_HIDDEN) pair_kernel<QFLOAT_HIDDEN><<<grid_of<QFLOAT_HIDDEN>(a, 128, 256), 256, 0, s>>>(a);
   else if (route[1] == 256) pair_kernel<QFLOAT_BF16><<<grid_of<QFLOAT_BF16>(a, 128, 256), 256, 0, s>>>(a);
   else if (out == QFLOAT_HIDDEN) return route[0] == 64 ? launch<QFLOAT_HIDDEN, Hidden64>(a, s) : launch<QFLOAT_HIDDEN, Hidden128>(a, s);

@@ -99,7 +99,7 @@ __global__ __launch_bounds__(WAVES * 64, SRC == FORM && KPW <= 2 ? 4 : 2) void d
       const int k = chunk * 16;
       const int64_t at = (int64_t)(tile.row + row) * p.row_K + k;
       if constexpr (SRC == ROWS) {
-        const QuantChunk x = k < p.row_K ? quant_load_chunk(p.x + at, p.row_K - k) : QuantChunk{};
+        const QuantChunk x = k < p.row_K ? qfloat_chunk(p.x + at, p.row_K - k) : QuantChunk{};
 #pragma unroll
         for (int q = 0; q < 16; ++q) v[q] = quant_element(x, q);
       } else {
@@ -156,7 +156,7 @@ __global__ __launch_bounds__(WAVES * 64, SRC == FORM && KPW <= 2 ? 4 : 2) void d
         for (int chunk = first; chunk - lane < nkb * 8; chunk += 64 * share) {
           load(row, chunk);
           const int in = p.row_K - chunk * 16;
-          const QuantChunk g = p.norm.weight && in > 0 ? quant_load_chunk(static_cast<const bf16_t*>(p.norm.weight) + chunk * 16, in) : QuantChunk{};
+          const QuantChunk g = p.norm.weight && in > 0 ? qfloat_chunk(static_cast<const bf16_t*>(p.norm.weight) + chunk * 16, in) : QuantChunk{};
 #pragma unroll
           for (int q = 0; q < 16; ++q) {
             float x = v[q];

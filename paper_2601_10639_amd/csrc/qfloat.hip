@@ -49,7 +49,7 @@ __global__ __launch_bounds__(256) void chunks_kernel(QfloatRowsArgs p) {
 #pragma unroll
       for (int g = 0; g < 4; ++g) hid[u][g] = live && at < p.K ? *reinterpret_cast<const f32x4_t*>(p.h + first + at + 4 * g) : f32x4_t{};   // (d_ff: multiples of 64)
     } else {
-      raw[u] = live && at < p.K ? quant_load_chunk(p.x + first + at, p.K - at) : QuantChunk{};
+      raw[u] = live && at < p.K ? qfloat_chunk(p.x + first + at, p.K - at) : QuantChunk{};
     }
   }
   auto value = [&](int u, int q) __attribute__((always_inline)) {
@@ -88,7 +88,7 @@ __global__ __launch_bounds__(256) void rows_kernel(QfloatRowsArgs p) {
   const bf16_t* const x = p.x + (int64_t)(live ? row : 0) * p.K;
   auto fetch = [&](int t) __attribute__((always_inline)) {
     const int c = t * LPR + l;
-    return live && c * 16 < p.K ? quant_load_chunk(x + c * 16, p.K - c * 16) : QuantChunk{};
+    return live && c * 16 < p.K ? qfloat_chunk(x + c * 16, p.K - c * 16) : QuantChunk{};
   };
   QuantChunk raw[HELD] = {};
   if constexpr (CPT > 0) {
@@ -140,7 +140,7 @@ __global__ __launch_bounds__(256) void rows_kernel(QfloatRowsArgs p) {
     const int c = t * LPR + l, in = p.K - c * 16;
     const QuantChunk x = chunk(t);
     QuantChunk g = {};
-    if (p.norm.weight && in > 0) g = quant_load_chunk(static_cast<const bf16_t*>(p.norm.weight) + c * 16, in);
+    if (p.norm.weight && in > 0) g = qfloat_chunk(static_cast<const bf16_t*>(p.norm.weight) + c * 16, in);
     float u[16];
 #pragma unroll
     for (int q = 0; q < 16; ++q) u[q] = quant_element(x, q);
@@ -173,7 +173,7 @@ __device__ __forceinline__ void load_tile(const bf16_t* x, int cols, int rows, i
 #pragma unroll
   for (int r = 0; r < 4; ++r) {
     const int in = quad * 4 + r;
-    raw[r] = in < rows && col < cols ? quant_load_chunk(x + (int64_t)in * cols + col, cols - col) : QuantChunk{};
+    raw[r] = in < rows && col < cols ? qfloat_chunk(x + (int64_t)in * cols + col, cols - col) : QuantChunk{};
   }
 }
 // a lane's four rows of a form whose rows have nkb blocks

@@ -20,6 +20,7 @@ FEW = {"8 channels": (3, 1000, 1000), "16 channels": (5, 3001, 2000), "32 channe
        "form, 32 rows": (50, 5000, 2000), "form, 32 rows, 16 channels": (250, 1030, 1100)}
 GATES = {"64x128": (100, 128, 320), "128x128": (1500, 192, 1600), "pair": (4400, 128, 2240), "few, inline": (8, 256, 1024), "few, by a kernel": (8, 128, 4160)}
 WEIGHT_SLICES = (3000, 300, 200)
+WEIGHTS = [(9001, 100, 129, 1), (5000, 130, 260, 3), (300, 2100, 2300, 1), (700, 1200, 1301, 3)]   # T, N, K, groups
 
 
 def check_rows(ctx, T, N, K, rows):
@@ -72,7 +73,7 @@ def test_few_rows_of_groups():
 
 
 def test_one_group_with_offsets():
-    """Rows in front of it and behind it are left as they were; the weight gradient is that of its rows, and not cut."""
+    """Rows in front of it and behind it are left as they were; the weight gradient is that of its rows."""
     T, N, K = WEIGHT_SLICES
     ctx = make_ctx(T, 64, 320, backward=True)
     for offsets in ([0, T], [7, T - 100], [5, 5], [T, T]):
@@ -83,6 +84,17 @@ def test_one_group_with_offsets():
 def test_weight_gradient_in_slices():
     T, N, K = WEIGHT_SLICES
     check_backward(make_ctx(T, 64, 320, backward=True), T, N, K)
+
+
+@pytest.mark.parametrize("T,N,K,groups", WEIGHTS)
+def test_weight_gradients_in_slices_and_pairs(T, N, K, groups):
+    """Also of groups without rows, and of one that has nearly all, whose slices are those of the average."""
+    ctx = make_ctx(T, 64, wide(K, N), groups=groups, backward=True)
+    if groups == 1:
+        check_backward(ctx, T, N, K)
+    else:
+        check_backward(ctx, T, N, K, groups, offsets_of(T, T, groups))
+        check_backward(ctx, T, N, K, groups, np.array([3] * (groups - 1) + [T - 60, T], np.int32))
 
 
 @pytest.mark.parametrize("T", [2, 40])

@@ -57,7 +57,9 @@ def test_gates_of_few_rows():
 
 def test_weight_gradient():
     T, N, K = G.WEIGHT_SLICES
-    assert tiles(N, K, -(-T // 128) * 256, F32) == (128, 128, 4)
+    assert tiles(N, K, -(-T // 64) * 128, F32) == (128, 128, 5)
+    for (T, N, K, groups), want in zip(G.WEIGHTS, [(128, 128, 16), (128, 128, 3), (128, 256, 1), (128, 256, 1)]):
+        assert tiles(N, K, -(-T // groups // 64) * 128, F32, groups) == want
 
 
 def test_slices_fit_their_room():
@@ -67,7 +69,7 @@ def test_slices_fit_their_room():
                 for out in (BF16, F32, HIDDEN):
                     for groups in (1, 4):
                         rows, cols, slices = tiles(T, N, K, out, groups)
-                        n = -(-T // rows) * -(-N // cols)
-                        assert slices == 1 or (groups == 1 and out != HIDDEN and n <= 256 and slices * n * rows * cols * 4 <= WS)
+                        n = -(-T // rows) * -(-N // cols) * (groups if out == F32 else 1)
+                        assert slices == 1 or ((groups == 1 or out == F32) and out != HIDDEN and slices * n <= 256 and slices * n * rows * cols * 4 <= WS)
                         nk = -(-K // 128)
                         assert -(-nk // slices) * (slices - 1) < nk          # every slice has a part of K
