@@ -26,7 +26,7 @@ namespace {
 
 constexpr uint32_t OOB = 0x80000000u;   // a buffer offset beyond any operand: reads as zero, is not stored
 constexpr int SC1 = 16;                 // cache policy bit of the buffer instructions: device scope
-constexpr int MAX_SLICES = 4, MAX_WEIGHT_SLICES = 16;
+constexpr int MAX_SLICES = 4, MAX_WEIGHT_SLICES = 8;
 
 __device__ __forceinline__ float sigmoidf_fast(float z) { return __builtin_amdgcn_rcpf(1.0f + __expf(-z)); }
 __device__ __forceinline__ void lds_dma_16(rsrc_t rs, char* lds_dst, uint32_t off, int soff) {
@@ -603,15 +603,22 @@ __device__ __forceinline__ bool last_slice(const QfloatGemmArgs& p, f32x16_t (&a
   for (int i = 0; i < MI; ++i)
 #pragma unroll
     for (int j = 0; j < NJ; ++j) acc[i][j] = f32x16_t{};
-  for (int s = 0; s < p.ksplit; ++s) {
-    f32x4_t v[N];
+  constexpr int SLICES = 32 / N;                               // whose loads are under way together
+  for (int s = 0; s < p.ksplit; s += SLICES) {
+    f32x4_t v[SLICES][N];
 #pragma unroll
-    for (int k = 0; k < N; ++k)
-      v[k] = __builtin_bit_cast(f32x4_t, __builtin_amdgcn_raw_buffer_load_b128(rw, (uint32_t)(lane * 16), (at + s * stride) * BYTES + k * 1024, SC1));
+    for (int u = 0; u < SLICES; ++u)
 #pragma unroll
-    for (int k = 0; k < N; ++k)
+      for (int k = 0; k < N; ++k)
+        v[u][k] = __builtin_bit_cast(f32x4_t, __builtin_amdgcn_raw_buffer_load_b128(rw, (uint32_t)(lane * 16), (at + min(s + u, p.ksplit - 1) * stride) * BYTES + k * 1024, SC1));
 #pragma unroll
-      for (int q = 0; q < 4; ++q) acc[k / 4 / NJ][k / 4 % NJ][4 * (k % 4) + q] += v[k][q];
+    for (int u = 0; u < SLICES; ++u) {
+      if (s + u >= p.ksplit) break;
+#pragma unroll
+      for (int k = 0; k < N; ++k)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) acc[k / 4 / NJ][k / 4 % NJ][4 * (k % 4) + q] += v[u][k][q];
+    }
   }
   __syncthreads();   // the ticket has been read: LDS may be used again
   return true;

@@ -97,15 +97,16 @@ __global__ __launch_bounds__(WAVES * 64, SRC == FORM && KPW <= 2 ? 4 : 2) void d
     float v[16];
     auto load = [&](int row, int chunk) __attribute__((always_inline)) {
       const int k = chunk * 16;
-      const int64_t at = (int64_t)(tile.row + row) * p.row_K + k;
+      const int64_t first = (int64_t)(tile.row + row) * p.row_K;
       if constexpr (SRC == ROWS) {
-        const QuantChunk x = k < p.row_K ? qfloat_chunk(p.x + at, p.row_K - k) : QuantChunk{};
+        QuantChunk x = qfloat_fetch(p.x + first, k, p.row_K);
+        qfloat_settle(x, p.row_K - k);
 #pragma unroll
         for (int q = 0; q < 16; ++q) v[q] = quant_element(x, q);
       } else {
 #pragma unroll
         for (int h = 0; h < 4; ++h) {                          // (d_ff is a multiple of 64)
-          const f32x4_t x = k < p.row_K ? *reinterpret_cast<const f32x4_t*>(p.h + at + h * 4) : f32x4_t{};
+          const f32x4_t x = k < p.row_K ? *reinterpret_cast<const f32x4_t*>(p.h + first + k + h * 4) : f32x4_t{};
 #pragma unroll
           for (int q = 0; q < 4; ++q) v[4 * h + q] = x[q];
         }
@@ -156,7 +157,11 @@ __global__ __launch_bounds__(WAVES * 64, SRC == FORM && KPW <= 2 ? 4 : 2) void d
         for (int chunk = first; chunk - lane < nkb * 8; chunk += 64 * share) {
           load(row, chunk);
           const int in = p.row_K - chunk * 16;
-          const QuantChunk g = p.norm.weight && in > 0 ? qfloat_chunk(static_cast<const bf16_t*>(p.norm.weight) + chunk * 16, in) : QuantChunk{};
+          QuantChunk g = {};
+          if (p.norm.weight) {
+            g = qfloat_fetch(static_cast<const bf16_t*>(p.norm.weight), chunk * 16, p.row_K);
+            qfloat_settle(g, in);
+          }
 #pragma unroll
           for (int q = 0; q < 16; ++q) {
             float x = v[q];

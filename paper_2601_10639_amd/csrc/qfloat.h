@@ -126,22 +126,29 @@ __device__ __forceinline__ uint32_t qfloat_magnitude(float v) {
   const uint32_t b = __float_as_uint(v) & 0x7fffffffu;
   return b < 0x7f800000u ? b : 0u;
 }
-// 16 values of a row that has `left` more, at least one (rows of an odd K begin at any 2-byte address).  What is behind the row reads as zero: its last
-// value is loaded in its place, so that the 16 loads are under way together (rows of 14155 x 1751 with each loaded by itself: 19 us, @).
-__device__ __forceinline__ QuantChunk qfloat_chunk(const bf16_t* p, int left) {
+// 16 values of a row of K from `at` on (rows of an odd K begin at any 2-byte address), in two steps: loads without a branch, which are all under way together,
+// then what lies behind the row's end made zero.  Near it the row's last 16 values are loaded, of a shorter row the last one again and again for those in front of
+// it, and moved down.  (With branches around the loads: 14155 x 1760 of rms norm 20 us, so
+// 18.5.)
+__device__ __forceinline__ QuantChunk qfloat_fetch(const bf16_t* row, int at, int K) {
   QuantChunk c;
-  if (left >= 16) {
-    __builtin_memcpy(c.w, p, 32);
+  if (K >= 16) {
+    __builtin_memcpy(c.w, row + min(at, K - 16), 32);
   } else {
-    uint32_t v[16];
 #pragma unroll
-    for (int q = 0; q < 16; ++q) v[q] = p[min(q, left - 1)];
-#pragma unroll
-    for (int q = 0; q < 16; ++q) v[q] = q < left ? v[q] : 0;
-#pragma unroll
-    for (int q = 0; q < 8; ++q) c.w[q] = v[2 * q] | v[2 * q + 1] << 16;
+    for (int q = 0; q < 8; ++q) c.w[q] = row[max(K - 16 + 2 * q, 0)] | (uint32_t)row[max(K - 15 + 2 * q, 0)] << 16;
   }
   return c;
+}
+__device__ __forceinline__ void qfloat_settle(QuantChunk& c, int left) {   // left: values from `at` to the row's end
+  if (left >= 16) return;
+  const int by = 16 - max(left, 0);
+#pragma unroll
+  for (int q = 0; q < 8; ++q) c.w[q] = by & 1 ? c.w[q] >> 16 | (q < 7 ? c.w[(q + 1) & 7] << 16 : 0) : c.w[q];
+#pragma unroll
+  for (int d = 1; d <= 8; d <<= 1)
+#pragma unroll
+    for (int q = 0; q < 8; ++q) c.w[q] = by & 2 * d ? (q + d < 8 ? c.w[(q + d) & 7] : 0) : c.w[q];
 }
 // The largest of n values.  Numbers alone are compared where some lane has others, which is seldom: as integers those are above all numbers.
 template <int N>

@@ -49,9 +49,12 @@ __global__ __launch_bounds__(256) void chunks_kernel(QfloatRowsArgs p) {
 #pragma unroll
       for (int g = 0; g < 4; ++g) hid[u][g] = live && at < p.K ? *reinterpret_cast<const f32x4_t*>(p.h + first + at + 4 * g) : f32x4_t{};   // (d_ff: multiples of 64)
     } else {
-      raw[u] = live && at < p.K ? qfloat_chunk(p.x + first + at, p.K - at) : QuantChunk{};
+      raw[u] = qfloat_fetch(p.x + first, at, p.K);
     }
   }
+  if constexpr (!HIDDEN)
+#pragma unroll
+    for (int u = 0; u < BLOCKS; ++u) qfloat_settle(raw[u], p.K - (kb0 + u) * 128 - c * 16);
   auto value = [&](int u, int q) __attribute__((always_inline)) {
     if constexpr (HIDDEN) return hid[u][q >> 2][q & 3];
     else return quant_element(raw[u], q);
@@ -76,32 +79,47 @@ __global__ __launch_bounds__(256) void chunks_kernel(QfloatRowsArgs p) {
 }
 
 // ---- rows behind a norm ---------------------------------------------------------------------------------------------
-// LPR neighbouring lanes have a row (256: the workgroup), CPT chunks of 16 values each (0: as many as there are, read again for each use).
+// LPR neighbouring lanes have a row (256: the workgroup), CPT chunks of 16 values each (0: as many as there are, read again for each use).  A row's chunks lie 512
+// bytes apart in the form, so the workgroup's rows are collected in LDS and stored together: 4 neighbouring rows are 64 bytes.  Few chunks a lane, so that many
+// wavefronts hide the loads: us with rms norm, of 16384 rows unless other
+//   K             512   1024   2048   2048 of 2048   4096   8192
+//   <32, 2>       8.3   12.1
+//   <64, 2>      12.5   12.5   19.8   5.8
+//   <32, 4>       8.7   12.4   21.0   7.2                          (<16, 8>: 9.0, 13.5, 24.4, 10.2)
+//   <64, 4>                                          35.3          (<32, 8>: 40.3)
+//   <64, 8>                                                 83     (103 without LDS)
+// A large copy moves what K 4096 reads and writes in 33 us.
 template <int LPR, int CPT>
 __global__ __launch_bounds__(256) void rows_kernel(QfloatRowsArgs p) {
-  __shared__ float red[4];
   constexpr int ROWS = 256 / LPR, HELD = CPT ? CPT : 1;
+  __shared__ float red[4];
+  __shared__ int places[ROWS];
+  __shared__ __attribute__((aligned(16))) u32x4_t out[256 * HELD];
   const int l = threadIdx.x % LPR, lane = threadIdx.x & 63;
   const int row = blockIdx.x * ROWS + threadIdx.x / LPR;
   const int chunks = (p.K + 127) / 128 * 8, nkb = chunks / 8;
   const bool live = row < p.groups.T;
   const bf16_t* const x = p.x + (int64_t)(live ? row : 0) * p.K;
-  auto fetch = [&](int t) __attribute__((always_inline)) {
-    const int c = t * LPR + l;
-    return live && c * 16 < p.K ? qfloat_chunk(x + c * 16, p.K - c * 16) : QuantChunk{};
+  auto fetch = [&](int t) __attribute__((always_inline)) { return qfloat_fetch(x, (t * LPR + l) * 16, p.K); };
+  auto settle = [&](int t, QuantChunk c) __attribute__((always_inline)) {
+    qfloat_settle(c, p.K - (t * LPR + l) * 16);
+    return c;
   };
   QuantChunk raw[HELD] = {};
   if constexpr (CPT > 0) {
 #pragma unroll
     for (int t = 0; t < CPT; ++t)
       if (t * LPR < chunks) raw[t] = fetch(t);
+#pragma unroll
+    for (int t = 0; t < CPT; ++t)
+      if (t * LPR < chunks) raw[t] = settle(t, raw[t]);
   }
   int place = live ? row : -1;
   if (p.groups.offsets) place = qfloat_place<(LPR < 64 ? LPR : 64)>(p.groups, row, lane);
   // (values are made of the packed ones at each use: held as floats they would cost half of the wavefronts)
   auto chunk = [&](int t) __attribute__((always_inline)) {
     if constexpr (CPT > 0) return raw[t];
-    else return fetch(t);
+    else return settle(t, fetch(t));
   };
   auto each_chunk = [&](auto f) __attribute__((always_inline)) {
     if constexpr (CPT > 0) {
@@ -135,12 +153,19 @@ __global__ __launch_bounds__(256) void rows_kernel(QfloatRowsArgs p) {
   };
   if (p.norm.kind == STEM_NORM_LAYER) mean = total(false);
   if (p.norm.kind != STEM_NORM_NONE) r = 1.0f / sqrtf(total(true) + p.norm.eps);
-  uint8_t* const out = p.q + (int64_t)(place >> 5) * 32 * chunks * 16 + (place & 31) * 16;
+  auto to = [&](int at, int c) __attribute__((always_inline)) {
+    return reinterpret_cast<u32x4_t*>(p.q + (int64_t)(at >> 5) * 32 * chunks * 16 + (at & 31) * 16 + (int64_t)(c >> 1) * 1024 + (c & 1) * 512);
+  };
+  // chunk c of the workgroup's row `of` until all are there (rotated: lanes that write a row's chunks, or read a chunk's rows, are on different banks)
+  auto kept = [&](int of, int c) __attribute__((always_inline)) -> u32x4_t& { return out[c * ROWS + ((of + c) & (ROWS - 1))]; };
   each_chunk([&](int t) __attribute__((always_inline)) {
     const int c = t * LPR + l, in = p.K - c * 16;
     const QuantChunk x = chunk(t);
     QuantChunk g = {};
-    if (p.norm.weight && in > 0) g = qfloat_chunk(static_cast<const bf16_t*>(p.norm.weight) + c * 16, in);
+    if (p.norm.weight) {
+      g = qfloat_fetch(static_cast<const bf16_t*>(p.norm.weight), c * 16, p.K);
+      qfloat_settle(g, in);
+    }
     float u[16];
 #pragma unroll
     for (int q = 0; q < 16; ++q) u[q] = quant_element(x, q);
@@ -159,10 +184,19 @@ __global__ __launch_bounds__(256) void rows_kernel(QfloatRowsArgs p) {
     uint32_t w[4];
 #pragma unroll
     for (int q = 0; q < 4; ++q) w[q] = qfloat_four(u[4 * q], u[4 * q + 1], u[4 * q + 2], u[4 * q + 3], s);
-    if (c >= chunks || place < 0) return;
-    *reinterpret_cast<u32x4_t*>(out + (int64_t)(c >> 1) * 1024 + (c & 1) * 512) = u32x4_t{w[0], w[1], w[2], w[3]};
-    if ((c & 7) == 0) p.scale[qfloat_scale_at(place, c >> 3, nkb)] = (uint8_t)s.byte;
+    if (c >= chunks) return;
+    const u32x4_t four = {w[0], w[1], w[2], w[3]};
+    if (CPT > 0) kept(threadIdx.x / LPR, c) = four;
+    else if (place >= 0) *to(place, c) = four;
+    if ((c & 7) == 0 && place >= 0) p.scale[qfloat_scale_at(place, c >> 3, nkb)] = (uint8_t)s.byte;
   });
+  if constexpr (CPT > 0) {
+    if (l == 0) places[threadIdx.x / LPR] = place;
+    __syncthreads();
+    const int of = threadIdx.x % ROWS, at = places[of];
+    if (at < 0) return;
+    for (int c = threadIdx.x / ROWS; c < chunks; c += LPR) *to(at, c) = kept(of, c);
+  }
 }
 
 // ---- tiles of 128 x 128 -----------------------------------------------------------------------------------------------------------
@@ -172,9 +206,10 @@ __global__ __launch_bounds__(256) void rows_kernel(QfloatRowsArgs p) {
 __device__ __forceinline__ void load_tile(const bf16_t* x, int cols, int rows, int quad, int col, QuantChunk (&raw)[4]) {
 #pragma unroll
   for (int r = 0; r < 4; ++r) {
-    const int in = quad * 4 + r;
-    raw[r] = in < rows && col < cols ? qfloat_chunk(x + (int64_t)in * cols + col, cols - col) : QuantChunk{};
+    raw[r] = qfloat_fetch(x + (int64_t)min(quad * 4 + r, rows - 1) * cols, col, cols);
   }
+#pragma unroll
+  for (int r = 0; r < 4; ++r) qfloat_settle(raw[r], quad * 4 + r < rows ? cols - col : 0);
 }
 // a lane's four rows of a form whose rows have nkb blocks
 __device__ __forceinline__ void store_rows(uint8_t* q, uint8_t* scale, int nkb, int row0, int kb, int c, const float (&v)[4][16], const QfloatScale (&s)[4]) {
@@ -290,8 +325,9 @@ hipError_t stem_qfloat_rows_launch(stem_ctx* ctx, const QfloatRowsArgs& a, hipSt
     const unsigned grid = (unsigned)((rows + 31) / 32 * ((nkb + BLOCKS - 1) / BLOCKS));
     if (a.h) chunks_kernel<true><<<grid, 256, 0, s>>>(a);
     else chunks_kernel<false><<<grid, 256, 0, s>>>(a);
-  } else if (a.K <= 2048) rows >= 2048 ? launch_rows<32, 4>(a, s) : launch_rows<64, 2>(a, s);
-  else if (a.K <= 4096) rows >= 2048 ? launch_rows<32, 8>(a, s) : launch_rows<256, 1>(a, s);
+  } else if (a.K <= 1024 && rows >= 8192) launch_rows<32, 2>(a, s);
+  else if (a.K <= 2048) launch_rows<64, 2>(a, s);
+  else if (a.K <= 4096) rows >= 2048 ? launch_rows<64, 4>(a, s) : launch_rows<256, 1>(a, s);
   else if (a.K <= 8192) rows >= 1024 ? launch_rows<64, 8>(a, s) : launch_rows<256, 2>(a, s);
   else launch_rows<256, 0>(a, s);
   return hipGetLastError();

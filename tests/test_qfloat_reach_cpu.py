@@ -58,7 +58,7 @@ def test_gates_of_few_rows():
 def test_weight_gradient():
     T, N, K = G.WEIGHT_SLICES
     assert tiles(N, K, -(-T // 64) * 128, F32) == (128, 128, 5)
-    for (T, N, K, groups), want in zip(G.WEIGHTS, [(128, 128, 16), (128, 128, 3), (128, 256, 1), (128, 256, 1)]):
+    for (T, N, K, groups), want in zip(G.WEIGHTS, [(128, 128, 8), (128, 128, 3), (128, 256, 1), (128, 256, 1)]):
         assert tiles(N, K, -(-T // groups // 64) * 128, F32, groups) == want
 
 
