@@ -800,8 +800,14 @@ extern "C" void stem_route_qfloat(int64_t T, int groups, int N, int K, int out, 
   if (out == QFLOAT_F32) {
     // T: rows of the output, all of it for each group; K: of an average group
     const int64_t n = tiles_of(T, 128, 128) * groups;
-    if (n > 256) cols = 256;
-    else slices = (int)std::min<int64_t>({MAX_WEIGHT_SLICES, nk / 8, 256 / n});
+    if (n > 256) {
+      // us: tiles of 128 x 128 one a compute unit, in rounds of 256; of 128 x 256 two, whose last round's alone are faster (4096 x 2001 x 2100 58 us and 47,
+      // 5178 x 2816 x 256 in 6 groups 23 and 35, 2978 x 848 x 7070 in 2 62 and 48, 9000 x 1999 x 1501 in 3 68 and 79)
+      const int64_t pairs = tiles_of(T, 128, 256) * groups, last = pairs % 512;
+      const double few = (double)((n + 255) / 256) * (0.4 * nk + 4);
+      const double two = (double)(pairs / 512) * (1.25 * nk + 16) + (last == 0 ? 0 : last <= 256 ? 0.68 * nk + 11 : 1.25 * nk + 16);
+      if (two < few) cols = 256;
+    } else slices = (int)std::min<int64_t>({MAX_WEIGHT_SLICES, nk / 8, 256 / n});
   } else if (out == QFLOAT_BF16 && cols == 64 && groups == 1) {
     slices = nk < 32 ? 1 : (int)std::min<int64_t>({MAX_SLICES, nk / 10, 240 / tiles(rows, cols)});
   }

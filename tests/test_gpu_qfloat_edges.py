@@ -20,7 +20,7 @@ FEW = {"8 channels": (3, 1000, 1000), "16 channels": (5, 3001, 2000), "32 channe
        "form, 32 rows": (50, 5000, 2000), "form, 32 rows, 16 channels": (250, 1030, 1100)}
 GATES = {"64x128": (100, 128, 320), "128x128": (1500, 192, 1600), "pair": (4400, 128, 2240), "few, inline": (8, 256, 1024), "few, by a kernel": (8, 128, 4160)}
 WEIGHT_SLICES = (3000, 300, 200)
-WEIGHTS = [(9001, 100, 129, 1), (5000, 130, 260, 3), (300, 2100, 2300, 1), (700, 1200, 1301, 3)]   # T, N, K, groups
+WEIGHTS = [(9001, 100, 129, 1), (5000, 130, 260, 3), (3200, 2100, 2300, 1), (900, 1000, 3899, 4)]   # T, N, K, groups
 
 
 def check_rows(ctx, T, N, K, rows):
