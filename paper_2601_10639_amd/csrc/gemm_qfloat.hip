@@ -779,9 +779,11 @@ hipError_t launch(const QfloatGemmArgs& a, hipStream_t s) {
 
 // ---- choice of the tile and of the K slices ----------------------------------------------------------------------------------------
 extern "C" void stem_route_qfloat(int64_t T, int groups, int N, int K, int out, int64_t ws_bytes, int32_t* route) {
-  const int64_t per_group = (T + groups - 1) / groups;       // of an average group, which is all that is known here
+  const int64_t per_group = (T + groups - 1) / groups;       // of an average group, which is all that is known here: uneven ones have more tiles that are not full
   auto tiles_of = [&](int64_t rows, int tm, int tn) { return (rows + tm - 1) / tm * ((N + tn - 1) / tn); };
-  auto tiles = [&](int tm, int tn) { return tiles_of(per_group, tm, tn) * groups; };
+  auto tiles = [&](int tm, int tn) {
+    return std::max((per_group + tm - 1) / tm * groups, groups > 1 ? (T + tm * (int64_t)groups / 2) / tm : 0) * ((N + tn - 1) / tn);
+  };
   const int nk = K / 128;
   int rows = 128, cols = 128, slices = 1;
   if (out == QFLOAT_HIDDEN) {
