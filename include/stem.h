@@ -333,9 +333,8 @@ stem_status stem_quant_ffn_forward(stem_ctx* ctx, const void* x, const int32_t* 
 /* ---- products and the layer in 8-bit floating point, for training and serving, by groups of rows (bf16 contexts) ------ */
 
 /* Q(v) of a block of 128 values: e is the least integer with max |v| <= 448 2^e (at least -126), and Q the values of 8-bit floating point (e4m3, to
- * nearest even) of v 2^-e, times 2^e.  Blocks are 128 values in a row of activations and gradients, counted from the row's first (or, where a product runs over
- * the rows, 128 rows of a column, counted from the first row of the group) and 128 x 128 of a matrix of weights, whose Q is therefore the same
- * whichever way it is read.  Sums are in fp32 and rounded once.  A NaN or an infinity makes NaN of what depends on it and of nothing else;
+ * nearest even) of v 2^-e, times 2^e.  Blocks are 128 values in a row of activations and gradients, counted from the row's first, and 128 x 128 of a matrix
+ * of weights, whose Q is therefore the same whichever way it is read.  Sums are in fp32 and rounded once.  A NaN or an infinity makes NaN of what depends on it and of nothing else;
  * the blocks' largest magnitude is that of their finite values.
  *
  * Groups.  Weights are groups matrices (1 to 512), one behind another, and rows offsets[g] .. offsets[g + 1] of the activations meet the g-th: offsets

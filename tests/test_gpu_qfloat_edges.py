@@ -299,3 +299,59 @@ def test_streams():
             L.stem_qfloat_linear(b, x, w, y2)
     torch.cuda.synchronize()
     assert torch.equal(y1, want) and torch.equal(y2, want)
+
+
+def test_two_graphs_of_one_context():
+    """Products in slices, whose room and counters both graphs share, replayed in turn with eager calls between."""
+    T, N, K = WEIGHT_SLICES
+    ctx = make_ctx(T, 64, 4160, backward=True)
+    dy, x, w = draw(1, T, N), draw(2, T, K), L.stem_qfloat_weights(ctx, draw(3, N, K, std=0.05), backward=True)
+    dx, dW = torch.zeros(T, K, dtype=bf, device=DEV), torch.zeros(N, K, device=DEV)
+    T2, N2, K2 = TILES["2 slices"]
+    x2, w2, res = draw(4, T2, K2), L.stem_qfloat_weights(ctx, draw(5, N2, K2, std=0.05)), draw(6, T2, N2)
+    y2 = torch.zeros(T2, N2, dtype=bf, device=DEV)
+    calls = [lambda: L.stem_qfloat_linear_backward(ctx, dy, x, w, dx, dW), lambda: L.stem_qfloat_linear(ctx, x2, w2, y2, residual=res)]
+    side, graphs = torch.cuda.Stream(), []
+    for call in calls:
+        with torch.cuda.stream(side):
+            call()
+        side.synchronize()
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[-1], stream=side):
+            call()
+    for seed in range(3):
+        dy.copy_(draw(50 + seed, T, N))
+        x2.copy_(draw(60 + seed, T2, K2))
+        for call in calls:
+            call()
+        want = dx.clone(), dW.clone(), y2.clone()
+        for _ in range(2):
+            for t in (dx, dW, y2):
+                t.zero_()
+            for g in graphs:
+                g.replay()
+            torch.cuda.synchronize()
+            assert all(torch.equal(a, b) for a, b in zip((dx, dW, y2), want))
+
+
+@pytest.mark.parametrize("T,N", [(5, 333), (300, 1001), (3000, 1503), (4090, 4090)])
+def test_input_residual_and_output_are_one(T, N):
+    ctx = make_ctx(T, 64, wide(N))
+    x, w, y = draw(1, T, N), L.stem_qfloat_weights(ctx, draw(2, N, N, std=0.05)), torch.empty(T, N, dtype=bf, device=DEV)
+    L.stem_qfloat_linear(ctx, x, w, y, residual=x)
+    L.stem_qfloat_linear(ctx, x, w, x, residual=x)
+    assert torch.equal(x, y)
+
+
+@pytest.mark.parametrize("T", [1, 7])
+def test_few_tokens_of_a_wide_layer(T):
+    """Rows too long to be made to operands in place: the gate product's tiles, then few rows of their form."""
+    check_ffn(make_ctx(T, 8256, 128), T, 8256, 128)
+
+
+@pytest.mark.parametrize("T,K", [(9000, 700), (9000, 1024), (2500, 2999), (2500, 4096), (1500, 5001), (130, 8000), (40, 9001)])
+def test_rows_behind_a_norm(T, K):
+    """Each number of lanes a row, chunk and row tails, by groups too."""
+    ctx = make_ctx(T, 64, wide(K), groups=3)
+    check_linear(ctx, T, 40, K, norm_kind=L.STEM_NORM_RMS)
+    check_linear(ctx, T, 40, K, 3, offsets_of(T, T, 3), norm_kind=L.STEM_NORM_LAYER)
