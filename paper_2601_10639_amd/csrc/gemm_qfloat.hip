@@ -324,7 +324,8 @@ __device__ __forceinline__ void load_ids(const QfloatGemmArgs& p, int m0, int ro
 
 // ---- 256 x 256 ----------------------------------------------------------------------------------------------------------------
 // 4 wavefronts of 4 x 4 accumulators, a ring of five 32 KB slots of one operand tile each: the loop of the 8-bit integer products (gemm_int8.hip), whose
-// instruction takes as long for the same bytes.
+// instruction takes as long for the same bytes.  16384 x 8192 -> 2048: 206 to 220 us, 2.5 to 2.67 10^15 a second, matrix units busy 78 % of the clocks: the chip's
+// power sets the rate.
 constexpr int SLOT = 32768;
 
 __global__ __launch_bounds__(256) void ring_kernel(QfloatGemmArgs p) {
@@ -448,6 +449,8 @@ __global__ __launch_bounds__(256) void ring_kernel(QfloatGemmArgs p) {
 // ---- 128 x 256, two workgroups a compute unit -----------------------------------------------------------------------------------------
 // 4 wavefronts of 2 x 4 accumulators, K tiles of 64 in a ring of three 24 KB slots: one workgroup's first loads and epilogue, which the gate product has a long
 // one of, run beside the other's products.  A K tile is one k-step: its fragments are read while the one before is multiplied, and its slot is free then.
+// The gate product of 16384 tokens of 2048 x 8192: 244 to 253 us (2.2 10^15 a second, matrix units busy 65 % of the clocks);
+// 8192 rows of 1024 x 4096 in 16 uneven groups 50 to 56.
 constexpr int PAIR_A = 8192, PAIR_SLOT = 24576;
 
 template <QfloatOut OUT>
@@ -778,6 +781,20 @@ hipError_t launch(const QfloatGemmArgs& a, hipStream_t s) {
 }  // namespace
 
 // ---- choice of the tile and of the K slices ----------------------------------------------------------------------------------------
+// The largest tile that leaves no compute unit idle: operand bytes go down with it, and the time with the number of rounds.  us of a product alone, rows x K -> N:
+//                              128 x 64   128 x 128   128 x 256   256 x 256
+//   1024 x 2048 -> 2048           8.6        10.2
+//   512 x 8192 -> 2048           18.7        23.1
+//   8192 x 1024 -> 640                       14.1        10.6        16.4
+//   8192 x 4096 -> 1100                      48.9        45.4        42.8
+//   8192 x 8192 -> 640                       53.1        44.4        69.1
+//   4096 x 4096 -> 4096                      72.0        55.8        51.8
+//   2000 x 1024 -> 1024, 16 groups 11.5       7.5        10.3
+// and of the gate product, whose tiles have whole blocks of 128 channels, 64 x 128 / 128 x 128 / 128 x 256: 64 x 2048 -> 8192 9.6 / 10.9, 1024 x 1024 -> 4096
+// 16.3 / 11.2, 8192 x 1024 -> 640 - / 16.8 / 13.2, 2048 x 2048 -> 3200 - / 24.9 / 19.4.
+// K slices fill what few tiles leave idle, where K is long: 700 x 8192 -> 200 whole 17.8, in 2, 3, 4 14.2, 11.7, 11.2; 1500 x 4096 -> 600 with its rows 20.8 and 20.0; 512 x
+// 8192 -> 2048 whole 18.7, in 2 16.8, but 1024 x 4096 -> 1024, also of 128 tiles, 11.4 and 11.9; 700 x 1999 -> 1001 7.5 and 9.1.  Weight gradients, us whole, in 4, 8, 16
+// slices: 14460 rows of 114 x 211 65, 24, 19, 20; 3344 of 327 x 74 18.5, 13.3, 12.7, 12.9; 8000 of 700 x 900 43, 22.5.
 extern "C" void stem_route_qfloat(int64_t T, int groups, int N, int K, int out, int64_t ws_bytes, int32_t* route) {
   const int64_t per_group = (T + groups - 1) / groups;       // of an average group, which is all that is known here: uneven ones have more tiles that are not full
   auto tiles_of = [&](int64_t rows, int tm, int tn) { return (rows + tm - 1) / tm * ((N + tn - 1) / tn); };
@@ -811,7 +828,7 @@ extern "C" void stem_route_qfloat(int64_t T, int groups, int N, int K, int out, 
       if (two < few) cols = 256;
     } else slices = (int)std::min<int64_t>({MAX_WEIGHT_SLICES, nk / 8, 256 / n});
   } else if (out == QFLOAT_BF16 && cols == 64 && groups == 1) {
-    slices = nk < 32 ? 1 : (int)std::min<int64_t>({MAX_SLICES, nk / 10, 240 / tiles(rows, cols)});
+    slices = nk < 32 ? 1 : (int)std::min<int64_t>({MAX_SLICES, nk / 10, (nk < 64 ? 240 : 256) / tiles(rows, cols)});
   }
   while (slices > 1 && slices * rows * cols * 4 * (out == QFLOAT_F32 ? tiles_of(T, 128, 128) * groups : tiles(rows, cols)) > ws_bytes) --slices;
   while (slices > 1 && (nk + slices - 1) / slices * (slices - 1) >= nk) --slices;   // every slice has a part of K
