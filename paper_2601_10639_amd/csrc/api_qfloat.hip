@@ -8,10 +8,11 @@ namespace {
 
 constexpr stem_norm no_norm = {STEM_NORM_NONE, 0.f, nullptr};
 constexpr int64_t MAX_CHANNELS = 1 << 22;
-// The layer of up to 8 rows: its gate product leaves fp32 hidden values, of which every workgroup of the down product makes its operands where they are few, else a
-// kernel between the two.  More rows: tiles of the gate product leave 8 bits.  us, the whole layer, hidden values inline / by a kernel: 2048 x 8192, 1, 4, 8 rows
-// 13.5 / 17.4, 16.7 / 18.1, 20.1 / 18.1; 1024 x 4096 8.4 / 11.8 at one row, 11.5 / 12.3 at 8, 16.6 / 14.3 at 16.
-constexpr int64_t GATE_ROWS = 8, HIDDEN_INLINE = 32768;
+// The layer of up to 16 rows, 8 by groups: its gate product leaves fp32 hidden values, of which every workgroup of the down product makes its operands where they are few,
+// else a kernel between the two.  More rows: tiles of the gate product leave 8 bits.  us, the whole layer, hidden values inline / by a kernel: 2048 x 8192, 1, 4, 8 rows
+// 13.5 / 17.4, 16.7 / 18.1, 20.1 / 18.1; 1024 x 4096 8.4 / 11.8 at one row, 11.5 / 12.3 at 8, 16.6 / 14.3 at 16.  In a graph of 16 layers, by tiles / by fp32 hidden values:
+// 512 x 1536 9 rows 13.3 / 10.7, 16 rows 13.4 / 11.6; 1024 x 4096 15.4 / 14.4 and 15.5 / 14.7; 2048 x 8192 24.0 / 22.7 and 24.2 / 23.4.
+constexpr int64_t GATE_ROWS = 16, GATE_ROWS_GROUPS = 8, HIDDEN_INLINE = 32768;
 constexpr int64_t MAX_FORM = INT32_MAX;   // elements of a form, which kernels address with 32 bits
 
 int64_t widest(const stem_ctx* c) { return std::max(c->desc.d_model, c->desc.d_ff); }
@@ -242,7 +243,7 @@ stem_status stem_qfloat_ffn_forward(stem_ctx* c, const void* x, const int32_t* i
   QfloatDecodeArgs b = decode_args(form(down_q, d, F), stem_qfloat_form(d, F), d, F, g);
   b.y = static_cast<bf16_t*>(y); b.residual = static_cast<const bf16_t*>(residual);
   b.A = h.q; b.sa = h.scale; b.a_bytes = h.bytes;
-  if (T <= GATE_ROWS && stem_qfloat_decode_inline(T, d) && T * F * 4 <= QFLOAT_WS) {
+  if (T <= (offsets ? GATE_ROWS_GROUPS : GATE_ROWS) && stem_qfloat_decode_inline(T, d) && T * F * 4 <= QFLOAT_WS) {
     QfloatDecodeArgs a = decode_args(form(gate_q, F, d), stem_qfloat_form(F, d), F, d, g);
     a.h_out = c->qfloat_ws;
     a.ids = ids; a.E = static_cast<const bf16_t*>(E); a.E_rows = (int)E_rows; a.flag = c->flag;

@@ -306,7 +306,7 @@ hipError_t stem_qfloat_decode_launch(stem_ctx* ctx, int kid, const QfloatDecodeA
   a.share = a.groups.T > 4 ? 1 : a.groups.T > 2 ? 2 : a.groups.T > 1 ? 4 : 8;
   int32_t route[3];
   stem_route_qfloat_decode(a.groups.T, a.groups.offsets ? a.groups.n : 1, a.N, a.K, !a.x && !a.h, route);
-  if (a.h_out) by_channels<1, ROWS, true>(a, route, s);        // (a gate product of up to 8 rows)
+  if (a.h_out) by_channels<1, ROWS, true>(a, route, s);        // (a gate product)
   else if (a.x) by_channels<1, ROWS, false>(a, route, s);
   else if (a.h) by_channels<1, HIDDEN, false>(a, route, s);
   else if (route[1] == 1) by_channels<1, FORM, false>(a, route, s);

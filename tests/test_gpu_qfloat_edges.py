@@ -18,7 +18,8 @@ TILES = {"ring": (4090, 4090, 4100), "pair": (3000, 1500, 300), "128x128": (2000
 FEW = {"8 channels": (3, 1000, 1000), "16 channels": (5, 3001, 2000), "32 channels": (16, 5000, 4096), "depth 8": (2, 200, 8192), "turns": (2, 130, 9000),
        "form, depth 1": (17, 1001, 999), "form, depth 2": (40, 333, 1999), "form, depth 4": (100, 500, 4000), "form, depth 8": (33, 300, 8192), "form, turns": (33, 300, 17000),
        "form, 32 rows": (50, 5000, 2000), "form, 32 rows, 16 channels": (250, 1030, 1100)}
-GATES = {"64x128": (100, 128, 320), "128x128": (1500, 192, 1600), "pair": (4400, 128, 2240), "few, inline": (8, 256, 1024), "few, by a kernel": (8, 128, 4160)}
+GATES = {"64x128": (100, 128, 320), "128x128": (1500, 192, 1600), "pair": (4400, 128, 2240), "few, inline": (8, 256, 1024), "few, by a kernel": (8, 128, 4160),
+         "16, by a kernel": (16, 192, 2112)}
 WEIGHT_SLICES = (3000, 300, 200)
 WEIGHTS = [(9001, 100, 129, 1), (5000, 130, 260, 3), (3200, 2100, 2300, 1), (900, 1000, 3899, 4)]   # T, N, K, groups
 

@@ -46,13 +46,13 @@ def test_few_rows(name, form, want):
 @pytest.mark.parametrize("name,want", [("64x128", (64, 128)), ("128x128", (128, 128)), ("pair", (128, 256))])
 def test_gates(name, want):
     T, d, F = G.GATES[name]
-    assert tiles(T, F, d, HIDDEN)[:2] == want and T > 8
+    assert tiles(T, F, d, HIDDEN)[:2] == want and T > 16
 
 
 def test_gates_of_few_rows():
-    for name, inline in (("few, inline", True), ("few, by a kernel", False)):
+    for name, inline in (("few, inline", True), ("few, by a kernel", False), ("16, by a kernel", False)):
         T, d, F = G.GATES[name]
-        assert T <= 8 and (T * F <= 32768) == inline
+        assert T <= 16 and (T * F <= 32768) == inline
 
 
 def test_weight_gradient():
