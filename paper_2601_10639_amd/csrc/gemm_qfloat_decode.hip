@@ -69,11 +69,12 @@ __global__ __launch_bounds__(WAVES * 64, SRC == FORM && KPW <= 2 ? 4 : 2) void d
   const bool mine = wave < CB * NT && out_row < rows && c * 4 < CH && left > 0;
   const int64_t to = (int64_t)(tile.row + out_row) * p.N + out_n;
   uint16_t meet[4] = {};
+  int id = 0;
+  if (GATE && mine) id = p.ids[tile.row + out_row];            // (first of all: what waits for a load waits for those in front of it)
   auto meeting = [&]() __attribute__((always_inline)) {
     if (!mine) return;
     const bf16_t* from = nullptr;
     if (GATE) {
-      int id = p.ids[tile.row + out_row];
       if ((unsigned)id >= (unsigned)p.E_rows) {   // reported to the host, clamped so no access leaves the table
         *p.flag = 1;
         id = id < 0 ? 0 : p.E_rows - 1;
@@ -96,21 +97,21 @@ __global__ __launch_bounds__(WAVES * 64, SRC == FORM && KPW <= 2 ? 4 : 2) void d
     // 16 values of a row, eight neighbouring lanes a block; zeros behind the row's end (quant_load_chunk's branch is the shorter code: with qfloat_fetch the layer of
     // 2048 x 8192 takes 13.5 us on one token, so 12.7)
     float v[16];
-    auto load = [&](int row, int chunk) __attribute__((always_inline)) {
+    QuantChunk raw;
+    f32x4_t hid[4];
+    auto request = [&](int row, int chunk) __attribute__((always_inline)) {
       const int k = chunk * 16;
       const int64_t at = (int64_t)(tile.row + row) * p.row_K + k;
       if constexpr (SRC == ROWS) {
-        const QuantChunk x = k < p.row_K ? quant_load_chunk(p.x + at, p.row_K - k) : QuantChunk{};
-#pragma unroll
-        for (int q = 0; q < 16; ++q) v[q] = quant_element(x, q);
+        raw = k < p.row_K ? quant_load_chunk(p.x + at, p.row_K - k) : QuantChunk{};
       } else {
 #pragma unroll
-        for (int h = 0; h < 4; ++h) {                          // (d_ff is a multiple of 64)
-          const f32x4_t x = k < p.row_K ? *reinterpret_cast<const f32x4_t*>(p.h + at + h * 4) : f32x4_t{};
-#pragma unroll
-          for (int q = 0; q < 4; ++q) v[4 * h + q] = x[q];
-        }
+        for (int h = 0; h < 4; ++h) hid[h] = k < p.row_K ? *reinterpret_cast<const f32x4_t*>(p.h + at + h * 4) : f32x4_t{};   // (d_ff is a multiple of 64)
       }
+    };
+    auto unpack = [&]() __attribute__((always_inline)) {
+#pragma unroll
+      for (int q = 0; q < 16; ++q) v[q] = SRC == ROWS ? quant_element(raw, q) : hid[q >> 2][q & 3];
     };
     auto keep = [&](int row, int chunk) __attribute__((always_inline)) {
       const QfloatScale s = qfloat_scale(max_of_eight(qfloat_top(v)));
@@ -126,13 +127,22 @@ __global__ __launch_bounds__(WAVES * 64, SRC == FORM && KPW <= 2 ? 4 : 2) void d
       // 8, 4, 2 wavefronts a row or one.  In loops: values that are read again from the nearest cache cost less than the instructions that would hold them, whose
       // first fetch is what short kernels wait for (one row of K 2048 with all chunks held and unrolled: 10.2 us against 9.5).
       const int share = p.share, turns = (rows * share + WAVES - 1) / WAVES, first = wave % share * 64 + lane;
+      const bool once = turns == 1 && p.K <= 1024 * share;     // a lane has one chunk: it is loaded in front of the weights, and once (2048 -> 8192, one row of
+                                                               // rms norm 5.5 us, so 5.0; the layer of 1536 x 5120 11.5 and 10.8)
+      QuantChunk weight = {};
+      if (once) {
+        request(wave / share < rows ? wave / share : 0, first);
+        if (p.norm.weight && first * 16 < p.row_K) weight = quant_load_chunk(static_cast<const bf16_t*>(p.norm.weight) + first * 16, p.row_K - first * 16);
+        weights(0);
+      }
       for (int turn = 0; turn < turns; ++turn) {
         const int at = turn * (WAVES / share) + wave / share, row = at < rows ? at : 0;
         float mean = 0.f, scale = 1.f;
         auto total = [&](bool squares) __attribute__((always_inline)) {
           float s = 0.f;
           for (int chunk = first; chunk * 16 < p.row_K; chunk += 64 * share) {
-            load(row, chunk);
+            if (!once) request(row, chunk);
+            unpack();
             const int in = p.row_K - chunk * 16;
 #pragma unroll
             for (int q = 0; q < 16; ++q) {
@@ -153,17 +163,21 @@ __global__ __launch_bounds__(WAVES * 64, SRC == FORM && KPW <= 2 ? 4 : 2) void d
         };
         if (p.norm.kind == STEM_NORM_LAYER) mean = total(false);
         if (p.norm.kind != STEM_NORM_NONE) scale = 1.0f / sqrtf(total(true) + p.norm.eps);
-        if (turn == 0) { weights(0); meeting(); }              // (behind the rows, which are waited for first)
+        if (turn == 0) {                                       // (behind the rows, which are waited for first)
+          if (!once) weights(0);
+          meeting();
+        }
         for (int chunk = first; chunk - lane < nkb * 8; chunk += 64 * share) {
-          load(row, chunk);
+          if (!once) request(row, chunk);
+          unpack();
           const int in = p.row_K - chunk * 16;
-          const QuantChunk g = p.norm.weight && in > 0 ? quant_load_chunk(static_cast<const bf16_t*>(p.norm.weight) + chunk * 16, in) : QuantChunk{};
+          if (!once && p.norm.weight && in > 0) weight = quant_load_chunk(static_cast<const bf16_t*>(p.norm.weight) + chunk * 16, in);
 #pragma unroll
           for (int q = 0; q < 16; ++q) {
             float x = v[q];
             if (p.norm.kind == STEM_NORM_LAYER) x -= mean;
             x *= scale;
-            if (p.norm.weight) x *= quant_element(g, q);
+            if (p.norm.weight) x *= quant_element(weight, q);
             v[q] = q < in ? x : 0.f;
           }
           keep(row, at < rows ? chunk : nkb * 8);
@@ -175,7 +189,8 @@ __global__ __launch_bounds__(WAVES * 64, SRC == FORM && KPW <= 2 ? 4 : 2) void d
       const int per = nkb * 8, all = rows * per;
       for (int i = threadIdx.x; i - (int)threadIdx.x < all; i += WAVES * 64) {
         const int row = min(i / per, rows - 1), chunk = i - row * per;   // (beyond the last row: chunks of it that are not kept)
-        load(row, chunk);
+        request(row, chunk);
+        unpack();
         keep(row, chunk);
       }
     }
