@@ -6,7 +6,7 @@
 // k alike; the bf16 instruction: 1e-8).  Rounded to bf16, or to 8 bits again, an output does not know it.  An fp32 weight gradient would, whose sums go on over
 // steps; so that product is made of the bf16 values themselves, exact products and fp32 sums, and nothing of it is quantised.
 //
-// Numbers.  A block of 128 values v (1 x 128 of a row or a column, 128 x 128 of a matrix of weights) has a scale 2^e, e the least integer with max |v| <=
+// Numbers.  A block of 128 values v (1 x 128 of a row, 128 x 128 of a matrix of weights) has a scale 2^e, e the least integer with max |v| <=
 // 448 2^e, at least -126, and the e4m3 values rne(v 2^-e).  v_mfma_scale_f32_32x32x64_f8f6f4 takes such exponents, a byte e + 127 for each row and
 // 32 k, and multiplies by them itself: a product of blocks needs no arithmetic but the matrix units', and sums stay in their fp32 accumulators
 // over all of K.  (A power of two costs a floating point format nothing but up to one of its 15 binades above the subnormal numbers; a scale that is
