@@ -4,7 +4,8 @@ that have weights of their own, and what brings tokens to such groups (experts) 
   linear    y = residual + Q(N(x)) Q(W_g)^T.  Q: blocks of 128 values of a row of x, of 128 x 128 of a matrix; with e the least integer for which the block's
             largest magnitude is at most 448 2^e (and at least -126), the values are those of 8-bit floating point (e4m3, round to nearest even) times 2^e.
             Rows offsets[g] .. offsets[g + 1] meet matrix g; rows behind the last group are left as they were.
-  grad      its backward pass: dx = Q(dy) Q(W_g), blocks of 128 along the row of dy; dW_g = dy^T x over the rows of a group, of the values as they are.
+  grad      its backward pass: dx = Q(dy) Q(W_g), blocks of 128 along the row of dy; dW_g = Q'(dy)^T Q'(x) over the rows of a group, Q' in blocks of 128 rows of
+            the group, column by column.
   ffn       the layer: y = x + Q(SiLU(Q(N(x)) Q(W_gate)^T) * E[ids]) Q(W_down)^T, by groups too.
   dispatch  (token, choice) pairs sorted by expert, stable; src: the pair of each row, place: the row of each pair, -1 where it has no expert; rows of x and the
             token ids in that order.
@@ -265,7 +266,7 @@ def _plain(s):
         dx = _by_groups(_rows(s["dy"]), s["qW"].transpose(1, 2), s["bounds"]).to(dt)
         dW = torch.empty(c["groups"], c["N"], c["K"], device=DEV, dtype=F32)
         for g, (lo, hi) in enumerate(zip(s["bounds"], s["bounds"][1:])):
-            dW[g] = s["dy"][lo:hi].float().t() @ s["x"][lo:hi].float() if hi > lo else 0.0
+            dW[g] = _rows(s["dy"][lo:hi].t()) @ _rows(s["x"][lo:hi].t()).t() if hi > lo else 0.0
         return dx, dW
     if op == "ffn":
         x = s["x"].float()
@@ -310,7 +311,7 @@ def _own(s):
         L.stem_qfloat_linear(s["ctx"], s["x"], s["pW"], s["y"], residual=s["res"], norm=s["norm"], offsets=s["offsets"])
         return s["y"]
     if op == "grad":
-        L.stem_qfloat_linear_backward(s["ctx"], s["dy"], s["x"], s["pW"], s["dx"], s["dW"], offsets=s["offsets"])
+        L.stem_qfloat_linear_backward_quantised(s["ctx"], s["dy"], s["x"], s["pW"], s["dx"], s["dW"], offsets=s["offsets"])
         return s["dx"], s["dW"]
     if op == "ffn":
         L.stem_qfloat_ffn_forward(s["ctx"], s["x"], s["ids"], s["pWg"], s["pWd"], s["E"], s["y"], residual=s["x"], norm=s["norm"], offsets=s["offsets"])
@@ -423,7 +424,7 @@ def exact(case, seed):
         for g in range(c["groups"]):
             lo, hi = s["bounds"][g], s["bounds"][g + 1]
             if hi > lo:
-                dW[g] = torch.mm(s["dy"][lo:hi].double().t().contiguous(), s["x"][lo:hi].double())
+                dW[g] = torch.mm(_q64(s["dy"][lo:hi].double(), 0).t().contiguous(), _q64(s["x"][lo:hi].double(), 0))
         return dx, dW
     if op == "ffn":
         x = s["x"].double()
