@@ -363,6 +363,10 @@ stem_status stem_qfloat_linear(stem_ctx* ctx, const void* x, int64_t T, int64_t 
  * zero (or left as it is). */
 stem_status stem_qfloat_linear_backward(stem_ctx* ctx, const void* dy, const void* x, int64_t T, int64_t K, const void* qt, int64_t N, int groups,
                                         const int32_t* offsets, void* dx, float* dW, int accumulate, void* stream);
+/* The same, but dW = Q'(dy)^T Q'(x): Q' in blocks of 128 rows of a group, counted from its first, column by column; the 8-bit values' products are exact, but that a
+ * magnitude which rounds up to 2^128 is an infinity, and their sums fp32. */
+stem_status stem_qfloat_linear_backward_quantised(stem_ctx* ctx, const void* dy, const void* x, int64_t T, int64_t K, const void* qt, int64_t N, int groups,
+                                                  const int32_t* offsets, void* dx, float* dW, int accumulate, void* stream);
 
 /* The layer: y = Q(SiLU(Q(N(x)) Q(W_gate)^T) * E[ids]) Q(W_down)^T (+ residual), W_gate and W_down those of the row's group; ids and the bf16 table (one for all
  * groups) as in stem_ffn_forward.  The hidden values are quantised as the gate product leaves them, not rounded before.  norm and residual may be NULL; y may be x and

@@ -88,6 +88,17 @@ def linear_backward(dy, x, W, offsets=None):
     return (dx, sx), (dW, sW)
 
 
+def weight_gradient_quantised(dy, x, groups, offsets=None):
+    """Q'(dy)^T Q'(x) over each group's rows, Q' in blocks of 128 of them, column by column; and its products' magnitudes."""
+    shape = (groups, dy.shape[1], x.shape[1])
+    dW, size = np.zeros(shape), np.zeros(shape)
+    for g, (lo, hi) in enumerate(bounds(offsets, x.shape[0], groups)):
+        if hi > lo:
+            a, b = blocks(dy[lo:hi], 0), blocks(x[lo:hi], 0)
+            dW[g], size[g] = a.T @ b, np.abs(a).T @ np.abs(b)
+    return dW, size
+
+
 def hidden(n, ids, Wg, E, offsets=None):
     z, _ = linear(n, Wg, offsets)
     with np.errstate(over="ignore"):

@@ -77,6 +77,63 @@ hipError_t decode_rows(stem_ctx* c, const void* x, int64_t K, const stem_norm* n
   return rows_form(c, x, a.groups, K, norm, f, s);
 }
 
+// Both forms of the gradients.  rounded: dW is of values in 8 bits
+stem_status linear_backward(stem_ctx* c, const char* who, bool rounded, const void* dy, const void* x, int64_t T, int64_t K, const void* qt, int64_t N,
+                            int groups, const int32_t* offsets, void* dx, float* dW, int accumulate, void* stream) {
+  STEM_TRY(stem_enter(c, T));
+  STEM_TRY(check_context(c, who, groups, true));
+  if (N < 1 || N > widest(c) || K < 1 || K > widest(c))
+    return stem_fail(c, STEM_ERR_SHAPE, "%s: gradients of [%lld, %lld] x [%lld, %lld]^T; K and N are up to %lld here", who, (long long)T, (long long)K,
+                     (long long)N, (long long)K, (long long)widest(c));
+  const int64_t rows = stem_qfloat_rows(T, groups);
+  STEM_TRY(check_form(c, who, rows * 2, std::max(N, K)));   // (dy and x are transposed in bf16)
+  STEM_TRY(check_form(c, who, N, K));
+  const size_t xb = (size_t)T * K * 2, yb = (size_t)T * N * 2, wb = (size_t)groups * N * K * 4;
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  if (T == 0) {
+    STEM_TRY(check_buffers(c, who, {}, {{dW, wb}}, false));
+    if (dW && !accumulate) HIP_TRY(c, stem_fill_zero(dW, wb, s));
+    return STEM_OK;
+  }
+  if (!dy || (dx && !qt) || (dW && !x)) return stem_fail(c, STEM_ERR_INVALID_ARG, "%s: null pointer argument", who);
+  if (!dx && !dW) return STEM_OK;
+  STEM_TRY(check_groups(c, who, offsets, groups));
+  const Buffer in_x = {dW ? x : nullptr, xb}, in_q = {dx ? qt : nullptr, (size_t)groups * stem_qfloat_form(K, N)};
+  STEM_TRY(check_buffers(c, who, {{dy, yb}, in_x, in_q}, {{dW, wb}}, false));
+  STEM_TRY(check_buffers(c, who, {in_q}, {{dx, xb}, {dW, wb}}, false));
+  STEM_TRY(check_apart(c, who, {{offsets, (size_t)(groups + 1) * 4}}, {{dx, xb}, {dW, wb}}));
+  const QfloatGroups g = {offsets, groups, (int)T};
+  const Form f = form(c->qfloat_x, rows, N);
+  const auto *g_in = static_cast<const bf16_t*>(dy), *x_in = static_cast<const bf16_t*>(x);
+  // Whole matrices of aligned rows are read as they lie; others are transposed first (of dy, together with its 8-bit form)
+  const bool as_stored = !rounded && groups == 1 && !offsets && N % 64 == 0 && K % 64 == 0 && wb <= INT32_MAX;
+  if (dW && !as_stored) {
+    HIP_TRY(c, stem_qfloat_turn_launch(c, {g_in, g, (int)N, c->qfloat_dyt, (int)rows * 2, dx ? f.q : nullptr, f.scale},
+                                       {x_in, g, (int)K, c->qfloat_xt, (int)rows * 2, nullptr, nullptr}, rounded, s));
+  } else if (dx) {
+    HIP_TRY(c, rows_form(c, dy, g, N, nullptr, f, s));
+  }
+  if (dW && as_stored) {
+    GemmArgs a = {};
+    a.A = g_in; a.lda = (int)N;
+    a.B = x_in; a.ldb = (int)K;
+    a.M = (int)N; a.N = (int)K; a.K = (int)T;
+    a.C = dW; a.accumulate = accumulate;
+    a.ws = c->splitk_ws; a.ws_bytes = c->splitk_bytes; a.tickets = c->tickets;
+    HIP_TRY(c, stem_gemm_bf16(c, K_QFLOAT_DW, OP_MC, OP_MC, EPI_F32, a, s));
+  } else if (dW) {
+    QfloatGemmArgs a = gemm_args(c, {c->qfloat_dyt, nullptr, stem_qfloat_pitch(N) * rows * 2}, {c->qfloat_xt, nullptr, 0}, 0, N, K, rows * 2, g);
+    a.c = dW; a.accumulate = accumulate;
+    HIP_TRY(c, stem_qfloat_gemm_launch(c, K_QFLOAT_DW, QFLOAT_F32, a, s));
+  }
+  if (dx) {
+    QfloatGemmArgs a = gemm_args(c, f, form(qt, K, N), stem_qfloat_form(K, N), T, K, N, g);
+    a.y = static_cast<bf16_t*>(dx);
+    HIP_TRY(c, stem_qfloat_gemm_launch(c, K_QFLOAT_DX, QFLOAT_BF16, a, s));
+  }
+  return STEM_OK;
+}
+
 }  // namespace
 
 extern "C" {
@@ -161,59 +218,12 @@ stem_status stem_qfloat_linear(stem_ctx* c, const void* x, int64_t T, int64_t K,
 
 stem_status stem_qfloat_linear_backward(stem_ctx* c, const void* dy, const void* x, int64_t T, int64_t K, const void* qt, int64_t N, int groups,
                                         const int32_t* offsets, void* dx, float* dW, int accumulate, void* stream) {
-  static const char who[] = "stem_qfloat_linear_backward";
-  STEM_TRY(stem_enter(c, T));
-  STEM_TRY(check_context(c, who, groups, true));
-  if (N < 1 || N > widest(c) || K < 1 || K > widest(c))
-    return stem_fail(c, STEM_ERR_SHAPE, "%s: gradients of [%lld, %lld] x [%lld, %lld]^T; K and N are up to %lld here", who, (long long)T, (long long)K,
-                     (long long)N, (long long)K, (long long)widest(c));
-  const int64_t rows = stem_qfloat_rows(T, groups);
-  STEM_TRY(check_form(c, who, rows * 2, std::max(N, K)));   // (dy and x are transposed in bf16)
-  STEM_TRY(check_form(c, who, N, K));
-  const size_t xb = (size_t)T * K * 2, yb = (size_t)T * N * 2, wb = (size_t)groups * N * K * 4;
-  hipStream_t s = static_cast<hipStream_t>(stream);
-  if (T == 0) {
-    STEM_TRY(check_buffers(c, who, {}, {{dW, wb}}, false));
-    if (dW && !accumulate) HIP_TRY(c, stem_fill_zero(dW, wb, s));
-    return STEM_OK;
-  }
-  if (!dy || (dx && !qt) || (dW && !x)) return stem_fail(c, STEM_ERR_INVALID_ARG, "%s: null pointer argument", who);
-  if (!dx && !dW) return STEM_OK;
-  STEM_TRY(check_groups(c, who, offsets, groups));
-  const Buffer in_x = {dW ? x : nullptr, xb}, in_q = {dx ? qt : nullptr, (size_t)groups * stem_qfloat_form(K, N)};
-  STEM_TRY(check_buffers(c, who, {{dy, yb}, in_x, in_q}, {{dW, wb}}, false));
-  STEM_TRY(check_buffers(c, who, {in_q}, {{dx, xb}, {dW, wb}}, false));
-  STEM_TRY(check_apart(c, who, {{offsets, (size_t)(groups + 1) * 4}}, {{dx, xb}, {dW, wb}}));
-  const QfloatGroups g = {offsets, groups, (int)T};
-  const Form f = form(c->qfloat_x, rows, N);
-  const auto *g_in = static_cast<const bf16_t*>(dy), *x_in = static_cast<const bf16_t*>(x);
-  // Whole matrices of aligned rows are read as they lie; others are transposed first (of dy, together with its 8-bit form)
-  const bool as_stored = groups == 1 && !offsets && N % 64 == 0 && K % 64 == 0 && wb <= INT32_MAX;
-  if (dW && !as_stored) {
-    HIP_TRY(c, stem_qfloat_turn_launch(c, {g_in, g, (int)N, c->qfloat_dyt, (int)rows * 2, dx ? f.q : nullptr, f.scale},
-                                       {x_in, g, (int)K, c->qfloat_xt, (int)rows * 2, nullptr, nullptr}, s));
-  } else if (dx) {
-    HIP_TRY(c, rows_form(c, dy, g, N, nullptr, f, s));
-  }
-  if (dW && as_stored) {
-    GemmArgs a = {};
-    a.A = g_in; a.lda = (int)N;
-    a.B = x_in; a.ldb = (int)K;
-    a.M = (int)N; a.N = (int)K; a.K = (int)T;
-    a.C = dW; a.accumulate = accumulate;
-    a.ws = c->splitk_ws; a.ws_bytes = c->splitk_bytes; a.tickets = c->tickets;
-    HIP_TRY(c, stem_gemm_bf16(c, K_QFLOAT_DW, OP_MC, OP_MC, EPI_F32, a, s));
-  } else if (dW) {
-    QfloatGemmArgs a = gemm_args(c, {c->qfloat_dyt, nullptr, stem_qfloat_pitch(N) * rows * 2}, {c->qfloat_xt, nullptr, 0}, 0, N, K, rows * 2, g);
-    a.c = dW; a.accumulate = accumulate;
-    HIP_TRY(c, stem_qfloat_gemm_launch(c, K_QFLOAT_DW, QFLOAT_F32, a, s));
-  }
-  if (dx) {
-    QfloatGemmArgs a = gemm_args(c, f, form(qt, K, N), stem_qfloat_form(K, N), T, K, N, g);
-    a.y = static_cast<bf16_t*>(dx);
-    HIP_TRY(c, stem_qfloat_gemm_launch(c, K_QFLOAT_DX, QFLOAT_BF16, a, s));
-  }
-  return STEM_OK;
+  return linear_backward(c, "stem_qfloat_linear_backward", false, dy, x, T, K, qt, N, groups, offsets, dx, dW, accumulate, stream);
+}
+
+stem_status stem_qfloat_linear_backward_quantised(stem_ctx* c, const void* dy, const void* x, int64_t T, int64_t K, const void* qt, int64_t N, int groups,
+                                                  const int32_t* offsets, void* dx, float* dW, int accumulate, void* stream) {
+  return linear_backward(c, "stem_qfloat_linear_backward_quantised", true, dy, x, T, K, qt, N, groups, offsets, dx, dW, accumulate, stream);
 }
 
 stem_status stem_qfloat_ffn_forward(stem_ctx* c, const void* x, const int32_t* ids, int64_t T, const stem_norm* norm, const void* gate_q,

@@ -369,14 +369,19 @@ PyObject* qfloat_linear(PyObject*, PyObject* const* args, Py_ssize_t n) {
   });
 }
 
-PyObject* qfloat_linear_backward(PyObject*, PyObject* const* args, Py_ssize_t n) {
-  return enter(args, n, 8, [](const Args& a, stem_ctx* c) {
+template <class F>
+PyObject* qfloat_backward(PyObject* const* args, Py_ssize_t n, F of) {
+  return enter(args, n, 8, [of](const Args& a, stem_ctx* c) {
     const int64_t T = a.rows(-1, 0);
     const Args::Qfloat w = a.qfloat(2);
     auto dy = a.shaped(0, ACT, T, w.N); auto x = a.shaped(1, ACT, T, w.K); auto dx = a.shaped(3, ACT, T, w.K);
     auto dW = a.cube(4, w.groups, w.N, w.K); auto o = a.shaped<int32_t>(5, I32, w.groups + 1); const int accumulate = a.flag(6); auto s = a.stream(7);
-    return [=] { return stem_qfloat_linear_backward(c, dy, x, T, w.K, w.qt, w.N, (int)w.groups, o, dx, dW, accumulate, s); };
+    return [=] { return of(c, dy, x, T, w.K, w.qt, w.N, (int)w.groups, o, dx, dW, accumulate, s); };
   });
+}
+PyObject* qfloat_linear_backward(PyObject*, PyObject* const* args, Py_ssize_t n) { return qfloat_backward(args, n, stem_qfloat_linear_backward); }
+PyObject* qfloat_linear_backward_quantised(PyObject*, PyObject* const* args, Py_ssize_t n) {
+  return qfloat_backward(args, n, stem_qfloat_linear_backward_quantised);
 }
 
 PyObject* qfloat_ffn_forward(PyObject*, PyObject* const* args, Py_ssize_t n) {
@@ -466,7 +471,7 @@ PyObject* off(PyObject*, PyObject*) {
 PyMethodDef methods[] = {FAST(ffn_forward), FAST(ffn_forward_residual), FAST(ffn_backward), FAST(ffn_up_forward), FAST(ffn_up_backward),
                          FAST(embed_grad), FAST(embed_grad_presorted), FAST(embed_sparse_adamw),
                          FAST(block_enter_forward), FAST(block_enter_backward), FAST(block_leave_forward), FAST(block_leave_backward), FAST(dropout),
-                         FAST(quant_linear), FAST(quant_ffn_forward), FAST(qfloat_linear), FAST(qfloat_linear_backward), FAST(qfloat_ffn_forward),
+                         FAST(quant_linear), FAST(quant_ffn_forward), FAST(qfloat_linear), FAST(qfloat_linear_backward), FAST(qfloat_linear_backward_quantised), FAST(qfloat_ffn_forward),
                          FAST(experts_sort), FAST(experts_dispatch), FAST(experts_combine), FAST(experts_combine_backward),
                          {"setup", setup, METH_VARARGS, nullptr}, {"off", off, METH_NOARGS, nullptr}, {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_bind", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};

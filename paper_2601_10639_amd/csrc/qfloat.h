@@ -3,8 +3,10 @@
 //
 // Sums.  The matrix instruction of this format adds eight products at a time, cut (towards zero) 13 binary digits below the largest of their exponents'
 // sums, and adds the result to its fp32 accumulator: measured, for normal values, 1.5e-5 of the result's norm whatever its length (instructions of 16, 64 and 128
-// k alike; the bf16 instruction: 1e-8).  Rounded to bf16, or to 8 bits again, an output does not know it.  An fp32 weight gradient would, whose sums go on over
-// steps; so that product is made of the bf16 values themselves, exact products and fp32 sums, and nothing of it is quantised.
+// k alike; the bf16 instruction: 1e-8).  Rounded to bf16, or to 8 bits again, an output hardly knows it.  An fp32 weight gradient would; so its products are the
+// bf16 instruction's, exact and summed in fp32.  It comes in two forms.  Of the bf16 values as they are: what is added up over steps keeps what 8 bits would lose, 3.8e-2 of
+// the norm of a gradient of normal values.  And of values rounded to 8 bits in blocks of 128 rows of the group, column by column: four significant bits, which bf16
+// has without rounding them again (but those that round up to 2^128, which are infinities there).
 //
 // Numbers.  A block of 128 values v (1 x 128 of a row, 128 x 128 of a matrix of weights) has a scale 2^e, e the least integer with max |v| <=
 // 448 2^e, at least -126, and the e4m3 values rne(v 2^-e).  v_mfma_scale_f32_32x32x64_f8f6f4 takes such exponents, a byte e + 127 for each row and
@@ -58,7 +60,7 @@ hipError_t stem_qfloat_weights_launch(stem_ctx* ctx, const QfloatTilesArgs& a, h
 
 // The transpose of x [T, cols] in bf16, as a weight gradient's product reads it: blocks of 32 columns x 16 rows, 1 KB, chunk h of column c, rows 8 h .., at
 // (32 h + c) * 16, one behind another along the rows; each group's rows begin at a multiple of 128 and are followed by zeros up to the next multiple of 64
-// at least.  And the form of x besides.
+// at least.  `rounded`: the values are Q's of blocks of 128 rows of the group, column by column.  And the form of x (of its values as they are) besides.
 struct QfloatTurnArgs {
   const bf16_t* x;
   QfloatGroups groups;
@@ -67,7 +69,7 @@ struct QfloatTurnArgs {
   int pitch;                // bytes of a row of it
   uint8_t *q, *scale;       // may be null
 };
-hipError_t stem_qfloat_turn_launch(stem_ctx* ctx, const QfloatTurnArgs& a, const QfloatTurnArgs& b, hipStream_t s);   // two of the same rows
+hipError_t stem_qfloat_turn_launch(stem_ctx* ctx, const QfloatTurnArgs& a, const QfloatTurnArgs& b, bool rounded, hipStream_t s);   // two of the same rows
 
 enum QfloatOut { QFLOAT_BF16 = 0, QFLOAT_F32, QFLOAT_HIDDEN };
 struct QfloatGemmArgs {
@@ -176,6 +178,14 @@ __device__ __forceinline__ uint32_t qfloat_four(float a, float b, float c, float
   w = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(w, a, b, s.scale, false);
   w = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(w, c, d, s.scale, true);
   return __builtin_bit_cast(uint32_t, w);
+}
+
+// and back: values 2 PAIR and 2 PAIR + 1 of four, times the scale, as two bf16 values
+template <int PAIR>
+__device__ __forceinline__ uint32_t qfloat_two_of(uint32_t four, const QfloatScale& s) {
+  typedef __attribute__((ext_vector_type(2))) float two_t;
+  const two_t v = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(four, s.scale, PAIR == 1);
+  return __builtin_amdgcn_perm(__float_as_uint(v[1]), __float_as_uint(v[0]), 0x07060302);
 }
 
 // ---- groups: every lane of a wavefront takes part -------------------------------------------------------------------------

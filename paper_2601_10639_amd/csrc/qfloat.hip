@@ -272,9 +272,44 @@ __global__ __launch_bounds__(256) void weights_kernel(QfloatTilesArgs p) {
   }
 }
 
+// The largest magnitude of each of a lane's 16 columns over the tile's 128 rows, numbers alone, as bits of bf16, two columns a word
+typedef __attribute__((ext_vector_type(2))) uint16_t u16x2_t;
+__device__ __forceinline__ void column_tops(const QuantChunk (&raw)[4], uint32_t (&top)[8], u32x4_t (&red)[4][8][2]) {
+  auto larger = [](uint32_t a, uint32_t b) __attribute__((always_inline)) {
+    return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(u16x2_t, a), __builtin_bit_cast(u16x2_t, b)));
+  };
+  auto number = [](uint32_t v) __attribute__((always_inline)) {
+    return ((v & 0x7fffu) < 0x7f80u ? v & 0x7fffu : 0u) | ((v & 0x7fff0000u) < 0x7f800000u ? v & 0x7fff0000u : 0u);
+  };
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = threadIdx.x & 7;
+#pragma unroll
+  for (int w = 0; w < 8; ++w) {
+    top[w] = 0;
+#pragma unroll
+    for (int r = 0; r < 4; ++r) top[w] = larger(top[w], number(raw[r].w[w]));
+#pragma unroll
+    for (int d = 8; d < 64; d <<= 1) top[w] = larger(top[w], (uint32_t)__shfl_xor((int)top[w], d));
+  }
+  if (lane < 8) {
+    red[wave][c][0] = u32x4_t{top[0], top[1], top[2], top[3]};
+    red[wave][c][1] = u32x4_t{top[4], top[5], top[6], top[7]};
+  }
+  __syncthreads();
+#pragma unroll
+  for (int v = 0; v < 4; ++v)
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const u32x4_t other = red[v][c][h];
+#pragma unroll
+      for (int q = 0; q < 4; ++q) top[4 * h + q] = larger(top[4 * h + q], other[q]);
+    }
+}
+
+template <bool ROUNDED>
 __global__ __launch_bounds__(256) void turn_kernel(QfloatTurnArgs first, QfloatTurnArgs second, int blocks) {
   constexpr int PITCH = 68;
   __shared__ __attribute__((aligned(16))) uint32_t words[128 * PITCH + 128];
+  __shared__ __attribute__((aligned(16))) u32x4_t red[ROUNDED ? 4 : 1][8][2];
   const int t = threadIdx.x, lane = t & 63, wave = t >> 6, quad = t >> 3, c = t & 7;
   const QfloatTurnArgs& p = (int)blockIdx.x < blocks ? first : second;
   const int b = (int)blockIdx.x < blocks ? blockIdx.x : blockIdx.x - blocks;
@@ -283,10 +318,23 @@ __global__ __launch_bounds__(256) void turn_kernel(QfloatTurnArgs first, QfloatT
   if (!qfloat_tile<128>(p.groups, tr, lane, tile)) return;
   QuantChunk raw[4];
   load_tile(p.x + (int64_t)tile.row * p.cols, p.cols, tile.rows, quad, tc * 128 + c * 16, raw);
+  uint32_t top[8];
+  if constexpr (ROUNDED) column_tops(raw, top, red);
 #pragma unroll
   for (int w = 0; w < 8; ++w) {                             // two columns at a time
     const int at = c * 16 + 2 * w;
     uint32_t* const to = words + at * PITCH + c * 16 + quad * 2;
+    if constexpr (ROUNDED) {
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const QfloatScale s = qfloat_scale(h ? top[w] & 0xffff0000u : top[w] << 16);
+        const uint32_t four = qfloat_four(quant_element(raw[0], 2 * w + h), quant_element(raw[1], 2 * w + h), quant_element(raw[2], 2 * w + h),
+                                          quant_element(raw[3], 2 * w + h), s);
+        to[h * PITCH] = qfloat_two_of<0>(four, s);
+        to[h * PITCH + 1] = qfloat_two_of<1>(four, s);
+      }
+      continue;
+    }
     to[0] = __builtin_amdgcn_perm(raw[1].w[w], raw[0].w[w], 0x05040100);
     to[1] = __builtin_amdgcn_perm(raw[3].w[w], raw[2].w[w], 0x05040100);
     to[PITCH] = __builtin_amdgcn_perm(raw[1].w[w], raw[0].w[w], 0x07060302);
@@ -342,9 +390,10 @@ hipError_t stem_qfloat_weights_launch(stem_ctx* ctx, const QfloatTilesArgs& a, h
   return hipGetLastError();
 }
 
-hipError_t stem_qfloat_turn_launch(stem_ctx* ctx, const QfloatTurnArgs& a, const QfloatTurnArgs& b, hipStream_t s) {
+hipError_t stem_qfloat_turn_launch(stem_ctx* ctx, const QfloatTurnArgs& a, const QfloatTurnArgs& b, bool rounded, hipStream_t s) {
   ProfScope prof(ctx, K_QFLOAT_TURN, s);
   const int64_t rows = stem_qfloat_rows(a.groups.T, a.groups.n) / 128, first = rows * ((a.cols + 127) / 128), second = rows * ((b.cols + 127) / 128);
-  turn_kernel<<<(unsigned)(first + second), 256, 0, s>>>(a, b, (int)first);
+  if (rounded) turn_kernel<true><<<(unsigned)(first + second), 256, 0, s>>>(a, b, (int)first);
+  else turn_kernel<false><<<(unsigned)(first + second), 256, 0, s>>>(a, b, (int)first);
   return hipGetLastError();
 }

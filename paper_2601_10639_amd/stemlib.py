@@ -29,7 +29,8 @@ SYMBOLS = [
     "stem_embed_grad", "stem_embed_grad_presorted", "stem_embed_grad_noalloc", "stem_embed_sparse_adamw",
     "stem_block_enter_forward", "stem_block_enter_backward", "stem_block_leave_forward", "stem_block_leave_backward", "stem_dropout",
     "stem_quant_bytes", "stem_quant_weights", "stem_quant_linear", "stem_quant_ffn_forward",
-    "stem_qfloat_reserve", "stem_qfloat_bytes", "stem_qfloat_weights", "stem_qfloat_linear", "stem_qfloat_linear_backward", "stem_qfloat_ffn_forward",
+    "stem_qfloat_reserve", "stem_qfloat_bytes", "stem_qfloat_weights", "stem_qfloat_linear", "stem_qfloat_linear_backward", "stem_qfloat_linear_backward_quantised",
+    "stem_qfloat_ffn_forward",
     "stem_experts_sort", "stem_experts_dispatch", "stem_experts_combine", "stem_experts_combine_backward",
     "stem_prefetch_rows", "stem_cache_init", "stem_prefetch_rows_cached", "stem_cache_state",
     "stem_edit_rows", "stem_profile_enable", "stem_profile_kernels", "stem_profile_read",
@@ -210,8 +211,9 @@ def lib() -> ctypes.CDLL:
         L.stem_qfloat_weights.restype = i32
         L.stem_qfloat_linear.argtypes = [vp, vp, i64, i64, norm, vp, i64, i32, vp, vp, vp, vp]
         L.stem_qfloat_linear.restype = i32
-        L.stem_qfloat_linear_backward.argtypes = [vp, vp, vp, i64, i64, vp, i64, i32, vp, vp, vp, i32, vp]
-        L.stem_qfloat_linear_backward.restype = i32
+        for f in (L.stem_qfloat_linear_backward, L.stem_qfloat_linear_backward_quantised):
+            f.argtypes = [vp, vp, vp, i64, i64, vp, i64, i32, vp, vp, vp, i32, vp]
+            f.restype = i32
         L.stem_qfloat_ffn_forward.argtypes = [vp, vp, vp, i64, norm, vp, vp, i32, vp, vp, i64, vp, vp, vp]
         L.stem_qfloat_ffn_forward.restype = i32
         L.stem_experts_sort.argtypes = [vp, vp, i64, i32, i32, vp, vp, vp, vp]
@@ -756,19 +758,29 @@ def stem_qfloat_linear(ctx: StemCtx, x, W: StemQfloat, y, residual=None, norm: s
         _check(ctx, st, "stem_qfloat_linear")
 
 
-def stem_qfloat_linear_backward(ctx: StemCtx, dy, x, W: StemQfloat, dx=None, dW=None, offsets=None, accumulate: bool = False, stream=None):
-    """dx = Q(dy) W_g; dW [groups, N, K] (or [N, K] of one) fp32 = dy^T x over each group's rows.  Either may be None, x without dW."""
-    st = (_bind or _load_bind()).qfloat_linear_backward(ctx, dy, x, W, dx, dW, offsets, accumulate, stream)
+def _qfloat_backward(name: str, native, ctx: StemCtx, dy, x, W: StemQfloat, dx, dW, offsets, accumulate: bool, stream):
+    st = native(ctx, dy, x, W, dx, dW, offsets, accumulate, stream)
     if st is None:   # not the ordinary call
         dt, T = ctx.torch_dtype, dy.shape[0]
         _, qt = _qfloat(W, W.N, W.K, "W")
         if dW is not None and W.groups == 1 and dW.dim() == 2:
             dW = dW.unsqueeze(0)
-        st = lib().stem_qfloat_linear_backward(ctx.handle, _shaped(dy, dt, (T, W.N), "dy"), _shaped(x, dt, (T, W.K), "x"), T, W.K, qt, W.N, W.groups,
-                                               _offsets(offsets, W.groups), _shaped(dx, dt, (T, W.K), "dx"),
-                                               _shaped(dW, torch.float32, (W.groups, W.N, W.K), "dW"), 1 if accumulate else 0, _stream(stream))
+        st = getattr(lib(), name)(ctx.handle, _shaped(dy, dt, (T, W.N), "dy"), _shaped(x, dt, (T, W.K), "x"), T, W.K, qt, W.N, W.groups,
+                                  _offsets(offsets, W.groups), _shaped(dx, dt, (T, W.K), "dx"),
+                                  _shaped(dW, torch.float32, (W.groups, W.N, W.K), "dW"), 1 if accumulate else 0, _stream(stream))
     if st != STEM_OK:
-        _check(ctx, st, "stem_qfloat_linear_backward")
+        _check(ctx, st, name)
+
+
+def stem_qfloat_linear_backward(ctx: StemCtx, dy, x, W: StemQfloat, dx=None, dW=None, offsets=None, accumulate: bool = False, stream=None):
+    """dx = Q(dy) W_g; dW [groups, N, K] (or [N, K] of one) fp32 = dy^T x over each group's rows.  Either may be None, x without dW."""
+    _qfloat_backward("stem_qfloat_linear_backward", (_bind or _load_bind()).qfloat_linear_backward, ctx, dy, x, W, dx, dW, offsets, accumulate, stream)
+
+
+def stem_qfloat_linear_backward_quantised(ctx: StemCtx, dy, x, W: StemQfloat, dx=None, dW=None, offsets=None, accumulate: bool = False, stream=None):
+    """The same with dW = Q'(dy)^T Q'(x), Q' in blocks of 128 rows of a group, column by column."""
+    _qfloat_backward("stem_qfloat_linear_backward_quantised", (_bind or _load_bind()).qfloat_linear_backward_quantised, ctx, dy, x, W, dx, dW, offsets,
+                     accumulate, stream)
 
 
 def stem_qfloat_ffn_forward(ctx: StemCtx, x, ids, gate: StemQfloat, down: StemQfloat, E, y, residual=None, norm: stem_norm | None = None, offsets=None,
