@@ -138,6 +138,27 @@ stem_status linear_backward(stem_ctx* c, const char* who, bool rounded, const vo
 
 extern "C" {
 
+// All buffers that are still to be had, or none: one that was left of a call that failed would have that call's size, for a later one of more groups.
+int stem_qfloat_room_take(stem_qfloat_room* r, int64_t tokens, int64_t wide, int64_t F, int groups, int backward, int (*take)(void**, int64_t), void (*give)(void*)) {
+  const int most = r->groups ? r->groups : groups;
+  const int64_t rows = stem_qfloat_rows(std::max<int64_t>(tokens, 1), most), turned = stem_qfloat_size(wide, rows) * 2;
+  const int64_t bytes[5] = {stem_qfloat_form(rows, wide), stem_qfloat_form(rows, F), QFLOAT_WS, turned, turned};
+  void* got[5] = {};
+  for (int i = 0; i < (backward ? 5 : 3); ++i) {
+    if (r->p[i]) continue;
+    const int failed = take(&got[i], bytes[i]);
+    if (!failed) continue;
+    while (i--)
+      if (got[i]) give(got[i]);
+    return failed;
+  }
+  for (int i = 0; i < 5; ++i)
+    if (got[i]) r->p[i] = got[i];
+  r->groups = most;
+  if (backward) r->backward = 1;
+  return 0;
+}
+
 int64_t stem_qfloat_bytes(int64_t N, int64_t K) { return N < 1 || K < 1 ? 0 : stem_qfloat_form(N, K); }
 
 stem_status stem_qfloat_reserve(stem_ctx* c, int groups, int backward) {
@@ -148,18 +169,17 @@ stem_status stem_qfloat_reserve(stem_ctx* c, int groups, int backward) {
   if (c->qfloat_groups && groups > c->qfloat_groups)
     return stem_fail(c, STEM_ERR_INVALID_ARG, "%s: reserved for %d groups before; the first call names the most", who, c->qfloat_groups);
   HIP_TRY(c, hipSetDevice(c->device));
-  const int most = c->qfloat_groups ? c->qfloat_groups : groups;
-  const int64_t T = std::max<int64_t>(c->max_tokens, 1), rows = stem_qfloat_rows(T, most), F = c->desc.d_ff, wide = widest(c);
-  auto need = [&](uint8_t** p, int64_t bytes) { return *p ? hipSuccess : hipMalloc(reinterpret_cast<void**>(p), (size_t)bytes); };
-  HIP_TRY(c, need(&c->qfloat_x, stem_qfloat_form(rows, wide)));
-  HIP_TRY(c, need(&c->qfloat_h, stem_qfloat_form(rows, F)));
-  if (!c->qfloat_ws) HIP_TRY(c, hipMalloc(reinterpret_cast<void**>(&c->qfloat_ws), QFLOAT_WS));
-  c->qfloat_groups = most;
-  if (backward) {
-    HIP_TRY(c, need(&c->qfloat_dyt, stem_qfloat_size(wide, rows) * 2));
-    HIP_TRY(c, need(&c->qfloat_xt, stem_qfloat_size(wide, rows) * 2));
-    c->qfloat_backward = 1;
-  }
+  stem_qfloat_room room = {c->qfloat_groups, c->qfloat_backward, {c->qfloat_x, c->qfloat_h, c->qfloat_ws, c->qfloat_dyt, c->qfloat_xt}};
+  HIP_TRY(c, static_cast<hipError_t>(stem_qfloat_room_take(
+                 &room, c->max_tokens, widest(c), c->desc.d_ff, groups, backward, [](void** p, int64_t bytes) { return (int)hipMalloc(p, (size_t)bytes); },
+                 [](void* p) { (void)hipFree(p); })));
+  c->qfloat_x = static_cast<uint8_t*>(room.p[0]);
+  c->qfloat_h = static_cast<uint8_t*>(room.p[1]);
+  c->qfloat_ws = static_cast<float*>(room.p[2]);
+  c->qfloat_dyt = static_cast<uint8_t*>(room.p[3]);
+  c->qfloat_xt = static_cast<uint8_t*>(room.p[4]);
+  c->qfloat_groups = room.groups;
+  c->qfloat_backward = room.backward;
   return STEM_OK;
 }
 
