@@ -430,7 +430,7 @@ PyObject* experts_combine_backward(PyObject*, PyObject* const* args, Py_ssize_t 
     const int64_t T = a.rows(-1, 1), k = a.columns(1), width = a.columns(0), rows = a.v[2] != Py_None ? a.rows(-1, 2) : a.v[3] != Py_None ? a.rows(-1, 3) : 0;
     auto dy = a.shaped(0, ACT, T, width); auto place = a.shaped<int32_t>(1, I32, T, k); auto dys = a.shaped(2, ACT, rows, width);
     auto ys = a.shaped(3, ACT, rows, width); auto w = a.shaped<float>(4, F32, T, k); auto dw = a.shaped<float>(5, F32, T, k); auto s = a.stream(6);
-    if (k > INT32_MAX) throw Unusual();
+    if (k > INT32_MAX || (dw && a.v[2] == Py_None && a.v[3] == Py_None)) throw Unusual();   // (rows that nobody has named)
     return [=] { return stem_experts_combine_backward(c, dy, ys, rows, width, place, w, T, (int)k, dys, dw, s); };
   });
 }

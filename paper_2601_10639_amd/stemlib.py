@@ -842,6 +842,8 @@ def stem_experts_combine_backward(ctx: StemCtx, dy, place, dys=None, ys=None, we
     st = (_bind or _load_bind()).experts_combine_backward(ctx, dy, place, dys, ys, weights, dweights, stream)
     if st is None:   # not the ordinary call
         dt, (T, k), width = ctx.torch_dtype, place.shape, dy.shape[1]
+        if dweights is not None and dys is None and ys is None and T > 0:   # (whose rows nobody has named)
+            raise StemError(STEM_ERR_INVALID_ARG, "stem_experts_combine_backward", "the weights' gradient needs ys")
         rows = next((t.shape[0] for t in (dys, ys) if t is not None), 0)
         st = lib().stem_experts_combine_backward(ctx.handle, _shaped(dy, dt, (T, width), "dy"), _shaped(ys, dt, (rows, width), "ys"), rows, width,
                                                  _shaped(place, torch.int32, (T, k), "place"), _shaped(weights, torch.float32, (T, k), "weights"), T, k,
