@@ -359,7 +359,8 @@ stem_status stem_qfloat_linear(stem_ctx* ctx, const void* x, int64_t T, int64_t 
 
 /* Its backward pass (without norm and residual, Q's own gradient taken as 1): dx [T,K] bf16 = Q(dy) Q(W_g), blocks of 128 along the row of dy; dW [groups,N,K]
  * fp32 = dy^T x over the group's rows, of the bf16 values as they are, in fp32 sums (a gradient that is added up over steps keeps what 8 bits would lose), overwritten, or
- * added to when accumulate != 0; a group without rows has a gradient of zero.  Either output may be NULL, x without dW and qt without dx; dx may lie over dy or x.  N, K up to max(d_model, d_ff).  T == 0: dW is
+ * added to when accumulate != 0; a group without rows has a gradient of zero.  Either output may be NULL, x without dW and qt without dx; dx may lie over dy or x.  N, K up to max(d_model, d_ff).  8-bit forms of dy
+ * (for dx, with the groups' padding) and of a W are below 2^31 bytes, and so are dy and x in bf16 (for dW, with the same padding).  T == 0: dW is
  * zero (or left as it is). */
 stem_status stem_qfloat_linear_backward(stem_ctx* ctx, const void* dy, const void* x, int64_t T, int64_t K, const void* qt, int64_t N, int groups,
                                         const int32_t* offsets, void* dx, float* dW, int accumulate, void* stream);

@@ -86,8 +86,10 @@ stem_status linear_backward(stem_ctx* c, const char* who, bool rounded, const vo
     return stem_fail(c, STEM_ERR_SHAPE, "%s: gradients of [%lld, %lld] x [%lld, %lld]^T; K and N are up to %lld here", who, (long long)T, (long long)K,
                      (long long)N, (long long)K, (long long)widest(c));
   const int64_t rows = stem_qfloat_rows(T, groups);
-  STEM_TRY(check_form(c, who, rows * 2, std::max(N, K)));   // (dy and x are transposed in bf16)
+  if (dx) STEM_TRY(check_form(c, who, rows, N));
   STEM_TRY(check_form(c, who, N, K));
+  if (dW && stem_qfloat_size(rows, std::max(N, K)) > MAX_FORM / 2)   // (its product addresses dy and x, or their transposes, with 32 bits)
+    return stem_fail(c, STEM_ERR_SHAPE, "%s: dy or x of %lld rows (padded) by %lld is 2^31 bytes or more in bf16", who, (long long)rows, (long long)std::max(N, K));
   const size_t xb = (size_t)T * K * 2, yb = (size_t)T * N * 2, wb = (size_t)groups * N * K * 4;
   hipStream_t s = static_cast<hipStream_t>(stream);
   if (T == 0) {
