@@ -2,14 +2,15 @@
 #pragma once
 #include "stem_internal.h"
 
-// (token, choice) pairs up to which a workgroup of the sort has 1024 of them, and 4096 beyond; and the most segments that sorts of up to this many have
+// (token, choice) pairs up to which a workgroup of the sort has 1024 of them, and 4096 beyond; and rows of counts that sorts of up to this many need: one for each
+// segment, and the totals
 #define EXPERTS_SMALL 65536
 inline int64_t stem_experts_segments(int64_t pairs) { return EXPERTS_SMALL / 1024 + pairs / 4096; }
 
 struct ExpertsSortArgs {
   const int32_t* experts;   // [pairs]
   int32_t pairs, n;
-  int32_t* counts;          // [segments][n]: of more than one segment
+  int32_t* counts;          // [segments + 1][n + 1]: of more than one segment
   int32_t *src, *place, *offsets;
   int32_t* flag;
 };

@@ -22,7 +22,10 @@ namespace {
 // place -1, and the rows behind the last expert's get src -1.
 // PLACE: the counts are taken again and the pairs placed; otherwise they are stored for the kernel that does.  Bound by latency: 128 pairs 3.7 us, 32768 pairs and 64
 // experts 5.0 and 6.3 in two launches.
-constexpr int TURNS = 4;
+// Up to SUMMED segments each placing workgroup adds up all segments' counts itself, which grows with their square; beyond, a kernel between the two leaves what is in front of
+// each segment, and the totals.  us, added up by each / by a kernel, pairs and experts: 2^17 and 64 13.8 / 16.4, 2^19 and 64 18.3 / 19.3, 2^19 and 512 29.8 / 24.5, 2^20 and 64
+// 29.7 / 24.1, 2^24 and 64 1470 / 187, 2^24 and 512 3730 / 250.
+constexpr int TURNS = 4, SUMMED = 128;
 
 __device__ __forceinline__ void in_order() {                // of LDS, within the wavefront
   __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
@@ -31,7 +34,7 @@ __device__ __forceinline__ void in_order() {                // of LDS, within th
 }
 
 template <int WAVES, bool PLACE>
-__global__ __launch_bounds__(WAVES * 64) void sort_kernel(ExpertsSortArgs p, int segments, int bits) {
+__global__ __launch_bounds__(WAVES * 64) void sort_kernel(ExpertsSortArgs p, int segments, int bits, bool summed) {
   extern __shared__ int32_t table[];                        // [WAVES][n + 1], then [n + 1] of first rows
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n = p.n, pitch = n + 1;
   int32_t* const mine = table + wave * pitch;
@@ -78,7 +81,13 @@ __global__ __launch_bounds__(WAVES * 64) void sort_kernel(ExpertsSortArgs p, int
   if (!PLACE) return;
   __syncthreads();
   // the rows in front of each expert's: in all segments, and of the expert itself in those before this one
-  if (segments > 1)
+  if (summed)
+    for (int e = threadIdx.x; e <= n; e += WAVES * 64) {
+      const int before = p.counts[(int64_t)blockIdx.x * pitch + e];
+      first[e] = p.counts[(int64_t)segments * pitch + e];
+      for (int w = 0; w < WAVES; ++w) table[w * pitch + e] += before;
+    }
+  else if (segments > 1)
     for (int e = threadIdx.x; e <= n; e += WAVES * 64) {
       int all = 0, before = 0;
       for (int s0 = 0; s0 < segments; s0 += 16) {              // 16 under way together
@@ -121,6 +130,41 @@ __global__ __launch_bounds__(WAVES * 64) void sort_kernel(ExpertsSortArgs p, int
     p.place[i] = e < n ? row : -1;
     p.src[row] = e < n ? i : -1;
   }
+}
+
+// Counts of the segments to what is in front of each, and the totals behind them.  A workgroup has 64 experts, a lane each, and its 16 wavefronts a strip of segments each, which they
+// read twice: what is in front of a strip is known once all are added up.
+__global__ __launch_bounds__(1024) void sum_kernel(ExpertsSortArgs p, int segments) {
+  constexpr int STRIPS = 16, TOGETHER = 16;
+  __shared__ int32_t sums[STRIPS][64];
+  const int lane = threadIdx.x & 63, strip = threadIdx.x >> 6, pitch = p.n + 1, e = blockIdx.x * 64 + lane;
+  const int per = (segments + STRIPS - 1) / STRIPS, lo = min(strip * per, segments), hi = min(lo + per, segments);
+  int32_t* const at = p.counts + min(e, p.n);
+  auto each = [&](auto f) __attribute__((always_inline)) {
+    for (int s0 = lo; s0 < hi; s0 += TOGETHER) {
+      int c[TOGETHER];
+#pragma unroll
+      for (int u = 0; u < TOGETHER; ++u) c[u] = at[(int64_t)min(s0 + u, hi - 1) * pitch];
+#pragma unroll
+      for (int u = 0; u < TOGETHER; ++u)
+        if (s0 + u < hi) f(s0 + u, c[u]);
+    }
+  };
+  int sum = 0;
+  each([&](int, int c) __attribute__((always_inline)) { sum += c; });
+  sums[strip][lane] = sum;
+  __syncthreads();
+  int before = 0, all = 0;
+  for (int s = 0; s < STRIPS; ++s) {
+    before += s < strip ? sums[s][lane] : 0;
+    all += sums[s][lane];
+  }
+  if (e > p.n) return;
+  each([&](int s, int c) __attribute__((always_inline)) {
+    at[(int64_t)s * pitch] = before;
+    before += c;
+  });
+  if (strip == 0) at[(int64_t)segments * pitch] = all;
 }
 
 // ---- rows ------------------------------------------------------------------------------------------------------------------
@@ -339,24 +383,34 @@ hipError_t by_type(const ExpertsRowsArgs& a, int64_t n, bool alone, F f) {
 }
 
 template <int WAVES>
-void launch_sort(const ExpertsSortArgs& a, hipStream_t s) {
-  constexpr int SEGMENT = WAVES * 64 * TURNS;
-  const int segments = a.pairs ? (a.pairs + SEGMENT - 1) / SEGMENT : 1;
+void launch_sort(const ExpertsSortArgs& a, const int32_t* route, hipStream_t s) {
+  const int segments = route[1];
+  const bool summed = route[2] == 3;
   int bits = 1;
   while (a.n >> bits) ++bits;
   const size_t lds = (size_t)(WAVES + 1) * (a.n + 1) * 4;
-  if (segments > 1) sort_kernel<WAVES, false><<<segments, WAVES * 64, lds, s>>>(a, segments, bits);
-  sort_kernel<WAVES, true><<<segments, WAVES * 64, lds, s>>>(a, segments, bits);
+  if (segments > 1) sort_kernel<WAVES, false><<<segments, WAVES * 64, lds, s>>>(a, segments, bits, false);
+  if (summed) sum_kernel<<<a.n / 64 + 1, 1024, 0, s>>>(a, segments);
+  sort_kernel<WAVES, true><<<segments, WAVES * 64, lds, s>>>(a, segments, bits, summed);
 }
 
 }  // namespace
 
+// {wavefronts of a workgroup, segments, launches}: one workgroup where it is enough, then segments whose counts are few to add and whose pairs are few to rank
+extern "C" void stem_route_experts_sort(int32_t pairs, int32_t* route) {
+  route[0] = pairs <= 256 ? 1 : pairs <= 1024 || (pairs > 4096 && pairs <= EXPERTS_SMALL) ? 4 : 16;
+  const int segment = route[0] * 64 * TURNS;
+  route[1] = pairs ? (pairs + segment - 1) / segment : 1;
+  route[2] = route[1] > SUMMED ? 3 : route[1] > 1 ? 2 : 1;
+}
+
 hipError_t stem_experts_sort_launch(stem_ctx* ctx, const ExpertsSortArgs& a, hipStream_t s) {
   ProfScope prof(ctx, K_EXPERTS_SORT, s);
-  // one workgroup where it is enough, then segments whose counts are few to add and whose pairs are few to rank
-  if (a.pairs <= 256) launch_sort<1>(a, s);
-  else if (a.pairs <= 1024 || (a.pairs > 4096 && a.pairs <= EXPERTS_SMALL)) launch_sort<4>(a, s);
-  else launch_sort<16>(a, s);
+  int32_t route[3];
+  stem_route_experts_sort(a.pairs, route);
+  if (route[0] == 1) launch_sort<1>(a, route, s);
+  else if (route[0] == 4) launch_sort<4>(a, route, s);
+  else launch_sort<16>(a, route, s);
   return hipGetLastError();
 }
 

@@ -304,6 +304,7 @@ void stem_route_quant(int M, int N, int K, int gate, int64_t ws_bytes, int32_t* 
 void stem_route_qfloat(int64_t T, int groups, int N, int K, int out, int64_t ws_bytes, int32_t* route);
 int stem_route_qfloat_few(int64_t T, int grouped, int N, int K);   // whether its weights go straight to registers instead
 void stem_route_qfloat_decode(int64_t T, int groups, int N, int K, int form, int32_t* route);   // and how; form: of rows that are in 8 bits already
+void stem_route_experts_sort(int32_t pairs, int32_t* route);   // a sort by expert: {wavefronts of a workgroup, segments, launches}
 // What stem_qfloat_reserve holds: forms of rows and of hidden values, room for K slices, two operands of a weight gradient (backward), for so many groups
 struct stem_qfloat_room { int groups, backward; void* p[5]; };
 int stem_qfloat_room_take(stem_qfloat_room* r, int64_t tokens, int64_t wide, int64_t F, int groups, int backward, int (*take)(void**, int64_t), void (*give)(void*));
