@@ -285,9 +285,11 @@ template <int NT, Source SRC, bool GATE>
 void by_channels(const QfloatDecodeArgs& a, const int32_t* route, hipStream_t s) {
   const int64_t n = a.groups.n < a.groups.T ? a.groups.n : a.groups.T, tiles = (a.groups.T + 16 * NT - 1) / (16 * NT) + (a.groups.offsets ? n - 1 : 0);
   const unsigned grid = (unsigned)(tiles * ((a.N + route[0] - 1) / route[0]));
-  if (route[0] == 8) by_depth<8, NT, SRC, GATE>(a, route[2], grid, s);
-  else if (route[0] == 16) by_depth<16, NT, SRC, GATE>(a, route[2], grid, s);
-  else by_depth<32, NT, SRC, GATE>(a, route[2], grid, s);
+  if constexpr (NT == 1) {
+    if (route[0] == 8) return by_depth<8, NT, SRC, GATE>(a, route[2], grid, s);
+    if (route[0] == 16) return by_depth<16, NT, SRC, GATE>(a, route[2], grid, s);
+  }
+  by_depth<32, NT, SRC, GATE>(a, route[2], grid, s);
 }
 
 }  // namespace
@@ -301,13 +303,13 @@ extern "C" int stem_route_qfloat_few(int64_t T, int grouped, int N, int K) {
 }
 
 // {channels and 16-row tiles of a workgroup, blocks of K that a wavefront has under way}.  About as many workgroups as compute units, if need be of 8 channels, half of whose
-// products count; of 32 rows where there are more workgroups than that helps (us, 16 / 32 rows: 64 of N 8192, K 2048 9.9 / 8.2, 256 of 1024 x 4096 9.5 / 8.6, 64 of
+// products count; of 32 rows, and then 32 channels, where there are more workgroups than that helps (us, 16 / 32 rows: 64 of N 8192, K 2048 9.9 / 8.2, 256 of 1024 x 4096 9.5 / 8.6, 64 of
 // 1024 x 4096 6.4 / 8.0).
 extern "C" void stem_route_qfloat_decode(int64_t T, int groups, int N, int K, int form, int32_t* route) {
   const int64_t n16 = (N + 15) / 16;
   route[1] = form && (T + 15) / 16 * n16 >= 1024 ? 2 : 1;
   const int64_t tiles = (T + 16 * route[1] - 1) / (16 * route[1]) + (groups < T ? groups : T) - 1, wgs = tiles * n16;
-  route[0] = wgs <= 128 ? 8 : wgs <= 256 ? 16 : 32;
+  route[0] = route[1] == 2 ? 32 : wgs <= 128 ? 8 : wgs <= 256 ? 16 : 32;   // (two tiles of rows: 512 workgroups of 16 channels at least)
   const int per = ((K + 127) / 128 + WAVES - 1) / WAVES;
   route[2] = per <= 1 ? 1 : per <= 2 ? 2 : per <= 4 ? 4 : 8;
 }
