@@ -586,7 +586,7 @@ struct Tiling {
 template <int MI, int NJ>
 __device__ __forceinline__ bool last_slice(const QfloatGemmArgs& p, f32x16_t (&acc)[MI][NJ], char* smem, int at, int stride, int slice, int tile, int lane) {
   constexpr int BYTES = MI * NJ * 4096, N = MI * NJ * 4;
-  const rsrc_t rw = resource(p.ws, (int64_t)p.ksplit * stride * BYTES);
+  const rsrc_t rw = resource(p.ws, p.ws_bytes);                // (of the room's size, not of what the slices would need: nothing leads behind it)
 #pragma unroll
   for (int k = 0; k < N; ++k) {
     const f32x16_t& a = acc[k / 4 / NJ][k / 4 % NJ];
