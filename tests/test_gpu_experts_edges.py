@@ -5,6 +5,7 @@ import torch
 
 from paper_2601_10639_amd import stemlib as L
 from tests.test_gpu_block_bind import count   # noqa: F401 (a fixture)
+from tests import test_gpu_experts as E
 from tests.test_gpu_experts import DEV, make_ctx
 
 pytestmark = pytest.mark.gpu
@@ -70,3 +71,13 @@ def test_graph_of_a_sort_of_many_pairs():
         graph.replay()
         torch.cuda.synchronize()
         assert all(torch.equal(p, q) for p, q in zip(a, b))
+
+
+# rows of more than one turn of a lane's pieces, with a last piece that lies over the one before it, and in place one element at a time
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("T,k,n,width", [(37, 2, 5, 2049), (30, 3, 4, 4099), (21, 2, 3, 8191), (19, 1, 3, 1025), (40, 4, 6, 2052), (3, 16, 9, 16387)])
+def test_rows_of_more_than_one_turn(T, k, n, width, dtype):
+    E.test_dispatch(T, k, n, width, dtype)
+    for weights in (True, False):
+        E.test_combine(T, k, n, width, weights, dtype)
+    E.test_combine_backward(T, k, n, width, dtype)
