@@ -204,7 +204,8 @@ __global__ __launch_bounds__(256) void rows_kernel(QfloatRowsArgs p) {
 // Lane t of the workgroup has rows 4 (t / 8) .. + 3 and columns 16 (t % 8) .. + 15: a row's magnitudes are eight neighbouring lanes'.  Four rows of a
 // column are a word (8 bits) or two (bf16) of the transpose, which goes through LDS to lie as that form does.  Columns' words are a pitch apart that keeps
 // 16-byte pieces whole, and some more every 16 columns, so that the lanes' stores fall into different banks.  Both transposes of a weight gradient, and the gradient's
-// form, of 16384 x (2001 + 2100): 60 us, 5 TB/s; weights of 8192 x 2048 to both forms 19 to 20.
+// form, of 16384 x (2001 + 2100): 60 us, 5 TB/s; of values rounded to 8 bits, 16384 x (1024 + 4096) 71 to 77 and 16384 x (2048 + 8192) 146 to 149, 5.3 TB/s both; weights of
+// 8192 x 2048 to both forms 14 to 15 one after another, 19 to 20 from memory.
 __device__ __forceinline__ void load_tile(const bf16_t* x, int cols, int rows, int quad, int col, QuantChunk (&raw)[4]) {
 #pragma unroll
   for (int r = 0; r < 4; ++r) {
